@@ -82,8 +82,8 @@ enum {
   STQ_E_ARG = -9,       /* an invalid scalar argument (step < 1, unknown dtype or flag, ...)  */
   STQ_E_STATE = -10,    /* call order: no statistics pending for stq_layer_stats              */
   STQ_E_TIMEOUT = -11,  /* a bounded wait inside a kernel ran out (stq_device_status)         */
-  STQ_E_TOO_LARGE = -12 /* the tensor exceeds the fixed capacity of an entry point that does  */
-                        /* not allocate (stq_grad_stats_static)                               */
+  STQ_E_TOO_LARGE = -12 /* the tensor exceeds a fixed capacity: of the entry point that does  */
+                        /* not allocate (stq_grad_stats_static), or of an 8-bit operator      */
 };
 
 enum { STQ_GRAD_F32 = 0, STQ_GRAD_BF16 = 1, STQ_GRAD_F16 = 2 };
@@ -261,6 +261,81 @@ uint64_t stq_launch_count(const stq_handle* h);
 /* Persistent grid the step kernel uses on this device (CTAs), and the device's SM count. */
 int stq_grid_size(const stq_handle* h);
 int stq_sm_count(const stq_handle* h);
+
+/* ---- 8-bit operators of a feed-forward block ---------------------------------------------------
+ * What a block's forward pass saves for its backward pass, held in 8 bits, and the products that read
+ * it: a root-mean-square norm and an activation that write 8-bit rows, the product of 8-bit rows with
+ * 8-bit weights, and all their gradients (straight through the rounding).  The same calls serve one
+ * token or a training batch.
+ *
+ * 8-bit rows: int8 codes q[rows][cols] with a row pitch of ldq bytes and one fp32 scale per row; the
+ * value is q * scale.  With amax = max |x| of the row: scale = amax / 127, q = rne(x * (127 / amax)).
+ * amax < 2^-100: scale 0 and codes 0.  A row that holds an infinity or a NaN: scale NaN and codes 0, so
+ * that everything computed from the row is NaN.  Code buffers are 16-byte aligned with a pitch that is a
+ * multiple of 16 (bytes beyond cols are neither read nor written); scale buffers are 4-byte aligned.
+ * Activation checkpoint: codes [rows][parts][ldck] and scales [rows][parts][ceil(cols/128)], one scale
+ * per 128 consecutive columns by the same rule; parts = 2 for the gated activation (gate, up), else 1.
+ *
+ * Matrices are row-major; ld* is the pitch in elements (>= the columns), pointers are aligned to their
+ * elements (16-byte alignment and pitches that are multiples of 8 run fastest).  dtype is STQ_GRAD_F32 or
+ * STQ_GRAD_BF16.  rows = 0 is allowed everywhere (a sum over no rows is written as zero).  Outputs must not
+ * overlap inputs (STQ_E_ALIAS).  Sums are held in fp32 (int32 in stq_q8_linear, exact) and are added in
+ * a fixed order: results are the same from run to run.
+ * Workspace: the backward calls and the products use a workspace of the handle, which grows on the first
+ * call that needs more (make that call before a stream capture); calls of one handle that overlap on
+ * the GPU would share it, so keep to one handle per stream. */
+
+/* kind of stq_q8_act: a = silu(z[:, :cols]) * z[:, cols:], or gelu(z), tanh form */
+enum { STQ_ACT_SILU_GATED = 1, STQ_ACT_GELU = 2 };
+/* columns that share a scale in an activation checkpoint */
+#define STQ_CKPT_BLOCK 128
+/* widest row of stq_q8_norm_backward, and longest sum of stq_q8_linear (127^2 * k fits 32 bits) */
+#define STQ_NORM_BWD_MAX_COLS 49152
+#define STQ_LINEAR_MAX_K 131072
+
+/* Plain rows to 8 bits (a weight [out][in] gets one scale per output channel). */
+int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t rows, uint32_t cols, int8_t* q,
+                uint64_t ldq, float* scale, void* stream);
+
+/* h = x + res (res and hsum NULL: h = x), rstd = 1 / sqrt(mean h^2 + eps) from the unrounded sum,
+ * y = h * rstd * weight as 8-bit rows.  Writes hsum (rounded to dtype), rstd[rows], codes, scales and, if
+ * `values` is not NULL, the bf16 values that the codes stand for.  weight: fp32[cols]. */
+int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uint64_t ldres, const float* weight,
+                float eps, int dtype, uint64_t rows, uint32_t cols, void* hsum, uint64_t ldh, float* rstd, int8_t* q,
+                uint64_t ldq, float* scale, void* values, uint64_t ldv, void* stream);
+
+/* With xh = hsum * rstd: dx = rstd * (weight dy - xh * mean(weight dy xh)) + dres, the gradient of x and
+ * of res alike; dweight[cols] = sum over rows of dy * xh, fp32.  dres (gradient that reaches hsum from
+ * elsewhere) may be NULL.  cols above STQ_NORM_BWD_MAX_COLS: STQ_E_TOO_LARGE. */
+int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const void* hsum, uint64_t ldh,
+                         const float* weight, const float* rstd, const void* dres, uint64_t lddres, int dtype,
+                         uint64_t rows, uint32_t cols, void* dx, uint64_t lddx, float* dweight, void* stream);
+
+/* a = act(z) as 8-bit rows [rows][cols]; z has cols columns, or 2 cols for STQ_ACT_SILU_GATED.  If ckq is not
+ * NULL, z is also written as an activation checkpoint; if `values` is not NULL, the bf16 values of the codes. */
+int stq_q8_act(stq_handle* h, const void* z, uint64_t ldz, int kind, int dtype, uint64_t rows, uint32_t cols, int8_t* q,
+               uint64_t ldq, float* scale, void* values, uint64_t ldv, int8_t* ckq, uint64_t ldck, float* ckscale,
+               void* stream);
+/* dz = act'(z) * da with z decoded from the checkpoint. */
+int stq_q8_act_backward(stq_handle* h, const void* da, uint64_t ldda, int kind, int dtype, uint64_t rows, uint32_t cols,
+                        const int8_t* ckq, uint64_t ldck, const float* ckscale, void* dz, uint64_t lddz, void* stream);
+
+/* out[t][n] = xscale[t] * wscale[n] * sum_k xq[t][k] * wq[n][k] + bias[n] (bias fp32 or NULL), the sum
+ * in exact 32-bit integers.  k above STQ_LINEAR_MAX_K: STQ_E_TOO_LARGE. */
+int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xscale, const int8_t* wq, uint64_t ldw,
+                  const float* wscale, const float* bias, uint64_t t, uint32_t n, uint32_t k, void* out, uint64_t ldo,
+                  int out_dtype, void* stream);
+/* dx[t][k] = sum_n dy[t][n] * wscale[n] * wq[n][k].  dy is bf16.  The 8-bit operand enters the matrix units as
+ * bf16(scale * code), relative error 2^-8 a term, for a bf16 result; as the sum of two bf16 numbers, 2^-17 a
+ * term, for an fp32 result. */
+int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t* wq, uint64_t ldw, const float* wscale,
+                     uint64_t t, uint32_t n, uint32_t k, void* dx, uint64_t lddx, int out_dtype, void* stream);
+/* dw[n][k] = sum_t dy[t][n] * xscale[t] * xq[t][k], in the same way. */
+int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t* xq, uint64_t ldx, const float* xscale,
+                     uint64_t t, uint32_t n, uint32_t k, void* dw, uint64_t lddw, int out_dtype, void* stream);
+/* db[n] = sum_t dy[t][n], fp32. */
+int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, uint64_t t, uint32_t n, float* db,
+                     void* stream);
 
 /* ---- transition decision (host only; Sec. 3.3-3.4, Algorithm 1 decision branch) -------------- */
 typedef struct stq_policy_cfg {

@@ -269,7 +269,7 @@ int stq_sm_count(const stq_handle* h);
  * token or a training batch.
  *
  * 8-bit rows: int8 codes q[rows][cols] with a row pitch of ldq bytes and one fp32 scale per row; the
- * value is q * scale.  With amax = max |x| of the row: scale = amax / 127, q = rne(x * (127 / amax)).
+ * value is q * scale.  With amax = max |x| of the row: scale = amax / 127, q = rne(x * (127 * fl(1/amax))).
  * amax < 2^-100: scale 0 and codes 0.  A row that holds an infinity or a NaN: scale NaN and codes 0, so
  * that everything computed from the row is NaN.  Code buffers are 16-byte aligned with a pitch that is a
  * multiple of 16 (bytes beyond cols are neither read nor written); scale buffers are 4-byte aligned.

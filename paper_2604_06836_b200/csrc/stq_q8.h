@@ -82,7 +82,8 @@ struct GemmArgs {
   uint64_t t;            // tokens
   uint32_t n, k;         // output and input channels
 };
-cudaError_t launch_q8_linear(const GemmArgs& a, cudaStream_t stream);
+// (err: the handle's flag, raised by a wait that ran out)
+cudaError_t launch_q8_linear(const GemmArgs& a, int sms, int* err, cudaStream_t stream);
 cudaError_t launch_q8_linear_dx(const GemmArgs& a, cudaStream_t stream);
 cudaError_t launch_q8_linear_dw(const GemmArgs& a, cudaStream_t stream);
 

@@ -249,7 +249,7 @@ int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xs
   a.out = out; a.ldo = ldo; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
   STQ_CUDA(h, cudaSetDevice(h->device));
-  STQ_CUDA(h, stq::launch_q8_linear(a, static_cast<cudaStream_t>(stream)));
+  STQ_CUDA(h, stq::launch_q8_linear(a, h->sm_count, h->d_err, static_cast<cudaStream_t>(stream)));
   h->launches++;
   return STQ_OK;
 }

@@ -47,16 +47,6 @@ __device__ __forceinline__ void tile_product(uint64_t m, uint32_t n, uint64_t de
 }
 
 template <class O>
-__global__ void __launch_bounds__(256) q8_linear_kernel(const GemmArgs a) {
-  tile_product<int>(
-      a.t, a.n, a.k, [&](uint64_t i, uint64_t c) { return (int)a.xq[i * a.ldx + c]; },
-      [&](uint64_t c, uint32_t j) { return (int)a.wq[j * a.ldw + c]; },
-      [&](uint64_t i, uint32_t j, int v) {
-        put<O>(a.out, i * a.ldo + j, (float)v * (a.xs[i] * a.ws[j]) + (a.bias ? a.bias[j] : 0.f));
-      });
-}
-
-template <class O>
 __global__ void __launch_bounds__(256) q8_linear_dx_kernel(const GemmArgs a) {
   const __nv_bfloat16* dy = static_cast<const __nv_bfloat16*>(a.dy);
   tile_product<float>(
@@ -77,14 +67,6 @@ __global__ void __launch_bounds__(256) q8_linear_dw_kernel(const GemmArgs a) {
 dim3 tiles(uint64_t m, uint32_t n) { return dim3((n + kT - 1) / kT, (unsigned)((m + kT - 1) / kT)); }
 
 }  // namespace
-
-cudaError_t launch_q8_linear(const GemmArgs& a, cudaStream_t stream) {
-  if (a.out_dtype == STQ_GRAD_F32)
-    q8_linear_kernel<float><<<tiles(a.t, a.n), 256, 0, stream>>>(a);
-  else
-    q8_linear_kernel<__nv_bfloat16><<<tiles(a.t, a.n), 256, 0, stream>>>(a);
-  return cudaGetLastError();
-}
 
 cudaError_t launch_q8_linear_dx(const GemmArgs& a, cudaStream_t stream) {
   if (a.out_dtype == STQ_GRAD_F32)

@@ -160,7 +160,8 @@ __device__ __forceinline__ void load_codes(const int8_t* row, uint32_t base, int
 // number and NaN above infinity, so one unsigned maximum also finds what must not be stored as a code.
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// How a row or block with largest magnitude `top` is coded: q = rne(x * inv) & mask, value q * scale.
+// How a row or block with largest magnitude `top` is coded: q = rne(x * inv) & mask, value q * scale.  (inv is
+// formed like that of the first moment's codes: 127 * fl(1/top).)
 struct Coding {
   float inv, scale;
   uint32_t mask;
@@ -169,7 +170,7 @@ __device__ __forceinline__ Coding coding_of(uint32_t top) {
   const float a = __uint_as_float(top);
   Coding c;
   c.mask = 0xffffffffu;
-  c.inv = 127.f / a;
+  c.inv = 127.f * (1.f / a);
   c.scale = a / 127.f;
   if (a < kTinyScale) { c.inv = 0.f; c.scale = 0.f; }
   // something in the row is not finite: no code can say so, the scale does

@@ -84,7 +84,9 @@ struct GemmArgs {
 };
 // (err: the handle's flag, raised by a wait that ran out)
 cudaError_t launch_q8_linear(const GemmArgs& a, int sms, int* err, cudaStream_t stream);
-cudaError_t launch_q8_linear_dx(const GemmArgs& a, cudaStream_t stream);
-cudaError_t launch_q8_linear_dw(const GemmArgs& a, cudaStream_t stream);
+// Bytes of workspace (aligned to 256) that a gradient needs; launches: how many kernels went out.
+size_t q8_grad_workspace(const GemmArgs& a, bool dw, int sms);
+cudaError_t launch_q8_linear_dx(const GemmArgs& a, void* ws, int sms, int* err, cudaStream_t stream, int* launches);
+cudaError_t launch_q8_linear_dw(const GemmArgs& a, void* ws, int sms, int* err, cudaStream_t stream, int* launches);
 
 }  // namespace stq

@@ -273,8 +273,11 @@ int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.out = dx; a.ldo = lddx; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
   STQ_CUDA(h, cudaSetDevice(h->device));
-  STQ_CUDA(h, stq::launch_q8_linear_dx(a, static_cast<cudaStream_t>(stream)));
-  h->launches++;
+  uint8_t* ws = nullptr;
+  int launches = 0;
+  if (const size_t need = stq::q8_grad_workspace(a, false, h->sm_count)) STQ_TRY(workspace(h, need, &ws));
+  STQ_CUDA(h, stq::launch_q8_linear_dx(a, ws, h->sm_count, h->d_err, static_cast<cudaStream_t>(stream), &launches));
+  h->launches += launches;
   return STQ_OK;
 }
 
@@ -298,8 +301,11 @@ int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.xq = xq; a.ldx = ldx; a.xs = xscale;
   a.out = dw; a.ldo = lddw; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
-  STQ_CUDA(h, stq::launch_q8_linear_dw(a, s));
-  h->launches++;
+  uint8_t* ws = nullptr;
+  int launches = 0;
+  if (const size_t need = stq::q8_grad_workspace(a, true, h->sm_count)) STQ_TRY(workspace(h, need, &ws));
+  STQ_CUDA(h, stq::launch_q8_linear_dw(a, ws, h->sm_count, h->d_err, s, &launches));
+  h->launches += launches;
   return STQ_OK;
 }
 

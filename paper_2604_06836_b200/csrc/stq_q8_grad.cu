@@ -1,0 +1,465 @@
+// Gradients of the 8-bit product on the tensor cores:
+//   dx[t][k] = sum_n dy[t][n] * ws[n] * wq[n][k]          (rows of the result: tokens, sum over output channels)
+//   dw[n][k] = sum_t dy[t][n] * xs[t] * xq[t][k]          (rows of the result: output channels, sum over tokens)
+// Both are D[m][j] = sum_c G(m, c) * s[c] * q[c][j] with the bf16 gradient G as it lies in memory (K-major for dx,
+// MN-major for dw) and an 8-bit operand q with j contiguous and a scale that varies along the sum.
+//
+// The matrix unit takes two bf16 operands, so the codes are turned into bf16(s * q) on the way: a code has 7 bits and
+// the scale 24, the product is rounded once, to 8 significant bits (relative error 2^-8 a term, random in sign).  That
+// is of the order of the rounding of a bf16 result; for an fp32 result (SPLIT) the remainder is kept as a second bf16
+// operand and multiplied too, 2^-17 a term.  Folding s into G would round as much and touch the larger operand.
+//
+// Per CTA: warp 0 copies tiles of G and q into a ring of stages, eight warps convert q, one warp issues the products,
+// four warps write results; accumulators are doubled in tensor memory as in the forward product.
+#include "../../include/stq.h"
+#include "stq_internal.h"
+#include "stq_q8.h"
+#include "stq_q8_mma.cuh"
+#include "stq_q8_tma.h"
+
+namespace stq {
+namespace {
+
+constexpr int kDepth = 64;             // length of the sum per stage
+constexpr int kStepK = 16;             // and per product instruction
+constexpr int kConvWarps = 8;
+constexpr int kThreadsG = 32 * (2 + 4 + kConvWarps);
+
+struct GradArgs {
+  const float* scale;                  // s[c]
+  void* out;                           // result, or the first of `splits` partial results of fp32
+  size_t ldo, split_stride;            // elements
+  uint64_t m;
+  uint32_t n, depth, ksteps;           // columns, length of the sum, its stages
+  uint32_t tiles_m, tiles_n, splits;
+  int align;
+  int* err;
+};
+
+template <int CG, int BN, bool SPLIT>
+struct GradShape {
+  static constexpr int kNB = BN / CG;                             // columns of the 8-bit operand in this CTA
+  static constexpr int kA = 128 * kDepth * 2, kQ = kDepth * kNB, kB = kDepth * kNB * 2;
+  static constexpr int kStage = kA + kQ + kB * (SPLIT ? 2 : 1);
+  static constexpr int kFit = (204 * 1024) / kStage;
+  static constexpr int kStages = kFit < 6 ? kFit : 6;
+  static constexpr int kCols = 2 * BN;
+  static constexpr int kSmem = kStages * kStage + 1024;
+};
+
+__device__ __forceinline__ uint64_t f2_pack(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t f2_bf16(uint64_t v) {
+  return bf16_pair(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+// Two codes (bytes `i`, `i + 1` of u, with 128 added) times the scale.  A byte placed under the exponent of 2^23 is the
+// number 2^23 + byte, so one exact subtraction gives the code.
+__device__ __forceinline__ uint64_t decode2(uint32_t u, int i, uint64_t scale2) {
+  const uint32_t lo = __byte_perm(u, 0x4b000000u, 0x7650 + i), hi = __byte_perm(u, 0x4b000000u, 0x7650 + i + 1);
+  constexpr uint32_t kMinus = 0xcb000080u;   // -(2^23 + 128)
+  return f2_mul(f2_add(f2_pack(lo, hi), f2_pack(kMinus, kMinus)), scale2);
+}
+
+template <int CG, int BN, bool SPLIT, bool DW, class O>
+__global__ void __launch_bounds__(kThreadsG, 1)
+q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_q, const GradArgs a) {
+  using S = GradShape<CG, BN, SPLIT>;
+  constexpr int kStages = S::kStages, kNB = S::kNB;
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[4 * kStages + 4];
+  __shared__ uint32_t tmem_slot;
+  __shared__ float stage[4][32 * 33];
+  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
+  // per stage: codes have landed (this CTA), gradient has landed (both CTAs, at the leader), codes are converted (both
+  // CTAs, at the leader), stage is free
+  const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * kStages, ready = full_g + 8 * kStages, empty = ready + 8 * kStages;
+  const uint32_t done = empty + 8 * kStages, freed = done + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  const bool leader = rank == 0;
+  const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG, tiles = a.tiles_m * a.tiles_n, work = tiles * a.splits;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      bar_init(full_q + 8 * i, 1);
+      bar_init(full_g + 8 * i, 1);
+      bar_init(ready + 8 * i, CG * kConvWarps);
+      bar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(done + 8 * i, 1);
+      bar_init(freed + 8 * i, 4 * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc<CG>(smem_addr(&tmem_slot), S::kCols);
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  mma_fence_after();
+  const uint32_t tmem = tmem_slot;
+
+  // work item -> tile and its share [k0, k1) of the stages of the sum
+  auto share = [&](uint32_t w, uint32_t& tile, uint32_t& k0, uint32_t& k1) {
+    const uint32_t sp = w / tiles;
+    tile = w - sp * tiles;
+    k0 = (uint32_t)((uint64_t)a.ksteps * sp / a.splits);
+    k1 = (uint32_t)((uint64_t)a.ksteps * (sp + 1) / a.splits);
+    return sp;
+  };
+
+  bool ok = true;
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t it = 0, tile, k0, k1;
+      const uint32_t full_g0 = CG == 2 ? peer_addr(full_g, 0) : full_g;
+      for (uint32_t w = unit; ok && w < work; w += units) {
+        share(w, tile, k0, k1);
+        const int row = (int)(tile % a.tiles_m) * 128 * CG + 128 * rank, col = (int)(tile / a.tiles_m) * BN + kNB * rank;
+        for (uint32_t k = k0; k < k1; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          if (!(ok = bar_wait(empty + 8 * s, ph ^ 1))) break;
+          const uint32_t at = ring + s * S::kStage, c = k * kDepth;
+          if (leader) bar_expect(full_g + 8 * s, CG * S::kA);
+          bar_expect(full_q + 8 * s, S::kQ);
+          tensor_load<1>(at + S::kA, &map_q, col, (int)c, full_q + 8 * s);
+          if constexpr (DW) {
+            tensor_load<CG>(at, &map_g, row, (int)c, full_g0 + 8 * s);
+            tensor_load<CG>(at + S::kA / 2, &map_g, row + 64, (int)c, full_g0 + 8 * s);
+          } else {
+            tensor_load<CG>(at, &map_g, (int)c, row, full_g0 + 8 * s);
+          }
+        }
+      }
+      if (!ok)      // leave no copy in flight
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
+          bar_wait(full_q + 8 * (i % kStages), (i / kStages) & 1);
+          if (leader) bar_wait(full_g + 8 * (i % kStages), (i / kStages) & 1);
+        }
+    }
+  } else if (warp == 1) {
+    if (leader && elect_one()) {
+      constexpr uint32_t id = idesc(kIdescBf16, 128 * CG, BN, DW, true);
+      uint32_t it = 0, n = 0, tile, k0, k1;
+      for (uint32_t w = unit; ok && w < work; w += units, ++n) {
+        share(w, tile, k0, k1);
+        const uint32_t acc = n & 1;
+        if (!(ok = bar_wait(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+        mma_fence_after();
+        for (uint32_t k = k0; k < k1; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          if (!(ok = bar_wait(full_g + 8 * s, ph) && bar_wait(ready + 8 * s, ph))) break;
+          mma_fence_after();
+          const uint32_t at = ring + s * S::kStage;
+          const uint64_t da = DW ? operand_desc(at, S::kA / 2, 1024) : operand_desc(at, 16, 1024);
+          const uint64_t db = operand_desc(at + S::kA + S::kQ, kDepth * 128, 1024);
+          constexpr uint32_t kStepA = DW ? (kStepK * 128) >> 4 : (kStepK * 2) >> 4, kStepB = (kStepK * 128) >> 4;
+#pragma unroll
+          for (int j = 0; j < kDepth / kStepK; ++j) {
+            mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + j * kStepB, id, (k - k0 | j) != 0);
+            if constexpr (SPLIT) mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + (S::kB >> 4) + j * kStepB, id, true);
+          }
+          mma_commit<CG>(empty + 8 * s);
+        }
+        if (ok) mma_commit<CG>(done + 8 * acc);
+      }
+    }
+  } else if (warp < 2 + kConvWarps) {
+    // A row of the stage has kNB codes: kNB / 16 lanes take 16 bytes each.
+    constexpr int kLanes = kNB / 16, kRowsAtOnce = kConvWarps * 32 / kLanes, kPasses = kDepth / kRowsAtOnce;
+    const int thread = threadIdx.x - 64, sub = thread % kLanes, row0 = thread / kLanes;
+    const uint32_t ready0 = CG == 2 ? peer_addr(ready, 0) : ready;
+    uint32_t it = 0, tile, k0, k1;
+    for (uint32_t w = unit; ok && w < work; w += units) {
+      share(w, tile, k0, k1);
+      float sc[kPasses];
+      auto scales = [&](uint32_t k) {
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          const uint32_t c = k * kDepth + p * kRowsAtOnce + row0;
+          sc[p] = c < a.depth ? __ldg(a.scale + c) : 0.f;
+        }
+      };
+      scales(k0);
+      for (uint32_t k = k0; k < k1; ++k, ++it) {
+        const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+        if (!(ok = bar_wait(full_q + 8 * s, ph))) break;
+        const uint32_t from = ring + s * S::kStage + S::kA, to = from + S::kQ;
+        uint32_t q[kPasses][4];
+        float now[kPasses];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          now[p] = sc[p];
+          asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(q[p][0]), "=r"(q[p][1]), "=r"(q[p][2]), "=r"(q[p][3])
+                       : "r"(from + (p * kRowsAtOnce + row0) * kNB + sub * 16));
+        }
+        if (k + 1 < k1) scales(k + 1);         // (the next stage's, so that their latency is hidden)
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) {
+          const uint32_t row = p * kRowsAtOnce + row0;
+          const uint32_t sb = __float_as_uint(now[p]);
+          const uint64_t s2 = f2_pack(sb, sb);
+          uint32_t v[8], lo[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint64_t x = decode2(q[p][i >> 1] ^ 0x80808080u, (i & 1) * 2, s2);
+            v[i] = f2_bf16(x);
+            if constexpr (SPLIT) {
+              const uint64_t neg = f2_pack((v[i] << 16) ^ 0x80000000u, (v[i] & 0xffff0000u) ^ 0x80000000u);
+              lo[i] = f2_bf16(f2_add(x, neg));
+            }
+          }
+          // 16 columns = two 16-byte pieces of the row's 128 bytes in its atom of 64 columns; the lanes of the second
+          // atom write theirs in the other order, so that eight lanes reach eight different pieces
+          const uint32_t atom = sub / 4, piece = (sub % 4) * 2, x7 = row & 7, odd = atom & 1;
+          const uint32_t base = to + atom * (kDepth * 128) + row * 128;
+#pragma unroll
+          for (int o = 0; o < (SPLIT ? 2 : 1); ++o) {
+            const uint32_t* u = o ? lo : v;
+            const uint32_t b = base + o * S::kB;
+            const uint32_t p0 = b + (((piece + odd) ^ x7) << 4), p1 = b + (((piece + 1 - odd) ^ x7) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p0), "r"(odd ? u[4] : u[0]), "r"(odd ? u[5] : u[1]),
+                         "r"(odd ? u[6] : u[2]), "r"(odd ? u[7] : u[3])
+                         : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p1), "r"(odd ? u[0] : u[4]), "r"(odd ? u[1] : u[5]),
+                         "r"(odd ? u[2] : u[6]), "r"(odd ? u[3] : u[7])
+                         : "memory");
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the products read shared memory by another path
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(ready0 + 8 * s);
+      }
+    }
+  } else {
+    const int quad = warp & 3;
+    const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
+    uint32_t n = 0, tile, k0, k1;
+    for (uint32_t w = unit; ok && w < work; w += units, ++n) {
+      const uint32_t sp = share(w, tile, k0, k1), acc = n & 1;
+      const uint64_t row = (uint64_t)(tile % a.tiles_m) * 128 * CG + 128 * rank + quad * 32;
+      const uint32_t col = tile / a.tiles_m * BN;
+      ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
+      if (!(ok = all_of_128(ok))) break;       // (the four warps leave together)
+      mma_fence_after();
+      const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN;
+      O* out = static_cast<O*>(a.out) + sp * a.split_stride + row * a.ldo + col;
+      const int rows = row >= a.m ? 0 : (int)min((uint64_t)32, a.m - row);
+#pragma unroll 2
+      for (int c = 0; c < BN; c += 32) {
+        if (col + c >= a.n) break;
+        uint32_t r[32];
+        tmem_load(from + c, r);
+        tmem_load_wait();
+        float v[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+        store_block<O, 32>(out + c, a.ldo, v, rows, (int)min(32u, a.n - col - c), a.align, lane, stage[quad]);
+      }
+      mma_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive_cluster(freed0 + 8 * acc);
+    }
+  }
+  if (!ok) *a.err = 1;
+  __syncwarp();
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  if (warp == 1) {
+    mma_fence_after();
+    tmem_free<CG>(tmem, S::kCols);
+  }
+}
+
+// out[r][c] = sum over splits of part[s][r][c] (rows of `ldp` floats, a multiple of 8), in order
+template <class O>
+__global__ void __launch_bounds__(256) q8_join_kernel(const float* part, size_t split_stride, uint32_t splits, size_t ldp,
+                                                      uint64_t rows, uint32_t cols, O* out, size_t ldo, int align) {
+  const uint32_t per_row = (uint32_t)(ldp / 4);
+  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= rows * per_row) return;
+  const uint64_t r = id / per_row;
+  const uint32_t c = (uint32_t)(id - r * per_row) * 4;
+  const float* p = part + r * ldp + c;
+  float4 s = *reinterpret_cast<const float4*>(p);
+  for (uint32_t i = 1; i < splits; ++i) {
+    const float4 v = *reinterpret_cast<const float4*>(p + i * split_stride);
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  O* o = out + r * ldo + c;
+  if (align >= 16 && c + 4 <= cols) {
+    if constexpr (sizeof(O) == 4)
+      *reinterpret_cast<float4*>(o) = s;
+    else
+      *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(s.x, s.y), bf16_pair(s.z, s.w));
+  } else {
+    const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i < cols) o[i] = static_cast<O>(v[i]);
+  }
+}
+
+// A gradient whose rows are not aligned to 16 bytes, copied to rows that are (the columns that pad a row are zero).
+__global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, size_t ldi, uint64_t rows, uint32_t cols,
+                                                       __nv_bfloat16* out, size_t ldo) {
+  const uint32_t per_row = (uint32_t)(ldo / 8);
+  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= rows * per_row) return;
+  const uint64_t r = id / per_row;
+  const uint32_t c = (uint32_t)(id - r * per_row) * 8;
+  const uint16_t* p = reinterpret_cast<const uint16_t*>(in) + r * ldi + c;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = c + 2 * i < cols ? p[2 * i] : 0u, hi = c + 2 * i + 1 < cols ? p[2 * i + 1] : 0u;
+    w[i] = lo | hi << 16;
+  }
+  *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+struct Plan {
+  int shape;                 // 0: pair of CTAs, 256 columns; 1: one CTA, 128 columns; 2: one CTA, 64 columns
+  uint32_t splits;
+};
+constexpr int kShapes[3][2] = {{2, 256}, {1, 128}, {1, 64}};
+
+// Time of a plan in clock cycles.  A stage takes 8192 multiply-adds a cycle and SM (twice as many of them for a split
+// operand) or, where that is longer, the copies and the conversion; a tile costs a fixed beginning and end; partial
+// results cost their way through memory and one more launch.
+Plan plan_of(uint64_t m, uint32_t n, uint32_t ksteps, bool split_operand, size_t out_elem, int sms) {
+  Plan best = {0, 1};
+  double least = 1e300;
+  for (int i = 0; i < 3; ++i) {
+    const int cg = kShapes[i][0], bn = kShapes[i][1];
+    const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg;
+    const double product = (cg == 2 ? 512.0 : 4.0 * bn) * (split_operand ? 2 : 1), other = cg == 2 ? 620.0 : 300.0 + 2.5 * bn;
+    const double stage = product > other ? product : other;
+    for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
+      if (sp > 1 && (double)m * n * sp * 4 > 256e6) break;      // (a quarter of a gigabyte of workspace at most)
+      const double rounds = (double)((tiles * sp + units - 1) / units);
+      double c = rounds * ((ksteps + sp - 1) / sp * stage + 2500.0);
+      if (sp > 1) c += (double)m * n * (4.0 * sp * 2 + out_elem) / 3000.0 + 4000.0;
+      if (c < least) { least = c; best = {i, sp}; }
+    }
+  }
+  return best;
+}
+
+struct Work {
+  Plan plan;
+  bool pitch;                // dy has to be copied
+  size_t lddy, part_bytes, pitch_bytes, ldp;
+};
+Work work_of(const GemmArgs& g, bool dw, int sms) {
+  Work w;
+  const uint64_t m = dw ? g.n : g.t, depth = dw ? g.t : g.n;
+  const size_t e = g.out_dtype == STQ_GRAD_F32 ? 4 : 2;
+  w.plan = plan_of(m, g.k, (uint32_t)((depth + kDepth - 1) / kDepth), e == 4, e, sms);
+  w.pitch = ((g.lddy & 7) != 0 && g.t > 1) || (reinterpret_cast<uintptr_t>(g.dy) & 15) != 0;
+  w.lddy = w.pitch || g.t == 1 ? ((size_t)g.n + 7) / 8 * 8 : g.lddy;
+  w.pitch_bytes = w.pitch ? (g.t * w.lddy * 2 + 255) / 256 * 256 : 0;
+  w.ldp = ((size_t)g.k + 7) / 8 * 8;
+  w.part_bytes = w.plan.splits > 1 ? w.plan.splits * m * w.ldp * 4 : 0;
+  return w;
+}
+
+template <int CG, int BN, bool SPLIT, bool DW, class O>
+cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t stream) {
+  using S = GradShape<CG, BN, SPLIT>;
+  GradArgs a;
+  const int8_t* q = DW ? g.xq : g.wq;
+  const size_t ldq = DW ? g.ldx : g.ldw;
+  a.scale = DW ? g.xs : g.ws;
+  a.m = DW ? g.n : g.t;
+  a.depth = (uint32_t)(DW ? g.t : g.n);
+  a.n = g.k;
+  a.ksteps = (a.depth + kDepth - 1) / kDepth;
+  a.out = out;
+  a.ldo = ldo;
+  a.split_stride = a.m * ldo;
+  a.splits = w.plan.splits;
+  a.tiles_m = (uint32_t)((a.m + 128 * CG - 1) / (128 * CG));
+  a.tiles_n = (a.n + BN - 1) / BN;
+  a.align = row_alignment(out, ldo * sizeof(O));
+  a.err = err;
+  CUtensorMap mg, mq;
+  cudaError_t e = make_tensor_map(&mg, dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
+  if (e == cudaSuccess) e = make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false);
+  auto* kernel = q8_grad_kernel<CG, BN, SPLIT, DW, O>;
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return e;
+  const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
+  return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, kThreadsG, S::kSmem, CG, stream, mg, mq, a);
+}
+
+template <bool SPLIT, bool DW, class O>
+cudaError_t by_shape(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t s) {
+  if (w.plan.shape == 0) return launch<2, 256, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  if (w.plan.shape == 1) return launch<1, 128, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  return launch<1, 64, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
+}
+
+template <bool DW>
+cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t stream, int* launches) {
+  const Work w = work_of(g, DW, sms);
+  const uint64_t m = DW ? g.n : g.t;
+  const bool f32 = g.out_dtype == STQ_GRAD_F32, split = w.plan.splits > 1;
+  const void* dy = g.dy;
+  *launches = 1;
+  if (w.pitch) {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(ws);
+    const uint64_t items = g.t * (w.lddy / 8);
+    q8_pitch_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(g.dy), g.lddy, g.t, g.n, to, w.lddy);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    dy = to;
+    ++*launches;
+  }
+  float* part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.pitch_bytes);
+  void* out = split ? part : g.out;
+  const size_t ldo = split ? w.ldp : g.ldo;
+  // (an fp32 result takes the split operand; partial results of a bf16 one are fp32 sums of the single operand)
+  cudaError_t e = f32 ? by_shape<true, DW, float>(g, w, dy, out, ldo, err, sms, stream)
+                  : split ? by_shape<false, DW, float>(g, w, dy, out, ldo, err, sms, stream)
+                          : by_shape<false, DW, __nv_bfloat16>(g, w, dy, out, ldo, err, sms, stream);
+  if (e != cudaSuccess || !split) return e;
+  const uint64_t items = m * (w.ldp / 4);
+  const unsigned grid = (unsigned)((items + 255) / 256);
+  if (f32)
+    q8_join_kernel<float><<<grid, 256, 0, stream>>>(part, m * w.ldp, w.plan.splits, w.ldp, m, g.k, static_cast<float*>(g.out), g.ldo,
+                                                    row_alignment(g.out, g.ldo * 4));
+  else
+    q8_join_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(part, m * w.ldp, w.plan.splits, w.ldp, m, g.k,
+                                                            static_cast<__nv_bfloat16*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 2));
+  ++*launches;
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t q8_grad_workspace(const GemmArgs& g, bool dw, int sms) {
+  const Work w = work_of(g, dw, sms);
+  return w.pitch_bytes + w.part_bytes;
+}
+cudaError_t launch_q8_linear_dx(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t stream, int* launches) {
+  return grad<false>(g, ws, sms, err, stream, launches);
+}
+cudaError_t launch_q8_linear_dw(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t stream, int* launches) {
+  return grad<true>(g, ws, sms, err, stream, launches);
+}
+
+}  // namespace stq

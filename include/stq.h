@@ -326,8 +326,8 @@ int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xs
                   const float* wscale, const float* bias, uint64_t t, uint32_t n, uint32_t k, void* out, uint64_t ldo,
                   int out_dtype, void* stream);
 /* dx[t][k] = sum_n dy[t][n] * wscale[n] * wq[n][k].  dy is bf16.  The 8-bit operand enters the matrix units as
- * bf16(scale * code), relative error 2^-8 a term, for a bf16 result; as the sum of two bf16 numbers, 2^-17 a
- * term, for an fp32 result. */
+ * bf16(scale * code), relative error 2^-8 a term, for a bf16 result; for an fp32 result as three bf16 numbers
+ * whose sum is fl32(scale * code). */
 int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t* wq, uint64_t ldw, const float* wscale,
                      uint64_t t, uint32_t n, uint32_t k, void* dx, uint64_t lddx, int out_dtype, void* stream);
 /* dw[n][k] = sum_t dy[t][n] * xscale[t] * xq[t][k], in the same way. */

@@ -4,13 +4,15 @@
 // Both are D[m][j] = sum_c G(m, c) * s[c] * q[c][j] with the bf16 gradient G as it lies in memory (K-major for dx,
 // MN-major for dw) and an 8-bit operand q with j contiguous and a scale that varies along the sum.
 //
-// The matrix unit takes two bf16 operands, so the codes are turned into bf16(s * q) on the way: a code has 7 bits and
-// the scale 24, the product is rounded once, to 8 significant bits (relative error 2^-8 a term, random in sign).  That
-// is of the order of the rounding of a bf16 result; for an fp32 result (SPLIT) the remainder is kept as a second bf16
-// operand and multiplied too, 2^-17 a term.  Folding s into G would round as much and touch the larger operand.
+// The matrix unit takes two bf16 operands, so the codes are turned into bf16 on the way.  For a bf16 result the operand
+// is bf16(s * q), one rounding to 8 significant bits (relative error 2^-8 a term, random in sign), which is of the order
+// of the rounding of the result itself.  For an fp32 result (PARTS = 3) the fp32 product s * q is cut into three bf16
+// numbers whose sum is exactly that product, and three products are added up: the error is that of fp32 arithmetic.
+// Folding s into G instead would round as much and touch the larger operand.
 //
-// Per CTA: warp 0 copies tiles of G and q into a ring of stages, eight warps convert q, one warp issues the products,
-// four warps write results; accumulators are doubled in tensor memory as in the forward product.
+// Per CTA: warp 0 copies tiles of G and q into a ring of stages, two groups of four warps convert q in alternate stages,
+// one warp issues the products, four warps write results; accumulators are doubled in tensor memory as in the forward
+// product.
 #include "../../include/stq.h"
 #include "stq_internal.h"
 #include "stq_q8.h"
@@ -22,8 +24,8 @@ namespace {
 
 constexpr int kDepth = 64;             // length of the sum per stage
 constexpr int kStepK = 16;             // and per product instruction
-constexpr int kConvWarps = 8;
-constexpr int kThreadsG = 32 * (2 + 4 + kConvWarps);
+constexpr int kGroups = 2, kGroupWarps = 4;        // conversion: groups of warps, a stage to a group
+constexpr int kThreadsG = 32 * (2 + 4 + kGroups * kGroupWarps);
 
 struct GradArgs {
   const float* scale;                  // s[c]
@@ -36,44 +38,75 @@ struct GradArgs {
   int* err;
 };
 
-template <int CG, int BN, bool SPLIT>
+template <int CG, int BN, int PARTS>
 struct GradShape {
   static constexpr int kNB = BN / CG;                             // columns of the 8-bit operand in this CTA
   static constexpr int kA = 128 * kDepth * 2, kQ = kDepth * kNB, kB = kDepth * kNB * 2;
-  static constexpr int kStage = kA + kQ + kB * (SPLIT ? 2 : 1);
+  static constexpr int kStage = kA + kQ + kB * PARTS;
   static constexpr int kFit = (204 * 1024) / kStage;
   static constexpr int kStages = kFit < 6 ? kFit : 6;
   static constexpr int kCols = 2 * BN;
   static constexpr int kSmem = kStages * kStage + 1024;
 };
 
-__device__ __forceinline__ uint64_t f2_pack(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
-__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+__device__ __forceinline__ uint32_t bf2_add(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t f2_bf16(uint64_t v) {
-  return bf16_pair(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+__device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
 }
 
-// Two codes (bytes `i`, `i + 1` of u, with 128 added) times the scale.  A byte placed under the exponent of 2^23 is the
-// number 2^23 + byte, so one exact subtraction gives the code.
-__device__ __forceinline__ uint64_t decode2(uint32_t u, int i, uint64_t scale2) {
-  const uint32_t lo = __byte_perm(u, 0x4b000000u, 0x7650 + i), hi = __byte_perm(u, 0x4b000000u, 0x7650 + i + 1);
-  constexpr uint32_t kMinus = 0xcb000080u;   // -(2^23 + 128)
-  return f2_mul(f2_add(f2_pack(lo, hi), f2_pack(kMinus, kMinus)), scale2);
+// A row's scale for two columns at a time: s = hi + lo up to 2^-17.
+struct Scale2 {
+  float s;
+  uint32_t hi, lo;
+};
+__device__ __forceinline__ Scale2 scale2_of(float s) {
+  Scale2 r;
+  r.s = s;
+  const __nv_bfloat16 h = __float2bfloat16_rn(s), l = __float2bfloat16_rn(s - __bfloat162float(h));
+  r.hi = (uint32_t)__bfloat16_as_ushort(h) * 0x10001u;
+  r.lo = (uint32_t)__bfloat16_as_ushort(l) * 0x10001u;
+  return r;
 }
 
-template <int CG, int BN, bool SPLIT, bool DW, class O>
+// Codes i, i + 1 (i = 0 or 2) of four codes as a pair of bf16(s * q), without a conversion instruction (those run at
+// an eighth of the rate of the arithmetic here).  The 7 low bits of a code under the exponent of 128 are the number
+// 128 + bits, its sign bit under that of -128 is -128 or -256; their sum is the code, exactly.
+__device__ __forceinline__ uint32_t decode_pair(uint32_t w, int i, const Scale2& s) {
+  const uint32_t t = __byte_perm(w, 0u, i == 0 ? 0x4140 : 0x4342);
+  const uint32_t q = bf2_add((t & 0x007f007fu) | 0x43004300u, (t & 0x00800080u) | 0xc300c300u);
+  return bf2_fma(q, s.hi, bf2_mul(q, s.lo));
+}
+
+// The same as three pairs whose sum is fl32(s * q): 8 bits of the product to each, cut off, the rest exact.
+__device__ __forceinline__ void decode_pair3(uint32_t w, int i, const Scale2& s, uint32_t (&out)[3]) {
+  float v[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)      // a byte under the exponent of 2^23 is 2^23 + byte
+    v[j] = (__uint_as_float(__byte_perm(w ^ 0x80808080u, 0x4b000000u, 0x7650 + i + j)) - 8388736.f) * s.s;
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+    const uint32_t lo = __float_as_uint(v[0]), hi = __float_as_uint(v[1]);
+    out[p] = __byte_perm(lo, hi, 0x7632);
+    v[0] -= __uint_as_float(lo & 0xffff0000u);
+    v[1] -= __uint_as_float(hi & 0xffff0000u);
+  }
+}
+
+template <int CG, int BN, int PARTS, bool DW, class O>
 __global__ void __launch_bounds__(kThreadsG, 1)
 q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_q, const GradArgs a) {
-  using S = GradShape<CG, BN, SPLIT>;
+  using S = GradShape<CG, BN, PARTS>;
   constexpr int kStages = S::kStages, kNB = S::kNB;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[4 * kStages + 4];
@@ -93,7 +126,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
     for (int i = 0; i < kStages; ++i) {
       bar_init(full_q + 8 * i, 1);
       bar_init(full_g + 8 * i, 1);
-      bar_init(ready + 8 * i, CG * kConvWarps);
+      bar_init(ready + 8 * i, CG * kGroupWarps);
       bar_init(empty + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -166,20 +199,25 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           constexpr uint32_t kStepA = DW ? (kStepK * 128) >> 4 : (kStepK * 2) >> 4, kStepB = (kStepK * 128) >> 4;
 #pragma unroll
           for (int j = 0; j < kDepth / kStepK; ++j) {
-            mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + j * kStepB, id, (k - k0 | j) != 0);
-            if constexpr (SPLIT) mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + (S::kB >> 4) + j * kStepB, id, true);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
+              mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + p * (S::kB >> 4) + j * kStepB, id, (k - k0 | j | p) != 0);
           }
           mma_commit<CG>(empty + 8 * s);
         }
         if (ok) mma_commit<CG>(done + 8 * acc);
       }
     }
-  } else if (warp < 2 + kConvWarps) {
+  } else if (warp < 2 + kGroups * kGroupWarps) {
     // A row of the stage has kNB codes: kNB / 16 lanes take 16 bytes each.
-    constexpr int kLanes = kNB / 16, kRowsAtOnce = kConvWarps * 32 / kLanes, kPasses = kDepth / kRowsAtOnce;
-    const int thread = threadIdx.x - 64, sub = thread % kLanes, row0 = thread / kLanes;
+    constexpr int kLanes = kNB / 16, kRowsAtOnce = kGroupWarps * 32 / kLanes, kPasses = kDepth / kRowsAtOnce;
+    const int group = (warp - 2) / kGroupWarps, thread = (threadIdx.x - 64) % (kGroupWarps * 32);
+    const uint32_t sub = thread % kLanes, row0 = thread / kLanes;
+    // 16 columns are two 16-byte pieces of the row's 128 bytes in its atom of 64 columns; the lanes of the second atom
+    // write theirs in the other order, so that eight lanes reach eight different pieces
+    const uint32_t atom = sub / 4, piece = (sub % 4) * 2, odd = atom & 1;
     const uint32_t ready0 = CG == 2 ? peer_addr(ready, 0) : ready;
-    uint32_t it = 0, tile, k0, k1;
+    uint32_t it = 0, tile, k0, k1;             // it: stages before this work item
     for (uint32_t w = unit; ok && w < work; w += units) {
       share(w, tile, k0, k1);
       float sc[kPasses];
@@ -187,53 +225,50 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
           const uint32_t c = k * kDepth + p * kRowsAtOnce + row0;
-          sc[p] = c < a.depth ? __ldg(a.scale + c) : 0.f;
+          sc[p] = k < k1 && c < a.depth ? __ldg(a.scale + c) : 0.f;
         }
       };
-      scales(k0);
-      for (uint32_t k = k0; k < k1; ++k, ++it) {
-        const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+      const uint32_t mine = (group + it) % kGroups;      // (kGroups = 2: the first stage of this item that is the group's)
+      scales(k0 + mine);
+      for (uint32_t k = k0 + mine; k < k1; k += kGroups) {
+        const uint32_t i = it + k - k0, s = i % kStages, ph = (i / kStages) & 1;
+        Scale2 now[kPasses];
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) now[p] = scale2_of(sc[p]);
+        scales(k + kGroups);                   // (for the group's next stage, so that their latency is hidden)
         if (!(ok = bar_wait(full_q + 8 * s, ph))) break;
         const uint32_t from = ring + s * S::kStage + S::kA, to = from + S::kQ;
         uint32_t q[kPasses][4];
-        float now[kPasses];
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          now[p] = sc[p];
+        for (int p = 0; p < kPasses; ++p)
           asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];"
                        : "=r"(q[p][0]), "=r"(q[p][1]), "=r"(q[p][2]), "=r"(q[p][3])
                        : "r"(from + (p * kRowsAtOnce + row0) * kNB + sub * 16));
-        }
-        if (k + 1 < k1) scales(k + 1);         // (the next stage's, so that their latency is hidden)
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
-          const uint32_t row = p * kRowsAtOnce + row0;
-          const uint32_t sb = __float_as_uint(now[p]);
-          const uint64_t s2 = f2_pack(sb, sb);
-          uint32_t v[8], lo[8];
+          const uint32_t row = p * kRowsAtOnce + row0, base = to + atom * (kDepth * 128) + row * 128;
+          uint32_t v[PARTS][8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint64_t x = decode2(q[p][i >> 1] ^ 0x80808080u, (i & 1) * 2, s2);
-            v[i] = f2_bf16(x);
-            if constexpr (SPLIT) {
-              const uint64_t neg = f2_pack((v[i] << 16) ^ 0x80000000u, (v[i] & 0xffff0000u) ^ 0x80000000u);
-              lo[i] = f2_bf16(f2_add(x, neg));
+          for (int j = 0; j < 8; ++j) {
+            // the order of the two halves follows that of the writes
+            const uint32_t word = odd ? q[p][(j >> 1) ^ 2] : q[p][j >> 1];
+            if constexpr (PARTS == 1) {
+              v[0][j] = decode_pair(word, (j & 1) * 2, now[p]);
+            } else {
+              uint32_t o[3];
+              decode_pair3(word, (j & 1) * 2, now[p], o);
+#pragma unroll
+              for (int x = 0; x < PARTS; ++x) v[x][j] = o[x];
             }
           }
-          // 16 columns = two 16-byte pieces of the row's 128 bytes in its atom of 64 columns; the lanes of the second
-          // atom write theirs in the other order, so that eight lanes reach eight different pieces
-          const uint32_t atom = sub / 4, piece = (sub % 4) * 2, x7 = row & 7, odd = atom & 1;
-          const uint32_t base = to + atom * (kDepth * 128) + row * 128;
+          const uint32_t x7 = row & 7, p0 = base + (((piece + odd) ^ x7) << 4), p1 = base + (((piece + 1 - odd) ^ x7) << 4);
 #pragma unroll
-          for (int o = 0; o < (SPLIT ? 2 : 1); ++o) {
-            const uint32_t* u = o ? lo : v;
-            const uint32_t b = base + o * S::kB;
-            const uint32_t p0 = b + (((piece + odd) ^ x7) << 4), p1 = b + (((piece + 1 - odd) ^ x7) << 4);
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p0), "r"(odd ? u[4] : u[0]), "r"(odd ? u[5] : u[1]),
-                         "r"(odd ? u[6] : u[2]), "r"(odd ? u[7] : u[3])
+          for (int x = 0; x < PARTS; ++x) {
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p0 + x * S::kB), "r"(v[x][0]), "r"(v[x][1]), "r"(v[x][2]),
+                         "r"(v[x][3])
                          : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p1), "r"(odd ? u[0] : u[4]), "r"(odd ? u[1] : u[5]),
-                         "r"(odd ? u[2] : u[6]), "r"(odd ? u[3] : u[7])
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(p1 + x * S::kB), "r"(v[x][4]), "r"(v[x][5]), "r"(v[x][6]),
+                         "r"(v[x][7])
                          : "memory");
           }
         }
@@ -241,6 +276,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(ready0 + 8 * s);
       }
+      it += k1 - k0;
     }
   } else {
     const int quad = warp & 3;
@@ -332,28 +368,28 @@ __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, 
 
 // ---- launches ------------------------------------------------------------------------------------------------------
 struct Plan {
-  int shape;                 // 0: pair of CTAs, 256 columns; 1: one CTA, 128 columns; 2: one CTA, 64 columns
+  int cg, bn;                // CTAs and columns of a tile
   uint32_t splits;
 };
-constexpr int kShapes[3][2] = {{2, 256}, {1, 128}, {1, 64}};
 
-// Time of a plan in clock cycles.  A stage takes 8192 multiply-adds a cycle and SM (twice as many of them for a split
-// operand) or, where that is longer, the copies and the conversion; a tile costs a fixed beginning and end; partial
+// Time of a plan in clock cycles.  A stage takes 4096 multiply-adds a cycle and SM (three times as many for an operand in
+// three parts) or, where that is longer, the copies and the conversion; a tile costs a fixed beginning and end; partial
 // results cost their way through memory and one more launch.
-Plan plan_of(uint64_t m, uint32_t n, uint32_t ksteps, bool split_operand, size_t out_elem, int sms) {
-  Plan best = {0, 1};
+Plan plan_of(uint64_t m, uint32_t n, uint32_t ksteps, int parts, size_t out_elem, int sms) {
+  static const int shapes[2][3][2] = {{{2, 256}, {1, 128}, {1, 64}}, {{2, 128}, {1, 64}, {1, 64}}};
+  Plan best = {0, 0, 1};
   double least = 1e300;
-  for (int i = 0; i < 3; ++i) {
-    const int cg = kShapes[i][0], bn = kShapes[i][1];
+  for (const auto& sh : shapes[parts == 3]) {
+    const int cg = sh[0], bn = sh[1];
     const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg;
-    const double product = (cg == 2 ? 512.0 : 4.0 * bn) * (split_operand ? 2 : 1), other = cg == 2 ? 620.0 : 300.0 + 2.5 * bn;
+    const double product = 2.0 * bn * parts, other = 200.0 + 2.5 * bn / cg * (parts == 3 ? 2 : 1);
     const double stage = product > other ? product : other;
     for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
       if (sp > 1 && (double)m * n * sp * 4 > 256e6) break;      // (a quarter of a gigabyte of workspace at most)
       const double rounds = (double)((tiles * sp + units - 1) / units);
       double c = rounds * ((ksteps + sp - 1) / sp * stage + 2500.0);
       if (sp > 1) c += (double)m * n * (4.0 * sp * 2 + out_elem) / 3000.0 + 4000.0;
-      if (c < least) { least = c; best = {i, sp}; }
+      if (c < least) { least = c; best = {cg, bn, sp}; }
     }
   }
   return best;
@@ -368,7 +404,7 @@ Work work_of(const GemmArgs& g, bool dw, int sms) {
   Work w;
   const uint64_t m = dw ? g.n : g.t, depth = dw ? g.t : g.n;
   const size_t e = g.out_dtype == STQ_GRAD_F32 ? 4 : 2;
-  w.plan = plan_of(m, g.k, (uint32_t)((depth + kDepth - 1) / kDepth), e == 4, e, sms);
+  w.plan = plan_of(m, g.k, (uint32_t)((depth + kDepth - 1) / kDepth), e == 4 ? 3 : 1, e, sms);
   w.pitch = ((g.lddy & 7) != 0 && g.t > 1) || (reinterpret_cast<uintptr_t>(g.dy) & 15) != 0;
   w.lddy = w.pitch || g.t == 1 ? ((size_t)g.n + 7) / 8 * 8 : g.lddy;
   w.pitch_bytes = w.pitch ? (g.t * w.lddy * 2 + 255) / 256 * 256 : 0;
@@ -377,9 +413,9 @@ Work work_of(const GemmArgs& g, bool dw, int sms) {
   return w;
 }
 
-template <int CG, int BN, bool SPLIT, bool DW, class O>
+template <int CG, int BN, int PARTS, bool DW, class O>
 cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t stream) {
-  using S = GradShape<CG, BN, SPLIT>;
+  using S = GradShape<CG, BN, PARTS>;
   GradArgs a;
   const int8_t* q = DW ? g.xq : g.wq;
   const size_t ldq = DW ? g.ldx : g.ldw;
@@ -399,18 +435,22 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, 
   CUtensorMap mg, mq;
   cudaError_t e = make_tensor_map(&mg, dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess) e = make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false);
-  auto* kernel = q8_grad_kernel<CG, BN, SPLIT, DW, O>;
+  auto* kernel = q8_grad_kernel<CG, BN, PARTS, DW, O>;
   if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
   return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, kThreadsG, S::kSmem, CG, stream, mg, mq, a);
 }
 
-template <bool SPLIT, bool DW, class O>
+template <int PARTS, bool DW, class O>
 cudaError_t by_shape(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t s) {
-  if (w.plan.shape == 0) return launch<2, 256, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
-  if (w.plan.shape == 1) return launch<1, 128, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
-  return launch<1, 64, SPLIT, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  if constexpr (PARTS == 1) {
+    if (w.plan.bn == 256) return launch<2, 256, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+    if (w.plan.bn == 128) return launch<1, 128, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  } else {
+    if (w.plan.bn == 128) return launch<2, 128, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  }
+  return launch<1, 64, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
 }
 
 template <bool DW>
@@ -432,10 +472,10 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   float* part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.pitch_bytes);
   void* out = split ? part : g.out;
   const size_t ldo = split ? w.ldp : g.ldo;
-  // (an fp32 result takes the split operand; partial results of a bf16 one are fp32 sums of the single operand)
-  cudaError_t e = f32 ? by_shape<true, DW, float>(g, w, dy, out, ldo, err, sms, stream)
-                  : split ? by_shape<false, DW, float>(g, w, dy, out, ldo, err, sms, stream)
-                          : by_shape<false, DW, __nv_bfloat16>(g, w, dy, out, ldo, err, sms, stream);
+  // (an fp32 result takes the operand in three parts; partial results of a bf16 one are fp32 sums of the single operand)
+  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, dy, out, ldo, err, sms, stream)
+                  : split ? by_shape<1, DW, float>(g, w, dy, out, ldo, err, sms, stream)
+                          : by_shape<1, DW, __nv_bfloat16>(g, w, dy, out, ldo, err, sms, stream);
   if (e != cudaSuccess || !split) return e;
   const uint64_t items = m * (w.ldp / 4);
   const unsigned grid = (unsigned)((items + 255) / 256);

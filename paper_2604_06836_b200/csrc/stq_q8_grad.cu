@@ -113,10 +113,10 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
   __shared__ uint32_t tmem_slot;
   __shared__ float stage[4][32 * 33];
   const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
-  // per stage: codes have landed (this CTA), gradient has landed (both CTAs, at the leader), codes are converted (both
-  // CTAs, at the leader), stage is free
-  const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * kStages, ready = full_g + 8 * kStages, empty = ready + 8 * kStages;
-  const uint32_t done = empty + 8 * kStages, freed = done + 16;
+  // per stage: codes have landed (this CTA), gradient has landed and codes are converted (both CTAs, at the leader),
+  // stage is free; per accumulator: done, read (both CTAs, at the leader)
+  const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * kStages, ready = full_g + 8 * kStages;
+  const uint32_t empty = ready + 8 * kStages, done = empty + 8 * kStages, freed = done + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0;
   const bool leader = rank == 0;
@@ -187,11 +187,11 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       for (uint32_t w = unit; ok && w < work; w += units, ++n) {
         share(w, tile, k0, k1);
         const uint32_t acc = n & 1;
-        if (!(ok = bar_wait(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+        if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
         mma_fence_after();
         for (uint32_t k = k0; k < k1; ++k, ++it) {
           const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-          if (!(ok = bar_wait(full_g + 8 * s, ph) && bar_wait(ready + 8 * s, ph))) break;
+          if (!(ok = bar_wait(full_g + 8 * s, ph) && bar_wait<CG == 2>(ready + 8 * s, ph))) break;
           mma_fence_after();
           const uint32_t at = ring + s * S::kStage;
           const uint64_t da = DW ? operand_desc(at, S::kA / 2, 1024) : operand_desc(at, 16, 1024);
@@ -274,7 +274,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the products read shared memory by another path
         __syncwarp();
-        if (lane == 0) bar_arrive_cluster(ready0 + 8 * s);
+        if (lane == 0) bar_arrive_leader<CG>(ready + 8 * s, ready0 + 8 * s, leader);
       }
       it += k1 - k0;
     }
@@ -305,7 +305,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       }
       mma_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive_cluster(freed0 + 8 * acc);
+      if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
     }
   }
   if (!ok) *a.err = 1;

@@ -51,7 +51,8 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
   __shared__ float scale_n[2][BN], bias_n[2][BN];
   __shared__ float stage[4][32 * 33];
   const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
-  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, freed = done + 16;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
+  const uint32_t freed = done + 16;      // accumulators are read (both CTAs, at the leader)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0;
   const bool leader = rank == 0;
@@ -100,7 +101,7 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       uint32_t it = 0, n = 0;
       for (uint32_t tile = unit; ok && tile < tiles; tile += units, ++n) {
         const uint32_t acc = n & 1;
-        if (!(ok = bar_wait(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+        if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
         mma_fence_after();
         for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
           const uint32_t s = it % kStages, ph = (it / kStages) & 1;
@@ -149,7 +150,7 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       }
       mma_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive_cluster(freed0 + 8 * acc);
+      if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
     }
   }
   if (!ok) *a.err = 1;

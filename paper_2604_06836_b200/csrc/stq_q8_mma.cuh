@@ -18,30 +18,44 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// Arrival on a barrier of this CTA or of another CTA of the cluster (address from peer_addr).
-__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// Arrival on a barrier of another CTA of the cluster (address from peer_addr).  The release is at CTA scope: it orders
+// this thread's shared-memory writes and tensor-memory reads, and nothing else that the waiting side goes on to use is
+// written here.  (A release at cluster scope also waits for every global access in flight: 1400 cycles measured behind
+// the loads of the scales.)
+__device__ __forceinline__ void bar_arrive_peer(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t peer_addr(uint32_t local, uint32_t rank) {
   uint32_t a;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(local), "r"(rank));
   return a;
 }
+template <bool CLUSTER>
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
+  if constexpr (CLUSTER)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
   return ok != 0;
 }
+// CLUSTER: arrivals come from another CTA of the cluster too.
+template <bool CLUSTER = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-  if (bar_try(bar, parity)) return true;
+  if (bar_try<CLUSTER>(bar, parity)) return true;
   const long long t0 = clock64();
-  while (!bar_try(bar, parity))
+  while (!bar_try<CLUSTER>(bar, parity))
     if (clock64() - t0 > kMmaWaitCycles) return false;
   return true;
 }
@@ -53,6 +67,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Arrival on the barrier of a pair's leader (or of the CTA itself): `bar` in this CTA, `bar0` its address at the leader.
+template <int CG>
+__device__ __forceinline__ void bar_arrive_leader(uint32_t bar, uint32_t bar0, bool leader) {
+  if (CG == 1 || leader)
+    bar_arrive(bar);
+  else
+    bar_arrive_peer(bar0);
 }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;

@@ -81,6 +81,7 @@ struct GemmArgs {
   int out_dtype;
   uint64_t t;            // tokens
   uint32_t n, k;         // output and input channels
+  int device;
 };
 // (err: the handle's flag, raised by a wait that ran out)
 cudaError_t launch_q8_linear(const GemmArgs& a, int sms, int* err, cudaStream_t stream);

@@ -248,6 +248,7 @@ int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xs
   a.bias = bias;
   a.out = out; a.ldo = ldo; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
+  a.device = h->device;
   STQ_CUDA(h, cudaSetDevice(h->device));
   STQ_CUDA(h, stq::launch_q8_linear(a, h->sm_count, h->d_err, static_cast<cudaStream_t>(stream)));
   h->launches++;
@@ -272,6 +273,7 @@ int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.wq = wq; a.ldw = ldw; a.ws = wscale;
   a.out = dx; a.ldo = lddx; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
+  a.device = h->device;
   STQ_CUDA(h, cudaSetDevice(h->device));
   uint8_t* ws = nullptr;
   int launches = 0;
@@ -301,6 +303,7 @@ int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.xq = xq; a.ldx = ldx; a.xs = xscale;
   a.out = dw; a.ldo = lddw; a.out_dtype = out_dtype;
   a.t = t; a.n = n; a.k = k;
+  a.device = h->device;
   uint8_t* ws = nullptr;
   int launches = 0;
   if (const size_t need = stq::q8_grad_workspace(a, true, h->sm_count)) STQ_TRY(workspace(h, need, &ws));

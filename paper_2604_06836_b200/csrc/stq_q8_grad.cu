@@ -436,7 +436,8 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, 
   cudaError_t e = make_tensor_map(&mg, dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess) e = make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false);
   auto* kernel = q8_grad_kernel<CG, BN, PARTS, DW, O>;
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  static std::atomic<uint64_t> seen;
+  if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
   return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, kThreadsG, S::kSmem, CG, stream, mg, mq, a);

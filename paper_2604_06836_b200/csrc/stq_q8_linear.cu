@@ -178,7 +178,8 @@ cudaError_t launch(const GemmArgs& g, int sms, int* err, cudaStream_t stream) {
   CUtensorMap mx, mw;
   cudaError_t e = make_tensor_map(&mx, g.xq, 1, g.t, g.k, g.ldx, 128, kBK, true);
   if (e == cudaSuccess) e = make_tensor_map(&mw, g.wq, 1, g.n, g.k, g.ldw, BN / CG, kBK, true);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(q8_linear_kernel<CG, BN, O>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  static std::atomic<uint64_t> seen;
+  if (e == cudaSuccess) e = allow_smem(q8_linear_kernel<CG, BN, O>, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n, most = sms / CG;
   return launch_cluster(q8_linear_kernel<CG, BN, O>, (unsigned)(tiles < most ? tiles : most) * CG, kThreads8, S::kSmem, CG,

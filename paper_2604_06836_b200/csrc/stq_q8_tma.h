@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace stq {
 
 // `elem` 1: bytes, 2: bf16.  The box is box_cols x box_rows elements, box_cols * elem <= 128 bytes; base and pitch are
@@ -15,6 +17,16 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* p, int elem, uint64_t 
 inline int row_alignment(const void* p, size_t pitch) {
   const uintptr_t b = reinterpret_cast<uintptr_t>(p) | pitch;
   return (b & 31) == 0 ? 32 : (b & 15) == 0 ? 16 : 1;
+}
+
+// Lets a kernel take `bytes` of dynamic shared memory; `seen` has a bit for each device where that is settled.
+template <class K>
+cudaError_t allow_smem(K kernel, size_t bytes, int device, std::atomic<uint64_t>& seen) {
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (bit && (seen.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) seen.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 template <class K, class... A>

@@ -18,6 +18,8 @@ from . import stq
 CKPT_BLOCK = 128                                   # STQ_CKPT_BLOCK: columns per scale of a checkpoint
 KINDS = {"silu_gated": 1, "gelu": 2}               # STQ_ACT_*
 _DTYPES = {torch.float32: stq.GRAD_F32, torch.bfloat16: stq.GRAD_BF16}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream)      # (a build of torch without CUDA)
 
 _fn = None
 
@@ -81,49 +83,82 @@ class ActOut(NamedTuple):
 
 
 # ---- arguments ---------------------------------------------------------------------------------------------------
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
-
-def _mat(name: str, t: torch.Tensor, dev: int, dtype=None, rows=None, cols=None) -> int:
-    """Checks a matrix and returns its row pitch in elements."""
-    _need(t.dim() == 2, f"{name} is a matrix")
-    d = t.device
-    _need(d.type == "cuda" and d.index == dev, f"{name} lives on the handle's device")
-    if dtype is not None:
-        _need(t.dtype == dtype, f"{name} is {dtype}, not {t.dtype}")
-    r, c = t.shape
-    _need(rows is None or r == rows, f"{name} has {rows} rows, not {r}")
-    _need(cols is None or c == cols, f"{name} has {cols} columns, not {c}")
+# The checks run on every call, also for a single token, so the usual case takes as few steps as it can; what is wrong
+# is found out only once something is.
+def _pitch(t: torch.Tensor, dev: int, dtype, rows, cols) -> int:
+    """Row pitch in elements of a matrix that is as it should be (None: anything goes), else -1."""
+    shape = t.shape
+    if len(shape) != 2 or t.get_device() != dev or (dtype is not None and t.dtype is not dtype):
+        return -1
+    r, c = shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        return -1
     ld, unit = t.stride()
-    _need(unit == 1 or c == 1, f"{name} has unit stride along a row")
-    if r <= 1:
-        return c if ld < c else ld
-    _need(ld >= c, f"{name}'s rows do not overlap")
+    if unit != 1 and c > 1:
+        return -1
+    if ld < c:
+        return c if r <= 1 else -1
     return ld
 
 
-def _vec(name: str, t: torch.Tensor, dev: int, n: int, dtype=torch.float32):
-    _need(t.dim() == 1 and t.shape[0] == n and t.dtype == dtype and t.is_contiguous(),
-          f"{name} is a contiguous {dtype} vector of {n}")
-    _need(t.device.type == "cuda" and t.device.index == dev, f"{name} lives on the handle's device")
+def _refuse(name: str, t: torch.Tensor, dev: int, dtype, rows, cols):
+    if t.dim() != 2:
+        raise ValueError(f"{name} is a matrix")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} lives on the handle's device")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} is {dtype}, not {t.dtype}")
+    r, c = t.shape
+    if rows is not None and r != rows:
+        raise ValueError(f"{name} has {rows} rows, not {r}")
+    if cols is not None and c != cols:
+        raise ValueError(f"{name} has {cols} columns, not {c}")
+    if t.stride(1) != 1 and c > 1:
+        raise ValueError(f"{name} has unit stride along a row")
+    raise ValueError(f"{name}'s rows do not overlap")
+
+
+def _mat(name: str, t: torch.Tensor, dev: int, dtype=None, rows=None, cols=None) -> int:
+    ld = _pitch(t, dev, dtype, rows, cols)
+    if ld < 0:
+        _refuse(name, t, dev, dtype, rows, cols)
+    return ld
+
+
+def _vec(name: str, t: torch.Tensor, dev: int, n: int):
+    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous float32 vector of {n}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} lives on the handle's device")
 
 
 def _rows(name: str, r: Rows8, dev: int, cols=None, rows=None) -> int:
-    ld = _mat(f"{name}.q", r.q, dev, torch.int8, rows, cols)
-    _vec(f"{name}.scale", r.scale, dev, r.q.shape[0])
-    return (ld + 15) // 16 * 16 if r.q.shape[0] <= 1 else ld
+    q, scale = r
+    ld = _pitch(q, dev, torch.int8, rows, cols)
+    if ld < 0:
+        _refuse(f"{name}.q", q, dev, torch.int8, rows, cols)
+    n = q.shape[0]
+    _vec(f"{name}.scale", scale, dev, n)
+    return (ld + 15) // 16 * 16 if n <= 1 else ld
 
 
 def _dtype(name: str, t: torch.Tensor) -> int:
-    _need(t.dtype in _DTYPES, f"{name} is float32 or bfloat16, not {t.dtype}")
-    return _DTYPES[t.dtype]
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{name} is float32 or bfloat16, not {t.dtype}")
+    return dt
 
 
 def _out_dtype(dtype) -> int:
-    _need(dtype in _DTYPES, f"dtype is float32 or bfloat16, not {dtype}")
-    return _DTYPES[dtype]
+    dt = _DTYPES.get(dtype)
+    if dt is None:
+        raise ValueError(f"dtype is float32 or bfloat16, not {dtype}")
+    return dt
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
 
 
 class _On:
@@ -144,13 +179,20 @@ class _On:
 
 
 def _stream(dev: int):
-    return torch.cuda.current_stream(dev).cuda_stream or None
+    return _raw_stream(dev) or None
+
+
+def _new(rows: int, cols: int, pitch: int, dtype, device) -> torch.Tensor:
+    return torch.empty_strided((rows, cols), (pitch, 1), dtype=dtype, device=device)
+
+
+def _new_vec(n: int, device) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=torch.float32, device=device)
 
 
 def alloc_rows(rows: int, cols: int, device) -> Rows8:
     """Uninitialised 8-bit rows with the pitch that the operators need."""
-    q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)
-    return Rows8(q if q.shape[1] == cols else q[:, :cols], torch.empty(rows, dtype=torch.float32, device=device))
+    return Rows8(_new(rows, cols, (cols + 15) // 16 * 16, torch.int8, device), _new_vec(rows, device))
 
 
 # ---- operators ---------------------------------------------------------------------------------------------------
@@ -165,8 +207,10 @@ def quantize_rows(handle: stq.Handle, x: torch.Tensor, *, out: Rows8 | None = No
     if out is None:
         out = alloc_rows(rows, cols, x.device)
     ldq = _rows("out", out, dev, cols, rows)
-    handle._check(_lib().stq_q8_rows(handle._h, x.data_ptr(), ldx, dt, rows, cols, out.q.data_ptr(), ldq,
-                                     out.scale.data_ptr(), _stream(dev)), "stq_q8_rows")
+    rc = _lib().stq_q8_rows(handle._h, x.data_ptr(), ldx, dt, rows, cols, out.q.data_ptr(), ldq,
+        out.scale.data_ptr(), _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_rows")
     return out
 
 
@@ -184,15 +228,17 @@ def norm(handle: stq.Handle, x: torch.Tensor, weight: torch.Tensor, *, residual:
     h, res_ptr, ldres, h_ptr = x, None, 0, None
     if residual is not None:
         ldres = _mat("residual", residual, dev, x.dtype, rows, cols)
-        h = torch.empty((rows, cols), dtype=x.dtype, device=device)
+        h = _new(rows, cols, cols, x.dtype, device)
         res_ptr, h_ptr = residual.data_ptr(), h.data_ptr()
     r = alloc_rows(rows, cols, device)
-    stats = torch.empty(rows, dtype=torch.float32, device=device)
-    vals = torch.empty((rows, cols), dtype=torch.bfloat16, device=device) if values else None
-    handle._check(_lib().stq_q8_norm(
+    stats = _new_vec(rows, device)
+    vals = _new(rows, cols, cols, torch.bfloat16, device) if values else None
+    rc = _lib().stq_q8_norm(
         handle._h, x.data_ptr(), ldx, res_ptr, ldres, weight.data_ptr(), eps, dt, rows, cols, h_ptr, cols,
         stats.data_ptr(), r.q.data_ptr(), (cols + 15) // 16 * 16, r.scale.data_ptr(),
-        None if vals is None else vals.data_ptr(), cols, _stream(dev)), "stq_q8_norm")
+        None if vals is None else vals.data_ptr(), cols, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_norm")
     return NormOut(h, r, stats, vals)
 
 
@@ -210,12 +256,14 @@ def norm_backward(handle: stq.Handle, dy: torch.Tensor, h: torch.Tensor, weight:
     _vec("weight", weight, dev, cols)
     _vec("rstd", rstd, dev, rows)
     ldres = 0 if dres is None else _mat("dres", dres, dev, dy.dtype, rows, cols)
-    dx = torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
-    dweight = torch.empty(cols, dtype=torch.float32, device=dy.device)
-    handle._check(_lib().stq_q8_norm_backward(
+    dx = _new(rows, cols, cols, dy.dtype, dy.device)
+    dweight = _new_vec(cols, dy.device)
+    rc = _lib().stq_q8_norm_backward(
         handle._h, dy.data_ptr(), lddy, h.data_ptr(), ldh, weight.data_ptr(), rstd.data_ptr(),
         None if dres is None else dres.data_ptr(), ldres, dt, rows, cols, dx.data_ptr(), cols, dweight.data_ptr(),
-        _stream(dev)), "stq_q8_norm_backward")
+        _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_norm_backward")
     return dx, dweight
 
 
@@ -226,7 +274,8 @@ def act(handle: stq.Handle, z: torch.Tensor, kind: str = "silu_gated", *, checkp
     if stream is not None:
         with _On(stream, (z,)):
             return act(handle, z, kind, checkpoint=checkpoint, values=values)
-    _need(kind in KINDS, "kind is one of " + ", ".join(KINDS))
+    if kind not in KINDS:
+        raise ValueError("kind is one of " + ", ".join(KINDS))
     dev = handle.device
     dt, ldz = _dtype("z", z), _mat("z", z, dev)
     parts = 2 if kind == "silu_gated" else 1
@@ -234,15 +283,17 @@ def act(handle: stq.Handle, z: torch.Tensor, kind: str = "silu_gated", *, checkp
     _need(cols * parts == z.shape[1], "a gated activation takes an even number of columns")
     device, pitch = z.device, (cols + 15) // 16 * 16
     r = alloc_rows(rows, cols, device)
-    vals = torch.empty((rows, cols), dtype=torch.bfloat16, device=device) if values else None
+    vals = _new(rows, cols, cols, torch.bfloat16, device) if values else None
     ck, ckq, cks = None, None, None
     if checkpoint:
         ck = Checkpoint8(torch.empty((rows, parts, pitch), dtype=torch.int8, device=device),
                          torch.empty((rows, parts, -(-cols // CKPT_BLOCK)), dtype=torch.float32, device=device), cols, kind)
         ckq, cks = ck.q.data_ptr(), ck.scale.data_ptr()
-    handle._check(_lib().stq_q8_act(
+    rc = _lib().stq_q8_act(
         handle._h, z.data_ptr(), ldz, KINDS[kind], dt, rows, cols, r.q.data_ptr(), pitch, r.scale.data_ptr(),
-        None if vals is None else vals.data_ptr(), cols, ckq, pitch, cks, _stream(dev)), "stq_q8_act")
+        None if vals is None else vals.data_ptr(), cols, ckq, pitch, cks, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_act")
     return ActOut(r, ck, vals)
 
 
@@ -260,10 +311,11 @@ def act_backward(handle: stq.Handle, da: torch.Tensor, checkpoint: Checkpoint8, 
     _need(q.device.index == dev and scale.device.index == dev and q.is_cuda and scale.is_cuda,
           "the checkpoint lives on the handle's device")
     dt, ldda = _dtype("da", da), _mat("da", da, dev, None, rows, cols)
-    dz = torch.empty((rows, parts * cols), dtype=da.dtype, device=da.device)
-    handle._check(_lib().stq_q8_act_backward(handle._h, da.data_ptr(), ldda, KINDS[kind], dt, rows, cols, q.data_ptr(),
-                                             pitch, scale.data_ptr(), dz.data_ptr(), parts * cols, _stream(dev)),
-                  "stq_q8_act_backward")
+    dz = _new(rows, parts * cols, parts * cols, da.dtype, da.device)
+    rc = _lib().stq_q8_act_backward(handle._h, da.data_ptr(), ldda, KINDS[kind], dt, rows, cols, q.data_ptr(),
+        pitch, scale.data_ptr(), dz.data_ptr(), parts * cols, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_act_backward")
     return dz
 
 
@@ -280,10 +332,12 @@ def linear(handle: stq.Handle, x: Rows8, w: Rows8, *, bias: torch.Tensor | None 
     n = w.q.shape[0]
     if bias is not None:
         _vec("bias", bias, dev, n)
-    out = torch.empty((t, n), dtype=dtype, device=x.q.device)
-    handle._check(_lib().stq_q8_linear(
+    out = _new(t, n, n, dtype, x.q.device)
+    rc = _lib().stq_q8_linear(
         handle._h, x.q.data_ptr(), ldx, x.scale.data_ptr(), w.q.data_ptr(), ldw, w.scale.data_ptr(),
-        None if bias is None else bias.data_ptr(), t, n, k, out.data_ptr(), n, odt, _stream(dev)), "stq_q8_linear")
+        None if bias is None else bias.data_ptr(), t, n, k, out.data_ptr(), n, odt, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_linear")
     return out
 
 
@@ -297,9 +351,11 @@ def linear_dx(handle: stq.Handle, dy: torch.Tensor, w: Rows8, *, dtype=torch.bfl
     n, k = w.q.shape
     lddy = _mat("dy", dy, dev, torch.bfloat16, None, n)
     t = dy.shape[0]
-    out = torch.empty((t, k), dtype=dtype, device=dy.device)
-    handle._check(_lib().stq_q8_linear_dx(handle._h, dy.data_ptr(), lddy, w.q.data_ptr(), ldw, w.scale.data_ptr(), t, n, k,
-                                          out.data_ptr(), k, odt, _stream(dev)), "stq_q8_linear_dx")
+    out = _new(t, k, k, dtype, dy.device)
+    rc = _lib().stq_q8_linear_dx(handle._h, dy.data_ptr(), lddy, w.q.data_ptr(), ldw, w.scale.data_ptr(), t, n, k,
+        out.data_ptr(), k, odt, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_linear_dx")
     return out
 
 
@@ -314,9 +370,11 @@ def linear_dw(handle: stq.Handle, dy: torch.Tensor, x: Rows8, *, dtype=torch.bfl
     t, k = x.q.shape
     lddy = _mat("dy", dy, dev, torch.bfloat16, t)
     n = dy.shape[1]
-    out = torch.empty((n, k), dtype=dtype, device=dy.device)
-    handle._check(_lib().stq_q8_linear_dw(handle._h, dy.data_ptr(), lddy, x.q.data_ptr(), ldx, x.scale.data_ptr(), t, n, k,
-                                          out.data_ptr(), k, odt, _stream(dev)), "stq_q8_linear_dw")
+    out = _new(n, k, k, dtype, dy.device)
+    rc = _lib().stq_q8_linear_dw(handle._h, dy.data_ptr(), lddy, x.q.data_ptr(), ldx, x.scale.data_ptr(), t, n, k,
+        out.data_ptr(), k, odt, _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_linear_dw")
     return out
 
 
@@ -328,7 +386,8 @@ def bias_grad(handle: stq.Handle, dy: torch.Tensor, *, stream=None) -> torch.Ten
     dev = handle.device
     dt, ld = _dtype("dy", dy), _mat("dy", dy, dev)
     t, n = dy.shape
-    out = torch.empty(n, dtype=torch.float32, device=dy.device)
-    handle._check(_lib().stq_q8_bias_grad(handle._h, dy.data_ptr(), ld, dt, t, n, out.data_ptr(), _stream(dev)),
-                  "stq_q8_bias_grad")
+    out = _new_vec(n, dy.device)
+    rc = _lib().stq_q8_bias_grad(handle._h, dy.data_ptr(), ld, dt, t, n, out.data_ptr(), _stream(dev))
+    if rc:
+        handle._check(rc, "stq_q8_bias_grad")
     return out

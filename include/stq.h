@@ -272,7 +272,7 @@ int stq_sm_count(const stq_handle* h);
  * value is q * scale.  With amax = max |x| of the row: scale = amax / 127, q = rne(x * (127 * fl(1/amax))).
  * amax < 2^-100: scale 0 and codes 0.  A row that holds an infinity or a NaN: scale NaN and codes 0, so
  * that everything computed from the row is NaN.  Code buffers are 16-byte aligned with a pitch that is a
- * multiple of 16 (bytes beyond cols are neither read nor written); scale buffers are 4-byte aligned.
+ * multiple of 16 (bytes beyond cols do not matter and are not written); scale buffers are 4-byte aligned.
  * Activation checkpoint: codes [rows][parts][ldck] and scales [rows][parts][ceil(cols/128)], one scale
  * per 128 consecutive columns by the same rule; parts = 2 for the gated activation (gate, up), else 1.
  *

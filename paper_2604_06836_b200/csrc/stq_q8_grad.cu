@@ -10,9 +10,14 @@
 // numbers whose sum is exactly that product, and three products are added up: the error is that of fp32 arithmetic.
 // Folding s into G instead would round as much and touch the larger operand.
 //
+// Two forms.  CONV: the codes are converted inside the product kernel, once per row of tiles of the result.  Otherwise a
+// small kernel writes the converted operand to the workspace first and the product kernel only copies and multiplies;
+// that pays once the result has many rows (plan_of), and only for the single operand: in three parts the products take
+// longer than the conversion anyway.  Both form the same operand.
+//
 // Per CTA: warp 0 copies tiles of G and q into a ring of stages, two groups of four warps convert q in alternate stages,
 // one warp issues the products, four warps write results; accumulators are doubled in tensor memory as in the forward
-// product.
+// product.  (Without conversion there are the copying, the issuing and the four writing warps.)
 #include "../../include/stq.h"
 #include "stq_internal.h"
 #include "stq_q8.h"
@@ -25,7 +30,6 @@ namespace {
 constexpr int kDepth = 64;             // length of the sum per stage
 constexpr int kStepK = 16;             // and per product instruction
 constexpr int kGroups = 2, kGroupWarps = 4;        // conversion: groups of warps, a stage to a group
-constexpr int kThreadsG = 32 * (2 + 4 + kGroups * kGroupWarps);
 
 struct GradArgs {
   const float* scale;                  // s[c]
@@ -38,10 +42,11 @@ struct GradArgs {
   int* err;
 };
 
-template <int CG, int BN, int PARTS>
+template <int CG, int BN, int PARTS, bool CONV>
 struct GradShape {
+  static constexpr int kThreads = 32 * (2 + 4 + (CONV ? kGroups * kGroupWarps : 0));
   static constexpr int kNB = BN / CG;                             // columns of the 8-bit operand in this CTA
-  static constexpr int kA = 128 * kDepth * 2, kQ = kDepth * kNB, kB = kDepth * kNB * 2;
+  static constexpr int kA = 128 * kDepth * 2, kQ = CONV ? kDepth * kNB : 0, kB = kDepth * kNB * 2;
   static constexpr int kStage = kA + kQ + kB * PARTS;
   static constexpr int kFit = (204 * 1024) / kStage;
   static constexpr int kStages = kFit < 6 ? kFit : 6;
@@ -103,10 +108,10 @@ __device__ __forceinline__ void decode_pair3(uint32_t w, int i, const Scale2& s,
   }
 }
 
-template <int CG, int BN, int PARTS, bool DW, class O>
-__global__ void __launch_bounds__(kThreadsG, 1)
+template <int CG, int BN, int PARTS, bool CONV, bool DW, class O>
+__global__ void __launch_bounds__((GradShape<CG, BN, PARTS, CONV>::kThreads), 1)
 q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_q, const GradArgs a) {
-  using S = GradShape<CG, BN, PARTS>;
+  using S = GradShape<CG, BN, PARTS, CONV>;
   constexpr int kStages = S::kStages, kNB = S::kNB;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[4 * kStages + 4];
@@ -163,9 +168,15 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           const uint32_t s = it % kStages, ph = (it / kStages) & 1;
           if (!(ok = bar_wait(empty + 8 * s, ph ^ 1))) break;
           const uint32_t at = ring + s * S::kStage, c = k * kDepth;
-          if (leader) bar_expect(full_g + 8 * s, CG * S::kA);
-          bar_expect(full_q + 8 * s, S::kQ);
-          tensor_load<1>(at + S::kA, &map_q, col, (int)c, full_q + 8 * s);
+          if (leader) bar_expect(full_g + 8 * s, CG * (S::kA + (CONV ? 0 : S::kB)));
+          if constexpr (CONV) {
+            bar_expect(full_q + 8 * s, S::kQ);
+            tensor_load<1>(at + S::kA, &map_q, col, (int)c, full_q + 8 * s);
+          } else {
+#pragma unroll
+            for (int i = 0; i < kNB / 64; ++i)
+              tensor_load<CG>(at + S::kA + i * (kDepth * 128), &map_q, col + 64 * i, (int)c, full_g0 + 8 * s);
+          }
           if constexpr (DW) {
             tensor_load<CG>(at, &map_g, row, (int)c, full_g0 + 8 * s);
             tensor_load<CG>(at + S::kA / 2, &map_g, row + 64, (int)c, full_g0 + 8 * s);
@@ -176,7 +187,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       }
       if (!ok)      // leave no copy in flight
         for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
-          bar_wait(full_q + 8 * (i % kStages), (i / kStages) & 1);
+          if (CONV) bar_wait(full_q + 8 * (i % kStages), (i / kStages) & 1);
           if (leader) bar_wait(full_g + 8 * (i % kStages), (i / kStages) & 1);
         }
     }
@@ -191,7 +202,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         mma_fence_after();
         for (uint32_t k = k0; k < k1; ++k, ++it) {
           const uint32_t s = it % kStages, ph = (it / kStages) & 1;
-          if (!(ok = bar_wait(full_g + 8 * s, ph) && bar_wait<CG == 2>(ready + 8 * s, ph))) break;
+          if (!(ok = bar_wait<CG == 2>(full_g + 8 * s, ph) && (!CONV || bar_wait<CG == 2>(ready + 8 * s, ph)))) break;
           mma_fence_after();
           const uint32_t at = ring + s * S::kStage;
           const uint64_t da = DW ? operand_desc(at, S::kA / 2, 1024) : operand_desc(at, 16, 1024);
@@ -208,7 +219,8 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         if (ok) mma_commit<CG>(done + 8 * acc);
       }
     }
-  } else if (warp < 2 + kGroups * kGroupWarps) {
+  } else if (CONV && warp < 2 + kGroups * kGroupWarps) {
+    if constexpr (CONV) {
     // A row of the stage has kNB codes: kNB / 16 lanes take 16 bytes each.
     constexpr int kLanes = kNB / 16, kRowsAtOnce = kGroupWarps * 32 / kLanes, kPasses = kDepth / kRowsAtOnce;
     const int group = (warp - 2) / kGroupWarps, thread = (threadIdx.x - 64) % (kGroupWarps * 32);
@@ -278,6 +290,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       }
       it += k1 - k0;
     }
+    }
   } else {
     const int quad = warp & 3;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
@@ -317,6 +330,35 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
     mma_fence_after();
     tmem_free<CG>(tmem, S::kCols);
   }
+}
+
+// The operand converted beforehand: `plane` rows of ld bf16 numbers; rows from `rows` on and columns from `cols` on are
+// zero.  16 columns to a thread.
+__global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t ldq, const float* scale, uint32_t rows,
+                                                         uint32_t cols, uint32_t plane, __nv_bfloat16* out, size_t ld) {
+  const uint32_t per_row = (uint32_t)((ld + 15) / 16);
+  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint64_t row = id / per_row;
+  if (row >= plane) return;
+  const uint32_t c = (uint32_t)(id - row * per_row) * 16;
+  uint32_t w[4] = {0, 0, 0, 0}, v[8];
+  float sc = 0.f;
+  if (row < rows) {
+    const uint4 x = *reinterpret_cast<const uint4*>(q + row * ldq + c);      // (a row's pitch is a multiple of 16)
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    sc = scale[row];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int left = (int)cols - (int)c - 4 * i;
+      if (left < 4) w[i] &= left <= 0 ? 0u : (1u << (8 * left)) - 1;
+    }
+  }
+  const Scale2 s = scale2_of(sc);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = decode_pair(w[j >> 1], (j & 1) * 2, s);
+  __nv_bfloat16* to = out + row * ld + c;
+  *reinterpret_cast<uint4*>(to) = make_uint4(v[0], v[1], v[2], v[3]);
+  if (c + 8 < ld) *reinterpret_cast<uint4*>(to + 8) = make_uint4(v[4], v[5], v[6], v[7]);
 }
 
 // out[r][c] = sum over splits of part[s][r][c] (rows of `ldp` floats, a multiple of 8), in order
@@ -369,53 +411,73 @@ __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, 
 // ---- launches ------------------------------------------------------------------------------------------------------
 struct Plan {
   int cg, bn;                // CTAs and columns of a tile
+  bool conv;                 // convert inside the product
   uint32_t splits;
 };
 
 // Time of a plan in clock cycles.  A stage takes 4096 multiply-adds a cycle and SM (three times as many for an operand in
 // three parts) or, where that is longer, the copies and the conversion; a tile costs a fixed beginning and end; partial
-// results cost their way through memory and one more launch.
-Plan plan_of(uint64_t m, uint32_t n, uint32_t ksteps, int parts, size_t out_elem, int sms) {
+// results and an operand converted beforehand cost their way through memory (3000 bytes a cycle) and one more launch.
+Plan plan_of(uint64_t m, uint32_t n, uint32_t depth, int parts, size_t out_elem, int sms) {
   static const int shapes[2][3][2] = {{{2, 256}, {1, 128}, {1, 64}}, {{2, 128}, {1, 64}, {1, 64}}};
-  Plan best = {0, 0, 1};
+  const uint32_t ksteps = (depth + kDepth - 1) / kDepth;
+  Plan best = {0, 0, true, 1};
   double least = 1e300;
+  auto weigh = [&](int cg, int bn, bool conv, double stage, double fixed) {
+    const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg;
+    for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
+      if (sp > 1 && (double)m * n * sp * 4 > 256e6) break;      // (a quarter of a gigabyte of partial results at most)
+      const double rounds = (double)((tiles * sp + units - 1) / units);
+      double c = fixed + rounds * ((ksteps + sp - 1) / sp * stage + 2500.0);
+      if (sp > 1) c += (double)m * n * (4.0 * sp * 2 + out_elem) / 3000.0 + 4000.0;
+      if (c < least) { least = c; best = {cg, bn, conv, sp}; }
+    }
+  };
   for (const auto& sh : shapes[parts == 3]) {
     const int cg = sh[0], bn = sh[1];
-    const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg;
-    const double product = 2.0 * bn * parts, other = 200.0 + 2.5 * bn / cg * (parts == 3 ? 2 : 1);
-    const double stage = product > other ? product : other;
-    for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
-      if (sp > 1 && (double)m * n * sp * 4 > 256e6) break;      // (a quarter of a gigabyte of workspace at most)
-      const double rounds = (double)((tiles * sp + units - 1) / units);
-      double c = rounds * ((ksteps + sp - 1) / sp * stage + 2500.0);
-      if (sp > 1) c += (double)m * n * (4.0 * sp * 2 + out_elem) / 3000.0 + 4000.0;
-      if (c < least) { least = c; best = {cg, bn, sp}; }
-    }
+    const double product = 2.0 * bn * parts, other = 200.0 + 2.5 * bn / cg * (parts == 3 ? 2 : 1) + (cg == 2 ? 150.0 : 0.0);
+    weigh(cg, bn, true, product > other ? product : other, 0.0);
   }
+  if (parts == 1 && (double)n * depth * 2 < 1e9) weigh(2, 256, false, 520.0, (double)n * depth * 5.0 / 3000.0 + 4000.0);
   return best;
 }
 
 struct Work {
   Plan plan;
   bool pitch;                // dy has to be copied
-  size_t lddy, part_bytes, pitch_bytes, ldp;
+  size_t lddy, ldp, ldb;     // pitches of dy, of the partial results and of the converted operand
+  uint32_t plane;
+  size_t pitch_bytes, part_bytes, conv_bytes;
 };
 Work work_of(const GemmArgs& g, bool dw, int sms) {
   Work w;
   const uint64_t m = dw ? g.n : g.t, depth = dw ? g.t : g.n;
   const size_t e = g.out_dtype == STQ_GRAD_F32 ? 4 : 2;
-  w.plan = plan_of(m, g.k, (uint32_t)((depth + kDepth - 1) / kDepth), e == 4 ? 3 : 1, e, sms);
+  const int parts = e == 4 ? 3 : 1;
+  auto up = [](size_t v, size_t to) { return (v + to - 1) / to * to; };
+  w.plan = plan_of(m, g.k, (uint32_t)depth, parts, e, sms);
   w.pitch = ((g.lddy & 7) != 0 && g.t > 1) || (reinterpret_cast<uintptr_t>(g.dy) & 15) != 0;
-  w.lddy = w.pitch || g.t == 1 ? ((size_t)g.n + 7) / 8 * 8 : g.lddy;
-  w.pitch_bytes = w.pitch ? (g.t * w.lddy * 2 + 255) / 256 * 256 : 0;
-  w.ldp = ((size_t)g.k + 7) / 8 * 8;
-  w.part_bytes = w.plan.splits > 1 ? w.plan.splits * m * w.ldp * 4 : 0;
+  w.lddy = w.pitch || g.t == 1 ? up(g.n, 8) : g.lddy;
+  w.pitch_bytes = w.pitch ? up(g.t * w.lddy * 2, 256) : 0;
+  w.ldp = up(g.k, 8);
+  w.part_bytes = w.plan.splits > 1 ? up(w.plan.splits * m * w.ldp * 4, 256) : 0;
+  w.ldb = up(g.k, 8);
+  w.plane = (uint32_t)up(depth, kDepth);
+  w.conv_bytes = w.plan.conv ? 0 : (size_t)w.plane * w.ldb * 2;
   return w;
 }
 
-template <int CG, int BN, int PARTS, bool DW, class O>
-cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t stream) {
-  using S = GradShape<CG, BN, PARTS>;
+// Where the product kernel reads and writes.
+struct Ends {
+  const void* dy;
+  const __nv_bfloat16* operand;
+  void* out;
+  size_t ldo;
+};
+
+template <int CG, int BN, int PARTS, bool CONV, bool DW, class O>
+cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, int sms, cudaStream_t stream) {
+  using S = GradShape<CG, BN, PARTS, CONV>;
   GradArgs a;
   const int8_t* q = DW ? g.xq : g.wq;
   const size_t ldq = DW ? g.ldx : g.ldw;
@@ -424,34 +486,37 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const void* dy, void* out, 
   a.depth = (uint32_t)(DW ? g.t : g.n);
   a.n = g.k;
   a.ksteps = (a.depth + kDepth - 1) / kDepth;
-  a.out = out;
-  a.ldo = ldo;
-  a.split_stride = a.m * ldo;
+  a.out = at.out;
+  a.ldo = at.ldo;
+  a.split_stride = a.m * at.ldo;
   a.splits = w.plan.splits;
   a.tiles_m = (uint32_t)((a.m + 128 * CG - 1) / (128 * CG));
   a.tiles_n = (a.n + BN - 1) / BN;
-  a.align = row_alignment(out, ldo * sizeof(O));
+  a.align = row_alignment(at.out, at.ldo * sizeof(O));
   a.err = err;
   CUtensorMap mg, mq;
-  cudaError_t e = make_tensor_map(&mg, dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
-  if (e == cudaSuccess) e = make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false);
-  auto* kernel = q8_grad_kernel<CG, BN, PARTS, DW, O>;
+  cudaError_t e = make_tensor_map(&mg, at.dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
+  if (e == cudaSuccess)
+    e = CONV ? make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false)
+             : make_tensor_map(&mq, at.operand, 2, w.plane, a.n, w.ldb, kDepth, 64, true);
+  auto* kernel = q8_grad_kernel<CG, BN, PARTS, CONV, DW, O>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
-  return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, kThreadsG, S::kSmem, CG, stream, mg, mq, a);
+  return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, stream, mg, mq, a);
 }
 
 template <int PARTS, bool DW, class O>
-cudaError_t by_shape(const GemmArgs& g, const Work& w, const void* dy, void* out, size_t ldo, int* err, int sms, cudaStream_t s) {
+cudaError_t by_shape(const GemmArgs& g, const Work& w, const Ends& at, int* err, int sms, cudaStream_t s) {
   if constexpr (PARTS == 1) {
-    if (w.plan.bn == 256) return launch<2, 256, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
-    if (w.plan.bn == 128) return launch<1, 128, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+    if (!w.plan.conv) return launch<2, 256, PARTS, false, DW, O>(g, w, at, err, sms, s);
+    if (w.plan.bn == 256) return launch<2, 256, PARTS, true, DW, O>(g, w, at, err, sms, s);
+    if (w.plan.bn == 128) return launch<1, 128, PARTS, true, DW, O>(g, w, at, err, sms, s);
   } else {
-    if (w.plan.bn == 128) return launch<2, 128, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+    if (w.plan.bn == 128) return launch<2, 128, PARTS, true, DW, O>(g, w, at, err, sms, s);
   }
-  return launch<1, 64, PARTS, DW, O>(g, w, dy, out, ldo, err, sms, s);
+  return launch<1, 64, PARTS, true, DW, O>(g, w, at, err, sms, s);
 }
 
 template <bool DW>
@@ -459,24 +524,33 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   const Work w = work_of(g, DW, sms);
   const uint64_t m = DW ? g.n : g.t;
   const bool f32 = g.out_dtype == STQ_GRAD_F32, split = w.plan.splits > 1;
-  const void* dy = g.dy;
+  uint8_t* base = static_cast<uint8_t*>(ws);
+  float* part = reinterpret_cast<float*>(base + w.pitch_bytes);
+  Ends at = {g.dy, nullptr, split ? part : g.out, split ? w.ldp : g.ldo};
   *launches = 1;
   if (w.pitch) {
-    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(ws);
+    __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base);
     const uint64_t items = g.t * (w.lddy / 8);
     q8_pitch_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(g.dy), g.lddy, g.t, g.n, to, w.lddy);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    dy = to;
+    at.dy = to;
     ++*launches;
   }
-  float* part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.pitch_bytes);
-  void* out = split ? part : g.out;
-  const size_t ldo = split ? w.ldp : g.ldo;
+  if (!w.plan.conv) {
+    __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base + w.pitch_bytes + w.part_bytes);
+    const uint64_t items = (uint64_t)w.plane * ((w.ldb + 15) / 16);
+    q8_convert_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(DW ? g.xq : g.wq, DW ? g.ldx : g.ldw, DW ? g.xs : g.ws,
+                                                                           (uint32_t)(DW ? g.t : g.n), g.k, w.plane, to, w.ldb);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    at.operand = to;
+    ++*launches;
+  }
   // (an fp32 result takes the operand in three parts; partial results of a bf16 one are fp32 sums of the single operand)
-  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, dy, out, ldo, err, sms, stream)
-                  : split ? by_shape<1, DW, float>(g, w, dy, out, ldo, err, sms, stream)
-                          : by_shape<1, DW, __nv_bfloat16>(g, w, dy, out, ldo, err, sms, stream);
+  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, at, err, sms, stream)
+                  : split ? by_shape<1, DW, float>(g, w, at, err, sms, stream)
+                          : by_shape<1, DW, __nv_bfloat16>(g, w, at, err, sms, stream);
   if (e != cudaSuccess || !split) return e;
   const uint64_t items = m * (w.ldp / 4);
   const unsigned grid = (unsigned)((items + 255) / 256);
@@ -494,7 +568,7 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
 
 size_t q8_grad_workspace(const GemmArgs& g, bool dw, int sms) {
   const Work w = work_of(g, dw, sms);
-  return w.pitch_bytes + w.part_bytes;
+  return w.pitch_bytes + w.part_bytes + w.conv_bytes;
 }
 cudaError_t launch_q8_linear_dx(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t stream, int* launches) {
   return grad<false>(g, ws, sms, err, stream, launches);

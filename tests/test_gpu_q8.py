@@ -326,6 +326,27 @@ def test_linear_backward(handle, t, n, k):
         assert torch.allclose(db, q8.bias_grad(handle, dys), rtol=0, atol=float(64 * U * dy.double().abs().sum(0).max()))
 
 
+@pytest.mark.parametrize("t,n,k,dtype", [(8200, 1608, 1603, BF), (8200, 1607, 1600, BF), (4100, 1608, 2056, F32), (1601, 8208, 1600, BF)])
+def test_linear_backward_of_a_batch(handle, t, n, k, dtype):
+    """Large results: for a bf16 one the 8-bit operand is converted ahead of the product, one launch more."""
+    x, w = codes(t, k, 1 + t, 0.05), codes(n, k, 2 + n, 0.002)
+    dy = (1e-3 * torch.randn(t, n, device="cuda", generator=gen(5))).to(BF)
+    rel = UB + 2.0 ** -17 if dtype == BF else 2.0 ** -17
+    before = handle.launch_count
+    dx = q8.linear_dx(handle, dy, w, dtype=dtype)
+    middle = handle.launch_count
+    dw = q8.linear_dw(handle, dy, x, dtype=dtype)
+    assert dtype == F32 or max(middle - before, handle.launch_count - middle) >= 2
+    near(dx, dy.double() @ dec(w), dy.double().abs() @ dec(w).abs() + 1e-300, dtype, rel)
+    near(dw, dy.double().T @ dec(x), dy.double().abs().T @ dec(x).abs() + 1e-300, dtype, rel)
+    w.scale[n - 1] = float("nan")
+    w.q[n - 1] = 0
+    assert torch.isnan(q8.linear_dx(handle, dy, w, dtype=dtype)).all()
+    x.scale[t - 1] = float("nan")
+    x.q[t - 1] = 0
+    assert torch.isnan(q8.linear_dw(handle, dy, x, dtype=dtype)).all()
+
+
 @pytest.mark.parametrize("t", [1, 5, 130])
 def test_linear_longest_sum_of_largest_codes(handle, t):
     """127^2 * 131072 fits 32 bits: no sum wraps or saturates."""

@@ -42,14 +42,14 @@ struct NormBwdArgs {
   const float* weight;
   const float* rstd;
   float* dweight;
-  float* partial;        // [groups][cols]
+  float* partial;        // [q8_norm_bwd_rows()][cols]
   uint64_t rows;
   uint32_t cols;
 };
-// Row groups of the backward pass (its partial sums of dweight need that many rows of `cols` floats).
+// Rows of `cols` floats that the backward pass needs for its partial sums of dweight.
 constexpr uint32_t kNormBwdMaxCols = 49152;   // widest row: the sums of the widest variant stay in shared memory
-uint32_t q8_norm_bwd_groups(uint64_t rows, uint32_t cols, int sms);
-cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, uint32_t groups, cudaStream_t stream);
+uint32_t q8_norm_bwd_rows(int dtype, const NormBwdArgs& a, int sms);
+cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream);
 
 struct ActBwdArgs {
   Mat da, dz;

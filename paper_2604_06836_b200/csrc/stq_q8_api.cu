@@ -162,9 +162,8 @@ int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const voi
   a.dx = {dx, lddx};
   a.weight = weight; a.rstd = rstd; a.dweight = dweight;
   a.rows = rows; a.cols = cols;
-  const uint32_t groups = stq::q8_norm_bwd_groups(rows, cols, h->sm_count);
-  STQ_TRY(workspace(h, (size_t)groups * cols, &a.partial));
-  STQ_CUDA(h, stq::launch_q8_norm_bwd(dtype, a, groups, s));
+  STQ_TRY(workspace(h, (size_t)stq::q8_norm_bwd_rows(dtype, a, h->sm_count) * cols, &a.partial));
+  STQ_CUDA(h, stq::launch_q8_norm_bwd(dtype, a, h->sm_count, s));
   h->launches += 2;
   return STQ_OK;
 }

@@ -29,136 +29,178 @@ __device__ __forceinline__ uint32_t col_of(uint32_t base, int lane, int e) {
   return base + (e / VEC) * 32 * VEC + lane * VEC + e % VEC;
 }
 
-__device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi) {
-  lo = __uint_as_float(w << 16);
-  hi = __uint_as_float(w & 0xffff0000u);
-}
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+__device__ __forceinline__ uint32_t pack2(float2 x) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x.x, x.y);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// the 8 elements of a lane in one unit of a row; columns from `cols` on read as zero and are not touched
+// Pairs of fp32 operations in one instruction.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<uint64_t*>(&r))
+      : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(*reinterpret_cast<uint64_t*>(&r))
+      : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(*reinterpret_cast<uint64_t*>(&r))
+      : "l"(*reinterpret_cast<const uint64_t*>(&a)), "l"(*reinterpret_cast<const uint64_t*>(&b)),
+        "l"(*reinterpret_cast<const uint64_t*>(&c)));
+  return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// The 8 elements of a lane in one unit of a row as they lie in memory, so that the loads of many units can be in flight
+// in few registers; columns from `cols` on read as zero and are not touched.
 template <class T, int VEC>
-__device__ __forceinline__ void load_unit(const T* row, uint32_t base, int lane, uint32_t cols, float (&v)[8]) {
-  if constexpr (VEC == 8) {
-    const uint32_t c = base + lane * 8;
-    if (c < cols) {
-      if constexpr (sizeof(T) == 2) {
-        const uint4 w = *reinterpret_cast<const uint4*>(row + c);
-        unpack2(w.x, v[0], v[1]); unpack2(w.y, v[2], v[3]); unpack2(w.z, v[4], v[5]); unpack2(w.w, v[6], v[7]);
-      } else {
-        const float4 a = *reinterpret_cast<const float4*>(row + c), b = *reinterpret_cast<const float4*>(row + c + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+struct Raw {
+  static constexpr int kWords = VEC == 1 ? 8 : 2 * (int)sizeof(T);   // (single elements take a register each)
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T* row, uint32_t base, int lane, uint32_t cols) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = 0u;
+    if constexpr (VEC == 8) {
+      const uint32_t c = base + lane * 8;
+      if (c < cols) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) {
+          const uint4 v = reinterpret_cast<const uint4*>(row + c)[i / 4];
+          w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+        }
+      }
+    } else if constexpr (VEC == 2) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t c = col_of<VEC>(base, lane, 2 * p);
+        if (c < cols) {
+          if constexpr (sizeof(T) == 2) {
+            w[p] = *reinterpret_cast<const uint32_t*>(row + c);
+          } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(row + c);
+            w[2 * p] = v.x; w[2 * p + 1] = v.y;
+          }
+        }
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.f;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; e += VEC) {
-      const uint32_t c = col_of<VEC>(base, lane, e);
-      if (c < cols) {
-        if constexpr (VEC == 2) {
-          if constexpr (sizeof(T) == 2) {
-            unpack2(*reinterpret_cast<const uint32_t*>(row + c), v[e], v[e + 1]);
-          } else {
-            const float2 a = *reinterpret_cast<const float2*>(row + c);
-            v[e] = a.x; v[e + 1] = a.y;
-          }
-        } else {
-          v[e] = static_cast<float>(row[c]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[e + i] = 0.f;
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t c = col_of<VEC>(base, lane, e);
+        if (c < cols) w[e] = sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[c] << 16
+                                            : reinterpret_cast<const uint32_t*>(row)[c];
       }
     }
   }
+  __device__ __forceinline__ float2 pair(int p) const {      // elements 2p, 2p + 1
+    if constexpr (sizeof(T) == 2 && VEC != 1) return make_float2(__uint_as_float(w[p] << 16), __uint_as_float(w[p] & 0xffff0000u));
+    return make_float2(__uint_as_float(w[2 * p % kWords]), __uint_as_float(w[(2 * p + 1) % kWords]));
+  }
+};
+
+template <class T, int VEC>
+__device__ __forceinline__ void load_unit(const T* row, uint32_t base, int lane, uint32_t cols, float2 (&v)[4]) {
+  Raw<T, VEC> r;
+  r.load(row, base, lane, cols);
+#pragma unroll
+  for (int p = 0; p < 4; ++p) v[p] = r.pair(p);
 }
 
 template <class T, int VEC>
-__device__ __forceinline__ void store_unit(T* row, uint32_t base, int lane, uint32_t cols, const float (&v)[8]) {
+__device__ __forceinline__ void store_unit(T* row, uint32_t base, int lane, uint32_t cols, const float2 (&v)[4]) {
   if constexpr (VEC == 8) {
     const uint32_t c = base + lane * 8;
     if (c >= cols) return;
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(row + c) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+      *reinterpret_cast<uint4*>(row + c) = make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3]));
     } else {
-      *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      *reinterpret_cast<float4*>(row + c) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+      *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; e += VEC) {
-      const uint32_t c = col_of<VEC>(base, lane, e);
-      if (c >= cols) continue;
+    for (int p = 0; p < 4; ++p) {
+      const uint32_t c = col_of<VEC>(base, lane, 2 * p);
       if constexpr (VEC == 2) {
+        if (c >= cols) continue;
         if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<uint32_t*>(row + c) = pack2(v[e], v[e + 1]);
+          *reinterpret_cast<uint32_t*>(row + c) = pack2(v[p]);
         else
-          *reinterpret_cast<float2*>(row + c) = make_float2(v[e], v[e + 1]);
+          *reinterpret_cast<float2*>(row + c) = v[p];
       } else {
-        row[c] = static_cast<T>(v[e]);
+        const uint32_t d = col_of<VEC>(base, lane, 2 * p + 1);
+        if (c < cols) row[c] = static_cast<T>(v[p].x);
+        if (d < cols) row[d] = static_cast<T>(v[p].y);
       }
     }
   }
 }
 
-// the codes of a lane's 8 elements, each the low byte of a word
+// the codes of a lane's 8 elements, four to a word
 template <int VEC>
-__device__ __forceinline__ void store_codes(int8_t* row, uint32_t base, int lane, uint32_t cols, const uint32_t (&k)[8]) {
+__device__ __forceinline__ void store_codes(int8_t* row, uint32_t base, int lane, uint32_t cols, const uint32_t (&k)[2]) {
   if constexpr (VEC == 8) {
     const uint32_t c = base + lane * 8;
-    if (c >= cols) return;
-    uint2 w;
-    w.x = __byte_perm(__byte_perm(k[0], k[1], 0x0040), __byte_perm(k[2], k[3], 0x0040), 0x5410);
-    w.y = __byte_perm(__byte_perm(k[4], k[5], 0x0040), __byte_perm(k[6], k[7], 0x0040), 0x5410);
-    *reinterpret_cast<uint2*>(row + c) = w;
+    if (c < cols) *reinterpret_cast<uint2*>(row + c) = make_uint2(k[0], k[1]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; e += VEC) {
-      const uint32_t c = col_of<VEC>(base, lane, e);
+      const uint32_t c = col_of<VEC>(base, lane, e), w = k[e / 4] >> (8 * (e & 3));
       if (c >= cols) continue;
       if constexpr (VEC == 2)
-        *reinterpret_cast<uint16_t*>(row + c) = (uint16_t)__byte_perm(k[e], k[e + 1], 0x0040);
+        *reinterpret_cast<uint16_t*>(row + c) = (uint16_t)w;
       else
-        row[c] = (int8_t)k[e];
+        row[c] = (int8_t)w;
     }
   }
 }
 
-// the 8 codes of a lane as numbers
+// the codes of a lane's 8 elements, four to a word, 128 added to each
 template <int VEC>
-__device__ __forceinline__ void load_codes(const int8_t* row, uint32_t base, int lane, uint32_t cols, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = 0.f;
+__device__ __forceinline__ void load_codes(const int8_t* row, uint32_t base, int lane, uint32_t cols, uint32_t (&k)[2]) {
+  k[0] = k[1] = 0u;
   if constexpr (VEC == 8) {
     const uint32_t c = base + lane * 8;
-    if (c >= cols) return;
-    const uint2 w = *reinterpret_cast<const uint2*>(row + c);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
+    if (c < cols) {
+      const uint2 w = *reinterpret_cast<const uint2*>(row + c);
+      k[0] = w.x; k[1] = w.y;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; e += VEC) {
       const uint32_t c = col_of<VEC>(base, lane, e);
       if (c >= cols) continue;
-      if constexpr (VEC == 2) {
-        const uint16_t w = *reinterpret_cast<const uint16_t*>(row + c);
-        v[e] = (float)(int8_t)w;
-        v[e + 1] = (float)(int8_t)(w >> 8);
-      } else {
-        v[e] = (float)row[c];
-      }
+      const uint32_t w = VEC == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(row + c) : (uint32_t)(uint8_t)row[c];
+      k[e / 4] |= w << (8 * (e & 3));
     }
   }
+  k[0] ^= 0x80808080u;
+  k[1] ^= 0x80808080u;
+}
+// elements 2p, 2p + 1 of such codes as numbers: a byte under the exponent of 2^23 is 2^23 + byte
+__device__ __forceinline__ float2 code_pair(const uint32_t (&k)[2], int p) {
+  const uint32_t w = k[p / 2];
+  const int i = (p & 1) * 2;
+  return add2(make_float2(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650 + i)),
+                          __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7651 + i))),
+              both(-8388736.f));
 }
 
 // Largest magnitudes travel as the bit patterns of |x|: they order like the numbers, infinity is above every
 // number and NaN above infinity, so one unsigned maximum also finds what must not be stored as a code.
-__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float max_abs(float m, float2 x) {      // max(m, |x.x|, |x.y|), NaN if one is
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(x.x), "f"(x.y));
+  return r;
+}
+__device__ __forceinline__ uint32_t bits_of(float m) { return __float_as_uint(m) & 0x7fffffffu; }
 
 // How a row or block with largest magnitude `top` is coded: q = rne(x * inv) & mask, value q * scale.  (inv is
 // formed like that of the first moment's codes: 127 * fl(1/top).)
@@ -171,29 +213,59 @@ __device__ __forceinline__ Coding coding_of(uint32_t top) {
   Coding c;
   c.mask = 0xffffffffu;
   c.inv = 127.f * (1.f / a);
-  c.scale = a / 127.f;
+  c.scale = a * (1.f / 127.f);
   if (a < kTinyScale) { c.inv = 0.f; c.scale = 0.f; }
   // something in the row is not finite: no code can say so, the scale does
   if (top >= 0x7f800000u) { c.inv = 0.f; c.scale = __uint_as_float(0x7fc00000u); c.mask = 0u; }
   return c;
 }
 // Round to nearest even by the addition of 1.5 * 2^23: the low byte of the sum is the two's complement code
-// (|x * inv| <= 127 up to a rounding).
-__device__ __forceinline__ uint32_t code_of(float x, const Coding& c) {
-  return __float_as_uint(__fadd_rn(__fmul_rn(x, c.inv), 12582912.f)) & c.mask;
+// (|x * inv| <= 127 up to a rounding), and the sum less 1.5 * 2^23 is the code as a number.
+constexpr float kRound = 12582912.f;
+__device__ __forceinline__ float2 rounded(float2 x, float inv) { return add2(mul2(x, both(inv)), both(kRound)); }
+__device__ __forceinline__ uint32_t codes4(float2 a, float2 b, uint32_t mask) {
+  return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
+                     __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410) & mask;
 }
-__device__ __forceinline__ float value_of(uint32_t code, const Coding& c) { return (float)(int8_t)code * c.scale; }
+// A unit of a row as codes and, if asked for, as the bf16 values that these stand for.
+template <int VEC>
+__device__ __forceinline__ void write_unit(const RowArgs& a, uint64_t row, uint32_t base, int lane, const float2 (&x)[4],
+                                           const Coding& c) {
+  float2 t[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) t[p] = rounded(x[p], c.inv);
+  const uint32_t k[2] = {codes4(t[0], t[1], c.mask), codes4(t[2], t[3], c.mask)};
+  store_codes<VEC>(a.q + row * a.ldq, base, lane, a.cols, k);
+  if (a.values.p) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) t[p] = mul2(add2(t[p], both(-kRound)), both(c.scale));
+    store_unit<__nv_bfloat16, VEC>(static_cast<__nv_bfloat16*>(a.values.p) + row * a.values.ld, base, lane, a.cols, t);
+  }
+}
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// 1 / (1 + exp(-x)): the special-function unit's exponential and reciprocal, 2^-22 each; an exponential that overflows
+// gives 0.
+__device__ __forceinline__ float2 sigmoid2(float2 x) {
+  float2 t = mul2(x, both(-1.4426950408889634f)), r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(t.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(t.y));
+  t = add2(t, both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(t.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(t.y));
+  return r;
+}
 constexpr float kGeluA = 1.5957691216057308f;             // 2 sqrt(2/pi): gelu(x) = x sigmoid(kGeluA (x + 0.044715 x^3))
 constexpr float kGeluB = 0.044715f;
+
+// Most warps that share a row, by the units that each of them keeps.
+__host__ __device__ constexpr int most_warps(int ns) { return ns == 1 ? 32 : 16; }
 
 // ---- activation (or plain rows) -> 8-bit rows, and the input into a checkpoint ----------------------------------
 // One row per CTA of `warps` warps, or, with one warp per row, four rows per CTA.  A lane keeps NS units' results
 // in registers between the row's maximum and the writing; rows of more than NS * warps units are read a second
 // time (the checkpoint is written in the first pass).
 template <class T, int VEC, int NS, int KIND>
-__global__ void __launch_bounds__(1024) q8_act_kernel(const RowArgs a, int warps) {
+__global__ void __launch_bounds__(most_warps(NS) * 32) q8_act_kernel(const RowArgs a, int warps) {
   __shared__ uint32_t sh[32];
   const int lane = threadIdx.x & 31;
   const int warp = warps == 1 ? 0 : threadIdx.x >> 5;
@@ -203,63 +275,70 @@ __global__ void __launch_bounds__(1024) q8_act_kernel(const RowArgs a, int warps
   const T* x = static_cast<const T*>(a.x.p) + row * a.x.ld;
   constexpr int kParts = KIND == kQ8SiluGated ? 2 : 1;
   const uint32_t blocks = (cols + kQ8Block - 1) / kQ8Block;
+  int8_t* ckq = a.ckq + row * kParts * a.ldck;
+  float* cks = a.cks + row * kParts * blocks;
 
   // NS units from `base` on: the results, and on the first pass the checkpoint of what they came from
-  auto produce = [&](uint32_t base, float (&r)[NS][8], bool keep) {
-    float in[kParts][NS][8];
+  auto produce = [&](uint32_t base, float2 (&r)[NS][4], bool keep) {
+    Raw<T, VEC> raw[NS][kParts];
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int p = 0; p < kParts; ++p) load_unit<T, VEC>(x + (size_t)p * cols, base + s * step, lane, cols, in[p][s]);
+      for (int p = 0; p < kParts; ++p) raw[s][p].load(x + (size_t)p * cols, base + s * step, lane, cols);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
+      const uint32_t b = base + s * step;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float g = in[0][s][e];
-        if constexpr (KIND == kQ8Copy) r[s][e] = g;
-        if constexpr (KIND == kQ8SiluGated) r[s][e] = g * sigmoid(g) * in[1][s][e];
-        if constexpr (KIND == kQ8Gelu) r[s][e] = g * sigmoid(kGeluA * (g + kGeluB * g * g * g));
+      for (int i = 0; i < 4; ++i) {
+        const float2 g = raw[s][0].pair(i);
+        if constexpr (KIND == kQ8Copy) r[s][i] = g;
+        if constexpr (KIND == kQ8SiluGated) r[s][i] = mul2(mul2(g, sigmoid2(g)), raw[s][kParts - 1].pair(i));
+        if constexpr (KIND == kQ8Gelu) {
+          const float2 u = mul2(both(kGeluA), mul2(g, fma2(mul2(both(kGeluB), g), g, both(1.f))));
+          r[s][i] = mul2(g, sigmoid2(u));
+        }
       }
       if (KIND != kQ8Copy && keep) {
-        const uint32_t b = base + s * step;
+        // VEC 8: lanes 0-15 and 16-31 hold a block each (per part); otherwise pairs 0-1 and 2-3 do
+        uint32_t t0[kParts], t1[kParts];
 #pragma unroll
         for (int p = 0; p < kParts; ++p) {
-          // VEC 8: lanes 0-15 and 16-31 hold a block each; otherwise registers 0-3 and 4-7 do
-          uint32_t t0 = 0, t1 = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            t0 = max(t0, mag(in[p][s][e]));
-            t1 = max(t1, mag(in[p][s][e + 4]));
-          }
+          t0[p] = bits_of(max_abs(max_abs(0.f, raw[s][p].pair(0)), raw[s][p].pair(1)));
+          t1[p] = bits_of(max_abs(max_abs(0.f, raw[s][p].pair(2)), raw[s][p].pair(3)));
           if constexpr (VEC == 8) {
-            t0 = max(t0, t1);
+            t0[p] = max(t0[p], t1[p]);
 #pragma unroll
-            for (int m = 8; m; m >>= 1) t0 = max(t0, __shfl_xor_sync(kFullMask, t0, m));
-            t1 = t0;
+            for (int m = 8; m; m >>= 1) t0[p] = max(t0[p], __shfl_xor_sync(kFullMask, t0[p], m));
           } else {
-            t0 = __reduce_max_sync(kFullMask, t0);
-            t1 = __reduce_max_sync(kFullMask, t1);
+            t0[p] = __reduce_max_sync(kFullMask, t0[p]);
+            t1[p] = __reduce_max_sync(kFullMask, t1[p]);
           }
-          const Coding c0 = coding_of(t0), c1 = VEC == 8 ? c0 : coding_of(t1);
-          uint32_t k[8];
+        }
+        // The maxima are turned into codings side by side, one to a lane: lane 0 (VEC 8: of each half) that of the
+        // first part, lane 1 of the second; without VEC 8 lanes 2 and 3 the second block's.
+        const int role = lane & (VEC == 8 ? 1 : 3);
+        uint32_t mine = t0[0];
+        if (kParts == 2 && (role & 1)) mine = t0[kParts - 1];
+        if (VEC != 8 && (role & 2)) mine = kParts == 2 && (role & 1) ? t1[kParts - 1] : t1[0];
+        const Coding own = coding_of(mine);
+        const uint32_t blk = b / kQ8Block + (VEC == 8 ? lane >> 4 : lane >> 1);
+        if ((VEC == 8 ? (lane & 15) < kParts : lane < 4 && (lane & 1) < kParts) && blk < blocks) cks[(lane & 1) * blocks + blk] = own.scale;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) k[e] = code_of(in[p][s][e], e < 4 ? c0 : c1);
-          const size_t at = row * kParts + p;
-          store_codes<VEC>(a.ckq + at * a.ldck, b, lane, cols, k);
-          const uint32_t blk = b / kQ8Block;
-          if constexpr (VEC == 8) {
-            if ((lane & 15) == 0 && blk + (lane >> 4) < blocks) a.cks[at * blocks + blk + (lane >> 4)] = c0.scale;
-          } else {
-            if (lane == 0 && blk < blocks) a.cks[at * blocks + blk] = c0.scale;
-            if (lane == 1 && blk + 1 < blocks) a.cks[at * blocks + blk + 1] = c1.scale;
-          }
+        for (int p = 0; p < kParts; ++p) {
+          const int from = VEC == 8 ? (lane & 16) + p : p;
+          const float inv0 = __shfl_sync(kFullMask, own.inv, from);
+          const float inv1 = VEC == 8 ? inv0 : __shfl_sync(kFullMask, own.inv, from + 2);
+          const uint32_t m0 = t0[p] < 0x7f800000u ? 0xffffffffu : 0u, m1 = VEC == 8 || t1[p] < 0x7f800000u ? 0xffffffffu : 0u;
+          const uint32_t k[2] = {codes4(rounded(raw[s][p].pair(0), inv0), rounded(raw[s][p].pair(1), inv0), m0),
+                                 codes4(rounded(raw[s][p].pair(2), inv1), rounded(raw[s][p].pair(3), inv1), VEC == 8 ? m0 : m1)};
+          store_codes<VEC>(ckq + p * a.ldck, b, lane, cols, k);
         }
       }
     }
   };
 
-  float r[NS][8];
-  uint32_t top = 0;
+  float2 r[NS][4];
+  float most = 0.f;
   const uint32_t first = warp * kUnit, span = step * NS;
   const bool once = cols <= span;
   for (uint32_t at = 0; at < cols; at += span) {
@@ -267,9 +346,9 @@ __global__ void __launch_bounds__(1024) q8_act_kernel(const RowArgs a, int warps
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, mag(r[s][e]));
+      for (int i = 0; i < 4; ++i) most = max_abs(most, r[s][i]);
   }
-  top = __reduce_max_sync(kFullMask, top);
+  uint32_t top = __reduce_max_sync(kFullMask, bits_of(most));
   if (warps > 1) {
     if (lane == 0) sh[warp] = top;
     __syncthreads();
@@ -280,19 +359,7 @@ __global__ void __launch_bounds__(1024) q8_act_kernel(const RowArgs a, int warps
   for (uint32_t at = 0; at < cols; at += span) {
     if (!once) produce(at + first, r, false);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const uint32_t b = at + first + s * step;
-      uint32_t k[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) k[e] = code_of(r[s][e], c);
-      store_codes<VEC>(a.q + row * a.ldq, b, lane, cols, k);
-      if (a.values.p) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = value_of(k[e], c);
-        store_unit<__nv_bfloat16, VEC>(static_cast<__nv_bfloat16*>(a.values.p) + row * a.values.ld, b, lane, cols, v);
-      }
-    }
+    for (int s = 0; s < NS; ++s) write_unit<VEC>(a, row, at + first + s * step, lane, r[s], c);
   }
 }
 
@@ -300,7 +367,7 @@ __global__ void __launch_bounds__(1024) q8_act_kernel(const RowArgs a, int warps
 // y = h * rstd * w with one rstd per row, so the codes of y are the codes of h * w (rstd cancels in x / max|x|) and
 // the row needs ONE reduction for both the sum of squares and the maximum.
 template <class T, int VEC, int NS>
-__global__ void __launch_bounds__(1024) q8_norm_kernel(const RowArgs a, int warps) {
+__global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowArgs a, int warps) {
   __shared__ uint32_t sh_top[32];
   __shared__ float sh_sum[32];
   const int lane = threadIdx.x & 31;
@@ -312,45 +379,43 @@ __global__ void __launch_bounds__(1024) q8_norm_kernel(const RowArgs a, int warp
   const T* res = a.res.p ? static_cast<const T*>(a.res.p) + row * a.res.ld : nullptr;
 
   // h * w of NS units; on the first pass h is written and its squares are added to `sum`
-  auto produce = [&](uint32_t base, float (&r)[NS][8], float& sum, bool keep) {
-    float w[NS][8];
+  auto produce = [&](uint32_t base, float2 (&r)[NS][4], float2& sum, bool keep) {
+    Raw<T, VEC> in[NS], other[NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) load_unit<T, VEC>(x, base + s * step, lane, cols, r[s]);
+    for (int s = 0; s < NS; ++s) in[s].load(x, base + s * step, lane, cols);
     if (res) {
-      float o[NS][8];
 #pragma unroll
-      for (int s = 0; s < NS; ++s) load_unit<T, VEC>(res, base + s * step, lane, cols, o[s]);
-#pragma unroll
-      for (int s = 0; s < NS; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[s][e] += o[s][e];
+      for (int s = 0; s < NS; ++s) other[s].load(res, base + s * step, lane, cols);
     }
 #pragma unroll
-    for (int s = 0; s < NS; ++s) load_unit<float, VEC>(a.weight, base + s * step, lane, cols, w[s]);
-#pragma unroll
     for (int s = 0; s < NS; ++s) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[s][i] = res ? add2(in[s].pair(i), other[s].pair(i)) : in[s].pair(i);
       if (keep && res)
         store_unit<T, VEC>(static_cast<T*>(a.h.p) + row * a.h.ld, base + s * step, lane, cols, r[s]);
+      float2 w[4];
+      load_unit<float, VEC>(a.weight, base + s * step, lane, cols, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum = fmaf(r[s][e], r[s][e], sum);
-        r[s][e] *= w[s][e];
+      for (int i = 0; i < 4; ++i) {
+        sum = fma2(r[s][i], r[s][i], sum);
+        r[s][i] = mul2(r[s][i], w[i]);
       }
     }
   };
 
-  float r[NS][8], sum = 0.f, unused = 0.f;
-  uint32_t top = 0;
+  float2 r[NS][4], sums = both(0.f), unused = both(0.f);
+  float most = 0.f;
   const uint32_t first = warp * kUnit, span = step * NS;
   const bool once = cols <= span;
   for (uint32_t at = 0; at < cols; at += span) {
-    produce(at + first, r, sum, true);
+    produce(at + first, r, sums, true);
 #pragma unroll
     for (int s = 0; s < NS; ++s)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, mag(r[s][e]));
+      for (int i = 0; i < 4; ++i) most = max_abs(most, r[s][i]);
   }
-  top = __reduce_max_sync(kFullMask, top);
+  uint32_t top = __reduce_max_sync(kFullMask, bits_of(most));
+  float sum = sums.x + sums.y;
 #pragma unroll
   for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(kFullMask, sum, m);
   if (warps > 1) {
@@ -373,89 +438,118 @@ __global__ void __launch_bounds__(1024) q8_norm_kernel(const RowArgs a, int warp
   for (uint32_t at = 0; at < cols; at += span) {
     if (!once) produce(at + first, r, unused, false);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const uint32_t b = at + first + s * step;
-      uint32_t k[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) k[e] = code_of(r[s][e], c);
-      store_codes<VEC>(a.q + row * a.ldq, b, lane, cols, k);
-      if (a.values.p) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = value_of(k[e], c);
-        store_unit<__nv_bfloat16, VEC>(static_cast<__nv_bfloat16*>(a.values.p) + row * a.values.ld, b, lane, cols, v);
-      }
-    }
+    for (int s = 0; s < NS; ++s) write_unit<VEC>(a, row, at + first + s * step, lane, r[s], c);
   }
 }
 
+constexpr int kBwdWarps = 16;                             // most warps to a row (two rows' operands live in registers)
+
 // ---- backward of the norm -----------------------------------------------------------------------------------------
-// dx = rstd (w dy - xh mean(w dy xh)) + dres with xh = h rstd; dweight = sum over rows of dy xh.  A group of `warps`
-// warps walks rows group, group + groups, ...; a lane's columns stay the same, so its share of dweight stays in
-// registers until the end.  The groups' shares are added in a fixed order by q8_colsum_finish_kernel.
+// dx = rstd (w dy - xh mean(w dy xh)) + dres with xh = h rstd; dweight = sum over rows of dy xh.  A CTA holds `gangs`
+// groups of `warps` warps; a group walks rows group, group + groups, ..., with the next row's loads in flight while a row
+// is summed and written.  A lane's columns stay the same, so its share of dweight stays in registers until the end; then
+// the CTA's groups add theirs up in shared memory, and q8_colsum_finish_kernel adds the CTAs', both in a fixed order.
 template <class T, int VEC, int NS>
-__global__ void __launch_bounds__(1024) q8_norm_bwd_kernel(const NormBwdArgs a, int warps, uint32_t groups) {
-  __shared__ float sh[2][32];
-  const int lane = threadIdx.x & 31;
-  const int warp = warps == 1 ? 0 : threadIdx.x >> 5;
-  const uint32_t group = warps == 1 ? blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
-  if (group >= groups) return;
+__global__ void __launch_bounds__(kBwdWarps * 32) q8_norm_bwd_kernel(const NormBwdArgs a, int warps, int gangs) {
+  extern __shared__ float dwsum[];
+  __shared__ float sh[2][kBwdWarps];
+  const int lane = threadIdx.x & 31, gang = (threadIdx.x >> 5) / warps, warp = (threadIdx.x >> 5) - gang * warps;
+  const uint32_t group = blockIdx.x * gangs + gang, groups = gridDim.x * gangs;
   const uint32_t cols = a.cols, step = kUnit * warps, first = warp * kUnit;
-  float w[NS][8], dw[NS][8];
+  float2 w[NS][4], dw[NS][4];
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
     load_unit<float, VEC>(a.weight, first + s * step, lane, cols, w[s]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[s][e] = 0.f;
+    for (int i = 0; i < 4; ++i) dw[s][i] = both(0.f);
   }
   const float inv_n = 1.f / (float)cols;
-  int flip = 0;
-  for (uint64_t row = group; row < a.rows; row += groups, flip ^= 1) {
-    const T* dy = static_cast<const T*>(a.dy.p) + row * a.dy.ld;
-    const T* h = static_cast<const T*>(a.h.p) + row * a.h.ld;
-    const float rstd = a.rstd[row];
-    float g[NS][8], xh[NS][8], o[NS][8], dot = 0.f;
+  const T* dy = static_cast<const T*>(a.dy.p) + group * a.dy.ld;
+  const T* h = static_cast<const T*>(a.h.p) + group * a.h.ld;
+  const T* dres = a.dres.p ? static_cast<const T*>(a.dres.p) + group * a.dres.ld : nullptr;
+  T* dx = static_cast<T*>(a.dx.p) + group * a.dx.ld;
+  Raw<T, VEC> rg[NS], rh[NS], ro[NS];
+  float rstd = 0.f;
+  auto fetch = [&](uint64_t row) {
+    rstd = a.rstd[row];
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      load_unit<T, VEC>(dy, first + s * step, lane, cols, g[s]);
-      load_unit<T, VEC>(h, first + s * step, lane, cols, xh[s]);
-      if (a.dres.p)
-        load_unit<T, VEC>(static_cast<const T*>(a.dres.p) + row * a.dres.ld, first + s * step, lane, cols, o[s]);
+      rg[s].load(dy, first + s * step, lane, cols);
+      rh[s].load(h, first + s * step, lane, cols);
+      if (dres) ro[s].load(dres, first + s * step, lane, cols);
     }
+    dy += (size_t)groups * a.dy.ld;
+    h += (size_t)groups * a.h.ld;
+    if (dres) dres += (size_t)groups * a.dres.ld;
+  };
+  if (group < a.rows) fetch(group);
+  int flip = 0;
+  for (uint64_t row = group; row < a.rows; row += groups, flip ^= 1, dx += (size_t)groups * a.dx.ld) {
+    const float rs = rstd;
+    float2 g[NS][4], xh[NS][4], dots = both(0.f);
+    Raw<T, VEC> o[NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s)
+    for (int s = 0; s < NS; ++s) {
+      if (a.dres.p) o[s] = ro[s];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        xh[s][e] *= rstd;
-        dw[s][e] = fmaf(g[s][e], xh[s][e], dw[s][e]);
-        g[s][e] *= w[s][e];
-        dot = fmaf(g[s][e], xh[s][e], dot);
+      for (int i = 0; i < 4; ++i) {
+        const float2 y = rg[s].pair(i);
+        xh[s][i] = mul2(rh[s].pair(i), both(rs));
+        dw[s][i] = fma2(y, xh[s][i], dw[s][i]);
+        g[s][i] = mul2(y, w[s][i]);
+        dots = fma2(g[s][i], xh[s][i], dots);
       }
+    }
+    if (row + groups < a.rows) fetch(row + groups);      // (in flight while this row is summed and written)
+    float dot = dots.x + dots.y;
 #pragma unroll
     for (int m = 16; m; m >>= 1) dot += __shfl_xor_sync(kFullMask, dot, m);
     if (warps > 1) {   // two buffers: a warp reaches the next row's store only after all have passed this row's barrier
-      if (lane == 0) sh[flip][warp] = dot;
-      __syncthreads();
-      dot = lane < warps ? sh[flip][lane] : 0.f;
+      if (lane == 0) sh[flip][gang * warps + warp] = dot;
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + gang), "r"(warps * 32) : "memory");
+      dot = lane < warps ? sh[flip][gang * warps + lane] : 0.f;
 #pragma unroll
       for (int m = 16; m; m >>= 1) dot += __shfl_xor_sync(kFullMask, dot, m);
     }
-    const float c = dot * inv_n;
-    T* dx = static_cast<T*>(a.dx.p) + row * a.dx.ld;
+    const float2 c = both(-dot * inv_n);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      float v[8];
+      float2 v[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = rstd * fmaf(-xh[s][e], c, g[s][e]);
-        if (a.dres.p) v[e] += o[s][e];
+      for (int i = 0; i < 4; ++i) {
+        v[i] = mul2(both(rs), fma2(xh[s][i], c, g[s][i]));
+        if (a.dres.p) v[i] = add2(v[i], o[s].pair(i));
       }
       store_unit<T, VEC>(dx, first + s * step, lane, cols, v);
     }
   }
+  for (int g = 0; g < gangs - 1; ++g) {
+    if (gang == g) {
 #pragma unroll
-  for (int s = 0; s < NS; ++s)
-    store_unit<float, VEC>(a.partial + (size_t)group * cols, first + s * step, lane, cols, dw[s]);
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = ((s * warps + warp) * 32 + lane) * 2 + i * 64 * NS * warps;
+          if (g > 0) dw[s][i] = add2(dw[s][i], make_float2(dwsum[at], dwsum[at + 1]));
+          dwsum[at] = dw[s][i].x;
+          dwsum[at + 1] = dw[s][i].y;
+        }
+    }
+    __syncthreads();
+  }
+  if (gang == gangs - 1) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      if (gangs > 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = ((s * warps + warp) * 32 + lane) * 2 + i * 64 * NS * warps;
+          dw[s][i] = add2(dw[s][i], make_float2(dwsum[at], dwsum[at + 1]));
+        }
+      }
+      store_unit<float, VEC>(a.partial + (size_t)blockIdx.x * cols, first + s * step, lane, cols, dw[s]);
+    }
+  }
 }
 
 // The same for rows that do not fit in registers: a row is read twice (the second time from L2) and the sums of
@@ -473,20 +567,22 @@ __global__ void __launch_bounds__(1024) q8_norm_bwd_wide_kernel(const NormBwdArg
     const T* dy = static_cast<const T*>(a.dy.p) + row * a.dy.ld;
     const T* h = static_cast<const T*>(a.h.p) + row * a.h.ld;
     const float rstd = a.rstd[row];
-    float dot = 0.f;
+    float2 dots = both(0.f);
     for (uint32_t b = warp * kUnit; b < cols; b += step) {
-      float g[8], xh[8], w[8];
+      float2 g[4], xh[4], w[4];
       load_unit<T, VEC>(dy, b, lane, cols, g);
       load_unit<T, VEC>(h, b, lane, cols, xh);
       load_unit<float, VEC>(a.weight, b, lane, cols, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t c = col_of<VEC>(b, lane, e);
-        const float p = g[e] * (xh[e] * rstd);
-        if (c < cols) dwsum[c] += p;
-        dot = fmaf(p, w[e], dot);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t c = col_of<VEC>(b, lane, 2 * i), d = col_of<VEC>(b, lane, 2 * i + 1);
+        const float2 p = mul2(g[i], mul2(xh[i], both(rstd)));
+        if (c < cols) dwsum[c] += p.x;
+        if (d < cols) dwsum[d] += p.y;
+        dots = fma2(p, w[i], dots);
       }
     }
+    float dot = dots.x + dots.y;
 #pragma unroll
     for (int m = 16; m; m >>= 1) dot += __shfl_xor_sync(kFullMask, dot, m);
     if (lane == 0) sh[flip][warp] = dot;
@@ -494,18 +590,18 @@ __global__ void __launch_bounds__(1024) q8_norm_bwd_wide_kernel(const NormBwdArg
     dot = lane < warps ? sh[flip][lane] : 0.f;
 #pragma unroll
     for (int m = 16; m; m >>= 1) dot += __shfl_xor_sync(kFullMask, dot, m);
-    const float c = dot / (float)cols;
+    const float2 c = both(-dot / (float)cols);
     T* dx = static_cast<T*>(a.dx.p) + row * a.dx.ld;
     for (uint32_t b = warp * kUnit; b < cols; b += step) {
-      float g[8], xh[8], w[8], o[8], v[8];
+      float2 g[4], xh[4], w[4], o[4], v[4];
       load_unit<T, VEC>(dy, b, lane, cols, g);
       load_unit<T, VEC>(h, b, lane, cols, xh);
       load_unit<float, VEC>(a.weight, b, lane, cols, w);
       if (a.dres.p) load_unit<T, VEC>(static_cast<const T*>(a.dres.p) + row * a.dres.ld, b, lane, cols, o);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[e] = rstd * fmaf(-(xh[e] * rstd), c, g[e] * w[e]);
-        if (a.dres.p) v[e] += o[e];
+      for (int i = 0; i < 4; ++i) {
+        v[i] = mul2(both(rstd), fma2(mul2(xh[i], both(rstd)), c, mul2(g[i], w[i])));
+        if (a.dres.p) v[i] = add2(v[i], o[i]);
       }
       store_unit<T, VEC>(dx, b, lane, cols, v);
     }
@@ -522,16 +618,19 @@ __global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, ui
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t base = blockIdx.x * kUnit, split = blockIdx.y;
   const uint64_t per = (rows + splits - 1) / splits, r0 = split * per, r1 = min(r0 + per, rows);
-  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
 #pragma unroll 4
   for (uint64_t r = r0 + warp; r < r1; r += 8) {
-    float v[8];
+    float2 v[4];
     load_unit<T, VEC>(static_cast<const T*>(x.p) + r * x.ld, base, lane, cols, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] += v[e];
+    for (int i = 0; i < 4; ++i) s[i] = add2(s[i], v[i]);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sh[warp][col_of<VEC>(0, lane, e)] = s[e];
+  for (int i = 0; i < 4; ++i) {
+    sh[warp][col_of<VEC>(0, lane, 2 * i)] = s[i].x;
+    sh[warp][col_of<VEC>(0, lane, 2 * i + 1)] = s[i].y;
+  }
   __syncthreads();
   const uint32_t c = base + threadIdx.x;
   float sum = 0.f;
@@ -569,29 +668,35 @@ __global__ void __launch_bounds__(256) q8_act_bwd_kernel(const ActBwdArgs a, uin
   const uint32_t base = (uint32_t)(id - row * units) * kUnit, cols = a.cols, blk = base / kQ8Block;
   const uint32_t blocks = (cols + kQ8Block - 1) / kQ8Block;
   constexpr int kParts = KIND == kQ8SiluGated ? 2 : 1;
-  float da[8], in[kParts][8];
-  load_unit<T, VEC>(static_cast<const T*>(a.da.p) + row * a.da.ld, base, lane, cols, da);
+  Raw<T, VEC> da;
+  da.load(static_cast<const T*>(a.da.p) + row * a.da.ld, base, lane, cols);
+  uint32_t k[kParts][2];
+  float s0[kParts], s1[kParts];
 #pragma unroll
   for (int p = 0; p < kParts; ++p) {
     const size_t at = row * kParts + p;
-    load_codes<VEC>(a.ckq + at * a.ldck, base, lane, cols, in[p]);
+    load_codes<VEC>(a.ckq + at * a.ldck, base, lane, cols, k[p]);
     const float* sc = a.cks + at * blocks + blk;
-    const float s0 = sc[0], s1 = blk + 1 < blocks ? sc[1] : 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) in[p][e] *= (VEC == 8 ? lane < 16 : e < 4) ? s0 : s1;
+    s0[p] = VEC != 8 || lane < 16 ? sc[0] : blk + 1 < blocks ? sc[1] : 0.f;      // (VEC 8: one block to a lane)
+    s1[p] = VEC == 8 ? s0[p] : blk + 1 < blocks ? sc[1] : 0.f;
   }
-  float d0[8], d1[8];
+  float2 d0[4], d1[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float g = in[0][e];
+  for (int i = 0; i < 4; ++i) {
+    const float2 g = mul2(code_pair(k[0], i), both(i < 2 ? s0[0] : s1[0])), y = da.pair(i);
     if constexpr (KIND == kQ8SiluGated) {
-      const float sg = sigmoid(g);
-      d0[e] = da[e] * in[kParts - 1][e] * (sg * fmaf(g, 1.f - sg, 1.f));
-      d1[e] = da[e] * (g * sg);
+      const float2 u = mul2(code_pair(k[kParts - 1], i), both(i < 2 ? s0[kParts - 1] : s1[kParts - 1]));
+      const float2 sg = sigmoid2(g);
+      const float2 t = mul2(y, sg);
+      d1[i] = mul2(t, g);
+      // y u sg (1 + g (1 - sg))
+      d0[i] = mul2(mul2(t, u), fma2(g, fma2(sg, both(-1.f), both(1.f)), both(1.f)));
     } else {
-      const float g2 = g * g;
-      const float sg = sigmoid(kGeluA * fmaf(kGeluB * g2, g, g));
-      d0[e] = da[e] * sg * fmaf(g * (1.f - sg), kGeluA * fmaf(3.f * kGeluB, g2, 1.f), 1.f);
+      const float2 g2 = mul2(g, g), v = mul2(both(kGeluA), mul2(g, fma2(both(kGeluB), g2, both(1.f))));
+      const float2 sg = sigmoid2(v);
+      // y sg (1 + g (1 - sg) kGeluA (1 + 3 kGeluB g^2))
+      const float2 in = mul2(both(kGeluA), fma2(both(3.f * kGeluB), g2, both(1.f)));
+      d0[i] = mul2(mul2(y, sg), fma2(mul2(g, fma2(sg, both(-1.f), both(1.f))), in, both(1.f)));
     }
   }
   T* dz = static_cast<T*>(a.dz.p) + row * a.dz.ld;
@@ -615,15 +720,19 @@ struct Width {
   }
 };
 
-// Warps per row and units per warp of the row kernels (rows of more than 64 units are read twice).
+// Warps per row and units per warp (rows of more units than warps can hold are read twice).  Few rows want many warps
+// to a row (one token of 6400 columns: 3.2 us with one unit to a warp, 3.5 with two).  Many rows want fewer warps that
+// wait for one another: the gated activation on 8192 x 6400 takes 147, 96 and 113 us with 1, 2 and 4 units to a warp,
+// the norm on 8192 x 4096 in bf16 55, 60 and 50 us (with narrower accesses 2 units were best there too).
 struct Shape {
   int warps, ns;
 };
-Shape shape_of(uint32_t cols) {
+Shape shape_of(int ns, uint32_t cols) {
   const uint32_t units = (cols + kUnit - 1) / kUnit;
-  const int ns = units <= 32 ? 1 : 2;
-  const uint32_t w = (units + ns - 1) / ns;
-  return {(int)(w < 32 ? w : 32), ns};
+  if (units == 1) ns = 1;
+  if (units > 32 && ns == 1) ns = 2;
+  const int w = (int)((units + ns - 1) / ns);
+  return {w < most_warps(ns) ? w : most_warps(ns), ns};
 }
 
 template <class F>
@@ -651,7 +760,7 @@ cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, cudaStream_t
   Width w;
   w.add(a.x, elem_bytes(dtype));
   w.add(a.values, 2);
-  const Shape sh = shape_of(a.cols);
+  const Shape sh = shape_of(a.rows < 256 ? 1 : 2, a.cols);
   const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
   const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {
@@ -674,14 +783,22 @@ cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream) {
   if (a.res.p) w.add(a.h, elem_bytes(dtype));
   w.add(a.values, 2);
   w.add(Mat{const_cast<float*>(a.weight), 0}, 4);
-  const Shape sh = shape_of(a.cols);
+  const int vec = w.vec(a.cols);
+  const bool few = a.rows < 1024;
+  const Shape sh = shape_of(dtype == STQ_GRAD_BF16 && vec == 8 ? (few || a.cols <= 2 * kUnit ? 1 : 4) : a.rows < 256 ? 1 : 2, a.cols);
   const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
   const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
-    return by_vec(w.vec(a.cols), [&](auto vec) {
+    if constexpr (sizeof(T) == 2) {
+      if (sh.ns == 4) {
+        q8_norm_kernel<T, 8, 4><<<grid, threads, 0, stream>>>(a, sh.warps);
+        return cudaGetLastError();
+      }
+    }
+    return by_vec(vec, [&](auto v) {
       return by_ns(sh.ns, [&](auto ns) {
-        q8_norm_kernel<T, vec(), ns()><<<grid, threads, 0, stream>>>(a, sh.warps);
+        q8_norm_kernel<T, v(), ns()><<<grid, threads, 0, stream>>>(a, sh.warps);
         return cudaGetLastError();
       });
     });
@@ -689,54 +806,63 @@ cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream) {
 }
 
 namespace {
-constexpr uint32_t kBwdRegCols = 32 * 2 * kUnit;   // widest row whose sums stay in registers (32 warps, 2 units each)
-Shape bwd_shape(uint32_t cols) {
+constexpr uint32_t kBwdRegCols = kBwdWarps * 2 * kUnit;   // widest row that stays in registers (2 units to a warp)
+struct BwdShape {
+  int warps, ns, gangs;
+  uint32_t ctas;             // rows of partial sums
+};
+// CTAs of at least 8 warps, as many as are resident at once with 80 (one unit to a warp) or 128 registers a thread.
+// Two units to a warp are faster where they fit (bf16, 8192 x 4096: 59 -> 47 us, 8192 x 1600: 36 -> 24 us) and slower where
+// they spill, which is with fp32 (4096 x 4096: 46 -> 78 us) and with single elements.
+BwdShape bwd_shape(uint64_t rows, uint32_t cols, int dtype, int vec, int sms) {
+  if (cols > kBwdRegCols) return {0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
   const uint32_t units = (cols + kUnit - 1) / kUnit;
-  const int ns = units <= 8 ? 1 : 2;
-  return {(int)((units + ns - 1) / ns), ns};
-}
-}  // namespace
-
-uint32_t q8_norm_bwd_groups(uint64_t rows, uint32_t cols, int sms) {
-  uint32_t most;
-  if (cols > kBwdRegCols) {
-    most = sms;
-  } else {
-    const Shape sh = bwd_shape(cols);
-    most = (uint32_t)sms * (sh.warps >= 32 ? 1 : 32 / sh.warps);
-  }
-  return (uint32_t)(rows < most ? rows : most);
+  const int ns = units > kBwdWarps || (units > 1 && dtype == STQ_GRAD_BF16 && vec > 1) ? 2 : 1;
+  const int warps = (int)((units + ns - 1) / ns), gangs = warps >= 8 ? 1 : 8 / warps;
+  const int per_sm = (ns == 1 ? 24 : 16) / (warps * gangs);
+  const uint64_t want = (rows + gangs - 1) / gangs, most = (uint64_t)sms * (per_sm < 1 ? 1 : per_sm);
+  return {warps, ns, gangs, (uint32_t)(want < most ? want : most)};
 }
 
-cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, uint32_t groups, cudaStream_t stream) {
+int bwd_vec(int dtype, const NormBwdArgs& a) {
   Width w;
   w.add(a.dy, elem_bytes(dtype));
   w.add(a.h, elem_bytes(dtype));
   w.add(a.dres, elem_bytes(dtype));
   w.add(a.dx, elem_bytes(dtype));
   w.add(Mat{const_cast<float*>(a.weight), 0}, 4);
+  return w.vec(a.cols);
+}
+}  // namespace
+
+uint32_t q8_norm_bwd_rows(int dtype, const NormBwdArgs& a, int sms) {
+  return bwd_shape(a.rows, a.cols, dtype, bwd_vec(dtype, a), sms).ctas;
+}
+
+cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream) {
+  const int width = bwd_vec(dtype, a);
+  const BwdShape sh = bwd_shape(a.rows, a.cols, dtype, width, sms);
   cudaError_t e = by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
-    return by_vec(w.vec(a.cols), [&](auto vec) {
+    return by_vec(width, [&](auto vec) {
       if (a.cols > kBwdRegCols) {
         const int bytes = (int)(a.cols * sizeof(float));
         cudaError_t e2 = cudaFuncSetAttribute(q8_norm_bwd_wide_kernel<T, vec()>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e2 != cudaSuccess) return e2;
-        q8_norm_bwd_wide_kernel<T, vec()><<<groups, 1024, bytes, stream>>>(a, groups);
+        q8_norm_bwd_wide_kernel<T, vec()><<<sh.ctas, 1024, bytes, stream>>>(a, sh.ctas);
         return cudaGetLastError();
       }
-      const Shape sh = bwd_shape(a.cols);
-      const unsigned grid = sh.warps == 1 ? (groups + 3) / 4 : groups;
-      const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
+      const int threads = sh.warps * sh.gangs * 32;
+      const size_t smem = sh.gangs > 1 ? (size_t)sh.warps * sh.ns * kUnit * 4 : 0;      // (at most 8 warps of 2 units then)
       if (sh.ns == 1)
-        q8_norm_bwd_kernel<T, vec(), 1><<<grid, threads, 0, stream>>>(a, sh.warps, groups);
+        q8_norm_bwd_kernel<T, vec(), 1><<<sh.ctas, threads, smem, stream>>>(a, sh.warps, sh.gangs);
       else
-        q8_norm_bwd_kernel<T, vec(), 2><<<grid, threads, 0, stream>>>(a, sh.warps, groups);
+        q8_norm_bwd_kernel<T, vec(), 2><<<sh.ctas, threads, smem, stream>>>(a, sh.warps, sh.gangs);
       return cudaGetLastError();
     });
   });
   if (e != cudaSuccess) return e;
-  q8_colsum_finish_kernel<<<(a.cols + 31) / 32, dim3(32, 32), 0, stream>>>(a.partial, groups, a.cols, a.dweight);
+  q8_colsum_finish_kernel<<<(a.cols + 31) / 32, dim3(32, 32), 0, stream>>>(a.partial, sh.ctas, a.cols, a.dweight);
   return cudaGetLastError();
 }
 

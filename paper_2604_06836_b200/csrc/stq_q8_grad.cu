@@ -116,7 +116,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[4 * kStages + 4];
   __shared__ uint32_t tmem_slot;
-  __shared__ float stage[4][32 * 33];
+  __shared__ __align__(16) uint8_t stage[4][kStageBytes];
   const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
   // per stage: codes have landed (this CTA), gradient has landed and codes are converted (both CTAs, at the leader),
   // stage is free; per accumulator: done, read (both CTAs, at the leader)
@@ -305,16 +305,13 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN;
       O* out = static_cast<O*>(a.out) + sp * a.split_stride + row * a.ldo + col;
       const int rows = row >= a.m ? 0 : (int)min((uint64_t)32, a.m - row);
-#pragma unroll 2
-      for (int c = 0; c < BN; c += 32) {
+      constexpr int kC = 128 / sizeof(O);
+#pragma unroll 1
+      for (int c = 0; c < BN; c += kC) {
         if (col + c >= a.n) break;
-        uint32_t r[32];
-        tmem_load(from + c, r);
-        tmem_load_wait();
-        float v[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-        store_block<O, 32>(out + c, a.ldo, v, rows, (int)min(32u, a.n - col - c), a.align, lane, stage[quad]);
+        float v[kC];
+        load_block(from + c, v);
+        store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
       }
       mma_fence_before();
       __syncwarp();

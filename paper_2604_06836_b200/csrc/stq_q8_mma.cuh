@@ -76,6 +76,9 @@ __device__ __forceinline__ void bar_arrive_leader(uint32_t bar, uint32_t bar0, b
   else
     bar_arrive_peer(bar0);
 }
+// The two halves of that: a CTA may write to another's shared memory once that one has arrived, so once it has started.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ bool elect_one() {
   uint32_t p;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
@@ -120,14 +123,7 @@ __device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
 __device__ __forceinline__ void mma_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void mma_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-// 16 or 32 columns of this warp's 32 lanes
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr));
-}
+// 32 columns of this warp's 32 lanes
 __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
@@ -139,6 +135,17 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
       : "r"(addr));
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+// N columns as they are (accumulators of fp32)
+template <int N>
+__device__ __forceinline__ void load_block(uint32_t addr, float (&v)[N]) {
+  uint32_t r[N / 32][32];
+#pragma unroll
+  for (int i = 0; i < N / 32; ++i) tmem_load(addr + 32 * i, r[i]);
+  tmem_load_wait();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i / 32][i % 32]);
+}
 
 // ---- products -------------------------------------------------------------------------------------------------
 // Shared-memory operand in the 128-byte swizzle.  K-major: rows of 128 bytes, groups of 8 rows 1024 bytes apart
@@ -208,40 +215,67 @@ __device__ __forceinline__ bool all_of_128(bool ok) {
   return r != 0;
 }
 
-// A warp's block of 32 rows x C columns, lane = row, to global memory; `rows` and `cols` of it lie inside the matrix.
-// Rows aligned to 32 or 16 bytes are written by their lanes; others go through shared memory, so that the lanes
-// of a store are neighbours in a row.
-template <class O, int C>
-__device__ __forceinline__ void store_block(O* base, size_t ld, const float (&v)[C], int rows, int cols, int align, int lane,
-                                            float* stage) {
+// A warp's block of 32 rows x 128 bytes, lane = row, to global memory; `rows` x `cols` of it lie inside the matrix.
+// Rows aligned to 32 or 16 bytes are written by their lanes.  Others go through shared memory (kStageBytes a warp): a row
+// is laid down there as far from a 16-byte boundary as it lies in global memory, so that all but its first and last
+// pieces move 16 bytes at a time, eight neighbouring lanes to a row.
+constexpr int kStageRow = 144, kStageBytes = 32 * kStageRow;
+template <class O>
+__device__ __forceinline__ void store_block(O* base, size_t ld, const float (&v)[128 / sizeof(O)], int rows, int cols, int align,
+                                            int lane, uint8_t* stage) {
+  constexpr int C = 128 / sizeof(O), kPiece = 16 / sizeof(O);
   if (align >= 16 && cols == C) {
     if (lane >= rows) return;
-    O* p = base + (size_t)lane * ld;
-    uint32_t w[C * sizeof(O) / 4];
+    uint8_t* p = reinterpret_cast<uint8_t*>(base + (size_t)lane * ld);
+    uint32_t w[32];
 #pragma unroll
-    for (int i = 0; i < (int)(C * sizeof(O) / 4); ++i)
-      w[i] = sizeof(O) == 2 ? bf16_pair(v[2 * i % C], v[(2 * i + 1) % C]) : __float_as_uint(v[i % C]);
+    for (int i = 0; i < 32; ++i) w[i] = sizeof(O) == 2 ? bf16_pair(v[2 * i % C], v[(2 * i + 1) % C]) : __float_as_uint(v[i % C]);
     if (align == 32) {
 #pragma unroll
-      for (int i = 0; i < (int)(C * sizeof(O) / 32); ++i)
-        store32(reinterpret_cast<uint8_t*>(p) + 32 * i,
-                *reinterpret_cast<const uint32_t(*)[8]>(&w[8 * i]));
+      for (int i = 0; i < 4; ++i) store32(p + 32 * i, *reinterpret_cast<const uint32_t(*)[8]>(&w[8 * i]));
     } else {
 #pragma unroll
-      for (int i = 0; i < (int)(C * sizeof(O) / 16); ++i)
-        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(p) + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(p + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
     }
     return;
   }
+  auto off = [&](int r) { return (int)(reinterpret_cast<uintptr_t>(base + (size_t)r * ld) & 15); };
   __syncwarp();
+  {
+    const int mis = off(lane);
+    uint32_t* to = reinterpret_cast<uint32_t*>(stage + lane * kStageRow + (mis & ~3));
+    if constexpr (sizeof(O) == 2) {
+      const bool odd = mis & 2;                                  // (a word holds an odd and the next even column then)
 #pragma unroll
-  for (int i = 0; i < C; ++i) stage[lane * 33 + i] = v[i];
+      for (int i = 0; i < 33; ++i) {
+        const float e0 = i < 32 ? v[2 * i % C] : 0.f, o0 = i < 32 ? v[(2 * i + 1) % C] : 0.f, before = i > 0 ? v[(2 * i - 1) % C] : 0.f;
+        if (i < 32 || odd) to[i] = odd ? bf16_pair(before, e0) : bf16_pair(e0, o0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) to[i] = __float_as_uint(v[i % C]);
+    }
+  }
   __syncwarp();
-  constexpr int kPer = 32 / C;                       // rows per store
-  const int r0 = lane / C, c = lane % C;
-#pragma unroll 8
-  for (int r = 0; r < 32; r += kPer)
-    if (r + r0 < rows && c < cols) base[(size_t)(r + r0) * ld + c] = static_cast<O>(stage[(r + r0) * 33 + c]);
+  if (cols == C) {
+#pragma unroll
+    for (int it = 0; it < 8; ++it) {                             // whole pieces, four rows at a time
+      const int r = it * 4 + lane / 8, mis = off(r), piece = lane % 8 + (mis != 0);
+      if (r < rows && piece < 8)
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(base + (size_t)r * ld) - mis + piece * 16) =
+            *reinterpret_cast<const uint4*>(stage + r * kStageRow + piece * 16);
+    }
+#pragma unroll
+    for (int it = 0; it < kPiece; ++it) {                        // what is left at both ends of a row: a piece's worth
+      const int r = it * (32 / kPiece) + lane / kPiece, k = lane % kPiece, mis = off(r), head = (16 - mis) / (int)sizeof(O);
+      const int e = k < head ? k : C - kPiece + k;
+      if (r < rows && mis != 0) base[(size_t)r * ld + e] = *reinterpret_cast<const O*>(stage + r * kStageRow + mis + e * sizeof(O));
+    }
+  } else {
+    for (int r = 0; r < rows; ++r)
+      for (int e = lane; e < cols; e += 32)
+        base[(size_t)r * ld + e] = *reinterpret_cast<const O*>(stage + r * kStageRow + off(r) + e * sizeof(O));
+  }
 }
 
 }  // namespace stq

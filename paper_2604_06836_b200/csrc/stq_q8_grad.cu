@@ -10,6 +10,11 @@
 // numbers whose sum is exactly that product, and three products are added up: the error is that of fp32 arithmetic.
 // Folding s into G instead would round as much and touch the larger operand.
 //
+// The matrix unit cuts its fp32 sums off instead of rounding them (measured: 2e-8 of the sum a step, always towards zero),
+// which adds up to 5e-6 over a sum of 1300.  For a bf16 result that is nothing; for an fp32 result the small parts go in
+// first, and every kChunk stages the sum is taken out and added, rounded to nearest, to a running sum that the writing
+// warps keep in tensor memory.
+//
 // Two forms.  CONV: the codes are converted inside the product kernel, once per row of tiles of the result.  Otherwise a
 // small kernel writes the converted operand to the workspace first and the product kernel only copies and multiplies;
 // that pays once the result has many rows (plan_of), and only for the single operand: in three parts the products take
@@ -50,7 +55,8 @@ struct GradShape {
   static constexpr int kStage = kA + kQ + kB * PARTS;
   static constexpr int kFit = (204 * 1024) / kStage;
   static constexpr int kStages = kFit < 6 ? kFit : 6;
-  static constexpr int kCols = 2 * BN;
+  static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
+  static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
   static constexpr int kSmem = kStages * kStage + 1024;
 };
 
@@ -195,13 +201,14 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
     if (leader && elect_one()) {
       constexpr uint32_t id = idesc(kIdescBf16, 128 * CG, BN, DW, true);
       uint32_t it = 0, n = 0, tile, k0, k1;
-      for (uint32_t w = unit; ok && w < work; w += units, ++n) {
+      for (uint32_t w = unit; ok && w < work; w += units) {
         share(w, tile, k0, k1);
-        const uint32_t acc = n & 1;
-        if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
-        mma_fence_after();
         for (uint32_t k = k0; k < k1; ++k, ++it) {
-          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = (k - k0) % S::kChunk;
+          if (place == 0) {
+            if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+            mma_fence_after();
+          }
           if (!(ok = bar_wait<CG == 2>(full_g + 8 * s, ph) && (!CONV || bar_wait<CG == 2>(ready + 8 * s, ph)))) break;
           mma_fence_after();
           const uint32_t at = ring + s * S::kStage;
@@ -209,14 +216,17 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           const uint64_t db = operand_desc(at + S::kA + S::kQ, kDepth * 128, 1024);
           constexpr uint32_t kStepA = DW ? (kStepK * 128) >> 4 : (kStepK * 2) >> 4, kStepB = (kStepK * 128) >> 4;
 #pragma unroll
-          for (int j = 0; j < kDepth / kStepK; ++j) {
+          for (int p = PARTS - 1; p >= 0; --p)                  // the smallest part first
 #pragma unroll
-            for (int p = 0; p < PARTS; ++p)
-              mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + p * (S::kB >> 4) + j * kStepB, id, (k - k0 | j | p) != 0);
-          }
+            for (int j = 0; j < kDepth / kStepK; ++j)
+              mma<CG, false>(tmem + acc * BN, da + j * kStepA, db + p * (S::kB >> 4) + j * kStepB, id,
+                             place != 0 || p < PARTS - 1 || j != 0);
           mma_commit<CG>(empty + 8 * s);
+          if (place == S::kChunk - 1 || k + 1 == k1) {
+            mma_commit<CG>(done + 8 * acc);
+            ++n;
+          }
         }
-        if (ok) mma_commit<CG>(done + 8 * acc);
       }
     }
   } else if (CONV && warp < 2 + kGroups * kGroupWarps) {
@@ -295,27 +305,51 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
     const int quad = warp & 3;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
     uint32_t n = 0, tile, k0, k1;
-    for (uint32_t w = unit; ok && w < work; w += units, ++n) {
-      const uint32_t sp = share(w, tile, k0, k1), acc = n & 1;
+    for (uint32_t w = unit; ok && w < work; w += units) {
+      const uint32_t sp = share(w, tile, k0, k1), lanes = (uint32_t)(quad * 32) << 16, running = tmem + lanes + 2 * BN;
       const uint64_t row = (uint64_t)(tile % a.tiles_m) * 128 * CG + 128 * rank + quad * 32;
       const uint32_t col = tile / a.tiles_m * BN;
-      ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-      if (!(ok = all_of_128(ok))) break;       // (the four warps leave together)
-      mma_fence_after();
-      const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN;
       O* out = static_cast<O*>(a.out) + sp * a.split_stride + row * a.ldo + col;
       const int rows = row >= a.m ? 0 : (int)min((uint64_t)32, a.m - row);
       constexpr int kC = 128 / sizeof(O);
+      uint32_t k = k0;
+      do {
+        const uint32_t acc = n & 1, from = tmem + lanes + acc * BN;
+        const bool first = k == k0, last = k1 - k <= (uint32_t)S::kChunk;
+        ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
+        if (!(ok = all_of_128(ok))) break;       // (the four warps leave together)
+        mma_fence_after();
 #pragma unroll 1
-      for (int c = 0; c < BN; c += kC) {
-        if (col + c >= a.n) break;
-        float v[kC];
-        load_block(from + c, v);
-        store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
-      }
-      mma_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+        for (int c = 0; c < BN; c += kC) {
+          if (col + c >= a.n) break;
+          float v[kC];
+          load_block(from + c, v);
+          if constexpr (PARTS == 3) {
+            static_assert(PARTS == 1 || kC == 32, "one block of columns to a load");
+            if (!first) {
+              float old[32];
+              load_block(running + c, old);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], old[i]);
+            }
+            if (!last) {
+              uint32_t r[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
+              tmem_store(running + c, r);
+              continue;
+            }
+          }
+          store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
+        }
+        if (PARTS == 3) tmem_store_wait();
+        mma_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+        ++n;
+        k += S::kChunk;
+        if (last) break;
+      } while (true);
     }
   }
   if (!ok) *a.err = 1;

@@ -221,8 +221,12 @@ __device__ __forceinline__ Coding coding_of(uint32_t top) {
 }
 // Round to nearest even by the addition of 1.5 * 2^23: the low byte of the sum is the two's complement code
 // (|x * inv| <= 127 up to a rounding), and the sum less 1.5 * 2^23 is the code as a number.
+// The product is rounded before the addition: single multiplications, since a packed pair of the two is contracted to a
+// fused one by the assembler (codes then differ where the exact product lies next to a tie).
 constexpr float kRound = 12582912.f;
-__device__ __forceinline__ float2 rounded(float2 x, float inv) { return add2(mul2(x, both(inv)), both(kRound)); }
+__device__ __forceinline__ float2 rounded(float2 x, float inv) {
+  return add2(make_float2(__fmul_rn(x.x, inv), __fmul_rn(x.y, inv)), both(kRound));
+}
 __device__ __forceinline__ uint32_t codes4(float2 a, float2 b, uint32_t mask) {
   return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040),
                      __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410) & mask;

@@ -347,6 +347,21 @@ def test_linear_backward_of_a_batch(handle, t, n, k, dtype):
     assert torch.isnan(q8.linear_dw(handle, dy, x, dtype=dtype)).all()
 
 
+@pytest.mark.parametrize("depth", [1003, 20000])
+def test_fp32_gradients_of_long_sums(handle, depth):
+    """Random signs: the result is far smaller than the terms' sum, and a bias of the sums would show.  At most 16 steps of
+    the matrix unit at full size go into a partial sum before it is added up in fp32, 2^-23 of the partial sum each."""
+    x, w = codes(depth, 300, 1, 0.05), codes(depth, 260, 2, 0.002)
+    dy = (1e-3 * torch.randn(depth, 264, device="cuda", generator=gen(5))).to(BF)
+    dw = q8.linear_dw(handle, dy, x, dtype=F32).double()
+    want = dy.double().T @ dec(x)
+    assert float((dw - want).norm() / want.norm()) <= 16 * 2.0 ** -23
+    dyt = (1e-3 * torch.randn(200, depth, device="cuda", generator=gen(6))).to(BF)
+    dx = q8.linear_dx(handle, dyt, w, dtype=F32).double()
+    want = dyt.double() @ dec(w)
+    assert float((dx - want).norm() / want.norm()) <= 16 * 2.0 ** -23
+
+
 @pytest.mark.parametrize("t", [1, 5, 130])
 def test_linear_longest_sum_of_largest_codes(handle, t):
     """127^2 * 131072 fits 32 bits: no sum wraps or saturates."""

@@ -1,0 +1,114 @@
+"""A feed-forward block that keeps everything it saves in 8 bits, as a torch module over the operators of ``q8``.
+
+    h   = x + residual                         (the residual stream)
+    n   = rmsnorm(h) * weight                  8-bit rows
+    z   = n w_in^T (+ b_in)                    8-bit product
+    a   = silu(z_gate) * z_up   or   gelu(z)   8-bit rows; z itself kept as an 8-bit checkpoint
+    y   = a w_out^T (+ b_out)                  8-bit product
+
+Between the forward and the backward pass the block holds n, a and z in 8 bits (with their scales), the 8-bit weights and
+h, which the stream carries anyway: per token of a gated block D + 3F + 2F/32 bytes next to h, against 2 (D + 3F) in bf16.
+Gradients pass straight through the roundings.  The master weights are fp32 parameters with fp32 gradients, as
+``optim.STQAdamW`` takes them.
+"""
+from __future__ import annotations
+
+import math
+from typing import Optional
+
+import torch
+
+from . import q8, stq
+
+
+class _Block(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, block, x, residual, weight, w_in, b_in, w_out, b_out):
+        hd = block.handle_for(x.device)
+        w8 = block.weights8 or block.quantized()
+        train = any(ctx.needs_input_grad)
+        n = q8.norm(hd, x, weight, residual=residual, eps=block.eps)
+        z = q8.linear(hd, n.rows, w8[0], bias=b_in)
+        a = q8.act(hd, z, block.kind, checkpoint=train)
+        y = q8.linear(hd, a.rows, w8[1], bias=b_out)
+        if train:
+            ctx.block, ctx.plain = block, residual is None
+            ctx.has_bias = b_in is not None, b_out is not None
+            ck = a.checkpoint
+            ctx.meta = ck.cols, ck.kind
+            ctx.save_for_backward(n.h, n.rstd, *n.rows, *a.rows, ck.q, ck.scale, weight, *w8[0], *w8[1])
+        # (an input that is returned as it is would be taken for a view of itself)
+        return y, (n.h.view_as(n.h) if residual is None else n.h)
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        h, rstd, nq, ns, aq, as_, cq, cs, weight, iq, is_, oq, os_ = ctx.saved_tensors
+        hd = ctx.block.handle_for(h.device)
+        dy, dh = dy.contiguous(), dh.contiguous()
+        rows8 = q8.Rows8
+        dw_out = q8.linear_dw(hd, dy, rows8(aq, as_), dtype=torch.float32)
+        db_out = q8.bias_grad(hd, dy) if ctx.has_bias[1] else None
+        dz = q8.act_backward(hd, q8.linear_dx(hd, dy, rows8(oq, os_)), q8.Checkpoint8(cq, cs, *ctx.meta))
+        dw_in = q8.linear_dw(hd, dz, rows8(nq, ns), dtype=torch.float32)
+        db_in = q8.bias_grad(hd, dz) if ctx.has_bias[0] else None
+        dx, dweight = q8.norm_backward(hd, q8.linear_dx(hd, dz, rows8(iq, is_)), h, weight, rstd, dres=dh)
+        return None, dx, None if ctx.plain else dx, dweight, dw_in, db_in, dw_out, db_out
+
+
+class FeedForward8(torch.nn.Module):
+    """norm -> product -> activation -> product, with 8-bit products and 8-bit saved state.
+
+    forward(x, residual=None) takes bf16 [..., width] and returns (y, h) with h = x + residual: the next block of a stack
+    gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on every
+    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving."""
+
+    def __init__(self, width: int, hidden: int, kind: str = "silu_gated", bias: bool = False, eps: float = 1e-6, device="cuda"):
+        super().__init__()
+        if kind not in q8.KINDS:
+            raise ValueError("kind is one of " + ", ".join(q8.KINDS))
+        self.kind, self.eps = kind, float(eps)
+        parts = 2 if kind == "silu_gated" else 1
+        new = lambda *s: torch.nn.Parameter(torch.empty(*s, dtype=torch.float32, device=device))  # noqa: E731
+        self.weight = torch.nn.Parameter(torch.ones(width, dtype=torch.float32, device=device))
+        self.w_in, self.w_out = new(parts * hidden, width), new(width, hidden)
+        torch.nn.init.normal_(self.w_in, std=1 / math.sqrt(width))
+        torch.nn.init.normal_(self.w_out, std=1 / math.sqrt(hidden))
+        self.b_in = torch.nn.Parameter(torch.zeros(parts * hidden, dtype=torch.float32, device=device)) if bias else None
+        self.b_out = torch.nn.Parameter(torch.zeros(width, dtype=torch.float32, device=device)) if bias else None
+        self.weights8 = None
+        self._handle: Optional[stq.Handle] = None
+
+    def handle_for(self, device: torch.device) -> stq.Handle:
+        if self._handle is None or self._handle.device != device.index:
+            self._handle = stq.Handle(device.index)
+        return self._handle
+
+    def __getstate__(self):
+        return {**self.__dict__, "_handle": None}      # (a copy makes its own)
+
+    def quantized(self):
+        """The two weights as 8-bit rows, a scale per output channel."""
+        hd = self.handle_for(self.w_in.device)
+        return q8.quantize_rows(hd, self.w_in.detach()), q8.quantize_rows(hd, self.w_out.detach())
+
+    def freeze(self):
+        """Quantizes the weights once and keeps them until ``thaw()``: for serving, where they do not change."""
+        self.weights8 = self.quantized()
+        return self
+
+    def thaw(self):
+        self.weights8 = None
+        return self
+
+    def saved_bytes(self, tokens: int) -> int:
+        """Bytes that a forward pass of so many tokens keeps for its backward pass, next to h and the weights."""
+        (hidden, width), up = self.w_out.t().shape, lambda n: (n + 15) // 16 * 16
+        parts = self.w_in.shape[0] // hidden
+        return tokens * (up(width) + up(hidden) + parts * (up(hidden) + 4 * -(-hidden // q8.CKPT_BLOCK)) + 12)
+
+    def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
+        if x.dtype != torch.bfloat16 or (residual is not None and residual.dtype != torch.bfloat16):
+            raise ValueError("FeedForward8 takes bfloat16 activations")
+        flat = lambda t: None if t is None else t.reshape(-1, t.shape[-1])  # noqa: E731
+        y, h = _Block.apply(self, flat(x), flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
+        return y.view(x.shape), h.view(x.shape)

@@ -491,6 +491,8 @@ int stq_create(stq_handle** out, int device) {
   if (cudaMalloc(reinterpret_cast<void**>(&h->d_err), 2 * sizeof(int)) != cudaSuccess ||
       cudaMemset(h->d_err, 0, 2 * sizeof(int)) != cudaSuccess ||
       cudaMalloc(reinterpret_cast<void**>(&h->d_scalars), 4 * sizeof(float)) != cudaSuccess ||
+      cudaMalloc(reinterpret_cast<void**>(&h->d_q8_counters), stq::kQ8Counters * sizeof(uint32_t)) != cudaSuccess ||
+      cudaMemset(h->d_q8_counters, 0, stq::kQ8Counters * sizeof(uint32_t)) != cudaSuccess ||
       cudaMalloc(reinterpret_cast<void**>(&h->d_sched), 3 * sizeof(stq::FastSched)) != cudaSuccess) {
     cudaEventDestroy(h->stage_ev);
     delete h;
@@ -523,6 +525,7 @@ int stq_destroy(stq_handle* h) {
   cudaFree(h->d_seg_sums);
   cudaFree(h->d_arena);
   cudaFree(h->d_q8);
+  cudaFree(h->d_q8_counters);
   for (cudaStream_t st : h->host_streams)
     if (st) cudaStreamDestroy(st);
   for (cudaEvent_t e : h->host_events) cudaEventDestroy(e);

@@ -8,6 +8,7 @@
 
 #include "../../include/stq.h"
 #include "stq_internal.h"
+#include "stq_q8.h"
 
 struct stq_handle {
   int device = 0;
@@ -68,6 +69,7 @@ struct stq_handle {
   // workspace of the 8-bit operators: partial sums of split products and column sums, a pitched copy of a gradient
   uint8_t* d_q8 = nullptr;
   size_t d_q8_cap = 0;
+  uint32_t* d_q8_counters = nullptr;   // kQ8Counters of them, zero between launches
 };
 
 namespace stq {

@@ -42,14 +42,17 @@ struct NormBwdArgs {
   const float* weight;
   const float* rstd;
   float* dweight;
-  float* partial;        // [q8_norm_bwd_rows()][cols]
+  float* partial;        // q8_norm_bwd_partial() floats
+  size_t ldp;            // columns, rounded up to a multiple of 8
+  uint32_t* counters;
   uint64_t rows;
   uint32_t cols;
 };
-// Rows of `cols` floats that the backward pass needs for its partial sums of dweight.
+// Counters in the handle, zero between launches, at which CTAs arrive whose partial sums are added up.
+constexpr uint32_t kQ8Counters = 4096;
 constexpr uint32_t kNormBwdMaxCols = 49152;   // widest row: the sums of the widest variant stay in shared memory
-uint32_t q8_norm_bwd_rows(int dtype, const NormBwdArgs& a, int sms);
-cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream);
+size_t q8_norm_bwd_partial(int dtype, const NormBwdArgs& a, int sms);
+cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream, int* launches);
 
 struct ActBwdArgs {
   Mat da, dz;
@@ -61,10 +64,11 @@ struct ActBwdArgs {
 };
 cudaError_t launch_q8_act_bwd(int dtype, Q8Kind kind, const ActBwdArgs& a, cudaStream_t stream);
 
-// out[c] = sum over rows of x[r][c], in fp32, through `splits` partial rows.
+// out[c] = sum over rows of x[r][c], in fp32, through q8_colsum_partial() floats of partial sums.
 uint32_t q8_colsum_splits(uint64_t rows, uint32_t cols, int sms);
-cudaError_t launch_q8_colsum(int dtype, Mat x, uint64_t rows, uint32_t cols, uint32_t splits, float* partial, float* out,
-                             cudaStream_t stream);
+size_t q8_colsum_partial(uint32_t cols, uint32_t splits);
+cudaError_t launch_q8_colsum(int dtype, Mat x, uint64_t rows, uint32_t cols, uint32_t splits, float* partial, uint32_t* counters,
+                             float* out, cudaStream_t stream);
 
 struct GemmArgs {
   const int8_t* xq;      // 8-bit operand whose row scales lie along the rows of the result (or along the sum)

@@ -162,9 +162,12 @@ int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const voi
   a.dx = {dx, lddx};
   a.weight = weight; a.rstd = rstd; a.dweight = dweight;
   a.rows = rows; a.cols = cols;
-  STQ_TRY(workspace(h, (size_t)stq::q8_norm_bwd_rows(dtype, a, h->sm_count) * cols, &a.partial));
-  STQ_CUDA(h, stq::launch_q8_norm_bwd(dtype, a, h->sm_count, s));
-  h->launches += 2;
+  a.ldp = ((size_t)cols + 7) / 8 * 8;
+  a.counters = h->d_q8_counters;
+  STQ_TRY(workspace(h, stq::q8_norm_bwd_partial(dtype, a, h->sm_count), &a.partial));
+  int launches = 0;
+  STQ_CUDA(h, stq::launch_q8_norm_bwd(dtype, a, h->sm_count, s, &launches));
+  h->launches += launches;
   return STQ_OK;
 }
 
@@ -325,9 +328,9 @@ int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, ui
   if (clash(o, in)) return STQ_E_ALIAS;
   const uint32_t splits = stq::q8_colsum_splits(t, n, h->sm_count);
   float* partial = nullptr;
-  if (splits > 1) STQ_TRY(workspace(h, (size_t)splits * n, &partial));
-  STQ_CUDA(h, stq::launch_q8_colsum(dtype, {const_cast<void*>(dy), lddy}, t, n, splits, partial, db, s));
-  h->launches += splits > 1 ? 2 : 1;
+  if (const size_t need = stq::q8_colsum_partial(n, splits)) STQ_TRY(workspace(h, need, &partial));
+  STQ_CUDA(h, stq::launch_q8_colsum(dtype, {const_cast<void*>(dy), lddy}, t, n, splits, partial, h->d_q8_counters, db, s));
+  h->launches++;
   return STQ_OK;
 }
 

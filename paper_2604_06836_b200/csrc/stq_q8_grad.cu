@@ -150,6 +150,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
   mma_fence_before();
   __syncthreads();
   if (CG == 2) cluster_sync_all();
+  asm volatile("griddepcontrol.wait;" ::: "memory");      // (launched while a copy or conversion kernel before it still runs)
   mma_fence_after();
   const uint32_t tmem = tmem_slot;
 
@@ -352,6 +353,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       } while (true);
     }
   }
+  asm volatile("griddepcontrol.launch_dependents;");
   if (!ok) *a.err = 1;
   __syncwarp();
   mma_fence_before();
@@ -367,6 +369,8 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
 // zero.  16 columns to a thread.
 __global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t ldq, const float* scale, uint32_t rows,
                                                          uint32_t cols, uint32_t plane, __nv_bfloat16* out, size_t ld) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
   const uint32_t per_row = (uint32_t)((ld + 15) / 16);
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint64_t row = id / per_row;
@@ -396,6 +400,7 @@ __global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t
 template <class O>
 __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, size_t split_stride, uint32_t splits, size_t ldp,
                                                       uint64_t rows, uint32_t cols, O* out, size_t ldo, int align) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t per_row = (uint32_t)(ldp / 4);
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= rows * per_row) return;
@@ -424,6 +429,7 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, size_t 
 // A gradient whose rows are not aligned to 16 bytes, copied to rows that are (the columns that pad a row are zero).
 __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, size_t ldi, uint64_t rows, uint32_t cols,
                                                        __nv_bfloat16* out, size_t ldo) {
+  asm volatile("griddepcontrol.launch_dependents;");
   const uint32_t per_row = (uint32_t)(ldo / 8);
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= rows * per_row) return;
@@ -535,7 +541,7 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, i
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
-  return launch_cluster(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, stream, mg, mq, a);
+  return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, w.pitch || !w.plan.conv, stream, mg, mq, a);
 }
 
 template <int PARTS, bool DW, class O>
@@ -571,9 +577,8 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   if (!w.plan.conv) {
     __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base + w.pitch_bytes + w.part_bytes);
     const uint64_t items = (uint64_t)w.plane * ((w.ldb + 15) / 16);
-    q8_convert_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(DW ? g.xq : g.wq, DW ? g.ldx : g.ldw, DW ? g.xs : g.ws,
-                                                                           (uint32_t)(DW ? g.t : g.n), g.k, w.plane, to, w.ldb);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_with(q8_convert_kernel, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, 1, w.pitch, stream,
+                                      DW ? g.xq : g.wq, DW ? g.ldx : g.ldw, DW ? g.xs : g.ws, (uint32_t)(DW ? g.t : g.n), g.k, w.plane, to, w.ldb);
     if (e != cudaSuccess) return e;
     at.operand = to;
     ++*launches;
@@ -585,14 +590,12 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   if (e != cudaSuccess || !split) return e;
   const uint64_t items = m * (w.ldp / 4);
   const unsigned grid = (unsigned)((items + 255) / 256);
-  if (f32)
-    q8_join_kernel<float><<<grid, 256, 0, stream>>>(part, m * w.ldp, w.plan.splits, w.ldp, m, g.k, static_cast<float*>(g.out), g.ldo,
-                                                    row_alignment(g.out, g.ldo * 4));
-  else
-    q8_join_kernel<__nv_bfloat16><<<grid, 256, 0, stream>>>(part, m * w.ldp, w.plan.splits, w.ldp, m, g.k,
-                                                            static_cast<__nv_bfloat16*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 2));
+  e = f32 ? launch_with(q8_join_kernel<float>, dim3(grid), dim3(256), 0, 1, true, stream, (const float*)part, m * w.ldp, w.plan.splits, w.ldp, m,
+                        g.k, static_cast<float*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 4))
+          : launch_with(q8_join_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, 1, true, stream, (const float*)part, m * w.ldp, w.plan.splits,
+                        w.ldp, m, g.k, static_cast<__nv_bfloat16*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 2));
   ++*launches;
-  return cudaGetLastError();
+  return e;
 }
 
 }  // namespace

@@ -495,7 +495,7 @@ cudaError_t launch_pairs(const GemmArgs& g, int sms, int* err, cudaStream_t stre
   if (e == cudaSuccess) e = allow_smem(q8_linear_kernel<BN, O>, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n, most = sms / 2;
-  return launch_cluster(q8_linear_kernel<BN, O>, (unsigned)(tiles < most ? tiles : most) * 2, kThreads8, S::kSmem, 2, stream, mx, mw, a);
+  return launch_with(q8_linear_kernel<BN, O>, (unsigned)(tiles < most ? tiles : most) * 2, kThreads8, S::kSmem, 2, false, stream, mx, mw, a);
 }
 
 template <int BN, class O>
@@ -511,7 +511,7 @@ cudaError_t launch_split(const GemmArgs& g, int size, int* err, cudaStream_t str
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(q8_linear_split_kernel<BN, O>, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
-  return launch_cluster(q8_linear_split_kernel<BN, O>, a.tiles_m * a.tiles_n * size, kThreads8, S::kSmem, size, stream, mx, mw, a, size == 8 ? 3 : size / 2);
+  return launch_with(q8_linear_split_kernel<BN, O>, a.tiles_m * a.tiles_n * size, kThreads8, S::kSmem, size, false, stream, mx, mw, a, size == 8 ? 3 : size / 2);
 }
 
 template <int T, int R, class O>

@@ -14,6 +14,7 @@
 #include "../../include/stq.h"
 #include "stq_internal.h"
 #include "stq_q8.h"
+#include "stq_q8_tma.h"
 
 namespace stq {
 namespace {
@@ -446,13 +447,82 @@ __global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowA
   }
 }
 
+// ---- sums over CTAs -------------------------------------------------------------------------------------------------
+// out[c] = sum over rows of rows[r][c] (pitch ld, a multiple of 4 floats), by all threads of a CTA, in order.
+__device__ __forceinline__ void sum_rows(const float* rows, uint32_t n, size_t ld, uint32_t cols, float* out, bool aligned) {
+  for (uint32_t c = threadIdx.x * 4; c < cols; c += blockDim.x * 4) {
+    float2 lo = both(0.f), hi = both(0.f);
+#pragma unroll 8
+    for (uint32_t r = 0; r < n; ++r) {
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(rows + r * ld + c));
+      lo = add2(lo, make_float2(v.x, v.y));
+      hi = add2(hi, make_float2(v.z, v.w));
+    }
+    if (aligned && c + 4 <= cols) {
+      *reinterpret_cast<float4*>(out + c) = make_float4(lo.x, lo.y, hi.x, hi.y);
+    } else {
+      const float v[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < cols) out[c + i] = v[i];
+    }
+  }
+}
+// True for the CTA that arrives last of `n` at a counter, which it sets back to zero; what the others wrote before they
+// arrived is visible to it.
+__device__ __forceinline__ bool arrived_last(uint32_t* counter, uint32_t n) {
+  __shared__ bool last;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    last = atomicAdd(counter, 1u) == n - 1;
+    if (last) *counter = 0;
+  }
+  __syncthreads();
+  if (last) __threadfence();
+  return last;
+}
+// Every CTA has written row blockIdx.x of `partial` (pitch ld).  Up to kJoin rows are added up by the CTA that comes last;
+// more of them by q8_join_rows_kernel, which spreads the columns over the device: on 8192 x 4096 the two take 47 us, with
+// everything joined inside one launch (in two levels) 59.
+constexpr uint32_t kJoin = 16;
+__device__ __forceinline__ void join_rows(float* partial, size_t ld, uint32_t cols, float* out, uint32_t* counter) {
+  const uint32_t n = gridDim.x;
+  if (n > kJoin) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    return;
+  }
+  if (n == 1)
+    __syncthreads();
+  else if (!arrived_last(counter, n))
+    return;
+  sum_rows(partial, n, ld, cols, out, (reinterpret_cast<uintptr_t>(out) & 15) == 0);
+}
+// 32 columns to a CTA, 32 shares of the rows added up in shared memory: a fixed order.
+__global__ void __launch_bounds__(1024) q8_join_rows_kernel(const float* partial, size_t ld, uint32_t n, uint32_t cols, float* out) {
+  __shared__ float sh[32][33];
+  const uint32_t c = blockIdx.x * 32 + threadIdx.x;
+  asm volatile("griddepcontrol.wait;" ::: "memory");      // (launched while the kernel before it still runs)
+  float s = 0.f;
+  if (c < cols) {
+#pragma unroll 4
+    for (uint32_t r = threadIdx.y; r < n; r += 32) s += __ldcg(partial + r * ld + c);
+  }
+  sh[threadIdx.y][threadIdx.x] = s;
+  __syncthreads();
+  s = sh[threadIdx.x][threadIdx.y];     // warp y adds the 32 shares of column y
+#pragma unroll
+  for (int m = 16; m; m >>= 1) s += __shfl_xor_sync(kFullMask, s, m);
+  if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < cols) out[blockIdx.x * 32 + threadIdx.y] = s;
+}
+
 constexpr int kBwdWarps = 16;                             // most warps to a row (two rows' operands live in registers)
 
 // ---- backward of the norm -----------------------------------------------------------------------------------------
 // dx = rstd (w dy - xh mean(w dy xh)) + dres with xh = h rstd; dweight = sum over rows of dy xh.  A CTA holds `gangs`
 // groups of `warps` warps; a group walks rows group, group + groups, ..., with the next row's loads in flight while a row
 // is summed and written.  A lane's columns stay the same, so its share of dweight stays in registers until the end; then
-// the CTA's groups add theirs up in shared memory, and q8_colsum_finish_kernel adds the CTAs', both in a fixed order.
+// the CTA's groups add theirs up in shared memory, and the CTAs' are joined, both in a fixed order.
 template <class T, int VEC, int NS>
 __global__ void __launch_bounds__(kBwdWarps * 32) q8_norm_bwd_kernel(const NormBwdArgs a, int warps, int gangs) {
   extern __shared__ float dwsum[];
@@ -551,9 +621,10 @@ __global__ void __launch_bounds__(kBwdWarps * 32) q8_norm_bwd_kernel(const NormB
           dw[s][i] = add2(dw[s][i], make_float2(dwsum[at], dwsum[at + 1]));
         }
       }
-      store_unit<float, VEC>(a.partial + (size_t)blockIdx.x * cols, first + s * step, lane, cols, dw[s]);
+      store_unit<float, VEC>(a.partial + blockIdx.x * a.ldp, first + s * step, lane, cols, dw[s]);
     }
   }
+  join_rows(a.partial, a.ldp, cols, a.dweight, a.counters);
 }
 
 // The same for rows that do not fit in registers: a row is read twice (the second time from L2) and the sums of
@@ -611,16 +682,19 @@ __global__ void __launch_bounds__(1024) q8_norm_bwd_wide_kernel(const NormBwdArg
     }
   }
   __syncthreads();
-  for (uint32_t c = threadIdx.x; c < cols; c += blockDim.x) a.partial[(size_t)blockIdx.x * cols + c] = dwsum[c];
+  for (uint32_t c = threadIdx.x; c < cols; c += blockDim.x) a.partial[blockIdx.x * a.ldp + c] = dwsum[c];
+  join_rows(a.partial, a.ldp, cols, a.dweight, a.counters);
 }
 
 // ---- column sums ---------------------------------------------------------------------------------------------------
-// partial[split][c] = sum over the split's rows; 8 warps share the rows of a split, 256 columns to a CTA.
+// A CTA sums 256 columns of one split of the rows, 8 warps sharing the rows; the last of the splits' CTAs adds their sums
+// up, in order.
 template <class T, int VEC>
-__global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, uint32_t cols, uint32_t splits, float* partial) {
+__global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, uint32_t cols, float* partial, float* out,
+                                                        uint32_t* counters) {
   __shared__ float sh[8][kUnit];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t base = blockIdx.x * kUnit, split = blockIdx.y;
+  const uint32_t base = blockIdx.x * kUnit, split = blockIdx.y, splits = gridDim.y;
   const uint64_t per = (rows + splits - 1) / splits, r0 = split * per, r1 = min(r0 + per, rows);
   float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
 #pragma unroll 4
@@ -640,25 +714,17 @@ __global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, ui
   float sum = 0.f;
 #pragma unroll
   for (int w = 0; w < 8; ++w) sum += sh[w][threadIdx.x];
-  if (c < cols) partial[(size_t)split * cols + c] = sum;
-}
-
-// out[c] = sum of partial[g][c] over g, in a fixed order: 32 columns to a CTA, 32 shares of the groups added up
-// in shared memory.
-__global__ void __launch_bounds__(1024) q8_colsum_finish_kernel(const float* partial, uint32_t groups, uint32_t cols, float* out) {
-  __shared__ float sh[32][33];
-  const uint32_t c = blockIdx.x * 32 + threadIdx.x;
-  float s = 0.f;
-  if (c < cols) {
-#pragma unroll 4
-    for (uint32_t g = threadIdx.y; g < groups; g += 32) s += partial[(size_t)g * cols + c];
+  if (splits == 1) {
+    if (c < cols) out[c] = sum;
+    return;
   }
-  sh[threadIdx.y][threadIdx.x] = s;
-  __syncthreads();
-  s = sh[threadIdx.x][threadIdx.y];     // warp y adds the 32 shares of column y
-#pragma unroll
-  for (int m = 16; m; m >>= 1) s += __shfl_xor_sync(kFullMask, s, m);
-  if (threadIdx.x == 0 && blockIdx.x * 32 + threadIdx.y < cols) out[blockIdx.x * 32 + threadIdx.y] = s;
+  float* mine = partial + (size_t)blockIdx.x * splits * kUnit;
+  mine[split * kUnit + threadIdx.x] = sum;
+  if (!arrived_last(counters + blockIdx.x, splits)) return;
+  sum = 0.f;
+#pragma unroll 8
+  for (uint32_t i = 0; i < splits; ++i) sum += __ldcg(mine + i * kUnit + threadIdx.x);
+  if (c < cols) out[c] = sum;
 }
 
 // ---- backward of the activations, from the checkpoint -------------------------------------------------------------
@@ -839,14 +905,16 @@ int bwd_vec(int dtype, const NormBwdArgs& a) {
 }
 }  // namespace
 
-uint32_t q8_norm_bwd_rows(int dtype, const NormBwdArgs& a, int sms) {
-  return bwd_shape(a.rows, a.cols, dtype, bwd_vec(dtype, a), sms).ctas;
+size_t q8_norm_bwd_partial(int dtype, const NormBwdArgs& a, int sms) {
+  const uint32_t n = bwd_shape(a.rows, a.cols, dtype, bwd_vec(dtype, a), sms).ctas;
+  return (size_t)n * a.ldp;
 }
 
-cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream) {
+cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStream_t stream, int* launches) {
   const int width = bwd_vec(dtype, a);
   const BwdShape sh = bwd_shape(a.rows, a.cols, dtype, width, sms);
-  cudaError_t e = by_type(dtype, [&](auto tv) {
+  *launches = sh.ctas > kJoin ? 2 : 1;
+  const cudaError_t e = by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
     return by_vec(width, [&](auto vec) {
       if (a.cols > kBwdRegCols) {
@@ -865,34 +933,32 @@ cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStr
       return cudaGetLastError();
     });
   });
-  if (e != cudaSuccess) return e;
-  q8_colsum_finish_kernel<<<(a.cols + 31) / 32, dim3(32, 32), 0, stream>>>(a.partial, sh.ctas, a.cols, a.dweight);
-  return cudaGetLastError();
+  if (e != cudaSuccess || sh.ctas <= kJoin) return e;
+  return launch_with(q8_join_rows_kernel, dim3((a.cols + 31) / 32), dim3(32, 32), 0, 1, true, stream, (const float*)a.partial, a.ldp, sh.ctas,
+                     a.cols, a.dweight);
 }
 
 uint32_t q8_colsum_splits(uint64_t rows, uint32_t cols, int sms) {
-  // about four CTAs of 8 warps per SM, at least 32 rows to a split
+  // about four CTAs of 8 warps per SM, at least 32 rows to a split; so many columns that there is no counter for each
+  // tile of them fill the device by themselves
   const uint32_t tiles = (cols + kUnit - 1) / kUnit, want = (uint32_t)(4 * sms + tiles - 1) / tiles;
   const uint64_t most = (rows + 31) / 32;
-  return (uint32_t)(want < most ? want : most);
+  return tiles > kQ8Counters ? 1 : (uint32_t)(want < most ? want : most);
 }
+size_t q8_colsum_partial(uint32_t cols, uint32_t splits) { return splits == 1 ? 0 : (size_t)((cols + kUnit - 1) / kUnit) * kUnit * splits; }
 
-cudaError_t launch_q8_colsum(int dtype, Mat x, uint64_t rows, uint32_t cols, uint32_t splits, float* partial, float* out,
-                             cudaStream_t stream) {
+cudaError_t launch_q8_colsum(int dtype, Mat x, uint64_t rows, uint32_t cols, uint32_t splits, float* partial, uint32_t* counters,
+                             float* out, cudaStream_t stream) {
   Width w;
   w.add(x, elem_bytes(dtype));
   const dim3 grid((cols + kUnit - 1) / kUnit, splits);
-  float* to = splits == 1 ? out : partial;
-  cudaError_t e = by_type(dtype, [&](auto tv) {
+  return by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
     return by_vec(w.vec(cols), [&](auto vec) {
-      q8_colsum_kernel<T, vec()><<<grid, 256, 0, stream>>>(x, rows, cols, splits, to);
+      q8_colsum_kernel<T, vec()><<<grid, 256, 0, stream>>>(x, rows, cols, partial, out, counters);
       return cudaGetLastError();
     });
   });
-  if (e != cudaSuccess || splits == 1) return e;
-  q8_colsum_finish_kernel<<<(cols + 31) / 32, dim3(32, 32), 0, stream>>>(partial, splits, cols, out);
-  return cudaGetLastError();
 }
 
 cudaError_t launch_q8_act_bwd(int dtype, Q8Kind kind, const ActBwdArgs& a, cudaStream_t stream) {

@@ -1,4 +1,4 @@
-// Host side of the tensor copies: maps of row-major matrices in the 128-byte swizzle.
+// Host side of the tensor copies (maps of row-major matrices in the 128-byte swizzle) and of launches with attributes.
 #pragma once
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -29,20 +29,30 @@ cudaError_t allow_smem(K kernel, size_t bytes, int device, std::atomic<uint64_t>
   return e;
 }
 
-template <class K, class... A>
-cudaError_t launch_cluster(K kernel, unsigned grid, unsigned threads, size_t smem, unsigned cluster, cudaStream_t stream,
-                           const A&... args) {
+// early: the kernel may start while the one before it in the stream still runs (it waits for that one's results itself).
+template <class... P, class... A>
+cudaError_t launch_with(void (*kernel)(P...), dim3 grid, dim3 threads, size_t smem, unsigned cluster, bool early, cudaStream_t stream,
+                        const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = threads;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = cluster;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
+  unsigned n = 0;
+  if (cluster > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = cluster;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (early) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
   cfg.attrs = at;
-  cfg.numAttrs = cluster > 1 ? 1 : 0;
+  cfg.numAttrs = n;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 

@@ -9,6 +9,7 @@
 // the last 128 can be told apart by lane or by register, which is what a checkpoint's block of 128 needs.
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/stq.h"
@@ -78,26 +79,24 @@ struct Raw {
           w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
         }
       }
-    } else if constexpr (VEC == 2) {
+    } else if (base + kUnit <= cols) {       // a whole unit: loads at fixed distances, nothing to ask
+      const T* from = row + base + lane * VEC;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const uint32_t c = col_of<VEC>(base, lane, 2 * p);
-        if (c < cols) {
-          if constexpr (sizeof(T) == 2) {
-            w[p] = *reinterpret_cast<const uint32_t*>(row + c);
-          } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(row + c);
-            w[2 * p] = v.x; w[2 * p + 1] = v.y;
-          }
-        }
-      }
+      for (int i = 0; i < 8 / VEC; ++i) one(from + i * 32 * VEC, i);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t c = col_of<VEC>(base, lane, e);
-        if (c < cols) w[e] = sizeof(T) == 2 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[c] << 16
-                                            : reinterpret_cast<const uint32_t*>(row)[c];
-      }
+      for (int i = 0; i < 8 / VEC; ++i)
+        if (base + i * 32 * VEC + lane * VEC < cols) one(row + base + i * 32 * VEC + lane * VEC, i);
+    }
+  }
+  __device__ __forceinline__ void one(const T* from, int i) {      // access i of VEC = 2 or 1
+    if constexpr (VEC == 2 && sizeof(T) == 2) {
+      w[i] = *reinterpret_cast<const uint32_t*>(from);
+    } else if constexpr (VEC == 2) {
+      const uint2 v = *reinterpret_cast<const uint2*>(from);
+      w[2 * i] = v.x; w[2 * i + 1] = v.y;
+    } else if constexpr (VEC == 1) {
+      w[i] = sizeof(T) == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(from) << 16 : *reinterpret_cast<const uint32_t*>(from);
     }
   }
   __device__ __forceinline__ float2 pair(int p) const {      // elements 2p, 2p + 1
@@ -126,20 +125,23 @@ __device__ __forceinline__ void store_unit(T* row, uint32_t base, int lane, uint
       *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
     }
   } else {
+    T* to = row + base + lane * VEC;
+    auto one = [&](int i) {
+      T* at = to + i * 32 * VEC;
+      if constexpr (VEC == 2 && sizeof(T) == 2)
+        *reinterpret_cast<uint32_t*>(at) = pack2(v[i % 4]);
+      else if constexpr (VEC == 2)
+        *reinterpret_cast<float2*>(at) = v[i % 4];
+      else
+        *at = static_cast<T>(i & 1 ? v[i / 2].y : v[i / 2].x);
+    };
+    if (base + kUnit <= cols) {
 #pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const uint32_t c = col_of<VEC>(base, lane, 2 * p);
-      if constexpr (VEC == 2) {
-        if (c >= cols) continue;
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<uint32_t*>(row + c) = pack2(v[p]);
-        else
-          *reinterpret_cast<float2*>(row + c) = v[p];
-      } else {
-        const uint32_t d = col_of<VEC>(base, lane, 2 * p + 1);
-        if (c < cols) row[c] = static_cast<T>(v[p].x);
-        if (d < cols) row[d] = static_cast<T>(v[p].y);
-      }
+      for (int i = 0; i < 8 / VEC; ++i) one(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i)
+        if (base + i * 32 * VEC + lane * VEC < cols) one(i);
     }
   }
 }
@@ -151,14 +153,21 @@ __device__ __forceinline__ void store_codes(int8_t* row, uint32_t base, int lane
     const uint32_t c = base + lane * 8;
     if (c < cols) *reinterpret_cast<uint2*>(row + c) = make_uint2(k[0], k[1]);
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; e += VEC) {
-      const uint32_t c = col_of<VEC>(base, lane, e), w = k[e / 4] >> (8 * (e & 3));
-      if (c >= cols) continue;
+    int8_t* to = row + base + lane * VEC;
+    auto one = [&](int i) {
+      const uint32_t w = k[i * VEC / 4] >> (8 * (i * VEC & 3));
       if constexpr (VEC == 2)
-        *reinterpret_cast<uint16_t*>(row + c) = (uint16_t)w;
+        *reinterpret_cast<uint16_t*>(to + i * 64) = (uint16_t)w;
       else
-        row[c] = (int8_t)w;
+        to[i * 32] = (int8_t)w;
+    };
+    if (base + kUnit <= cols) {
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i) one(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i)
+        if (base + i * 32 * VEC + lane * VEC < cols) one(i);
     }
   }
 }
@@ -174,12 +183,18 @@ __device__ __forceinline__ void load_codes(const int8_t* row, uint32_t base, int
       k[0] = w.x; k[1] = w.y;
     }
   } else {
+    const int8_t* from = row + base + lane * VEC;
+    auto one = [&](int i) {
+      const uint32_t w = VEC == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(from + i * 64) : (uint32_t)(uint8_t)from[i * 32];
+      k[i * VEC / 4] |= w << (8 * (i * VEC & 3));
+    };
+    if (base + kUnit <= cols) {
 #pragma unroll
-    for (int e = 0; e < 8; e += VEC) {
-      const uint32_t c = col_of<VEC>(base, lane, e);
-      if (c >= cols) continue;
-      const uint32_t w = VEC == 2 ? (uint32_t)*reinterpret_cast<const uint16_t*>(row + c) : (uint32_t)(uint8_t)row[c];
-      k[e / 4] |= w << (8 * (e & 3));
+      for (int i = 0; i < 8 / VEC; ++i) one(i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8 / VEC; ++i)
+        if (base + i * 32 * VEC + lane * VEC < cols) one(i);
     }
   }
   k[0] ^= 0x80808080u;
@@ -879,19 +894,40 @@ namespace {
 constexpr uint32_t kBwdRegCols = kBwdWarps * 2 * kUnit;   // widest row that stays in registers (2 units to a warp)
 struct BwdShape {
   int warps, ns, gangs;
+  size_t smem;
   uint32_t ctas;             // rows of partial sums
 };
-// CTAs of at least 8 warps, as many as are resident at once with 80 (one unit to a warp) or 128 registers a thread.
+// CTAs of a kernel that an SM holds at once, asked for once per number of warps (the same on every device of this kind).
+template <class T, int VEC, int NS>
+int bwd_resident(int warps, size_t smem) {
+  static std::atomic<int> known[kBwdWarps + 1];
+  int n = known[warps].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, q8_norm_bwd_kernel<T, VEC, NS>, warps * 32, smem) != cudaSuccess || n < 1) n = 1;
+    known[warps].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// CTAs of at least 8 warps, as many as are resident at once (with more, some would start when the others are done).
 // Two units to a warp are faster where they fit (bf16, 8192 x 4096: 59 -> 47 us, 8192 x 1600: 36 -> 24 us) and slower where
 // they spill, which is with fp32 (4096 x 4096: 46 -> 78 us) and with single elements.
 BwdShape bwd_shape(uint64_t rows, uint32_t cols, int dtype, int vec, int sms) {
-  if (cols > kBwdRegCols) return {0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
+  if (cols > kBwdRegCols) return {0, 0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
   const uint32_t units = (cols + kUnit - 1) / kUnit;
   const int ns = units > kBwdWarps || (units > 1 && dtype == STQ_GRAD_BF16 && vec > 1) ? 2 : 1;
   const int warps = (int)((units + ns - 1) / ns), gangs = warps >= 8 ? 1 : 8 / warps;
-  const int per_sm = (ns == 1 ? 24 : 16) / (warps * gangs);
-  const uint64_t want = (rows + gangs - 1) / gangs, most = (uint64_t)sms * (per_sm < 1 ? 1 : per_sm);
-  return {warps, ns, gangs, (uint32_t)(want < most ? want : most)};
+  const size_t smem = gangs > 1 ? (size_t)warps * ns * kUnit * 4 : 0;      // (at most 8 warps of 2 units then)
+  int per_sm = 1;
+  by_type(dtype, [&](auto tv) {
+    using T = decltype(tv);
+    return by_vec(vec, [&](auto v) {
+      per_sm = ns == 1 ? bwd_resident<T, v(), 1>(warps * gangs, smem) : bwd_resident<T, v(), 2>(warps * gangs, smem);
+      return cudaSuccess;
+    });
+  });
+  const uint64_t want = (rows + gangs - 1) / gangs, most = (uint64_t)sms * per_sm;
+  return {warps, ns, gangs, smem, (uint32_t)(want < most ? want : most)};
 }
 
 int bwd_vec(int dtype, const NormBwdArgs& a) {
@@ -925,11 +961,10 @@ cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStr
         return cudaGetLastError();
       }
       const int threads = sh.warps * sh.gangs * 32;
-      const size_t smem = sh.gangs > 1 ? (size_t)sh.warps * sh.ns * kUnit * 4 : 0;      // (at most 8 warps of 2 units then)
       if (sh.ns == 1)
-        q8_norm_bwd_kernel<T, vec(), 1><<<sh.ctas, threads, smem, stream>>>(a, sh.warps, sh.gangs);
+        q8_norm_bwd_kernel<T, vec(), 1><<<sh.ctas, threads, sh.smem, stream>>>(a, sh.warps, sh.gangs);
       else
-        q8_norm_bwd_kernel<T, vec(), 2><<<sh.ctas, threads, smem, stream>>>(a, sh.warps, sh.gangs);
+        q8_norm_bwd_kernel<T, vec(), 2><<<sh.ctas, threads, sh.smem, stream>>>(a, sh.warps, sh.gangs);
       return cudaGetLastError();
     });
   });

@@ -38,11 +38,13 @@ constexpr int kGroups = 2, kGroupWarps = 4;        // conversion: groups of warp
 
 struct GradArgs {
   const float* scale;                  // s[c]
-  void* out;                           // result, or the first of `splits` partial results of fp32
-  size_t ldo, split_stride;            // elements
+  void* out;
+  size_t ldo;                          // elements
+  float* part;                         // partial results of the tiles whose sum is shared, a tile to each
   uint64_t m;
   uint32_t n, depth, ksteps;           // columns, length of the sum, its stages
-  uint32_t tiles_m, tiles_n, splits;
+  uint32_t tiles_m, tiles;
+  uint32_t full, splits;               // tiles from `full` on are shared by `splits` work items each
   int align;
   int* err;
 };
@@ -131,7 +133,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0;
   const bool leader = rank == 0;
-  const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG, tiles = a.tiles_m * a.tiles_n, work = tiles * a.splits;
+  const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG, work = a.full + (a.tiles - a.full) * a.splits;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kStages; ++i) {
@@ -156,11 +158,15 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
 
   // work item -> tile and its share [k0, k1) of the stages of the sum
   auto share = [&](uint32_t w, uint32_t& tile, uint32_t& k0, uint32_t& k1) {
-    const uint32_t sp = w / tiles;
-    tile = w - sp * tiles;
-    k0 = (uint32_t)((uint64_t)a.ksteps * sp / a.splits);
-    k1 = (uint32_t)((uint64_t)a.ksteps * (sp + 1) / a.splits);
-    return sp;
+    tile = w;
+    k0 = 0;
+    k1 = a.ksteps;
+    if (w >= a.full) {
+      const uint32_t i = w - a.full, sp = i % a.splits;
+      tile = a.full + i / a.splits;
+      k0 = (uint32_t)((uint64_t)a.ksteps * sp / a.splits);
+      k1 = (uint32_t)((uint64_t)a.ksteps * (sp + 1) / a.splits);
+    }
   };
 
   bool ok = true;
@@ -307,10 +313,12 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
     uint32_t n = 0, tile, k0, k1;
     for (uint32_t w = unit; ok && w < work; w += units) {
-      const uint32_t sp = share(w, tile, k0, k1), lanes = (uint32_t)(quad * 32) << 16, running = tmem + lanes + 2 * BN;
+      share(w, tile, k0, k1);
+      const uint32_t lanes = (uint32_t)(quad * 32) << 16, running = tmem + lanes + 2 * BN;
       const uint64_t row = (uint64_t)(tile % a.tiles_m) * 128 * CG + 128 * rank + quad * 32;
       const uint32_t col = tile / a.tiles_m * BN;
-      O* out = static_cast<O*>(a.out) + sp * a.split_stride + row * a.ldo + col;
+      O* out = static_cast<O*>(a.out) + row * a.ldo + col;
+      float* part = w >= a.full && a.splits > 1 ? a.part + ((size_t)(w - a.full) * CG * 128 + 128 * rank + quad * 32) * BN : nullptr;
       const int rows = row >= a.m ? 0 : (int)min((uint64_t)32, a.m - row);
       constexpr int kC = 128 / sizeof(O);
       uint32_t k = k0;
@@ -341,7 +349,13 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
               continue;
             }
           }
-          store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < kC; i += 32)
+              store_block<float>(part + c + i, BN, *reinterpret_cast<const float(*)[32]>(&v[i]), 32, 32, 32, lane, stage[quad]);
+          } else {
+            store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
+          }
         }
         if (PARTS == 3) tmem_store_wait();
         mma_fence_before();
@@ -396,24 +410,27 @@ __global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t
   if (c + 8 < ld) *reinterpret_cast<uint4*>(to + 8) = make_uint4(v[4], v[5], v[6], v[7]);
 }
 
-// out[r][c] = sum over splits of part[s][r][c] (rows of `ldp` floats, a multiple of 8), in order
+// The shared tiles from their partial results, added in order: 4 columns to a thread.
 template <class O>
-__global__ void __launch_bounds__(256) q8_join_kernel(const float* part, size_t split_stride, uint32_t splits, size_t ldp,
-                                                      uint64_t rows, uint32_t cols, O* out, size_t ldo, int align) {
+__global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first,
+                                                      uint32_t count, uint32_t tiles_m, uint64_t m, uint32_t n, O* out, size_t ldo, int align) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t per_row = (uint32_t)(ldp / 4);
+  const uint32_t per_row = tile_n / 4, per_tile = per_row * tile_m;
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= rows * per_row) return;
-  const uint64_t r = id / per_row;
-  const uint32_t c = (uint32_t)(id - r * per_row) * 4;
-  const float* p = part + r * ldp + c;
-  float4 s = *reinterpret_cast<const float4*>(p);
+  const uint32_t t = (uint32_t)(id / per_tile), in = (uint32_t)(id - (uint64_t)t * per_tile);
+  if (t >= count) return;
+  const uint64_t row = (uint64_t)((first + t) % tiles_m) * tile_m + in / per_row;
+  const uint32_t col = (first + t) / tiles_m * tile_n + in % per_row * 4;
+  if (row >= m || col >= n) return;
+  const float4* p = reinterpret_cast<const float4*>(part) + (size_t)t * splits * per_tile + in;
+  float4 s = __ldcg(p);
+#pragma unroll 4
   for (uint32_t i = 1; i < splits; ++i) {
-    const float4 v = *reinterpret_cast<const float4*>(p + i * split_stride);
+    const float4 v = __ldcg(p + (size_t)i * per_tile);
     s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
   }
-  O* o = out + r * ldo + c;
-  if (align >= 16 && c + 4 <= cols) {
+  O* o = out + row * ldo + col;
+  if (align >= 16 && col + 4 <= n) {
     if constexpr (sizeof(O) == 4)
       *reinterpret_cast<float4*>(o) = s;
     else
@@ -422,7 +439,7 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, size_t 
     const float v[4] = {s.x, s.y, s.z, s.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (c + i < cols) o[i] = static_cast<O>(v[i]);
+      if (col + i < n) o[i] = static_cast<O>(v[i]);
   }
 }
 
@@ -449,7 +466,7 @@ __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, 
 struct Plan {
   int cg, bn;                // CTAs and columns of a tile
   bool conv;                 // convert inside the product
-  uint32_t splits;
+  uint32_t tiles, full, splits;      // the tiles that do not fill a round are shared by `splits` work items each
 };
 
 // Time of a plan in clock cycles.  A stage takes 4096 multiply-adds a cycle and SM (three times as many for an operand in
@@ -458,16 +475,19 @@ struct Plan {
 Plan plan_of(uint64_t m, uint32_t n, uint32_t depth, int parts, size_t out_elem, int sms) {
   static const int shapes[2][3][2] = {{{2, 256}, {1, 128}, {1, 64}}, {{2, 128}, {1, 64}, {1, 64}}};
   const uint32_t ksteps = (depth + kDepth - 1) / kDepth;
-  Plan best = {0, 0, true, 1};
+  Plan best = {};
   double least = 1e300;
   auto weigh = [&](int cg, int bn, bool conv, double stage, double fixed) {
-    const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg;
+    const uint64_t tiles = ((m + 128 * cg - 1) / (128 * cg)) * ((n + bn - 1) / bn), units = sms / cg, rounds = tiles / units;
+    const uint64_t full = rounds * units, rest = tiles - full;
     for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
-      if (sp > 1 && (double)m * n * sp * 4 > 256e6) break;      // (a quarter of a gigabyte of partial results at most)
-      const double rounds = (double)((tiles * sp + units - 1) / units);
-      double c = fixed + rounds * ((ksteps + sp - 1) / sp * stage + 2500.0);
-      if (sp > 1) c += (double)m * n * (4.0 * sp * 2 + out_elem) / 3000.0 + 4000.0;
-      if (c < least) { least = c; best = {cg, bn, conv, sp}; }
+      const double part = sp > 1 ? (double)rest * sp * cg * 128 * bn : 0.0;
+      if (part * 4 > 256e6) break;      // (a quarter of a gigabyte of partial results at most)
+      double c = fixed + rounds * (ksteps * stage + 2500.0);
+      if (rest) c += (double)((rest * sp + units - 1) / units) * ((ksteps + sp - 1) / sp * stage + 2500.0);
+      if (sp > 1) c += (part * 8 + (double)rest * cg * 128 * bn * out_elem) / 3000.0 + 4000.0;
+      if (c < least) { least = c; best = {cg, bn, conv, (uint32_t)tiles, (uint32_t)(sp > 1 ? full : tiles), sp}; }
+      if (!rest) break;
     }
   };
   for (const auto& sh : shapes[parts == 3]) {
@@ -482,7 +502,7 @@ Plan plan_of(uint64_t m, uint32_t n, uint32_t depth, int parts, size_t out_elem,
 struct Work {
   Plan plan;
   bool pitch;                // dy has to be copied
-  size_t lddy, ldp, ldb;     // pitches of dy, of the partial results and of the converted operand
+  size_t lddy, ldb;          // pitches of dy and of the converted operand
   uint32_t plane;
   size_t pitch_bytes, part_bytes, conv_bytes;
 };
@@ -496,8 +516,7 @@ Work work_of(const GemmArgs& g, bool dw, int sms) {
   w.pitch = ((g.lddy & 7) != 0 && g.t > 1) || (reinterpret_cast<uintptr_t>(g.dy) & 15) != 0;
   w.lddy = w.pitch || g.t == 1 ? up(g.n, 8) : g.lddy;
   w.pitch_bytes = w.pitch ? up(g.t * w.lddy * 2, 256) : 0;
-  w.ldp = up(g.k, 8);
-  w.part_bytes = w.plan.splits > 1 ? up(w.plan.splits * m * w.ldp * 4, 256) : 0;
+  w.part_bytes = (size_t)(w.plan.splits > 1 ? w.plan.tiles - w.plan.full : 0) * w.plan.splits * w.plan.cg * 128 * w.plan.bn * 4;
   w.ldb = up(g.k, 8);
   w.plane = (uint32_t)up(depth, kDepth);
   w.conv_bytes = w.plan.conv ? 0 : (size_t)w.plane * w.ldb * 2;
@@ -508,8 +527,7 @@ Work work_of(const GemmArgs& g, bool dw, int sms) {
 struct Ends {
   const void* dy;
   const __nv_bfloat16* operand;
-  void* out;
-  size_t ldo;
+  float* part;
 };
 
 template <int CG, int BN, int PARTS, bool CONV, bool DW, class O>
@@ -523,13 +541,14 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, i
   a.depth = (uint32_t)(DW ? g.t : g.n);
   a.n = g.k;
   a.ksteps = (a.depth + kDepth - 1) / kDepth;
-  a.out = at.out;
-  a.ldo = at.ldo;
-  a.split_stride = a.m * at.ldo;
+  a.out = g.out;
+  a.ldo = g.ldo;
+  a.part = at.part;
+  a.tiles = w.plan.tiles;
+  a.full = w.plan.full;
   a.splits = w.plan.splits;
   a.tiles_m = (uint32_t)((a.m + 128 * CG - 1) / (128 * CG));
-  a.tiles_n = (a.n + BN - 1) / BN;
-  a.align = row_alignment(at.out, at.ldo * sizeof(O));
+  a.align = row_alignment(g.out, g.ldo * sizeof(O));
   a.err = err;
   CUtensorMap mg, mq;
   cudaError_t e = make_tensor_map(&mg, at.dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
@@ -540,7 +559,7 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, i
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
-  const uint64_t items = (uint64_t)a.tiles_m * a.tiles_n * a.splits, most = sms / CG;
+  const uint64_t items = a.full + (uint64_t)(a.tiles - a.full) * a.splits, most = sms / CG;
   return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, w.pitch || !w.plan.conv, stream, mg, mq, a);
 }
 
@@ -560,10 +579,9 @@ template <bool DW>
 cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t stream, int* launches) {
   const Work w = work_of(g, DW, sms);
   const uint64_t m = DW ? g.n : g.t;
-  const bool f32 = g.out_dtype == STQ_GRAD_F32, split = w.plan.splits > 1;
+  const bool f32 = g.out_dtype == STQ_GRAD_F32;
   uint8_t* base = static_cast<uint8_t*>(ws);
-  float* part = reinterpret_cast<float*>(base + w.pitch_bytes);
-  Ends at = {g.dy, nullptr, split ? part : g.out, split ? w.ldp : g.ldo};
+  Ends at = {g.dy, nullptr, reinterpret_cast<float*>(base + w.pitch_bytes)};
   *launches = 1;
   if (w.pitch) {
     __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base);
@@ -583,17 +601,15 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
     at.operand = to;
     ++*launches;
   }
-  // (an fp32 result takes the operand in three parts; partial results of a bf16 one are fp32 sums of the single operand)
-  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, at, err, sms, stream)
-                  : split ? by_shape<1, DW, float>(g, w, at, err, sms, stream)
-                          : by_shape<1, DW, __nv_bfloat16>(g, w, at, err, sms, stream);
-  if (e != cudaSuccess || !split) return e;
-  const uint64_t items = m * (w.ldp / 4);
-  const unsigned grid = (unsigned)((items + 255) / 256);
-  e = f32 ? launch_with(q8_join_kernel<float>, dim3(grid), dim3(256), 0, 1, true, stream, (const float*)part, m * w.ldp, w.plan.splits, w.ldp, m,
-                        g.k, static_cast<float*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 4))
-          : launch_with(q8_join_kernel<__nv_bfloat16>, dim3(grid), dim3(256), 0, 1, true, stream, (const float*)part, m * w.ldp, w.plan.splits,
-                        w.ldp, m, g.k, static_cast<__nv_bfloat16*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 2));
+  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, at, err, sms, stream) : by_shape<1, DW, __nv_bfloat16>(g, w, at, err, sms, stream);
+  if (e != cudaSuccess || w.plan.splits == 1) return e;
+  const uint32_t count = w.plan.tiles - w.plan.full, tile_m = w.plan.cg * 128, tiles_m = (uint32_t)((m + tile_m - 1) / tile_m);
+  const dim3 grid((unsigned)(((uint64_t)count * tile_m * (w.plan.bn / 4) + 255) / 256));
+  e = f32 ? launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m, (uint32_t)w.plan.bn,
+                        w.plan.full, count, tiles_m, m, g.k, static_cast<float*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 4))
+          : launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m,
+                        (uint32_t)w.plan.bn, w.plan.full, count, tiles_m, m, g.k, static_cast<__nv_bfloat16*>(g.out), g.ldo,
+                        row_alignment(g.out, g.ldo * 2));
   ++*launches;
   return e;
 }

@@ -297,7 +297,7 @@ enum { STQ_ACT_SILU_GATED = 1, STQ_ACT_GELU = 2 };
 int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t rows, uint32_t cols, int8_t* q,
                 uint64_t ldq, float* scale, void* stream);
 
-/* h = x + res (res and hsum NULL: h = x), rstd = 1 / sqrt(mean h^2 + eps) from the unrounded sum,
+/* h = x + res (res and hsum NULL: h = x), rstd = 1 / sqrt(mean h^2 + eps) from the unrounded sum, eps > 0,
  * y = h * rstd * weight as 8-bit rows.  Writes hsum (rounded to dtype), rstd[rows], codes, scales and, if
  * `values` is not NULL, the bf16 values that the codes stand for.  weight: fp32[cols]. */
 int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uint64_t ldres, const float* weight,

@@ -443,23 +443,40 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_
   }
 }
 
-// A gradient whose rows are not aligned to 16 bytes, copied to rows that are (the columns that pad a row are zero).
+// A gradient whose rows are not aligned to 16 bytes, copied to rows that are.  A warp moves 256 columns: its lanes load the
+// 16-byte pieces that hold them (the first and last may reach outside the row, never outside the piece of an element of
+// it), take the next piece from the next lane and shift the two into place.
 __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, size_t ldi, uint64_t rows, uint32_t cols,
                                                        __nv_bfloat16* out, size_t ldo) {
   asm volatile("griddepcontrol.launch_dependents;");
-  const uint32_t per_row = (uint32_t)(ldo / 8);
-  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= rows * per_row) return;
-  const uint64_t r = id / per_row;
-  const uint32_t c = (uint32_t)(id - r * per_row) * 8;
-  const uint16_t* p = reinterpret_cast<const uint16_t*>(in) + r * ldi + c;
-  uint32_t w[4];
+  const uint32_t per_row = (cols + 255) / 256;
+  const uint64_t id = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5), row = id / per_row;
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31;
+  const uint32_t base = (uint32_t)(id - row * per_row) * 256;
+  const uintptr_t from = reinterpret_cast<uintptr_t>(in + row * ldi + base), end = reinterpret_cast<uintptr_t>(in + row * ldi + cols);
+  const uint32_t off = from & 15;
+  const uintptr_t piece = from - off + 16 * lane;
+  uint4 v = make_uint4(0, 0, 0, 0), next = v;
+  if (piece < end) v = *reinterpret_cast<const uint4*>(piece);
+  if (lane == 31 && off && piece + 16 < end) next = *reinterpret_cast<const uint4*>(piece + 16);
+  uint32_t w[8] = {v.x, v.y, v.z, v.w, __shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1),
+                   __shfl_down_sync(0xffffffffu, v.z, 1), __shfl_down_sync(0xffffffffu, v.w, 1)};
+  if (lane == 31) { w[4] = next.x; w[5] = next.y; w[6] = next.z; w[7] = next.w; }
+  if (off & 8) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t lo = c + 2 * i < cols ? p[2 * i] : 0u, hi = c + 2 * i + 1 < cols ? p[2 * i + 1] : 0u;
-    w[i] = lo | hi << 16;
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
   }
-  *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  if (off & 4) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  }
+  if (off & 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  }
+  const uint32_t c = base + lane * 8;
+  if (c < cols) *reinterpret_cast<uint4*>(out + row * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -585,8 +602,8 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   *launches = 1;
   if (w.pitch) {
     __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base);
-    const uint64_t items = g.t * (w.lddy / 8);
-    q8_pitch_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(g.dy), g.lddy, g.t, g.n, to, w.lddy);
+    const uint64_t items = g.t * ((g.n + 255) / 256);      // (a warp each)
+    q8_pitch_kernel<<<(unsigned)((items + 7) / 8), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(g.dy), g.lddy, g.t, g.n, to, w.lddy);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     at.dy = to;

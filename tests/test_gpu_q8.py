@@ -433,6 +433,27 @@ def test_another_stream_and_a_captured_graph(handle):
     own.close()
 
 
+def test_offsets_beyond_32_bits(handle):
+    """Rows 2^31 elements apart: the third begins 2^32 elements into its buffer."""
+    ld = 2 ** 31 + 8
+    big = torch.zeros(2 * ld + 512, dtype=BF, device="cuda")
+    x = hidden(3, 512, 1, BF)
+    far = big.as_strided((3, 512), (ld, 1))
+    far.copy_(x)
+    w, wt = torch.ones(512, device="cuda"), codes(512, 64, 2)
+    for a, b in ((q8.norm(handle, far, w, values=True), q8.norm(handle, x, w, values=True)),):
+        assert torch.equal(a.rows.q, b.rows.q) and torch.equal(a.values, b.values)
+    a, b = q8.act(handle, far, "silu_gated", checkpoint=True), q8.act(handle, x, "silu_gated", checkpoint=True)
+    assert torch.equal(a.rows.q, b.rows.q) and torch.equal(a.checkpoint.q[:, :, :256], b.checkpoint.q[:, :, :256])
+    assert torch.equal(q8.quantize_rows(handle, far).q, q8.quantize_rows(handle, x).q)
+    assert torch.equal(q8.linear_dx(handle, far, wt), q8.linear_dx(handle, x, wt))
+    assert torch.equal(q8.linear_dw(handle, far, codes(3, 64, 3)), q8.linear_dw(handle, x, codes(3, 64, 3)))
+    assert torch.equal(q8.bias_grad(handle, far), q8.bias_grad(handle, x))
+    rstd = torch.ones(3, device="cuda")
+    a, b = q8.norm_backward(handle, far, far, w, rstd), q8.norm_backward(handle, x, x, w, rstd)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 # ---- refusals --------------------------------------------------------------------------------------------------------
 def test_refusals_of_the_binding(handle):
     x, w = hidden(4, 64, 1), torch.ones(64, device="cuda")

@@ -101,18 +101,29 @@ __device__ __forceinline__ uint32_t decode_pair(uint32_t w, int i, const Scale2&
   return bf2_fma(q, s.hi, bf2_mul(q, s.lo));
 }
 
+__device__ __forceinline__ uint64_t f2_pair(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // The same as three pairs whose sum is fl32(s * q): 8 bits of the product to each, cut off, the rest exact.
 __device__ __forceinline__ void decode_pair3(uint32_t w, int i, const Scale2& s, uint32_t (&out)[3]) {
-  float v[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j)      // a byte under the exponent of 2^23 is 2^23 + byte
-    v[j] = (__uint_as_float(__byte_perm(w ^ 0x80808080u, 0x4b000000u, 0x7650 + i + j)) - 8388736.f) * s.s;
+  const uint32_t u = w ^ 0x80808080u, sb = __float_as_uint(s.s);      // a byte under the exponent of 2^23 is 2^23 + byte
+  constexpr uint32_t kMinus = 0xcb000080u;                            // -(2^23 + 128)
+  uint64_t v = f2_mul(f2_add(f2_pair(__byte_perm(u, 0x4b000000u, 0x7650 + i), __byte_perm(u, 0x4b000000u, 0x7651 + i)), f2_pair(kMinus, kMinus)),
+                      f2_pair(sb, sb));
 #pragma unroll
   for (int p = 0; p < 3; ++p) {
-    const uint32_t lo = __float_as_uint(v[0]), hi = __float_as_uint(v[1]);
+    const uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
     out[p] = __byte_perm(lo, hi, 0x7632);
-    v[0] -= __uint_as_float(lo & 0xffff0000u);
-    v[1] -= __uint_as_float(hi & 0xffff0000u);
+    if (p < 2) v = f2_add(v, f2_pair((lo & 0xffff0000u) ^ 0x80000000u, (hi & 0xffff0000u) ^ 0x80000000u));
   }
 }
 

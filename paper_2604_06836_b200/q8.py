@@ -15,6 +15,8 @@ import torch
 
 from . import stq
 
+_F32, _BF16, _I8 = torch.float32, torch.bfloat16, torch.int8
+_empty = torch.empty_strided
 CKPT_BLOCK = 128                                   # STQ_CKPT_BLOCK: columns per scale of a checkpoint
 KINDS = {"silu_gated": 1, "gelu": 2}               # STQ_ACT_*
 _DTYPES = {torch.float32: stq.GRAD_F32, torch.bfloat16: stq.GRAD_BF16}
@@ -126,7 +128,7 @@ def _mat(name: str, t: torch.Tensor, dev: int, dtype=None, rows=None, cols=None)
 
 
 def _vec(name: str, t: torch.Tensor, dev: int, n: int):
-    if t.shape != (n,) or t.dtype is not torch.float32 or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype is not _F32 or not t.is_contiguous():
         raise ValueError(f"{name} is a contiguous float32 vector of {n}")
     if t.get_device() != dev:
         raise ValueError(f"{name} lives on the handle's device")
@@ -134,12 +136,12 @@ def _vec(name: str, t: torch.Tensor, dev: int, n: int):
 
 def _rows(name: str, r: Rows8, dev: int, cols=None, rows=None) -> int:
     q, scale = r
-    ld = _pitch(q, dev, torch.int8, rows, cols)
+    ld = _pitch(q, dev, _I8, rows, cols)
     if ld < 0:
-        _refuse(f"{name}.q", q, dev, torch.int8, rows, cols)
+        _refuse(name + ".q", q, dev, _I8, rows, cols)
     n = q.shape[0]
-    _vec(f"{name}.scale", scale, dev, n)
-    return (ld + 15) // 16 * 16 if n <= 1 else ld
+    _vec(name + ".scale", scale, dev, n)
+    return (ld + 15) & ~15 if n <= 1 else ld
 
 
 def _dtype(name: str, t: torch.Tensor) -> int:
@@ -178,16 +180,12 @@ class _On:
         self._ctx.__exit__(*a)
 
 
-def _stream(dev: int):
-    return _raw_stream(dev) or None
-
-
 def _new(rows: int, cols: int, pitch: int, dtype, device) -> torch.Tensor:
-    return torch.empty_strided((rows, cols), (pitch, 1), dtype=dtype, device=device)
+    return _empty((rows, cols), (pitch, 1), dtype=dtype, device=device)
 
 
 def _new_vec(n: int, device) -> torch.Tensor:
-    return torch.empty_strided((n,), (1,), dtype=torch.float32, device=device)
+    return _empty((n,), (1,), dtype=_F32, device=device)
 
 
 def alloc_rows(rows: int, cols: int, device) -> Rows8:
@@ -207,8 +205,8 @@ def quantize_rows(handle: stq.Handle, x: torch.Tensor, *, out: Rows8 | None = No
     if out is None:
         out = alloc_rows(rows, cols, x.device)
     ldq = _rows("out", out, dev, cols, rows)
-    rc = _lib().stq_q8_rows(handle._h, x.data_ptr(), ldx, dt, rows, cols, out.q.data_ptr(), ldq,
-        out.scale.data_ptr(), _stream(dev))
+    rc = (_fn or _lib()).stq_q8_rows(handle._h, x.data_ptr(), ldx, dt, rows, cols, out.q.data_ptr(), ldq,
+        out.scale.data_ptr(), _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_rows")
     return out
@@ -221,25 +219,29 @@ def norm(handle: stq.Handle, x: torch.Tensor, weight: torch.Tensor, *, residual:
         with _On(stream, (x, weight, residual)):
             return norm(handle, x, weight, residual=residual, eps=eps, values=values)
     dev = handle.device
+    kind = x.dtype
     dt, ldx = _dtype("x", x), _mat("x", x, dev)
     rows, cols = x.shape
     _vec("weight", weight, dev, cols)
-    device = x.device
+    device, pitch = x.device, (cols + 15) & ~15
     h, res_ptr, ldres, h_ptr = x, None, 0, None
     if residual is not None:
-        ldres = _mat("residual", residual, dev, x.dtype, rows, cols)
-        h = _new(rows, cols, cols, x.dtype, device)
+        ldres = _mat("residual", residual, dev, kind, rows, cols)
+        h = _empty((rows, cols), (cols, 1), dtype=kind, device=device)
         res_ptr, h_ptr = residual.data_ptr(), h.data_ptr()
-    r = alloc_rows(rows, cols, device)
-    stats = _new_vec(rows, device)
-    vals = _new(rows, cols, cols, torch.bfloat16, device) if values else None
-    rc = _lib().stq_q8_norm(
+    q = _empty((rows, cols), (pitch, 1), dtype=_I8, device=device)
+    scale = _empty((rows,), (1,), dtype=_F32, device=device)
+    stats = _empty((rows,), (1,), dtype=_F32, device=device)
+    vals, v_ptr = None, None
+    if values:
+        vals = _empty((rows, cols), (cols, 1), dtype=_BF16, device=device)
+        v_ptr = vals.data_ptr()
+    rc = (_fn or _lib()).stq_q8_norm(
         handle._h, x.data_ptr(), ldx, res_ptr, ldres, weight.data_ptr(), eps, dt, rows, cols, h_ptr, cols,
-        stats.data_ptr(), r.q.data_ptr(), (cols + 15) // 16 * 16, r.scale.data_ptr(),
-        None if vals is None else vals.data_ptr(), cols, _stream(dev))
+        stats.data_ptr(), q.data_ptr(), pitch, scale.data_ptr(), v_ptr, cols, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_norm")
-    return NormOut(h, r, stats, vals)
+    return NormOut(h, Rows8(q, scale), stats, vals)
 
 
 def norm_backward(handle: stq.Handle, dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor, *,
@@ -258,10 +260,10 @@ def norm_backward(handle: stq.Handle, dy: torch.Tensor, h: torch.Tensor, weight:
     ldres = 0 if dres is None else _mat("dres", dres, dev, dy.dtype, rows, cols)
     dx = _new(rows, cols, cols, dy.dtype, dy.device)
     dweight = _new_vec(cols, dy.device)
-    rc = _lib().stq_q8_norm_backward(
+    rc = (_fn or _lib()).stq_q8_norm_backward(
         handle._h, dy.data_ptr(), lddy, h.data_ptr(), ldh, weight.data_ptr(), rstd.data_ptr(),
         None if dres is None else dres.data_ptr(), ldres, dt, rows, cols, dx.data_ptr(), cols, dweight.data_ptr(),
-        _stream(dev))
+        _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_norm_backward")
     return dx, dweight
@@ -281,20 +283,22 @@ def act(handle: stq.Handle, z: torch.Tensor, kind: str = "silu_gated", *, checkp
     parts = 2 if kind == "silu_gated" else 1
     rows, cols = z.shape[0], z.shape[1] // parts
     _need(cols * parts == z.shape[1], "a gated activation takes an even number of columns")
-    device, pitch = z.device, (cols + 15) // 16 * 16
-    r = alloc_rows(rows, cols, device)
-    vals = _new(rows, cols, cols, torch.bfloat16, device) if values else None
-    ck, ckq, cks = None, None, None
+    device, pitch = z.device, (cols + 15) & ~15
+    q = _empty((rows, cols), (pitch, 1), dtype=_I8, device=device)
+    scale = _empty((rows,), (1,), dtype=_F32, device=device)
+    vals, v_ptr, ck, ckq, cks = None, None, None, None, None
+    if values:
+        vals = _empty((rows, cols), (cols, 1), dtype=_BF16, device=device)
+        v_ptr = vals.data_ptr()
     if checkpoint:
-        ck = Checkpoint8(torch.empty((rows, parts, pitch), dtype=torch.int8, device=device),
-                         torch.empty((rows, parts, -(-cols // CKPT_BLOCK)), dtype=torch.float32, device=device), cols, kind)
+        ck = Checkpoint8(torch.empty((rows, parts, pitch), dtype=_I8, device=device),
+                         torch.empty((rows, parts, -(-cols // CKPT_BLOCK)), dtype=_F32, device=device), cols, kind)
         ckq, cks = ck.q.data_ptr(), ck.scale.data_ptr()
-    rc = _lib().stq_q8_act(
-        handle._h, z.data_ptr(), ldz, KINDS[kind], dt, rows, cols, r.q.data_ptr(), pitch, r.scale.data_ptr(),
-        None if vals is None else vals.data_ptr(), cols, ckq, pitch, cks, _stream(dev))
+    rc = (_fn or _lib()).stq_q8_act(handle._h, z.data_ptr(), ldz, KINDS[kind], dt, rows, cols, q.data_ptr(), pitch,
+                                    scale.data_ptr(), v_ptr, cols, ckq, pitch, cks, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_act")
-    return ActOut(r, ck, vals)
+    return ActOut(Rows8(q, scale), ck, vals)
 
 
 def act_backward(handle: stq.Handle, da: torch.Tensor, checkpoint: Checkpoint8, *, stream=None) -> torch.Tensor:
@@ -312,8 +316,8 @@ def act_backward(handle: stq.Handle, da: torch.Tensor, checkpoint: Checkpoint8, 
           "the checkpoint lives on the handle's device")
     dt, ldda = _dtype("da", da), _mat("da", da, dev, None, rows, cols)
     dz = _new(rows, parts * cols, parts * cols, da.dtype, da.device)
-    rc = _lib().stq_q8_act_backward(handle._h, da.data_ptr(), ldda, KINDS[kind], dt, rows, cols, q.data_ptr(),
-        pitch, scale.data_ptr(), dz.data_ptr(), parts * cols, _stream(dev))
+    rc = (_fn or _lib()).stq_q8_act_backward(handle._h, da.data_ptr(), ldda, KINDS[kind], dt, rows, cols, q.data_ptr(),
+        pitch, scale.data_ptr(), dz.data_ptr(), parts * cols, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_act_backward")
     return dz
@@ -327,15 +331,16 @@ def linear(handle: stq.Handle, x: Rows8, w: Rows8, *, bias: torch.Tensor | None 
             return linear(handle, x, w, bias=bias, dtype=dtype)
     dev = handle.device
     odt, ldx = _out_dtype(dtype), _rows("x", x, dev)
-    t, k = x.q.shape
+    (xq, xs), (wq, ws) = x, w
+    t, k = xq.shape
     ldw = _rows("w", w, dev, k)
-    n = w.q.shape[0]
+    n = wq.shape[0]
     if bias is not None:
         _vec("bias", bias, dev, n)
-    out = _new(t, n, n, dtype, x.q.device)
-    rc = _lib().stq_q8_linear(
-        handle._h, x.q.data_ptr(), ldx, x.scale.data_ptr(), w.q.data_ptr(), ldw, w.scale.data_ptr(),
-        None if bias is None else bias.data_ptr(), t, n, k, out.data_ptr(), n, odt, _stream(dev))
+    out = _empty((t, n), (n, 1), dtype=dtype, device=xq.device)
+    rc = (_fn or _lib()).stq_q8_linear(
+        handle._h, xq.data_ptr(), ldx, xs.data_ptr(), wq.data_ptr(), ldw, ws.data_ptr(),
+        None if bias is None else bias.data_ptr(), t, n, k, out.data_ptr(), n, odt, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_linear")
     return out
@@ -352,8 +357,8 @@ def linear_dx(handle: stq.Handle, dy: torch.Tensor, w: Rows8, *, dtype=torch.bfl
     lddy = _mat("dy", dy, dev, torch.bfloat16, None, n)
     t = dy.shape[0]
     out = _new(t, k, k, dtype, dy.device)
-    rc = _lib().stq_q8_linear_dx(handle._h, dy.data_ptr(), lddy, w.q.data_ptr(), ldw, w.scale.data_ptr(), t, n, k,
-        out.data_ptr(), k, odt, _stream(dev))
+    rc = (_fn or _lib()).stq_q8_linear_dx(handle._h, dy.data_ptr(), lddy, w.q.data_ptr(), ldw, w.scale.data_ptr(), t, n, k,
+        out.data_ptr(), k, odt, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_linear_dx")
     return out
@@ -371,8 +376,8 @@ def linear_dw(handle: stq.Handle, dy: torch.Tensor, x: Rows8, *, dtype=torch.bfl
     lddy = _mat("dy", dy, dev, torch.bfloat16, t)
     n = dy.shape[1]
     out = _new(n, k, k, dtype, dy.device)
-    rc = _lib().stq_q8_linear_dw(handle._h, dy.data_ptr(), lddy, x.q.data_ptr(), ldx, x.scale.data_ptr(), t, n, k,
-        out.data_ptr(), k, odt, _stream(dev))
+    rc = (_fn or _lib()).stq_q8_linear_dw(handle._h, dy.data_ptr(), lddy, x.q.data_ptr(), ldx, x.scale.data_ptr(), t, n, k,
+        out.data_ptr(), k, odt, _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_linear_dw")
     return out
@@ -387,7 +392,7 @@ def bias_grad(handle: stq.Handle, dy: torch.Tensor, *, stream=None) -> torch.Ten
     dt, ld = _dtype("dy", dy), _mat("dy", dy, dev)
     t, n = dy.shape
     out = _new_vec(n, dy.device)
-    rc = _lib().stq_q8_bias_grad(handle._h, dy.data_ptr(), ld, dt, t, n, out.data_ptr(), _stream(dev))
+    rc = (_fn or _lib()).stq_q8_bias_grad(handle._h, dy.data_ptr(), ld, dt, t, n, out.data_ptr(), _raw_stream(dev))
     if rc:
         handle._check(rc, "stq_q8_bias_grad")
     return out

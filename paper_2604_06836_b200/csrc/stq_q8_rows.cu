@@ -707,12 +707,12 @@ __global__ void __launch_bounds__(1024) q8_norm_bwd_wide_kernel(const NormBwdArg
 template <class T, int VEC>
 __global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, uint32_t cols, float* partial, float* out,
                                                         uint32_t* counters) {
-  __shared__ float sh[8][kUnit];
+  __shared__ __align__(16) float sh[8][kUnit];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t base = blockIdx.x * kUnit, split = blockIdx.y, splits = gridDim.y;
   const uint64_t per = (rows + splits - 1) / splits, r0 = split * per, r1 = min(r0 + per, rows);
   float2 s[4] = {both(0.f), both(0.f), both(0.f), both(0.f)};
-#pragma unroll 4
+#pragma unroll 8
   for (uint64_t r = r0 + warp; r < r1; r += 8) {
     float2 v[4];
     load_unit<T, VEC>(static_cast<const T*>(x.p) + r * x.ld, base, lane, cols, v);
@@ -736,10 +736,18 @@ __global__ void __launch_bounds__(256) q8_colsum_kernel(Mat x, uint64_t rows, ui
   float* mine = partial + (size_t)blockIdx.x * splits * kUnit;
   mine[split * kUnit + threadIdx.x] = sum;
   if (!arrived_last(counters + blockIdx.x, splits)) return;
-  sum = 0.f;
+  // four columns and every fourth split to a thread, then the four shares of a column
+  const uint32_t quarter = threadIdx.x >> 6, at = (threadIdx.x & 63) * 4;
+  float2 lo = both(0.f), hi = both(0.f);
 #pragma unroll 8
-  for (uint32_t i = 0; i < splits; ++i) sum += __ldcg(mine + i * kUnit + threadIdx.x);
-  if (c < cols) out[c] = sum;
+  for (uint32_t i = quarter; i < splits; i += 4) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(mine + i * kUnit + at));
+    lo = add2(lo, make_float2(v.x, v.y));
+    hi = add2(hi, make_float2(v.z, v.w));
+  }
+  *reinterpret_cast<float4*>(&sh[quarter][at]) = make_float4(lo.x, lo.y, hi.x, hi.y);
+  __syncthreads();
+  if (c < cols) out[c] = (sh[0][threadIdx.x] + sh[1][threadIdx.x]) + (sh[2][threadIdx.x] + sh[3][threadIdx.x]);
 }
 
 // ---- backward of the activations, from the checkpoint -------------------------------------------------------------
@@ -916,8 +924,9 @@ BwdShape bwd_shape(uint64_t rows, uint32_t cols, int dtype, int vec, int sms) {
   if (cols > kBwdRegCols) return {0, 0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
   const uint32_t units = (cols + kUnit - 1) / kUnit;
   const int ns = units > kBwdWarps || (units > 1 && dtype == STQ_GRAD_BF16 && vec > 1) ? 2 : 1;
-  const int warps = (int)((units + ns - 1) / ns), gangs = warps >= 8 ? 1 : 8 / warps;
-  const size_t smem = gangs > 1 ? (size_t)warps * ns * kUnit * 4 : 0;      // (at most 8 warps of 2 units then)
+  const int warps = (int)((units + ns - 1) / ns), most_of = ns == 2 ? kBwdWarps : 8;
+  const int gangs = warps >= most_of ? 1 : most_of / warps;
+  const size_t smem = gangs > 1 ? (size_t)warps * ns * kUnit * 4 : 0;      // (at most 8 warps then: 16 KB)
   int per_sm = 1;
   by_type(dtype, [&](auto tv) {
     using T = decltype(tv);

@@ -45,7 +45,7 @@ struct GradArgs {
   uint32_t n, depth, ksteps;           // columns, length of the sum, its stages
   uint32_t tiles_m, tiles;
   uint32_t full, splits;               // tiles from `full` on are shared by `splits` work items each
-  int align;
+  int aligned;                         // the rows of `out` are aligned to 16 bytes: map_o describes it
   int* err;
 };
 
@@ -59,7 +59,7 @@ struct GradShape {
   static constexpr int kStages = kFit < 6 ? kFit : 6;
   static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
   static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
-  static constexpr int kSmem = kStages * kStage + 1024;
+  static constexpr int kSmem = kStages * kStage + 4 * kStageBytes + 1024;
 };
 
 __device__ __forceinline__ uint32_t bf2_add(uint32_t a, uint32_t b) {
@@ -129,14 +129,14 @@ __device__ __forceinline__ void decode_pair3(uint32_t w, int i, const Scale2& s,
 
 template <int CG, int BN, int PARTS, bool CONV, bool DW, class O>
 __global__ void __launch_bounds__((GradShape<CG, BN, PARTS, CONV>::kThreads), 1)
-q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_q, const GradArgs a) {
+q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_o,
+               const GradArgs a) {
   using S = GradShape<CG, BN, PARTS, CONV>;
   constexpr int kStages = S::kStages, kNB = S::kNB;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[4 * kStages + 4];
   __shared__ uint32_t tmem_slot;
-  __shared__ __align__(16) uint8_t stage[4][kStageBytes];
-  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
+  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u, stages = ring + kStages * S::kStage;
   // per stage: codes have landed (this CTA), gradient has landed and codes are converted (both CTAs, at the leader),
   // stage is free; per accumulator: done, read (both CTAs, at the leader)
   const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * kStages, ready = full_g + 8 * kStages;
@@ -337,7 +337,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         const uint32_t acc = n & 1, from = tmem + lanes + acc * BN;
         const bool first = k == k0, last = k1 - k <= (uint32_t)S::kChunk;
         ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-        if (!(ok = all_of_128(ok))) break;       // (the four warps leave together)
+        if (!(ok = all_of<128>(ok))) break;       // (the four warps leave together)
         mma_fence_after();
 #pragma unroll 1
         for (int c = 0; c < BN; c += kC) {
@@ -362,10 +362,11 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           }
           if (part) {
 #pragma unroll
-            for (int i = 0; i < kC; i += 32)
-              store_block<float>(part + c + i, BN, *reinterpret_cast<const float(*)[32]>(&v[i]), 32, 32, 32, lane, stage[quad]);
-          } else {
-            store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
+            for (int i = 0; i < kC; i += 32) store_part(part + c + i, BN, v + i, lane);
+          } else if (!a.aligned) {
+            store_ragged(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), lane, raw + (stages - smem_addr(raw)) + quad * kStageBytes);
+          } else if (rows > 0) {
+            store_block<O>(&map_o, (int)(col + c), (int)row, v, lane, stages + quad * kStageBytes);
           }
         }
         if (PARTS == 3) tmem_store_wait();
@@ -377,6 +378,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
         if (last) break;
       } while (true);
     }
+    store_blocks_done(lane);
   }
   asm volatile("griddepcontrol.launch_dependents;");
   if (!ok) *a.err = 1;
@@ -424,7 +426,7 @@ __global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t
 // The shared tiles from their partial results, added in order: 4 columns to a thread.
 template <class O>
 __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first,
-                                                      uint32_t count, uint32_t tiles_m, uint64_t m, uint32_t n, O* out, size_t ldo, int align) {
+                                                      uint32_t count, uint32_t tiles_m, uint64_t m, uint32_t n, O* out, size_t ldo, bool aligned) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t per_row = tile_n / 4, per_tile = per_row * tile_m;
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
@@ -441,7 +443,7 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_
     s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
   }
   O* o = out + row * ldo + col;
-  if (align >= 16 && col + 4 <= n) {
+  if (aligned && col + 4 <= n) {
     if constexpr (sizeof(O) == 4)
       *reinterpret_cast<float4*>(o) = s;
     else
@@ -576,19 +578,20 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, i
   a.full = w.plan.full;
   a.splits = w.plan.splits;
   a.tiles_m = (uint32_t)((a.m + 128 * CG - 1) / (128 * CG));
-  a.align = row_alignment(g.out, g.ldo * sizeof(O));
+  a.aligned = rows_aligned(g.out, g.ldo * sizeof(O));
   a.err = err;
-  CUtensorMap mg, mq;
+  CUtensorMap mg, mq, mo = {};
   cudaError_t e = make_tensor_map(&mg, at.dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess)
     e = CONV ? make_tensor_map(&mq, q, 1, a.depth, a.n, ldq, kDepth, S::kNB, false)
              : make_tensor_map(&mq, at.operand, 2, w.plane, a.n, w.ldb, kDepth, 64, true);
+  if (e == cudaSuccess && a.aligned) e = make_tensor_map(&mo, g.out, sizeof(O), a.m, a.n, g.ldo, 32, 128 / sizeof(O), true);
   auto* kernel = q8_grad_kernel<CG, BN, PARTS, CONV, DW, O>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t items = a.full + (uint64_t)(a.tiles - a.full) * a.splits, most = sms / CG;
-  return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, w.pitch || !w.plan.conv, stream, mg, mq, a);
+  return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, w.pitch || !w.plan.conv, stream, mg, mq, mo, a);
 }
 
 template <int PARTS, bool DW, class O>
@@ -634,10 +637,10 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   const uint32_t count = w.plan.tiles - w.plan.full, tile_m = w.plan.cg * 128, tiles_m = (uint32_t)((m + tile_m - 1) / tile_m);
   const dim3 grid((unsigned)(((uint64_t)count * tile_m * (w.plan.bn / 4) + 255) / 256));
   e = f32 ? launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m, (uint32_t)w.plan.bn,
-                        w.plan.full, count, tiles_m, m, g.k, static_cast<float*>(g.out), g.ldo, row_alignment(g.out, g.ldo * 4))
+                        w.plan.full, count, tiles_m, m, g.k, static_cast<float*>(g.out), g.ldo, rows_aligned(g.out, g.ldo * 4))
           : launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m,
                         (uint32_t)w.plan.bn, w.plan.full, count, tiles_m, m, g.k, static_cast<__nv_bfloat16*>(g.out), g.ldo,
-                        row_alignment(g.out, g.ldo * 2));
+                        rows_aligned(g.out, g.ldo * 2));
   ++*launches;
   return e;
 }

@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kBK = 128;               // bytes (= elements) of the sum per stage
 constexpr int kMmaK = 32;              // elements of the sum per product instruction
-constexpr int kThreads8 = 192;
+constexpr int kThreads8 = 192;         // split kernel: two working warps and four that write
+constexpr int kWriters = 8;            // pairs: writing warps, two to each quarter of the rows
 
 struct LinearArgs {
   const float* xs;
@@ -29,35 +30,36 @@ struct LinearArgs {
   uint32_t n, ksteps;
   uint32_t tiles_m, tiles_n;
   uint32_t box;                        // split kernel: tokens per tensor copy
-  int align;                           // bytes that the rows of `out` are aligned to (32, 16, or less)
+  int aligned;                         // the rows of `out` are aligned to 16 bytes: map_o describes it
   int* err;
 };
 
 // ---- batches ---------------------------------------------------------------------------------------------------------
 // Warp 0 keeps a ring of shared-memory stages full with tensor copies (128 bytes of the sum at a time, 128-byte swizzle,
 // out-of-range rows and columns read as zero), warp 1 issues the products into one of two accumulators in tensor
-// memory, warps 2-5 turn the other accumulator into results.  Each CTA of a pair holds 128 tokens and half of the
-// channels of the tile; the leader issues the products of both.
+// memory, warps 2-9 turn the other accumulator into results.  Each CTA of a pair holds 128 tokens and half of the
+// channels of the tile; the leader issues the products of both.  Writing a tile takes as long as 20 stages of products
+// with four warps, half of that with eight (8192 x 1600 x 6400, 13 stages to a tile: 80 -> 67 us).
 template <int BN>
 struct LinearShape {
   static constexpr int kA = 128 * kBK, kB = BN / 2 * kBK, kStage = kA + kB;
-  static constexpr int kFit = (200 * 1024) / kStage;
+  static constexpr int kFit = (180 * 1024) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kCols = 2 * BN;                         // tensor memory: two accumulators
-  static constexpr int kSmem = kStages * kStage + 1024;        // (+ alignment of the swizzle atoms)
+  static constexpr int kSmem = kStages * kStage + kWriters * kStageBytes + 1024;      // (+ alignment of the swizzle atoms)
 };
 
 template <int BN, class O>
-__global__ void __launch_bounds__(kThreads8, 1)
-q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const LinearArgs a) {
+__global__ void __launch_bounds__(64 + 32 * kWriters, 1)
+q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_o,
+                 const LinearArgs a) {
   using S = LinearShape<BN>;
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
   __shared__ uint32_t tmem_slot;
-  __shared__ float scale_n[2][BN], bias_n[2][BN];
-  __shared__ __align__(16) uint8_t stage[4][kStageBytes];
-  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u;
+  __shared__ float4 scale_n[2][BN / 4], bias_n[2][BN / 4];
+  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u, stages = ring + kStages * S::kStage;
   const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages;
   const uint32_t freed = done + 16;      // accumulators are read (both CTAs, at the leader)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -72,7 +74,7 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(done + 8 * i, 1);
-      bar_init(freed + 8 * i, 8);
+      bar_init(freed + 8 * i, 2 * kWriters);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -125,38 +127,49 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
       }
     }
   } else {
-    const int quad = warp & 3, thread = threadIdx.x - 64;     // (a warp reaches the 32 lanes 32 * (warp % 4) of tensor memory)
+    // a warp reaches the 32 lanes 32 * (warp % 4) of tensor memory; it takes half of their columns
+    const int quad = warp & 3, half = (warp - 2) / 4, thread = threadIdx.x - 64;
     const uint32_t freed0 = peer_addr(freed, 0);
     uint32_t n = 0;
     for (uint32_t tile = unit; ok && tile < tiles; tile += units, ++n) {
       const uint32_t acc = n & 1;
       const uint64_t row = (uint64_t)(tile % a.tiles_m) * 256 + 128 * rank + quad * 32;
       const uint32_t col = tile / a.tiles_m * BN;
-      for (int c = thread; c < BN; c += 128) {
-        scale_n[acc][c] = col + c < a.n ? a.ws[col + c] : 0.f;
-        bias_n[acc][c] = a.bias && col + c < a.n ? a.bias[col + c] : 0.f;
+      for (int c = thread; c < BN; c += 32 * kWriters) {
+        reinterpret_cast<float*>(scale_n[acc])[c] = col + c < a.n ? a.ws[col + c] : 0.f;
+        reinterpret_cast<float*>(bias_n[acc])[c] = a.bias && col + c < a.n ? a.bias[col + c] : 0.f;
       }
       const float xs = row + lane < a.t ? a.xs[row + lane] : 0.f;
       ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-      if (!(ok = all_of_128(ok))) break;       // (the four warps leave together; the scales above are visible to all)
+      if (!(ok = all_of<32 * kWriters>(ok))) break;       // (the writing warps leave together; the scales above are visible to all)
       mma_fence_after();
       const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN;
       O* out = static_cast<O*>(a.out) + row * a.ldo + col;
       const int rows = row >= a.t ? 0 : (int)min((uint64_t)32, a.t - row);
       constexpr int kC = 128 / sizeof(O);
 #pragma unroll 1
-      for (int c = 0; c < BN; c += kC) {
+      for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += kC) {
         if (col + c >= a.n) break;
         float v[kC];
         load_block(from + c, v);
 #pragma unroll
-        for (int i = 0; i < kC; ++i) v[i] = fmaf((float)__float_as_int(v[i]), xs * scale_n[acc][c + i], bias_n[acc][c + i]);
-        store_block(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), a.align, lane, stage[quad]);
+        for (int i = 0; i < kC; i += 4) {
+          const float4 ws = scale_n[acc][(c + i) / 4], b = bias_n[acc][(c + i) / 4];
+          v[i] = fmaf((float)__float_as_int(v[i]), xs * ws.x, b.x);
+          v[i + 1] = fmaf((float)__float_as_int(v[i + 1]), xs * ws.y, b.y);
+          v[i + 2] = fmaf((float)__float_as_int(v[i + 2]), xs * ws.z, b.z);
+          v[i + 3] = fmaf((float)__float_as_int(v[i + 3]), xs * ws.w, b.w);
+        }
+        if (!a.aligned)
+          store_ragged(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), lane, raw + (stages - smem_addr(raw)) + (warp - 2) * kStageBytes);
+        else if (rows > 0)
+          store_block<O>(&map_o, (int)(col + c), (int)row, v, lane, stages + (warp - 2) * kStageBytes);
       }
       mma_fence_before();
       __syncwarp();
       if (lane == 0) bar_arrive_leader<2>(freed + 8 * acc, freed0 + 8 * acc, leader);
     }
+    store_blocks_done(lane);
   }
   if (!ok) *a.err = 1;
   __syncwarp();
@@ -479,7 +492,7 @@ LinearArgs args_of(const GemmArgs& g, int tile_m, int tile_n, int* err) {
   a.t = g.t; a.n = g.n; a.ksteps = (g.k + kBK - 1) / kBK;
   a.tiles_m = (uint32_t)((g.t + tile_m - 1) / tile_m);
   a.tiles_n = (g.n + tile_n - 1) / tile_n;
-  a.align = row_alignment(g.out, g.ldo * sizeof(O));
+  a.aligned = rows_aligned(g.out, g.ldo * sizeof(O));
   a.err = err;
   return a;
 }
@@ -488,14 +501,15 @@ template <int BN, class O>
 cudaError_t launch_pairs(const GemmArgs& g, int sms, int* err, cudaStream_t stream) {
   using S = LinearShape<BN>;
   const LinearArgs a = args_of<O>(g, 256, BN, err);
-  CUtensorMap mx, mw;
+  CUtensorMap mx, mw, mo = {};
   cudaError_t e = make_tensor_map(&mx, g.xq, 1, g.t, g.k, g.ldx, 128, kBK, true);
   if (e == cudaSuccess) e = make_tensor_map(&mw, g.wq, 1, g.n, g.k, g.ldw, BN / 2, kBK, true);
+  if (e == cudaSuccess && a.aligned) e = make_tensor_map(&mo, g.out, sizeof(O), g.t, g.n, g.ldo, 32, 128 / sizeof(O), true);
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(q8_linear_kernel<BN, O>, S::kSmem, g.device, seen);
   if (e != cudaSuccess) return e;
   const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n, most = sms / 2;
-  return launch_with(q8_linear_kernel<BN, O>, (unsigned)(tiles < most ? tiles : most) * 2, kThreads8, S::kSmem, 2, false, stream, mx, mw, a);
+  return launch_with(q8_linear_kernel<BN, O>, (unsigned)(tiles < most ? tiles : most) * 2, 64 + 32 * kWriters, S::kSmem, 2, false, stream, mx, mw, mo, a);
 }
 
 template <int BN, class O>

@@ -214,41 +214,74 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// True if `ok` is true in all of the 128 threads that share barrier 1 (whole warps); a barrier for them too.
-__device__ __forceinline__ bool all_of_128(bool ok) {
+// True if `ok` is true in all of the N threads that share barrier 1 (whole warps); a barrier for them too.
+template <int N>
+__device__ __forceinline__ bool all_of(bool ok) {
   uint32_t r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)ok)
+      : "r"((uint32_t)ok), "n"(N)
       : "memory");
   return r != 0;
 }
 
-// A warp's block of 32 rows x 128 bytes, lane = row, to global memory; `rows` x `cols` of it lie inside the matrix.
-// Rows aligned to 32 or 16 bytes are written by their lanes.  Others go through shared memory (kStageBytes a warp): a row
-// is laid down there as far from a 16-byte boundary as it lies in global memory, so that all but its first and last
-// pieces move 16 bytes at a time, eight neighbouring lanes to a row.
-constexpr int kStageRow = 144, kStageBytes = 32 * kStageRow;
+// ---- results ------------------------------------------------------------------------------------------------------
+// A warp's block of 32 rows x 128 bytes, lane = row.
+constexpr int kStageRow = 144, kStageBytes = 5 * 1024;      // shared memory for it, a multiple of the swizzle's 1024 bytes
+
+// To a matrix whose rows are aligned to 16 bytes: through shared memory (128-byte swizzle: eight lanes write eight
+// different pieces) and one tensor copy, which leaves out what lies outside the matrix.  The next block waits until the
+// copy has read this one.
 template <class O>
-__device__ __forceinline__ void store_block(O* base, size_t ld, const float (&v)[128 / sizeof(O)], int rows, int cols, int align,
-                                            int lane, uint8_t* stage) {
-  constexpr int C = 128 / sizeof(O), kPiece = 16 / sizeof(O);
-  if (align >= 16 && cols == C) {
-    if (lane >= rows) return;
-    uint8_t* p = reinterpret_cast<uint8_t*>(base + (size_t)lane * ld);
-    uint32_t w[32];
+__device__ __forceinline__ void block_words(const float (&v)[128 / sizeof(O)], uint32_t (&w)[32]) {
+  constexpr int C = 128 / sizeof(O);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) w[i] = sizeof(O) == 2 ? bf16_pair(v[2 * i % C], v[(2 * i + 1) % C]) : __float_as_uint(v[i % C]);
-    if (align == 32) {
+  for (int i = 0; i < 32; ++i) w[i] = sizeof(O) == 2 ? bf16_pair(v[2 * i % C], v[(2 * i + 1) % C]) : __float_as_uint(v[i % C]);
+}
+template <class O>
+__device__ __forceinline__ void store_block(const CUtensorMap* map, int x, int y, const float (&v)[128 / sizeof(O)], int lane, uint32_t stage) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  uint32_t w[32];
+  block_words<O>(v, w);
+  __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) store32(p + 32 * i, *reinterpret_cast<const uint32_t(*)[8]>(&w[8 * i]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(p + 16 * i) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-    }
-    return;
+  for (int i = 0; i < 8; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(w[4 * i]),
+                 "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                 : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(stage)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
+}
+// Before a warp ends (or reuses its shared memory for anything else): its copies are done.
+__device__ __forceinline__ void store_blocks_done(int lane) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  __syncwarp();
+}
+
+// To workspace rows of `ld` floats, aligned to 32 bytes.
+__device__ __forceinline__ void store_part(float* base, size_t ld, const float* v, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(v[8 * i + j]);
+    store32(base + lane * ld + 8 * i, w);
+  }
+}
+
+// To a matrix whose rows are not: `rows` x `cols` of the block lie inside it.  A row is laid down in shared memory as far
+// from a 16-byte boundary as it lies in global memory, so that all but its first and last pieces move 16 bytes at a time,
+// eight neighbouring lanes to a row.
+template <class O>
+__device__ __forceinline__ void store_ragged(O* base, size_t ld, const float (&v)[128 / sizeof(O)], int rows, int cols, int lane,
+                                             uint8_t* stage) {
+  constexpr int C = 128 / sizeof(O), kPiece = 16 / sizeof(O);
   auto off = [&](int r) { return (int)(reinterpret_cast<uintptr_t>(base + (size_t)r * ld) & 15); };
   __syncwarp();
   {

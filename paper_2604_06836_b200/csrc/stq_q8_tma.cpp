@@ -19,7 +19,7 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* p, int elem, uint64_t 
   if (!encode) return cudaErrorNotSupported;
   const cuuint64_t dims[2] = {cols, rows}, strides[1] = {pitch * (uint64_t)elem};
   const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
-  const CUresult r = encode(map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2,
+  const CUresult r = encode(map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2,
                             const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                             swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);

@@ -8,16 +8,13 @@
 
 namespace stq {
 
-// `elem` 1: bytes, 2: bf16.  The box is box_cols x box_rows elements, box_cols * elem <= 128 bytes; base and pitch are
+// `elem` 1: bytes, 2: bf16, 4: fp32.  The box is box_cols x box_rows elements, box_cols * elem <= 128 bytes; base and pitch are
 // multiples of 16 bytes; elements outside rows x cols read as zero.
 cudaError_t make_tensor_map(CUtensorMap* map, const void* p, int elem, uint64_t rows, uint64_t cols, uint64_t pitch,
                             uint32_t box_rows, uint32_t box_cols, bool swizzle);
 
-// Largest of 32, 16, 1 bytes that every row of a matrix with this pitch in bytes is aligned to.
-inline int row_alignment(const void* p, size_t pitch) {
-  const uintptr_t b = reinterpret_cast<uintptr_t>(p) | pitch;
-  return (b & 31) == 0 ? 32 : (b & 15) == 0 ? 16 : 1;
-}
+// Whether every row of a matrix with this pitch in bytes is aligned to 16 bytes.
+inline bool rows_aligned(const void* p, size_t pitch) { return ((reinterpret_cast<uintptr_t>(p) | pitch) & 15) == 0; }
 
 // Lets a kernel take `bytes` of dynamic shared memory; `seen` has a bit for each device where that is settled.
 template <class K>

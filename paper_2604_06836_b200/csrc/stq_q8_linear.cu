@@ -38,8 +38,9 @@ struct LinearArgs {
 // Warp 0 keeps a ring of shared-memory stages full with tensor copies (128 bytes of the sum at a time, 128-byte swizzle,
 // out-of-range rows and columns read as zero), warp 1 issues the products into one of two accumulators in tensor
 // memory, warps 2-9 turn the other accumulator into results.  Each CTA of a pair holds 128 tokens and half of the
-// channels of the tile; the leader issues the products of both.  Writing a tile takes as long as 20 stages of products
-// with four warps, half of that with eight (8192 x 1600 x 6400, 13 stages to a tile: 80 -> 67 us).
+// channels of the tile; the leader issues the products of both.  Where a tile has few stages the writing bounds the
+// kernel: with four warps and stores by row it took as long as 20 stages of products; eight warps and tensor copies of
+// whole lines take 8192 x 768 x 2304 from 22.7 to 17.1 us and 8192 x 1600 x 6400 (13 stages) from 84 to 76 at the power cap.
 template <int BN>
 struct LinearShape {
   static constexpr int kA = 128 * kBK, kB = BN / 2 * kBK, kStage = kA + kB;

@@ -268,15 +268,21 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           sc[p] = k < k1 && c < a.depth ? __ldg(a.scale + c) : 0.f;
         }
       };
-      const uint32_t mine = (group + it) % kGroups;      // (kGroups = 2: the first stage of this item that is the group's)
+      const uint32_t mine = (group + kGroups - it % kGroups) % kGroups;      // the group's first stage of this item
       scales(k0 + mine);
-      for (uint32_t k = k0 + mine; k < k1; k += kGroups) {
+      for (uint32_t k = k0; k < k1; ++k) {
+        // A barrier tells only whether its latest phase has the parity asked for.  Where a slot of the ring serves both
+        // groups in turn, a group that skipped the other's stages could take the phase before the last for the one it
+        // needs (copies may complete out of order), so there every group waits for every stage.
         const uint32_t i = it + k - k0, s = i % kStages, ph = (i / kStages) & 1;
+        const bool own = i % kGroups == (uint32_t)group;
+        if (kStages % kGroups == 0 && !own) continue;
+        if (!(ok = bar_wait(full_q + 8 * s, ph))) break;
+        if (!own) continue;
         Scale2 now[kPasses];
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) now[p] = scale2_of(sc[p]);
         scales(k + kGroups);                   // (for the group's next stage, so that their latency is hidden)
-        if (!(ok = bar_wait(full_q + 8 * s, ph))) break;
         const uint32_t from = ring + s * S::kStage + S::kA, to = from + S::kQ;
         uint32_t q[kPasses][4];
 #pragma unroll

@@ -45,7 +45,7 @@ struct GradArgs {
   uint32_t n, depth, ksteps;           // columns, length of the sum, its stages
   uint32_t tiles_m, tiles;
   uint32_t full, splits;               // tiles from `full` on are shared by `splits` work items each
-  int aligned;                         // the rows of `out` are aligned to 16 bytes: map_o describes it
+  int aligned;                         // tensor copies can write `out`: map_o describes it
   int* err;
 };
 
@@ -584,7 +584,7 @@ cudaError_t launch(const GemmArgs& g, const Work& w, const Ends& at, int* err, i
   a.full = w.plan.full;
   a.splits = w.plan.splits;
   a.tiles_m = (uint32_t)((a.m + 128 * CG - 1) / (128 * CG));
-  a.aligned = rows_aligned(g.out, g.ldo * sizeof(O));
+  a.aligned = copy_fits(g.out, g.k * sizeof(O), g.ldo * sizeof(O));
   a.err = err;
   CUtensorMap mg, mq, mo = {};
   cudaError_t e = make_tensor_map(&mg, at.dy, 2, g.t, g.n, w.lddy, DW ? 64 : 128, 64, true);

@@ -30,7 +30,7 @@ struct LinearArgs {
   uint32_t n, ksteps;
   uint32_t tiles_m, tiles_n;
   uint32_t box;                        // split kernel: tokens per tensor copy
-  int aligned;                         // the rows of `out` are aligned to 16 bytes: map_o describes it
+  int aligned;                         // tensor copies can write `out`: map_o describes it
   int* err;
 };
 
@@ -493,7 +493,7 @@ LinearArgs args_of(const GemmArgs& g, int tile_m, int tile_n, int* err) {
   a.t = g.t; a.n = g.n; a.ksteps = (g.k + kBK - 1) / kBK;
   a.tiles_m = (uint32_t)((g.t + tile_m - 1) / tile_m);
   a.tiles_n = (g.n + tile_n - 1) / tile_n;
-  a.aligned = rows_aligned(g.out, g.ldo * sizeof(O));
+  a.aligned = copy_fits(g.out, g.n * sizeof(O), g.ldo * sizeof(O));
   a.err = err;
   return a;
 }

@@ -230,7 +230,7 @@ __device__ __forceinline__ bool all_of(bool ok) {
 // A warp's block of 32 rows x 128 bytes, lane = row.
 constexpr int kStageRow = 144, kStageBytes = 5 * 1024;      // shared memory for it, a multiple of the swizzle's 1024 bytes
 
-// To a matrix whose rows are aligned to 16 bytes: through shared memory (128-byte swizzle: eight lanes write eight
+// To a matrix whose rows are aligned to 16 bytes and whole numbers of them: through shared memory (128-byte swizzle: eight lanes write eight
 // different pieces) and one tensor copy, which leaves out what lies outside the matrix.  The next block waits until the
 // copy has read this one.
 template <class O>

@@ -16,6 +16,10 @@ cudaError_t make_tensor_map(CUtensorMap* map, const void* p, int elem, uint64_t 
 // Whether every row of a matrix with this pitch in bytes is aligned to 16 bytes.
 inline bool rows_aligned(const void* p, size_t pitch) { return ((reinterpret_cast<uintptr_t>(p) | pitch) & 15) == 0; }
 
+// Whether tensor copies can write a matrix: rows on 16 bytes, and whole numbers of 16 bytes (at a row's end a copy to memory
+// is cut off by pieces of 16 bytes, not by elements, and would write into what lies between the rows).
+inline bool copy_fits(const void* p, size_t row, size_t pitch) { return rows_aligned(p, row | pitch); }
+
 // Lets a kernel take `bytes` of dynamic shared memory; `seen` has a bit for each device where that is settled.
 template <class K>
 cudaError_t allow_smem(K kernel, size_t bytes, int device, std::atomic<uint64_t>& seen) {

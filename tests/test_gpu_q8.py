@@ -454,6 +454,46 @@ def test_offsets_beyond_32_bits(handle):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("extra", [8, 3, 1])
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("t,n,k", [(5, 72, 40), (90, 136, 264), (700, 1030, 520), (700, 1032, 513)])
+def test_results_with_a_pitch_leave_what_lies_between_rows(handle, t, n, k, dtype, extra):
+    """The C calls write rows of any pitch, on any aligned address, and nothing between them."""
+    L, h, dt = q8._lib(), handle._h, 0 if dtype == F32 else 1
+    x, w = codes(t, k, 1, 0.05), codes(n, k, 2, 0.002)
+    dy = torch.randn(t, n, device="cuda", generator=gen(3)).to(BF)
+
+    def into(rows, cols, call):
+        ld = cols + extra
+        buf = torch.full((rows * ld + 64,), 7.0, device="cuda").to(dtype)
+        for shift in (0, 1, 8):
+            buf.fill_(7.0)
+            assert call(buf.data_ptr() + shift * buf.element_size(), ld) == 0
+            body = buf[shift:shift + rows * ld].view(rows, ld)
+            assert (body[:, cols:] == 7.0).all() and (buf[:shift] == 7.0).all() and (buf[shift + rows * ld:] == 7.0).all()
+            yield body[:, :cols]
+
+    P = torch.Tensor.data_ptr
+    ldx, ldw = x.q.stride(0), w.q.stride(0)
+    for got in into(t, n, lambda o, ld: L.stq_q8_linear(h, P(x.q), ldx, P(x.scale), P(w.q), ldw, P(w.scale), None, t, n, k, o, ld, dt, None)):
+        assert torch.equal(got, q8.linear(handle, x, w, dtype=dtype))
+    for got in into(t, k, lambda o, ld: L.stq_q8_linear_dx(h, P(dy), n, P(w.q), ldw, P(w.scale), t, n, k, o, ld, dt, None)):
+        assert torch.equal(got, q8.linear_dx(handle, dy, w, dtype=dtype))
+    for got in into(n, k, lambda o, ld: L.stq_q8_linear_dw(h, P(dy), n, P(x.q), ldx, P(x.scale), t, n, k, o, ld, dt, None)):
+        assert torch.equal(got, q8.linear_dw(handle, dy, x, dtype=dtype))
+    z = hidden(t, 2 * k, 4, dtype)
+    ck = q8.act(handle, z, "silu_gated", checkpoint=True).checkpoint
+    da = hidden(t, k, 5, dtype)
+    for got in into(t, 2 * k, lambda o, ld: L.stq_q8_act_backward(h, P(da), k, 1, dt, t, k, P(ck.q), ck.q.shape[2], P(ck.scale), o, ld, None)):
+        assert torch.equal(got, q8.act_backward(handle, da, ck))
+    g, rstd, dw = torch.ones(k, device="cuda"), torch.ones(t, device="cuda"), torch.empty(k, device="cuda")
+    hh = hidden(t, k, 6, dtype)
+    for got in into(t, k, lambda o, ld: L.stq_q8_norm_backward(h, P(da), k, P(hh), k, P(g), P(rstd), None, 0, dt, t, k, o, ld, P(dw), None)):
+        xh, up = hh.double(), da.double()          # (rstd and weight are 1)
+        want, size = up - xh * (up * xh).mean(1, keepdim=True), up.abs() + xh.abs() * (up * xh).abs().mean(1, keepdim=True)
+        assert ((got.double() - want).abs() <= 64 * U * size + (UB * 1.01 * want.abs() if dtype == BF else 0)).all()
+
+
 # ---- refusals --------------------------------------------------------------------------------------------------------
 def test_refusals_of_the_binding(handle):
     x, w = hidden(4, 64, 1), torch.ones(64, device="cuda")

@@ -454,6 +454,34 @@ def test_offsets_beyond_32_bits(handle):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("t,n,k", [(1, 70, 41), (7, 70, 41), (40, 77, 131), (300, 1283, 769), (2500, 1285, 1030), (8200, 1603, 1603)])
+def test_what_lies_between_rows_does_not_matter(handle, t, n, k):
+    """Codes and gradients whose rows are followed by anything up to their pitch: the largest codes, NaN."""
+    def dirty(r):
+        rows, cols = r.q.shape
+        full = torch.full((rows, (cols + 15) // 16 * 16), 127, dtype=torch.int8, device="cuda")
+        full[:, :cols] = r.q
+        return q8.Rows8(full[:, :cols], r.scale)
+
+    def clean(r):
+        rows, cols = r.q.shape
+        full = torch.zeros((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device="cuda")
+        full[:, :cols] = r.q
+        return q8.Rows8(full[:, :cols], r.scale)
+
+    x, w = codes(t, k, 1, 0.05), codes(n, k, 2, 0.002)
+    dy = torch.randn(t, n, device="cuda", generator=gen(3)).to(BF)
+    wide = torch.full((t, (n + 7) // 8 * 8), float("nan"), device="cuda", dtype=BF)
+    wide[:, :n] = dy
+    for dtype in (F32, BF):
+        assert torch.equal(q8.linear(handle, dirty(x), dirty(w), dtype=dtype), q8.linear(handle, clean(x), clean(w), dtype=dtype))
+        for g in (dy, wide[:, :n]):
+            dx, dw = q8.linear_dx(handle, g, dirty(w), dtype=dtype), q8.linear_dw(handle, g, dirty(x), dtype=dtype)
+            assert torch.equal(dx, q8.linear_dx(handle, dy, clean(w), dtype=dtype))
+            assert torch.equal(dw, q8.linear_dw(handle, dy, clean(x), dtype=dtype))
+    assert torch.equal(q8.bias_grad(handle, wide[:, :n]).isnan(), torch.zeros(n, dtype=torch.bool, device="cuda"))
+
+
 @pytest.mark.parametrize("extra", [8, 3, 1])
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("t,n,k", [(5, 72, 40), (90, 136, 264), (700, 1030, 520), (700, 1032, 513)])

@@ -525,6 +525,11 @@ int stq_destroy(stq_handle* h) {
   cudaFree(h->d_seg_sums);
   cudaFree(h->d_arena);
   cudaFree(h->d_q8);
+  while (stq::KeptBuffer* kept = h->q8_kept) {
+    h->q8_kept = kept->next;
+    cudaFree(kept->p);
+    delete kept;
+  }
   cudaFree(h->d_q8_counters);
   for (cudaStream_t st : h->host_streams)
     if (st) cudaStreamDestroy(st);

@@ -10,6 +10,13 @@
 #include "stq_internal.h"
 #include "stq_q8.h"
 
+namespace stq {
+struct KeptBuffer {
+  void* p;
+  KeptBuffer* next;
+};
+}  // namespace stq
+
 struct stq_handle {
   int device = 0;
   int sm_count = 0;
@@ -69,6 +76,8 @@ struct stq_handle {
   // workspace of the 8-bit operators: partial sums of split products and column sums, a pitched copy of a gradient
   uint8_t* d_q8 = nullptr;
   size_t d_q8_cap = 0;
+  bool q8_in_graph = false;            // a captured graph uses d_q8: when it is replaced it stays until the handle goes,
+  stq::KeptBuffer* q8_kept = nullptr;  // in this list
   uint32_t* d_q8_counters = nullptr;   // kQ8Counters of them, zero between launches
 };
 

@@ -1,4 +1,6 @@
 // C-ABI host layer of the 8-bit operators: argument checks, workspace, launches.
+#include <new>
+
 #include "stq_handle.h"
 #include "stq_q8.h"
 
@@ -59,9 +61,30 @@ int check_codes(const void* q, uint64_t ldq, uint64_t cols, const void* scale) {
     if (rc__ != STQ_OK) return rc__; \
   } while (0)
 
+// The workspace of a call on `stream`.  It grows by being replaced.  A graph that was captured with the old buffer goes on
+// using it whenever it is replayed, so such a buffer is not freed.
 template <class T>
-int workspace(stq_handle* h, size_t count, T** out) {
-  STQ_TRY(grow(h, h->d_q8, h->d_q8_cap, count * sizeof(T)));
+int workspace(stq_handle* h, size_t count, cudaStream_t stream, T** out) {
+  const size_t need = count * sizeof(T);
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  STQ_CUDA(h, cudaStreamIsCapturing(stream, &status));
+  const bool capturing = status != cudaStreamCaptureStatusNone;
+  if (need > h->d_q8_cap) {
+    if (capturing) {      // (an allocation would end the capture)
+      h->cuda_err = "the workspace cannot grow while the stream is captured: make a call of this size before";
+      return STQ_E_WORKSPACE;
+    }
+    if (h->q8_in_graph) {
+      auto* kept = new (std::nothrow) stq::KeptBuffer{h->d_q8, h->q8_kept};
+      if (!kept) return STQ_E_WORKSPACE;
+      h->q8_kept = kept;
+      h->d_q8 = nullptr;
+      h->d_q8_cap = 0;
+      h->q8_in_graph = false;
+    }
+    STQ_TRY(grow(h, h->d_q8, h->d_q8_cap, need));
+  }
+  h->q8_in_graph |= capturing;
   *out = reinterpret_cast<T*>(h->d_q8);
   return STQ_OK;
 }
@@ -164,7 +187,7 @@ int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const voi
   a.rows = rows; a.cols = cols;
   a.ldp = ((size_t)cols + 7) / 8 * 8;
   a.counters = h->d_q8_counters;
-  STQ_TRY(workspace(h, stq::q8_norm_bwd_partial(dtype, a, h->sm_count), &a.partial));
+  STQ_TRY(workspace(h, stq::q8_norm_bwd_partial(dtype, a, h->sm_count), s, &a.partial));
   int launches = 0;
   STQ_CUDA(h, stq::launch_q8_norm_bwd(dtype, a, h->sm_count, s, &launches));
   h->launches += launches;
@@ -277,10 +300,11 @@ int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.t = t; a.n = n; a.k = k;
   a.device = h->device;
   STQ_CUDA(h, cudaSetDevice(h->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
   uint8_t* ws = nullptr;
   int launches = 0;
-  if (const size_t need = stq::q8_grad_workspace(a, false, h->sm_count)) STQ_TRY(workspace(h, need, &ws));
-  STQ_CUDA(h, stq::launch_q8_linear_dx(a, ws, h->sm_count, h->d_err, static_cast<cudaStream_t>(stream), &launches));
+  if (const size_t need = stq::q8_grad_workspace(a, false, h->sm_count)) STQ_TRY(workspace(h, need, s, &ws));
+  STQ_CUDA(h, stq::launch_q8_linear_dx(a, ws, h->sm_count, h->d_err, s, &launches));
   h->launches += launches;
   return STQ_OK;
 }
@@ -308,7 +332,7 @@ int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
   a.device = h->device;
   uint8_t* ws = nullptr;
   int launches = 0;
-  if (const size_t need = stq::q8_grad_workspace(a, true, h->sm_count)) STQ_TRY(workspace(h, need, &ws));
+  if (const size_t need = stq::q8_grad_workspace(a, true, h->sm_count)) STQ_TRY(workspace(h, need, s, &ws));
   STQ_CUDA(h, stq::launch_q8_linear_dw(a, ws, h->sm_count, h->d_err, s, &launches));
   h->launches += launches;
   return STQ_OK;
@@ -328,7 +352,7 @@ int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, ui
   if (clash(o, in)) return STQ_E_ALIAS;
   const uint32_t splits = stq::q8_colsum_splits(t, n, h->sm_count);
   float* partial = nullptr;
-  if (const size_t need = stq::q8_colsum_partial(n, splits)) STQ_TRY(workspace(h, need, &partial));
+  if (const size_t need = stq::q8_colsum_partial(n, splits)) STQ_TRY(workspace(h, need, s, &partial));
   STQ_CUDA(h, stq::launch_q8_colsum(dtype, {const_cast<void*>(dy), lddy}, t, n, splits, partial, h->d_q8_counters, db, s));
   h->launches++;
   return STQ_OK;

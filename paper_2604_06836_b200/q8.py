@@ -4,7 +4,9 @@ product of 8-bit rows with 8-bit weights, and their gradients, which read what t
 Thin binding over the ``stq_q8_*`` calls of libstq, like ``stq``: torch supplies memory and streams, every
 operator runs in the library's kernels.  All matrices are two-dimensional with unit stride along a row; any row pitch
 is taken.  Each call enqueues its work on the current stream of the handle's device (or on ``stream``) and does not
-synchronise.  One handle serves one stream at a time: its workspace is shared by the calls made through it.
+synchronise, except where a backward call needs more workspace than any before it (the old one is then freed).  One
+handle serves one stream at a time: its workspace is shared by the calls made through it, and by the graphs captured
+with it, which stay valid as long as the handle does.
 """
 from __future__ import annotations
 

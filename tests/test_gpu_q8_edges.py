@@ -1,0 +1,92 @@
+"""The 8-bit operators at the edges of the numbers' range, and after calls that failed."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2604_06836_b200 import q8, stq   # noqa: E402
+
+BF, F32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24          # half an ulp of fp32
+
+
+@pytest.fixture(scope="module")
+def handle():
+    h = stq.Handle()
+    yield h
+    h.device_status()
+    h.close()
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def backward(h, t, n, k, seed):
+    """One of each backward call that uses the workspace, as a function of nothing, and the inputs it reads."""
+    g = gen(seed)
+    dy = torch.randn(t, n, device="cuda", generator=g).to(BF)
+    x, w = (q8.quantize_rows(h, torch.randn(r, k, device="cuda", generator=g)) for r in (t, n))
+    hid, weight = torch.randn(t, n, device="cuda", generator=g).to(BF), torch.ones(n, device="cuda")
+    rstd = hid.float().square().mean(1).rsqrt()
+
+    def call():
+        return [q8.linear_dx(h, dy, w, dtype=F32), q8.linear_dw(h, dy, x, dtype=F32), q8.linear_dw(h, dy, x),
+                q8.bias_grad(h, dy), *q8.norm_backward(h, dy, hid, weight, rstd)]
+    return call, dy
+
+
+# ---- workspace -------------------------------------------------------------------------------------------------------
+def test_a_captured_graph_outlives_the_growth_of_the_workspace():
+    h = stq.Handle()
+    small, dy = backward(h, 300, 261, 128, 1)                  # (odd rows of dy: copied to the workspace)
+    small()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = small()
+    grown = []
+    for t, n, k in ((2000, 1285, 640), (5000, 1285, 2056)):    # more workspace twice over
+        large, _ = backward(h, t, n, k, 2)
+        grown.append((large, large()))
+    # whatever had been freed would be handed out here
+    other = [torch.full((1 << 20,), 3.0, device="cuda") for _ in range(64)]
+    dy.copy_(torch.randn(dy.shape, device="cuda", generator=gen(3)).to(BF))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(bool((o == 3.0).all()) for o in other)
+    own = stq.Handle()
+    fresh, dy2 = backward(own, 300, 261, 128, 1)
+    dy2.copy_(dy)
+    for a, b in zip(captured, fresh()):
+        assert torch.equal(a, b)
+    for large, before in grown:
+        for a, b in zip(large(), before):
+            assert torch.equal(a, b)
+    h.device_status(), own.device_status()
+    del graph
+    h.close(), own.close()
+
+
+def test_the_workspace_does_not_grow_during_a_capture():
+    h = stq.Handle()
+    call, _ = backward(h, 300, 261, 128, 1)
+    x = torch.ones(64, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = x + 1
+        with pytest.raises(stq.StqError, match="captured") as e:
+            call()
+        y = y + 1
+    assert e.value.code == -8
+    graph.replay()                                             # the capture went on
+    assert (y == 3.0).all()
+    want = call()
+    with torch.cuda.graph(graph2 := torch.cuda.CUDAGraph()):
+        got = call()
+    graph2.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    del graph2
+    h.close()

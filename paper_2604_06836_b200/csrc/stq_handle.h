@@ -103,7 +103,12 @@ inline int grow(stq_handle* h, T*& p, size_t& cap, size_t need) {
   cap = 0;
   size_t want = need + need / 4 + 256;
   cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&p), want * sizeof(T));
-  if (e != cudaSuccess) { h->cuda_err = cudaGetErrorString(e); p = nullptr; return STQ_E_WORKSPACE; }
+  if (e != cudaSuccess) {
+    h->cuda_err = cudaGetErrorString(e);
+    (void)cudaGetLastError();      // (or the next launch that is asked for its error would report this one)
+    p = nullptr;
+    return STQ_E_WORKSPACE;
+  }
   cap = want;
   return STQ_OK;
 }

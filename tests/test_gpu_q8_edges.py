@@ -37,6 +37,21 @@ def backward(h, t, n, k, seed):
 
 
 # ---- workspace -------------------------------------------------------------------------------------------------------
+def test_a_workspace_that_cannot_be_had_leaves_the_handle_usable():
+    """The sizes ask for a copy of half a terabyte (dy lies on an odd address): refused before anything is launched."""
+    h = stq.Handle()
+    L, buf, q, s = q8._lib(), torch.zeros(4096, device="cuda"), torch.zeros(128, 64, dtype=torch.int8, device="cuda"), torch.ones(128, device="cuda")
+    before = h.launch_count
+    rc = L.stq_q8_linear_dx(h._h, buf.data_ptr() + 2, 128, q.data_ptr(), 64, s.data_ptr(), 2 ** 31 - 1, 128, 64,
+                            1 << 46, 64, 1, None)      # (an address nothing lives at; it is compared and never touched)
+    assert rc == -8 and h.launch_count == before
+    x = torch.randn(5, 64, device="cuda", generator=gen(1))
+    r = q8.quantize_rows(h, x)
+    assert int(r.q.abs().max()) == 127
+    h.device_status()
+    h.close()
+
+
 def test_a_captured_graph_outlives_the_growth_of_the_workspace():
     h = stq.Handle()
     small, dy = backward(h, 300, 261, 128, 1)                  # (odd rows of dy: copied to the workspace)

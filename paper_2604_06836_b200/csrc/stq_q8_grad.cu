@@ -27,6 +27,7 @@
 #include "stq_internal.h"
 #include "stq_q8.h"
 #include "stq_q8_mma.cuh"
+#include "stq_q8_ring.h"
 #include "stq_q8_tma.h"
 
 namespace stq {
@@ -133,13 +134,14 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
                const GradArgs a) {
   using S = GradShape<CG, BN, PARTS, CONV>;
   constexpr int kStages = S::kStages, kNB = S::kNB;
+  using Codes = ArrivalRing<kStages, kGroups>;
   extern __shared__ uint8_t raw[];
-  __shared__ uint64_t bars[4 * kStages + 4];
+  __shared__ uint64_t bars[Codes::kBars + 3 * kStages + 4];
   __shared__ uint32_t tmem_slot;
   const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u, stages = ring + kStages * S::kStage;
-  // per stage: codes have landed (this CTA), gradient has landed and codes are converted (both CTAs, at the leader),
-  // stage is free; per accumulator: done, read (both CTAs, at the leader)
-  const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * kStages, ready = full_g + 8 * kStages;
+  // codes have landed (this CTA, see ArrivalRing); per stage: gradient has landed and codes are converted (both CTAs, at the
+  // leader), stage is free; per accumulator: done, read (both CTAs, at the leader)
+  const uint32_t full_q = smem_addr(bars), full_g = full_q + 8 * Codes::kBars, ready = full_g + 8 * kStages;
   const uint32_t empty = ready + 8 * kStages, done = empty + 8 * kStages, freed = done + 16;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CG == 2 ? cluster_rank() : 0;
@@ -147,8 +149,8 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
   const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG, work = a.full + (a.tiles - a.full) * a.splits;
 
   if (threadIdx.x == 0) {
+    for (int i = 0; i < Codes::kBars; ++i) bar_init(full_q + 8 * i, 1);
     for (int i = 0; i < kStages; ++i) {
-      bar_init(full_q + 8 * i, 1);
       bar_init(full_g + 8 * i, 1);
       bar_init(ready + 8 * i, CG * kGroupWarps);
       bar_init(empty + 8 * i, 1);
@@ -194,8 +196,9 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
           const uint32_t at = ring + s * S::kStage, c = k * kDepth;
           if (leader) bar_expect(full_g + 8 * s, CG * (S::kA + (CONV ? 0 : S::kB)));
           if constexpr (CONV) {
-            bar_expect(full_q + 8 * s, S::kQ);
-            tensor_load<1>(at + S::kA, &map_q, col, (int)c, full_q + 8 * s);
+            const uint32_t landed = full_q + 8 * Codes::bar(it);
+            bar_expect(landed, S::kQ);
+            tensor_load<1>(at + S::kA, &map_q, col, (int)c, landed);
           } else {
 #pragma unroll
             for (int i = 0; i < kNB / 64; ++i)
@@ -211,7 +214,7 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       }
       if (!ok)      // leave no copy in flight
         for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) {
-          if (CONV) bar_wait(full_q + 8 * (i % kStages), (i / kStages) & 1);
+          if (CONV) bar_wait(full_q + 8 * Codes::bar(i), Codes::parity(i));
           if (leader) bar_wait(full_g + 8 * (i % kStages), (i / kStages) & 1);
         }
     }
@@ -270,15 +273,9 @@ q8_grad_kernel(const __grid_constant__ CUtensorMap map_g, const __grid_constant_
       };
       const uint32_t mine = (group + kGroups - it % kGroups) % kGroups;      // the group's first stage of this item
       scales(k0 + mine);
-      for (uint32_t k = k0; k < k1; ++k) {
-        // A barrier tells only whether its latest phase has the parity asked for.  Where a slot of the ring serves both
-        // groups in turn, a group that skipped the other's stages could take the phase before the last for the one it
-        // needs (copies may complete out of order), so there every group waits for every stage.
-        const uint32_t i = it + k - k0, s = i % kStages, ph = (i / kStages) & 1;
-        const bool own = i % kGroups == (uint32_t)group;
-        if (kStages % kGroups == 0 && !own) continue;
-        if (!(ok = bar_wait(full_q + 8 * s, ph))) break;
-        if (!own) continue;
+      for (uint32_t k = k0 + mine; k < k1; k += kGroups) {
+        const uint32_t i = it + k - k0, s = i % kStages;
+        if (!(ok = bar_wait(full_q + 8 * Codes::bar(i), Codes::parity(i)))) break;
         Scale2 now[kPasses];
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) now[p] = scale2_of(sc[p]);

@@ -43,7 +43,7 @@ class _Block(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy, dh):
         h, rstd, nq, ns, aq, as_, cq, cs, weight, iq, is_, oq, os_ = ctx.saved_tensors
-        hd = ctx.block.handle_for(h.device)
+        hd = ctx.block.ordered_handle(h.device)
         dy, dh = dy.contiguous(), dh.contiguous()
         rows8 = q8.Rows8
         dw_out = q8.linear_dw(hd, dy, rows8(aq, as_), dtype=torch.float32)
@@ -60,7 +60,10 @@ class FeedForward8(torch.nn.Module):
 
     forward(x, residual=None) takes bf16 [..., width] and returns (y, h) with h = x + residual: the next block of a stack
     gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on every
-    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving."""
+    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving.
+
+    Passes may run on any streams: backward passes, which share a workspace, are put in order one after the other.  A
+    captured graph that holds a backward pass must not be replayed while another backward pass of the block runs."""
 
     def __init__(self, width: int, hidden: int, kind: str = "silu_gated", bias: bool = False, eps: float = 1e-6, device="cuda"):
         super().__init__()
@@ -77,14 +80,26 @@ class FeedForward8(torch.nn.Module):
         self.b_out = torch.nn.Parameter(torch.zeros(width, dtype=torch.float32, device=device)) if bias else None
         self.weights8 = None
         self._handle: Optional[stq.Handle] = None
+        self._last = None      # the stream of the last backward pass
 
     def handle_for(self, device: torch.device) -> stq.Handle:
         if self._handle is None or self._handle.device != device.index:
-            self._handle = stq.Handle(device.index)
+            self._handle, self._last = stq.Handle(device.index), None
         return self._handle
 
+    def ordered_handle(self, device: torch.device) -> stq.Handle:
+        """The handle for a backward pass on the current stream.  Backward calls share the handle's workspace, so the stream
+        waits for the one of the last backward pass.  (A capture runs nothing: who replays the graph keeps the order.)"""
+        hd = self.handle_for(device)
+        if not torch.cuda.is_current_stream_capturing():
+            stream = torch.cuda.current_stream(device)
+            if self._last is not None and self._last != stream:
+                stream.wait_stream(self._last)
+            self._last = stream
+        return hd
+
     def __getstate__(self):
-        return {**self.__dict__, "_handle": None}      # (a copy makes its own)
+        return {**self.__dict__, "_handle": None, "_last": None}      # (a copy makes its own)
 
     def quantized(self):
         """The two weights as 8-bit rows, a scale per output channel."""

@@ -1,0 +1,54 @@
+"""What the feed-forward block keeps, saves and refuses: weights in 8 bits, checkpoints, gradients nobody asked for."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2604_06836_b200 import ffn8, q8   # noqa: E402
+from paper_2604_06836_b200.ffn8 import FeedForward8   # noqa: E402
+from paper_2604_06836_b200.optim import STQAdamW   # noqa: E402
+
+BF = torch.bfloat16
+
+
+def block(width=72, hidden=136, kind="silu_gated", bias=False, seed=0):
+    torch.manual_seed(seed)
+    return FeedForward8(width, hidden, kind, bias)
+
+
+def tokens(t=20, width=72, seed=1):
+    return torch.randn(t, width, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)).to(BF)
+
+
+def served(m, x):
+    with torch.no_grad():
+        return m(x)[0]
+
+
+# ---- streams ---------------------------------------------------------------------------------------------------------
+def test_backward_passes_on_two_streams():
+    """Both passes use the block's workspace; neither may see the other's partial sums."""
+    m = block(392, 1000, bias=True)
+    xs = [tokens(t, 392, t).requires_grad_(True) for t in (1500, 1700)]
+    dys = [tokens(t, 392, 7 * t) for t in (1500, 1700)]
+
+    def gradients(y, x, dy):
+        return torch.autograd.grad(y, [x, *m.parameters()], dy)
+    want = [gradients(m(x)[0], x, dy) for x, dy in zip(xs, dys)]
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        ys = []
+        for s, x in zip(streams, xs):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                ys.append(m(x)[0])
+        torch.cuda.synchronize()
+        got = []
+        for s, y, x, dy in zip(streams, ys, xs, dys):
+            with torch.cuda.stream(s):
+                got.append(gradients(y, x, dy))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            for u, v in zip(a, b):
+                assert torch.equal(u, v)
+    m.handle_for(xs[0].device).device_status()

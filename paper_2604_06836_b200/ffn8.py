@@ -21,6 +21,18 @@ import torch
 from . import q8, stq
 
 
+class _Final(torch.autograd.Function):
+    """Hands gradients on that nothing may differentiate again: the kernels that formed them leave no graph behind, and
+    without this they would pass for constants.  (`anchor` requires a gradient, whatever the others do.)"""
+    @staticmethod
+    def forward(ctx, anchor, *grads):
+        return tuple(None if g is None else g.view_as(g) for g in grads)
+
+    @staticmethod
+    def backward(ctx, *dd):
+        raise RuntimeError("FeedForward8 has no second derivatives")
+
+
 class _Block(torch.autograd.Function):
     @staticmethod
     def forward(ctx, block, x, residual, weight, w_in, b_in, w_out, b_out):
@@ -42,6 +54,14 @@ class _Block(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy, dh):
+        with torch.no_grad():
+            grads = _Block.gradients(ctx, dy, dh)
+        if torch.is_grad_enabled():      # create_graph
+            return _Final.apply(torch.empty(0, requires_grad=True), *grads)
+        return grads
+
+    @staticmethod
+    def gradients(ctx, dy, dh):
         h, rstd, nq, ns, aq, as_, cq, cs, weight, iq, is_, oq, os_ = ctx.saved_tensors
         hd = ctx.block.ordered_handle(h.device)
         dy, dh = dy.contiguous(), dh.contiguous()

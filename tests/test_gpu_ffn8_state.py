@@ -52,3 +52,16 @@ def test_backward_passes_on_two_streams():
             for u, v in zip(a, b):
                 assert torch.equal(u, v)
     m.handle_for(xs[0].device).device_status()
+
+
+# ---- derivatives -----------------------------------------------------------------------------------------------------
+def test_a_second_derivative_is_refused():
+    """The kernels leave no graph behind them: differentiating their gradients again must not pass for a constant."""
+    m, x = block(), tokens().requires_grad_(True)
+    y, h = m(x)
+    for dy in (torch.ones_like(y), torch.ones_like(y).requires_grad_(True)):
+        (g,) = torch.autograd.grad(y, x, dy, create_graph=True, retain_graph=True)
+        with pytest.raises(RuntimeError, match="second"):
+            (g.float().square().sum() + x.float().square().sum()).backward(retain_graph=True)
+    (plain,) = torch.autograd.grad(y, x, torch.ones_like(y))
+    assert torch.equal(plain, g)                          # the first derivative is as it was

@@ -35,10 +35,9 @@ class _Final(torch.autograd.Function):
 
 class _Block(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, block, x, residual, weight, w_in, b_in, w_out, b_out):
+    def forward(ctx, block, train, x, residual, weight, w_in, b_in, w_out, b_out):
         hd = block.handle_for(x.device)
         w8 = block.weights8 or block.quantized()
-        train = any(ctx.needs_input_grad)
         n = q8.norm(hd, x, weight, residual=residual, eps=block.eps)
         z = q8.linear(hd, n.rows, w8[0], bias=b_in)
         a = q8.act(hd, z, block.kind, checkpoint=train)
@@ -72,7 +71,7 @@ class _Block(torch.autograd.Function):
         dw_in = q8.linear_dw(hd, dz, rows8(nq, ns), dtype=torch.float32)
         db_in = q8.bias_grad(hd, dz) if ctx.has_bias[0] else None
         dx, dweight = q8.norm_backward(hd, q8.linear_dx(hd, dz, rows8(iq, is_)), h, weight, rstd, dres=dh)
-        return None, dx, None if ctx.plain else dx, dweight, dw_in, db_in, dw_out, db_out
+        return None, None, dx, None if ctx.plain else dx, dweight, dw_in, db_in, dw_out, db_out
 
 
 class FeedForward8(torch.nn.Module):
@@ -145,5 +144,8 @@ class FeedForward8(torch.nn.Module):
         if x.dtype != torch.bfloat16 or (residual is not None and residual.dtype != torch.bfloat16):
             raise ValueError("FeedForward8 takes bfloat16 activations")
         flat = lambda t: None if t is None else t.reshape(-1, t.shape[-1])  # noqa: E731
-        y, h = _Block.apply(self, flat(x), flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
+        given = (flat(x), flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
+        # (inside a Function neither the grad mode nor needs_input_grad tells whether a backward pass can follow)
+        train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given)
+        y, h = _Block.apply(self, train, *given)
         return y.view(x.shape), h.view(x.shape)

@@ -65,3 +65,23 @@ def test_a_second_derivative_is_refused():
             (g.float().square().sum() + x.float().square().sum()).backward(retain_graph=True)
     (plain,) = torch.autograd.grad(y, x, torch.ones_like(y))
     assert torch.equal(plain, g)                          # the first derivative is as it was
+
+
+# ---- what a pass saves -----------------------------------------------------------------------------------------------
+def test_nothing_is_saved_where_no_gradient_is_taken(monkeypatch):
+    asked = []
+
+    def act(*a, _real=q8.act, **kw):
+        asked.append(bool(kw.get("checkpoint")))
+        return _real(*a, **kw)
+    monkeypatch.setattr(q8, "act", act)
+    m, x = block(), tokens()
+    y = m(x)[0]
+    assert asked == [True] and y.requires_grad
+    with torch.no_grad():
+        assert torch.equal(m(x)[0], y) and torch.equal(m.freeze()(x)[0], y)
+    with torch.inference_mode():
+        assert torch.equal(m(x)[0], y)
+    m.requires_grad_(False)
+    assert not m(x)[0].requires_grad
+    assert asked == [True] + [False] * 4

@@ -43,9 +43,7 @@ class _Block(torch.autograd.Function):
         a = q8.act(hd, z, block.kind, checkpoint=train)
         y = q8.linear(hd, a.rows, w8[1], bias=b_out)
         if train:
-            ctx.block, ctx.plain = block, residual is None
-            ctx.has_bias = b_in is not None, b_out is not None
-            ck = a.checkpoint
+            ctx.block, ck = block, a.checkpoint
             ctx.meta = ck.cols, ck.kind
             ctx.save_for_backward(n.h, n.rstd, *n.rows, *a.rows, ck.q, ck.scale, weight, *w8[0], *w8[1])
         # (an input that is returned as it is would be taken for a view of itself)
@@ -65,13 +63,23 @@ class _Block(torch.autograd.Function):
         hd = ctx.block.ordered_handle(h.device)
         dy, dh = dy.contiguous(), dh.contiguous()
         rows8 = q8.Rows8
-        dw_out = q8.linear_dw(hd, dy, rows8(aq, as_), dtype=torch.float32)
-        db_out = q8.bias_grad(hd, dy) if ctx.has_bias[1] else None
-        dz = q8.act_backward(hd, q8.linear_dx(hd, dy, rows8(oq, os_)), q8.Checkpoint8(cq, cs, *ctx.meta))
-        dw_in = q8.linear_dw(hd, dz, rows8(nq, ns), dtype=torch.float32)
-        db_in = q8.bias_grad(hd, dz) if ctx.has_bias[0] else None
-        dx, dweight = q8.norm_backward(hd, q8.linear_dx(hd, dz, rows8(iq, is_)), h, weight, rstd, dres=dh)
-        return None, None, dx, None if ctx.plain else dx, dweight, dw_in, db_in, dw_out, db_out
+        _, _, for_x, for_res, for_weight, for_w_in, for_b_in, for_w_out, for_b_out = ctx.needs_input_grad
+        dx = dweight = dw_in = db_in = dw_out = db_out = None      # (formed only if somebody asks)
+        if for_w_out:
+            dw_out = q8.linear_dw(hd, dy, rows8(aq, as_), dtype=torch.float32)
+        if for_b_out:
+            db_out = q8.bias_grad(hd, dy)
+        before_z = for_x or for_res or for_weight
+        if before_z or for_w_in or for_b_in:
+            dz = q8.act_backward(hd, q8.linear_dx(hd, dy, rows8(oq, os_)), q8.Checkpoint8(cq, cs, *ctx.meta))
+            if for_w_in:
+                dw_in = q8.linear_dw(hd, dz, rows8(nq, ns), dtype=torch.float32)
+            if for_b_in:
+                db_in = q8.bias_grad(hd, dz)
+            if before_z:
+                dx, dweight = q8.norm_backward(hd, q8.linear_dx(hd, dz, rows8(iq, is_)), h, weight, rstd, dres=dh)
+        return (None, None, dx if for_x else None, dx if for_res else None, dweight if for_weight else None, dw_in, db_in,
+                dw_out, db_out)
 
 
 class FeedForward8(torch.nn.Module):

@@ -67,6 +67,38 @@ def test_a_second_derivative_is_refused():
     assert torch.equal(plain, g)                          # the first derivative is as it was
 
 
+def test_no_gradient_is_formed_that_nobody_asked_for(monkeypatch):
+    count = {}
+    for name in ("linear_dw", "linear_dx", "bias_grad", "norm_backward", "act_backward"):
+        def call(*a, _real=getattr(q8, name), _name=name, **kw):
+            count[_name] = count.get(_name, 0) + 1
+            return _real(*a, **kw)
+        monkeypatch.setattr(q8, name, call)
+    m, x = block(bias=True), tokens().requires_grad_(True)
+    m(x)[0].float().square().sum().backward()
+    full = x.grad
+    assert count == {"linear_dw": 2, "linear_dx": 2, "bias_grad": 2, "norm_backward": 1, "act_backward": 1}
+    dw = m.w_out.grad
+
+    count.clear()                                         # frozen weights: the input's gradient only
+    m.requires_grad_(False)
+    x.grad = None
+    m(x)[0].float().square().sum().backward()
+    assert torch.equal(x.grad, full)
+    assert count == {"linear_dx": 2, "norm_backward": 1, "act_backward": 1}
+
+    count.clear()                                         # the last product's weight only
+    m.w_out.requires_grad_(True)
+    m.w_out.grad = None
+    m(x.detach())[0].float().square().sum().backward()
+    assert torch.equal(m.w_out.grad, dw) and count == {"linear_dw": 1}
+
+    count.clear()                                         # the first product's too: up to z, and no further
+    m.w_in.requires_grad_(True)
+    m(x.detach())[0].float().square().sum().backward()
+    assert m.w_in.grad is not None and count == {"linear_dw": 2, "linear_dx": 1, "act_backward": 1}
+
+
 # ---- what a pass saves -----------------------------------------------------------------------------------------------
 def test_nothing_is_saved_where_no_gradient_is_taken(monkeypatch):
     asked = []

@@ -21,6 +21,10 @@ import torch
 from . import q8, stq
 
 
+def _version(p: torch.Tensor):
+    return None if p.is_inference() else p._version      # (how often torch has seen it change)
+
+
 class _Final(torch.autograd.Function):
     """Hands gradients on that nothing may differentiate again: the kernels that formed them leave no graph behind, and
     without this they would pass for constants.  (`anchor` requires a gradient, whatever the others do.)"""
@@ -35,9 +39,8 @@ class _Final(torch.autograd.Function):
 
 class _Block(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, block, train, x, residual, weight, w_in, b_in, w_out, b_out):
+    def forward(ctx, block, w8, train, x, residual, weight, w_in, b_in, w_out, b_out):
         hd = block.handle_for(x.device)
-        w8 = block.weights8 or block.quantized()
         n = q8.norm(hd, x, weight, residual=residual, eps=block.eps)
         z = q8.linear(hd, n.rows, w8[0], bias=b_in)
         a = q8.act(hd, z, block.kind, checkpoint=train)
@@ -63,7 +66,7 @@ class _Block(torch.autograd.Function):
         hd = ctx.block.ordered_handle(h.device)
         dy, dh = dy.contiguous(), dh.contiguous()
         rows8 = q8.Rows8
-        _, _, for_x, for_res, for_weight, for_w_in, for_b_in, for_w_out, for_b_out = ctx.needs_input_grad
+        _, _, _, for_x, for_res, for_weight, for_w_in, for_b_in, for_w_out, for_b_out = ctx.needs_input_grad
         dx = dweight = dw_in = db_in = dw_out = db_out = None      # (formed only if somebody asks)
         if for_w_out:
             dw_out = q8.linear_dw(hd, dy, rows8(aq, as_), dtype=torch.float32)
@@ -78,8 +81,8 @@ class _Block(torch.autograd.Function):
                 db_in = q8.bias_grad(hd, dz)
             if before_z:
                 dx, dweight = q8.norm_backward(hd, q8.linear_dx(hd, dz, rows8(iq, is_)), h, weight, rstd, dres=dh)
-        return (None, None, dx if for_x else None, dx if for_res else None, dweight if for_weight else None, dw_in, db_in,
-                dw_out, db_out)
+        return (None, None, None, dx if for_x else None, dx if for_res else None, dweight if for_weight else None, dw_in,
+                db_in, dw_out, db_out)
 
 
 class FeedForward8(torch.nn.Module):
@@ -87,7 +90,9 @@ class FeedForward8(torch.nn.Module):
 
     forward(x, residual=None) takes bf16 [..., width] and returns (y, h) with h = x + residual: the next block of a stack
     gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on every
-    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving.
+    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving.  A frozen block
+    quantizes them again where they have changed since (loading, an optimizer step, any change that torch counts, a move to
+    another device), and for every pass that differentiates them.
 
     Passes may run on any streams: backward passes, which share a workspace, are put in order one after the other.  A
     captured graph that holds a backward pass must not be replayed while another backward pass of the block runs."""
@@ -106,6 +111,8 @@ class FeedForward8(torch.nn.Module):
         self.b_in = torch.nn.Parameter(torch.zeros(parts * hidden, dtype=torch.float32, device=device)) if bias else None
         self.b_out = torch.nn.Parameter(torch.zeros(width, dtype=torch.float32, device=device)) if bias else None
         self.weights8 = None
+        self._of = None        # what weights8 was quantized from: the parameters, their versions, on which stream and when
+        self._in_graphs = []   # codes that captured graphs read
         self._handle: Optional[stq.Handle] = None
         self._last = None      # the stream of the last backward pass
 
@@ -126,7 +133,8 @@ class FeedForward8(torch.nn.Module):
         return hd
 
     def __getstate__(self):
-        return {**self.__dict__, "_handle": None, "_last": None}      # (a copy makes its own)
+        # (a copy makes its own, and quantizes its own weights)
+        return {**self.__dict__, "_handle": None, "_last": None, "_of": None, "_in_graphs": []}
 
     def quantized(self):
         """The two weights as 8-bit rows, a scale per output channel."""
@@ -135,12 +143,49 @@ class FeedForward8(torch.nn.Module):
 
     def freeze(self):
         """Quantizes the weights once and keeps them until ``thaw()``: for serving, where they do not change."""
-        self.weights8 = self.quantized()
+        with torch.inference_mode(False):      # (a later pass may have to save them)
+            self.weights8 = self.quantized()
+        self._of = None
+        if not torch.cuda.is_current_stream_capturing():      # (a capture has not computed anything yet)
+            stream, done = torch.cuda.current_stream(self.w_in.device), torch.cuda.Event()
+            done.record(stream)
+            self._of = self.w_in, _version(self.w_in), self.w_out, _version(self.w_out), stream.cuda_stream, done
         return self
 
     def thaw(self):
-        self.weights8 = None
+        self.weights8 = self._of = None
         return self
+
+    def _codes(self, differentiated: bool):
+        """The 8-bit weights for a pass on the current stream."""
+        if self.weights8 is None:
+            return self.quantized()
+        if differentiated:      # they are about to change, by an optimizer that may write them behind torch's back
+            self._of = None
+            return self.quantized()
+        of, capturing = self._of, torch.cuda.is_current_stream_capturing()
+        w_in, w_out = self.w_in, self.w_out
+        if of is None or of[0] is not w_in or of[1] != _version(w_in) or of[2] is not w_out or of[3] != _version(w_out):
+            if capturing:       # (every replay quantizes)
+                return self.quantized()
+            self.freeze()
+        elif capturing:         # the graph goes on reading them, whatever the block serves by then
+            if all(c is not self.weights8 for c in self._in_graphs):
+                self._in_graphs.append(self.weights8)
+        elif of[4] != q8._raw_stream(w_in.device.index):      # another stream than the one that wrote them
+            stream = torch.cuda.current_stream(w_in.device)
+            stream.wait_event(of[5])
+            for r in self.weights8:
+                r.q.record_stream(stream), r.scale.record_stream(stream)
+        return self.weights8
+
+    def _apply(self, *args, **kw):
+        self._of = None            # (parameters that move or change their type keep their version)
+        return super()._apply(*args, **kw)
+
+    def _load_from_state_dict(self, *args, **kw):
+        self._of = None
+        return super()._load_from_state_dict(*args, **kw)
 
     def saved_bytes(self, tokens: int) -> int:
         """Bytes that a forward pass of so many tokens keeps for its backward pass, next to h and the weights."""
@@ -155,5 +200,6 @@ class FeedForward8(torch.nn.Module):
         given = (flat(x), flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
         # (inside a Function neither the grad mode nor needs_input_grad tells whether a backward pass can follow)
         train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given)
-        y, h = _Block.apply(self, train, *given)
+        w8 = self._codes(train and (self.w_in.requires_grad or self.w_out.requires_grad))
+        y, h = _Block.apply(self, w8, train, *given)
         return y.view(x.shape), h.view(x.shape)

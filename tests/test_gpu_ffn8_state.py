@@ -117,3 +117,80 @@ def test_nothing_is_saved_where_no_gradient_is_taken(monkeypatch):
     m.requires_grad_(False)
     assert not m(x)[0].requires_grad
     assert asked == [True] + [False] * 4
+
+
+# ---- frozen weights ----------------------------------------------------------------------------------------------------
+def test_a_frozen_block_serves_the_weights_it_has():
+    x = tokens()
+    other = block(seed=5)
+    want = served(other, x)
+
+    m = block().freeze()
+    m.load_state_dict(other.state_dict())
+    assert torch.equal(served(m, x), want)
+    m = block().freeze()
+    m.load_state_dict({k: v.clone() for k, v in other.state_dict().items()}, assign=True)
+    assert torch.equal(served(m, x), want)
+    m = block().freeze()
+    m.w_in, m.w_out = other.w_in, other.w_out
+    assert torch.equal(served(m, x), want)
+    m = block().freeze()
+    with torch.no_grad():
+        for p, q in zip(m.parameters(), other.parameters()):
+            p.copy_(q)
+    assert torch.equal(served(m, x), want)
+    kept = m.weights8
+    assert kept is not None and torch.equal(served(m, x), want) and m.weights8 is kept      # (quantized once, then kept)
+    m.cpu()
+    m.cuda()
+    assert torch.equal(served(m, x), want)
+
+
+def test_frozen_weights_on_another_stream_and_in_a_graph():
+    x = tokens()
+    m, other = block(1600, 3000), block(1600, 3000, seed=5)
+    x = tokens(4, 1600)
+    want, want2 = served(m, x), served(other, x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        m.freeze()                                        # here; used there at once
+        with torch.cuda.stream(side):
+            got = served(m, x)
+        side.synchronize()
+        assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = served(m, x)
+    m.load_state_dict(other.state_dict())
+    assert torch.equal(served(m, x), want2)
+    fill = [torch.full((1 << 20,), 7, dtype=torch.int8, device="cuda") for _ in range(32)]
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(captured, want)                    # the graph serves what it was captured with
+    m.load_state_dict(block(1600, 3000).state_dict())
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):        # weights that changed before a capture are quantized in it
+        captured = served(m, x)
+    assert torch.equal(served(m, x), want) and len(fill) == 32
+    with torch.inference_mode():
+        m.load_state_dict(other.state_dict())
+        assert torch.equal(m(x)[0], want2)
+    m.requires_grad_(False)                               # codes that were made there can be saved here
+    xg = x.clone().requires_grad_(True)
+    m(xg)[0].float().sum().backward()
+    assert float(xg.grad.abs().max()) > 0
+
+
+def test_a_frozen_block_is_trained_on_its_weights():
+    """A pass that differentiates the weights quantizes them as they are, frozen or not; what it serves afterwards is new."""
+    x = tokens()
+    a, b = block(), block().freeze()
+    for m in (a, b):
+        opt = STQAdamW(m.parameters(), lr=1e-2, weight_decay=0.0, policy="fixed", init_bits=8)
+        for _ in range(3):
+            opt.zero_grad()
+            m(x)[0].float().square().sum().backward()
+            opt.step()
+    for p, q in zip(a.parameters(), b.parameters()):
+        assert torch.equal(p, q)
+    assert torch.equal(served(a, x), served(b, x))

@@ -156,6 +156,7 @@ class STQAdamW(torch.optim.Optimizer):
                                    self.policy.is_decision_step(t + 1)) else 0
         if new_m is None or ((new_m == self.bits_m).all() and (new_v == self.bits_v).all()):
             self.handle.step(self._table(), flags=flags, **hp)
+            torch.autograd.graph.increment_version(self._params)      # (written behind torch's back)
             self._fetch_carried(flags)
             return loss
         out = []
@@ -172,6 +173,7 @@ class STQAdamW(torch.optim.Optimizer):
                 stq.alloc_codes(n, bv, self.device), stq.alloc_scales(n, bv, self.block, self.device, self.v_log))
             out.append(stq.QState(mc, ms, bm, vc, vs, bv, self.v_log))
         self.handle.step(stq.table(self._rows(out)), flags=flags, **hp)
+        torch.autograd.graph.increment_version(self._params)
         self._fetch_carried(flags)
         torch.cuda.current_stream(self.device).synchronize()     # the old buffers are released below
         self.states = out

@@ -194,3 +194,17 @@ def test_a_frozen_block_is_trained_on_its_weights():
     for p, q in zip(a.parameters(), b.parameters()):
         assert torch.equal(p, q)
     assert torch.equal(served(a, x), served(b, x))
+
+
+def test_a_step_of_the_quantized_optimizer_reaches_a_frozen_block():
+    x = tokens()
+    m = block()
+    opt = STQAdamW(m.parameters(), lr=1e-2, weight_decay=0.0, policy="fixed", init_bits=8)
+    m(x)[0].float().square().sum().backward()
+    before = served(m.freeze(), x)
+    opt.step()
+    after = served(m, x)
+    assert not torch.equal(after, before) and torch.equal(after, served(m.thaw(), x))
+    v = m.w_in._version
+    opt.step()
+    assert m.w_in._version > v                            # torch sees the change too

@@ -25,6 +25,14 @@ def _version(p: torch.Tensor):
     return None if p.is_inference() else p._version      # (how often torch has seen it change)
 
 
+def _flat(t):
+    """[..., width] as rows that the operators take: unit stride, no two rows in the same place."""
+    if t is None:
+        return None
+    t = t.reshape(-1, t.shape[-1])
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
 class _Final(torch.autograd.Function):
     """Hands gradients on that nothing may differentiate again: the kernels that formed them leave no graph behind, and
     without this they would pass for constants.  (`anchor` requires a gradient, whatever the others do.)"""
@@ -88,7 +96,7 @@ class _Block(torch.autograd.Function):
 class FeedForward8(torch.nn.Module):
     """norm -> product -> activation -> product, with 8-bit products and 8-bit saved state.
 
-    forward(x, residual=None) takes bf16 [..., width] and returns (y, h) with h = x + residual: the next block of a stack
+    forward(x, residual=None) takes bf16 [..., width] in any layout and returns (y, h) with h = x + residual: the next block of a stack
     gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on every
     forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving.  A frozen block
     quantizes them again where they have changed since (loading, an optimizer step, any change that torch counts, a move to
@@ -196,8 +204,7 @@ class FeedForward8(torch.nn.Module):
     def forward(self, x: torch.Tensor, residual: torch.Tensor | None = None):
         if x.dtype != torch.bfloat16 or (residual is not None and residual.dtype != torch.bfloat16):
             raise ValueError("FeedForward8 takes bfloat16 activations")
-        flat = lambda t: None if t is None else t.reshape(-1, t.shape[-1])  # noqa: E731
-        given = (flat(x), flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
+        given = (_flat(x), _flat(residual), self.weight, self.w_in, self.b_in, self.w_out, self.b_out)
         # (inside a Function neither the grad mode nor needs_input_grad tells whether a backward pass can follow)
         train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in given)
         w8 = self._codes(train and (self.w_in.requires_grad or self.w_out.requires_grad))

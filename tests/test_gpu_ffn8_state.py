@@ -208,3 +208,20 @@ def test_a_step_of_the_quantized_optimizer_reaches_a_frozen_block():
     v = m.w_in._version
     opt.step()
     assert m.w_in._version > v                            # torch sees the change too
+
+
+# ---- layouts -----------------------------------------------------------------------------------------------------------
+def test_activations_in_any_layout():
+    m, x, r = block(), tokens(24), tokens(24, seed=2)
+    y, h = m(x, r)
+    wide = torch.zeros(24, 80, device="cuda", dtype=BF)
+    wide[:, :72] = x
+    for v in (x.t().contiguous().t(), wide[:, :72], x.view(2, 3, 4, 72).permute(1, 0, 2, 3).contiguous().permute(1, 0, 2, 3)):
+        yv, hv = m(v, r.view(v.shape))
+        assert yv.shape == v.shape and torch.equal(yv.reshape(24, 72), y) and torch.equal(hv.reshape(24, 72), h)
+    one = x[:1].clone().requires_grad_(True)              # one residual row for all tokens
+    ye, he = m(x, one.expand(24, 72))
+    assert torch.equal(ye, m(x, one.detach().repeat(24, 1))[0])
+    he.float().sum().backward()
+    assert torch.equal(one.grad, torch.full_like(one, 24.0))
+    assert torch.equal(m(x.t().contiguous().t())[1], x)

@@ -247,7 +247,8 @@ int stq_step_host(stq_handle* h, const stq_tensor* tensors, int L, const stq_hpa
 /* Synchronises `stream` and reports whether any kernel launched through this handle gave up on a
  * bounded wait (its asynchronous copies did not complete in ~2 s): STQ_E_TIMEOUT, else STQ_OK.
  * The device never spins without a limit; after a time-out the outputs of that launch are
- * undefined and the handle should be destroyed. */
+ * undefined and the handle should be destroyed.  The 8-bit operators return STQ_E_TIMEOUT by themselves
+ * from the first call that finds such a launch behind it. */
 int stq_device_status(stq_handle* h, void* stream);
 
 /* Exercises the time-out path without stalling anything: launches a one-warp kernel that waits, with

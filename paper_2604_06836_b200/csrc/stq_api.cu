@@ -488,8 +488,10 @@ int stq_create(stq_handle** out, int device) {
   h->grid = h->sm_count * stq::step_ctas_per_sm();
   h->fast_grid = h->sm_count * stq::fast_ctas_per_sm();
   if (h->fast_grid > stq::kFastMaxGrid) h->fast_grid = stq::kFastMaxGrid;
-  if (cudaMalloc(reinterpret_cast<void**>(&h->d_err), 2 * sizeof(int)) != cudaSuccess ||
-      cudaMemset(h->d_err, 0, 2 * sizeof(int)) != cudaSuccess ||
+  if (cudaHostAlloc(reinterpret_cast<void**>(&h->h_err), sizeof(int), cudaHostAllocMapped) != cudaSuccess ||
+      cudaHostGetDevicePointer(reinterpret_cast<void**>(&h->d_err), h->h_err, 0) != cudaSuccess ||
+      cudaMalloc(reinterpret_cast<void**>(&h->d_valid), sizeof(int)) != cudaSuccess ||
+      cudaMemset(h->d_valid, 0, sizeof(int)) != cudaSuccess ||
       cudaMalloc(reinterpret_cast<void**>(&h->d_scalars), 4 * sizeof(float)) != cudaSuccess ||
       cudaMalloc(reinterpret_cast<void**>(&h->d_q8_counters), stq::kQ8Counters * sizeof(uint32_t)) != cudaSuccess ||
       cudaMemset(h->d_q8_counters, 0, stq::kQ8Counters * sizeof(uint32_t)) != cudaSuccess ||
@@ -498,6 +500,7 @@ int stq_create(stq_handle** out, int device) {
     delete h;
     return STQ_E_WORKSPACE;
   }
+  *h->h_err = 0;
   // (without the side stream everything simply runs in order on the caller's stream)
   if (cudaStreamCreateWithFlags(&h->side, cudaStreamNonBlocking) != cudaSuccess ||
       cudaEventCreateWithFlags(&h->ev_fork, cudaEventDisableTiming) != cudaSuccess ||
@@ -516,7 +519,7 @@ int stq_destroy(stq_handle* h) {
   if (h->stage_busy) cudaEventSynchronize(h->stage_ev);
   cudaFree(h->d_table);
   cudaFree(h->d_tile_map);
-  cudaFree(h->d_err);
+  cudaFree(h->d_valid);
   cudaFree(h->d_sched);
   cudaFree(h->d_scalars);
   cudaFree(h->d_partials);
@@ -536,6 +539,7 @@ int stq_destroy(stq_handle* h) {
   for (cudaEvent_t e : h->host_events) cudaEventDestroy(e);
   if (h->h_stage) cudaFreeHost(h->h_stage);
   if (h->h_stats) cudaFreeHost(h->h_stats);
+  cudaFreeHost(h->h_err);      // (the calls above have waited for the device)
   if (h->stage_ev) cudaEventDestroy(h->stage_ev);
   if (h->side) cudaStreamDestroy(h->side);
   if (h->ev_fork) cudaEventDestroy(h->ev_fork);
@@ -589,7 +593,7 @@ int stq_step(stq_handle* h, const stq_tensor* tensors, int L, const stq_hparams*
     sc.dev_scalars = h->d_scalars;
   }
   if (stats) {   // a step skipped through found_inf writes no partial sums: record whether this one will
-    STQ_CUDA(h, stq::launch_stats_valid(hp->found_inf, h->d_err + 1, s));
+    STQ_CUDA(h, stq::launch_stats_valid(hp->found_inf, h->d_valid, s));
     h->launches++;
   }
   rc = run(h, stq::kStep, hp->grad_dtype, stats, sc, s);
@@ -605,7 +609,7 @@ int stq_grad_stats(stq_handle* h, const stq_tensor* tensors, int L, int grad_dty
   if (rc != STQ_OK) return rc;
   stq::StepConsts sc;
   std::memset(&sc, 0, sizeof(sc));
-  STQ_CUDA(h, stq::launch_stats_valid(nullptr, h->d_err + 1, s));
+  STQ_CUDA(h, stq::launch_stats_valid(nullptr, h->d_valid, s));
   h->launches++;
   rc = run(h, stq::kStatsOnly, grad_dtype, true, sc, s);
   if (rc == STQ_OK) h->stats_L = L;
@@ -635,7 +639,7 @@ int stq_layer_stats(stq_handle* h, double* out, int L, void* stream) {
   h->launches += 2;
   STQ_CUDA(h, cudaMemcpyAsync(h->h_stats, h->d_stats, sizeof(double) * 4 * (size_t)L, cudaMemcpyDeviceToHost, s));
   int* h_valid = reinterpret_cast<int*>(h->h_stats + 4 * (size_t)L);
-  STQ_CUDA(h, cudaMemcpyAsync(h_valid, h->d_err + 1, sizeof(int), cudaMemcpyDeviceToHost, s));
+  STQ_CUDA(h, cudaMemcpyAsync(h_valid, h->d_valid, sizeof(int), cudaMemcpyDeviceToHost, s));
   STQ_CUDA(h, cudaStreamSynchronize(s));
   if (*h_valid == 0) {        // the step that was to carry the sums was skipped (found_inf): nothing to report
     h->stats_L = 0;
@@ -649,10 +653,8 @@ int stq_device_status(stq_handle* h, void* stream) {
   if (!h) return STQ_E_NULL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   STQ_CUDA(h, cudaSetDevice(h->device));
-  int flag = 0;
-  STQ_CUDA(h, cudaMemcpyAsync(&flag, h->d_err, sizeof(int), cudaMemcpyDeviceToHost, s));
   STQ_CUDA(h, cudaStreamSynchronize(s));
-  return flag ? STQ_E_TIMEOUT : STQ_OK;
+  return stq::gave_up(h) ? STQ_E_TIMEOUT : STQ_OK;
 }
 
 int stq_repack(stq_handle* h, const stq_tensor* tensors, int L, void* stream) {

@@ -39,8 +39,11 @@ struct stq_handle {
   int fast_grid = 0;
   bool any_lp = false;              // some tensor of the current table wants a low-precision copy
   bool any_variant = false;         // some tensor's second moment uses a code only the generic kernel serves
-  int* d_err = nullptr;         // [0] raised by a kernel whose bounded wait ran out; [1] non-zero if the last call
-                                // that carried statistics really produced them (a skipped step does not)
+  // Raised by a kernel whose bounded wait ran out.  It lies in host memory that the device writes to, so that later calls
+  // see it without waiting for anything.
+  int* h_err = nullptr;         // as the host sees it
+  int* d_err = nullptr;         // as the device does
+  int* d_valid = nullptr;       // non-zero if the last call that carried statistics really produced them (a skipped step does not)
   float* d_scalars = nullptr;   // {step_size, rsqrt_bc2, lr} when the step count lives on the device
   stq::FastSched* d_sched = nullptr;   // two work lists of the main step kernel (fused bodies, width changes)
 
@@ -84,6 +87,9 @@ struct stq_handle {
 namespace stq {
 
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Whether a bounded wait of an earlier launch is known to have run out.
+inline bool gave_up(const stq_handle* h) { return *static_cast<const volatile int*>(h->h_err) != 0; }
 
 inline int fail_cuda(stq_handle* h, cudaError_t e) {
   h->cuda_err = cudaGetErrorString(e);

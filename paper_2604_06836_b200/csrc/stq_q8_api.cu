@@ -40,6 +40,8 @@ bool clash(const Span (&out)[N], const Span (&in)[M]) {
   return false;
 }
 
+// (results of a launch that gave up are invalid, and so is what is computed from them: the handle's later calls say so)
+int check_handle(const stq_handle* h) { return !h ? STQ_E_NULL : stq::gave_up(h) ? STQ_E_TIMEOUT : STQ_OK; }
 int check_dtype(int dtype) { return dtype == STQ_GRAD_F32 || dtype == STQ_GRAD_BF16 ? STQ_OK : STQ_E_ARG; }
 int check_size(uint64_t rows, uint64_t cols) {
   if (cols == 0) return STQ_E_NUMEL;
@@ -100,7 +102,7 @@ extern "C" {
 
 int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t rows, uint32_t cols, int8_t* q,
                 uint64_t ldq, float* scale, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(rows, cols));
   if (rows == 0) return STQ_OK;
@@ -121,7 +123,7 @@ int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t 
 int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uint64_t ldres, const float* weight,
                 float eps, int dtype, uint64_t rows, uint32_t cols, void* hsum, uint64_t ldh, float* rstd, int8_t* q,
                 uint64_t ldq, float* scale, void* values, uint64_t ldv, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(rows, cols));
   if (!(eps > 0.f)) return STQ_E_ARG;
@@ -158,7 +160,7 @@ int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uin
 int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const void* hsum, uint64_t ldh,
                          const float* weight, const float* rstd, const void* dres, uint64_t lddres, int dtype,
                          uint64_t rows, uint32_t cols, void* dx, uint64_t lddx, float* dweight, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(rows, cols));
   if (cols > STQ_NORM_BWD_MAX_COLS) return STQ_E_TOO_LARGE;
@@ -197,7 +199,7 @@ int stq_q8_norm_backward(stq_handle* h, const void* dy, uint64_t lddy, const voi
 int stq_q8_act(stq_handle* h, const void* z, uint64_t ldz, int kind, int dtype, uint64_t rows, uint32_t cols, int8_t* q,
                uint64_t ldq, float* scale, void* values, uint64_t ldv, int8_t* ckq, uint64_t ldck, float* ckscale,
                void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   if (kind != STQ_ACT_SILU_GATED && kind != STQ_ACT_GELU) return STQ_E_ARG;
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(rows, cols));
@@ -226,7 +228,7 @@ int stq_q8_act(stq_handle* h, const void* z, uint64_t ldz, int kind, int dtype, 
 
 int stq_q8_act_backward(stq_handle* h, const void* da, uint64_t ldda, int kind, int dtype, uint64_t rows, uint32_t cols,
                         const int8_t* ckq, uint64_t ldck, const float* ckscale, void* dz, uint64_t lddz, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   if (kind != STQ_ACT_SILU_GATED && kind != STQ_ACT_GELU) return STQ_E_ARG;
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(rows, cols));
@@ -254,7 +256,7 @@ int stq_q8_act_backward(stq_handle* h, const void* da, uint64_t ldda, int kind, 
 int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xscale, const int8_t* wq, uint64_t ldw,
                   const float* wscale, const float* bias, uint64_t t, uint32_t n, uint32_t k, void* out, uint64_t ldo,
                   int out_dtype, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(out_dtype));
   STQ_TRY(check_size(t, n));
   STQ_TRY(check_size(t, k));
@@ -282,7 +284,7 @@ int stq_q8_linear(stq_handle* h, const int8_t* xq, uint64_t ldx, const float* xs
 
 int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t* wq, uint64_t ldw, const float* wscale,
                      uint64_t t, uint32_t n, uint32_t k, void* dx, uint64_t lddx, int out_dtype, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(out_dtype));
   STQ_TRY(check_size(t, n));
   STQ_TRY(check_size(t, k));
@@ -311,7 +313,7 @@ int stq_q8_linear_dx(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
 
 int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t* xq, uint64_t ldx, const float* xscale,
                      uint64_t t, uint32_t n, uint32_t k, void* dw, uint64_t lddw, int out_dtype, void* stream) {
-  if (!h) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
   STQ_TRY(check_dtype(out_dtype));
   STQ_TRY(check_size(t, n));
   STQ_TRY(check_size(t, k));
@@ -340,7 +342,8 @@ int stq_q8_linear_dw(stq_handle* h, const void* dy, uint64_t lddy, const int8_t*
 
 int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, uint64_t t, uint32_t n, float* db,
                      void* stream) {
-  if (!h || !db) return STQ_E_NULL;
+  STQ_TRY(check_handle(h));
+  if (!db) return STQ_E_NULL;
   STQ_TRY(check_dtype(dtype));
   STQ_TRY(check_size(t, n));
   if (!aligned(db, 4)) return STQ_E_ALIGN;

@@ -6,7 +6,8 @@ operator runs in the library's kernels.  All matrices are two-dimensional with u
 is taken.  Each call enqueues its work on the current stream of the handle's device (or on ``stream``) and does not
 synchronise, except where a backward call needs more workspace than any before it (the old one is then freed).  One
 handle serves one stream at a time: its workspace is shared by the calls made through it, and by the graphs captured
-with it, which stay valid as long as the handle does.
+with it, which stay valid as long as the handle does.  Once a wait inside a kernel has run out (its results are invalid
+then), the handle's next call raises StqError with code -11; ``Handle.device_status()`` synchronises and asks.
 """
 from __future__ import annotations
 

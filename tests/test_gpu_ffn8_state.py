@@ -225,3 +225,20 @@ def test_activations_in_any_layout():
     he.float().sum().backward()
     assert torch.equal(one.grad, torch.full_like(one, 24.0))
     assert torch.equal(m(x.t().contiguous().t())[1], x)
+
+
+# ---- failures ----------------------------------------------------------------------------------------------------------
+def test_a_wait_that_ran_out_is_reported_by_the_next_call():
+    from paper_2604_06836_b200 import stq
+    m, x = block(), tokens()
+    m(x)
+    hd = m.handle_for(x.device)
+    hd.selftest_wait_timeout()
+    torch.cuda.synchronize()
+    with pytest.raises(stq.StqError) as e:
+        m(x)
+    assert e.value.code == -11
+    with pytest.raises(stq.StqError) as e:
+        q8.bias_grad(hd, x)
+    assert e.value.code == -11
+    assert served(block(), x).shape == x.shape            # a fresh handle works

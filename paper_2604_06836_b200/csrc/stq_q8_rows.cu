@@ -455,9 +455,15 @@ __global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowA
     for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(kFullMask, sum, m);
   }
   const float rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
+  // Where h * w is so small that it would be stored as zeros, but y may not be (eps holds rstd down, and that can be far
+  // above 1), y itself is coded: the largest |y| is the product of the largest |h * w| and rstd, rounded like every other.
+  const bool lift = __uint_as_float(top) < kTinyScale;
+  if (lift) top = bits_of(__uint_as_float(top) * rstd);
   Coding c = coding_of(top);
-  c.scale *= rstd;                                       // the scale of y; c.inv codes h * w
-  if (!(__uint_as_float(top) * rstd >= kTinyScale) && c.mask) { c.inv = 0.f; c.scale = 0.f; }
+  if (!lift) {
+    c.scale *= rstd;                                     // the scale of y; c.inv codes h * w
+    if (!(__uint_as_float(top) * rstd >= kTinyScale) && c.mask) { c.inv = 0.f; c.scale = 0.f; }
+  }
   if (rstd != rstd) { c.mask = 0u; c.scale = rstd; }
   if (warp == 0 && lane == 0) {
     a.scale[row] = c.scale;
@@ -465,6 +471,12 @@ __global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowA
   }
   for (uint32_t at = 0; at < cols; at += span) {
     if (!once) produce(at + first, r, unused, false);
+    if (lift) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[s][i] = mul2(r[s][i], both(rstd));
+    }
 #pragma unroll
     for (int s = 0; s < NS; ++s) write_unit<VEC>(a, row, at + first + s * step, lane, r[s], c);
   }

@@ -105,3 +105,27 @@ def test_the_workspace_does_not_grow_during_a_capture():
         assert torch.equal(a, b)
     del graph2
     h.close()
+
+
+# ---- norm ------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,cols", [(4, 96), (3, 257), (2, 2048), (1100, 1536), (2, 16640)])
+@pytest.mark.parametrize("size,eps", [(1e-32, 1e-6), (1e-33, 1e-12), (3e-30, 1e-6), (1e-35, 1e-6)])
+def test_norm_of_small_rows(handle, rows, cols, dtype, size, eps):
+    """eps lifts small rows: whether a row is stored as zeros goes by the norm's result, not by h * weight."""
+    x = (size * torch.randn(rows, cols, device="cuda", generator=gen(cols))).to(dtype)
+    w = 1 + 0.1 * torch.randn(cols, device="cuda", generator=gen(2))
+    out = q8.norm(handle, x, w, eps=eps, values=True)
+    xd = x.double()
+    y = xd * (xd.square().mean(1, keepdim=True) + eps).rsqrt() * w.double()
+    top = y.abs().amax(1)
+    clear = (top / 2.0 ** -100 - 1).abs() > 1e-5          # (a row on the limit may go either way)
+    zero = top < 2.0 ** -100
+    scale, codes = out.rows.scale.double(), out.rows.q.double()
+    assert (scale[zero & clear] == 0).all() and (codes[zero & clear] == 0).all()
+    keep = ~zero & clear
+    # rstd, the product with it, the scale: a few roundings each; codes off by that much next to a tie
+    assert ((scale - top / 127).abs()[keep] <= 16 * U * top[keep] / 127).all()
+    quot = y[keep] * (127 / top[keep])[:, None]
+    assert ((codes[keep] - quot).abs() <= 0.5 + 127 * 16 * U).all()
+    assert torch.equal(out.values, (out.rows.q.float() * out.rows.scale[:, None]).to(BF))

@@ -34,6 +34,10 @@ struct LinearArgs {
   int* err;
 };
 
+// A result from its integer sum, the same in every kernel.  The scales are applied one after the other: their product may
+// leave the range of fp32 where the result does not (two small scales lose digits, two large ones make a sum of 0 a NaN).
+__device__ __forceinline__ float scaled(int sum, float xs, float ws, float bias) { return fmaf((float)sum * xs, ws, bias); }
+
 // ---- batches ---------------------------------------------------------------------------------------------------------
 // Warp 0 keeps a ring of shared-memory stages full with tensor copies (128 bytes of the sum at a time, 128-byte swizzle,
 // out-of-range rows and columns read as zero), warp 1 issues the products into one of two accumulators in tensor
@@ -156,10 +160,10 @@ q8_linear_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constan
 #pragma unroll
         for (int i = 0; i < kC; i += 4) {
           const float4 ws = scale_n[acc][(c + i) / 4], b = bias_n[acc][(c + i) / 4];
-          v[i] = fmaf((float)__float_as_int(v[i]), xs * ws.x, b.x);
-          v[i + 1] = fmaf((float)__float_as_int(v[i + 1]), xs * ws.y, b.y);
-          v[i + 2] = fmaf((float)__float_as_int(v[i + 2]), xs * ws.z, b.z);
-          v[i + 3] = fmaf((float)__float_as_int(v[i + 3]), xs * ws.w, b.w);
+          v[i] = scaled(__float_as_int(v[i]), xs, ws.x, b.x);
+          v[i + 1] = scaled(__float_as_int(v[i + 1]), xs, ws.y, b.y);
+          v[i + 2] = scaled(__float_as_int(v[i + 2]), xs, ws.z, b.z);
+          v[i + 3] = scaled(__float_as_int(v[i + 3]), xs, ws.w, b.w);
         }
         if (!a.aligned)
           store_ragged(out + c, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col - c), lane, raw + (stages - smem_addr(raw)) + (warp - 2) * kStageBytes);
@@ -308,7 +312,7 @@ q8_linear_split_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_c
         if (p < size) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(meet + ((p * 128 + row) * pitch + c) * 4));
         sum += x;
       }
-      if (in) static_cast<O*>(a.out)[(size_t)(row0 + row) * a.ldo + c0 + c] = static_cast<O>(fmaf((float)sum, scale_t[row] * ws, b));
+      if (in) static_cast<O*>(a.out)[(size_t)(row0 + row) * a.ldo + c0 + c] = static_cast<O>(scaled(sum, scale_t[row], ws, b));
     }
   }
   if (!ok) *a.err = 1;
@@ -392,7 +396,7 @@ __global__ void __launch_bounds__(256) q8_linear_few_kernel(const int8_t* xq, si
     }
   const uint32_t t = lane / R, n = n0 + lane % R;
   if (lane < T * R && t < a.t && n < a.n)
-    static_cast<O*>(a.out)[t * a.ldo + n] = static_cast<O>(fmaf((float)mine, a.xs[t] * a.ws[n], a.bias ? a.bias[n] : 0.f));
+    static_cast<O*>(a.out)[t * a.ldo + n] = static_cast<O>(scaled(mine, a.xs[t], a.ws[n], a.bias ? a.bias[n] : 0.f));
 }
 
 // ---- up to 16 tokens -----------------------------------------------------------------------------------------------------
@@ -480,7 +484,7 @@ __global__ void __launch_bounds__(256) q8_linear_stream_kernel(const int8_t* xq,
 #pragma unroll
     for (int p = 0; p < 8; ++p) sum += part[(p * kTok + t) * kPitch + c];
     static_cast<O*>(a.out)[(t0 + t) * a.ldo + n0 + c] =
-        static_cast<O>(fmaf((float)sum, a.xs[t0 + t] * a.ws[n0 + c], a.bias ? a.bias[n0 + c] : 0.f));
+        static_cast<O>(scaled(sum, a.xs[t0 + t], a.ws[n0 + c], a.bias ? a.bias[n0 + c] : 0.f));
   }
 }
 

@@ -129,3 +129,25 @@ def test_norm_of_small_rows(handle, rows, cols, dtype, size, eps):
     quot = y[keep] * (127 / top[keep])[:, None]
     assert ((codes[keep] - quot).abs() <= 0.5 + 127 * 16 * U).all()
     assert torch.equal(out.values, (out.rows.q.float() * out.rows.scale[:, None]).to(BF))
+
+
+# ---- products --------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("t", [1, 3, 12, 130, 300, 3000])
+def test_scales_whose_product_leaves_the_range(handle, t):
+    """The result is in range although the product of its two scales is not: neither lost digits nor NaN."""
+    n, k = 264, 320
+    g = gen(t)
+    codes = [q8.alloc_rows(r, k, "cuda") for r in (t, n)]
+    for r in codes:
+        r.q.copy_(torch.randint(-127, 128, r.q.shape, device="cuda", generator=g, dtype=torch.int32).to(torch.int8))
+    x, w = codes
+    w.q[5] = 0                                             # a sum of zero
+    for sx, sw in ((2.0 ** -90 * 1.1, 2.0 ** -50 * 1.3), (2.0 ** 60 * 1.1, 2.0 ** 50 * 1.3), (2.0 ** 80 * 1.1, 2.0 ** 60 * 1.3)):
+        x.scale.fill_(sx), w.scale.fill_(sw)
+        sums = x.q.double() @ w.q.double().T
+        want = sums * x.scale.double()[:, None] * w.scale.double()
+        got = q8.linear(handle, x, w, dtype=F32).double()
+        fits = (want.abs() < 3.3e38) & ((want.abs() > 2.0 ** -120) | (sums == 0))
+        assert fits.any()
+        assert ((got - want).abs()[fits] <= 4 * U * want.abs()[fits]).all()
+        assert (got[:, 5] == 0).all()

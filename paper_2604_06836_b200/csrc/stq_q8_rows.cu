@@ -282,6 +282,14 @@ __device__ __forceinline__ float2 sigmoid2(float2 x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(t.y));
   return r;
 }
+// x held to [-most, most], NaN kept
+__device__ __forceinline__ float2 held(float2 x, float most) {
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(most));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(most));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-most));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-most));
+  return x;
+}
 constexpr float kGeluA = 1.5957691216057308f;             // 2 sqrt(2/pi): gelu(x) = x sigmoid(kGeluA (x + 0.044715 x^3))
 constexpr float kGeluB = 0.044715f;
 
@@ -805,11 +813,12 @@ __global__ void __launch_bounds__(256) q8_act_bwd_kernel(const ActBwdArgs a, uin
       // y u sg (1 + g (1 - sg))
       d0[i] = mul2(mul2(t, u), fma2(g, fma2(sg, both(-1.f), both(1.f)), both(1.f)));
     } else {
-      const float2 g2 = mul2(g, g), v = mul2(both(kGeluA), mul2(g, fma2(both(kGeluB), g2, both(1.f))));
+      // y sg (1 + x (1 - sg) kGeluA (1 + 3 kGeluB x^2)).  From |x| = 14 on the derivative is 0 or 1 in fp32, so x is held
+      // there: its cube would overflow and meet the 0.
+      const float2 x = held(g, 20.f), x2 = mul2(x, x), v = mul2(both(kGeluA), mul2(x, fma2(both(kGeluB), x2, both(1.f))));
       const float2 sg = sigmoid2(v);
-      // y sg (1 + g (1 - sg) kGeluA (1 + 3 kGeluB g^2))
-      const float2 in = mul2(both(kGeluA), fma2(both(3.f * kGeluB), g2, both(1.f)));
-      d0[i] = mul2(mul2(y, sg), fma2(mul2(g, fma2(sg, both(-1.f), both(1.f))), in, both(1.f)));
+      const float2 in = mul2(both(kGeluA), fma2(both(3.f * kGeluB), x2, both(1.f)));
+      d0[i] = mul2(mul2(y, sg), fma2(mul2(x, fma2(sg, both(-1.f), both(1.f))), in, both(1.f)));
     }
   }
   T* dz = static_cast<T*>(a.dz.p) + row * a.dz.ld;

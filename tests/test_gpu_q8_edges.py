@@ -151,3 +151,33 @@ def test_scales_whose_product_leaves_the_range(handle, t):
         assert fits.any()
         assert ((got - want).abs()[fits] <= 4 * U * want.abs()[fits]).all()
         assert (got[:, 5] == 0).all()
+
+
+# ---- activations -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("kind", ["silu_gated", "gelu"])
+@pytest.mark.parametrize("cols", [128, 131, 258])
+def test_act_backward_of_large_inputs(handle, kind, dtype, cols):
+    """The derivative of a saturated activation is 0 or 1, up to the type's largest and lowest values."""
+    parts = 2 if kind == "silu_gated" else 1
+    sizes = [15.0, 40.0, 1e6, 2e13, 1e15, 1e20, 3.3e38]
+    z = torch.randn(2 * len(sizes), parts * cols, device="cuda", generator=gen(5))
+    for i, s in enumerate(sizes):
+        z[2 * i, 3], z[2 * i + 1, 3] = s, -s
+    ck = q8.act(handle, z.to(dtype), kind, checkpoint=True).checkpoint
+    da = torch.randn(z.shape[0], cols, device="cuda", generator=gen(6)).to(dtype)
+    dz = q8.act_backward(handle, da, ck).double()
+    kept = ck.values().double().requires_grad_(True)
+    if kind == "silu_gated":
+        a = kept[:, :cols] * torch.sigmoid(kept[:, :cols]) * kept[:, cols:]
+    else:
+        a = torch.nn.functional.gelu(kept, approximate="tanh")
+    a.backward(da.double())
+    want = kept.grad
+    assert torch.isfinite(dz).all()
+    ok = want.abs() < 3.3e38
+    kd = kept.detach().abs()
+    # where the sigmoid is not saturated the size of the terms, |g| <= 40, carries the exponent's rounding
+    size = da.double().abs().repeat(1, parts) * (1 + kd.clamp(max=40)) * (1 + (kd[:, cols:].repeat(1, 2) if parts == 2 else 0))
+    tol = 1e-5 * size + 1e-5 * want.abs() + (2.0 ** -8 * 1.01 * want.abs() if dtype == BF else 0)
+    assert ((dz - want).abs() <= tol)[ok].all()

@@ -928,29 +928,44 @@ cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream) {
 }
 
 namespace {
-constexpr uint32_t kBwdRegCols = kBwdWarps * 2 * kUnit;   // widest row that stays in registers (2 units to a warp)
 struct BwdShape {
-  int warps, ns, gangs;
+  int warps, ns, gangs;      // (0 warps: the wide kernel)
   size_t smem;
   uint32_t ctas;             // rows of partial sums
 };
-// CTAs of a kernel that an SM holds at once, asked for once per number of warps (the same on every device of this kind).
+// Whether there is a variant with two units to a warp, for rows of 17 to 32 units (with one they end at 16; without the
+// variant the wide kernel takes over).  Next to the wide kernel, in us on 4096 rows of 5120 to 5122 and of 8190 to 8192
+// columns:       16-byte accesses          pairs                 single elements
+//   bf16         33.5 (84), 42.6 (117)     - , 47.4 (75)         113 (82), 144 (114)
+//   fp32         86.7 (111), 113 (159)     89.0 (74), 108 (108)  78.0 (79), 99.3 (112)
+// (all but the first two spill, 200 to 324 bytes).
+constexpr bool two_units(size_t elem, int vec) { return elem == 2 ? vec != 1 : vec != 2; }
+bool bwd_wide(uint32_t cols, int dtype, int vec) { return cols > kBwdWarps * (two_units(elem_bytes(dtype), vec) ? 2 : 1) * kUnit; }
+
+template <class T, int VEC, class F>
+cudaError_t by_units(int ns, F f) {
+  if constexpr (two_units(sizeof(T), VEC))
+    if (ns == 2) return f(std::integral_constant<int, 2>());
+  return f(std::integral_constant<int, 1>());
+}
+// CTAs of a kernel that an SM holds at once, asked for once per number of warps to a row, which decides the rest (the same
+// on every device of this kind).
 template <class T, int VEC, int NS>
-int bwd_resident(int warps, size_t smem) {
+int bwd_resident(int warps, int gangs, size_t smem) {
   static std::atomic<int> known[kBwdWarps + 1];
   int n = known[warps].load(std::memory_order_relaxed);
   if (n == 0) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, q8_norm_bwd_kernel<T, VEC, NS>, warps * 32, smem) != cudaSuccess || n < 1) n = 1;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, q8_norm_bwd_kernel<T, VEC, NS>, warps * gangs * 32, smem) != cudaSuccess || n < 1) n = 1;
     known[warps].store(n, std::memory_order_relaxed);
   }
   return n;
 }
 
 // CTAs of at least 8 warps, as many as are resident at once (with more, some would start when the others are done).
-// Two units to a warp are faster where they fit (bf16, 8192 x 4096: 59 -> 47 us, 8192 x 1600: 36 -> 24 us) and slower where
-// they spill, which is with fp32 (4096 x 4096: 46 -> 78 us) and with single elements.
+// Where one unit to a warp is enough, two are faster with bf16 in 16-byte accesses or pairs (8192 x 4096: 59 -> 47 us,
+// 8192 x 1600: 36 -> 24 us) and slower with fp32 (4096 x 4096: 46 -> 78 us) and single elements.
 BwdShape bwd_shape(uint64_t rows, uint32_t cols, int dtype, int vec, int sms) {
-  if (cols > kBwdRegCols) return {0, 0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
+  if (bwd_wide(cols, dtype, vec)) return {0, 0, 0, 0, (uint32_t)(rows < (uint64_t)sms ? rows : sms)};
   const uint32_t units = (cols + kUnit - 1) / kUnit;
   const int ns = units > kBwdWarps || (units > 1 && dtype == STQ_GRAD_BF16 && vec > 1) ? 2 : 1;
   const int warps = (int)((units + ns - 1) / ns), most_of = ns == 2 ? kBwdWarps : 8;
@@ -960,8 +975,10 @@ BwdShape bwd_shape(uint64_t rows, uint32_t cols, int dtype, int vec, int sms) {
   by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
     return by_vec(vec, [&](auto v) {
-      per_sm = ns == 1 ? bwd_resident<T, v(), 1>(warps * gangs, smem) : bwd_resident<T, v(), 2>(warps * gangs, smem);
-      return cudaSuccess;
+      return by_units<T, v()>(ns, [&](auto n) {
+        per_sm = bwd_resident<T, v(), n()>(warps, gangs, smem);
+        return cudaSuccess;
+      });
     });
   });
   const uint64_t want = (rows + gangs - 1) / gangs, most = (uint64_t)sms * per_sm;
@@ -991,7 +1008,7 @@ cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStr
   const cudaError_t e = by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
     return by_vec(width, [&](auto vec) {
-      if (a.cols > kBwdRegCols) {
+      if (sh.warps == 0) {
         const int bytes = (int)(a.cols * sizeof(float));
         cudaError_t e2 = cudaFuncSetAttribute(q8_norm_bwd_wide_kernel<T, vec()>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e2 != cudaSuccess) return e2;
@@ -999,11 +1016,10 @@ cudaError_t launch_q8_norm_bwd(int dtype, const NormBwdArgs& a, int sms, cudaStr
         return cudaGetLastError();
       }
       const int threads = sh.warps * sh.gangs * 32;
-      if (sh.ns == 1)
-        q8_norm_bwd_kernel<T, vec(), 1><<<sh.ctas, threads, sh.smem, stream>>>(a, sh.warps, sh.gangs);
-      else
-        q8_norm_bwd_kernel<T, vec(), 2><<<sh.ctas, threads, sh.smem, stream>>>(a, sh.warps, sh.gangs);
-      return cudaGetLastError();
+      return by_units<T, vec()>(sh.ns, [&](auto n) {
+        q8_norm_bwd_kernel<T, vec(), n()><<<sh.ctas, threads, sh.smem, stream>>>(a, sh.warps, sh.gangs);
+        return cudaGetLastError();
+      });
     });
   });
   if (e != cudaSuccess || sh.ctas <= kJoin) return e;

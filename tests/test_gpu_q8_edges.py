@@ -131,6 +131,27 @@ def test_norm_of_small_rows(handle, rows, cols, dtype, size, eps):
     assert torch.equal(out.values, (out.rows.q.float() * out.rows.scale[:, None]).to(BF))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("cols", [4096, 4097, 4098, 4104, 5121, 8190, 8191, 8192, 8193, 8194, 8200])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_norm_backward_where_its_variants_change(handle, rows, cols, dtype):
+    g = gen(rows + cols)
+    h, dy, dres = ((s * torch.randn(rows, cols, device="cuda", generator=g)).to(dtype) for s in (2.0, 1e-3, 1e-3))
+    w = 1 + 0.1 * torch.randn(cols, device="cuda", generator=g)
+    rstd = (h.double().square().mean(1) + 1e-6).rsqrt().float()
+    dx, dw = q8.norm_backward(handle, dy, h, w, rstd, dres=dres)
+    rs = rstd.double()[:, None]
+    xh, up = h.double() * rs, dy.double() * w.double()
+    want = rs * (up - xh * (up * xh).mean(1, keepdim=True)) + dres.double()
+    # a sum of `cols` terms in a tree of at most 8 * 32 and log2 steps; the mean of terms of either sign is small beside them
+    size = rs * (up.abs() + xh.abs() * (up * xh).abs().mean(1, keepdim=True)) + dres.double().abs()
+    tol = 64 * U * size + (2.0 ** -8 * 1.01 * want.abs() if dtype == BF else 0)
+    assert ((dx.double() - want).abs() <= tol).all()
+    assert ((dw.double() - (dy.double() * xh).sum(0)).abs() <= 64 * U * (dy.double() * xh).abs().sum(0)).all()
+    again = q8.norm_backward(handle, dy, h, w, rstd, dres=dres)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
 # ---- products --------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("t", [1, 3, 12, 130, 300, 3000])
 def test_scales_whose_product_leaves_the_range(handle, t):

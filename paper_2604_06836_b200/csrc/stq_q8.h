@@ -34,8 +34,8 @@ struct RowArgs {
   float* cks;            // its scales [rows][parts][ceil(cols/128)]
 };
 
-cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, cudaStream_t stream);
-cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream);
+cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, int sms, cudaStream_t stream);
+cudaError_t launch_q8_norm(int dtype, const RowArgs& a, int sms, cudaStream_t stream);
 
 struct NormBwdArgs {
   Mat dy, h, dres, dx;   // dres may be null

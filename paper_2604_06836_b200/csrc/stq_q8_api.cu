@@ -115,7 +115,7 @@ int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t 
   a.rows = rows; a.cols = cols;
   a.q = q; a.ldq = ldq; a.scale = scale;
   STQ_CUDA(h, cudaSetDevice(h->device));
-  STQ_CUDA(h, stq::launch_q8_act(dtype, stq::kQ8Copy, a, static_cast<cudaStream_t>(stream)));
+  STQ_CUDA(h, stq::launch_q8_act(dtype, stq::kQ8Copy, a, h->sm_count, static_cast<cudaStream_t>(stream)));
   h->launches++;
   return STQ_OK;
 }
@@ -152,7 +152,7 @@ int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uin
   a.q = q; a.ldq = ldq; a.scale = scale;
   a.values = {values, ldv};
   STQ_CUDA(h, cudaSetDevice(h->device));
-  STQ_CUDA(h, stq::launch_q8_norm(dtype, a, static_cast<cudaStream_t>(stream)));
+  STQ_CUDA(h, stq::launch_q8_norm(dtype, a, h->sm_count, static_cast<cudaStream_t>(stream)));
   h->launches++;
   return STQ_OK;
 }
@@ -221,7 +221,7 @@ int stq_q8_act(stq_handle* h, const void* z, uint64_t ldz, int kind, int dtype, 
   a.ckq = ckq; a.ldck = ldck; a.cks = ckscale;
   STQ_CUDA(h, cudaSetDevice(h->device));
   STQ_CUDA(h, stq::launch_q8_act(dtype, kind == STQ_ACT_SILU_GATED ? stq::kQ8SiluGated : stq::kQ8Gelu, a,
-                                 static_cast<cudaStream_t>(stream)));
+                                 h->sm_count, static_cast<cudaStream_t>(stream)));
   h->launches++;
   return STQ_OK;
 }

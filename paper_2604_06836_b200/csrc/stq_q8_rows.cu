@@ -842,17 +842,25 @@ struct Width {
   }
 };
 
-// Warps per row and units per warp (rows of more units than warps can hold are read twice).  Few rows want many warps
-// to a row (one token of 6400 columns: 3.2 us with one unit to a warp, 3.5 with two).  Many rows want fewer warps that
-// wait for one another: the gated activation on 8192 x 6400 takes 147, 96 and 113 us with 1, 2 and 4 units to a warp,
-// the norm on 8192 x 4096 in bf16 55, 60 and 50 us (with narrower accesses 2 units were best there too).
+// Warps per row and units per warp.  One unit to a warp, so many warps to a row, is fastest as long as the device holds all
+// rows at once (32 warps an SM); beyond that fewer warps, with several units each, wait for one another.  Rows of more units
+// than 16 warps keep are read twice: with 4 units to a warp, which only the norm of bf16 in 16-byte accesses has, those are
+// the rows of more than 64 units, and for them 2 are faster again.  In us with 1, 2 (and 4) units to a warp, * what is taken:
+//   rows x columns        512 x 1600       256 x 4096       512 x 4096       8192 x 1600       8192 x 4096
+//   norm, bf16            3.33* 3.31 3.66  3.80* 3.69 3.84  7.38 5.87 6.37*  26.5 24.2 22.2*   57.0 53.2 43.3*
+//   norm, fp32            5.01* 5.15       5.51* 5.55       8.92 8.09*       35.1 31.0*        86.2 68.9*
+//   rows x columns        4096 x 512       64 x 10240       256 x 16384      4096 x 16384      4096 x 20480
+//   norm, bf16            6.97 5.51* 7.32  - 5.01 3.81*     - 10.4 10.9*     - 109 102*        - 138* 188
+//   rows x columns        512 x 1600       128 x 6400       256 x 6400       8192 x 1600       8192 x 6400
+//   gated, checkpoint     3.16* 3.66       3.30* 3.65       6.55 5.69*       30.5 25.8*        131 89.8*
+//   rows x columns        512 x 1600       128 x 6400       512 x 6400       6400 x 1600       6400 x 6400
+//   plain rows, fp32      2.29* 2.30       2.43* 2.42       6.02 5.34*       11.1 10.1*        43.5 35.1*
 struct Shape {
   int warps, ns;
 };
-Shape shape_of(int ns, uint32_t cols) {
+Shape shape_of(uint64_t rows, uint32_t cols, int most_ns, int sms) {
   const uint32_t units = (cols + kUnit - 1) / kUnit;
-  if (units == 1) ns = 1;
-  if (units > 32 && ns == 1) ns = 2;
+  const int ns = units == 1 || (units <= 32 && rows * units <= 32ull * sms) ? 1 : units == 2 || units > 64 ? 2 : most_ns;
   const int w = (int)((units + ns - 1) / ns);
   return {w < most_warps(ns) ? w : most_warps(ns), ns};
 }
@@ -878,11 +886,11 @@ size_t elem_bytes(int dtype) { return dtype == STQ_GRAD_F32 ? 4 : 2; }
 
 }  // namespace
 
-cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, cudaStream_t stream) {
+cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, int sms, cudaStream_t stream) {
   Width w;
   w.add(a.x, elem_bytes(dtype));
   w.add(a.values, 2);
-  const Shape sh = shape_of(a.rows < 256 ? 1 : 2, a.cols);
+  const Shape sh = shape_of(a.rows, a.cols, 2, sms);
   const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
   const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {
@@ -898,7 +906,7 @@ cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, cudaStream_t
   });
 }
 
-cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream) {
+cudaError_t launch_q8_norm(int dtype, const RowArgs& a, int sms, cudaStream_t stream) {
   Width w;
   w.add(a.x, elem_bytes(dtype));
   w.add(a.res, elem_bytes(dtype));
@@ -906,8 +914,7 @@ cudaError_t launch_q8_norm(int dtype, const RowArgs& a, cudaStream_t stream) {
   w.add(a.values, 2);
   w.add(Mat{const_cast<float*>(a.weight), 0}, 4);
   const int vec = w.vec(a.cols);
-  const bool few = a.rows < 1024;
-  const Shape sh = shape_of(dtype == STQ_GRAD_BF16 && vec == 8 ? (few || a.cols <= 2 * kUnit ? 1 : 4) : a.rows < 256 ? 1 : 2, a.cols);
+  const Shape sh = shape_of(a.rows, a.cols, dtype == STQ_GRAD_BF16 && vec == 8 ? 4 : 2, sms);
   const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
   const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {

@@ -132,6 +132,34 @@ def test_norm_of_small_rows(handle, rows, cols, dtype, size, eps):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("rows,cols", [(4736, 200), (4737, 200), (2368, 512), (2369, 512), (2369, 510), (676, 1600), (677, 1600), (677, 1601),
+                                       (296, 4096), (297, 4096), (148, 8192), (149, 8192), (300, 8190), (5, 8200), (300, 10240), (300, 16384),
+                                       (5, 16392), (300, 16392)])
+def test_row_kernels_where_their_shape_changes(handle, rows, cols, dtype):
+    """The same rows alone and among others, on both sides of every limit: the norm, the gated activation with its
+    checkpoint, plain rows."""
+    g = gen(rows + cols)
+    x, res = (torch.randn(rows, cols, device="cuda", generator=g).to(dtype) for _ in range(2))
+    w = 1 + 0.1 * torch.randn(cols, device="cuda", generator=g)
+    out = q8.norm(handle, x, w, residual=res, eps=1e-6)
+    hd = x.double() + res.double()
+    rstd = (hd.square().mean(1) + 1e-6).rsqrt()
+    y = hd * rstd[:, None] * w.double()
+    top = y.abs().amax(1, keepdim=True)
+    assert torch.equal(out.h, (x.float() + res.float()).to(dtype)) and ((out.rstd.double() - rstd).abs() <= 40 * U * rstd).all()
+    assert ((out.rows.scale.double() - top[:, 0] / 127).abs() <= 48 * U * top[:, 0] / 127).all()
+    assert ((out.rows.q.double() - y * (127 / top)).abs() <= 0.5 + 127 * 5 * U).all()
+    few = slice(rows - 2, rows)
+    r = q8.quantize_rows(handle, x)
+    z = torch.cat([x, res], dim=1)
+    a = q8.act(handle, z, "silu_gated", checkpoint=True)
+    r2, a2 = q8.quantize_rows(handle, x[few]), q8.act(handle, z[few], "silu_gated", checkpoint=True)
+    assert torch.equal(r.q[few], r2.q) and torch.equal(r.scale[few], r2.scale)
+    assert torch.equal(a.rows.q[few], a2.rows.q) and torch.equal(a.rows.scale[few], a2.rows.scale)
+    assert torch.equal(a.checkpoint.q[few, :, :cols], a2.checkpoint.q[:, :, :cols]) and torch.equal(a.checkpoint.scale[few], a2.checkpoint.scale)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("cols", [4096, 4097, 4098, 4104, 5121, 8190, 8191, 8192, 8193, 8194, 8200])
 @pytest.mark.parametrize("rows", [3, 300])
 def test_norm_backward_where_its_variants_change(handle, rows, cols, dtype):

@@ -271,8 +271,8 @@ __device__ __forceinline__ void write_unit(const RowArgs& a, uint64_t row, uint3
   }
 }
 
-// 1 / (1 + exp(-x)): the special-function unit's exponential and reciprocal, 2^-22 each; an exponential that overflows
-// gives 0.
+// 1 / (1 + exp(-x)): the special-function unit's exponential and reciprocal, 2^-22 each, and the rounding of the exponential's
+// argument, |x| 2^-24 of the result where that is small; an exponential that overflows gives 0.
 __device__ __forceinline__ float2 sigmoid2(float2 x) {
   float2 t = mul2(x, both(-1.4426950408889634f)), r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(t.x));

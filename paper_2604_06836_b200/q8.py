@@ -350,7 +350,8 @@ def linear(handle: stq.Handle, x: Rows8, w: Rows8, *, bias: torch.Tensor | None 
 
 
 def linear_dx(handle: stq.Handle, dy: torch.Tensor, w: Rows8, *, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
-    """Gradient of ``linear``'s input: dy [t, n] (bfloat16) times the values of w [n, k]."""
+    """Gradient of ``linear``'s input: dy [t, n] (bfloat16) times the values of w [n, k].  For a bfloat16 result the values
+    are rounded to bfloat16 on the way, with float32 they are not."""
     if stream is not None:
         with _On(stream, (dy, *w)):
             return linear_dx(handle, dy, w, dtype=dtype)
@@ -369,7 +370,7 @@ def linear_dx(handle: stq.Handle, dy: torch.Tensor, w: Rows8, *, dtype=torch.bfl
 
 def linear_dw(handle: stq.Handle, dy: torch.Tensor, x: Rows8, *, dtype=torch.bfloat16, stream=None) -> torch.Tensor:
     """Gradient of ``linear``'s weight from its input as it was saved in 8 bits: dy [t, n] (bfloat16) transposed times
-    the values of x [t, k]."""
+    the values of x [t, k].  For a bfloat16 result the values are rounded to bfloat16 on the way, with float32 they are not."""
     if stream is not None:
         with _On(stream, (dy, *x)):
             return linear_dw(handle, dy, x, dtype=dtype)

@@ -305,7 +305,8 @@ int stq_q8_rows(stq_handle* h, const void* x, uint64_t ldx, int dtype, uint64_t 
 /* h = x + res (res and hsum NULL: h = x), rstd = 1 / sqrt(mean h^2 + eps) from the unrounded sum, eps > 0,
  * y = h * rstd * weight as 8-bit rows.  Writes hsum (rounded to dtype), rstd[rows], codes, scales and, if
  * `values` is not NULL, the bf16 values that the codes stand for.  weight: fp32[cols].  Whether a row is stored
- * as zeros goes by y.  The mean of squares is held in fp32: from |h| of about 1e19 on it is infinite, and y zero. */
+ * as zeros goes by y (and with eps below 2^-40 also by h * weight, below 2^-120).  The mean of squares is held in
+ * fp32: from |h| of about 1e19 on it is infinite, and y zero. */
 int stq_q8_norm(stq_handle* h, const void* x, uint64_t ldx, const void* res, uint64_t ldres, const float* weight,
                 float eps, int dtype, uint64_t rows, uint32_t cols, void* hsum, uint64_t ldh, float* rstd, int8_t* q,
                 uint64_t ldq, float* scale, void* values, uint64_t ldv, void* stream);

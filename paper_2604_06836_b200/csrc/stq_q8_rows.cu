@@ -22,6 +22,7 @@ namespace {
 
 constexpr uint32_t kFullMask = 0xffffffffu;
 constexpr float kTinyScale = 7.8886090522101181e-31f;   // 2^-100: rows and blocks below it are stored as zeros
+constexpr float kTinyProduct = 7.5231638452626401e-37f; // 2^-120: the least h * w that the norm codes
 constexpr uint32_t kUnit = 256;
 
 // column of element e (0..7) of `lane` in the unit that begins at `base`
@@ -232,13 +233,13 @@ struct Coding {
   float inv, scale;
   uint32_t mask;
 };
-__device__ __forceinline__ Coding coding_of(uint32_t top) {
+__device__ __forceinline__ Coding coding_of(uint32_t top, float tiny = kTinyScale) {
   const float a = __uint_as_float(top);
   Coding c;
   c.mask = 0xffffffffu;
   c.inv = 127.f * (1.f / a);
   c.scale = a * (1.f / 127.f);
-  if (a < kTinyScale) { c.inv = 0.f; c.scale = 0.f; }
+  if (a < tiny) { c.inv = 0.f; c.scale = 0.f; }
   // something in the row is not finite: no code can say so, the scale does
   if (top >= 0x7f800000u) { c.inv = 0.f; c.scale = __uint_as_float(0x7fc00000u); c.mask = 0u; }
   return c;
@@ -463,15 +464,11 @@ __global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowA
     for (int m = 16; m; m >>= 1) sum += __shfl_xor_sync(kFullMask, sum, m);
   }
   const float rstd = 1.f / sqrtf(sum / (float)cols + a.eps);
-  // Where h * w is so small that it would be stored as zeros, but y may not be (eps holds rstd down, and that can be far
-  // above 1), y itself is coded: the largest |y| is the product of the largest |h * w| and rstd, rounded like every other.
-  const bool lift = __uint_as_float(top) < kTinyScale;
-  if (lift) top = bits_of(__uint_as_float(top) * rstd);
-  Coding c = coding_of(top);
-  if (!lift) {
-    c.scale *= rstd;                                     // the scale of y; c.inv codes h * w
-    if (!(__uint_as_float(top) * rstd >= kTinyScale) && c.mask) { c.inv = 0.f; c.scale = 0.f; }
-  }
+  // Whether the row is stored as zeros goes by y, which eps can lift far above h * w.  127 / max|h * w| is in range from 2^-120
+  // on; what lies below has a y below 2^-100 unless eps is below 2^-40.
+  Coding c = coding_of(top, kTinyProduct);
+  c.scale *= rstd;                                       // the scale of y; c.inv codes h * w
+  if (!(__uint_as_float(top) * rstd >= kTinyScale) && c.mask) { c.inv = 0.f; c.scale = 0.f; }
   if (rstd != rstd) { c.mask = 0u; c.scale = rstd; }
   if (warp == 0 && lane == 0) {
     a.scale[row] = c.scale;
@@ -479,12 +476,6 @@ __global__ void __launch_bounds__(most_warps(NS) * 32) q8_norm_kernel(const RowA
   }
   for (uint32_t at = 0; at < cols; at += span) {
     if (!once) produce(at + first, r, unused, false);
-    if (lift) {
-#pragma unroll
-      for (int s = 0; s < NS; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[s][i] = mul2(r[s][i], both(rstd));
-    }
 #pragma unroll
     for (int s = 0; s < NS; ++s) write_unit<VEC>(a, row, at + first + s * step, lane, r[s], c);
   }
@@ -842,27 +833,45 @@ struct Width {
   }
 };
 
-// Warps per row and units per warp.  One unit to a warp, so many warps to a row, is fastest as long as the device holds all
-// rows at once (32 warps an SM); beyond that fewer warps, with several units each, wait for one another.  Rows of more units
-// than 16 warps keep are read twice: with 4 units to a warp, which only the norm of bf16 in 16-byte accesses has, those are
-// the rows of more than 64 units, and for them 2 are faster again.  In us with 1, 2 (and 4) units to a warp, * what is taken:
-//   rows x columns        512 x 1600       256 x 4096       512 x 4096       8192 x 1600       8192 x 4096
-//   norm, bf16            3.33* 3.31 3.66  3.80* 3.69 3.84  7.38 5.87 6.37*  26.5 24.2 22.2*   57.0 53.2 43.3*
-//   norm, fp32            5.01* 5.15       5.51* 5.55       8.92 8.09*       35.1 31.0*        86.2 68.9*
-//   rows x columns        4096 x 512       64 x 10240       256 x 16384      4096 x 16384      4096 x 20480
-//   norm, bf16            6.97 5.51* 7.32  - 5.01 3.81*     - 10.4 10.9*     - 109 102*        - 138* 188
-//   rows x columns        512 x 1600       128 x 6400       256 x 6400       8192 x 1600       8192 x 6400
-//   gated, checkpoint     3.16* 3.66       3.30* 3.65       6.55 5.69*       30.5 25.8*        131 89.8*
-//   rows x columns        512 x 1600       128 x 6400       512 x 6400       6400 x 1600       6400 x 6400
-//   plain rows, fp32      2.29* 2.30       2.43* 2.42       6.02 5.34*       11.1 10.1*        43.5 35.1*
+// Warps per row and units per warp.  One unit to a warp, so many warps to a row, is fastest as long as all rows run at once;
+// beyond that fewer warps, with several units each, wait for one another.  Rows of more units than 16 warps keep are read
+// twice: with 4 units to a warp, which only the norm of bf16 in 16-byte accesses has, those are the rows of more than 64
+// units, and for them 2 are faster again.  (Just past a whole number of rounds each choice loses up to 15 % to one whose
+// rounds fit: norm, bf16, 512 x 6400 8.7 us with one unit, 10.0 with the four that are taken.)  In us with 1, 2 (and 4) units
+// to a warp, * what is taken:
+//   rows x columns        585 x 1600       857 x 1600       1342 x 1600      512 x 4096       750 x 4096      8192 x 4096
+//   norm, bf16            3.30* 3.55 4.31  4.82* 5.00 5.79  7.18 7.69 6.78*  6.03* 5.80 6.73  8.44 8.65 7.70*  57.0 53.2 43.3*
+//   norm, fp32            4.90* 5.33       6.20* 6.15       8.74 9.44*       8.75 7.91*       10.7 11.2*       86.2 68.9*
+//   rows x columns        4096 x 512       64 x 10240       256 x 16384      4096 x 16384     4096 x 20480
+//   norm, bf16            6.31* 5.52 7.39  - 5.01 3.81*     - 10.4 10.9*     - 109 102*       - 138* 188
+//   rows x columns        585 x 1600       671 x 1600       96 x 6400        163 x 6400       8192 x 6400
+//   gated, checkpoint     3.31* 3.64       4.49 4.02*       3.30* 3.47       5.30 4.52*       131 89.8*
+//   rows x columns        512 x 1600       1600 x 1600      128 x 6400       512 x 6400       6400 x 6400
+//   plain rows, fp32      2.29* 2.30       4.78 4.52*       2.43* 2.42       6.02 5.34*       43.5 35.1*
 struct Shape {
   int warps, ns;
+  unsigned grid;
+  int threads;
 };
-Shape shape_of(uint64_t rows, uint32_t cols, int most_ns, int sms) {
+// CTAs of a kernel that an SM holds at once, asked for once per number of warps (the same on every device of this kind).
+template <auto* KERNEL>
+int resident(int warps) {
+  static std::atomic<int> known[33];
+  int n = known[warps].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, KERNEL, warps * 32, 0) != cudaSuccess || n < 1) n = 1;
+    known[warps].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+// ONE: the kernel with one unit to a warp; most: the most units that a warp keeps.
+template <auto* ONE>
+Shape shape_of(uint64_t rows, uint32_t cols, int most, int sms) {
   const uint32_t units = (cols + kUnit - 1) / kUnit;
-  const int ns = units == 1 || (units <= 32 && rows * units <= 32ull * sms) ? 1 : units == 2 || units > 64 ? 2 : most_ns;
-  const int w = (int)((units + ns - 1) / ns);
-  return {w < most_warps(ns) ? w : most_warps(ns), ns};
+  const bool at_once = units <= 32 && (rows <= (uint64_t)sms || rows <= (uint64_t)sms * resident<ONE>((int)units));
+  const int ns = units == 1 || at_once ? 1 : units == 2 || units > 64 ? 2 : most;
+  const int w = (int)((units + ns - 1) / ns), warps = w < most_warps(ns) ? w : most_warps(ns);
+  return {warps, ns, (unsigned)(warps == 1 ? (rows + 3) / 4 : rows), warps == 1 ? 128 : warps * 32};
 }
 
 template <class F>
@@ -890,18 +899,19 @@ cudaError_t launch_q8_act(int dtype, Q8Kind kind, const RowArgs& a, int sms, cud
   Width w;
   w.add(a.x, elem_bytes(dtype));
   w.add(a.values, 2);
-  const Shape sh = shape_of(a.rows, a.cols, 2, sms);
-  const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
-  const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
     return by_vec(w.vec(a.cols), [&](auto vec) {
-      return by_ns(sh.ns, [&](auto ns) {
-        if (kind == kQ8Copy) q8_act_kernel<T, vec(), ns(), kQ8Copy><<<grid, threads, 0, stream>>>(a, sh.warps);
-        if (kind == kQ8SiluGated) q8_act_kernel<T, vec(), ns(), kQ8SiluGated><<<grid, threads, 0, stream>>>(a, sh.warps);
-        if (kind == kQ8Gelu) q8_act_kernel<T, vec(), ns(), kQ8Gelu><<<grid, threads, 0, stream>>>(a, sh.warps);
-        return cudaGetLastError();
-      });
+      auto launch = [&](auto k) {
+        const Shape sh = shape_of<q8_act_kernel<T, vec(), 1, k()>>(a.rows, a.cols, 2, sms);
+        return by_ns(sh.ns, [&](auto ns) {
+          q8_act_kernel<T, vec(), ns(), k()><<<sh.grid, sh.threads, 0, stream>>>(a, sh.warps);
+          return cudaGetLastError();
+        });
+      };
+      if (kind == kQ8SiluGated) return launch(std::integral_constant<int, kQ8SiluGated>());
+      if (kind == kQ8Gelu) return launch(std::integral_constant<int, kQ8Gelu>());
+      return launch(std::integral_constant<int, kQ8Copy>());
     });
   });
 }
@@ -913,21 +923,19 @@ cudaError_t launch_q8_norm(int dtype, const RowArgs& a, int sms, cudaStream_t st
   if (a.res.p) w.add(a.h, elem_bytes(dtype));
   w.add(a.values, 2);
   w.add(Mat{const_cast<float*>(a.weight), 0}, 4);
-  const int vec = w.vec(a.cols);
-  const Shape sh = shape_of(a.rows, a.cols, dtype == STQ_GRAD_BF16 && vec == 8 ? 4 : 2, sms);
-  const unsigned grid = (unsigned)(sh.warps == 1 ? (a.rows + 3) / 4 : a.rows);
-  const int threads = sh.warps == 1 ? 128 : sh.warps * 32;
   return by_type(dtype, [&](auto tv) {
     using T = decltype(tv);
-    if constexpr (sizeof(T) == 2) {
-      if (sh.ns == 4) {
-        q8_norm_kernel<T, 8, 4><<<grid, threads, 0, stream>>>(a, sh.warps);
-        return cudaGetLastError();
+    return by_vec(w.vec(a.cols), [&](auto vec) {
+      constexpr int kMost = sizeof(T) == 2 && vec() == 8 ? 4 : 2;
+      const Shape sh = shape_of<q8_norm_kernel<T, vec(), 1>>(a.rows, a.cols, kMost, sms);
+      if constexpr (kMost == 4) {
+        if (sh.ns == 4) {
+          q8_norm_kernel<T, vec(), 4><<<sh.grid, sh.threads, 0, stream>>>(a, sh.warps);
+          return cudaGetLastError();
+        }
       }
-    }
-    return by_vec(vec, [&](auto v) {
       return by_ns(sh.ns, [&](auto ns) {
-        q8_norm_kernel<T, v(), ns()><<<grid, threads, 0, stream>>>(a, sh.warps);
+        q8_norm_kernel<T, vec(), ns()><<<sh.grid, sh.threads, 0, stream>>>(a, sh.warps);
         return cudaGetLastError();
       });
     });

@@ -837,7 +837,7 @@ struct Width {
 // beyond that fewer warps, with several units each, wait for one another.  Rows of more units than 16 warps keep are read
 // twice: with 4 units to a warp, which only the norm of bf16 in 16-byte accesses has, those are the rows of more than 64
 // units, and for them 2 are faster again.  (Just past a whole number of rounds each choice loses up to 15 % to one whose
-// rounds fit: norm, bf16, 512 x 6400 8.7 us with one unit, 10.0 with the four that are taken.)  In us with 1, 2 (and 4) units
+// rounds fit: norm, bf16, 512 x 6400 9.0 us with one unit, 10.3 with the four that are taken.)  In us with 1, 2 (and 4) units
 // to a warp, * what is taken:
 //   rows x columns        585 x 1600       857 x 1600       1342 x 1600      512 x 4096       750 x 4096      8192 x 4096
 //   norm, bf16            3.30* 3.55 4.31  4.82* 5.00 5.79  7.18 7.69 6.78*  6.03* 5.80 6.73  8.44 8.65 7.70*  57.0 53.2 43.3*

@@ -283,12 +283,10 @@ int stq_sm_count(const stq_handle* h);
  * overlap inputs (STQ_E_ALIAS).  Sums are held in fp32 (int32 in stq_q8_linear, exact) and are added in
  * a fixed order: results are the same from run to run.
  * Workspace: the backward calls use a workspace of the handle.  A call that needs more of it than any before
- * allocates (and, unless a captured graph uses the old buffer, frees that and so synchronises the device).
- * While a stream is captured it cannot grow: such a call returns STQ_E_WORKSPACE and leaves the capture as
- * it is; make a call of the same sizes before.  A buffer that a captured graph uses stays until
- * stq_destroy, so that the graph can be replayed after larger calls; the graph must not be replayed after
- * that.  Calls and replays of one handle that overlap on the GPU would share the workspace, so keep to one
- * handle per stream. */
+ * allocates, and outside a capture frees the old buffer, which synchronises the device.  A buffer that a
+ * captured graph uses stays until stq_destroy, so that the graph can be replayed after larger calls; the
+ * graph must not be replayed after that.  Calls and replays of one handle that overlap on the GPU would
+ * share the workspace, so keep to one handle per stream. */
 
 /* kind of stq_q8_act: a = silu(z[:, :cols]) * z[:, cols:], or gelu(z), tanh form */
 enum { STQ_ACT_SILU_GATED = 1, STQ_ACT_GELU = 2 };

@@ -63,8 +63,15 @@ int check_codes(const void* q, uint64_t ldq, uint64_t cols, const void* scale) {
     if (rc__ != STQ_OK) return rc__; \
   } while (0)
 
+// Lets this thread allocate while one of its streams is captured.
+struct AllocInCapture {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  AllocInCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~AllocInCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
 // The workspace of a call on `stream`.  It grows by being replaced.  A graph that was captured with the old buffer goes on
-// using it whenever it is replayed, so such a buffer is not freed.
+// using it whenever it is replayed, so such a buffer is not freed; nor is any during a capture, where freeing would wait.
 template <class T>
 int workspace(stq_handle* h, size_t count, cudaStream_t stream, T** out) {
   const size_t need = count * sizeof(T);
@@ -72,11 +79,7 @@ int workspace(stq_handle* h, size_t count, cudaStream_t stream, T** out) {
   STQ_CUDA(h, cudaStreamIsCapturing(stream, &status));
   const bool capturing = status != cudaStreamCaptureStatusNone;
   if (need > h->d_q8_cap) {
-    if (capturing) {      // (an allocation would end the capture)
-      h->cuda_err = "the workspace cannot grow while the stream is captured: make a call of this size before";
-      return STQ_E_WORKSPACE;
-    }
-    if (h->q8_in_graph) {
+    if (h->d_q8 && (h->q8_in_graph || capturing)) {
       auto* kept = new (std::nothrow) stq::KeptBuffer{h->d_q8, h->q8_kept};
       if (!kept) return STQ_E_WORKSPACE;
       h->q8_kept = kept;
@@ -84,6 +87,7 @@ int workspace(stq_handle* h, size_t count, cudaStream_t stream, T** out) {
       h->d_q8_cap = 0;
       h->q8_in_graph = false;
     }
+    AllocInCapture relaxed;
     STQ_TRY(grow(h, h->d_q8, h->d_q8_cap, need));
   }
   h->q8_in_graph |= capturing;

@@ -82,29 +82,29 @@ def test_a_captured_graph_outlives_the_growth_of_the_workspace():
     h.close(), own.close()
 
 
-def test_the_workspace_does_not_grow_during_a_capture():
-    h = stq.Handle()
-    call, _ = backward(h, 300, 261, 128, 1)
-    x = torch.ones(64, device="cuda")
+@pytest.mark.parametrize("mode", ["global", "thread_local", "relaxed"])
+def test_the_workspace_grows_during_a_capture(mode):
+    h, own = stq.Handle(), stq.Handle()
+    first, _ = backward(h, 130, 261, 128, 4)
+    first()                                                    # (a buffer that the capture replaces)
+    call, dy = backward(h, 300, 261, 128, 1)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        y = x + 1
-        with pytest.raises(stq.StqError, match="captured") as e:
-            call()
-        y = y + 1
-    assert e.value.code == -8
-    graph.replay()                                             # the capture went on
-    assert (y == 3.0).all()
-    want = call()
-    with torch.cuda.graph(graph2 := torch.cuda.CUDAGraph()):
+    with torch.cuda.graph(graph, capture_error_mode=mode):
         got = call()
-    graph2.replay()
-    torch.cuda.synchronize()
-    for a, b in zip(got, want):
-        assert torch.equal(a, b)
-    del graph2
-    h.close()
+    large, _ = backward(h, 2000, 1285, 640, 2)
+    large()
+    fresh, dy2 = backward(own, 300, 261, 128, 1)
+    for seed in (5, 6):
+        dy.copy_(torch.randn(dy.shape, device="cuda", generator=gen(seed)).to(BF))
+        dy2.copy_(dy)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, fresh()):
+            assert torch.equal(a, b)
+    h.device_status(), own.device_status()
+    del graph
+    h.close(), own.close()
 
 
 # ---- norm ------------------------------------------------------------------------------------------------------------

@@ -805,7 +805,7 @@ __global__ void __launch_bounds__(256) q8_act_bwd_kernel(const ActBwdArgs a, uin
       d0[i] = mul2(mul2(t, u), fma2(g, fma2(sg, both(-1.f), both(1.f)), both(1.f)));
     } else {
       // y sg (1 + x (1 - sg) kGeluA (1 + 3 kGeluB x^2)).  From |x| = 14 on the derivative is 0 or 1 in fp32, so x is held
-      // there: its cube would overflow and meet the 0.
+      // at 20: its cube would overflow and meet the 0.
       const float2 x = held(g, 20.f), x2 = mul2(x, x), v = mul2(both(kGeluA), mul2(x, fma2(both(kGeluB), x2, both(1.f))));
       const float2 sg = sigmoid2(v);
       const float2 in = mul2(both(kGeluA), fma2(both(3.f * kGeluB), x2, both(1.f)));
@@ -953,7 +953,7 @@ struct BwdShape {
 // columns:       16-byte accesses          pairs                 single elements
 //   bf16         33.5 (84), 42.6 (117)     - , 47.4 (75)         113 (82), 144 (114)
 //   fp32         86.7 (111), 113 (159)     89.0 (74), 108 (108)  78.0 (79), 99.3 (112)
-// (all but the first two spill, 200 to 324 bytes).
+// (bf16 in 16-byte accesses and pairs spill at most 16 bytes, the others 200 to 324).
 constexpr bool two_units(size_t elem, int vec) { return elem == 2 ? vec != 1 : vec != 2; }
 bool bwd_wide(uint32_t cols, int dtype, int vec) { return cols > kBwdWarps * (two_units(elem_bytes(dtype), vec) ? 2 : 1) * kUnit; }
 

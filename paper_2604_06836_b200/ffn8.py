@@ -96,11 +96,12 @@ class _Block(torch.autograd.Function):
 class FeedForward8(torch.nn.Module):
     """norm -> product -> activation -> product, with 8-bit products and 8-bit saved state.
 
-    forward(x, residual=None) takes bf16 [..., width] in any layout and returns (y, h) with h = x + residual: the next block of a stack
-    gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on every
-    forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving.  A frozen block
-    quantizes them again where they have changed since (loading, an optimizer step, any change that torch counts, a move to
-    another device), and for every pass that differentiates them.
+    forward(x, residual=None) takes bf16 [..., width] in any layout and returns (y, h) with h = x + residual: the next block
+    of a stack gets them as its x and residual.  kind: "silu_gated" or "gelu".  In training the weights are quantized on
+    every forward pass (an optimizer step has changed them); ``freeze()`` quantizes them once, for serving under
+    ``torch.no_grad()``.  A frozen block quantizes them again where they have changed since (loading, an optimizer step, any
+    change that torch counts, a move to another device), and for every pass that differentiates them.  There are no second
+    derivatives: differentiating the gradients raises.
 
     Passes may run on any streams: backward passes, which share a workspace, are put in order one after the other.  A
     captured graph that holds a backward pass must not be replayed while another backward pass of the block runs."""

@@ -9,10 +9,12 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstq.so")
 SOURCES = ["stq_step_fast.cu", "stq_step_variants.cu", "stq_step_split.cu", "stq_kernels.cu", "stq_static_stats.cu",
-           "stq_q8_rows.cu", "stq_q8_linear.cu", "stq_q8_grad.cu", "stq_q8_tma.cpp", "stq_q8_api.cu", "stq_api.cu", "stq_policy.cpp"]
+           "stq_q8_rows.cu", "stq_q8_linear.cu", "stq_q8_grad.cu", "stq_q8_tma.cpp", "stq_q8_api.cu",
+           "stq_vocab_scores.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_api.cu", "stq_policy.cpp"]
 HEADERS = [os.path.join(CSRC, "stq_internal.h"), os.path.join(CSRC, "stq_handle.h"), os.path.join(CSRC, "stq_q8.h"),
            os.path.join(CSRC, "stq_q8_mma.cuh"), os.path.join(CSRC, "stq_q8_tma.h"), os.path.join(CSRC, "stq_q8_ring.h"),
-           os.path.join(CSRC, "stq_step_fast.cuh"), os.path.join(os.path.dirname(HERE), "include", "stq.h")]
+           os.path.join(CSRC, "stq_checks.h"), os.path.join(CSRC, "stq_rowcopy.cuh"), os.path.join(CSRC, "stq_vocab.h"),
+           os.path.join(CSRC, "stq_vocab_ranges.h"), os.path.join(CSRC, "stq_step_fast.cuh"), os.path.join(os.path.dirname(HERE), "include", "stq.h")]
 
 # -fmad=false: the code-deciding arithmetic must not be contracted; fused operations are written
 # explicitly where they are wanted.

@@ -29,6 +29,7 @@
 #include "stq_q8_mma.cuh"
 #include "stq_q8_ring.h"
 #include "stq_q8_tma.h"
+#include "stq_rowcopy.cuh"
 
 namespace stq {
 namespace {
@@ -459,40 +460,14 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_
   }
 }
 
-// A gradient whose rows are not aligned to 16 bytes, copied to rows that are.  A warp moves 256 columns: its lanes load the
-// 16-byte pieces that hold them (the first and last may reach outside the row, never outside the piece of an element of
-// it), take the next piece from the next lane and shift the two into place.
+// Rows that are not aligned to 16 bytes, copied to rows that are: 256 columns to a warp.
 __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, size_t ldi, uint64_t rows, uint32_t cols,
                                                        __nv_bfloat16* out, size_t ldo) {
   asm volatile("griddepcontrol.launch_dependents;");
   const uint32_t per_row = (cols + 255) / 256;
   const uint64_t id = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5), row = id / per_row;
   if (row >= rows) return;
-  const int lane = threadIdx.x & 31;
-  const uint32_t base = (uint32_t)(id - row * per_row) * 256;
-  const uintptr_t from = reinterpret_cast<uintptr_t>(in + row * ldi + base), end = reinterpret_cast<uintptr_t>(in + row * ldi + cols);
-  const uint32_t off = from & 15;
-  const uintptr_t piece = from - off + 16 * lane;
-  uint4 v = make_uint4(0, 0, 0, 0), next = v;
-  if (piece < end) v = *reinterpret_cast<const uint4*>(piece);
-  if (lane == 31 && off && piece + 16 < end) next = *reinterpret_cast<const uint4*>(piece + 16);
-  uint32_t w[8] = {v.x, v.y, v.z, v.w, __shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1),
-                   __shfl_down_sync(0xffffffffu, v.z, 1), __shfl_down_sync(0xffffffffu, v.w, 1)};
-  if (lane == 31) { w[4] = next.x; w[5] = next.y; w[6] = next.z; w[7] = next.w; }
-  if (off & 8) {
-#pragma unroll
-    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
-  }
-  if (off & 4) {
-#pragma unroll
-    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
-  }
-  if (off & 2) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-  }
-  const uint32_t c = base + lane * 8;
-  if (c < cols) *reinterpret_cast<uint4*>(out + row * ldo + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  copy_row_part(in + row * ldi, cols, (uint32_t)(id - row * per_row) * 256, out + row * ldo, threadIdx.x & 31);
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -619,9 +594,7 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   *launches = 1;
   if (w.pitch) {
     __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(base);
-    const uint64_t items = g.t * ((g.n + 255) / 256);      // (a warp each)
-    q8_pitch_kernel<<<(unsigned)((items + 7) / 8), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(g.dy), g.lddy, g.t, g.n, to, w.lddy);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = launch_pitch(g.dy, g.lddy, g.t, g.n, to, w.lddy, stream);
     if (e != cudaSuccess) return e;
     at.dy = to;
     ++*launches;
@@ -635,21 +608,30 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
     at.operand = to;
     ++*launches;
   }
-  cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, at, err, sms, stream) : by_shape<1, DW, __nv_bfloat16>(g, w, at, err, sms, stream);
+  const cudaError_t e = f32 ? by_shape<3, DW, float>(g, w, at, err, sms, stream) : by_shape<1, DW, __nv_bfloat16>(g, w, at, err, sms, stream);
   if (e != cudaSuccess || w.plan.splits == 1) return e;
   const uint32_t count = w.plan.tiles - w.plan.full, tile_m = w.plan.cg * 128, tiles_m = (uint32_t)((m + tile_m - 1) / tile_m);
-  const dim3 grid((unsigned)(((uint64_t)count * tile_m * (w.plan.bn / 4) + 255) / 256));
-  e = f32 ? launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m, (uint32_t)w.plan.bn,
-                        w.plan.full, count, tiles_m, m, g.k, static_cast<float*>(g.out), g.ldo, rows_aligned(g.out, g.ldo * 4))
-          : launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, (const float*)at.part, w.plan.splits, tile_m,
-                        (uint32_t)w.plan.bn, w.plan.full, count, tiles_m, m, g.k, static_cast<__nv_bfloat16*>(g.out), g.ldo,
-                        rows_aligned(g.out, g.ldo * 2));
   ++*launches;
-  return e;
+  return launch_join(at.part, w.plan.splits, tile_m, w.plan.bn, w.plan.full, count, tiles_m, m, g.k, g.out, g.ldo, f32, stream);
 }
 
 }  // namespace
 
+cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first, uint32_t count, uint32_t tiles_m,
+                        uint64_t m, uint32_t n, void* out, size_t ldo, bool f32, cudaStream_t stream) {
+  const dim3 grid((unsigned)(((uint64_t)count * tile_m * (tile_n / 4) + 255) / 256));
+  if (f32)
+    return launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, tiles_m, m, n,
+                       static_cast<float*>(out), ldo, rows_aligned(out, ldo * 4));
+  return launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, tiles_m, m, n,
+                     static_cast<__nv_bfloat16*>(out), ldo, rows_aligned(out, ldo * 2));
+}
+cudaError_t launch_pitch(const void* in, size_t ldi, uint64_t rows, uint32_t cols, void* out, size_t ldo, cudaStream_t stream) {
+  const uint64_t items = rows * ((cols + 255) / 256);      // (a warp each)
+  q8_pitch_kernel<<<(unsigned)((items + 7) / 8), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(in), ldi, rows, cols,
+                                                                   static_cast<__nv_bfloat16*>(out), ldo);
+  return cudaGetLastError();
+}
 size_t q8_grad_workspace(const GemmArgs& g, bool dw, int sms) {
   const Work w = work_of(g, dw, sms);
   return w.pitch_bytes + w.part_bytes + w.conv_bytes;

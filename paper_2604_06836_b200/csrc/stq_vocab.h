@@ -1,0 +1,113 @@
+// Internal interface between the host layer of the vocabulary cross entropy (stq_vocab_api.cu) and its kernels.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace stq {
+
+// Rows are compact: only tokens that count have one, in the tokens' order (`count` of them, known on the device alone).
+// Without compaction every token has a row, and those that do not count get zeros.
+struct VocabRows {
+  const void* x;              // bf16 hidden states, a row each
+  size_t ldx;
+  uint32_t rows;              // rows of x that exist
+  uint32_t most;              // rows at most, a multiple of 256 (of 128 for a single tile)
+  const uint32_t* count;      // on the device, or null: `rows`
+  const uint32_t* token;      // row -> token, or null: the same
+  const int32_t* row;         // token -> row or -1, or null
+};
+
+// What the products of hidden states and the matrix need.
+struct VocabArgs {
+  VocabRows r;
+  const void* w;              // bf16 [v][d]
+  size_t ldw;
+  const float* bias;          // [v], or null
+  uint32_t v, d;
+  const int64_t* target;      // of a token
+  int64_t ignore;
+  uint32_t t;
+  int device;
+};
+
+// ---- rows (stq_vocab_scores.cu) ----------------------------------------------------------------------------------
+// Tokens that count -> compact rows; rows up to `most` behind them are zero.
+struct GatherArgs {
+  const void* x;
+  size_t ldx;
+  uint32_t t, d, most;
+  const int64_t* target;
+  int64_t ignore;
+  void* out;
+  size_t ldo;
+  uint32_t* count;
+  uint32_t* token;
+  int32_t* row;
+};
+cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
+
+// Tiles of the products: `cg` CTAs share 128 * cg rows and `bn` columns.
+struct VocabShape {
+  int cg, bn;
+};
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms);
+
+// Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
+uint32_t vocab_parts(const VocabArgs& a, VocabShape s);
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, float2* part, int sms, int* err, cudaStream_t stream);
+// loss and lse of all tokens from the parts.  x and ldx: the tokens' hidden states as they were given.
+cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
+                                float* lse, cudaStream_t stream);
+
+// Gradients of the logits of entries [v0, v1), p[plane][row][v - v0]: `planes` bf16 numbers (1 or 3) whose sum they are,
+// plane i at row i * most; pitch ldp, a multiple of 64.  dbias: sums over 32 rows each, [most / 32][ldp], or null.
+struct VocabGradOut {
+  void* p;
+  size_t ldp;
+  int planes;
+  float* dbias;
+  const float* lse;
+  const float* dloss;
+};
+cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape s, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,
+                                 cudaStream_t stream);
+
+// ---- gradients (stq_vocab_grad.cu) ---------------------------------------------------------------------------------
+// dw[v0 + i][:] = sum over rows of p[row][i] x[row][:].  part: vocab_dw_partial() floats.
+struct VocabDw {
+  VocabRows r;
+  const void* p;
+  size_t ldp;
+  uint32_t cols, d;           // v1 - v0
+  void* dw;                   // row v0
+  size_t lddw;
+  bool f32;
+  int device;
+};
+size_t vocab_dw_partial(const VocabDw& a, int sms);
+cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches);
+
+// planes[c][row][:] (+)= share c of the sum over [v0, v0 + cols) of p[row][i] w[v0 + i][:].  The sums of all tiles, one after
+// the other, are cut into equal ranges, one for each pair of CTAs; what different pairs have of a tile goes to different planes.
+// All pieces but the last are equally long (`first` columns): the last adds to what they left.
+struct VocabDx {
+  VocabRows r;
+  const void* p;
+  size_t ldp;
+  const void* w;              // row v0
+  size_t ldw;
+  uint32_t cols, d, first;
+  bool begin;                 // the first piece
+  float* planes;
+  size_t ldd;                 // columns of a plane, a multiple of 32
+  uint32_t plane_rows;        // rows of all planes together
+  int device;
+};
+size_t vocab_dx_rows(uint32_t most, size_t ldd);      // rows of planes that suffice
+cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream);
+// dx of all tokens (zero for those that do not count) from the planes.
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream);
+cudaError_t launch_vocab_dbias(const float* part, size_t ldp, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream);
+
+}  // namespace stq

@@ -1,0 +1,249 @@
+// C-ABI host layer of the vocabulary cross entropy: argument checks, workspace, launches.
+#include "stq_checks.h"
+#include "stq_q8.h"
+#include "stq_q8_tma.h"
+#include "stq_vocab.h"
+
+using namespace stq;
+
+namespace {
+
+constexpr uint32_t kTokensAtOnce = 32768;       // of a loss: bounds its workspace (tokens do not depend on one another)
+constexpr size_t kPieceBytes = 256u << 20;      // of gradients of logits that exist at a time
+
+size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
+
+// Places in the workspace, one after the other; the first pass only adds up.
+struct Arena {
+  uint8_t* base = nullptr;
+  size_t at = 0;
+  template <class T>
+  T* take(size_t count) {
+    T* p = base ? reinterpret_cast<T*>(base + at) : nullptr;
+    at += up(count * sizeof(T), 256);
+    return p;
+  }
+};
+
+// Rows of x that the products can read: those of tokens that count, aligned, or x as it is.
+struct Rows {
+  bool gather, pitch_w;
+  uint16_t *x, *w;
+  size_t ldx, ldw;
+  uint32_t *count, *token;
+  int32_t* row;
+
+  Rows(const VocabArgs& a, const void* x_, size_t ldx_) {
+    // (up to one tile of tokens there is nothing to gain from leaving some out)
+    gather = a.t > 128 || !rows_aligned(x_, a.t > 1 ? ldx_ * 2 : 0);
+    pitch_w = !rows_aligned(a.w, a.v > 1 ? a.ldw * 2 : 0);
+    ldx = up(a.d, 8);
+    ldw = up(a.d, 8);
+  }
+  void place(Arena& m, const VocabArgs& a, uint32_t most) {
+    x = gather ? m.take<uint16_t>(most * ldx) : nullptr;
+    count = gather ? m.take<uint32_t>(1) : nullptr;
+    token = gather ? m.take<uint32_t>(most) : nullptr;
+    row = gather ? m.take<int32_t>(a.t) : nullptr;
+    w = pitch_w ? m.take<uint16_t>((size_t)a.v * ldw) : nullptr;
+  }
+};
+
+uint32_t most_rows(uint32_t t) { return t <= 128 ? 128 : (uint32_t)up(t, 256); }
+
+// Sets a.r (and the aligned copy of w) up on the stream.
+cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, bool with_w, cudaStream_t s, int* launches) {
+  const uint32_t most = most_rows(a.t);
+  a.r = {x, a.t > 1 ? ldx : up(a.d, 8), a.t, most, nullptr, nullptr, nullptr};
+  if (r.gather) {
+    const GatherArgs g = {x, ldx, a.t, a.d, most, a.target, a.ignore, r.x, r.ldx, r.count, r.token, r.row};
+    const cudaError_t e = launch_vocab_gather(g, s);
+    if (e != cudaSuccess) return e;
+    a.r = {r.x, r.ldx, most, most, r.count, r.token, r.row};
+    ++*launches;
+  }
+  if (r.pitch_w && with_w) {
+    const cudaError_t e = launch_pitch(a.w, a.ldw, a.v, a.d, r.w, r.ldw, s);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  if (r.pitch_w) {
+    a.w = r.w;
+    a.ldw = r.ldw;
+  } else if (a.v == 1) {
+    a.ldw = up(a.d, 8);
+  }
+  return cudaSuccess;
+}
+
+int check(const stq_handle* h, const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias, const int64_t* target, uint64_t t,
+          uint32_t v, uint32_t d) {
+  STQ_TRY(check_handle(h));
+  STQ_TRY(check_size(t, d));
+  STQ_TRY(check_size(t, v));
+  if (t > STQ_VOCAB_MAX_TOKENS || d > STQ_VOCAB_MAX_WIDTH) return STQ_E_TOO_LARGE;
+  if (t == 0) return STQ_OK;
+  STQ_TRY(check_mat(x, ldx, d, 2));
+  STQ_TRY(check_mat(w, ldw, d, 2));
+  if (!target) return STQ_E_NULL;
+  return aligned(target, 8) && aligned(bias, 4) ? STQ_OK : STQ_E_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias, const int64_t* target,
+                   int64_t ignore_index, uint64_t t, uint32_t v, uint32_t d, float* loss, float* lse, void* stream) {
+  STQ_TRY(check(h, x, ldx, w, ldw, bias, target, t, v, d));
+  if (t == 0) return STQ_OK;
+  if (!loss || !lse) return STQ_E_NULL;
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return STQ_E_ALIGN;
+  const Span out[] = {{loss, t * 4}, {lse, t * 4}};
+  const Span in[] = {mat(x, ldx, t, d, 2), mat(w, ldw, v, d, 2), {bias, v * 4ull}, {target, t * 8}};
+  if (clash(out, in)) return STQ_E_ALIAS;
+  STQ_CUDA(h, cudaSetDevice(h->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+
+  VocabArgs a = {};
+  a.w = w; a.ldw = ldw; a.bias = bias;
+  a.v = v; a.d = d;
+  a.ignore = ignore_index;
+  a.device = h->device;
+  // (the blocks of tokens share one workspace, laid out for the largest)
+  a.t = (uint32_t)(t < kTokensAtOnce ? t : kTokensAtOnce);
+  a.target = target;
+  Rows r(a, x, ldx);
+  const uint32_t most = most_rows(a.t);
+  const VocabShape shape = vocab_shape(a.t, v, d, h->sm_count);
+  const uint32_t parts = vocab_parts(a, shape);
+  Arena m;
+  float2* part = nullptr;
+  for (int pass = 0; pass < 2; ++pass) {
+    m.at = 0;
+    r.place(m, a, most);
+    part = m.take<float2>((size_t)parts * most);
+    if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
+  }
+  for (uint64_t t0 = 0; t0 < t; t0 += kTokensAtOnce) {
+    VocabArgs b = a;
+    b.t = (uint32_t)(t - t0 < kTokensAtOnce ? t - t0 : kTokensAtOnce);
+    b.target = target + t0;
+    const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
+    int launches = 2;
+    STQ_CUDA(h, prepare_rows(b, r, xb, ldx, t0 == 0, s, &launches));
+    STQ_CUDA(h, launch_vocab_parts(b, shape, part, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, launch_vocab_finish(b, xb, ldx, part, parts, loss + t0, lse + t0, s));
+    h->launches += launches;
+  }
+  return STQ_OK;
+}
+
+int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias,
+                            const int64_t* target, int64_t ignore_index, const float* lse, uint64_t t, uint32_t v, uint32_t d, void* dx,
+                            uint64_t lddx, void* dw, uint64_t lddw, int dw_dtype, float* dbias, void* stream) {
+  STQ_TRY(check(h, x, ldx, w, ldw, bias, target, t, v, d));
+  STQ_TRY(check_dtype(dw_dtype));
+  const size_t e = elem(dw_dtype);
+  if (dw) STQ_TRY(check_mat(dw, lddw, d, e));
+  if (!aligned(dbias, 4)) return STQ_E_ALIGN;
+  STQ_CUDA(h, cudaSetDevice(h->device));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (t == 0) {
+    if (dw) STQ_TRY(zero(h, dw, lddw, v, d, e, s));
+    if (dbias) STQ_TRY(zero(h, dbias, v, 1, v, 4, s));
+    return STQ_OK;
+  }
+  if (dx) STQ_TRY(check_mat(dx, lddx, d, 2));
+  if (!dloss || !lse) return STQ_E_NULL;
+  if (!aligned(dloss, 4) || !aligned(lse, 4)) return STQ_E_ALIGN;
+  const Span out[] = {mat(dx, lddx, t, d, 2), mat(dw, lddw, v, d, e), {dbias, v * 4ull}};
+  const Span in[] = {mat(x, ldx, t, d, 2), mat(w, ldw, v, d, 2), {bias, v * 4ull}, {target, t * 8}, {dloss, t * 4}, {lse, t * 4}};
+  if (clash(out, in)) return STQ_E_ALIAS;
+  if (!dx && !dw && !dbias) return STQ_OK;
+
+  VocabArgs a = {};
+  a.w = w; a.ldw = ldw; a.bias = bias;
+  a.v = v; a.d = d;
+  a.t = (uint32_t)t;
+  a.target = target;
+  a.ignore = ignore_index;
+  a.device = h->device;
+  Rows r(a, x, ldx);
+  const uint32_t most = most_rows(a.t);
+  const int planes = dw && dw_dtype == STQ_GRAD_F32 ? 3 : 1;
+  // pieces of the vocabulary: equal but for the last
+  const size_t fit = kPieceBytes / ((size_t)most * 2 * planes) / 256 * 256, tiles = up(v, 256) / 256, widest = (fit < 256 ? 256 : fit) / 256;
+  const size_t pieces = (tiles + widest - 1) / widest;
+  const uint32_t cols = (uint32_t)((tiles + pieces - 1) / pieces * 256 < v ? (tiles + pieces - 1) / pieces * 256 : v);
+  VocabGradOut o = {nullptr, up(cols, 64), planes, nullptr, lse, dloss};
+  VocabDw gw = {};
+  gw.ldp = o.ldp;
+  gw.cols = cols; gw.d = d;
+  gw.lddw = lddw;
+  gw.f32 = dw_dtype == STQ_GRAD_F32;
+  gw.device = h->device;
+  gw.r.most = most;
+  VocabDx gx = {};
+  gx.ldp = o.ldp;
+  gx.d = d; gx.first = cols;
+  gx.ldd = up(d, 32);
+  gx.plane_rows = (uint32_t)vocab_dx_rows(most, gx.ldd);
+  gx.device = h->device;
+  // (a last piece may share its tiles in another way than the others)
+  const uint32_t last = (uint32_t)(v - (v - 1) / cols * cols);
+  size_t partial = dw ? vocab_dw_partial(gw, h->sm_count) : 0;
+  if (dw && last != cols) {
+    VocabDw l = gw;
+    l.cols = last;
+    const size_t p = vocab_dw_partial(l, h->sm_count);
+    if (p > partial) partial = p;
+  }
+  Arena m;
+  float* part = nullptr;
+  for (int pass = 0; pass < 2; ++pass) {
+    m.at = 0;
+    r.place(m, a, most);
+    o.p = m.take<uint16_t>((size_t)most * planes * o.ldp);
+    o.dbias = dbias ? m.take<float>(most / 32 * o.ldp) : nullptr;
+    part = partial ? m.take<float>(partial) : nullptr;
+    gx.planes = dx ? m.take<float>(gx.plane_rows * gx.ldd) : nullptr;
+    if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
+  }
+  int launches = 0;
+  STQ_CUDA(h, prepare_rows(a, r, x, ldx, true, s, &launches));
+  gw.r = gx.r = a.r;
+  gw.p = gx.p = o.p;
+  gx.ldw = a.ldw;
+  for (uint32_t v0 = 0; v0 < v; v0 += cols) {
+    const uint32_t n = v - v0 < cols ? v - v0 : cols;
+    STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
+    ++launches;
+    if (dbias) {
+      STQ_CUDA(h, launch_vocab_dbias(o.dbias, o.ldp, a.r, n, dbias + v0, s));
+      ++launches;
+    }
+    if (dw) {
+      int more = 0;
+      gw.cols = n;
+      gw.dw = static_cast<uint8_t*>(dw) + (size_t)v0 * lddw * e;
+      STQ_CUDA(h, launch_vocab_dw(gw, part, h->sm_count, h->d_err, s, &more));
+      launches += more;
+    }
+    if (dx) {
+      gx.cols = n;
+      gx.begin = v0 == 0;
+      gx.w = static_cast<const uint16_t*>(a.w) + (size_t)v0 * a.ldw;
+      STQ_CUDA(h, launch_vocab_dx(gx, h->sm_count, h->d_err, s));
+      ++launches;
+    }
+  }
+  if (dx) {
+    STQ_CUDA(h, launch_vocab_dx_finish(gx, last, a.t, dx, lddx, h->sm_count, s));
+    ++launches;
+  }
+  h->launches += launches;
+  return STQ_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,531 @@
+// Gradients of the vocabulary cross entropy from those of the logits, p (stq_vocab_scores.cu):
+//   dw[i][:] = sum over rows r of p[r][i] x[r][:]      (rows of the result: entries of the vocabulary)
+//   dx[r][:] = sum over entries i of p[r][i] w[i][:]   (rows of the result: tokens)
+// p lies row by row, so dw reads it MN-major and dx K-major; x and w are read MN-major, as they lie.  Nothing is transposed.
+//
+// dw: its sum is over the tokens, complete within a piece of the vocabulary.  For a bf16 result p is bf16 too (2^-8 a term,
+// random in sign, as large as the rounding of the result).  For an fp32 result p comes in three bf16 parts that are together
+// exactly the fp32 gradient, and the sum leaves the matrix unit, which cuts its sums off instead of rounding them, every 128
+// terms and is added, rounded, to a running sum in tensor memory.
+//
+// dx: its sum is over the vocabulary, so every piece adds to it, in fp32 in memory (copies that add: nothing is read back).
+// The tiles are few (8192 x 1600: 224 for 74 pairs of CTAs), so the sums of all tiles, one after the other, are cut into
+// equal ranges.  What different pairs have of a tile goes to different planes, which are added in a fixed order at the end.
+#include <cuda_bf16.h>
+
+#include "../../include/stq.h"
+#include "stq_q8.h"
+#include "stq_q8_mma.cuh"
+#include "stq_q8_tma.h"
+#include "stq_vocab.h"
+#include "stq_vocab_ranges.h"
+
+namespace stq {
+namespace {
+
+constexpr int kDepth = 64;
+constexpr int kStepK = 16;
+constexpr int kMaxTilesN = 512;        // tiles along a row of dx
+
+struct GradArgs {
+  const uint32_t* count;
+  uint32_t rows, most;
+  uint32_t n, bn;                      // columns of the result, and of a tile
+  uint32_t units;
+  // dw
+  void* out;
+  size_t ldo;
+  uint32_t m;                          // rows of the result
+  uint32_t tiles_m, tiles, full, splits;   // tiles from `full` on are shared by `splits` work items each
+  float* part;
+  int aligned;
+  // dx
+  uint32_t ksteps, first;              // stages of this piece and of the first one
+  uint32_t plane_rows;
+  int begin;
+  int* err;
+};
+
+template <int CG, int BN, int PARTS>
+struct GradShape {
+  static constexpr int kThreads = 32 * 6;
+  static constexpr int kNB = BN / CG < 64 ? 64 : BN / CG;         // columns that are copied: whole 128-byte rows
+  static constexpr int kA = 128 * kDepth * 2, kB = kDepth * kNB * 2;
+  static constexpr int kStage = kA * PARTS + kB;
+  static constexpr int kFit = (204 * 1024) / kStage;
+  static constexpr int kStages = kFit < 8 ? kFit : 8;
+  static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
+  static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
+  static constexpr int kSmem = kStages * kStage + 4 * kStageBytes + 1024;
+};
+
+// A warp's block of 32 rows x 32 columns of fp32, added to memory by a tensor copy.
+__device__ __forceinline__ void add_block(const CUtensorMap* map, int x, int y, const float (&v)[32], int lane, uint32_t stage) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(__float_as_uint(v[4 * i])),
+                 "r"(__float_as_uint(v[4 * i + 1])), "r"(__float_as_uint(v[4 * i + 2])), "r"(__float_as_uint(v[4 * i + 3]))
+                 : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(stage)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+
+// One work item: tile (its row and column), stages [k0, k1) of its sum, and where the result goes.
+struct Item {
+  uint32_t tile, row, col, k0, k1;
+  int share;                           // dx: the plane; dw: number of the partial result, -1 for the whole sum
+};
+
+// DW: rows of the result are entries of the vocabulary.  O: type of dw (dx: float).
+template <int CG, int BN, int PARTS, bool DW, class O>
+__global__ void __launch_bounds__((GradShape<CG, BN, PARTS>::kThreads), 1)
+vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
+                  const GradArgs a) {
+  using S = GradShape<CG, BN, PARTS>;
+  constexpr int kStages = S::kStages;
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[2 * kStages + 4];
+  __shared__ uint32_t tmem_slot;
+  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u, outs = ring + kStages * S::kStage;
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, freed = done + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  const bool leader = rank == 0;
+  const uint32_t unit = blockIdx.x / CG;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      bar_init(full + 8 * i, 1);
+      bar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(done + 8 * i, 1);
+      bar_init(freed + 8 * i, 4 * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc<CG>(smem_addr(&tmem_slot), S::kCols);
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  mma_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const uint32_t count = a.count ? *a.count : a.rows;
+
+  const uint32_t tiles_n = (a.n + a.bn - 1) / a.bn;
+  const uint32_t ksteps = DW ? (count + kDepth - 1) / kDepth : a.ksteps;
+  const Ranges ranges(DW ? 0 : count, 128 * CG, tiles_n, a.ksteps, a.units, a.plane_rows);
+  const Ranges before(DW ? 0 : count, 128 * CG, tiles_n, a.first, a.units, a.plane_rows);
+  // calls f(item) for each of this unit's items, in order, until it returns false
+  auto items = [&](auto&& f) {
+    if constexpr (DW) {
+      const uint32_t work = a.full + (a.tiles - a.full) * a.splits;
+      for (uint32_t w = unit; w < work; w += a.units) {
+        Item it = {w, 0, 0, 0, ksteps, -1};
+        if (w >= a.full) {
+          const uint32_t i = w - a.full, sp = i % a.splits;
+          it.tile = a.full + i / a.splits;
+          it.k0 = (uint32_t)((uint64_t)ksteps * sp / a.splits);
+          it.k1 = (uint32_t)((uint64_t)ksteps * (sp + 1) / a.splits);
+          it.share = (int)i;
+        }
+        it.row = it.tile % a.tiles_m * 128 * CG;
+        it.col = it.tile / a.tiles_m * a.bn;
+        if (!f(it)) return;
+      }
+    } else {
+      if (unit >= ranges.U) return;
+      const uint64_t end = ranges.begin(unit + 1);
+      for (uint64_t s = ranges.begin(unit); s < end;) {
+        const uint32_t tile = (uint32_t)(s / ranges.ksteps);
+        const uint64_t t0 = (uint64_t)tile * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
+        const Item it = {tile, tile % ranges.tiles_m * 128 * CG, tile / ranges.tiles_m * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
+                         (int)(unit - ranges.unit_of(t0))};
+        if (!f(it)) return;
+        s = stop;
+      }
+    }
+  };
+
+  bool ok = true;
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t it = 0;
+      const uint32_t full0 = CG == 2 ? peer_addr(full, 0) : full;
+      items([&](const Item& w) {
+        const int row = (int)(w.row + 128 * rank), col = (int)(w.col + a.bn / CG * rank);
+        for (uint32_t k = w.k0; k < w.k1; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          if (!(ok = bar_wait(empty + 8 * s, ph ^ 1))) return false;
+          const uint32_t at = ring + s * S::kStage;
+          const int c = (int)(k * kDepth);
+          if (leader) bar_expect(full + 8 * s, CG * S::kStage);
+#pragma unroll
+          for (int i = 0; i < S::kNB / 64; ++i) tensor_load<CG>(at + PARTS * S::kA + i * (kDepth * 128), &map_b, col + 64 * i, c, full0 + 8 * s);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) {
+            if constexpr (DW) {
+              tensor_load<CG>(at + p * S::kA, &map_p, row, c + p * (int)a.most, full0 + 8 * s);
+              tensor_load<CG>(at + p * S::kA + S::kA / 2, &map_p, row + 64, c + p * (int)a.most, full0 + 8 * s);
+            } else {
+              tensor_load<CG>(at, &map_p, c, row, full0 + 8 * s);
+            }
+          }
+        }
+        return true;
+      });
+      if (!ok && leader)      // leave no copy in flight
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) bar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+    }
+  } else if (warp == 1) {
+    if (leader && elect_one()) {
+      const uint32_t id = idesc(kIdescBf16, 128 * CG, (int)a.bn, DW, true);
+      uint32_t it = 0, n = 0;
+      items([&](const Item& w) {
+        for (uint32_t k = w.k0; k < w.k1; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = (k - w.k0) % S::kChunk;
+          if (place == 0) {
+            if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) return false;
+            mma_fence_after();
+          }
+          if (!(ok = bar_wait<CG == 2>(full + 8 * s, ph))) return false;
+          mma_fence_after();
+          const uint32_t at = ring + s * S::kStage;
+          const uint64_t da = DW ? operand_desc(at, S::kA / 2, 1024) : operand_desc(at, 16, 1024);
+          const uint64_t db = operand_desc(at + PARTS * S::kA, kDepth * 128, 1024);
+          constexpr uint32_t kStepA = DW ? (kStepK * 128) >> 4 : (kStepK * 2) >> 4, kStepB = (kStepK * 128) >> 4;
+#pragma unroll
+          for (int p = PARTS - 1; p >= 0; --p)                  // the smallest part first
+#pragma unroll
+            for (int j = 0; j < kDepth / kStepK; ++j)
+              mma<CG, false>(tmem + acc * BN, da + p * (S::kA >> 4) + j * kStepA, db + j * kStepB, id, place != 0 || p < PARTS - 1 || j != 0);
+          mma_commit<CG>(empty + 8 * s);
+          if (place == S::kChunk - 1 || k + 1 == w.k1) {
+            mma_commit<CG>(done + 8 * acc);
+            ++n;
+          }
+        }
+        return true;
+      });
+    }
+  } else {
+    const int quad = warp & 3;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + quad * kStageBytes;
+    const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
+    uint32_t n = 0;
+    constexpr int kC = 128 / sizeof(O);
+    items([&](const Item& w) {
+      const uint32_t row = w.row + 128 * rank + quad * 32, running = tmem + lanes + 2 * BN;
+      const uint32_t end = min(a.bn, a.n - w.col);
+      const bool add = !DW && !a.begin && (uint32_t)w.share < before.shares(w.tile);
+      // Blocks of kC columns; the last one of a tile begins early where the tile is not a whole number of them (what is
+      // written twice that way is the same, what is added must not be).
+      auto blocks = [&](auto&& f) {
+#pragma unroll 1
+        for (uint32_t c = 0; c < end; c += kC) {
+          const uint32_t over = c + kC > a.bn ? c + kC - a.bn : 0;
+          f(c - over, over);
+        }
+      };
+      auto emit = [&](uint32_t c, uint32_t over, float(&v)[kC]) {
+        const uint32_t col = w.col + c;
+        if constexpr (DW) {
+          O* out = static_cast<O*>(a.out) + (size_t)row * a.ldo + col;
+          const int rows = row >= a.m ? 0 : (int)min(32u, a.m - row);
+          if (w.share >= 0) {
+            float* part = a.part + ((size_t)w.share * CG * 128 + 128 * rank + quad * 32) * a.bn;
+#pragma unroll
+            for (int i = 0; i < kC; i += 32) store_part(part + c + i, a.bn, v + i, lane);
+          } else if (!a.aligned) {
+            if (col < a.n) store_ragged(out, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col), lane, raw + (stage - smem_addr(raw)));
+          } else if (rows > 0) {
+            store_block<O>(&map_o, (int)col, (int)row, v, lane, stage);
+          }
+        } else {
+          const int y = (int)((uint32_t)w.share * ranges.tiles_m * 128 * CG + row);
+          if (add) {
+#pragma unroll
+            for (int i = 0; i < kC; ++i) v[i] = i < (int)over ? 0.f : v[i];
+            add_block(&map_o, (int)col, y, v, lane, stage);
+          } else {
+            store_block<float>(&map_o, (int)col, y, v, lane, stage);
+          }
+        }
+      };
+      if (w.k0 == w.k1) {                         // (no token counts, or fewer stages than shares)
+        blocks([&](uint32_t c, uint32_t over) {
+          float v[kC];
+#pragma unroll
+          for (int i = 0; i < kC; ++i) v[i] = 0.f;
+          emit(c, over, v);
+        });
+        return true;
+      }
+      for (uint32_t k = w.k0; k < w.k1; k += min((uint32_t)S::kChunk, w.k1 - k), ++n) {
+        const uint32_t acc = n & 1, from = tmem + lanes + acc * BN;
+        const bool first = k == w.k0, last = w.k1 - k <= (uint32_t)S::kChunk;
+        ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
+        if (!(ok = all_of<128>(ok))) return false;       // (the four warps leave together)
+        mma_fence_after();
+        blocks([&](uint32_t c, uint32_t over) {
+          float v[kC];
+          load_block(from + c, v);
+          if constexpr (PARTS == 3) {
+            static_assert(PARTS == 1 || kC == 32, "one block of columns to a load");
+            if (!first) {
+              float old[32];
+              load_block(running + c, old);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], old[i]);
+            }
+            if (!last) {
+              uint32_t r[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
+              tmem_store(running + c, r);
+              return;
+            }
+          }
+          emit(c, over, v);
+        });
+        if (PARTS == 3) tmem_store_wait();
+        mma_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+      }
+      return true;
+    });
+    store_blocks_done(lane);
+  }
+  if (!ok) *a.err = 1;
+  __syncwarp();
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  if (warp == 1) {
+    mma_fence_after();
+    tmem_free<CG>(tmem, S::kCols);
+  }
+}
+
+// dx of eight tokens to a CTA, eight columns to a thread: the planes of a row, added in order.
+__global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, size_t ldd, uint32_t plane_rows, const uint32_t* count_at, uint32_t rows,
+                                                        const int32_t* row_of, uint32_t tile_m, uint32_t bn, uint32_t first, uint32_t last,
+                                                        uint32_t units, uint32_t t, uint32_t d, __nv_bfloat16* dx, size_t lddx, bool aligned) {
+  __shared__ uint32_t shares[2][kMaxTilesN];
+  __shared__ uint32_t tile_row[2];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t count = count_at ? *count_at : rows, tiles_n = (d + bn - 1) / bn, t0 = blockIdx.x * 8;
+  const Ranges r0(count, tile_m, tiles_n, first, units, plane_rows), r1(count, tile_m, tiles_n, last, units, plane_rows);
+  // (eight tokens that follow one another have rows in at most two tiles)
+  auto row = [&](uint32_t i) { return i >= t ? -1 : row_of ? row_of[i] : (int32_t)i; };
+  if (threadIdx.x == 0) {
+    uint32_t lo = 0xffffffffu;
+    for (uint32_t i = t0; i < t0 + 8; ++i)
+      if (row(i) >= 0) lo = min(lo, (uint32_t)row(i) / tile_m);
+    tile_row[0] = lo;
+  }
+  __syncthreads();
+  const uint32_t lo = tile_row[0];
+  if (lo != 0xffffffffu)
+    for (uint32_t i = threadIdx.x; i < 2 * tiles_n; i += 256) {
+      const uint32_t m = lo + i / tiles_n, n = i % tiles_n;
+      if (m < r0.tiles_m) shares[i / tiles_n][n] = max(r0.shares(n * r0.tiles_m + m), r1.shares(n * r0.tiles_m + m));
+    }
+  __syncthreads();
+  const uint32_t per_row = (d + 7) / 8;
+  for (uint32_t i = threadIdx.x; i < 8 * per_row; i += 256) {
+    const uint32_t tok = t0 + i / per_row, c = i % per_row * 8;
+    if (tok >= t) break;
+    const int32_t at = row(tok);
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (at >= 0) {      // (a tile's columns are a multiple of 16: the eight lie in one tile)
+      const uint32_t n = shares[at / tile_m - lo][c / bn];
+      for (uint32_t p = 0; p < n; ++p) {
+        const float* from = planes + ((size_t)p * r0.tiles_m * tile_m + at) * ldd + c;
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(from)), v = __ldcg(reinterpret_cast<const float4*>(from + 4));
+        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
+        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+      }
+    }
+    __nv_bfloat16* to = dx + (size_t)tok * lddx + c;
+    if (aligned && c + 8 <= d) {
+      *reinterpret_cast<uint4*>(to) = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3]), bf16_pair(s[4], s[5]), bf16_pair(s[6], s[7]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < d) to[j] = __float2bfloat16_rn(s[j]);
+    }
+  }
+}
+
+// Column sums of the partial sums of 32 rows each: 32 columns to a CTA, every eighth row to a warp.
+__global__ void __launch_bounds__(256) dbias_kernel(const float* part, size_t ldp, const uint32_t* count_at, uint32_t rows, uint32_t cols, float* out) {
+  __shared__ float sums[8][33];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t groups = ((count_at ? *count_at : rows) + 31) / 32, c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < cols)
+    for (uint32_t g = warp; g < groups; g += 8) s += __ldcg(part + (size_t)g * ldp + c);
+  sums[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || c >= cols) return;
+  for (int i = 1; i < 8; ++i) s += sums[i][lane];
+  out[c] = s;
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
+
+// Columns of a tile: as many equal tiles as the widest allowed makes necessary.
+uint32_t tile_columns(uint32_t n, uint32_t widest, uint32_t unit) {
+  const uint32_t tiles = (n + widest - 1) / widest, bn = up((n + tiles - 1) / tiles, unit);
+  return bn < 64 ? 64 : bn;
+}
+
+struct DwPlan {
+  int cg, bn_max;
+  uint32_t bn, tiles_m, tiles, full, splits;
+};
+// Time of a plan in clock cycles, as for the 8-bit products: a stage is 4096 multiply-adds a cycle and SM, a tile has a beginning
+// and an end, partial results go through memory once more.
+DwPlan dw_plan(const VocabDw& a, int sms) {
+  const uint32_t ksteps = (a.r.most + kDepth - 1) / kDepth;
+  const int shapes[2][2][2] = {{{2, 256}, {1, 128}}, {{2, 128}, {1, 64}}};
+  const int parts = a.f32 ? 3 : 1;
+  DwPlan best = {};
+  double least = 1e300;
+  for (const auto& sh : shapes[a.f32]) {
+    DwPlan p = {sh[0], sh[1], tile_columns(a.d, sh[1], a.f32 ? 32 : 16), (a.cols + 128 * sh[0] - 1) / (128 * sh[0]), 0, 0, 0};
+    p.tiles = p.tiles_m * ((a.d + p.bn - 1) / p.bn);
+    const double stage = 2.0 * p.bn * parts + (p.cg == 1 ? 40.0 * parts : 0.0);
+    const uint64_t units = sms / p.cg, rounds = p.tiles / units, full = rounds * units, rest = p.tiles - full;
+    for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
+      const double part = sp > 1 ? (double)rest * sp * p.cg * 128 * p.bn : 0.0;
+      if (part * 4 > 128e6) break;      // (an eighth of a gigabyte of partial results at most)
+      double c = rounds * (ksteps * stage + 2500.0);
+      if (rest) c += (double)((rest * sp + units - 1) / units) * ((ksteps + sp - 1) / sp * stage + 2500.0);
+      if (sp > 1) c += (part * 8 + (double)rest * p.cg * 128 * p.bn * (a.f32 ? 4 : 2)) / 3000.0 + 4000.0;
+      if (c < least) {
+        least = c;
+        best = p;
+        best.full = (uint32_t)(sp > 1 ? full : p.tiles);
+        best.splits = sp;
+      }
+      if (!rest) break;
+    }
+  }
+  return best;
+}
+
+template <int CG, int BN, int PARTS, bool DW, class O>
+cudaError_t launch(const VocabRows& r, const void* p, size_t ldp, const void* b, uint64_t b_rows, uint32_t b_cols, size_t ldb, void* out,
+                   uint64_t out_rows, size_t ldo, uint64_t items, GradArgs g, int device, int sms, int* err, cudaStream_t stream) {
+  using S = GradShape<CG, BN, PARTS>;
+  g.count = r.count;
+  g.rows = r.rows;
+  g.most = r.most;
+  g.err = err;
+  const uint64_t most = sms / CG;
+  g.units = (uint32_t)(items < most ? items : most);
+  CUtensorMap mp, mb, mo = {};
+  cudaError_t e = make_tensor_map(&mp, p, 2, (uint64_t)r.most * PARTS, ldp, ldp, DW ? 64 : 128, 64, true);
+  if (e == cudaSuccess) e = make_tensor_map(&mb, b, 2, b_rows, b_cols, ldb, 64, 64, true);
+  if (e == cudaSuccess && (!DW || g.aligned)) e = make_tensor_map(&mo, out, sizeof(O), out_rows, DW ? g.n : ldo, ldo, 32, 128 / sizeof(O), true);
+  auto* kernel = vocab_grad_kernel<CG, BN, PARTS, DW, O>;
+  static std::atomic<uint64_t> seen;
+  if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, device, seen);
+  if (e != cudaSuccess) return e;
+  return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, g);
+}
+
+// Tiles of dx.  (A single tile of rows needs no pair.)
+struct DxShape {
+  int cg;
+  uint32_t bn;
+};
+DxShape dx_shape(const VocabDx& a) {
+  const int cg = a.r.most > 128 ? 2 : 1;
+  return {cg, tile_columns(a.d, 128 * cg, 16)};
+}
+
+}  // namespace
+
+size_t vocab_dw_partial(const VocabDw& a, int sms) {
+  const DwPlan p = dw_plan(a, sms);
+  return p.splits > 1 ? (size_t)(p.tiles - p.full) * p.splits * p.cg * 128 * p.bn : 0;
+}
+
+cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches) {
+  const DwPlan p = dw_plan(a, sms);
+  GradArgs g = {};
+  g.n = a.d;
+  g.bn = p.bn;
+  g.out = a.dw;
+  g.ldo = a.lddw;
+  g.m = a.cols;
+  g.tiles_m = p.tiles_m;
+  g.tiles = p.tiles;
+  g.full = p.full;
+  g.splits = p.splits;
+  g.part = part;
+  const size_t e = a.f32 ? 4 : 2;
+  g.aligned = copy_fits(a.dw, a.d * e, a.lddw * e);
+  const uint64_t items = p.full + (uint64_t)(p.tiles - p.full) * p.splits;
+  cudaError_t rc;
+  const auto go = [&](auto launch_fn) {
+    return launch_fn(a.r, a.p, a.ldp, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, items, g, a.device, sms, err, stream);
+  };
+  if (a.f32)
+    rc = p.cg == 2 ? go(launch<2, 128, 3, true, float>) : go(launch<1, 64, 3, true, float>);
+  else
+    rc = p.cg == 2 ? go(launch<2, 256, 1, true, __nv_bfloat16>) : go(launch<1, 128, 1, true, __nv_bfloat16>);
+  *launches = 1;
+  if (rc != cudaSuccess || p.splits == 1) return rc;
+  ++*launches;
+  return launch_join(part, p.splits, p.cg * 128, p.bn, p.full, p.tiles - p.full, p.tiles_m, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
+}
+
+size_t vocab_dx_rows(uint32_t most, size_t ldd) {
+  // two planes, and for few tokens more, as long as they are small
+  const size_t fit = (16u << 20) / ldd;
+  return 2 * (size_t)most > fit ? 2 * (size_t)most : fit;
+}
+
+cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream) {
+  const DxShape s = dx_shape(a);
+  GradArgs g = {};
+  g.n = a.d;
+  g.bn = s.bn;
+  g.ksteps = (a.cols + kDepth - 1) / kDepth;
+  g.first = (a.first + kDepth - 1) / kDepth;
+  g.plane_rows = a.plane_rows;
+  g.begin = a.begin;
+  const uint64_t items = sms / s.cg;
+  if (s.cg == 2)
+    return launch<2, 256, 1, false, float>(a.r, a.p, a.ldp, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
+  return launch<1, 128, 1, false, float>(a.r, a.p, a.ldp, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
+}
+
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream) {
+  const DxShape s = dx_shape(a);
+  return launch_with(dx_finish_kernel, dim3((t + 7) / 8), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
+                     a.r.row, (uint32_t)(128 * s.cg), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), t, a.d,
+                     static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2));
+}
+
+cudaError_t launch_vocab_dbias(const float* part, size_t ldp, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream) {
+  return launch_with(dbias_kernel, dim3((cols + 31) / 32), dim3(256), 0, 1, true, stream, part, ldp, r.count, r.rows, cols, dbias);
+}
+
+}  // namespace stq

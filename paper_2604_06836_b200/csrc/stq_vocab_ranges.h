@@ -1,0 +1,36 @@
+// How the sums of the tiles of dx are shared out.
+#pragma once
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define STQ_BOTH __host__ __device__
+#else
+#define STQ_BOTH
+#endif
+
+namespace stq {
+
+// Tiles of dx, and which units (CTAs or pairs) add to which: unit u has stages [u S / U, (u + 1) S / U) of the S = tiles * ksteps.
+struct Ranges {
+  uint32_t tiles_m, tiles, ksteps, U;
+  uint64_t S;
+  STQ_BOTH Ranges(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t k, uint32_t units, uint32_t plane_rows) {
+    tiles_m = (rows + tile_m - 1) / tile_m;
+    tiles = tiles_m * tiles_n;
+    ksteps = k;
+    S = (uint64_t)tiles * k;
+    U = 0;
+    if (S == 0) return;
+    // so long a range that no tile has more units than there are planes
+    const uint32_t planes = plane_rows / (tiles_m * tile_m), least = planes > 2 ? (k + planes - 2) / (planes - 1) : k;
+    const uint64_t most = S / least;
+    U = (uint32_t)(units < most ? units : most);
+  }
+  STQ_BOTH uint64_t begin(uint32_t u) const { return u * S / U; }
+  STQ_BOTH uint32_t unit_of(uint64_t s) const { return (uint32_t)(((s + 1) * U - 1) / S); }
+  STQ_BOTH uint32_t shares(uint32_t tile) const {
+    return unit_of((uint64_t)tile * ksteps + ksteps - 1) - unit_of((uint64_t)tile * ksteps) + 1;
+  }
+};
+
+}  // namespace stq

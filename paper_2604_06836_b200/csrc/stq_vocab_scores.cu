@@ -1,0 +1,463 @@
+// Cross entropy over a vocabulary without keeping the logits z[t][i] = x[t] . w[i] + b[i]:
+//   lse[t] = log sum_i exp z[t][i],  loss[t] = lse[t] - z[t][target[t]],  dz[t][i] = dloss[t] (exp(z[t][i] - lse[t]) - [i = target[t]])
+// One kernel forms the logits tile by tile in tensor memory and either reduces them (a maximum and a sum of exp a row and
+// part of the vocabulary, joined by a second kernel) or, with lse known, turns them into their gradients, in bf16, for one
+// piece of the vocabulary at a time; stq_vocab_grad.cu multiplies these with w and x.  The logits are formed twice that way:
+// 2 t v d operations more, against 4 t v bytes held between the passes.
+//
+// Tokens without a loss (padding, what a masked language model does not predict) take no part: their rows are left out
+// first (gather_kernel).  How many are left is known on the device alone, so every kernel reads it there.
+#include <cuda_bf16.h>
+
+#include "../../include/stq.h"
+#include "stq_q8_mma.cuh"
+#include "stq_q8_tma.h"
+#include "stq_rowcopy.cuh"
+#include "stq_vocab.h"
+
+namespace stq {
+namespace {
+
+constexpr int kDepth = 64;             // length of the sum per stage: 128 bytes of bf16
+constexpr int kStepK = 16;             // and per product instruction
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// ---- rows ----------------------------------------------------------------------------------------------------------
+constexpr int kGatherRows = 32;        // tokens to a CTA
+
+// Every CTA counts the targets before its tokens and in all, so that nothing has to be passed between CTAs.
+__global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ uint32_t sums[2][8];
+  __shared__ int32_t where[kGatherRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t t0 = blockIdx.x * kGatherRows;
+  uint32_t before = 0, all = 0;
+  for (uint32_t i = threadIdx.x; i < a.t; i += 256) {
+    const uint32_t counts = a.target[i] != a.ignore;
+    all += counts;
+    before += i < t0 ? counts : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) { sums[0][warp] = before; sums[1][warp] = all; }
+  __syncthreads();
+  before = all = 0;
+  for (int i = 0; i < 8; ++i) { before += sums[0][i]; all += sums[1][i]; }
+  if (warp == 0) {
+    const uint32_t t = t0 + lane;
+    const bool counts = t < a.t && a.target[t] != a.ignore;
+    const uint32_t mask = __ballot_sync(0xffffffffu, counts);
+    const int32_t to = counts ? (int32_t)(before + __popc(mask & ((1u << lane) - 1))) : -1;
+    where[lane] = to;
+    if (t < a.t) a.row[t] = to;
+    if (counts) a.token[to] = t;
+    if (blockIdx.x == 0 && lane == 0) *a.count = all;
+  }
+  __syncthreads();
+  const uint32_t per_row = (a.d + 255) / 256;
+  const uint16_t* x = static_cast<const uint16_t*>(a.x);
+  uint16_t* out = static_cast<uint16_t*>(a.out);
+  for (uint32_t i = warp; i < kGatherRows * per_row; i += 8) {
+    const uint32_t r = i / per_row, part = i - r * per_row;
+    if (where[r] >= 0) copy_row_part(x + (size_t)(t0 + r) * a.ldx, a.d, part * 256, out + (size_t)where[r] * a.ldo, lane);
+  }
+  // the rest of the last tile: what is multiplied with zeros must be finite
+  const uint32_t end = min(a.most, (all + 255) / 256 * 256);
+  for (uint32_t r = all + blockIdx.x; r < end; r += gridDim.x)
+    for (uint32_t c = threadIdx.x * 8; c < a.ldo; c += 256 * 8) *reinterpret_cast<uint4*>(out + (size_t)r * a.ldo + c) = make_uint4(0, 0, 0, 0);
+}
+
+// ---- products ------------------------------------------------------------------------------------------------------
+struct ScoreArgs {
+  const uint32_t* count;
+  uint32_t rows, most;
+  uint32_t v0, v1, ksteps, tiles_n;
+  const float* bias;
+  // loss
+  float2* part;
+  // gradients
+  const uint32_t* token;
+  const int64_t* target;
+  int64_t ignore;
+  const float* lse;
+  const float* dloss;
+  float* dbias;
+  size_t ldp;
+  int* err;
+};
+
+constexpr int kWriters = 8;            // warps that take results out of tensor memory: two to each quarter of its lanes
+
+template <int CG, int BN, int PLANES>  // PLANES = 0: the loss
+struct ScoreShape {
+  static constexpr int kThreads = 32 * (2 + kWriters);
+  static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
+  static constexpr int kOut = PLANES ? kWriters * kStageBytes : 0;
+  static constexpr int kFit = (225 * 1024 - kOut) / kStage;
+  static constexpr int kStages = kFit < 8 ? kFit : 8;
+  static constexpr int kSmem = kStages * kStage + kOut + 1024;
+};
+
+// Sums over the lanes: lane i gets that of v[i].
+__device__ __forceinline__ float lane_sums(float (&v)[32], int lane) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const bool up = lane & o;
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const float give = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+      v[i] = __fadd_rn(keep, __shfl_xor_sync(0xffffffffu, give, o));
+    }
+  }
+  return v[0];
+}
+
+template <int CG, int BN, int PLANES>
+__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES>::kThreads), 1)
+score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_p,
+             const ScoreArgs a) {
+  using S = ScoreShape<CG, BN, PLANES>;
+  constexpr int kStages = S::kStages, kNB = BN / CG;
+  extern __shared__ uint8_t raw[];
+  __shared__ uint64_t bars[2 * kStages + 4];
+  __shared__ uint32_t tmem_slot;
+  const uint32_t ring = (smem_addr(raw) + 1023u) & ~1023u, outs = ring + kStages * S::kStage;
+  // per stage: has landed (both CTAs, at the leader), is free; per accumulator: done, read (both CTAs, at the leader)
+  const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, done = empty + 8 * kStages, freed = done + 16;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+  const bool leader = rank == 0;
+  const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      bar_init(full + 8 * i, 1);
+      bar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(done + 8 * i, 1);
+      bar_init(freed + 8 * i, kWriters * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc<CG>(smem_addr(&tmem_slot), 2 * BN);
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
+  mma_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const uint32_t count = a.count ? *a.count : a.rows;
+  const uint32_t tiles_m = (count + 128 * CG - 1) / (128 * CG), tiles = tiles_m * a.tiles_n;
+
+  bool ok = true;
+  if (warp == 0) {
+    if (elect_one()) {
+      uint32_t it = 0;
+      const uint32_t full0 = CG == 2 ? peer_addr(full, 0) : full;
+      for (uint32_t w = unit; ok && w < tiles; w += units) {
+        const int row = (int)(w % tiles_m * 128 * CG + 128 * rank), col = (int)(a.v0 + w / tiles_m * BN + kNB * rank);
+        for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          if (!(ok = bar_wait(empty + 8 * s, ph ^ 1))) break;
+          const uint32_t at = ring + s * S::kStage;
+          if (leader) bar_expect(full + 8 * s, CG * S::kStage);
+          tensor_load<CG>(at, &map_x, (int)(k * kDepth), row, full0 + 8 * s);
+          tensor_load<CG>(at + S::kA, &map_w, (int)(k * kDepth), col, full0 + 8 * s);
+        }
+      }
+      if (!ok && leader)      // leave no copy in flight
+        for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i) bar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+    }
+  } else if (warp == 1) {
+    if (leader && elect_one()) {
+      constexpr uint32_t id = idesc(kIdescBf16, 128 * CG, BN, false, false);
+      uint32_t it = 0, n = 0;
+      for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
+        const uint32_t acc = n & 1;
+        if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+        mma_fence_after();
+        for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          if (!(ok = bar_wait<CG == 2>(full + 8 * s, ph))) break;
+          mma_fence_after();
+          const uint64_t da = operand_desc(ring + s * S::kStage, 16, 1024), db = operand_desc(ring + s * S::kStage + S::kA, 16, 1024);
+#pragma unroll
+          for (int j = 0; j < kDepth / kStepK; ++j)
+            mma<CG, false>(tmem + acc * BN, da + j * ((kStepK * 2) >> 4), db + j * ((kStepK * 2) >> 4), id, k != 0 || j != 0);
+          mma_commit<CG>(empty + 8 * s);
+          if (k + 1 == a.ksteps) mma_commit<CG>(done + 8 * acc);
+        }
+      }
+    }
+  } else {
+    const int quad = warp & 3, half = (warp - 2) / 4;
+    const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
+    uint32_t n = 0;
+    for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
+      const uint32_t acc = n & 1, from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN + half * (BN / 2);
+      const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
+      const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * BN + half * (BN / 2);
+      // gradients: what this row is multiplied with, its normaliser and its target, if that lies in these columns
+      float g = 0.f, lse = 0.f;
+      int32_t hit = -1;
+      bool real = false;
+      if constexpr (PLANES > 0) {
+        if (row < count) {
+          const uint32_t t = a.token ? a.token[row] : row;
+          const int64_t to = a.target[t];
+          real = to != a.ignore;
+          if (real) {
+            g = a.dloss[t];
+            lse = a.lse[t];
+            if (to >= col0 && to < col0 + BN / 2) hit = (int32_t)(to - col0);
+          }
+        }
+      }
+      ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
+      if (!(ok = all_of<32 * kWriters>(ok))) break;       // (the writing warps leave together)
+      mma_fence_after();
+      auto add_bias = [&](float(&v)[32], uint32_t col) {
+        if (a.bias) {
+          const float mine = col + lane < a.v1 ? __ldg(a.bias + col + lane) : 0.f;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, mine, i));
+        }
+      };
+      if constexpr (PLANES == 0) {
+        float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 32) {
+          const uint32_t col = col0 + c;
+          if (col >= a.v1) break;
+          float v[32];
+          load_block(from + c, v);
+          add_bias(v, col);
+          if (col + 32 > a.v1) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (col + i >= a.v1) v[i] = -INFINITY;
+          }
+          float top = m;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) top = fmaxf(top, v[i]);
+          // (nothing but -inf so far, or NaN, which fmaxf passes over: measured from 0 they add 0 or NaN)
+          const float ref = top == -INFINITY ? 0.f : top, shift = -ref * kLog2e;
+          s = s * ex2(__fmul_rn(__fadd_rn(m, -ref), kLog2e));
+          float more[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 32; ++i) more[i & 3] = __fadd_rn(more[i & 3], ex2(__fmaf_rn(v[i], kLog2e, shift)));
+          s = __fadd_rn(s, __fadd_rn(__fadd_rn(more[0], more[1]), __fadd_rn(more[2], more[3])));
+          m = top;
+        }
+        if (row < a.most) a.part[(size_t)(2 * tile + half) * a.most + row] = make_float2(m, s);
+      } else {
+        const uint32_t out = outs + (warp - 2) * kStageBytes;
+#pragma unroll 1
+        for (int c = 0; c < BN / 2; c += 64) {
+          const uint32_t col = col0 + c;
+          if (col - a.v0 >= a.ldp) break;
+          float v[64];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float(&b)[32] = *reinterpret_cast<float(*)[32]>(v + 32 * h);
+            load_block(from + c + 32 * h, b);
+            add_bias(b, col + 32 * h);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              const float p = ex2(__fmul_rn(__fadd_rn(b[i], -lse), kLog2e));
+              const float z = __fmul_rn(g, hit == c + 32 * h + i ? __fadd_rn(p, -1.f) : p);
+              b[i] = real && col + 32 * h + i < a.v1 ? z : 0.f;
+            }
+          }
+          if (a.dbias) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float b[32];
+#pragma unroll
+              for (int i = 0; i < 32; ++i) b[i] = v[32 * h + i];
+              const float sum = lane_sums(b, lane);
+              a.dbias[(size_t)(row0 / 32) * a.ldp + (col - a.v0) + 32 * h + lane] = sum;
+            }
+          }
+          // the next part holds what this one's rounding left (exactly: three parts of 8 bits are the 24 of fp32)
+#pragma unroll
+          for (int p = 0; p < PLANES; ++p) {
+            store_block<__nv_bfloat16>(&map_p, (int)(col - a.v0), (int)(row0 + p * a.most), v, lane, out);
+            if (p + 1 < PLANES) {
+#pragma unroll
+              for (int i = 0; i < 64; ++i) v[i] = __fadd_rn(v[i], -__bfloat162float(__float2bfloat16_rn(v[i])));
+            }
+          }
+        }
+      }
+      mma_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+    }
+    if constexpr (PLANES > 0) store_blocks_done(lane);
+  }
+  if (!ok) *a.err = 1;
+  __syncwarp();
+  mma_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();
+  if (warp == 1) {
+    mma_fence_after();
+    tmem_free<CG>(tmem, 2 * BN);
+  }
+}
+
+// 32 tokens to a CTA: eight warps share the parts of each, then each warp forms the logits of four targets, in fp32 from the
+// bf16 operands.  (Taken from the tensor memory they would carry the matrix unit's cut-off sums.)
+__global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const uint16_t* x, size_t ldx, const float2* part, uint32_t parts,
+                                                     float* loss, float* lse) {
+  __shared__ float2 sums[8][33];
+  __shared__ float chosen[32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t t0 = blockIdx.x * 32;
+  const uint16_t* w = static_cast<const uint16_t*>(a.w);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t t = t0 + 4 * warp + i;
+    float z = 0.f;
+    if (t < a.t) {
+      const int64_t to = a.target[t];
+      if (to == a.ignore) {
+        z = 0.f;
+      } else if (to < 0 || to >= (int64_t)a.v) {
+        z = __int_as_float(0x7fc00000);
+      } else {
+        const uint16_t *p = x + (size_t)t * ldx, *q = w + (size_t)to * a.ldw;
+        float s[2] = {0.f, 0.f};
+        if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 3) == 0) {
+          for (uint32_t c = 2 * lane; c + 1 < a.d; c += 64) {
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(p + c), y = *reinterpret_cast<const uint32_t*>(q + c);
+            s[0] = __fmaf_rn(__uint_as_float(u << 16), __uint_as_float(y << 16), s[0]);
+            s[1] = __fmaf_rn(__uint_as_float(u & 0xffff0000u), __uint_as_float(y & 0xffff0000u), s[1]);
+          }
+          if ((a.d & 1) && lane == 0) s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[a.d - 1] << 16), __uint_as_float((uint32_t)q[a.d - 1] << 16), s[0]);
+        } else {
+          for (uint32_t c = lane; c < a.d; c += 32) s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[c] << 16), __uint_as_float((uint32_t)q[c] << 16), s[0]);
+        }
+        z = s[0] + s[1];
+        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        if (a.bias) z += a.bias[to];
+      }
+    }
+    if (lane == 0) chosen[4 * warp + i] = z;
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const uint32_t t = t0 + lane;
+  int32_t row = -1;
+  if (t < a.t) row = a.r.row ? a.r.row[t] : a.target[t] != a.ignore ? (int32_t)t : -1;
+  float m = -INFINITY, s = 0.f;
+  if (row >= 0) {
+    for (uint32_t i = warp; i < parts; i += 8) {
+      const float2 p = __ldcg(part + (size_t)i * a.r.most + row);
+      const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
+      s = __fadd_rn(__fmul_rn(s, ex2((m - ref) * kLog2e)), __fmul_rn(p.y, ex2((p.x - ref) * kLog2e)));
+      m = top;
+    }
+  }
+  sums[warp][lane] = make_float2(m, s);
+  __syncthreads();
+  if (warp != 0 || t >= a.t) return;
+  for (int i = 1; i < 8; ++i) {
+    const float2 p = sums[i][lane];
+    const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
+    s = __fadd_rn(__fmul_rn(s, ex2((m - ref) * kLog2e)), __fmul_rn(p.y, ex2((p.x - ref) * kLog2e)));
+    m = top;
+  }
+  const float total = row < 0 ? 0.f : (m == -INFINITY ? 0.f : m) + logf(s), z = chosen[lane];
+  // (the NaN of a target outside the vocabulary goes into lse as well: all gradients of the token are NaN)
+  lse[t] = z != z && row >= 0 ? z : total;
+  loss[t] = row < 0 ? 0.f : total - z;
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+template <int CG, int BN, int PLANES>
+cudaError_t launch(const VocabArgs& a, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
+  using S = ScoreShape<CG, BN, PLANES>;
+  s.count = a.r.count;
+  s.rows = a.r.rows;
+  s.most = a.r.most;
+  s.bias = a.bias;
+  s.ksteps = (a.d + kDepth - 1) / kDepth;
+  s.tiles_n = (s.v1 - s.v0 + BN - 1) / BN;
+  CUtensorMap mx, mw, mp = {};
+  cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, 128, kDepth, true);
+  if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, BN / CG, kDepth, true);
+  if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->planes, o->ldp, o->ldp, 32, 64, true);
+  auto* kernel = score_kernel<CG, BN, PLANES>;
+  static std::atomic<uint64_t> seen;
+  if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, a.device, seen);
+  if (e != cudaSuccess) return e;
+  const uint64_t items = (uint64_t)((a.r.rows + 128 * CG - 1) / (128 * CG)) * s.tiles_n, most = sms / CG;
+  return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, true, stream, mx, mw, mp, s);
+}
+
+template <int PLANES>
+cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
+  if (sh.bn == 256) return launch<2, 256, PLANES>(a, s, o, sms, stream);
+  return launch<1, 128, PLANES>(a, s, o, sms, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
+  gather_kernel<<<(a.t + kGatherRows - 1) / kGatherRows, 256, 0, stream>>>(a);
+  return cudaGetLastError();
+}
+
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms) {
+  if (rows <= 128) return {1, 128};
+  const uint32_t k = (d + kDepth - 1) / kDepth;
+  auto cost = [&](int cg, int bn, double stage) {
+    const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + bn - 1) / bn), units = sms / cg;
+    return (double)((tiles + units - 1) / units) * (k * stage + 2500.0);
+  };
+  return cost(2, 256, 512.0) <= cost(1, 128, 300.0) ? VocabShape{2, 256} : VocabShape{1, 128};
+}
+
+uint32_t vocab_parts(const VocabArgs& a, VocabShape s) { return 2 * ((a.v + s.bn - 1) / s.bn); }
+
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, float2* part, int sms, int* err, cudaStream_t stream) {
+  ScoreArgs s = {};
+  s.v0 = 0;
+  s.v1 = a.v;
+  s.part = part;
+  s.err = err;
+  return by_shape<0>(a, sh, s, nullptr, sms, stream);
+}
+
+cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss, float* lse,
+                                cudaStream_t stream) {
+  return launch_with(finish_kernel, dim3((a.t + 31) / 32), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts,
+                     loss, lse);
+}
+
+cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,
+                                 cudaStream_t stream) {
+  ScoreArgs s = {};
+  s.v0 = v0;
+  s.v1 = v1;
+  s.token = a.r.token;
+  s.target = a.target;
+  s.ignore = a.ignore;
+  s.lse = o.lse;
+  s.dloss = o.dloss;
+  s.dbias = o.dbias;
+  s.ldp = o.ldp;
+  s.err = err;
+  return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream) : by_shape<1>(a, sh, s, &o, sms, stream);
+}
+
+}  // namespace stq

@@ -368,6 +368,31 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
                             const float* bias, const int64_t* target, int64_t ignore_index, const float* lse, uint64_t t, uint32_t v,
                             uint32_t d, void* dx, uint64_t lddx, void* dw, uint64_t lddw, int dw_dtype, float* dbias, void* stream);
 
+/* ---- norm of all gradients, and clipping ----------------------------------------------------------
+ *   norm = inv * sqrt(sum over all tensors of g^2),  factor = inv * min(1, max_norm / (norm + eps))
+ * inv_scale: DEVICE pointer to one float, 1 / loss scale, or NULL (1).  norm and factor: DEVICE pointers to one float each,
+ * written on `stream`; the calls do not synchronise.  factor is what stq_hparams.inv_grad_scale takes: the step then applies
+ * it, and the gradients are not written.  max_norm > 0; infinity: no clipping, factor = inv.  found_inf (optional, DEVICE):
+ * set to 1 if the norm is infinite or NaN, else left as it is.  An infinite norm makes the factor 0, a NaN makes it NaN.
+ * Squares are summed in fp32 over up to 64 numbers and in double beyond, in double throughout where fp32's range does not
+ * suffice; always in the same order.  Addresses and lengths travel as launch parameters: the gradients may lie elsewhere in every
+ * call, and a captured graph keeps those it was captured with.  Workspace, streams and graphs: as for the 8-bit operators. */
+typedef struct stq_grad {
+  const void* grad;    /* numel numbers of `dtype`, aligned to their size (16-byte alignment runs fastest) */
+  void* out;           /* stq_grad_clip: grad * factor, of `out_dtype`; may be `grad` itself, and may overlap no
+                          other gradient or result of the call.  stq_grad_norm ignores it                       */
+  uint64_t numel;      /* 0 is allowed; below 2^40                                                             */
+  int32_t dtype;       /* STQ_GRAD_F32, STQ_GRAD_BF16 or STQ_GRAD_F16, each tensor its own                       */
+  int32_t out_dtype;   /* the same as dtype, or STQ_GRAD_F32                                                  */
+} stq_grad;
+
+int stq_grad_norm(stq_handle* h, const stq_grad* grads, int n, const float* inv_scale, float max_norm, float eps, float* norm, float* factor,
+                  float* found_inf, void* stream);
+/* The same, and out = grad * factor, rounded once.  Where every result lies in place of its gradient and the factor is 1, nothing is
+ * written. */
+int stq_grad_clip(stq_handle* h, const stq_grad* grads, int n, const float* inv_scale, float max_norm, float eps, float* norm, float* factor,
+                  float* found_inf, void* stream);
+
 /* ---- transition decision (host only; Sec. 3.3-3.4, Algorithm 1 decision branch) -------------- */
 typedef struct stq_policy_cfg {
   double alpha;         /* EMA factor of the three global running statistics                  */

@@ -33,9 +33,10 @@ struct Rows {
   uint32_t *count, *token;
   int32_t* row;
 
-  Rows(const VocabArgs& a, const void* x_, size_t ldx_) {
-    // (up to one tile of tokens there is nothing to gain from leaving some out)
-    gather = a.t > 128 || !rows_aligned(x_, a.t > 1 ? ldx_ * 2 : 0);
+  Rows(const VocabArgs& a, const void* x_, size_t ldx_, bool backward) {
+    // For a loss of up to one tile of tokens there is nothing to gain from leaving some out.  (For dw there is: what a token
+    // without a loss holds may be NaN, and its product with 0 too.)
+    gather = backward || a.t > 128 || !rows_aligned(x_, a.t > 1 ? ldx_ * 2 : 0);
     pitch_w = !rows_aligned(a.w, a.v > 1 ? a.ldw * 2 : 0);
     ldx = up(a.d, 8);
     ldw = up(a.d, 8);
@@ -113,7 +114,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   // (the blocks of tokens share one workspace, laid out for the largest)
   a.t = (uint32_t)(t < kTokensAtOnce ? t : kTokensAtOnce);
   a.target = target;
-  Rows r(a, x, ldx);
+  Rows r(a, x, ldx, false);
   const uint32_t most = most_rows(a.t);
   const VocabShape shape = vocab_shape(a.t, v, d, h->sm_count);
   const uint32_t parts = vocab_parts(a, shape);
@@ -169,7 +170,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   a.target = target;
   a.ignore = ignore_index;
   a.device = h->device;
-  Rows r(a, x, ldx);
+  Rows r(a, x, ldx, true);
   const uint32_t most = most_rows(a.t);
   const int planes = dw && dw_dtype == STQ_GRAD_F32 ? 3 : 1;
   // pieces of the vocabulary: equal but for the last

@@ -250,11 +250,12 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < 32; ++i) top = fmaxf(top, v[i]);
           // (nothing but -inf so far, or NaN, which fmaxf passes over: measured from 0 they add 0 or NaN)
-          const float ref = top == -INFINITY ? 0.f : top, shift = -ref * kLog2e;
+          // (subtracted before it is scaled: a logit may be the lowest number there is)
+          const float ref = top == -INFINITY ? 0.f : top;
           s = s * ex2(__fmul_rn(__fadd_rn(m, -ref), kLog2e));
           float more[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) more[i & 3] = __fadd_rn(more[i & 3], ex2(__fmaf_rn(v[i], kLog2e, shift)));
+          for (int i = 0; i < 32; ++i) more[i & 3] = __fadd_rn(more[i & 3], ex2(__fmul_rn(__fadd_rn(v[i], -ref), kLog2e)));
           s = __fadd_rn(s, __fadd_rn(__fadd_rn(more[0], more[1]), __fadd_rn(more[2], more[3])));
           m = top;
         }

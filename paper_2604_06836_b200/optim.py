@@ -21,7 +21,7 @@ from typing import Iterable
 import numpy as np
 import torch
 
-from . import stq
+from . import clip, stq
 
 
 class STQAdamW(torch.optim.Optimizer):
@@ -41,17 +41,24 @@ class STQAdamW(torch.optim.Optimizer):
     With ``found_inf`` set, ``step()`` reads it on the host first (one small synchronising copy): a step
     with a non-finite gradient is left out entirely, so the step count t, the bias corrections and the
     decision schedule follow the steps actually taken and no statistics of a skipped step reach the policy.
+    max_norm: clips the gradients to this 2-norm over all of them (after unscaling).  One more pass reads the
+    gradients; the step applies the factor as it reads them, so they are not written.  Statistics of a decision
+    step are those of the clipped gradients, in both orders.  ``self.last_norm`` is the norm before clipping, on
+    the device.  With ``found_inf`` set, a norm that is not finite raises it too, and the step is left out.
     """
 
     def __init__(self, params: Iterable, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay: float = 0.01, *, block: int = 128, init_bits=16, policy: str = "paper",
                  interval: int = 10, alpha: float = 0.1, tau: float = 100.0, eps_stat: float = 1e-8,
-                 v_log: str = "poly", decoupled_weight_decay: bool = True, order: str = "paper"):
+                 v_log: str = "poly", decoupled_weight_decay: bool = True, order: str = "paper",
+                 max_norm: float | None = None):
         if policy not in ("paper", "fixed"):
             raise ValueError("policy is 'paper' or 'fixed'")
         if order not in ("paper", "fused"):
             raise ValueError("order is 'paper' or 'fused'")
-        self.order = order
+        if max_norm is not None and not max_norm > 0.0:
+            raise ValueError("max_norm is positive")
+        self.order, self.max_norm, self.last_norm = order, max_norm, None
         self._carried_stats = None        # sums that rode on the last step (fused order), fetched right after it
         if block not in (32, 64, 128, 256, 512, 1024):
             raise ValueError("block is a power of two in 32..1024")
@@ -123,6 +130,20 @@ class STQAdamW(torch.optim.Optimizer):
             self._tbl_key = key
         return self._tbl
 
+    def _clip_factor(self):
+        """What the step multiplies the gradients with: 1 / loss scale, and what clips them."""
+        if self.max_norm is None:
+            return self.grad_scaler_inv
+        for p in self._params:
+            if p.grad is None:
+                raise ValueError("every parameter needs a gradient (frozen parameters do not belong here)")
+            if not p.grad.is_contiguous():
+                p.grad = p.grad.contiguous()
+        r = clip.grad_norm(self.handle, [p.grad for p in self._params], max_norm=self.max_norm, inv_scale=self.grad_scaler_inv,
+                           found_inf=self.found_inf)
+        self.last_norm = r.norm
+        return r.factor
+
     # ---- the step -----------------------------------------------------------------------------------
     @torch.no_grad()
     def step(self, closure=None):
@@ -130,6 +151,7 @@ class STQAdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        scale = self._clip_factor()
         if self.found_inf is not None and float(self.found_inf.item()) != 0.0:
             self.skipped_steps += 1       # nothing is launched, t does not advance, carried statistics are kept
             return loss
@@ -137,7 +159,7 @@ class STQAdamW(torch.optim.Optimizer):
         t = self.t
         hp = dict(lr=self.param_groups[0]["lr"], beta1=self.betas[0], beta2=self.betas[1], eps=self.eps, t=t,
                   grad_dtype=self._grad_dtype(), decoupled_wd=self.decoupled,
-                  inv_grad_scale=self.grad_scaler_inv, found_inf=self.found_inf, sr_seed=self.sr_seed)
+                  inv_grad_scale=scale, found_inf=self.found_inf, sr_seed=self.sr_seed)
         new_m = new_v = None
         if self.policy_kind == "paper" and self.policy.is_decision_step(t):
             stats, self._carried_stats = self._carried_stats, None    # fused order: they rode on the previous step
@@ -145,8 +167,8 @@ class STQAdamW(torch.optim.Optimizer):
                 tbl = self._table()
                 self.handle.grad_stats(tbl, hp["grad_dtype"])
                 stats = self.handle.layer_stats(len(self._params))
-                if self.grad_scaler_inv is not None:   # the pre-pass sees the scaled gradients: unscale the sums
-                    s = float(self.grad_scaler_inv.item())
+                if scale is not None:   # the pre-pass sees the scaled gradients: unscale (and clip) the sums
+                    s = float(scale.item())
                     stats[:, 0:2] *= s
                     stats[:, 2] *= s * s
             bits, self.last_scores = self.policy.decide(stats, t)

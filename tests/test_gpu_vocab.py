@@ -4,7 +4,9 @@ Tolerances.  U = 2^-24 and UB = 2^-8 are half steps of fp32 and bf16.  A logit i
 addition cut off (one step, 2 U) and the products exact: it is off by dz <= 2 U (d / 16 + 2) a with a = the sum of the products'
 magnitudes.  lse is off by the largest dz of the row and by the roundings of exp, of a sum that is joined in a few hundred steps of
 which at most 2 v / 128 + 64 follow one another, and of log.  A gradient of a logit g (p - [hit]) is off by g p e with
-e = dz + error of lse + 8 U (|z - lse| + 2), and by UB of itself where it is rounded to bf16.
+e = dz + error of lse + 8 U (|z - lse| + 2), and by UB of itself where it is rounded to bf16.  Below the normal numbers, 2^-126, all
+of this is absolute: an exp that is smaller may come out as 0, which g carries on, and so may the product with g and each of the three
+parts that it is passed on in: (|g| + 4) 2^-126.
 """
 import pytest
 import torch
@@ -67,7 +69,7 @@ class Definition:
         g = torch.where(self.counts, dloss.double(), 0.0)[:, None]
         e = dz + self.elog[:, None] + 8 * U * ((z - lse[:, None]).abs() + 2)
         grad = p.scatter_add(1, at, -torch.ones_like(p[:, :1])) * g
-        off = p * e * g.abs()
+        off = p * e * g.abs() + (g.abs() + 4) * 2.0 ** -126 * (g != 0)
         self.x, self.w, self.grad, self.off = x, w, grad, off
         self.t, self.v = t, v
 
@@ -115,3 +117,227 @@ def test_loss_and_gradients(handle, t, d, v, dtype):
         x, w, target, b, dloss = inputs(t, d, v, t + d + v, bias, masked)
         out, grads = run(handle, x, w, target, b, dloss, dtype)
         Definition(x, w, target, b, dloss).check(out, grads, dtype, f"{t} {d} {v} {bias}")
+
+
+def test_many_pieces_of_the_vocabulary(handle):
+    """The gradients of the logits of 9000 tokens exist for 14336 entries at a time (4608 in three parts): three pieces, and seven."""
+    x, w, target, b, dloss = inputs(9000, 72, 30001, 5, True, 0.1)
+    d = Definition(x, w, target, b, dloss)
+    for dtype in (BF, F32):
+        out, grads = run(handle, x, w, target, b, dloss, dtype)
+        d.check(out, grads, dtype, "pieces")
+
+
+def test_more_tokens_than_a_loss_takes_at_once(handle):
+    x, w, target, b, dloss = inputs(70001, 16, 300, 6, True, 0.5)
+    d = Definition(x, w, target, b, dloss)
+    out, grads = run(handle, x, w, target, b, dloss, F32)
+    d.check(out, grads, F32, "tokens")
+
+
+@pytest.mark.parametrize("extra,shift", [(8, 0), (8, 8), (3, 0), (1, 1), (0, 3)])
+@pytest.mark.parametrize("t", [5, 300])
+def test_pitches_and_alignment(handle, t, extra, shift):
+    x, w, target, b, dloss = inputs(t, 200, 333, 8, True, 0.2)
+    want_out, want = run(handle, x, w, target, b, dloss, BF)
+    for fill in (7.0, float("nan")):      # what lies between the rows does not matter
+        xp, wp = pitched(x, extra, shift, fill), pitched(w, extra, shift, fill)
+        out, grads = run(handle, xp, wp, target, b, dloss, BF)
+        assert torch.equal(out.lse, want_out.lse) and torch.equal(grads.dx, want.dx) and torch.equal(grads.dw, want.dw)
+        Definition(x, w, target, b, dloss).check(out, grads, BF, "pitch")
+
+
+def test_which_gradients_are_asked_for(handle):
+    x, w, target, b, dloss = inputs(300, 128, 700, 9, True, 0.2)
+    out, want = run(handle, x, w, target, b, dloss, F32)
+    for dx in (True, False):
+        for dw in (True, False):
+            for db in (True, False):
+                g = vocab.loss_backward(handle, dloss, x, w, target, out.lse, bias=b, dtype=F32, want_dx=dx, want_dw=dw, want_dbias=db)
+                for got, full, asked in zip(g, want, (dx, dw, db)):
+                    assert (got is not None) == asked and (got is None or torch.equal(got, full))
+    g = vocab.loss_backward(handle, dloss, x, w, target, out.lse, want_dbias=True)      # (of a bias of zeros)
+    assert g.dbias.shape == (700,)
+
+
+@pytest.mark.parametrize("t", [1, 100, 129, 700])
+def test_no_token_counts(handle, t):
+    x, w, target, b, dloss = inputs(t, 128, 300, 3, True)
+    target.fill_(IGNORE)
+    for dtype in (BF, F32):
+        out, grads = run(handle, x, w, target, b, dloss, dtype)
+        assert all((v == 0).all() for v in (*out, *grads))
+
+
+def test_no_tokens(handle):
+    x, w, target, b, dloss = inputs(0, 128, 300, 3, True)
+    out, grads = run(handle, x, w, target, b, dloss, F32)
+    assert out.loss.shape == (0,) and grads.dx.shape == (0, 128) and (grads.dw == 0).all() and (grads.dbias == 0).all()
+
+
+@pytest.mark.parametrize("t", [100, 500])
+def test_ignored_tokens_may_hold_anything(handle, t):
+    """NaN, infinities and huge values of tokens without a loss reach nothing, nor does their dloss."""
+    x, w, target, b, dloss = inputs(t, 128, 700, 4, True, 0.4)
+    want_out, want = run(handle, x, w, target, b, dloss, F32)
+    off = target == IGNORE
+    for value in (float("nan"), float("inf"), 3e38):
+        x2, d2 = x.clone(), dloss.clone()
+        x2[off] = value
+        d2[off] = value
+        out, grads = run(handle, x2, w, target, b, d2, F32)
+        assert all(torch.equal(a, c) for a, c in zip((*out, *grads), (*want_out, *want)))
+
+
+def test_another_ignore_index(handle):
+    x, w, target, b, dloss = inputs(300, 128, 700, 4, False, 0.4)
+    want = vocab.loss(handle, x, w, target)
+    other = torch.where(target == IGNORE, 5, torch.where(target == 5, 6, target))
+    out = vocab.loss(handle, x, w, other, ignore_index=5)
+    keep = target != 5
+    assert torch.equal(out.lse[keep], want.lse[keep])
+
+
+@pytest.mark.parametrize("t", [100, 500])
+def test_targets_outside_the_vocabulary_give_nan(handle, t):
+    x, w, target, b, dloss = inputs(t, 128, 700, 4, False, 0.2)
+    want_out, want = run(handle, x, w, target, b, dloss, BF)
+    for bad in (700, -1, -99, 2 ** 40, -2 ** 63):
+        wrong = target.clone()
+        wrong[17] = bad
+        out, grads = run(handle, x, w, wrong, b, dloss, BF)
+        assert out.loss[17].isnan() and out.lse[17].isnan() and grads.dx[17].isnan().all() and grads.dw.isnan().any()
+        others = torch.arange(t, device="cuda") != 17
+        assert torch.equal(out.loss[others], want_out.loss[others]) and torch.equal(grads.dx[others], want.dx[others])
+
+
+@pytest.mark.parametrize("t", [60, 400])
+def test_entries_out_of_the_vocabulary(handle, t):
+    """A bias of -inf, or of the lowest number: probability 0, no gradient, also where they fill whole tiles."""
+    x, w, target, b, dloss = inputs(t, 64, 1500, 4, True)
+    target = target % 300
+    live = torch.arange(1500, device="cuda") < 300
+    d = Definition(x, w[live], target, b[live], dloss)
+    for low in (-float("inf"), -3.4e38):
+        cut = torch.where(live, b, low)
+        out, grads = run(handle, x, w, target, cut, dloss, F32)
+        d.check(out, vocab.LossGrads(grads.dx, grads.dw[live], grads.dbias[live]), F32, str(low))
+        assert (grads.dw[~live] == 0).all() and (grads.dbias[~live] == 0).all()
+    # all of the vocabulary: there is nothing to normalise
+    out = vocab.loss(handle, x, w, target, bias=torch.full_like(b, -float("inf")))
+    assert (out.lse == -float("inf")).all() and out.loss.isnan().all()
+    # a target that is out: its loss is infinite, the others are as they were
+    wrong = target.clone()
+    wrong[3] = 1400
+    o = vocab.loss(handle, x, w, wrong, bias=torch.where(live, b, -float("inf")))
+    assert o.loss[3] == float("inf") and torch.equal(o.lse[4:], vocab.loss(handle, x, w, target, bias=torch.where(live, b, -float("inf"))).lse[4:])
+
+
+@pytest.mark.parametrize("t", [60, 400])
+def test_infinities_and_nan_stay_in_their_row(handle, t):
+    x, w, target, b, dloss = inputs(t, 64, 900, 4)
+    want_out, want = run(handle, x, w, target, b, dloss, BF)
+    x = x.clone()
+    x[5, 3], x[9, 0] = float("nan"), float("inf")
+    out, grads = run(handle, x, w, target, b, dloss, BF)
+    rows = torch.ones(t, dtype=torch.bool, device="cuda")
+    rows[5] = rows[9] = False
+    assert out.loss[5].isnan() and out.loss[9].isnan() and grads.dx[5].isnan().all()
+    assert torch.equal(out.loss[rows], want_out.loss[rows]) and torch.equal(grads.dx[rows], want.dx[rows])
+
+
+def test_logits_far_apart(handle):
+    """Logits in the thousands: one entry has all of the probability."""
+    x, w, target, b, dloss = inputs(300, 64, 900, 4, sharp=500.0)
+    out, grads = run(handle, x, w, target, b, dloss, F32)
+    Definition(x, w, target, b, dloss).check(out, grads, F32, "sharp")
+
+
+def test_the_same_from_run_to_run(handle):
+    x, w, target, b, dloss = inputs(700, 300, 3000, 4, True, 0.3)
+    first = run(handle, x, w, target, b, dloss, F32)
+    for _ in range(3):
+        again = run(handle, x, w, target, b, dloss, F32)
+        assert all(torch.equal(a, c) for p, q in zip(first, again) for a, c in zip(p, q))
+
+
+def test_gradients_against_differences(handle):
+    """The loss along +-2^-7 in w and in x, on numbers that bf16 holds exactly: (L+ - L-) / 2h is the derivative up to h^2 q^3, q the
+    largest change of a logit per unit, and to the error of the two losses over 2h."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    t, d, v, h = 200, 32, 150, 2.0 ** -7
+    pick = lambda n, m, a: torch.randint(-a, a + 1, (n, m), device="cuda", generator=g)      # noqa: E731
+    x, w = (pick(t, d, 31) * 2.0 ** -6).to(BF), (pick(v, d, 31) * 2.0 ** -6).to(BF)
+    ux, uw = pick(t, d, 1).float(), pick(v, d, 1).float()
+    target = torch.randint(0, v, (t,), device="cuda", generator=g)
+    dloss = torch.randn(t, device="cuda", generator=g)
+    out, grads = run(handle, x, w, target, None, dloss, F32)
+    total = lambda a, c: float((vocab.loss(handle, a, c, target).loss.double() * dloss.double()).sum())      # noqa: E731
+    weight = float(dloss.abs().sum())
+    for kind in ("w", "x"):
+        at = lambda s: total(x, (w.float() + s * h * uw).to(BF)) if kind == "w" else total((x.float() + s * h * ux).to(BF), w)      # noqa: E731
+        slope = (at(1) - at(-1)) / (2 * h)
+        got = float((grads.dw.double() * uw).sum()) if kind == "w" else float((grads.dx.double() * ux).sum())
+        change = (x.float() @ uw.T if kind == "w" else ux @ w.float().T).abs().max()
+        tol = weight * float(h * h * change ** 3 + 64 * U / h) + (0 if kind == "w" else 2 * UB * float((grads.dx.double().abs() * ux.abs()).sum()))
+        assert abs(got - slope) <= tol and tol < 0.2 * abs(slope) + 0.2 * weight, (kind, got, slope, tol)
+
+
+def test_on_another_stream_and_in_a_graph(handle):
+    x, w, target, b, dloss = inputs(500, 128, 2000, 4, True, 0.3)
+    want = run(handle, x, w, target, b, dloss, BF)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    x2 = torch.zeros_like(x)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(2000000)
+        x2.copy_(x)
+    out = vocab.loss(handle, x2, w, target, bias=b, stream=s)
+    grads = vocab.loss_backward(handle, dloss, x2, w, target, out.lse, bias=b, stream=s)
+    s.synchronize()
+    assert all(torch.equal(a, c) for p, q in zip(want, (out, grads)) for a, c in zip(p, q))
+
+    hd = stq.Handle()      # (its workspace grows inside the capture)
+    to = target.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, grads = run(hd, x2, w, to, b, dloss, BF)
+    big = inputs(3000, 256, 5000, 5)
+    run(hd, *big, F32)      # a larger call replaces the workspace; the graph keeps its own
+    for masked in (0.0, 0.9):      # how many tokens count is read on the device
+        new = inputs(500, 128, 2000, 11, True, masked)
+        x2.copy_(new[0]), to.copy_(new[2])
+        graph.replay()
+        Definition(x2, w, to, b, dloss).check(out, grads, BF, f"graph {masked}")
+    hd.device_status()
+    del graph
+
+
+def test_refusals(handle):
+    x, w, target, b, dloss = inputs(10, 64, 100, 1, True)
+    lse = dloss.clone()
+    for call, what in ((lambda: vocab.loss(handle, x.float(), w, target), "bfloat16"),
+                       (lambda: vocab.loss(handle, x, w.half(), target), "bfloat16"),
+                       (lambda: vocab.loss(handle, x[:, :63], w, target), "63 columns"),
+                       (lambda: vocab.loss(handle, x.T, w, target), "unit stride|columns"),
+                       (lambda: vocab.loss(handle, x, w, target.int()), "int64"),
+                       (lambda: vocab.loss(handle, x, w, target[:9]), "int64"),
+                       (lambda: vocab.loss(handle, x, w, target, bias=b.to(BF)), "float32"),
+                       (lambda: vocab.loss(handle, x, w.cpu(), target), "device"),
+                       (lambda: vocab.loss_backward(handle, dloss[:9], x, w, target, lse), "dloss"),
+                       (lambda: vocab.loss_backward(handle, dloss, x, w, target, lse.double()), "lse"),
+                       (lambda: vocab.loss_backward(handle, dloss, x, w, target, lse, dtype=torch.float16), "dtype")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    with pytest.raises(stq.StqError) as e:
+        vocab.loss(handle, x, w[:0], target)
+    assert e.value.code == -6
+    L, p = vocab._lib(), lambda t: t.data_ptr()      # noqa: E731
+    out = torch.empty(10, device="cuda")
+    assert L.stq_vocab_loss(handle._h, p(x), 64, p(w), 64, None, p(target), -100, 10, 100, 64, p(out), p(out), None) == -5
+    assert L.stq_vocab_loss(handle._h, p(x), 63, p(w), 64, None, p(target), -100, 10, 100, 64, p(out), p(lse), None) == -9
+    assert L.stq_vocab_loss(handle._h, p(x), 64, p(w), 64, None, None, -100, 10, 100, 64, p(out), p(lse), None) == -1
+    assert L.stq_vocab_loss(handle._h, p(x), 64, p(w), 64, None, p(target), -100, 262145, 100, 64, p(out), p(lse), None) == -12
+    assert L.stq_vocab_loss_backward(handle._h, p(dloss), p(x), 64, p(w), 64, None, p(target), -100, p(lse), 10, 100, 64, p(x), 64, None, 0, 0,
+                                     None, None) == -5

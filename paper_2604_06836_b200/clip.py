@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+from array import array
 from typing import NamedTuple, Optional, Sequence
 
 import torch
@@ -17,13 +18,10 @@ import torch
 from . import stq
 from .q8 import _F32, _empty, _On, _raw_stream
 
+_address_of, _length_of, _device_of = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device
 _DT = {torch.float32: stq.GRAD_F32, torch.bfloat16: stq.GRAD_BF16, torch.float16: stq.GRAD_F16}
 
 _fn = None
-
-
-class _Grad(C.Structure):
-    _fields_ = [("grad", C.c_uint64), ("out", C.c_uint64), ("numel", C.c_uint64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 def _lib() -> C.CDLL:
@@ -65,30 +63,37 @@ def _refuse(name, t, dev):
 
 
 def _table(grads, out, dev):
-    """Rows of the call as one array of integers (the layout of stq_grad), and their number."""
-    rows, n, get = [], 0, _DT.get
-    add = rows.extend
-    for k, g in enumerate(grads):
-        if g is None:
-            continue
-        dt = get(getattr(g, "dtype", None))
-        if dt is None or g.get_device() != dev or not (g.is_contiguous() or _dense(g)):
-            _refuse("gradients", g, dev)
-        at = g.data_ptr()
-        if out is None:
-            add((at, at, g.numel(), dt | dt << 32))
-        else:
-            o = out[k]
-            odt = get(getattr(o, "dtype", None))
-            if odt is None or o.get_device() != dev:
+    """Rows of the call as one array of integers (the layout of stq_grad), and their number.  (A model has hundreds of tensors: one
+    pass of the interpreter for each thing to know of them, and what is wrong is found out only once something is.)"""
+    if any(g is None for g in grads):
+        out = None if out is None else [o for g, o in zip(grads, out) if g is not None]
+        grads = [g for g in grads if g is not None]
+    n = len(grads)
+    try:
+        types = [_DT[g.dtype] for g in grads]
+        if any(d != dev for d in map(_device_of, grads)) or not all(g.is_contiguous() or _dense(g) for g in grads):
+            raise KeyError
+    except (KeyError, AttributeError):
+        for g in grads:
+            if not isinstance(g, torch.Tensor) or g.dtype not in _DT or g.get_device() != dev or not _dense(g):
+                _refuse("gradients", g, dev)
+        raise
+    rows = array("Q", bytes(32 * n))
+    rows[0::4] = rows[1::4] = array("Q", map(_address_of, grads))
+    rows[2::4] = array("Q", map(_length_of, grads))
+    if out is not None:
+        for g, o, dt in zip(grads, out, types):
+            if not isinstance(o, torch.Tensor) or o.get_device() != dev or o.dtype not in _DT:
                 _refuse("results", o, dev)
-            if o.shape != g.shape or (o.stride() != g.stride() and not (g.is_contiguous() and o.is_contiguous())):
+            if o.shape != g.shape or not (g.is_contiguous() and o.is_contiguous() or o.stride() == g.stride()):
                 raise ValueError("a result has the shape and strides of its gradient")
-            if odt != dt and odt != stq.GRAD_F32:
+            if _DT[o.dtype] != dt and o.dtype is not _F32:
                 raise ValueError("a result has the type of its gradient or float32")
-            add((at, o.data_ptr(), g.numel(), dt | odt << 32))
-        n += 1
-    return (C.c_uint64 * len(rows))(*rows), n
+        rows[1::4] = array("Q", map(_address_of, out))
+        rows[3::4] = array("Q", [dt | _DT[o.dtype] << 32 for dt, o in zip(types, out)])
+    else:
+        rows[3::4] = array("Q", [dt | dt << 32 for dt in types])
+    return rows, n
 
 
 def _scalar(name, t, dev):
@@ -108,7 +113,7 @@ def _call(fn, what, handle, grads, out, max_norm, inv_scale, found_inf, eps) -> 
     rows, n = _table(grads, out, dev)
     both = _empty((2,), (1,), dtype=_F32, device=f"cuda:{dev}")
     at = both.data_ptr()
-    rc = fn(handle._h, rows, n, inv, max_norm, eps, at, at + 4, flag, _raw_stream(dev))
+    rc = fn(handle._h, rows.buffer_info()[0] if n else None, n, inv, max_norm, eps, at, at + 4, flag, _raw_stream(dev))
     if rc:
         handle._check(rc, what)
     return Norm(both[0], both[1])
@@ -135,6 +140,9 @@ def clip_grads(handle: stq.Handle, grads: Sequence[Optional[torch.Tensor]], max_
         with _On(stream, (*grads, *(out or ()), inv_scale, found_inf)):
             return clip_grads(handle, grads, max_norm, inv_scale=inv_scale, found_inf=found_inf, eps=eps, out=out)
     r = _call((_fn or _lib()).stq_grad_clip, "stq_grad_clip", handle, grads, out, max_norm, inv_scale, found_inf, eps)
-    written = [t for g, t in zip(grads, grads if out is None else out) if g is not None and not t.is_inference()]
-    torch.autograd.graph.increment_version(written)      # (written behind torch's back)
+    # (written behind torch's back)
+    written = [t for g, t in zip(grads, grads if out is None else out) if g is not None]
+    if any(map(torch.Tensor.is_inference, written)):
+        written = [t for t in written if not t.is_inference()]
+    torch.autograd.graph.increment_version(written)
     return r

@@ -194,6 +194,14 @@ __device__ __forceinline__ void scale_piece(const Chunk& c, int64_t from, const 
   for (int i = 0; i < kPer; ++i) x[i] = __fmul_rn(number<TYPE>(v, i), f);
   const uint64_t to = c.out + from * kSize;
   if (from >= 0 && from + kPer <= (int64_t)c.numel && (to & 15) == 0) {
+    if constexpr (OUT == STQ_GRAD_F32 && kPer == 8) {      // (32 bytes at once: halves of sectors cost as much as whole ones)
+      if ((to & 31) == 0) {
+        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]),
+                     "f"(x[5]), "f"(x[6]), "f"(x[7])
+                     : "memory");
+        return;
+      }
+    }
     if constexpr (OUT == STQ_GRAD_F32) {
 #pragma unroll
       for (int i = 0; i < kPer; i += 4)

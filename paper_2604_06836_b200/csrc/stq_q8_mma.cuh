@@ -260,6 +260,32 @@ __device__ __forceinline__ void store_block(const CUtensorMap* map, int x, int y
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
+// The same through one of two places in shared memory, 4096 bytes each, in turn (n counts the blocks), so that a copy has the time
+// of a whole block to read its own.  ADD: added to what is there (fp32).
+template <class O, bool ADD = false>
+__device__ __forceinline__ void put_block(const CUtensorMap* map, int x, int y, const float (&v)[128 / sizeof(O)], int lane, uint32_t stages, uint32_t& n) {
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+  const uint32_t stage = stages + (n++ & 1) * 4096;
+  uint32_t w[32];
+  block_words<O>(v, w);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(w[4 * i]),
+                 "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                 : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    if constexpr (ADD)
+      asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(stage)
+                   : "memory");
+    else
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(stage)
+                   : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
 // Before a warp ends (or reuses its shared memory for anything else): its copies are done.
 __device__ __forceinline__ void store_blocks_done(int lane) {
   if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");

@@ -16,6 +16,7 @@ struct VocabRows {
   const uint32_t* count;      // on the device, or null: `rows`
   const uint32_t* token;      // row -> token, or null: the same
   const int32_t* row;         // token -> row or -1, or null
+  const float* scale;         // gradients: what they are multiplied with at the end (GatherArgs), on the device
 };
 
 // What the products of hidden states and the matrix need.
@@ -44,6 +45,11 @@ struct GatherArgs {
   uint32_t* count;
   uint32_t* token;
   int32_t* row;
+  // Gradients: the largest |dloss| of the tokens that count (1 if that is 0 or infinite).  The gradients of the logits are formed for
+  // dloss / scale: for a mean over tokens that is 1, and the 1 of p - 1 then has no rounding in bf16.
+  const float* dloss;
+  float* scale;
+  bool aligned;               // (set by the launch) rows are whole 16-byte pieces
 };
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
 
@@ -60,13 +66,14 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, float2* part, i
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
                                 float* lse, cudaStream_t stream);
 
-// Gradients of the logits of entries [v0, v1), p[plane][row][v - v0]: `planes` bf16 numbers (1 or 3) whose sum they are,
-// plane i at row i * most; pitch ldp, a multiple of 64.  dbias: sums over 32 rows each, [most / 32][ldp], or null.
+// Gradients of the logits of entries [v0, v1), divided by scale, p[plane][row][v - v0]: `planes` bf16 numbers (1 or 3) whose sum they are,
+// plane i at row i * most; pitch ldp, a multiple of 64.  dbias: sums over 32 rows each, [most / 32] of pitch ldb, or null.
 struct VocabGradOut {
   void* p;
   size_t ldp;
   int planes;
   float* dbias;
+  size_t ldb;
   const float* lse;
   const float* dloss;
 };
@@ -74,7 +81,7 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape s, uint32_t v0, 
                                  cudaStream_t stream);
 
 // ---- gradients (stq_vocab_grad.cu) ---------------------------------------------------------------------------------
-// dw[v0 + i][:] = sum over rows of p[row][i] x[row][:].  part: vocab_dw_partial() floats.
+// dw[v0 + i][:] = scale * sum over rows of p[row][i] x[row][:].  part: vocab_dw_partial() floats.
 struct VocabDw {
   VocabRows r;
   const void* p;
@@ -106,8 +113,8 @@ struct VocabDx {
 };
 size_t vocab_dx_rows(uint32_t most, size_t ldd);      // rows of planes that suffice
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream);
-// dx of all tokens (zero for those that do not count) from the planes.
+// dx of all tokens (zero for those that do not count): scale * the sum of the planes.
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream);
-cudaError_t launch_vocab_dbias(const float* part, size_t ldp, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream);
+cudaError_t launch_vocab_dbias(const float* part, size_t ldb, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream);
 
 }  // namespace stq

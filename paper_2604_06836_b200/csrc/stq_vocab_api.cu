@@ -32,6 +32,7 @@ struct Rows {
   size_t ldx, ldw;
   uint32_t *count, *token;
   int32_t* row;
+  float* scale;
 
   Rows(const VocabArgs& a, const void* x_, size_t ldx_, bool backward) {
     // For a loss of up to one tile of tokens there is nothing to gain from leaving some out.  (For dw there is: what a token
@@ -46,6 +47,7 @@ struct Rows {
     count = gather ? m.take<uint32_t>(1) : nullptr;
     token = gather ? m.take<uint32_t>(most) : nullptr;
     row = gather ? m.take<int32_t>(a.t) : nullptr;
+    scale = gather ? m.take<float>(1) : nullptr;
     w = pitch_w ? m.take<uint16_t>((size_t)a.v * ldw) : nullptr;
   }
 };
@@ -53,14 +55,16 @@ struct Rows {
 uint32_t most_rows(uint32_t t) { return t <= 128 ? 128 : (uint32_t)up(t, 256); }
 
 // Sets a.r (and the aligned copy of w) up on the stream.
-cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, bool with_w, cudaStream_t s, int* launches) {
+// (dloss: for the gradients)
+cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, const float* dloss, bool with_w, cudaStream_t s, int* launches) {
   const uint32_t most = most_rows(a.t);
-  a.r = {x, a.t > 1 ? ldx : up(a.d, 8), a.t, most, nullptr, nullptr, nullptr};
+  a.r = {x, a.t > 1 ? ldx : up(a.d, 8), a.t, most, nullptr, nullptr, nullptr, nullptr};
   if (r.gather) {
-    const GatherArgs g = {x, ldx, a.t, a.d, most, a.target, a.ignore, r.x, r.ldx, r.count, r.token, r.row};
+    const GatherArgs g = {x, ldx, a.t, a.d, most, a.target, a.ignore, r.x, r.ldx, r.count, r.token, r.row, dloss,
+                          dloss ? r.scale : nullptr, false};
     const cudaError_t e = launch_vocab_gather(g, s);
     if (e != cudaSuccess) return e;
-    a.r = {r.x, r.ldx, most, most, r.count, r.token, r.row};
+    a.r = {r.x, r.ldx, most, most, r.count, r.token, r.row, r.scale};
     ++*launches;
   }
   if (r.pitch_w && with_w) {
@@ -132,7 +136,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     b.target = target + t0;
     const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
     int launches = 2;
-    STQ_CUDA(h, prepare_rows(b, r, xb, ldx, t0 == 0, s, &launches));
+    STQ_CUDA(h, prepare_rows(b, r, xb, ldx, nullptr, t0 == 0, s, &launches));
     STQ_CUDA(h, launch_vocab_parts(b, shape, part, h->sm_count, h->d_err, s));
     STQ_CUDA(h, launch_vocab_finish(b, xb, ldx, part, parts, loss + t0, lse + t0, s));
     h->launches += launches;
@@ -177,7 +181,11 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   const size_t fit = kPieceBytes / ((size_t)most * 2 * planes) / 256 * 256, tiles = up(v, 256) / 256, widest = (fit < 256 ? 256 : fit) / 256;
   const size_t pieces = (tiles + widest - 1) / widest;
   const uint32_t cols = (uint32_t)((tiles + pieces - 1) / pieces * 256 < v ? (tiles + pieces - 1) / pieces * 256 : v);
-  VocabGradOut o = {nullptr, up(cols, 64), planes, nullptr, lse, dloss};
+  VocabGradOut o = {nullptr, up(cols, 64), planes, nullptr, 0, lse, dloss};
+  // sums for dbias: of the whole vocabulary, if that is not too much, and joined once; else piece by piece
+  const size_t db_rows = most / 32;
+  const bool db_once = db_rows * up(v, 64) * 4 <= kPieceBytes / 4;
+  o.ldb = db_once ? up(v, 64) : o.ldp;
   VocabDw gw = {};
   gw.ldp = o.ldp;
   gw.cols = cols; gw.d = d;
@@ -201,27 +209,29 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
     if (p > partial) partial = p;
   }
   Arena m;
-  float* part = nullptr;
+  float *part = nullptr, *db_part = nullptr;
   for (int pass = 0; pass < 2; ++pass) {
     m.at = 0;
     r.place(m, a, most);
     o.p = m.take<uint16_t>((size_t)most * planes * o.ldp);
-    o.dbias = dbias ? m.take<float>(most / 32 * o.ldp) : nullptr;
+    db_part = dbias ? m.take<float>(db_rows * o.ldb) : nullptr;
     part = partial ? m.take<float>(partial) : nullptr;
     gx.planes = dx ? m.take<float>(gx.plane_rows * gx.ldd) : nullptr;
     if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
   }
   int launches = 0;
-  STQ_CUDA(h, prepare_rows(a, r, x, ldx, true, s, &launches));
+  STQ_CUDA(h, prepare_rows(a, r, x, ldx, dloss, true, s, &launches));
   gw.r = gx.r = a.r;
   gw.p = gx.p = o.p;
   gx.ldw = a.ldw;
   for (uint32_t v0 = 0; v0 < v; v0 += cols) {
     const uint32_t n = v - v0 < cols ? v - v0 : cols;
+    o.dbias = db_part && db_once ? db_part + v0 : db_part;
     STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
     ++launches;
-    if (dbias) {
-      STQ_CUDA(h, launch_vocab_dbias(o.dbias, o.ldp, a.r, n, dbias + v0, s));
+    const bool all = v0 + n == v;
+    if (dbias && (!db_once || all)) {
+      STQ_CUDA(h, db_once ? launch_vocab_dbias(db_part, o.ldb, a.r, v, dbias, s) : launch_vocab_dbias(db_part, o.ldb, a.r, n, dbias + v0, s));
       ++launches;
     }
     if (dw) {

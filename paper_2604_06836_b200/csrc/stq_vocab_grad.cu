@@ -33,6 +33,7 @@ struct GradArgs {
   uint32_t n, bn;                      // columns of the result, and of a tile
   uint32_t units;
   // dw
+  const float* scale;
   void* out;
   size_t ldo;
   uint32_t m;                          // rows of the result
@@ -52,30 +53,13 @@ struct GradShape {
   static constexpr int kNB = BN / CG < 64 ? 64 : BN / CG;         // columns that are copied: whole 128-byte rows
   static constexpr int kA = 128 * kDepth * 2, kB = kDepth * kNB * 2;
   static constexpr int kStage = kA * PARTS + kB;
-  static constexpr int kFit = (204 * 1024) / kStage;
+  static constexpr int kOut = 2 * 4096;                           // a writing warp's blocks on their way out
+  static constexpr int kFit = (192 * 1024) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
   static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
-  static constexpr int kSmem = kStages * kStage + 4 * kStageBytes + 1024;
+  static constexpr int kSmem = kStages * kStage + 4 * kOut + 1024;
 };
-
-// A warp's block of 32 rows x 32 columns of fp32, added to memory by a tensor copy.
-__device__ __forceinline__ void add_block(const CUtensorMap* map, int x, int y, const float (&v)[32], int lane, uint32_t stage) {
-  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(stage + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(__float_as_uint(v[4 * i])),
-                 "r"(__float_as_uint(v[4 * i + 1])), "r"(__float_as_uint(v[4 * i + 2])), "r"(__float_as_uint(v[4 * i + 3]))
-                 : "memory");
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  __syncwarp();
-  if (lane == 0) {
-    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(stage)
-                 : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-  }
-}
 
 // One work item: tile (its row and column), stages [k0, k1) of its sum, and where the result goes.
 struct Item {
@@ -219,10 +203,12 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     }
   } else {
     const int quad = warp & 3;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + quad * kStageBytes;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + quad * S::kOut;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
-    uint32_t n = 0;
+    static_assert(S::kOut >= 32 * kStageRow, "room for a ragged block");
+    uint32_t n = 0, puts = 0;
     constexpr int kC = 128 / sizeof(O);
+    const float scale = DW ? *a.scale : 1.f;
     items([&](const Item& w) {
       const uint32_t row = w.row + 128 * rank + quad * 32, running = tmem + lanes + 2 * BN;
       const uint32_t end = min(a.bn, a.n - w.col);
@@ -239,6 +225,8 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
       auto emit = [&](uint32_t c, uint32_t over, float(&v)[kC]) {
         const uint32_t col = w.col + c;
         if constexpr (DW) {
+#pragma unroll
+          for (int i = 0; i < kC; ++i) v[i] = __fmul_rn(v[i], scale);
           O* out = static_cast<O*>(a.out) + (size_t)row * a.ldo + col;
           const int rows = row >= a.m ? 0 : (int)min(32u, a.m - row);
           if (w.share >= 0) {
@@ -248,16 +236,16 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
           } else if (!a.aligned) {
             if (col < a.n) store_ragged(out, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col), lane, raw + (stage - smem_addr(raw)));
           } else if (rows > 0) {
-            store_block<O>(&map_o, (int)col, (int)row, v, lane, stage);
+            put_block<O>(&map_o, (int)col, (int)row, v, lane, stage, puts);
           }
         } else {
           const int y = (int)((uint32_t)w.share * ranges.tiles_m * 128 * CG + row);
           if (add) {
 #pragma unroll
             for (int i = 0; i < kC; ++i) v[i] = i < (int)over ? 0.f : v[i];
-            add_block(&map_o, (int)col, y, v, lane, stage);
+            put_block<float, true>(&map_o, (int)col, y, v, lane, stage, puts);
           } else {
-            store_block<float>(&map_o, (int)col, y, v, lane, stage);
+            put_block<float>(&map_o, (int)col, y, v, lane, stage, puts);
           }
         }
       };
@@ -317,45 +305,63 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
   }
 }
 
-// dx of eight tokens to a CTA, eight columns to a thread: the planes of a row, added in order.
+// dx of up to eight tokens to a CTA, eight columns to a thread: the planes of a row, added in order.  (What does not depend on the planes
+// was there before the kernel that writes them began: it is worked out while that one still runs.)
 __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, size_t ldd, uint32_t plane_rows, const uint32_t* count_at, uint32_t rows,
                                                         const int32_t* row_of, uint32_t tile_m, uint32_t bn, uint32_t first, uint32_t last,
-                                                        uint32_t units, uint32_t t, uint32_t d, __nv_bfloat16* dx, size_t lddx, bool aligned) {
-  __shared__ uint32_t shares[2][kMaxTilesN];
-  __shared__ uint32_t tile_row[2];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t count = count_at ? *count_at : rows, tiles_n = (d + bn - 1) / bn, t0 = blockIdx.x * 8;
-  const Ranges r0(count, tile_m, tiles_n, first, units, plane_rows), r1(count, tile_m, tiles_n, last, units, plane_rows);
-  // (eight tokens that follow one another have rows in at most two tiles)
-  auto row = [&](uint32_t i) { return i >= t ? -1 : row_of ? row_of[i] : (int32_t)i; };
-  if (threadIdx.x == 0) {
-    uint32_t lo = 0xffffffffu;
-    for (uint32_t i = t0; i < t0 + 8; ++i)
-      if (row(i) >= 0) lo = min(lo, (uint32_t)row(i) / tile_m);
-    tile_row[0] = lo;
+                                                        uint32_t units, const float* scale_at, uint32_t t, uint32_t each, uint32_t d, __nv_bfloat16* dx,
+                                                        size_t lddx, bool aligned) {
+  __shared__ uint8_t shares[2][kMaxTilesN];
+  __shared__ int32_t row[8];
+  __shared__ uint32_t lowest;
+  const uint32_t count = count_at ? *count_at : rows, tiles_n = (d + bn - 1) / bn, t0 = blockIdx.x * each;
+  const float scale = *scale_at;
+  // (tokens that follow one another have rows in at most two tiles)
+  if (threadIdx.x < 32) {
+    const uint32_t i = t0 + threadIdx.x;
+    const int32_t r = threadIdx.x >= each || i >= t ? -1 : row_of ? row_of[i] : (int32_t)i;
+    if (threadIdx.x < 8) row[threadIdx.x] = r;
+    const uint32_t lo = __reduce_min_sync(0xffffffffu, r < 0 ? 0xffffffffu : (uint32_t)r / tile_m);
+    if (threadIdx.x == 0) lowest = lo;
   }
   __syncthreads();
-  const uint32_t lo = tile_row[0];
-  if (lo != 0xffffffffu)
+  const uint32_t lo = lowest;
+  if (lo != 0xffffffffu) {
+    const Ranges r0(count, tile_m, tiles_n, first, units, plane_rows), r1(count, tile_m, tiles_n, last, units, plane_rows);
     for (uint32_t i = threadIdx.x; i < 2 * tiles_n; i += 256) {
       const uint32_t m = lo + i / tiles_n, n = i % tiles_n;
-      if (m < r0.tiles_m) shares[i / tiles_n][n] = max(r0.shares(n * r0.tiles_m + m), r1.shares(n * r0.tiles_m + m));
+      if (m < r0.tiles_m) shares[i / tiles_n][n] = (uint8_t)max(r0.shares(n * r0.tiles_m + m), r1.shares(n * r0.tiles_m + m));
     }
+  }
   __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t per_row = (d + 7) / 8;
-  for (uint32_t i = threadIdx.x; i < 8 * per_row; i += 256) {
-    const uint32_t tok = t0 + i / per_row, c = i % per_row * 8;
+  const size_t plane = (size_t)((count + tile_m - 1) / tile_m) * tile_m * ldd;
+  for (uint32_t i = threadIdx.x; i < each * per_row; i += 256) {
+    const uint32_t k = i / per_row, tok = t0 + k, c = i % per_row * 8;
     if (tok >= t) break;
-    const int32_t at = row(tok);
+    const int32_t at = row[k];
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (at >= 0) {      // (a tile's columns are a multiple of 16: the eight lie in one tile)
       const uint32_t n = shares[at / tile_m - lo][c / bn];
-      for (uint32_t p = 0; p < n; ++p) {
-        const float* from = planes + ((size_t)p * r0.tiles_m * tile_m + at) * ldd + c;
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(from)), v = __ldcg(reinterpret_cast<const float4*>(from + 4));
-        s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-        s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+      const float* from = planes + (size_t)at * ldd + c;
+      for (uint32_t p = 0; p < n; p += 4, from += 4 * plane) {
+        float4 u[4], v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (p + j < n) {
+            u[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane));
+            v[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane + 4));
+          }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (p + j < n) {
+            s[0] += u[j].x; s[1] += u[j].y; s[2] += u[j].z; s[3] += u[j].w;
+            s[4] += v[j].x; s[5] += v[j].y; s[6] += v[j].z; s[7] += v[j].w;
+          }
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] *= scale;
     }
     __nv_bfloat16* to = dx + (size_t)tok * lddx + c;
     if (aligned && c + 8 <= d) {
@@ -369,19 +375,21 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, siz
 }
 
 // Column sums of the partial sums of 32 rows each: 32 columns to a CTA, every eighth row to a warp.
-__global__ void __launch_bounds__(256) dbias_kernel(const float* part, size_t ldp, const uint32_t* count_at, uint32_t rows, uint32_t cols, float* out) {
+__global__ void __launch_bounds__(256) dbias_kernel(const float* part, size_t ldb, const uint32_t* count_at, uint32_t rows, const float* scale,
+                                                    uint32_t cols, float* out) {
   __shared__ float sums[8][33];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t groups = ((count_at ? *count_at : rows) + 31) / 32, c = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (c < cols)
-    for (uint32_t g = warp; g < groups; g += 8) s += __ldcg(part + (size_t)g * ldp + c);
+#pragma unroll 4
+    for (uint32_t g = warp; g < groups; g += 8) s += __ldcg(part + (size_t)g * ldb + c);
   sums[warp][lane] = s;
   __syncthreads();
   if (warp != 0 || c >= cols) return;
   for (int i = 1; i < 8; ++i) s += sums[i][lane];
-  out[c] = s;
+  out[c] = s * *scale;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -435,6 +443,7 @@ cudaError_t launch(const VocabRows& r, const void* p, size_t ldp, const void* b,
   g.count = r.count;
   g.rows = r.rows;
   g.most = r.most;
+  g.scale = r.scale;
   g.err = err;
   const uint64_t most = sms / CG;
   g.units = (uint32_t)(items < most ? items : most);
@@ -519,13 +528,17 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
 
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream) {
   const DxShape s = dx_shape(a);
-  return launch_with(dx_finish_kernel, dim3((t + 7) / 8), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
-                     a.r.row, (uint32_t)(128 * s.cg), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), t, a.d,
+  // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
+  uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
+  if (each > 8) each = 8;
+  return launch_with(dx_finish_kernel, dim3((t + each - 1) / each), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
+                     a.r.row, (uint32_t)(128 * s.cg), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), a.r.scale, t, each, a.d,
                      static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2));
 }
 
-cudaError_t launch_vocab_dbias(const float* part, size_t ldp, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream) {
-  return launch_with(dbias_kernel, dim3((cols + 31) / 32), dim3(256), 0, 1, true, stream, part, ldp, r.count, r.rows, cols, dbias);
+cudaError_t launch_vocab_dbias(const float* part, size_t ldb, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream) {
+  return launch_with(dbias_kernel, dim3((cols + 31) / 32), dim3(256), 0, 1, true, stream, part, ldb, r.count, r.rows, r.scale, cols,
+                     dbias);
 }
 
 }  // namespace stq

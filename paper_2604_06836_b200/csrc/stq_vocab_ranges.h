@@ -23,11 +23,13 @@ struct Ranges {
     if (S == 0) return;
     // so long a range that no tile has more units than there are planes
     const uint32_t planes = plane_rows / (tiles_m * tile_m), least = planes > 2 ? (k + planes - 2) / (planes - 1) : k;
-    const uint64_t most = S / least;
+    const uint64_t most = ratio(S, least);
     U = (uint32_t)(units < most ? units : most);
   }
-  STQ_BOTH uint64_t begin(uint32_t u) const { return u * S / U; }
-  STQ_BOTH uint32_t unit_of(uint64_t s) const { return (uint32_t)(((s + 1) * U - 1) / S); }
+  STQ_BOTH uint64_t begin(uint32_t u) const { return ratio(u * S, U); }
+  STQ_BOTH uint32_t unit_of(uint64_t s) const { return (uint32_t)ratio((s + 1) * U - 1, S); }
+  // (a division of 64 bits takes a GPU ten times as long)
+  STQ_BOTH static uint64_t ratio(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
   STQ_BOTH uint32_t shares(uint32_t tile) const {
     return unit_of((uint64_t)tile * ksteps + ksteps - 1) - unit_of((uint64_t)tile * ksteps) + 1;
   }

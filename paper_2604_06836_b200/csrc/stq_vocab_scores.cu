@@ -29,20 +29,40 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // ---- rows ----------------------------------------------------------------------------------------------------------
-constexpr int kGatherRows = 32;        // tokens to a CTA
+constexpr int kGatherRows = 16;        // tokens to a CTA
+constexpr int kScan = 8;               // targets that a thread has on the way
 
 // Every CTA counts the targets before its tokens and in all, so that nothing has to be passed between CTAs.
 __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ uint32_t sums[2][8];
+  __shared__ float tops[8];
   __shared__ int32_t where[kGatherRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t t0 = blockIdx.x * kGatherRows;
   uint32_t before = 0, all = 0;
-  for (uint32_t i = threadIdx.x; i < a.t; i += 256) {
-    const uint32_t counts = a.target[i] != a.ignore;
-    all += counts;
-    before += i < t0 ? counts : 0;
+  float top = 0.f;
+  const bool scan = a.scale && blockIdx.x == 0;
+  for (uint32_t i0 = threadIdx.x; i0 < a.t; i0 += 256 * kScan) {
+    int64_t to[kScan];
+    float g[kScan];
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      const uint32_t i = i0 + 256 * j;
+      to[j] = i < a.t ? __ldg(a.target + i) : a.ignore;
+      g[j] = scan && i < a.t ? __ldg(a.dloss + i) : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < kScan; ++j) {
+      const uint32_t counts = to[j] != a.ignore;
+      all += counts;
+      before += i0 + 256 * j < t0 ? counts : 0;
+      if (counts) top = fmaxf(top, fabsf(g[j]));
+    }
+  }
+  if (scan) {
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (lane == 0) tops[warp] = top;
   }
   before = __reduce_add_sync(0xffffffffu, before);
   all = __reduce_add_sync(0xffffffffu, all);
@@ -50,23 +70,44 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
   __syncthreads();
   before = all = 0;
   for (int i = 0; i < 8; ++i) { before += sums[0][i]; all += sums[1][i]; }
+  if (scan && threadIdx.x == 0) {
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, tops[i]);
+    *a.scale = top > 0.f && top < INFINITY ? top : 1.f;
+  }
   if (warp == 0) {
     const uint32_t t = t0 + lane;
-    const bool counts = t < a.t && a.target[t] != a.ignore;
+    const bool mine = lane < kGatherRows && t < a.t, counts = mine && a.target[t] != a.ignore;
     const uint32_t mask = __ballot_sync(0xffffffffu, counts);
     const int32_t to = counts ? (int32_t)(before + __popc(mask & ((1u << lane) - 1))) : -1;
-    where[lane] = to;
-    if (t < a.t) a.row[t] = to;
+    if (lane < kGatherRows) where[lane] = to;
+    if (mine) a.row[t] = to;
     if (counts) a.token[to] = t;
     if (blockIdx.x == 0 && lane == 0) *a.count = all;
   }
   __syncthreads();
-  const uint32_t per_row = (a.d + 255) / 256;
   const uint16_t* x = static_cast<const uint16_t*>(a.x);
   uint16_t* out = static_cast<uint16_t*>(a.out);
-  for (uint32_t i = warp; i < kGatherRows * per_row; i += 8) {
-    const uint32_t r = i / per_row, part = i - r * per_row;
-    if (where[r] >= 0) copy_row_part(x + (size_t)(t0 + r) * a.ldx, a.d, part * 256, out + (size_t)where[r] * a.ldo, lane);
+  if (a.aligned) {
+    const uint32_t per_row = a.d / 8;      // 16-byte pieces
+    for (uint32_t i0 = threadIdx.x; i0 < kGatherRows * per_row; i0 += 256 * 4) {
+      uint4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t i = i0 + 256 * j, r = i / per_row;
+        if (i < kGatherRows * per_row && where[r] >= 0) v[j] = __ldg(reinterpret_cast<const uint4*>(x + (size_t)(t0 + r) * a.ldx) + (i - r * per_row));
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t i = i0 + 256 * j, r = i / per_row;
+        if (i < kGatherRows * per_row && where[r] >= 0) *(reinterpret_cast<uint4*>(out + (size_t)where[r] * a.ldo) + (i - r * per_row)) = v[j];
+      }
+    }
+  } else {
+    const uint32_t per_row = (a.d + 255) / 256;
+    for (uint32_t i = warp; i < kGatherRows * per_row; i += 8) {
+      const uint32_t r = i / per_row, part = i - r * per_row;
+      if (where[r] >= 0) copy_row_part(x + (size_t)(t0 + r) * a.ldx, a.d, part * 256, out + (size_t)where[r] * a.ldo, lane);
+    }
   }
   // the rest of the last tile: what is multiplied with zeros must be finite
   const uint32_t end = min(a.most, (all + 255) / 256 * 256);
@@ -88,8 +129,9 @@ struct ScoreArgs {
   int64_t ignore;
   const float* lse;
   const float* dloss;
+  const float* scale;
   float* dbias;
-  size_t ldp;
+  size_t ldb;
   int* err;
 };
 
@@ -99,8 +141,8 @@ template <int CG, int BN, int PLANES>  // PLANES = 0: the loss
 struct ScoreShape {
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
-  static constexpr int kOut = PLANES ? kWriters * kStageBytes : 0;
-  static constexpr int kFit = (225 * 1024 - kOut) / kStage;
+  static constexpr int kOut = PLANES ? kWriters * 2 * 4096 : 0;
+  static constexpr int kFit = ((PLANES ? 224 : 192) * 1024 - kOut) / kStage;      // (the loss leaves room for CTAs of the kernel after it)
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kSmem = kStages * kStage + kOut + 1024;
 };
@@ -156,6 +198,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   mma_fence_after();
   const uint32_t tmem = tmem_slot;
   const uint32_t count = a.count ? *a.count : a.rows;
+  const float scale = PLANES > 0 ? *a.scale : 1.f;
   const uint32_t tiles_m = (count + 128 * CG - 1) / (128 * CG), tiles = tiles_m * a.tiles_n;
 
   bool ok = true;
@@ -201,7 +244,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   } else {
     const int quad = warp & 3, half = (warp - 2) / 4;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
-    uint32_t n = 0;
+    uint32_t n = 0, puts = 0;
     for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
       const uint32_t acc = n & 1, from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN + half * (BN / 2);
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
@@ -216,67 +259,86 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           const int64_t to = a.target[t];
           real = to != a.ignore;
           if (real) {
-            g = a.dloss[t];
+            g = __fdiv_rn(a.dloss[t], scale);
             lse = a.lse[t];
             if (to >= col0 && to < col0 + BN / 2) hit = (int32_t)(to - col0);
           }
         }
       }
+      float bias[BN / 64];      // of column 32 i + lane
+      if (a.bias) {
+#pragma unroll
+        for (int i = 0; i < BN / 64; ++i) bias[i] = col0 + 32 * i + lane < a.v1 ? __ldg(a.bias + col0 + 32 * i + lane) : 0.f;
+      }
       ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
       if (!(ok = all_of<32 * kWriters>(ok))) break;       // (the writing warps leave together)
       mma_fence_after();
-      auto add_bias = [&](float(&v)[32], uint32_t col) {
+      auto add_bias = [&](float(&v)[32], float mine) {
         if (a.bias) {
-          const float mine = col + lane < a.v1 ? __ldg(a.bias + col + lane) : 0.f;
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, mine, i));
         }
       };
       if constexpr (PLANES == 0) {
         float m = -INFINITY, s = 0.f;
-#pragma unroll 1
+#pragma unroll
         for (int c = 0; c < BN / 2; c += 32) {
           const uint32_t col = col0 + c;
           if (col >= a.v1) break;
           float v[32];
           load_block(from + c, v);
-          add_bias(v, col);
+          add_bias(v, bias[c / 32]);
           if (col + 32 > a.v1) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (col + i >= a.v1) v[i] = -INFINITY;
           }
-          float top = m;
+          float tops[4] = {m, m, m, m};
 #pragma unroll
-          for (int i = 0; i < 32; ++i) top = fmaxf(top, v[i]);
+          for (int i = 0; i < 32; ++i) tops[i & 3] = fmaxf(tops[i & 3], v[i]);
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
           // (nothing but -inf so far, or NaN, which fmaxf passes over: measured from 0 they add 0 or NaN)
           // (subtracted before it is scaled: a logit may be the lowest number there is)
           const float ref = top == -INFINITY ? 0.f : top;
           s = s * ex2(__fmul_rn(__fadd_rn(m, -ref), kLog2e));
-          float more[4] = {0.f, 0.f, 0.f, 0.f};
+          float2 more[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          const float2 less = make_float2(-ref, -ref), scale2 = make_float2(kLog2e, kLog2e);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) more[i & 3] = __fadd_rn(more[i & 3], ex2(__fmul_rn(__fadd_rn(v[i], -ref), kLog2e)));
-          s = __fadd_rn(s, __fadd_rn(__fadd_rn(more[0], more[1]), __fadd_rn(more[2], more[3])));
+          for (int i = 0; i < 32; i += 2) {
+            const float2 e = __fmul2_rn(__fadd2_rn(make_float2(v[i], v[i + 1]), less), scale2);
+            more[i / 2 & 1] = __fadd2_rn(more[i / 2 & 1], make_float2(ex2(e.x), ex2(e.y)));
+          }
+          s = __fadd_rn(s, __fadd_rn(__fadd_rn(more[0].x, more[0].y), __fadd_rn(more[1].x, more[1].y)));
           m = top;
         }
         if (row < a.most) a.part[(size_t)(2 * tile + half) * a.most + row] = make_float2(m, s);
       } else {
-        const uint32_t out = outs + (warp - 2) * kStageBytes;
-#pragma unroll 1
+        const uint32_t out = outs + (warp - 2) * 2 * 4096;
+#pragma unroll
         for (int c = 0; c < BN / 2; c += 64) {
           const uint32_t col = col0 + c;
-          if (col - a.v0 >= a.ldp) break;
+          if (col >= a.v1) break;
           float v[64];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float(&b)[32] = *reinterpret_cast<float(*)[32]>(v + 32 * h);
             load_block(from + c + 32 * h, b);
-            add_bias(b, col + 32 * h);
+            add_bias(b, bias[c / 32 + h]);
+            const float2 less = make_float2(-lse, -lse), scale2 = make_float2(kLog2e, kLog2e), g2 = make_float2(g, g);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float p = ex2(__fmul_rn(__fadd_rn(b[i], -lse), kLog2e));
-              const float z = __fmul_rn(g, hit == c + 32 * h + i ? __fadd_rn(p, -1.f) : p);
-              b[i] = real && col + 32 * h + i < a.v1 ? z : 0.f;
+            for (int i = 0; i < 32; i += 2) {
+              const float2 e = __fmul2_rn(__fadd2_rn(make_float2(b[i], b[i + 1]), less), scale2);
+              float2 p = make_float2(ex2(e.x), ex2(e.y));
+              if (hit == c + 32 * h + i) p.x = __fadd_rn(p.x, -1.f);
+              if (hit == c + 32 * h + i + 1) p.y = __fadd_rn(p.y, -1.f);
+              p = __fmul2_rn(g2, p);
+              b[i] = real ? p.x : 0.f;
+              b[i + 1] = real ? p.y : 0.f;
+            }
+            if (col + 32 * h + 32 > a.v1) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col + 32 * h + i >= a.v1) b[i] = 0.f;
             }
           }
           if (a.dbias) {
@@ -286,13 +348,13 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
               for (int i = 0; i < 32; ++i) b[i] = v[32 * h + i];
               const float sum = lane_sums(b, lane);
-              a.dbias[(size_t)(row0 / 32) * a.ldp + (col - a.v0) + 32 * h + lane] = sum;
+              a.dbias[(size_t)(row0 / 32) * a.ldb + (col - a.v0) + 32 * h + lane] = sum;
             }
           }
           // the next part holds what this one's rounding left (exactly: three parts of 8 bits are the 24 of fp32)
 #pragma unroll
           for (int p = 0; p < PLANES; ++p) {
-            store_block<__nv_bfloat16>(&map_p, (int)(col - a.v0), (int)(row0 + p * a.most), v, lane, out);
+            put_block<__nv_bfloat16>(&map_p, (int)(col - a.v0), (int)(row0 + p * a.most), v, lane, out, puts);
             if (p + 1 < PLANES) {
 #pragma unroll
               for (int i = 0; i < 64; ++i) v[i] = __fadd_rn(v[i], -__bfloat162float(__float2bfloat16_rn(v[i])));
@@ -317,35 +379,47 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
   }
 }
 
-// 32 tokens to a CTA: eight warps share the parts of each, then each warp forms the logits of four targets, in fp32 from the
-// bf16 operands.  (Taken from the tensor memory they would carry the matrix unit's cut-off sums.)
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
+  return make_float2(top, __fadd_rn(__fmul_rn(a.y, ex2((a.x - ref) * kLog2e)), __fmul_rn(b.y, ex2((b.x - ref) * kLog2e))));
+}
+
+// R tokens to a CTA: 256 / R threads share the parts of each.  Before that, while the products may still run, a warp forms the logit
+// of a token's target, in fp32 from the bf16 operands.  (Taken from the tensor memory it would carry the matrix unit's cut-off sums.)
+template <int R>
 __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const uint16_t* x, size_t ldx, const float2* part, uint32_t parts,
                                                      float* loss, float* lse) {
-  __shared__ float2 sums[8][33];
-  __shared__ float chosen[32];
+  __shared__ float2 sums[8][R];
+  __shared__ float chosen[R];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t t0 = blockIdx.x * 32;
+  const uint32_t t0 = blockIdx.x * R;
   const uint16_t* w = static_cast<const uint16_t*>(a.w);
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t t = t0 + 4 * warp + i;
+  for (int i = warp; i < R; i += 8) {
+    const uint32_t t = t0 + i;
     float z = 0.f;
-    if (t < a.t) {
-      const int64_t to = a.target[t];
-      if (to == a.ignore) {
-        z = 0.f;
-      } else if (to < 0 || to >= (int64_t)a.v) {
+    const int64_t to = t < a.t ? a.target[t] : a.ignore;
+    if (to != a.ignore) {
+      if (to < 0 || to >= (int64_t)a.v) {
         z = __int_as_float(0x7fc00000);
       } else {
         const uint16_t *p = x + (size_t)t * ldx, *q = w + (size_t)to * a.ldw;
         float s[2] = {0.f, 0.f};
-        if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 3) == 0) {
-          for (uint32_t c = 2 * lane; c + 1 < a.d; c += 64) {
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(p + c), y = *reinterpret_cast<const uint32_t*>(q + c);
-            s[0] = __fmaf_rn(__uint_as_float(u << 16), __uint_as_float(y << 16), s[0]);
-            s[1] = __fmaf_rn(__uint_as_float(u & 0xffff0000u), __uint_as_float(y & 0xffff0000u), s[1]);
+        if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
+          const uint32_t whole = a.d & ~7u;
+#pragma unroll 4
+          for (uint32_t c = 8 * lane; c < whole; c += 256) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4*>(p + c)), y = __ldg(reinterpret_cast<const uint4*>(q + c));
+            const uint32_t us[4] = {u.x, u.y, u.z, u.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              s[0] = __fmaf_rn(__uint_as_float(us[j] << 16), __uint_as_float(ys[j] << 16), s[0]);
+              s[1] = __fmaf_rn(__uint_as_float(us[j] & 0xffff0000u), __uint_as_float(ys[j] & 0xffff0000u), s[1]);
+            }
           }
-          if ((a.d & 1) && lane == 0) s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[a.d - 1] << 16), __uint_as_float((uint32_t)q[a.d - 1] << 16), s[0]);
+          if (lane < (a.d & 7))
+            s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[whole + lane] << 16), __uint_as_float((uint32_t)q[whole + lane] << 16), s[0]);
         } else {
+#pragma unroll 8
           for (uint32_t c = lane; c < a.d; c += 32) s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[c] << 16), __uint_as_float((uint32_t)q[c] << 16), s[0]);
         }
         z = s[0] + s[1];
@@ -353,31 +427,35 @@ __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const ui
         if (a.bias) z += a.bias[to];
       }
     }
-    if (lane == 0) chosen[4 * warp + i] = z;
+    if (lane == 0) chosen[i] = z;
   }
+  constexpr int kGroups = 256 / R;
+  const int mine = threadIdx.x % R, group = threadIdx.x / R;
+  const uint32_t t = t0 + mine;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t t = t0 + lane;
   int32_t row = -1;
   if (t < a.t) row = a.r.row ? a.r.row[t] : a.target[t] != a.ignore ? (int32_t)t : -1;
-  float m = -INFINITY, s = 0.f;
+  float2 sum = make_float2(-INFINITY, 0.f);
   if (row >= 0) {
-    for (uint32_t i = warp; i < parts; i += 8) {
-      const float2 p = __ldcg(part + (size_t)i * a.r.most + row);
-      const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
-      s = __fadd_rn(__fmul_rn(s, ex2((m - ref) * kLog2e)), __fmul_rn(p.y, ex2((p.x - ref) * kLog2e)));
-      m = top;
+    for (uint32_t i0 = group; i0 < parts; i0 += 8 * kGroups) {
+      float2 p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        p[j] = i0 + j * kGroups < parts ? __ldcg(part + (size_t)(i0 + j * kGroups) * a.r.most + row) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int j = 0; j < o; ++j) p[j] = join(p[j], p[j + o]);
+      sum = join(sum, p[0]);
     }
   }
-  sums[warp][lane] = make_float2(m, s);
+#pragma unroll
+  for (int o = R; o < 32; o <<= 1) sum = join(sum, make_float2(__shfl_xor_sync(0xffffffffu, sum.x, o), __shfl_xor_sync(0xffffffffu, sum.y, o)));
+  if (lane < R) sums[warp][lane] = sum;
   __syncthreads();
-  if (warp != 0 || t >= a.t) return;
-  for (int i = 1; i < 8; ++i) {
-    const float2 p = sums[i][lane];
-    const float top = fmaxf(m, p.x), ref = top == -INFINITY ? 0.f : top;
-    s = __fadd_rn(__fmul_rn(s, ex2((m - ref) * kLog2e)), __fmul_rn(p.y, ex2((p.x - ref) * kLog2e)));
-    m = top;
-  }
-  const float total = row < 0 ? 0.f : (m == -INFINITY ? 0.f : m) + logf(s), z = chosen[lane];
+  if (threadIdx.x >= R || t >= a.t) return;
+  for (int i = 1; i < 8; ++i) sum = join(sum, sums[i][mine]);
+  const float total = row < 0 ? 0.f : (sum.x == -INFINITY ? 0.f : sum.x) + logf(sum.y), z = chosen[mine];
   // (the NaN of a target outside the vocabulary goes into lse as well: all gradients of the token are NaN)
   lse[t] = z != z && row >= 0 ? z : total;
   loss[t] = row < 0 ? 0.f : total - z;
@@ -414,18 +492,21 @@ cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, cons
 }  // namespace
 
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
-  gather_kernel<<<(a.t + kGatherRows - 1) / kGatherRows, 256, 0, stream>>>(a);
+  GatherArgs g = a;
+  g.aligned = rows_aligned(a.x, a.ldx * 2) && a.d % 8 == 0;
+  gather_kernel<<<(a.t + kGatherRows - 1) / kGatherRows, 256, 0, stream>>>(g);
   return cudaGetLastError();
 }
 
 VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms) {
   if (rows <= 128) return {1, 128};
   const uint32_t k = (d + kDepth - 1) / kDepth;
-  auto cost = [&](int cg, int bn, double stage) {
+  // (a tile takes as long as its products or, beside the next one's, as its results)
+  auto cost = [&](int cg, int bn, double stage, double results) {
     const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + bn - 1) / bn), units = sms / cg;
-    return (double)((tiles + units - 1) / units) * (k * stage + 2500.0);
+    return (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
   };
-  return cost(2, 256, 512.0) <= cost(1, 128, 300.0) ? VocabShape{2, 256} : VocabShape{1, 128};
+  return cost(2, 256, 512.0, 4000.0) <= cost(1, 128, 300.0, 2500.0) ? VocabShape{2, 256} : VocabShape{1, 128};
 }
 
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s) { return 2 * ((a.v + s.bn - 1) / s.bn); }
@@ -441,8 +522,11 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, float2* part, 
 
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss, float* lse,
                                 cudaStream_t stream) {
-  return launch_with(finish_kernel, dim3((a.t + 31) / 32), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts,
-                     loss, lse);
+  // (few tokens: more threads to each)
+  auto go = [&](auto* kernel, uint32_t r) {
+    return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts, loss, lse);
+  };
+  return a.t <= 2048 ? go(finish_kernel<4>, 4) : go(finish_kernel<32>, 32);
 }
 
 cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,
@@ -455,8 +539,9 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0,
   s.ignore = a.ignore;
   s.lse = o.lse;
   s.dloss = o.dloss;
+  s.scale = a.r.scale;
   s.dbias = o.dbias;
-  s.ldp = o.ldp;
+  s.ldb = o.ldb;
   s.err = err;
   return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream) : by_shape<1>(a, sh, s, &o, sms, stream);
 }

@@ -87,10 +87,10 @@ struct GemmArgs {
   uint32_t n, k;         // output and input channels
   int device;
 };
-// Tiles first .. first + count of a result [m][n] (tiles_m of them to a column of tiles), each from `splits` partial results
+// Tiles first .. first + count of a result [m][n] (`line` of them to a row of tiles, or to a column of them), each from `splits` partial results
 // [tile_m][tile_n] that follow one another, added in order.
-cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first, uint32_t count, uint32_t tiles_m,
-                        uint64_t m, uint32_t n, void* out, size_t ldo, bool f32, cudaStream_t stream);
+cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first, uint32_t count, uint32_t line,
+                        bool by_rows, uint64_t m, uint32_t n, void* out, size_t ldo, bool f32, cudaStream_t stream);
 // bf16 rows at any address, copied to rows whose pitch ldo is a multiple of 8 elements (whole 16-byte pieces are written).
 cudaError_t launch_pitch(const void* in, size_t ldi, uint64_t rows, uint32_t cols, void* out, size_t ldo, cudaStream_t stream);
 // (err: the handle's flag, raised by a wait that ran out)

@@ -430,14 +430,16 @@ __global__ void __launch_bounds__(256) q8_convert_kernel(const int8_t* q, size_t
 // The shared tiles from their partial results, added in order: 4 columns to a thread.
 template <class O>
 __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first,
-                                                      uint32_t count, uint32_t tiles_m, uint64_t m, uint32_t n, O* out, size_t ldo, bool aligned) {
+                                                      uint32_t count, uint32_t line, bool by_rows, uint64_t m, uint32_t n, O* out, size_t ldo,
+                                                      bool aligned) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const uint32_t per_row = tile_n / 4, per_tile = per_row * tile_m;
   const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x;
   const uint32_t t = (uint32_t)(id / per_tile), in = (uint32_t)(id - (uint64_t)t * per_tile);
   if (t >= count) return;
-  const uint64_t row = (uint64_t)((first + t) % tiles_m) * tile_m + in / per_row;
-  const uint32_t col = (first + t) / tiles_m * tile_n + in % per_row * 4;
+  const uint32_t along = (first + t) % line, across = (first + t) / line;
+  const uint64_t row = (uint64_t)(by_rows ? across : along) * tile_m + in / per_row;
+  const uint32_t col = (by_rows ? along : across) * tile_n + in % per_row * 4;
   if (row >= m || col >= n) return;
   const float4* p = reinterpret_cast<const float4*>(part) + (size_t)t * splits * per_tile + in;
   float4 s = __ldcg(p);
@@ -612,18 +614,18 @@ cudaError_t grad(const GemmArgs& g, void* ws, int sms, int* err, cudaStream_t st
   if (e != cudaSuccess || w.plan.splits == 1) return e;
   const uint32_t count = w.plan.tiles - w.plan.full, tile_m = w.plan.cg * 128, tiles_m = (uint32_t)((m + tile_m - 1) / tile_m);
   ++*launches;
-  return launch_join(at.part, w.plan.splits, tile_m, w.plan.bn, w.plan.full, count, tiles_m, m, g.k, g.out, g.ldo, f32, stream);
+  return launch_join(at.part, w.plan.splits, tile_m, w.plan.bn, w.plan.full, count, tiles_m, false, m, g.k, g.out, g.ldo, f32, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first, uint32_t count, uint32_t tiles_m,
-                        uint64_t m, uint32_t n, void* out, size_t ldo, bool f32, cudaStream_t stream) {
+cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uint32_t tile_n, uint32_t first, uint32_t count, uint32_t line,
+                        bool by_rows, uint64_t m, uint32_t n, void* out, size_t ldo, bool f32, cudaStream_t stream) {
   const dim3 grid((unsigned)(((uint64_t)count * tile_m * (tile_n / 4) + 255) / 256));
   if (f32)
-    return launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, tiles_m, m, n,
+    return launch_with(q8_join_kernel<float>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, line, by_rows, m, n,
                        static_cast<float*>(out), ldo, rows_aligned(out, ldo * 4));
-  return launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, tiles_m, m, n,
+  return launch_with(q8_join_kernel<__nv_bfloat16>, grid, dim3(256), 0, 1, true, stream, part, splits, tile_m, tile_n, first, count, line, by_rows, m, n,
                      static_cast<__nv_bfloat16*>(out), ldo, rows_aligned(out, ldo * 2));
 }
 cudaError_t launch_pitch(const void* in, size_t ldi, uint64_t rows, uint32_t cols, void* out, size_t ldo, cudaStream_t stream) {

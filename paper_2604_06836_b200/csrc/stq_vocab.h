@@ -57,7 +57,8 @@ cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
 struct VocabShape {
   int cg, bn;
 };
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms);
+// (cost, if wanted: the time in clock cycles)
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* cost = nullptr);
 
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s);
@@ -66,11 +67,12 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, float2* part, i
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
                                 float* lse, cudaStream_t stream);
 
-// Gradients of the logits of entries [v0, v1), divided by scale, p[plane][row][v - v0]: `planes` bf16 numbers (1 or 3) whose sum they are,
-// plane i at row i * most; pitch ldp, a multiple of 64.  dbias: sums over 32 rows each, [most / 32] of pitch ldb, or null.
+// Gradients of the logits of entries [v0, v1), divided by scale: `planes` bf16 numbers (1 or 3) whose sum they are.  They lie in panels
+// of 64 entries, p[plane][(v - v0) / 64][row][(v - v0) % 64], `panels` to a plane and `most` rows to a panel, so that every box that is
+// copied (64 entries, any rows) is one range of memory.  dbias: sums over 32 rows each, [most / 32] of pitch ldb, or null.
 struct VocabGradOut {
   void* p;
-  size_t ldp;
+  uint32_t panels;
   int planes;
   float* dbias;
   size_t ldb;
@@ -85,7 +87,7 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape s, uint32_t v0, 
 struct VocabDw {
   VocabRows r;
   const void* p;
-  size_t ldp;
+  uint32_t panels;
   uint32_t cols, d;           // v1 - v0
   void* dw;                   // row v0
   size_t lddw;
@@ -93,6 +95,7 @@ struct VocabDw {
   int device;
 };
 size_t vocab_dw_partial(const VocabDw& a, int sms);
+double vocab_dw_cost(const VocabDw& a, int sms);      // in clock cycles
 cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches);
 
 // planes[c][row][:] (+)= share c of the sum over [v0, v0 + cols) of p[row][i] w[v0 + i][:].  The sums of all tiles, one after
@@ -101,7 +104,7 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
 struct VocabDx {
   VocabRows r;
   const void* p;
-  size_t ldp;
+  uint32_t panels;
   const void* w;              // row v0
   size_t ldw;
   uint32_t cols, d, first;

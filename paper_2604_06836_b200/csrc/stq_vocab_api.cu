@@ -81,6 +81,29 @@ cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, const
   return cudaSuccess;
 }
 
+// Entries of the vocabulary to a piece (the last piece has what is left): as many tiles as fit, or somewhat fewer where the tiles of the
+// products then fill their last round better.
+uint32_t piece_of(const VocabArgs& a, VocabDw g, size_t entry, bool dw, int sms) {
+  const uint32_t tiles = (uint32_t)(up(a.v, 256) / 256);
+  const size_t fit = kPieceBytes / entry / 256;
+  if (fit >= tiles) return a.v;
+  const uint32_t widest = fit < 1 ? 1 : (uint32_t)fit;
+  auto cost = [&](uint32_t cols) {
+    double c, extra = 60000.0;      // (of a piece: launches, beginnings and ends)
+    vocab_shape(a.t, cols, a.d, sms, &c);
+    g.cols = cols;
+    return c + extra + (dw ? vocab_dw_cost(g, sms) : 0.0);
+  };
+  uint32_t best = widest;
+  double least = 1e300;
+  for (uint32_t w = widest; w > widest - widest / 3 && w > 0; --w) {
+    const uint32_t last = a.v - (tiles - 1) / w * w * 256;
+    const double c = ((tiles - 1) / w) * cost(w * 256) + cost(last);
+    if (c < least) { least = c; best = w; }
+  }
+  return best * 256;
+}
+
 int check(const stq_handle* h, const void* x, uint64_t ldx, const void* w, uint64_t ldw, const float* bias, const int64_t* target, uint64_t t,
           uint32_t v, uint32_t d) {
   STQ_TRY(check_handle(h));
@@ -177,24 +200,22 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   Rows r(a, x, ldx, true);
   const uint32_t most = most_rows(a.t);
   const int planes = dw && dw_dtype == STQ_GRAD_F32 ? 3 : 1;
-  // pieces of the vocabulary: equal but for the last
-  const size_t fit = kPieceBytes / ((size_t)most * 2 * planes) / 256 * 256, tiles = up(v, 256) / 256, widest = (fit < 256 ? 256 : fit) / 256;
-  const size_t pieces = (tiles + widest - 1) / widest;
-  const uint32_t cols = (uint32_t)((tiles + pieces - 1) / pieces * 256 < v ? (tiles + pieces - 1) / pieces * 256 : v);
-  VocabGradOut o = {nullptr, up(cols, 64), planes, nullptr, 0, lse, dloss};
-  // sums for dbias: of the whole vocabulary, if that is not too much, and joined once; else piece by piece
-  const size_t db_rows = most / 32;
-  const bool db_once = db_rows * up(v, 64) * 4 <= kPieceBytes / 4;
-  o.ldb = db_once ? up(v, 64) : o.ldp;
   VocabDw gw = {};
-  gw.ldp = o.ldp;
-  gw.cols = cols; gw.d = d;
+  gw.d = d;
   gw.lddw = lddw;
   gw.f32 = dw_dtype == STQ_GRAD_F32;
   gw.device = h->device;
   gw.r.most = most;
+  const uint32_t cols = piece_of(a, gw, (size_t)most * 2 * planes, dw != nullptr, h->sm_count);
+  VocabGradOut o = {nullptr, (uint32_t)(up(cols, 64) / 64), planes, nullptr, 0, lse, dloss};
+  gw.panels = o.panels;
+  gw.cols = cols;
+  // sums for dbias: of the whole vocabulary, if that is not too much, and joined once; else piece by piece
+  const size_t db_rows = most / 32;
+  const bool db_once = db_rows * up(v, 64) * 4 <= kPieceBytes / 4;
+  o.ldb = db_once ? up(v, 64) : up(cols, 64);
   VocabDx gx = {};
-  gx.ldp = o.ldp;
+  gx.panels = o.panels;
   gx.d = d; gx.first = cols;
   gx.ldd = up(d, 32);
   gx.plane_rows = (uint32_t)vocab_dx_rows(most, gx.ldd);
@@ -213,7 +234,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   for (int pass = 0; pass < 2; ++pass) {
     m.at = 0;
     r.place(m, a, most);
-    o.p = m.take<uint16_t>((size_t)most * planes * o.ldp);
+    o.p = m.take<uint16_t>((size_t)most * planes * o.panels * 64);
     db_part = dbias ? m.take<float>(db_rows * o.ldb) : nullptr;
     part = partial ? m.take<float>(partial) : nullptr;
     gx.planes = dx ? m.take<float>(gx.plane_rows * gx.ldd) : nullptr;

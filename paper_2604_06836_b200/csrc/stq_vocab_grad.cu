@@ -29,7 +29,7 @@ constexpr int kMaxTilesN = 512;        // tiles along a row of dx
 
 struct GradArgs {
   const uint32_t* count;
-  uint32_t rows, most;
+  uint32_t rows, most, panels;
   uint32_t n, bn;                      // columns of the result, and of a tile
   uint32_t units;
   // dw
@@ -37,7 +37,7 @@ struct GradArgs {
   void* out;
   size_t ldo;
   uint32_t m;                          // rows of the result
-  uint32_t tiles_m, tiles, full, splits;   // tiles from `full` on are shared by `splits` work items each
+  uint32_t tiles, full, splits;        // tiles from `full` on are shared by `splits` work items each
   float* part;
   int aligned;
   // dx
@@ -122,17 +122,17 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
           it.k1 = (uint32_t)((uint64_t)ksteps * (sp + 1) / a.splits);
           it.share = (int)i;
         }
-        it.row = it.tile % a.tiles_m * 128 * CG;
-        it.col = it.tile / a.tiles_m * a.bn;
+        it.row = it.tile / tiles_n * 128 * CG;      // (row by row: the tiles of a row read the same columns of p)
+        it.col = it.tile % tiles_n * a.bn;
         if (!f(it)) return;
       }
     } else {
       if (unit >= ranges.U) return;
       const uint64_t end = ranges.begin(unit + 1);
       for (uint64_t s = ranges.begin(unit); s < end;) {
-        const uint32_t tile = (uint32_t)(s / ranges.ksteps);
-        const uint64_t t0 = (uint64_t)tile * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
-        const Item it = {tile, tile % ranges.tiles_m * 128 * CG, tile / ranges.tiles_m * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
+        const uint32_t q = (uint32_t)(s / ranges.ksteps), tile = ranges.tile(q);
+        const uint64_t t0 = (uint64_t)q * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
+        const Item it = {tile, tile / tiles_n * 128 * CG, tile % tiles_n * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
                          (int)(unit - ranges.unit_of(t0))};
         if (!f(it)) return;
         s = stop;
@@ -158,10 +158,11 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
 #pragma unroll
           for (int p = 0; p < PARTS; ++p) {
             if constexpr (DW) {
-              tensor_load<CG>(at + p * S::kA, &map_p, row, c + p * (int)a.most, full0 + 8 * s);
-              tensor_load<CG>(at + p * S::kA + S::kA / 2, &map_p, row + 64, c + p * (int)a.most, full0 + 8 * s);
+              const int panel = p * (int)a.panels + row / 64;
+              tensor_load<CG>(at + p * S::kA, &map_p, 0, panel * (int)a.most + c, full0 + 8 * s);
+              tensor_load<CG>(at + p * S::kA + S::kA / 2, &map_p, 0, (panel + 1) * (int)a.most + c, full0 + 8 * s);
             } else {
-              tensor_load<CG>(at, &map_p, c, row, full0 + 8 * s);
+              tensor_load<CG>(at, &map_p, 0, (int)k * (int)a.most + row, full0 + 8 * s);
             }
           }
         }
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, siz
     const Ranges r0(count, tile_m, tiles_n, first, units, plane_rows), r1(count, tile_m, tiles_n, last, units, plane_rows);
     for (uint32_t i = threadIdx.x; i < 2 * tiles_n; i += 256) {
       const uint32_t m = lo + i / tiles_n, n = i % tiles_n;
-      if (m < r0.tiles_m) shares[i / tiles_n][n] = (uint8_t)max(r0.shares(n * r0.tiles_m + m), r1.shares(n * r0.tiles_m + m));
+      if (m < r0.tiles_m) shares[i / tiles_n][n] = (uint8_t)max(r0.shares(m * tiles_n + n), r1.shares(m * tiles_n + n));
     }
   }
   __syncthreads();
@@ -404,6 +405,7 @@ uint32_t tile_columns(uint32_t n, uint32_t widest, uint32_t unit) {
 struct DwPlan {
   int cg, bn_max;
   uint32_t bn, tiles_m, tiles, full, splits;
+  double cost;
 };
 // Time of a plan in clock cycles, as for the 8-bit products: a stage is 4096 multiply-adds a cycle and SM, a tile has a beginning
 // and an end, partial results go through memory once more.
@@ -414,7 +416,7 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
   DwPlan best = {};
   double least = 1e300;
   for (const auto& sh : shapes[a.f32]) {
-    DwPlan p = {sh[0], sh[1], tile_columns(a.d, sh[1], a.f32 ? 32 : 16), (a.cols + 128 * sh[0] - 1) / (128 * sh[0]), 0, 0, 0};
+    DwPlan p = {sh[0], sh[1], tile_columns(a.d, sh[1], a.f32 ? 32 : 16), (a.cols + 128 * sh[0] - 1) / (128 * sh[0]), 0, 0, 0, 0.0};
     p.tiles = p.tiles_m * ((a.d + p.bn - 1) / p.bn);
     const double stage = 2.0 * p.bn * parts + (p.cg == 1 ? 40.0 * parts : 0.0);
     const uint64_t units = sms / p.cg, rounds = p.tiles / units, full = rounds * units, rest = p.tiles - full;
@@ -429,6 +431,7 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
         best = p;
         best.full = (uint32_t)(sp > 1 ? full : p.tiles);
         best.splits = sp;
+        best.cost = c;
       }
       if (!rest) break;
     }
@@ -437,18 +440,19 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
 }
 
 template <int CG, int BN, int PARTS, bool DW, class O>
-cudaError_t launch(const VocabRows& r, const void* p, size_t ldp, const void* b, uint64_t b_rows, uint32_t b_cols, size_t ldb, void* out,
+cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const void* b, uint64_t b_rows, uint32_t b_cols, size_t ldb, void* out,
                    uint64_t out_rows, size_t ldo, uint64_t items, GradArgs g, int device, int sms, int* err, cudaStream_t stream) {
   using S = GradShape<CG, BN, PARTS>;
   g.count = r.count;
   g.rows = r.rows;
   g.most = r.most;
+  g.panels = panels;
   g.scale = r.scale;
   g.err = err;
   const uint64_t most = sms / CG;
   g.units = (uint32_t)(items < most ? items : most);
   CUtensorMap mp, mb, mo = {};
-  cudaError_t e = make_tensor_map(&mp, p, 2, (uint64_t)r.most * PARTS, ldp, ldp, DW ? 64 : 128, 64, true);
+  cudaError_t e = make_tensor_map(&mp, p, 2, (uint64_t)r.most * panels * PARTS, 64, 64, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess) e = make_tensor_map(&mb, b, 2, b_rows, b_cols, ldb, 64, 64, true);
   if (e == cudaSuccess && (!DW || g.aligned)) e = make_tensor_map(&mo, out, sizeof(O), out_rows, DW ? g.n : ldo, ldo, 32, 128 / sizeof(O), true);
   auto* kernel = vocab_grad_kernel<CG, BN, PARTS, DW, O>;
@@ -475,6 +479,8 @@ size_t vocab_dw_partial(const VocabDw& a, int sms) {
   return p.splits > 1 ? (size_t)(p.tiles - p.full) * p.splits * p.cg * 128 * p.bn : 0;
 }
 
+double vocab_dw_cost(const VocabDw& a, int sms) { return dw_plan(a, sms).cost; }
+
 cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches) {
   const DwPlan p = dw_plan(a, sms);
   GradArgs g = {};
@@ -483,7 +489,6 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
   g.out = a.dw;
   g.ldo = a.lddw;
   g.m = a.cols;
-  g.tiles_m = p.tiles_m;
   g.tiles = p.tiles;
   g.full = p.full;
   g.splits = p.splits;
@@ -493,7 +498,7 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
   const uint64_t items = p.full + (uint64_t)(p.tiles - p.full) * p.splits;
   cudaError_t rc;
   const auto go = [&](auto launch_fn) {
-    return launch_fn(a.r, a.p, a.ldp, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, items, g, a.device, sms, err, stream);
+    return launch_fn(a.r, a.p, a.panels, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, items, g, a.device, sms, err, stream);
   };
   if (a.f32)
     rc = p.cg == 2 ? go(launch<2, 128, 3, true, float>) : go(launch<1, 64, 3, true, float>);
@@ -502,7 +507,7 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
   *launches = 1;
   if (rc != cudaSuccess || p.splits == 1) return rc;
   ++*launches;
-  return launch_join(part, p.splits, p.cg * 128, p.bn, p.full, p.tiles - p.full, p.tiles_m, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
+  return launch_join(part, p.splits, p.cg * 128, p.bn, p.full, p.tiles - p.full, p.tiles / p.tiles_m, true, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
 }
 
 size_t vocab_dx_rows(uint32_t most, size_t ldd) {
@@ -522,8 +527,8 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
   g.begin = a.begin;
   const uint64_t items = sms / s.cg;
   if (s.cg == 2)
-    return launch<2, 256, 1, false, float>(a.r, a.p, a.ldp, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
-  return launch<1, 128, 1, false, float>(a.r, a.p, a.ldp, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
+    return launch<2, 256, 1, false, float>(a.r, a.p, a.panels, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
+  return launch<1, 128, 1, false, float>(a.r, a.p, a.panels, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
 }
 
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream) {

@@ -10,7 +10,7 @@
 
 namespace stq {
 
-// Tiles of dx, and which units (CTAs or pairs) add to which: unit u has stages [u S / U, (u + 1) S / U) of the S = tiles * ksteps.
+// Tiles of dx, row by row, and which units (CTAs or pairs) add to which: unit u has stages [u S / U, (u + 1) S / U) of the S = tiles * ksteps.
 struct Ranges {
   uint32_t tiles_m, tiles, ksteps, U;
   uint64_t S;
@@ -30,8 +30,19 @@ struct Ranges {
   STQ_BOTH uint32_t unit_of(uint64_t s) const { return (uint32_t)ratio((s + 1) * U - 1, S); }
   // (a division of 64 bits takes a GPU ten times as long)
   STQ_BOTH static uint64_t ratio(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
+  // Tile number q of the order that the ranges are cut in.  A unit has r tiles or so, one after the other: they are chosen so that at any
+  // time the units' tiles are neighbours (whole rows of tiles, which read the same rows of p).
+  STQ_BOTH uint32_t tile(uint32_t q) const {
+    const uint32_t r = tiles / U, c = r > 1 ? tiles / r : 0;
+    return q < r * c ? q % r * c + q / r : q;
+  }
+  STQ_BOTH uint32_t place(uint32_t tile) const {      // (its inverse)
+    const uint32_t r = tiles / U, c = r > 1 ? tiles / r : 0;
+    return tile < r * c ? tile % c * r + tile / c : tile;
+  }
   STQ_BOTH uint32_t shares(uint32_t tile) const {
-    return unit_of((uint64_t)tile * ksteps + ksteps - 1) - unit_of((uint64_t)tile * ksteps) + 1;
+    const uint64_t at = (uint64_t)place(tile) * ksteps;
+    return unit_of(at + ksteps - 1) - unit_of(at) + 1;
   }
 };
 

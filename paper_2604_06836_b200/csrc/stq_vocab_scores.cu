@@ -132,6 +132,7 @@ struct ScoreArgs {
   const float* scale;
   float* dbias;
   size_t ldb;
+  uint32_t panels;
   int* err;
 };
 
@@ -354,7 +355,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           // the next part holds what this one's rounding left (exactly: three parts of 8 bits are the 24 of fp32)
 #pragma unroll
           for (int p = 0; p < PLANES; ++p) {
-            put_block<__nv_bfloat16>(&map_p, (int)(col - a.v0), (int)(row0 + p * a.most), v, lane, out, puts);
+            put_block<__nv_bfloat16>(&map_p, 0, (int)((p * a.panels + (col - a.v0) / 64) * a.most + row0), v, lane, out, puts);
             if (p + 1 < PLANES) {
 #pragma unroll
               for (int i = 0; i < 64; ++i) v[i] = __fadd_rn(v[i], -__bfloat162float(__float2bfloat16_rn(v[i])));
@@ -474,7 +475,7 @@ cudaError_t launch(const VocabArgs& a, ScoreArgs s, const VocabGradOut* o, int s
   CUtensorMap mx, mw, mp = {};
   cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, 128, kDepth, true);
   if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, BN / CG, kDepth, true);
-  if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->planes, o->ldp, o->ldp, 32, 64, true);
+  if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->panels * o->planes, 64, 64, 32, 64, true);
   auto* kernel = score_kernel<CG, BN, PLANES>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, a.device, seen);
@@ -498,15 +499,17 @@ cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms) {
-  if (rows <= 128) return {1, 128};
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* cost) {
   const uint32_t k = (d + kDepth - 1) / kDepth;
   // (a tile takes as long as its products or, beside the next one's, as its results)
-  auto cost = [&](int cg, int bn, double stage, double results) {
+  auto cycles = [&](int cg, int bn, double stage, double results) {
     const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + bn - 1) / bn), units = sms / cg;
     return (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
   };
-  return cost(2, 256, 512.0, 4000.0) <= cost(1, 128, 300.0, 2500.0) ? VocabShape{2, 256} : VocabShape{1, 128};
+  const double pair = cycles(2, 256, 512.0, 4000.0), one = cycles(1, 128, 300.0, 2500.0);
+  const bool wide = rows > 128 && pair <= one;
+  if (cost) *cost = wide ? pair : one;
+  return wide ? VocabShape{2, 256} : VocabShape{1, 128};
 }
 
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s) { return 2 * ((a.v + s.bn - 1) / s.bn); }
@@ -542,6 +545,7 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0,
   s.scale = a.r.scale;
   s.dbias = o.dbias;
   s.ldb = o.ldb;
+  s.panels = o.panels;
   s.err = err;
   return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream) : by_shape<1>(a, sh, s, &o, sms, stream);
 }

@@ -29,8 +29,10 @@ extern "C" int check(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t 
     shortest = e - b < shortest ? e - b : shortest;
   }
   if (longest - shortest > 1) return 6;
-  for (uint32_t t = 0; t < r.tiles; ++t) {
-    const uint32_t n = r.shares(t), first = r.unit_of((uint64_t)t * k);
+  for (uint32_t q = 0; q < r.tiles; ++q) {
+    const uint32_t tile = r.tile(q);
+    if (tile >= r.tiles || r.place(tile) != q) return 9;                     // not a permutation
+    const uint32_t t = q, n = r.shares(tile), first = r.unit_of((uint64_t)t * k);
     if (n == 0 || n > planes) return 7;                                      // more than there are planes for
     uint32_t seen = 0;
     for (uint32_t u = first; u < r.U && r.begin(u) < (uint64_t)(t + 1) * k; ++u) seen += r.begin(u + 1) > (uint64_t)t * k;

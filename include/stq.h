@@ -351,7 +351,7 @@ int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, ui
  * ignore_index have loss 0, lse 0 and no gradient, and take no part in the products.  Any other target outside
  * 0..v-1 gives loss and lse NaN, and NaN gradients.  A bias of -inf takes an entry out of the vocabulary.
  * All sums are held in fp32 and added in a fixed order.  Workspace, streams and graphs: as for the 8-bit
- * operators above (for the gradients about 256 MB of gradients of logits, 2 copies of x in fp32 and one in
+ * operators above (for the gradients up to 512 MB of gradients of logits, 2 copies of x in fp32 and one in
  * bf16; a copy of w where its rows are not aligned to 16 bytes). */
 #define STQ_VOCAB_MAX_TOKENS 262144
 #define STQ_VOCAB_MAX_WIDTH 65536

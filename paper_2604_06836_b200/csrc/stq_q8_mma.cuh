@@ -216,14 +216,14 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// True if `ok` is true in all of the N threads that share barrier 1 (whole warps); a barrier for them too.
+// True if `ok` is true in all of the N threads that share barrier `id` (whole warps); a barrier for them too.
 template <int N>
-__device__ __forceinline__ bool all_of(bool ok) {
+__device__ __forceinline__ bool all_of(bool ok, int id = 1) {
   uint32_t r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)ok), "n"(N)
+      : "r"((uint32_t)ok), "n"(N), "r"(id)
       : "memory");
   return r != 0;
 }
@@ -260,12 +260,12 @@ __device__ __forceinline__ void store_block(const CUtensorMap* map, int x, int y
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
-// The same through one of two places in shared memory, 4096 bytes each, in turn (n counts the blocks), so that a copy has the time
+// The same through one of PLACES in shared memory, 4096 bytes each, in turn (n counts the blocks): with two, a copy has the time
 // of a whole block to read its own.  ADD: added to what is there (fp32).
-template <class O, bool ADD = false>
+template <class O, bool ADD = false, int PLACES = 2>
 __device__ __forceinline__ void put_block(const CUtensorMap* map, int x, int y, const float (&v)[128 / sizeof(O)], int lane, uint32_t stages, uint32_t& n) {
-  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-  const uint32_t stage = stages + (n++ & 1) * 4096;
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PLACES - 1) : "memory");
+  const uint32_t stage = stages + n++ % PLACES * 4096;
   uint32_t w[32];
   block_words<O>(v, w);
   __syncwarp();

@@ -114,7 +114,7 @@ struct VocabDx {
   uint32_t plane_rows;        // rows of all planes together
   int device;
 };
-size_t vocab_dx_rows(uint32_t most, size_t ldd);      // rows of planes that suffice
+size_t vocab_dx_rows(uint32_t most, uint32_t d, size_t ldd);      // rows of planes that suffice
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream);
 // dx of all tokens (zero for those that do not count): scale * the sum of the planes.
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream);

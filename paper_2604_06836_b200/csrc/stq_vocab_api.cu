@@ -9,7 +9,7 @@ using namespace stq;
 namespace {
 
 constexpr uint32_t kTokensAtOnce = 32768;       // of a loss: bounds its workspace (tokens do not depend on one another)
-constexpr size_t kPieceBytes = 256u << 20;      // of gradients of logits that exist at a time
+constexpr size_t kPieceBytes = 512u << 20;      // of gradients of logits that exist at a time
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
 
@@ -201,6 +201,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   const uint32_t most = most_rows(a.t);
   const int planes = dw && dw_dtype == STQ_GRAD_F32 ? 3 : 1;
   VocabDw gw = {};
+  gw.dw = dw;
   gw.d = d;
   gw.lddw = lddw;
   gw.f32 = dw_dtype == STQ_GRAD_F32;
@@ -212,13 +213,13 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   gw.cols = cols;
   // sums for dbias: of the whole vocabulary, if that is not too much, and joined once; else piece by piece
   const size_t db_rows = most / 32;
-  const bool db_once = db_rows * up(v, 64) * 4 <= kPieceBytes / 4;
+  const bool db_once = db_rows * up(v, 64) * 4 <= kPieceBytes / 8;
   o.ldb = db_once ? up(v, 64) : up(cols, 64);
   VocabDx gx = {};
   gx.panels = o.panels;
   gx.d = d; gx.first = cols;
   gx.ldd = up(d, 32);
-  gx.plane_rows = (uint32_t)vocab_dx_rows(most, gx.ldd);
+  gx.plane_rows = (uint32_t)vocab_dx_rows(most, d, gx.ldd);
   gx.device = h->device;
   // (a last piece may share its tiles in another way than the others)
   const uint32_t last = (uint32_t)(v - (v - 1) / cols * cols);

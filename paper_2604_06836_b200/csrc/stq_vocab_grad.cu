@@ -25,6 +25,7 @@ namespace {
 
 constexpr int kDepth = 64;
 constexpr int kStepK = 16;
+constexpr int kWriters = 8;             // warps that take results out of tensor memory: two groups of four
 constexpr int kMaxTilesN = 512;        // tiles along a row of dx
 
 struct GradArgs {
@@ -47,18 +48,24 @@ struct GradArgs {
   int* err;
 };
 
-template <int CG, int BN, int PARTS>
+// MT: blocks of 128 * CG rows in a tile.  A pair's SMs take in 64 bytes a cycle each, which is what a tile of 256 x 256 needs (32 KB for
+// 512 cycles of products); with two blocks of rows to one of columns it needs three quarters of that.  Both accumulators of the tensor
+// memory then belong to one tile, so its results leave while nothing is multiplied: that pays where the sums are long.
+template <int CG, int BN, int PARTS, int MT>
 struct GradShape {
-  static constexpr int kThreads = 32 * 6;
+  static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kNB = BN / CG < 64 ? 64 : BN / CG;         // columns that are copied: whole 128-byte rows
   static constexpr int kA = 128 * kDepth * 2, kB = kDepth * kNB * 2;
-  static constexpr int kStage = kA * PARTS + kB;
-  static constexpr int kOut = 2 * 4096;                           // a writing warp's blocks on their way out
-  static constexpr int kFit = (192 * 1024) / kStage;
+  static constexpr int kStage = kA * PARTS * MT + kB;
+  // A writing warp's blocks on their way out; two where there is room for them beside the stages.  (One ragged block takes 4.5 KB.)
+  static constexpr int kPlaces = MT == 1 && PARTS == 1 ? 2 : 1;
+  static constexpr int kOut = kPlaces == 2 ? 8192 : MT == 1 ? kStageBytes : 4096;
+  static constexpr int kFit = (224 * 1024 - kWriters * kOut) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
   static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
-  static constexpr int kSmem = kStages * kStage + 4 * kOut + 1024;
+  static constexpr int kSmem = kStages * kStage + kWriters * kOut + 1024;
+  static_assert(MT == 1 || PARTS == 1, "the running sum takes the place of the second block");
 };
 
 // One work item: tile (its row and column), stages [k0, k1) of its sum, and where the result goes.
@@ -68,11 +75,12 @@ struct Item {
 };
 
 // DW: rows of the result are entries of the vocabulary.  O: type of dw (dx: float).
-template <int CG, int BN, int PARTS, bool DW, class O>
-__global__ void __launch_bounds__((GradShape<CG, BN, PARTS>::kThreads), 1)
+template <int CG, int BN, int PARTS, int MT, bool DW, class O>
+__global__ void __launch_bounds__((GradShape<CG, BN, PARTS, MT>::kThreads), 1)
 vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
                   const GradArgs a) {
-  using S = GradShape<CG, BN, PARTS>;
+  using S = GradShape<CG, BN, PARTS, MT>;
+  constexpr int kTileM = 128 * CG * MT;
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
@@ -91,7 +99,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(done + 8 * i, 1);
-      bar_init(freed + 8 * i, 4 * CG);
+      bar_init(freed + 8 * i, kWriters / MT * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -107,8 +115,8 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
 
   const uint32_t tiles_n = (a.n + a.bn - 1) / a.bn;
   const uint32_t ksteps = DW ? (count + kDepth - 1) / kDepth : a.ksteps;
-  const Ranges ranges(DW ? 0 : count, 128 * CG, tiles_n, a.ksteps, a.units, a.plane_rows);
-  const Ranges before(DW ? 0 : count, 128 * CG, tiles_n, a.first, a.units, a.plane_rows);
+  const Ranges ranges(DW ? 0 : count, kTileM, tiles_n, a.ksteps, a.units, a.plane_rows);
+  const Ranges before(DW ? 0 : count, kTileM, tiles_n, a.first, a.units, a.plane_rows);
   // calls f(item) for each of this unit's items, in order, until it returns false
   auto items = [&](auto&& f) {
     if constexpr (DW) {
@@ -122,7 +130,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
           it.k1 = (uint32_t)((uint64_t)ksteps * (sp + 1) / a.splits);
           it.share = (int)i;
         }
-        it.row = it.tile / tiles_n * 128 * CG;      // (row by row: the tiles of a row read the same columns of p)
+        it.row = it.tile / tiles_n * kTileM;      // (row by row: the tiles of a row read the same columns of p)
         it.col = it.tile % tiles_n * a.bn;
         if (!f(it)) return;
       }
@@ -132,7 +140,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
       for (uint64_t s = ranges.begin(unit); s < end;) {
         const uint32_t q = (uint32_t)(s / ranges.ksteps), tile = ranges.tile(q);
         const uint64_t t0 = (uint64_t)q * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
-        const Item it = {tile, tile / tiles_n * 128 * CG, tile % tiles_n * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
+        const Item it = {tile, tile / tiles_n * kTileM, tile % tiles_n * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
                          (int)(unit - ranges.unit_of(t0))};
         if (!f(it)) return;
         s = stop;
@@ -154,15 +162,15 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
           const int c = (int)(k * kDepth);
           if (leader) bar_expect(full + 8 * s, CG * S::kStage);
 #pragma unroll
-          for (int i = 0; i < S::kNB / 64; ++i) tensor_load<CG>(at + PARTS * S::kA + i * (kDepth * 128), &map_b, col + 64 * i, c, full0 + 8 * s);
+          for (int i = 0; i < S::kNB / 64; ++i) tensor_load<CG>(at + S::kStage - S::kB + i * (kDepth * 128), &map_b, col + 64 * i, c, full0 + 8 * s);
 #pragma unroll
-          for (int p = 0; p < PARTS; ++p) {
+          for (int p = 0; p < PARTS * MT; ++p) {      // (parts of a block, or blocks)
+            const int r = row + (MT > 1 ? p * 128 * CG : 0), first = MT > 1 ? 0 : p * (int)a.panels;
             if constexpr (DW) {
-              const int panel = p * (int)a.panels + row / 64;
-              tensor_load<CG>(at + p * S::kA, &map_p, 0, panel * (int)a.most + c, full0 + 8 * s);
-              tensor_load<CG>(at + p * S::kA + S::kA / 2, &map_p, 0, (panel + 1) * (int)a.most + c, full0 + 8 * s);
+              tensor_load<CG>(at + p * S::kA, &map_p, 0, (first + r / 64) * (int)a.most + c, full0 + 8 * s);
+              tensor_load<CG>(at + p * S::kA + S::kA / 2, &map_p, 0, (first + r / 64 + 1) * (int)a.most + c, full0 + 8 * s);
             } else {
-              tensor_load<CG>(at, &map_p, 0, (int)k * (int)a.most + row, full0 + 8 * s);
+              tensor_load<CG>(at + p * S::kA, &map_p, 0, (int)k * (int)a.most + r, full0 + 8 * s);
             }
           }
         }
@@ -177,48 +185,50 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
       uint32_t it = 0, n = 0;
       items([&](const Item& w) {
         for (uint32_t k = w.k0; k < w.k1; ++k, ++it) {
-          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = (k - w.k0) % S::kChunk;
-          if (place == 0) {
-            if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) return false;
-            mma_fence_after();
-          }
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, place = (k - w.k0) % S::kChunk;
+          const bool last = place == S::kChunk - 1 || k + 1 == w.k1;
           if (!(ok = bar_wait<CG == 2>(full + 8 * s, ph))) return false;
-          mma_fence_after();
           const uint32_t at = ring + s * S::kStage;
           const uint64_t da = DW ? operand_desc(at, S::kA / 2, 1024) : operand_desc(at, 16, 1024);
-          const uint64_t db = operand_desc(at + PARTS * S::kA, kDepth * 128, 1024);
+          const uint64_t db = operand_desc(at + S::kStage - S::kB, kDepth * 128, 1024);
           constexpr uint32_t kStepA = DW ? (kStepK * 128) >> 4 : (kStepK * 2) >> 4, kStepB = (kStepK * 128) >> 4;
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p)                  // the smallest part first
+          for (int b = 0; b < MT; ++b) {
+            // one block to a tile: the accumulators are used in turn; two: each has its own
+            const uint32_t acc = MT == 1 ? n & 1 : b, use = MT == 1 ? n >> 1 : n;
+            if (place == 0 && !(ok = bar_wait<CG == 2>(freed + 8 * acc, (use & 1) ^ 1))) return false;
+            mma_fence_after();
 #pragma unroll
-            for (int j = 0; j < kDepth / kStepK; ++j)
-              mma<CG, false>(tmem + acc * BN, da + p * (S::kA >> 4) + j * kStepA, db + j * kStepB, id, place != 0 || p < PARTS - 1 || j != 0);
-          mma_commit<CG>(empty + 8 * s);
-          if (place == S::kChunk - 1 || k + 1 == w.k1) {
-            mma_commit<CG>(done + 8 * acc);
-            ++n;
+            for (int p = PARTS - 1; p >= 0; --p)                  // the smallest part first
+#pragma unroll
+              for (int j = 0; j < kDepth / kStepK; ++j)
+                mma<CG, false>(tmem + acc * BN, da + (b + p) * (S::kA >> 4) + j * kStepA, db + j * kStepB, id, place != 0 || p < PARTS - 1 || j != 0);
+            if (last) mma_commit<CG>(done + 8 * acc);
           }
+          mma_commit<CG>(empty + 8 * s);
+          n += last;
         }
         return true;
       });
     }
   } else {
-    const int quad = warp & 3;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + quad * S::kOut;
+    // (a group has a block of rows or, of a single block, every other block of columns)
+    const int quad = warp & 3, group = (warp - 2) / 4, block = MT == 1 ? 0 : group;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + (warp - 2) * S::kOut;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
-    static_assert(S::kOut >= 32 * kStageRow, "room for a ragged block");
+    static_assert(MT > 1 || S::kOut >= 32 * kStageRow, "room for a ragged block");
     uint32_t n = 0, puts = 0;
     constexpr int kC = 128 / sizeof(O);
     const float scale = DW ? *a.scale : 1.f;
     items([&](const Item& w) {
-      const uint32_t row = w.row + 128 * rank + quad * 32, running = tmem + lanes + 2 * BN;
+      const uint32_t within = block * 128 * CG + 128 * rank + quad * 32, row = w.row + within, running = tmem + lanes + 2 * BN;
       const uint32_t end = min(a.bn, a.n - w.col);
       const bool add = !DW && !a.begin && (uint32_t)w.share < before.shares(w.tile);
       // Blocks of kC columns; the last one of a tile begins early where the tile is not a whole number of them (what is
       // written twice that way is the same, what is added must not be).
       auto blocks = [&](auto&& f) {
 #pragma unroll 1
-        for (uint32_t c = 0; c < end; c += kC) {
+        for (uint32_t c = MT == 1 ? group * kC : 0; c < end; c += MT == 1 ? 2 * kC : kC) {
           const uint32_t over = c + kC > a.bn ? c + kC - a.bn : 0;
           f(c - over, over);
         }
@@ -231,22 +241,22 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
           O* out = static_cast<O*>(a.out) + (size_t)row * a.ldo + col;
           const int rows = row >= a.m ? 0 : (int)min(32u, a.m - row);
           if (w.share >= 0) {
-            float* part = a.part + ((size_t)w.share * CG * 128 + 128 * rank + quad * 32) * a.bn;
+            float* part = a.part + ((size_t)w.share * kTileM + within) * a.bn;
 #pragma unroll
             for (int i = 0; i < kC; i += 32) store_part(part + c + i, a.bn, v + i, lane);
-          } else if (!a.aligned) {
+          } else if (MT == 1 && !a.aligned) {
             if (col < a.n) store_ragged(out, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col), lane, raw + (stage - smem_addr(raw)));
           } else if (rows > 0) {
-            put_block<O>(&map_o, (int)col, (int)row, v, lane, stage, puts);
+            put_block<O, false, S::kPlaces>(&map_o, (int)col, (int)row, v, lane, stage, puts);
           }
         } else {
-          const int y = (int)((uint32_t)w.share * ranges.tiles_m * 128 * CG + row);
+          const int y = (int)((uint32_t)w.share * ranges.tiles_m * kTileM + row);
           if (add) {
 #pragma unroll
             for (int i = 0; i < kC; ++i) v[i] = i < (int)over ? 0.f : v[i];
-            put_block<float, true>(&map_o, (int)col, y, v, lane, stage, puts);
+            put_block<float, true, S::kPlaces>(&map_o, (int)col, y, v, lane, stage, puts);
           } else {
-            put_block<float>(&map_o, (int)col, y, v, lane, stage, puts);
+            put_block<float, false, S::kPlaces>(&map_o, (int)col, y, v, lane, stage, puts);
           }
         }
       };
@@ -260,10 +270,10 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
         return true;
       }
       for (uint32_t k = w.k0; k < w.k1; k += min((uint32_t)S::kChunk, w.k1 - k), ++n) {
-        const uint32_t acc = n & 1, from = tmem + lanes + acc * BN;
+        const uint32_t acc = MT == 1 ? n & 1 : block, from = tmem + lanes + acc * BN;
         const bool first = k == w.k0, last = w.k1 - k <= (uint32_t)S::kChunk;
-        ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-        if (!(ok = all_of<128>(ok))) return false;       // (the four warps leave together)
+        ok = bar_wait(done + 8 * acc, (MT == 1 ? n >> 1 : n) & 1);
+        if (!(ok = all_of<32 * kWriters / MT>(ok, 1 + block))) return false;       // (the warps of an accumulator leave together)
         mma_fence_after();
         blocks([&](uint32_t c, uint32_t over) {
           float v[kC];
@@ -403,7 +413,7 @@ uint32_t tile_columns(uint32_t n, uint32_t widest, uint32_t unit) {
 }
 
 struct DwPlan {
-  int cg, bn_max;
+  int cg, bn_max, mt;
   uint32_t bn, tiles_m, tiles, full, splits;
   double cost;
 };
@@ -411,21 +421,27 @@ struct DwPlan {
 // and an end, partial results go through memory once more.
 DwPlan dw_plan(const VocabDw& a, int sms) {
   const uint32_t ksteps = (a.r.most + kDepth - 1) / kDepth;
-  const int shapes[2][2][2] = {{{2, 256}, {1, 128}}, {{2, 128}, {1, 64}}};
+  // CTAs, widest tile, blocks of rows; time of the copies of a stage
+  const struct { int cg, bn, mt; double copies; } shapes[2][3] = {{{2, 256, 2, 800.0}, {2, 256, 1, 530.0}, {1, 128, 1, 530.0}},
+                                                                  {{2, 128, 1, 930.0}, {1, 64, 1, 930.0}, {0, 0, 0, 0.0}}};
   const int parts = a.f32 ? 3 : 1;
+  const size_t e = a.f32 ? 4 : 2;
   DwPlan best = {};
   double least = 1e300;
   for (const auto& sh : shapes[a.f32]) {
-    DwPlan p = {sh[0], sh[1], tile_columns(a.d, sh[1], a.f32 ? 32 : 16), (a.cols + 128 * sh[0] - 1) / (128 * sh[0]), 0, 0, 0, 0.0};
+    if (sh.cg == 0 || (sh.mt > 1 && !copy_fits(a.dw, a.d * e, a.lddw * e))) continue;
+    const uint32_t tile_m = 128 * sh.cg * sh.mt;
+    DwPlan p = {sh.cg, sh.bn, sh.mt, tile_columns(a.d, sh.bn, a.f32 ? 32 : 16), (a.cols + tile_m - 1) / tile_m, 0, 0, 0, 0.0};
     p.tiles = p.tiles_m * ((a.d + p.bn - 1) / p.bn);
-    const double stage = 2.0 * p.bn * parts + (p.cg == 1 ? 40.0 * parts : 0.0);
+    const double products = 2.0 * p.bn * parts * sh.mt, stage = products > sh.copies ? products : sh.copies;
     const uint64_t units = sms / p.cg, rounds = p.tiles / units, full = rounds * units, rest = p.tiles - full;
     for (uint32_t sp = 1; sp <= 32 && sp * 4 <= (ksteps < 4 ? 4 : ksteps); ++sp) {
-      const double part = sp > 1 ? (double)rest * sp * p.cg * 128 * p.bn : 0.0;
+      const double part = sp > 1 ? (double)rest * sp * tile_m * p.bn : 0.0;
       if (part * 4 > 128e6) break;      // (an eighth of a gigabyte of partial results at most)
-      double c = rounds * (ksteps * stage + 2500.0);
-      if (rest) c += (double)((rest * sp + units - 1) / units) * ((ksteps + sp - 1) / sp * stage + 2500.0);
-      if (sp > 1) c += (part * 8 + (double)rest * p.cg * 128 * p.bn * (a.f32 ? 4 : 2)) / 3000.0 + 4000.0;
+      const double ends = 2500.0 * sh.mt;
+      double c = rounds * (ksteps * stage + ends);
+      if (rest) c += (double)((rest * sp + units - 1) / units) * ((ksteps + sp - 1) / sp * stage + ends);
+      if (sp > 1) c += (part * 8 + (double)rest * tile_m * p.bn * e) / 3000.0 + 4000.0;
       if (c < least) {
         least = c;
         best = p;
@@ -439,10 +455,10 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
   return best;
 }
 
-template <int CG, int BN, int PARTS, bool DW, class O>
+template <int CG, int BN, int PARTS, int MT, bool DW, class O>
 cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const void* b, uint64_t b_rows, uint32_t b_cols, size_t ldb, void* out,
                    uint64_t out_rows, size_t ldo, uint64_t items, GradArgs g, int device, int sms, int* err, cudaStream_t stream) {
-  using S = GradShape<CG, BN, PARTS>;
+  using S = GradShape<CG, BN, PARTS, MT>;
   g.count = r.count;
   g.rows = r.rows;
   g.most = r.most;
@@ -455,28 +471,28 @@ cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const voi
   cudaError_t e = make_tensor_map(&mp, p, 2, (uint64_t)r.most * panels * PARTS, 64, 64, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess) e = make_tensor_map(&mb, b, 2, b_rows, b_cols, ldb, 64, 64, true);
   if (e == cudaSuccess && (!DW || g.aligned)) e = make_tensor_map(&mo, out, sizeof(O), out_rows, DW ? g.n : ldo, ldo, 32, 128 / sizeof(O), true);
-  auto* kernel = vocab_grad_kernel<CG, BN, PARTS, DW, O>;
+  auto* kernel = vocab_grad_kernel<CG, BN, PARTS, MT, DW, O>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, device, seen);
   if (e != cudaSuccess) return e;
   return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, g);
 }
 
-// Tiles of dx.  (A single tile of rows needs no pair.)
+// Tiles of dx: a single one for few tokens, and two blocks of rows where there are enough of them for every pair.
 struct DxShape {
-  int cg;
+  int cg, mt;
   uint32_t bn;
 };
-DxShape dx_shape(const VocabDx& a) {
-  const int cg = a.r.most > 128 ? 2 : 1;
-  return {cg, tile_columns(a.d, 128 * cg, 16)};
+DxShape dx_shape(uint32_t most, uint32_t d) {
+  const int cg = most > 128 ? 2 : 1;
+  return {cg, most >= 8192 ? 2 : 1, tile_columns(d, 128 * cg, 16)};
 }
 
 }  // namespace
 
 size_t vocab_dw_partial(const VocabDw& a, int sms) {
   const DwPlan p = dw_plan(a, sms);
-  return p.splits > 1 ? (size_t)(p.tiles - p.full) * p.splits * p.cg * 128 * p.bn : 0;
+  return p.splits > 1 ? (size_t)(p.tiles - p.full) * p.splits * p.cg * p.mt * 128 * p.bn : 0;
 }
 
 double vocab_dw_cost(const VocabDw& a, int sms) { return dw_plan(a, sms).cost; }
@@ -501,23 +517,26 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
     return launch_fn(a.r, a.p, a.panels, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, items, g, a.device, sms, err, stream);
   };
   if (a.f32)
-    rc = p.cg == 2 ? go(launch<2, 128, 3, true, float>) : go(launch<1, 64, 3, true, float>);
+    rc = p.cg == 2 ? go(launch<2, 128, 3, 1, true, float>) : go(launch<1, 64, 3, 1, true, float>);
   else
-    rc = p.cg == 2 ? go(launch<2, 256, 1, true, __nv_bfloat16>) : go(launch<1, 128, 1, true, __nv_bfloat16>);
+    rc = p.mt == 2   ? go(launch<2, 256, 1, 2, true, __nv_bfloat16>)
+         : p.cg == 2 ? go(launch<2, 256, 1, 1, true, __nv_bfloat16>)
+                     : go(launch<1, 128, 1, 1, true, __nv_bfloat16>);
   *launches = 1;
   if (rc != cudaSuccess || p.splits == 1) return rc;
   ++*launches;
-  return launch_join(part, p.splits, p.cg * 128, p.bn, p.full, p.tiles - p.full, p.tiles / p.tiles_m, true, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
+  return launch_join(part, p.splits, p.cg * p.mt * 128, p.bn, p.full, p.tiles - p.full, p.tiles / p.tiles_m, true, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
 }
 
-size_t vocab_dx_rows(uint32_t most, size_t ldd) {
+size_t vocab_dx_rows(uint32_t most, uint32_t d, size_t ldd) {
   // two planes, and for few tokens more, as long as they are small
-  const size_t fit = (16u << 20) / ldd;
-  return 2 * (size_t)most > fit ? 2 * (size_t)most : fit;
+  const DxShape s = dx_shape(most, d);
+  const size_t fit = (16u << 20) / ldd, two = 2 * (size_t)up(most, 128 * s.cg * s.mt);
+  return two > fit ? two : fit;
 }
 
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream) {
-  const DxShape s = dx_shape(a);
+  const DxShape s = dx_shape(a.r.most, a.d);
   GradArgs g = {};
   g.n = a.d;
   g.bn = s.bn;
@@ -525,19 +544,20 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
   g.first = (a.first + kDepth - 1) / kDepth;
   g.plane_rows = a.plane_rows;
   g.begin = a.begin;
-  const uint64_t items = sms / s.cg;
-  if (s.cg == 2)
-    return launch<2, 256, 1, false, float>(a.r, a.p, a.panels, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
-  return launch<1, 128, 1, false, float>(a.r, a.p, a.panels, a.w, a.cols, a.d, a.ldw, a.planes, a.plane_rows, a.ldd, items, g, a.device, sms, err, stream);
+  const auto go = [&](auto launch_fn) {
+    return launch_fn(a.r, a.p, a.panels, a.w, (uint64_t)a.cols, a.d, a.ldw, a.planes, (uint64_t)a.plane_rows, a.ldd, (uint64_t)(sms / s.cg), g, a.device,
+                     sms, err, stream);
+  };
+  return s.mt == 2 ? go(launch<2, 256, 1, 2, false, float>) : s.cg == 2 ? go(launch<2, 256, 1, 1, false, float>) : go(launch<1, 128, 1, 1, false, float>);
 }
 
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream) {
-  const DxShape s = dx_shape(a);
+  const DxShape s = dx_shape(a.r.most, a.d);
   // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
   uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
   if (each > 8) each = 8;
   return launch_with(dx_finish_kernel, dim3((t + each - 1) / each), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
-                     a.r.row, (uint32_t)(128 * s.cg), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), a.r.scale, t, each, a.d,
+                     a.r.row, (uint32_t)(128 * s.cg * s.mt), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), a.r.scale, t, each, a.d,
                      static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2));
 }
 

@@ -120,7 +120,7 @@ def test_loss_and_gradients(handle, t, d, v, dtype):
 
 
 def test_many_pieces_of_the_vocabulary(handle):
-    """The gradients of the logits of 9000 tokens exist for 14336 entries at a time (4608 in three parts): three pieces, and seven."""
+    """The gradients of the logits of 9000 tokens exist for some 28000 entries at a time (9000 in three parts): two pieces, and four."""
     x, w, target, b, dloss = inputs(9000, 72, 30001, 5, True, 0.1)
     d = Definition(x, w, target, b, dloss)
     for dtype in (BF, F32):

@@ -1,16 +1,19 @@
-"""Builds libstq.so (the C-ABI library) in-tree with nvcc for sm_100a."""
+"""Builds libstq.so (the C-ABI library) in-tree with nvcc for sm_100a, and _lists.so (a Python module over torch's headers)."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstq.so")
+LISTS, LISTS_SOURCE = os.path.join(HERE, "_lists.so"), os.path.join(CSRC, "stq_lists.cpp")
 SOURCES = ["stq_step_fast.cu", "stq_step_variants.cu", "stq_step_split.cu", "stq_kernels.cu", "stq_static_stats.cu",
            "stq_q8_rows.cu", "stq_q8_linear.cu", "stq_q8_grad.cu", "stq_q8_tma.cpp", "stq_q8_api.cu",
-           "stq_vocab_scores.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_clip.cu",
+           "stq_vocab_scores.cu", "stq_vocab_few.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_clip.cu",
            "stq_api.cu", "stq_policy.cpp"]
 HEADERS = [os.path.join(CSRC, "stq_internal.h"), os.path.join(CSRC, "stq_handle.h"), os.path.join(CSRC, "stq_q8.h"),
            os.path.join(CSRC, "stq_q8_mma.cuh"), os.path.join(CSRC, "stq_q8_tma.h"), os.path.join(CSRC, "stq_q8_ring.h"),
@@ -33,15 +36,31 @@ def nvcc() -> str:
     raise RuntimeError("nvcc not found")
 
 
-def stale() -> bool:
-    if not os.path.exists(LIB):
+def older(target: str, deps) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
+    t = os.path.getmtime(target)
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def stale() -> bool:
+    return older(LIB, [os.path.join(CSRC, s) for s in SOURCES] + HEADERS)
+
+
+def build_lists(force: bool = False) -> str:
+    if not force and not older(LISTS, [LISTS_SOURCE, HEADERS[-1]]):
+        return LISTS
+    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
+    inc, tmp = os.path.join(torch_dir, "include"), LISTS + f".tmp{os.getpid()}"
+    subprocess.check_call([
+        "g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-I{inc}", f"-I{inc}/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
+        "-o", tmp, LISTS_SOURCE, f"-L{torch_dir}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, LISTS)
+    return LISTS
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_lists(force)
     if not force and not stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"

@@ -63,6 +63,10 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* c
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s);
 cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, float2* part, int sms, int* err, cudaStream_t stream);
+// The same for few tokens, without tiles (stq_vocab_few.cu): how many parts there are then, or 0 if there are too many tokens or
+// columns for it.  x and ldx: the hidden states as they were given.
+uint32_t vocab_few_parts(uint32_t t, uint32_t v, uint32_t d, int sms);
+cudaError_t launch_vocab_few(const VocabArgs& a, const void* x, size_t ldx, float2* part, int sms, cudaStream_t stream);
 // loss and lse of all tokens from the parts.  x and ldx: the tokens' hidden states as they were given.
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
                                 float* lse, cudaStream_t stream);

@@ -144,7 +144,8 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   Rows r(a, x, ldx, false);
   const uint32_t most = most_rows(a.t);
   const VocabShape shape = vocab_shape(a.t, v, d, h->sm_count);
-  const uint32_t parts = vocab_parts(a, shape);
+  const uint32_t few = t <= kTokensAtOnce ? vocab_few_parts(a.t, v, d, h->sm_count) : 0, parts = few ? few : vocab_parts(a, shape);
+  if (few) r.gather = false;
   Arena m;
   float2* part = nullptr;
   for (int pass = 0; pass < 2; ++pass) {
@@ -160,7 +161,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
     int launches = 2;
     STQ_CUDA(h, prepare_rows(b, r, xb, ldx, nullptr, t0 == 0, s, &launches));
-    STQ_CUDA(h, launch_vocab_parts(b, shape, part, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, few ? launch_vocab_few(b, xb, ldx, part, h->sm_count, s) : launch_vocab_parts(b, shape, part, h->sm_count, h->d_err, s));
     STQ_CUDA(h, launch_vocab_finish(b, xb, ldx, part, parts, loss + t0, lse + t0, s));
     h->launches += launches;
   }

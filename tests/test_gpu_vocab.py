@@ -110,6 +110,19 @@ SIZES = [(1, 1, 1), (1, 64, 100), (1, 1600, 1283), (2, 8, 2), (3, 77, 131), (61,
          (5000, 32, 77)]
 
 
+@pytest.mark.parametrize("d", [1, 7, 8, 33, 250, 1000, 1024, 1032, 1601, 2050, 4096, 5000])
+@pytest.mark.parametrize("t", [1, 3, 8, 9, 16, 17])
+def test_few_tokens(handle, t, d):
+    """Up to 16 tokens (and as many as their shared memory holds) go by the matrix, read in other steps than tiles."""
+    for v in (1, 15, 16, 17, 250, 9001):
+        x, w, target, b, dloss = inputs(t, d, v, t + d + v, v % 2 == 1, 0.2 if t > 2 else 0.0)
+        out = vocab.loss(handle, x, w, target, bias=b)
+        Definition(x, w, target, b, dloss).check(out, None, BF, f"{t} {d} {v}")
+        wp, xp = pitched(w, 8 + (-d) % 8, 0, float("nan")), pitched(x, 3, 1, float("nan"))      # (rows of w stay aligned)
+        again = vocab.loss(handle, xp, wp, target, bias=b)
+        assert torch.equal(out.lse, again.lse)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("t,d,v", SIZES)
 def test_loss_and_gradients(handle, t, d, v, dtype):
@@ -211,7 +224,7 @@ def test_targets_outside_the_vocabulary_give_nan(handle, t):
         assert torch.equal(out.loss[others], want_out.loss[others]) and torch.equal(grads.dx[others], want.dx[others])
 
 
-@pytest.mark.parametrize("t", [60, 400])
+@pytest.mark.parametrize("t", [12, 60, 400])
 def test_entries_out_of_the_vocabulary(handle, t):
     """A bias of -inf, or of the lowest number: probability 0, no gradient, also where they fill whole tiles."""
     x, w, target, b, dloss = inputs(t, 64, 1500, 4, True)
@@ -233,7 +246,7 @@ def test_entries_out_of_the_vocabulary(handle, t):
     assert o.loss[3] == float("inf") and torch.equal(o.lse[4:], vocab.loss(handle, x, w, target, bias=torch.where(live, b, -float("inf"))).lse[4:])
 
 
-@pytest.mark.parametrize("t", [60, 400])
+@pytest.mark.parametrize("t", [12, 60, 400])
 def test_infinities_and_nan_stay_in_their_row(handle, t):
     x, w, target, b, dloss = inputs(t, 64, 900, 4)
     want_out, want = run(handle, x, w, target, b, dloss, BF)

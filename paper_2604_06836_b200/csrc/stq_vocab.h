@@ -100,7 +100,9 @@ struct VocabDw {
 };
 size_t vocab_dw_partial(const VocabDw& a, int sms);
 double vocab_dw_cost(const VocabDw& a, int sms);      // in clock cycles
-cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches);
+cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream);
+// Adds shares of tiles up, if the plan has any.
+cudaError_t launch_vocab_dw_join(const VocabDw& a, const float* part, int sms, cudaStream_t stream, int* launches);
 
 // planes[c][row][:] (+)= share c of the sum over [v0, v0 + cols) of p[row][i] w[v0 + i][:].  The sums of all tiles, one after
 // the other, are cut into equal ranges, one for each pair of CTAs; what different pairs have of a tile goes to different planes.
@@ -113,6 +115,7 @@ struct VocabDx {
   size_t ldw;
   uint32_t cols, d, first;
   bool begin;                 // the first piece
+  bool beside;                // launched right after dw of the same piece
   float* planes;
   size_t ldd;                 // columns of a plane, a multiple of 32
   uint32_t plane_rows;        // rows of all planes together

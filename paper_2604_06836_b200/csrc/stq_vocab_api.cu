@@ -258,19 +258,20 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
       ++launches;
     }
     if (dw) {
-      int more = 0;
       gw.cols = n;
       gw.dw = static_cast<uint8_t*>(dw) + (size_t)v0 * lddw * e;
-      STQ_CUDA(h, launch_vocab_dw(gw, part, h->sm_count, h->d_err, s, &more));
-      launches += more;
+      STQ_CUDA(h, launch_vocab_dw(gw, part, h->sm_count, h->d_err, s));
+      ++launches;
     }
     if (dx) {
       gx.cols = n;
       gx.begin = v0 == 0;
+      gx.beside = dw != nullptr;
       gx.w = static_cast<const uint16_t*>(a.w) + (size_t)v0 * a.ldw;
       STQ_CUDA(h, launch_vocab_dx(gx, h->sm_count, h->d_err, s));
       ++launches;
     }
+    if (dw) STQ_CUDA(h, launch_vocab_dw_join(gw, part, h->sm_count, s, &launches));
   }
   if (dx) {
     STQ_CUDA(h, launch_vocab_dx_finish(gx, last, a.t, dx, lddx, h->sm_count, s));

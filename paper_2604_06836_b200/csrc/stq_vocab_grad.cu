@@ -44,7 +44,7 @@ struct GradArgs {
   // dx
   uint32_t ksteps, first;              // stages of this piece and of the first one
   uint32_t plane_rows;
-  int begin;
+  int begin, beside;
   int* err;
 };
 
@@ -107,7 +107,9 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
   mma_fence_before();
   __syncthreads();
   if (CG == 2) cluster_sync_all();
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // dx does not need what the kernel before it, dw's, computes: once that one has begun, all that came before it is done.  It starts on
+  // SMs that dw has no more work for, and ends after it (below).
+  if (DW || !a.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   mma_fence_after();
   const uint32_t tmem = tmem_slot;
@@ -305,6 +307,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     });
     store_blocks_done(lane);
   }
+  if (!DW && a.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!ok) *a.err = 1;
   __syncwarp();
   mma_fence_before();
@@ -497,7 +500,7 @@ size_t vocab_dw_partial(const VocabDw& a, int sms) {
 
 double vocab_dw_cost(const VocabDw& a, int sms) { return dw_plan(a, sms).cost; }
 
-cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream, int* launches) {
+cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cudaStream_t stream) {
   const DwPlan p = dw_plan(a, sms);
   GradArgs g = {};
   g.n = a.d;
@@ -522,8 +525,12 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
     rc = p.mt == 2   ? go(launch<2, 256, 1, 2, true, __nv_bfloat16>)
          : p.cg == 2 ? go(launch<2, 256, 1, 1, true, __nv_bfloat16>)
                      : go(launch<1, 128, 1, 1, true, __nv_bfloat16>);
-  *launches = 1;
-  if (rc != cudaSuccess || p.splits == 1) return rc;
+  return rc;
+}
+
+cudaError_t launch_vocab_dw_join(const VocabDw& a, const float* part, int sms, cudaStream_t stream, int* launches) {
+  const DwPlan p = dw_plan(a, sms);
+  if (p.splits == 1) return cudaSuccess;
   ++*launches;
   return launch_join(part, p.splits, p.cg * p.mt * 128, p.bn, p.full, p.tiles - p.full, p.tiles / p.tiles_m, true, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
 }
@@ -544,6 +551,7 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
   g.first = (a.first + kDepth - 1) / kDepth;
   g.plane_rows = a.plane_rows;
   g.begin = a.begin;
+  g.beside = a.beside;
   const auto go = [&](auto launch_fn) {
     return launch_fn(a.r, a.p, a.panels, a.w, (uint64_t)a.cols, a.d, a.ldw, a.planes, (uint64_t)a.plane_rows, a.ldd, (uint64_t)(sms / s.cg), g, a.device,
                      sms, err, stream);

@@ -34,6 +34,7 @@ constexpr int kScan = 8;               // targets that a thread has on the way
 
 // Every CTA counts the targets before its tokens and in all, so that nothing has to be passed between CTAs.
 __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ uint32_t sums[2][8];
   __shared__ float tops[8];
@@ -104,9 +105,19 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
     }
   } else {
     const uint32_t per_row = (a.d + 255) / 256;
-    for (uint32_t i = warp; i < kGatherRows * per_row; i += 8) {
-      const uint32_t r = i / per_row, part = i - r * per_row;
-      if (where[r] >= 0) copy_row_part(x + (size_t)(t0 + r) * a.ldx, a.d, part * 256, out + (size_t)where[r] * a.ldo, lane);
+    for (uint32_t i0 = warp; i0 < kGatherRows * per_row; i0 += 8 * 4) {
+      RowPart p[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t i = i0 + 8 * j, r = i / per_row;
+        if (i < kGatherRows * per_row && where[r] >= 0) p[j].load(x + (size_t)(t0 + r) * a.ldx, a.d, (i - r * per_row) * 256, lane);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t i = i0 + 8 * j, r = i / per_row;
+        if (i < kGatherRows * per_row && where[r] >= 0)
+          p[j].store(x + (size_t)(t0 + r) * a.ldx, a.d, (i - r * per_row) * 256, out + (size_t)where[r] * a.ldo, lane);
+      }
     }
   }
   // the rest of the last tile: what is multiplied with zeros must be finite
@@ -403,7 +414,9 @@ __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const ui
       if (to < 0 || to >= (int64_t)a.v) {
         z = __int_as_float(0x7fc00000);
       } else {
-        const uint16_t *p = x + (size_t)t * ldx, *q = w + (size_t)to * a.ldw;
+        // (a gathered row is aligned; it was there before the products began)
+        const uint16_t *p = a.r.row ? static_cast<const uint16_t*>(a.r.x) + (size_t)a.r.row[t] * a.r.ldx : x + (size_t)t * ldx;
+        const uint16_t* q = w + (size_t)to * a.ldw;
         float s[2] = {0.f, 0.f};
         if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
           const uint32_t whole = a.d & ~7u;
@@ -434,6 +447,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const ui
   const int mine = threadIdx.x % R, group = threadIdx.x / R;
   const uint32_t t = t0 + mine;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");
   int32_t row = -1;
   if (t < a.t) row = a.r.row ? a.r.row[t] : a.target[t] != a.ignore ? (int32_t)t : -1;
   float2 sum = make_float2(-INFINITY, 0.f);
@@ -495,8 +509,7 @@ cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, cons
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
   GatherArgs g = a;
   g.aligned = rows_aligned(a.x, a.ldx * 2) && a.d % 8 == 0;
-  gather_kernel<<<(a.t + kGatherRows - 1) / kGatherRows, 256, 0, stream>>>(g);
-  return cudaGetLastError();
+  return launch_with(gather_kernel, dim3((a.t + kGatherRows - 1) / kGatherRows), dim3(256), 0, 1, true, stream, g);
 }
 
 VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* cost) {

@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libstq.so")
 LISTS, LISTS_SOURCE = os.path.join(HERE, "_lists.so"), os.path.join(CSRC, "stq_lists.cpp")
 SOURCES = ["stq_step_fast.cu", "stq_step_variants.cu", "stq_step_split.cu", "stq_kernels.cu", "stq_static_stats.cu",
            "stq_q8_rows.cu", "stq_q8_linear.cu", "stq_q8_grad.cu", "stq_q8_tma.cpp", "stq_q8_api.cu",
-           "stq_vocab_scores.cu", "stq_vocab_few.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_clip.cu",
+           "stq_vocab_scores.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_clip.cu",
            "stq_api.cu", "stq_policy.cpp"]
 HEADERS = [os.path.join(CSRC, "stq_internal.h"), os.path.join(CSRC, "stq_handle.h"), os.path.join(CSRC, "stq_q8.h"),
            os.path.join(CSRC, "stq_q8_mma.cuh"), os.path.join(CSRC, "stq_q8_tma.h"), os.path.join(CSRC, "stq_q8_ring.h"),

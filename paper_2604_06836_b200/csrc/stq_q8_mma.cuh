@@ -216,14 +216,14 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// True if `ok` is true in all of the N threads that share barrier `id` (whole warps); a barrier for them too.
+// True if `ok` is true in all of the N threads that share barrier 1 (whole warps); a barrier for them too.
 template <int N>
-__device__ __forceinline__ bool all_of(bool ok, int id = 1) {
+__device__ __forceinline__ bool all_of(bool ok) {
   uint32_t r;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %3, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"((uint32_t)ok), "n"(N), "r"(id)
+      : "r"((uint32_t)ok), "n"(N)
       : "memory");
   return r != 0;
 }

@@ -53,20 +53,18 @@ struct GatherArgs {
 };
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
 
-// Tiles of the products: `cg` CTAs share 128 * cg rows and `bn` columns.
+// Tiles of the products: `cg` CTAs share 128 * cg rows and `wide` entries of the vocabulary.  The loss takes any width that the matrix
+// units do, the gradients whole panels (below).  cost, if wanted: the time in clock cycles.
 struct VocabShape {
-  int cg, bn;
+  int cg;
+  uint32_t wide;
 };
-// (cost, if wanted: the time in clock cycles)
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* cost = nullptr);
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int sms, double* cost = nullptr);
 
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
-uint32_t vocab_parts(const VocabArgs& a, VocabShape s);
-cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, float2* part, int sms, int* err, cudaStream_t stream);
-// The same for few tokens, without tiles (stq_vocab_few.cu): how many parts there are then, or 0 if there are too many tokens or
-// columns for it.  x and ldx: the hidden states as they were given.
-uint32_t vocab_few_parts(uint32_t t, uint32_t v, uint32_t d, int sms);
-cudaError_t launch_vocab_few(const VocabArgs& a, const void* x, size_t ldx, float2* part, int sms, cudaStream_t stream);
+uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms);
+// (most: the one that the parts were counted for)
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, float2* part, int sms, int* err, cudaStream_t stream);
 // loss and lse of all tokens from the parts.  x and ldx: the tokens' hidden states as they were given.
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
                                 float* lse, cudaStream_t stream);

@@ -37,7 +37,7 @@ struct Rows {
   Rows(const VocabArgs& a, const void* x_, size_t ldx_, bool backward) {
     // For a loss of up to one tile of tokens there is nothing to gain from leaving some out.  (For dw there is: what a token
     // without a loss holds may be NaN, and its product with 0 too.)
-    gather = backward || a.t > 128 || !rows_aligned(x_, a.t > 1 ? ldx_ * 2 : 0);
+    gather = backward || a.t > 256 || !rows_aligned(x_, a.t > 1 ? ldx_ * 2 : 0);
     pitch_w = !rows_aligned(a.w, a.v > 1 ? a.ldw * 2 : 0);
     ldx = up(a.d, 8);
     ldw = up(a.d, 8);
@@ -90,7 +90,7 @@ uint32_t piece_of(const VocabArgs& a, VocabDw g, size_t entry, bool dw, int sms)
   const uint32_t widest = fit < 1 ? 1 : (uint32_t)fit;
   auto cost = [&](uint32_t cols) {
     double c, extra = 60000.0;      // (of a piece: launches, beginnings and ends)
-    vocab_shape(a.t, cols, a.d, sms, &c);
+    vocab_shape(a.t, cols, a.d, true, sms, &c);
     g.cols = cols;
     return c + extra + (dw ? vocab_dw_cost(g, sms) : 0.0);
   };
@@ -143,9 +143,8 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   a.target = target;
   Rows r(a, x, ldx, false);
   const uint32_t most = most_rows(a.t);
-  const VocabShape shape = vocab_shape(a.t, v, d, h->sm_count);
-  const uint32_t few = t <= kTokensAtOnce ? vocab_few_parts(a.t, v, d, h->sm_count) : 0, parts = few ? few : vocab_parts(a, shape);
-  if (few) r.gather = false;
+  const VocabShape shape = vocab_shape(a.t, v, d, false, h->sm_count);
+  const uint32_t parts = vocab_parts(a, shape, most, h->sm_count);
   Arena m;
   float2* part = nullptr;
   for (int pass = 0; pass < 2; ++pass) {
@@ -161,7 +160,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
     int launches = 2;
     STQ_CUDA(h, prepare_rows(b, r, xb, ldx, nullptr, t0 == 0, s, &launches));
-    STQ_CUDA(h, few ? launch_vocab_few(b, xb, ldx, part, h->sm_count, s) : launch_vocab_parts(b, shape, part, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, launch_vocab_parts(b, shape, most, part, h->sm_count, h->d_err, s));
     STQ_CUDA(h, launch_vocab_finish(b, xb, ldx, part, parts, loss + t0, lse + t0, s));
     h->launches += launches;
   }
@@ -250,7 +249,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   for (uint32_t v0 = 0; v0 < v; v0 += cols) {
     const uint32_t n = v - v0 < cols ? v - v0 : cols;
     o.dbias = db_part && db_once ? db_part + v0 : db_part;
-    STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, true, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
     ++launches;
     const bool all = v0 + n == v;
     if (dbias && (!db_once || all)) {

@@ -138,12 +138,13 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
       }
     } else {
       if (unit >= ranges.U) return;
-      const uint64_t end = ranges.begin(unit + 1);
-      for (uint64_t s = ranges.begin(unit); s < end;) {
+      const uint32_t u = ranges.unit(unit);
+      const uint64_t end = ranges.begin(u + 1);
+      for (uint64_t s = ranges.begin(u); s < end;) {
         const uint32_t q = (uint32_t)(s / ranges.ksteps), tile = ranges.tile(q);
         const uint64_t t0 = (uint64_t)q * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
         const Item it = {tile, tile / tiles_n * kTileM, tile % tiles_n * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
-                         (int)(unit - ranges.unit_of(t0))};
+                         (int)(u - ranges.unit_of(t0))};
         if (!f(it)) return;
         s = stop;
       }
@@ -275,7 +276,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
         const uint32_t acc = MT == 1 ? n & 1 : block, from = tmem + lanes + acc * BN;
         const bool first = k == w.k0, last = w.k1 - k <= (uint32_t)S::kChunk;
         ok = bar_wait(done + 8 * acc, (MT == 1 ? n >> 1 : n) & 1);
-        if (!(ok = all_of<32 * kWriters / MT>(ok, 1 + block))) return false;       // (the warps of an accumulator leave together)
+        if (!(ok = __all_sync(0xffffffffu, ok))) return false;
         mma_fence_after();
         blocks([&](uint32_t c, uint32_t over) {
           float v[kC];
@@ -481,7 +482,7 @@ cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const voi
   return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, g);
 }
 
-// Tiles of dx: a single one for few tokens, and two blocks of rows where there are enough of them for every pair.
+// Tiles of dx: a CTA's for few tokens, and two blocks of rows where there are enough of them for every pair.
 struct DxShape {
   int cg, mt;
   uint32_t bn;

@@ -12,20 +12,27 @@ namespace stq {
 
 // Tiles of dx, row by row, and which units (CTAs or pairs) add to which: unit u has stages [u S / U, (u + 1) S / U) of the S = tiles * ksteps.
 struct Ranges {
-  uint32_t tiles_m, tiles, ksteps, U;
+  uint32_t tiles_m, tiles, ksteps, U, split;
   uint64_t S;
   STQ_BOTH Ranges(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t k, uint32_t units, uint32_t plane_rows) {
     tiles_m = (rows + tile_m - 1) / tile_m;
     tiles = tiles_m * tiles_n;
     ksteps = k;
     S = (uint64_t)tiles * k;
-    U = 0;
+    U = split = 0;
     if (S == 0) return;
     // so long a range that no tile has more units than there are planes
     const uint32_t planes = plane_rows / (tiles_m * tile_m), least = planes > 2 ? (k + planes - 2) / (planes - 1) : k;
     const uint64_t most = ratio(S, least);
     U = (uint32_t)(units < most ? units : most);
+    // few tiles: every tile in as many ranges, if that leaves no more than a sixteenth of the units without one.  Then those that have
+    // the same share of a row of tiles run side by side, and read whole rows of w together.
+    const uint32_t even = U > tiles ? U / tiles * tiles : 0;
+    split = even && U - even <= U / 16 ? even / tiles : 0;
+    if (split) U = even;
   }
+  // The unit whose range the i-th CTA or pair takes.
+  STQ_BOTH uint32_t unit(uint32_t i) const { return split ? i % tiles * split + i / tiles : i; }
   STQ_BOTH uint64_t begin(uint32_t u) const { return ratio(u * S, U); }
   STQ_BOTH uint32_t unit_of(uint64_t s) const { return (uint32_t)ratio((s + 1) * U - 1, S); }
   // (a division of 64 bits takes a GPU ten times as long)

@@ -131,6 +131,9 @@ struct ScoreArgs {
   const uint32_t* count;
   uint32_t rows, most;
   uint32_t v0, v1, ksteps, tiles_n;
+  uint32_t wide;           // entries of the vocabulary to a tile, at most BN
+  int merge;               // the loss of a single tile of rows: a CTA's tiles make one part
+  uint32_t stage_bytes;    // that are copied to a stage (of a CTA)
   const float* bias;
   // loss
   float2* part;
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES>::kThreads), 1)
 score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_p,
              const ScoreArgs a) {
   using S = ScoreShape<CG, BN, PLANES>;
-  constexpr int kStages = S::kStages, kNB = BN / CG;
+  constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
   __shared__ uint32_t tmem_slot;
@@ -219,12 +222,12 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       uint32_t it = 0;
       const uint32_t full0 = CG == 2 ? peer_addr(full, 0) : full;
       for (uint32_t w = unit; ok && w < tiles; w += units) {
-        const int row = (int)(w % tiles_m * 128 * CG + 128 * rank), col = (int)(a.v0 + w / tiles_m * BN + kNB * rank);
+        const int row = (int)(w % tiles_m * 128 * CG + 128 * rank), col = (int)(a.v0 + w / tiles_m * a.wide + a.wide / CG * rank);
         for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
           const uint32_t s = it % kStages, ph = (it / kStages) & 1;
           if (!(ok = bar_wait(empty + 8 * s, ph ^ 1))) break;
           const uint32_t at = ring + s * S::kStage;
-          if (leader) bar_expect(full + 8 * s, CG * S::kStage);
+          if (leader) bar_expect(full + 8 * s, CG * a.stage_bytes);
           tensor_load<CG>(at, &map_x, (int)(k * kDepth), row, full0 + 8 * s);
           tensor_load<CG>(at + S::kA, &map_w, (int)(k * kDepth), col, full0 + 8 * s);
         }
@@ -234,7 +237,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     }
   } else if (warp == 1) {
     if (leader && elect_one()) {
-      constexpr uint32_t id = idesc(kIdescBf16, 128 * CG, BN, false, false);
+      const uint32_t id = idesc(kIdescBf16, 128 * CG, (int)a.wide, false, false);
       uint32_t it = 0, n = 0;
       for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
         const uint32_t acc = n & 1;
@@ -257,10 +260,12 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     const int quad = warp & 3, half = (warp - 2) / 4;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
     uint32_t n = 0, puts = 0;
+    float m = -INFINITY, s = 0.f;      // the loss: maximum and sum of exp of this row over a part
     for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
       const uint32_t acc = n & 1, from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN + half * (BN / 2);
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
-      const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * BN + half * (BN / 2);
+      const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + half * (BN / 2);
+      const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
       // gradients: what this row is multiplied with, its normaliser and its target, if that lies in these columns
       float g = 0.f, lse = 0.f;
       int32_t hit = -1;
@@ -280,10 +285,10 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       float bias[BN / 64];      // of column 32 i + lane
       if (a.bias) {
 #pragma unroll
-        for (int i = 0; i < BN / 64; ++i) bias[i] = col0 + 32 * i + lane < a.v1 ? __ldg(a.bias + col0 + 32 * i + lane) : 0.f;
+        for (int i = 0; i < BN / 64; ++i) bias[i] = col0 + 32 * i + lane < end ? __ldg(a.bias + col0 + 32 * i + lane) : 0.f;
       }
       ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-      if (!(ok = all_of<32 * kWriters>(ok))) break;       // (the writing warps leave together)
+      if (!(ok = __all_sync(0xffffffffu, ok))) break;
       mma_fence_after();
       auto add_bias = [&](float(&v)[32], float mine) {
         if (a.bias) {
@@ -292,18 +297,17 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
       };
       if constexpr (PLANES == 0) {
-        float m = -INFINITY, s = 0.f;
 #pragma unroll
         for (int c = 0; c < BN / 2; c += 32) {
           const uint32_t col = col0 + c;
-          if (col >= a.v1) break;
+          if (col >= end) break;
           float v[32];
           load_block(from + c, v);
           add_bias(v, bias[c / 32]);
-          if (col + 32 > a.v1) {
+          if (col + 32 > end) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (col + i >= a.v1) v[i] = -INFINITY;
+              if (col + i >= end) v[i] = -INFINITY;
           }
           float tops[4] = {m, m, m, m};
 #pragma unroll
@@ -323,13 +327,18 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           s = __fadd_rn(s, __fadd_rn(__fadd_rn(more[0].x, more[0].y), __fadd_rn(more[1].x, more[1].y)));
           m = top;
         }
-        if (row < a.most) a.part[(size_t)(2 * tile + half) * a.most + row] = make_float2(m, s);
+        const uint32_t part = a.merge ? unit : tile;
+        if (!a.merge || w + units >= tiles) {
+          if (row < a.most) a.part[(size_t)(2 * part + half) * a.most + row] = make_float2(m, s);
+          m = -INFINITY;
+          s = 0.f;
+        }
       } else {
         const uint32_t out = outs + (warp - 2) * 2 * 4096;
 #pragma unroll
         for (int c = 0; c < BN / 2; c += 64) {
           const uint32_t col = col0 + c;
-          if (col >= a.v1) break;
+          if (col >= end) break;
           float v[64];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -347,10 +356,10 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
               b[i] = real ? p.x : 0.f;
               b[i + 1] = real ? p.y : 0.f;
             }
-            if (col + 32 * h + 32 > a.v1) {
+            if (col + 32 * h + 32 > end) {
 #pragma unroll
               for (int i = 0; i < 32; ++i)
-                if (col + 32 * h + i >= a.v1) b[i] = 0.f;
+                if (col + 32 * h + i >= end) b[i] = 0.f;
             }
           }
           if (a.dbias) {
@@ -477,31 +486,42 @@ __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const ui
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
+// CTAs or pairs of them that a product is launched with.
+uint32_t units_of(VocabShape s, uint32_t rows, uint32_t tiles_n, int sms) {
+  const uint64_t items = (uint64_t)((rows + 128 * s.cg - 1) / (128 * s.cg)) * tiles_n, most = sms / s.cg;
+  return (uint32_t)(items < most ? items : most);
+}
+bool merged(VocabShape s, uint32_t most) { return most <= 128u * s.cg; }
+
 template <int CG, int BN, int PLANES>
-cudaError_t launch(const VocabArgs& a, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
+cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
   using S = ScoreShape<CG, BN, PLANES>;
   s.count = a.r.count;
   s.rows = a.r.rows;
   s.most = a.r.most;
   s.bias = a.bias;
   s.ksteps = (a.d + kDepth - 1) / kDepth;
-  s.tiles_n = (s.v1 - s.v0 + BN - 1) / BN;
+  // few tokens: no more rows are copied than there are, in steps of the swizzle's eight (rows of zeros behind the matrix take longer
+  // than others: 17 tokens, 1600 x 50257, 45 us with 128 rows, 33 with 24; what a product reads behind them is what an earlier stage
+  // left, and stays in its rows)
+  const uint32_t rows = CG == 1 && a.r.rows < 128 ? (a.r.rows + 7) / 8 * 8 : 128;
+  s.wide = sh.wide;
+  s.tiles_n = (s.v1 - s.v0 + s.wide - 1) / s.wide;
+  s.stage_bytes = (rows + s.wide / CG) * kDepth * 2;
   CUtensorMap mx, mw, mp = {};
-  cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, 128, kDepth, true);
-  if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, BN / CG, kDepth, true);
+  cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, rows, kDepth, true);
+  if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, s.wide / CG, kDepth, true);
   if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->panels * o->planes, 64, 64, 32, 64, true);
   auto* kernel = score_kernel<CG, BN, PLANES>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, a.device, seen);
   if (e != cudaSuccess) return e;
-  const uint64_t items = (uint64_t)((a.r.rows + 128 * CG - 1) / (128 * CG)) * s.tiles_n, most = sms / CG;
-  return launch_with(kernel, (unsigned)(items < most ? items : most) * CG, S::kThreads, S::kSmem, CG, true, stream, mx, mw, mp, s);
+  return launch_with(kernel, units_of(sh, a.r.rows, s.tiles_n, sms) * CG, S::kThreads, S::kSmem, CG, true, stream, mx, mw, mp, s);
 }
 
 template <int PLANES>
 cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
-  if (sh.bn == 256) return launch<2, 256, PLANES>(a, s, o, sms, stream);
-  return launch<1, 128, PLANES>(a, s, o, sms, stream);
+  return sh.cg == 2 ? launch<2, 256, PLANES>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES>(a, sh, s, o, sms, stream);
 }
 
 }  // namespace
@@ -509,29 +529,44 @@ cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, cons
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
   GatherArgs g = a;
   g.aligned = rows_aligned(a.x, a.ldx * 2) && a.d % 8 == 0;
-  return launch_with(gather_kernel, dim3((a.t + kGatherRows - 1) / kGatherRows), dim3(256), 0, 1, true, stream, g);
+  const uint32_t ctas = (a.t + kGatherRows - 1) / kGatherRows;      // (more of them for few tokens: there are rows of zeros to write)
+  return launch_with(gather_kernel, dim3(ctas < 32 ? 32 : ctas), dim3(256), 0, 1, true, stream, g);
 }
 
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int sms, double* cost) {
-  const uint32_t k = (d + kDepth - 1) / kDepth;
-  // (a tile takes as long as its products or, beside the next one's, as its results)
-  auto cycles = [&](int cg, int bn, double stage, double results) {
-    const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + bn - 1) / bn), units = sms / cg;
-    return (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
-  };
-  const double pair = cycles(2, 256, 512.0, 4000.0), one = cycles(1, 128, 300.0, 2500.0);
-  const bool wide = rows > 128 && pair <= one;
-  if (cost) *cost = wide ? pair : one;
-  return wide ? VocabShape{2, 256} : VocabShape{1, 128};
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int sms, double* cost) {
+  const uint32_t k = (d + kDepth - 1) / kDepth, step = panels ? 64 : 16;
+  VocabShape best = {1, 128};
+  double least = 1e300;
+  // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle; a tile takes as long as its
+  // stages or, beside the next one's, as its results.  Of the widths, the one whose tiles fill their last round best.
+  for (int cg = rows > 128 ? 2 : 1; cg > 0; --cg)
+    for (uint32_t wide = 128 * cg; wide >= 64u * cg; wide -= step) {
+      const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + wide - 1) / wide), units = sms / cg;
+      const double copied = (rows < 128 ? rows : 128) * 128.0 + wide / cg * 128.0;
+      double stage = 2.0 * wide;
+      if (copied / 62.0 > stage) stage = copied / 62.0;
+      const double results = 500.0 + (cg == 2 ? 14.0 : 16.0) * wide;
+      const double c = (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
+      if (c < 0.99 * least) {
+        least = c;
+        best = {cg, wide};
+      }
+    }
+  if (cost) *cost = least;
+  return best;
 }
 
-uint32_t vocab_parts(const VocabArgs& a, VocabShape s) { return 2 * ((a.v + s.bn - 1) / s.bn); }
+uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms) {
+  const uint32_t tiles = (a.v + s.wide - 1) / s.wide;
+  return 2 * (merged(s, most) ? units_of(s, most, tiles, sms) : tiles);
+}
 
-cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, float2* part, int sms, int* err, cudaStream_t stream) {
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most, float2* part, int sms, int* err, cudaStream_t stream) {
   ScoreArgs s = {};
   s.v0 = 0;
   s.v1 = a.v;
   s.part = part;
+  s.merge = merged(sh, most);
   s.err = err;
   return by_shape<0>(a, sh, s, nullptr, sms, stream);
 }

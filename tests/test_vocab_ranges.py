@@ -20,7 +20,13 @@ extern "C" int check(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t 
   if (r.U == 0 || r.U > units) return 2;
   if (r.begin(0) != 0 || r.begin(r.U) != r.S) return 3;
   const uint32_t planes = plane_rows / (r.tiles_m * tile_m);
-  uint64_t longest = 0, shortest = ~0ull;
+  if (r.split && r.U != r.split * r.tiles) return 10;
+  uint64_t longest = 0, shortest = ~0ull, units_seen = 0;
+  for (uint32_t i = 0; i < r.U; ++i) {
+    if (r.unit(i) >= r.U) return 11;
+    units_seen += r.unit(i);
+  }
+  if (units_seen != (uint64_t)r.U * (r.U - 1) / 2) return 12;                // some unit twice
   for (uint32_t u = 0; u < r.U; ++u) {
     const uint64_t b = r.begin(u), e = r.begin(u + 1);
     if (e <= b) return 4;                                                    // nothing to do

@@ -465,6 +465,7 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const float* part, uint32_
 // Rows that are not aligned to 16 bytes, copied to rows that are: 256 columns to a warp.
 __global__ void __launch_bounds__(256) q8_pitch_kernel(const __nv_bfloat16* in, size_t ldi, uint64_t rows, uint32_t cols,
                                                        __nv_bfloat16* out, size_t ldo) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
   const uint32_t per_row = (cols + 255) / 256;
   const uint64_t id = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5), row = id / per_row;
@@ -630,9 +631,8 @@ cudaError_t launch_join(const float* part, uint32_t splits, uint32_t tile_m, uin
 }
 cudaError_t launch_pitch(const void* in, size_t ldi, uint64_t rows, uint32_t cols, void* out, size_t ldo, cudaStream_t stream) {
   const uint64_t items = rows * ((cols + 255) / 256);      // (a warp each)
-  q8_pitch_kernel<<<(unsigned)((items + 7) / 8), 256, 0, stream>>>(static_cast<const __nv_bfloat16*>(in), ldi, rows, cols,
-                                                                   static_cast<__nv_bfloat16*>(out), ldo);
-  return cudaGetLastError();
+  return launch_with(q8_pitch_kernel, dim3((unsigned)((items + 7) / 8)), dim3(256), 0, 1, true, stream, static_cast<const __nv_bfloat16*>(in), ldi, rows,
+                     cols, static_cast<__nv_bfloat16*>(out), ldo);
 }
 size_t q8_grad_workspace(const GemmArgs& g, bool dw, int sms) {
   const Work w = work_of(g, dw, sms);

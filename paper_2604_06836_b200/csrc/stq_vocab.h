@@ -121,8 +121,15 @@ struct VocabDx {
 };
 size_t vocab_dx_rows(uint32_t most, uint32_t d, size_t ldd);      // rows of planes that suffice
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream);
-// dx of all tokens (zero for those that do not count): scale * the sum of the planes.
-cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream);
-cudaError_t launch_vocab_dbias(const float* part, size_t ldb, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream);
+// dbias of `cols` entries from the sums over 32 rows each.
+struct VocabDbias {
+  const float* part;
+  size_t ldb;
+  uint32_t cols;
+  float* out;
+};
+cudaError_t launch_vocab_dbias(const VocabDbias& a, const VocabRows& r, cudaStream_t stream);
+// dx of all tokens (zero for those that do not count): scale * the sum of the planes.  With db, dbias too.
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream);
 
 }  // namespace stq

@@ -251,9 +251,8 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
     o.dbias = db_part && db_once ? db_part + v0 : db_part;
     STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, true, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
     ++launches;
-    const bool all = v0 + n == v;
-    if (dbias && (!db_once || all)) {
-      STQ_CUDA(h, db_once ? launch_vocab_dbias(db_part, o.ldb, a.r, v, dbias, s) : launch_vocab_dbias(db_part, o.ldb, a.r, n, dbias + v0, s));
+    if (dbias && !db_once) {
+      STQ_CUDA(h, launch_vocab_dbias({db_part, o.ldb, n, dbias + v0}, a.r, s));
       ++launches;
     }
     if (dw) {
@@ -272,10 +271,11 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
     }
     if (dw) STQ_CUDA(h, launch_vocab_dw_join(gw, part, h->sm_count, s, &launches));
   }
-  if (dx) {
-    STQ_CUDA(h, launch_vocab_dx_finish(gx, last, a.t, dx, lddx, h->sm_count, s));
-    ++launches;
-  }
+  const VocabDbias db = {db_part, o.ldb, v, dbias};
+  const bool join_db = dbias && db_once;
+  if (dx) STQ_CUDA(h, launch_vocab_dx_finish(gx, last, a.t, dx, lddx, join_db ? &db : nullptr, h->sm_count, s));
+  else if (join_db) STQ_CUDA(h, launch_vocab_dbias(db, a.r, s));
+  if (dx || join_db) ++launches;
   h->launches += launches;
   return STQ_OK;
 }

@@ -320,12 +320,48 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
   }
 }
 
+// Column sums of the partial sums of 32 rows each: 32 columns to a CTA, every eighth row to a warp.
+struct DbiasArgs {
+  const float* part;
+  size_t ldb;
+  const uint32_t* count;
+  uint32_t rows;
+  const float* scale;
+  uint32_t cols;
+  float* out;
+};
+__device__ __forceinline__ void dbias_block(const DbiasArgs& a, uint32_t block) {
+  __shared__ float sums[8][33];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t groups = ((a.count ? *a.count : a.rows) + 31) / 32, c = block * 32 + lane;
+  float s = 0.f;
+  if (c < a.cols) {
+#pragma unroll 4
+    for (uint32_t g = warp; g < groups; g += 8) s += __ldcg(a.part + (size_t)g * a.ldb + c);
+  }
+  sums[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || c >= a.cols) return;
+  for (int i = 1; i < 8; ++i) s += sums[i][lane];
+  a.out[c] = s * *a.scale;
+}
+__global__ void __launch_bounds__(256) dbias_kernel(const DbiasArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  dbias_block(a, blockIdx.x);
+}
+
 // dx of up to eight tokens to a CTA, eight columns to a thread: the planes of a row, added in order.  (What does not depend on the planes
-// was there before the kernel that writes them began: it is worked out while that one still runs.)
+// was there before the kernel that writes them began: it is worked out while that one still runs.)  CTAs behind those of the tokens
+// have columns of dbias.
 __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, size_t ldd, uint32_t plane_rows, const uint32_t* count_at, uint32_t rows,
                                                         const int32_t* row_of, uint32_t tile_m, uint32_t bn, uint32_t first, uint32_t last,
                                                         uint32_t units, const float* scale_at, uint32_t t, uint32_t each, uint32_t d, __nv_bfloat16* dx,
-                                                        size_t lddx, bool aligned) {
+                                                        size_t lddx, bool aligned, uint32_t ctas, const DbiasArgs db) {
+  if (blockIdx.x >= ctas) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    dbias_block(db, blockIdx.x - ctas);
+    return;
+  }
   __shared__ uint8_t shares[2][kMaxTilesN];
   __shared__ int32_t row[8];
   __shared__ uint32_t lowest;
@@ -387,24 +423,6 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, siz
         if (c + j < d) to[j] = __float2bfloat16_rn(s[j]);
     }
   }
-}
-
-// Column sums of the partial sums of 32 rows each: 32 columns to a CTA, every eighth row to a warp.
-__global__ void __launch_bounds__(256) dbias_kernel(const float* part, size_t ldb, const uint32_t* count_at, uint32_t rows, const float* scale,
-                                                    uint32_t cols, float* out) {
-  __shared__ float sums[8][33];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t groups = ((count_at ? *count_at : rows) + 31) / 32, c = blockIdx.x * 32 + lane;
-  float s = 0.f;
-  if (c < cols)
-#pragma unroll 4
-    for (uint32_t g = warp; g < groups; g += 8) s += __ldcg(part + (size_t)g * ldb + c);
-  sums[warp][lane] = s;
-  __syncthreads();
-  if (warp != 0 || c >= cols) return;
-  for (int i = 1; i < 8; ++i) s += sums[i][lane];
-  out[c] = s * *scale;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -481,6 +499,8 @@ cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const voi
   if (e != cudaSuccess) return e;
   return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, g);
 }
+
+DbiasArgs dbias_args(const VocabDbias& a, const VocabRows& r) { return {a.part, a.ldb, r.count, r.rows, r.scale, a.cols, a.out}; }
 
 // Tiles of dx: a CTA's for few tokens, and two blocks of rows where there are enough of them for every pair.
 struct DxShape {
@@ -560,19 +580,20 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
   return s.mt == 2 ? go(launch<2, 256, 1, 2, false, float>) : s.cg == 2 ? go(launch<2, 256, 1, 1, false, float>) : go(launch<1, 128, 1, 1, false, float>);
 }
 
-cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, int sms, cudaStream_t stream) {
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream) {
   const DxShape s = dx_shape(a.r.most, a.d);
   // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
   uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
   if (each > 8) each = 8;
-  return launch_with(dx_finish_kernel, dim3((t + each - 1) / each), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
+  const uint32_t ctas = (t + each - 1) / each;
+  const DbiasArgs d = db ? dbias_args(*db, a.r) : DbiasArgs{};
+  return launch_with(dx_finish_kernel, dim3(ctas + (d.cols + 31) / 32), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
                      a.r.row, (uint32_t)(128 * s.cg * s.mt), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), a.r.scale, t, each, a.d,
-                     static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2));
+                     static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2), ctas, d);
 }
 
-cudaError_t launch_vocab_dbias(const float* part, size_t ldb, const VocabRows& r, uint32_t cols, float* dbias, cudaStream_t stream) {
-  return launch_with(dbias_kernel, dim3((cols + 31) / 32), dim3(256), 0, 1, true, stream, part, ldb, r.count, r.rows, r.scale, cols,
-                     dbias);
+cudaError_t launch_vocab_dbias(const VocabDbias& a, const VocabRows& r, cudaStream_t stream) {
+  return launch_with(dbias_kernel, dim3((a.cols + 31) / 32), dim3(256), 0, 1, true, stream, dbias_args(a, r));
 }
 
 }  // namespace stq

@@ -335,6 +335,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
       } else {
         const uint32_t out = outs + (warp - 2) * 2 * 4096;
+        const float2 less = make_float2(-lse, -lse), scale2 = make_float2(kLog2e, kLog2e), g2 = make_float2(g, g);
 #pragma unroll
         for (int c = 0; c < BN / 2; c += 64) {
           const uint32_t col = col0 + c;
@@ -345,22 +346,33 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             float(&b)[32] = *reinterpret_cast<float(*)[32]>(v + 32 * h);
             load_block(from + c + 32 * h, b);
             add_bias(b, bias[c / 32 + h]);
-            const float2 less = make_float2(-lse, -lse), scale2 = make_float2(kLog2e, kLog2e), g2 = make_float2(g, g);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               const float2 e = __fmul2_rn(__fadd2_rn(make_float2(b[i], b[i + 1]), less), scale2);
-              float2 p = make_float2(ex2(e.x), ex2(e.y));
-              if (hit == c + 32 * h + i) p.x = __fadd_rn(p.x, -1.f);
-              if (hit == c + 32 * h + i + 1) p.y = __fadd_rn(p.y, -1.f);
-              p = __fmul2_rn(g2, p);
-              b[i] = real ? p.x : 0.f;
-              b[i + 1] = real ? p.y : 0.f;
+              b[i] = ex2(e.x);
+              b[i + 1] = ex2(e.y);
             }
-            if (col + 32 * h + 32 > end) {
+          }
+          const int at = hit - c;      // (few rows have their target in the block)
+          if (__any_sync(0xffffffffu, at >= 0 && at < 64)) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col + 32 * h + i >= end) b[i] = 0.f;
-            }
+            for (int i = 0; i < 64; ++i)
+              if (at == i) v[i] = __fadd_rn(v[i], -1.f);
+          }
+#pragma unroll
+          for (int i = 0; i < 64; i += 2) {
+            const float2 z = __fmul2_rn(g2, make_float2(v[i], v[i + 1]));
+            v[i] = z.x;
+            v[i + 1] = z.y;
+          }
+          if (!real) {                 // (whatever the logits of a row that does not count are)
+#pragma unroll
+            for (int i = 0; i < 64; ++i) v[i] = 0.f;
+          }
+          if (col + 64 > end) {
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (col + i >= end) v[i] = 0.f;
           }
           if (a.dbias) {
 #pragma unroll
@@ -378,7 +390,13 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             put_block<__nv_bfloat16>(&map_p, 0, (int)((p * a.panels + (col - a.v0) / 64) * a.most + row0), v, lane, out, puts);
             if (p + 1 < PLANES) {
 #pragma unroll
-              for (int i = 0; i < 64; ++i) v[i] = __fadd_rn(v[i], -__bfloat162float(__float2bfloat16_rn(v[i])));
+              for (int i = 0; i < 64; i += 2) {
+                const uint32_t w = bf16_pair(v[i], v[i + 1]);      // (the words that have just been put)
+                const float2 rest = __fadd2_rn(make_float2(v[i], v[i + 1]),
+                                               make_float2(__uint_as_float((w << 16) ^ 0x80000000u), __uint_as_float((w & 0xffff0000u) ^ 0x80000000u)));
+                v[i] = rest.x;
+                v[i + 1] = rest.y;
+              }
             }
           }
         }
@@ -501,10 +519,10 @@ cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGr
   s.most = a.r.most;
   s.bias = a.bias;
   s.ksteps = (a.d + kDepth - 1) / kDepth;
-  // few tokens: no more rows are copied than there are, in steps of the swizzle's eight (rows of zeros behind the matrix take longer
-  // than others: 17 tokens, 1600 x 50257, 45 us with 128 rows, 33 with 24; what a product reads behind them is what an earlier stage
-  // left, and stays in its rows)
-  const uint32_t rows = CG == 1 && a.r.rows < 128 ? (a.r.rows + 7) / 8 * 8 : 128;
+  // few tokens: no more rows are copied than there are.  (Rows of zeros behind the matrix take longer than others: 17 tokens,
+  // 1600 x 50257, 45 us with 128 rows, 30 with 17.  What a product reads behind them is what an earlier stage left, and stays in its
+  // rows.)
+  const uint32_t rows = CG == 1 && a.r.rows < 128 ? a.r.rows : 128;
   s.wide = sh.wide;
   s.tiles_n = (s.v1 - s.v0 + s.wide - 1) / s.wide;
   s.stage_bytes = (rows + s.wide / CG) * kDepth * 2;
@@ -537,13 +555,15 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int s
   const uint32_t k = (d + kDepth - 1) / kDepth, step = panels ? 64 : 16;
   VocabShape best = {1, 128};
   double least = 1e300;
-  // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle; a tile takes as long as its
-  // stages or, beside the next one's, as its results.  Of the widths, the one whose tiles fill their last round best.
+  // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle, and 400 cycles at least (the
+  // ring holds six, and what is in flight must cover the memory's latency: 1 token, 1600 x 50257, 38 us in tiles of 64, 30 in tiles of
+  // 128); a tile takes as long as its stages or, beside the next one's, as its results.  Of the widths, the one whose tiles fill their
+  // last round best.
   for (int cg = rows > 128 ? 2 : 1; cg > 0; --cg)
     for (uint32_t wide = 128 * cg; wide >= 64u * cg; wide -= step) {
       const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + wide - 1) / wide), units = sms / cg;
       const double copied = (rows < 128 ? rows : 128) * 128.0 + wide / cg * 128.0;
-      double stage = 2.0 * wide;
+      double stage = 2.0 * wide > 400.0 ? 2.0 * wide : 400.0;
       if (copied / 62.0 > stage) stage = copied / 62.0;
       const double results = 500.0 + (cg == 2 ? 14.0 : 16.0) * wide;
       const double c = (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;

@@ -53,13 +53,13 @@ struct GatherArgs {
 };
 cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
 
-// Tiles of the products: `cg` CTAs share 128 * cg rows and `wide` entries of the vocabulary.  The loss takes any width that the matrix
-// units do, the gradients whole panels (below).  cost, if wanted: the time in clock cycles.
+// Tiles of the products: `cg` CTAs share 128 * cg rows and `wide` entries of the vocabulary.  The loss (planes = 0) takes any width that
+// the matrix units do, the gradients whole panels (below), those in three parts narrow ones.  cost, if wanted: the time in clock cycles.
 struct VocabShape {
   int cg;
   uint32_t wide;
 };
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int sms, double* cost = nullptr);
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sms, double* cost = nullptr);
 
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms);

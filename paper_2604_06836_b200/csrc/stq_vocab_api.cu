@@ -83,14 +83,14 @@ cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, const
 
 // Entries of the vocabulary to a piece (the last piece has what is left): as many tiles as fit, or somewhat fewer where the tiles of the
 // products then fill their last round better.
-uint32_t piece_of(const VocabArgs& a, VocabDw g, size_t entry, bool dw, int sms) {
+uint32_t piece_of(const VocabArgs& a, VocabDw g, int planes, bool dw, int sms) {
   const uint32_t tiles = (uint32_t)(up(a.v, 256) / 256);
-  const size_t fit = kPieceBytes / entry / 256;
+  const size_t fit = kPieceBytes / ((size_t)g.r.most * 2 * planes) / 256;
   if (fit >= tiles) return a.v;
   const uint32_t widest = fit < 1 ? 1 : (uint32_t)fit;
   auto cost = [&](uint32_t cols) {
     double c, extra = 60000.0;      // (of a piece: launches, beginnings and ends)
-    vocab_shape(a.t, cols, a.d, true, sms, &c);
+    vocab_shape(a.t, cols, a.d, planes, sms, &c);
     g.cols = cols;
     return c + extra + (dw ? vocab_dw_cost(g, sms) : 0.0);
   };
@@ -143,7 +143,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   a.target = target;
   Rows r(a, x, ldx, false);
   const uint32_t most = most_rows(a.t);
-  const VocabShape shape = vocab_shape(a.t, v, d, false, h->sm_count);
+  const VocabShape shape = vocab_shape(a.t, v, d, 0, h->sm_count);
   const uint32_t parts = vocab_parts(a, shape, most, h->sm_count);
   Arena m;
   float2* part = nullptr;
@@ -207,7 +207,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   gw.f32 = dw_dtype == STQ_GRAD_F32;
   gw.device = h->device;
   gw.r.most = most;
-  const uint32_t cols = piece_of(a, gw, (size_t)most * 2 * planes, dw != nullptr, h->sm_count);
+  const uint32_t cols = piece_of(a, gw, planes, dw != nullptr, h->sm_count);
   VocabGradOut o = {nullptr, (uint32_t)(up(cols, 64) / 64), planes, nullptr, 0, lse, dloss};
   gw.panels = o.panels;
   gw.cols = cols;
@@ -249,7 +249,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   for (uint32_t v0 = 0; v0 < v; v0 += cols) {
     const uint32_t n = v - v0 < cols ? v - v0 : cols;
     o.dbias = db_part && db_once ? db_part + v0 : db_part;
-    STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, true, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, launch_vocab_dlogits(a, vocab_shape(a.t, n, d, planes, h->sm_count), v0, v0 + n, o, h->sm_count, h->d_err, s));
     ++launches;
     if (dbias && !db_once) {
       STQ_CUDA(h, launch_vocab_dbias({db_part, o.ldb, n, dbias + v0}, a.r, s));

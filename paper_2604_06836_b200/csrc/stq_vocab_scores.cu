@@ -152,8 +152,14 @@ struct ScoreArgs {
 
 constexpr int kWriters = 8;            // warps that take results out of tensor memory: two to each quarter of its lanes
 
+// The matrix unit cuts its fp32 sums off instead of rounding them, always towards zero: over a sum of 4096 a logit lost 2e-6 of itself,
+// and the loss 4e-6 where the vocabulary is small.  For the loss, and for gradients in three parts (an fp32 result), the sum
+// therefore leaves the unit every kChunk stages and is added, rounded, in registers.  (The accumulators take turns, so the next part is
+// multiplied meanwhile.)  For gradients in one bf16 number that error is nothing.
 template <int CG, int BN, int PLANES>  // PLANES = 0: the loss
 struct ScoreShape {
+  static constexpr bool kExact = PLANES != 1;
+  static constexpr int kChunk = kExact ? 8 : 1 << 30;
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
   static constexpr int kOut = PLANES ? kWriters * 2 * 4096 : 0;
@@ -239,20 +245,24 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     if (leader && elect_one()) {
       const uint32_t id = idesc(kIdescBf16, 128 * CG, (int)a.wide, false, false);
       uint32_t it = 0, n = 0;
-      for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
-        const uint32_t acc = n & 1;
-        if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
-        mma_fence_after();
+      for (uint32_t w = unit; ok && w < tiles; w += units) {
         for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
-          const uint32_t s = it % kStages, ph = (it / kStages) & 1;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = k % S::kChunk;
+          if (place == 0) {
+            if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
+            mma_fence_after();
+          }
           if (!(ok = bar_wait<CG == 2>(full + 8 * s, ph))) break;
           mma_fence_after();
           const uint64_t da = operand_desc(ring + s * S::kStage, 16, 1024), db = operand_desc(ring + s * S::kStage + S::kA, 16, 1024);
 #pragma unroll
           for (int j = 0; j < kDepth / kStepK; ++j)
-            mma<CG, false>(tmem + acc * BN, da + j * ((kStepK * 2) >> 4), db + j * ((kStepK * 2) >> 4), id, k != 0 || j != 0);
+            mma<CG, false>(tmem + acc * BN, da + j * ((kStepK * 2) >> 4), db + j * ((kStepK * 2) >> 4), id, place != 0 || j != 0);
           mma_commit<CG>(empty + 8 * s);
-          if (k + 1 == a.ksteps) mma_commit<CG>(done + 8 * acc);
+          if (place == S::kChunk - 1 || k + 1 == a.ksteps) {
+            mma_commit<CG>(done + 8 * acc);
+            ++n;
+          }
         }
       }
     }
@@ -261,8 +271,8 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
     uint32_t n = 0, puts = 0;
     float m = -INFINITY, s = 0.f;      // the loss: maximum and sum of exp of this row over a part
-    for (uint32_t w = unit; ok && w < tiles; w += units, ++n) {
-      const uint32_t acc = n & 1, from = tmem + ((uint32_t)(quad * 32) << 16) + acc * BN + half * (BN / 2);
+    const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16) + half * (BN / 2);
+    for (uint32_t w = unit; ok && w < tiles; w += units) {
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
       const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + half * (BN / 2);
       const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
@@ -287,13 +297,50 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
         for (int i = 0; i < BN / 64; ++i) bias[i] = col0 + 32 * i + lane < end ? __ldg(a.bias + col0 + 32 * i + lane) : 0.f;
       }
-      ok = bar_wait(done + 8 * acc, (n >> 1) & 1);
-      if (!(ok = __all_sync(0xffffffffu, ok))) break;
-      mma_fence_after();
-      auto add_bias = [&](float(&v)[32], float mine) {
+      float z[S::kExact ? BN / 2 : 32];      // logits: of all columns of the tile, or of a block of them
+      auto release = [&](uint32_t acc) {
+        mma_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+      };
+      if constexpr (S::kExact) {
+#pragma unroll
+        for (int i = 0; i < BN / 2; ++i) z[i] = 0.f;
+        for (uint32_t k = 0; k < a.ksteps; k += S::kChunk, ++n) {
+          ok = bar_wait(done + 8 * (n & 1), (n >> 1) & 1);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          mma_fence_after();
+#pragma unroll
+          for (int c = 0; c < BN / 2; c += 32) {
+            if (col0 + c >= end) break;
+            float v[32];
+            load_block(mine + (n & 1) * BN + c, v);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float2 sum = __fadd2_rn(make_float2(z[c + i], z[c + i + 1]), make_float2(v[i], v[i + 1]));
+              z[c + i] = sum.x;
+              z[c + i + 1] = sum.y;
+            }
+          }
+          release(n & 1);
+        }
+        if (!ok) break;
+      } else {
+        ok = bar_wait(done + 8 * (n & 1), (n >> 1) & 1);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        mma_fence_after();
+      }
+      // the 32 logits from column c (a constant after unrolling) on, with their bias
+      auto logits = [&](int c, float(&v)[32]) {
+        if constexpr (S::kExact) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] = z[c + i];
+        } else {
+          load_block(mine + (n & 1) * BN + c, v);
+        }
         if (a.bias) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, mine, i));
+          for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, bias[c / 32], i));
         }
       };
       if constexpr (PLANES == 0) {
@@ -302,8 +349,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           const uint32_t col = col0 + c;
           if (col >= end) break;
           float v[32];
-          load_block(from + c, v);
-          add_bias(v, bias[c / 32]);
+          logits(c, v);
           if (col + 32 > end) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -344,8 +390,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float(&b)[32] = *reinterpret_cast<float(*)[32]>(v + 32 * h);
-            load_block(from + c + 32 * h, b);
-            add_bias(b, bias[c / 32 + h]);
+            logits(c + 32 * h, b);
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
               const float2 e = __fmul2_rn(__fadd2_rn(make_float2(b[i], b[i + 1]), less), scale2);
@@ -401,9 +446,10 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
         }
       }
-      mma_fence_before();
-      __syncwarp();
-      if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+      if constexpr (!S::kExact) {
+        release(n & 1);
+        ++n;
+      }
     }
     if constexpr (PLANES > 0) store_blocks_done(lane);
   }
@@ -539,7 +585,8 @@ cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGr
 
 template <int PLANES>
 cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
-  return sh.cg == 2 ? launch<2, 256, PLANES>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES>(a, sh, s, o, sms, stream);
+  constexpr int kPair = PLANES == 3 ? 128 : 256;
+  return sh.cg == 2 ? launch<2, kPair, PLANES>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES>(a, sh, s, o, sms, stream);
 }
 
 }  // namespace
@@ -551,8 +598,8 @@ cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
   return launch_with(gather_kernel, dim3(ctas < 32 ? 32 : ctas), dim3(256), 0, 1, true, stream, g);
 }
 
-VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int sms, double* cost) {
-  const uint32_t k = (d + kDepth - 1) / kDepth, step = panels ? 64 : 16;
+VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sms, double* cost) {
+  const uint32_t k = (d + kDepth - 1) / kDepth, step = planes ? 64 : 16;
   VocabShape best = {1, 128};
   double least = 1e300;
   // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle, and 400 cycles at least (the
@@ -560,12 +607,12 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, bool panels, int s
   // 128); a tile takes as long as its stages or, beside the next one's, as its results.  Of the widths, the one whose tiles fill their
   // last round best.
   for (int cg = rows > 128 ? 2 : 1; cg > 0; --cg)
-    for (uint32_t wide = 128 * cg; wide >= 64u * cg; wide -= step) {
+    for (uint32_t wide = planes == 3 ? 128 : 128 * cg; wide >= (planes == 3 ? 128u : 64u * cg); wide -= step) {
       const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + wide - 1) / wide), units = sms / cg;
       const double copied = (rows < 128 ? rows : 128) * 128.0 + wide / cg * 128.0;
       double stage = 2.0 * wide > 400.0 ? 2.0 * wide : 400.0;
       if (copied / 62.0 > stage) stage = copied / 62.0;
-      const double results = 500.0 + (cg == 2 ? 14.0 : 16.0) * wide;
+      const double results = 500.0 + (cg == 2 ? 14.0 : 16.0) * (planes == 3 ? 2.0 : 1.0) * wide;
       const double c = (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
       if (c < 0.99 * least) {
         least = c;

@@ -644,7 +644,7 @@ cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, c
   auto go = [&](auto* kernel, uint32_t r) {
     return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts, loss, lse);
   };
-  return a.t <= 2048 ? go(finish_kernel<4>, 4) : go(finish_kernel<32>, 32);
+  return a.t <= 2048 ? go(finish_kernel<4>, 4) : go(finish_kernel<8>, 8);
 }
 
 cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,

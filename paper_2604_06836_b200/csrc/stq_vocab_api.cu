@@ -8,7 +8,8 @@ using namespace stq;
 
 namespace {
 
-constexpr uint32_t kTokensAtOnce = 32768;       // of a loss: bounds its workspace (tokens do not depend on one another)
+constexpr uint32_t kTokensAtOnce = 32768;       // of a loss, at most (tokens do not depend on one another), and
+constexpr size_t kPartBytes = 256u << 20;       // of its parts: together they bound its workspace
 constexpr size_t kPieceBytes = 512u << 20;      // of gradients of logits that exist at a time
 
 size_t up(size_t v, size_t to) { return (v + to - 1) / to * to; }
@@ -139,7 +140,9 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   a.ignore = ignore_index;
   a.device = h->device;
   // (the blocks of tokens share one workspace, laid out for the largest)
-  a.t = (uint32_t)(t < kTokensAtOnce ? t : kTokensAtOnce);
+  const size_t fit = kPartBytes / (16 * (up(v, 128) / 128)) / 256 * 256;
+  const uint32_t at_once = fit < 256 ? 256 : fit < kTokensAtOnce ? (uint32_t)fit : kTokensAtOnce;
+  a.t = (uint32_t)(t < at_once ? t : at_once);
   a.target = target;
   Rows r(a, x, ldx, false);
   const uint32_t most = most_rows(a.t);
@@ -153,9 +156,9 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     part = m.take<float2>((size_t)parts * most);
     if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
   }
-  for (uint64_t t0 = 0; t0 < t; t0 += kTokensAtOnce) {
+  for (uint64_t t0 = 0; t0 < t; t0 += at_once) {
     VocabArgs b = a;
-    b.t = (uint32_t)(t - t0 < kTokensAtOnce ? t - t0 : kTokensAtOnce);
+    b.t = (uint32_t)(t - t0 < at_once ? t - t0 : at_once);
     b.target = target + t0;
     const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
     int launches = 2;

@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(256) dbias_kernel(const DbiasArgs a) {
   dbias_block(a, blockIdx.x);
 }
 
-// dx of up to eight tokens to a CTA, eight columns to a thread: the planes of a row, added in order.  (What does not depend on the planes
+// dx of up to eight tokens to a CTA, four columns to a thread: the planes of a row, added in order.  (What does not depend on the planes
 // was there before the kernel that writes them began: it is worked out while that one still runs.)  CTAs behind those of the tokens
 // have columns of dbias.
 __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, size_t ldd, uint32_t plane_rows, const uint32_t* count_at, uint32_t rows,
@@ -386,40 +386,34 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, siz
   }
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t per_row = (d + 7) / 8;
+  const uint32_t per_row = (d + 3) / 4;
   const size_t plane = (size_t)((count + tile_m - 1) / tile_m) * tile_m * ldd;
   for (uint32_t i = threadIdx.x; i < each * per_row; i += 256) {
-    const uint32_t k = i / per_row, tok = t0 + k, c = i % per_row * 8;
+    const uint32_t k = i / per_row, tok = t0 + k, c = i % per_row * 4;
     if (tok >= t) break;
     const int32_t at = row[k];
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (at >= 0) {      // (a tile's columns are a multiple of 16: the eight lie in one tile)
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (at >= 0) {      // (a tile's columns are a multiple of 16: the four lie in one tile)
       const uint32_t n = shares[at / tile_m - lo][c / bn];
       const float* from = planes + (size_t)at * ldd + c;
-      for (uint32_t p = 0; p < n; p += 4, from += 4 * plane) {
-        float4 u[4], v[4];
+      for (uint32_t p = 0; p < n; p += 8, from += 8 * plane) {
+        float4 u[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (p + j < n) {
-            u[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane));
-            v[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane + 4));
-          }
+        for (int j = 0; j < 8; ++j)
+          if (p + j < n) u[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane));
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (p + j < n) {
-            s[0] += u[j].x; s[1] += u[j].y; s[2] += u[j].z; s[3] += u[j].w;
-            s[4] += v[j].x; s[5] += v[j].y; s[6] += v[j].z; s[7] += v[j].w;
-          }
+        for (int j = 0; j < 8; ++j)
+          if (p + j < n) { s[0] += u[j].x; s[1] += u[j].y; s[2] += u[j].z; s[3] += u[j].w; }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] *= scale;
+      for (int j = 0; j < 4; ++j) s[j] *= scale;
     }
     __nv_bfloat16* to = dx + (size_t)tok * lddx + c;
-    if (aligned && c + 8 <= d) {
-      *reinterpret_cast<uint4*>(to) = make_uint4(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3]), bf16_pair(s[4], s[5]), bf16_pair(s[6], s[7]));
+    if (aligned && c + 4 <= d) {
+      *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3]));
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < 4; ++j)
         if (c + j < d) to[j] = __float2bfloat16_rn(s[j]);
     }
   }

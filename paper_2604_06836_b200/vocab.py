@@ -75,7 +75,9 @@ def loss(handle: stq.Handle, x: torch.Tensor, w: torch.Tensor, target: torch.Ten
             return loss(handle, x, w, target, bias=bias, ignore_index=ignore_index)
     dev = handle.device
     t, d, v, ldx, ldw = _given(dev, x, w, target, bias)
-    out, lse = (_empty((t,), (1,), dtype=_F32, device=x.device) for _ in range(2))
+    device = x.device
+    out = _empty((t,), (1,), dtype=_F32, device=device)
+    lse = _empty((t,), (1,), dtype=_F32, device=device)
     rc = (_fn or _lib()).stq_vocab_loss(handle._h, x.data_ptr(), ldx, w.data_ptr(), ldw, None if bias is None else bias.data_ptr(),
                                         target.data_ptr(), ignore_index, t, v, d, out.data_ptr(), lse.data_ptr(), _raw_stream(dev))
     if rc:

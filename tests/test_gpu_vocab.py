@@ -354,3 +354,60 @@ def test_refusals(handle):
     assert L.stq_vocab_loss(handle._h, p(x), 64, p(w), 64, None, p(target), -100, 262145, 100, 64, p(out), p(lse), None) == -12
     assert L.stq_vocab_loss_backward(handle._h, p(dloss), p(x), 64, p(w), 64, None, p(target), -100, p(lse), 10, 100, 64, p(x), 64, None, 0, 0,
                                      None, None) == -5
+
+
+def test_a_wait_that_ran_out_is_reported():
+    """A handle with a launch behind it that gave up refuses both operators without synchronising."""
+    from paper_2604_06836_b200 import clip
+    hd = stq.Handle()
+    x, w, target, b, dloss = inputs(10, 64, 100, 1)
+    out = vocab.loss(hd, x, w, target)
+    hd.selftest_wait_timeout()
+    torch.cuda.synchronize()
+    for call in (lambda: vocab.loss(hd, x, w, target), lambda: vocab.loss_backward(hd, dloss, x, w, target, out.lse),
+                 lambda: clip.grad_norm(hd, [dloss])):
+        with pytest.raises(stq.StqError) as e:
+            call()
+        assert e.value.code == -11
+    hd.close()
+
+
+def test_a_large_vocabulary_bounds_the_tokens_at_once(handle):
+    """The parts of a loss fit 256 MB: of 600 000 entries 3400 tokens or so at a time, here in three blocks."""
+    x, w, target, b, dloss = inputs(9001, 16, 600001, 3, True, 0.3, sharp=1.0)
+    out = vocab.loss(handle, x, w, target, bias=b)
+    for rows in (slice(0, 200), slice(3400, 3700), slice(8900, 9001)):
+        Definition(x[rows], w, target[rows], b, dloss[rows]).check(vocab.LossOut(out.loss[rows], out.lse[rows]), None, BF, str(rows))
+    whole = torch.cat([vocab.loss(handle, x[i:i + 2000], w, target[i:i + 2000], bias=b).lse for i in range(0, 9001, 2000)])
+    assert float((whole - out.lse).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-30, 1e30])
+def test_dloss_of_any_size(handle, scale):
+    """The logits' gradients are formed relative to the largest dloss, so its size does not matter to them."""
+    x, w, target, b, dloss = inputs(200, 64, 300, 2, True, 0.2)
+    out, want = run(handle, x, w, target, b, dloss, F32)
+    big = vocab.loss_backward(handle, dloss * 1e3 * scale, x, w, target, out.lse, bias=b, dtype=F32)
+    for a, c in ((big.dw, want.dw), (big.dbias, want.dbias)):
+        assert float((a.double() / (1e3 * scale) - c.double()).abs().max()) <= 1e-6 * float(c.abs().max()) + 1e-45 / (1e3 * scale)
+
+
+def test_dloss_of_zero_and_of_infinity(handle):
+    x, w, target, b, dloss = inputs(200, 64, 300, 2, True)
+    out = vocab.loss(handle, x, w, target, bias=b)
+    zero = vocab.loss_backward(handle, torch.zeros_like(dloss), x, w, target, out.lse, bias=b, dtype=F32)
+    assert all((g == 0).all() for g in zero)
+    one = torch.zeros_like(dloss)
+    one[7] = float("inf")
+    g = vocab.loss_backward(handle, one, x, w, target, out.lse, bias=b, dtype=F32)
+    rows = torch.arange(200, device="cuda") != 7
+    assert (g.dx[rows] == 0).all() and not g.dx[7].isfinite().any()
+
+
+def test_tokens_that_repeat(handle):
+    """The same row many times, and one target for all: what adds up in dw adds up in order."""
+    x, w, target, b, dloss = inputs(1, 72, 500, 2)
+    x, target, dloss = x.repeat(1500, 1), target.repeat(1500), torch.full((1500,), 1 / 1500, device="cuda")
+    out, grads = run(handle, x, w, target, b, dloss, F32)
+    assert (out.loss == out.loss[0]).all() and (grads.dx == grads.dx[0]).all()
+    Definition(x, w, target, b, dloss).check(out, grads, F32, "repeated")

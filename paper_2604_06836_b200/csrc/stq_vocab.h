@@ -102,9 +102,8 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
 // Adds shares of tiles up, if the plan has any.
 cudaError_t launch_vocab_dw_join(const VocabDw& a, const float* part, int sms, cudaStream_t stream, int* launches);
 
-// planes[c][row][:] (+)= share c of the sum over [v0, v0 + cols) of p[row][i] w[v0 + i][:].  The sums of all tiles, one after
-// the other, are cut into equal ranges, one for each pair of CTAs; what different pairs have of a tile goes to different planes.
-// All pieces but the last are equally long (`first` columns): the last adds to what they left.
+// plane[row][:] (+)= sum over [v0, v0 + cols) of p[row][i] w[v0 + i][:], or segments of that sum (stq_vocab_ranges.h), a tile to each.
+// All pieces but the last are equally long (`first` columns).
 struct VocabDx {
   VocabRows r;
   const void* p;
@@ -114,12 +113,11 @@ struct VocabDx {
   uint32_t cols, d, first;
   bool begin;                 // the first piece
   bool beside;                // launched right after dw of the same piece
-  float* planes;
-  size_t ldd;                 // columns of a plane, a multiple of 32
-  uint32_t plane_rows;        // rows of all planes together
+  float *plane, *segments;
+  size_t ldd;                 // columns of the plane, a multiple of 32
   int device;
 };
-size_t vocab_dx_rows(uint32_t most, uint32_t d, size_t ldd);      // rows of planes that suffice
+void vocab_dx_space(uint32_t most, uint32_t d, size_t ldd, int sms, size_t* plane, size_t* segments);      // floats that suffice
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream);
 // dbias of `cols` entries from the sums over 32 rows each.
 struct VocabDbias {
@@ -129,7 +127,7 @@ struct VocabDbias {
   float* out;
 };
 cudaError_t launch_vocab_dbias(const VocabDbias& a, const VocabRows& r, cudaStream_t stream);
-// dx of all tokens (zero for those that do not count): scale * the sum of the planes.  With db, dbias too.
-cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream);
+// dx of all tokens (zero for those that do not count): scale times the plane or the sum of the segments.  With db, dbias too.
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream);
 
 }  // namespace stq

@@ -222,8 +222,9 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   gx.panels = o.panels;
   gx.d = d; gx.first = cols;
   gx.ldd = up(d, 32);
-  gx.plane_rows = (uint32_t)vocab_dx_rows(most, d, gx.ldd);
   gx.device = h->device;
+  size_t plane = 0, segments = 0;
+  vocab_dx_space(most, d, gx.ldd, h->sm_count, &plane, &segments);
   // (a last piece may share its tiles in another way than the others)
   const uint32_t last = (uint32_t)(v - (v - 1) / cols * cols);
   size_t partial = dw ? vocab_dw_partial(gw, h->sm_count) : 0;
@@ -241,7 +242,8 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
     o.p = m.take<uint16_t>((size_t)most * planes * o.panels * 64);
     db_part = dbias ? m.take<float>(db_rows * o.ldb) : nullptr;
     part = partial ? m.take<float>(partial) : nullptr;
-    gx.planes = dx ? m.take<float>(gx.plane_rows * gx.ldd) : nullptr;
+    gx.plane = dx ? m.take<float>(plane) : nullptr;
+    gx.segments = dx ? m.take<float>(segments) : nullptr;
     if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
   }
   int launches = 0;
@@ -276,7 +278,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
   }
   const VocabDbias db = {db_part, o.ldb, v, dbias};
   const bool join_db = dbias && db_once;
-  if (dx) STQ_CUDA(h, launch_vocab_dx_finish(gx, last, a.t, dx, lddx, join_db ? &db : nullptr, h->sm_count, s));
+  if (dx) STQ_CUDA(h, launch_vocab_dx_finish(gx, a.t, dx, lddx, join_db ? &db : nullptr, h->sm_count, s));
   else if (join_db) STQ_CUDA(h, launch_vocab_dbias(db, a.r, s));
   if (dx || join_db) ++launches;
   h->launches += launches;

@@ -43,7 +43,6 @@ struct GradArgs {
   int aligned;
   // dx
   uint32_t ksteps, first;              // stages of this piece and of the first one
-  uint32_t plane_rows;
   int begin, beside;
   int* err;
 };
@@ -71,14 +70,14 @@ struct GradShape {
 // One work item: tile (its row and column), stages [k0, k1) of its sum, and where the result goes.
 struct Item {
   uint32_t tile, row, col, k0, k1;
-  int share;                           // dx: the plane; dw: number of the partial result, -1 for the whole sum
+  int share;                           // number of the segment (dx) or of the partial result (dw), -1 for the whole sum
 };
 
 // DW: rows of the result are entries of the vocabulary.  O: type of dw (dx: float).
 template <int CG, int BN, int PARTS, int MT, bool DW, class O>
 __global__ void __launch_bounds__((GradShape<CG, BN, PARTS, MT>::kThreads), 1)
 vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_o,
-                  const GradArgs a) {
+                  const __grid_constant__ CUtensorMap map_s, const GradArgs a) {
   using S = GradShape<CG, BN, PARTS, MT>;
   constexpr int kTileM = 128 * CG * MT;
   constexpr int kStages = S::kStages;
@@ -117,8 +116,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
 
   const uint32_t tiles_n = (a.n + a.bn - 1) / a.bn;
   const uint32_t ksteps = DW ? (count + kDepth - 1) / kDepth : a.ksteps;
-  const Ranges ranges(DW ? 0 : count, kTileM, tiles_n, a.ksteps, a.units, a.plane_rows);
-  const Ranges before(DW ? 0 : count, kTileM, tiles_n, a.first, a.units, a.plane_rows);
+  const Ranges ranges(DW ? 0 : count, kTileM, tiles_n, a.first, a.units);
   // calls f(item) for each of this unit's items, in order, until it returns false
   auto items = [&](auto&& f) {
     if constexpr (DW) {
@@ -137,16 +135,14 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
         if (!f(it)) return;
       }
     } else {
-      if (unit >= ranges.U) return;
+      for (uint32_t q = unit; q < ranges.whole; q += a.units)
+        if (!f(Item{q, q / tiles_n * kTileM, q % tiles_n * a.bn, 0, a.ksteps, -1})) return;
+      if (ranges.rest == 0 || unit >= ranges.U) return;
       const uint32_t u = ranges.unit(unit);
-      const uint64_t end = ranges.begin(u + 1);
-      for (uint64_t s = ranges.begin(u); s < end;) {
-        const uint32_t q = (uint32_t)(s / ranges.ksteps), tile = ranges.tile(q);
-        const uint64_t t0 = (uint64_t)q * ranges.ksteps, stop = t0 + ranges.ksteps < end ? t0 + ranges.ksteps : end;
-        const Item it = {tile, tile / tiles_n * kTileM, tile % tiles_n * a.bn, (uint32_t)(s - t0), (uint32_t)(stop - t0),
-                         (int)(u - ranges.unit_of(t0))};
+      for (uint32_t r = ranges.tile_first(u); r <= ranges.tile_last(u); ++r) {
+        const uint32_t q = ranges.whole + r;
+        const Item it = {q, q / tiles_n * kTileM, q % tiles_n * a.bn, ranges.begin(r, u, a.ksteps), ranges.begin(r, u + 1, a.ksteps), (int)(r + u)};
         if (!f(it)) return;
-        s = stop;
       }
     }
   };
@@ -226,7 +222,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     items([&](const Item& w) {
       const uint32_t within = block * 128 * CG + 128 * rank + quad * 32, row = w.row + within, running = tmem + lanes + 2 * BN;
       const uint32_t end = min(a.bn, a.n - w.col);
-      const bool add = !DW && !a.begin && (uint32_t)w.share < before.shares(w.tile);
+      const bool add = !DW && !a.begin;
       // Blocks of kC columns; the last one of a tile begins early where the tile is not a whole number of them (what is
       // written twice that way is the same, what is added must not be).
       auto blocks = [&](auto&& f) {
@@ -253,17 +249,19 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
             put_block<O, false, S::kPlaces>(&map_o, (int)col, (int)row, v, lane, stage, puts);
           }
         } else {
-          const int y = (int)((uint32_t)w.share * ranges.tiles_m * kTileM + row);
+          const CUtensorMap* map = w.share < 0 ? &map_o : &map_s;
+          const int x = (int)(w.share < 0 ? col : c), y = (int)(w.share < 0 ? row : (uint32_t)w.share * kTileM + within);
           if (add) {
 #pragma unroll
             for (int i = 0; i < kC; ++i) v[i] = i < (int)over ? 0.f : v[i];
-            put_block<float, true, S::kPlaces>(&map_o, (int)col, y, v, lane, stage, puts);
+            put_block<float, true, S::kPlaces>(map, x, y, v, lane, stage, puts);
           } else {
-            put_block<float, false, S::kPlaces>(&map_o, (int)col, y, v, lane, stage, puts);
+            put_block<float, false, S::kPlaces>(map, x, y, v, lane, stage, puts);
           }
         }
       };
       if (w.k0 == w.k1) {                         // (no token counts, or fewer stages than shares)
+        if (add) return true;
         blocks([&](uint32_t c, uint32_t over) {
           float v[kC];
 #pragma unroll
@@ -350,71 +348,94 @@ __global__ void __launch_bounds__(256) dbias_kernel(const DbiasArgs a) {
   dbias_block(a, blockIdx.x);
 }
 
-// dx of up to eight tokens to a CTA, four columns to a thread: the planes of a row, added in order.  (What does not depend on the planes
-// was there before the kernel that writes them began: it is worked out while that one still runs.)  CTAs behind those of the tokens
-// have columns of dbias.
-__global__ void __launch_bounds__(256) dx_finish_kernel(const float* planes, size_t ldd, uint32_t plane_rows, const uint32_t* count_at, uint32_t rows,
-                                                        const int32_t* row_of, uint32_t tile_m, uint32_t bn, uint32_t first, uint32_t last,
-                                                        uint32_t units, const float* scale_at, uint32_t t, uint32_t each, uint32_t d, __nv_bfloat16* dx,
-                                                        size_t lddx, bool aligned, uint32_t ctas, const DbiasArgs db) {
-  if (blockIdx.x >= ctas) {
+// dx of up to eight tokens to a CTA, four columns to a thread: what the plane has of a whole tile, or the segments of one, added in order.
+// (What does not depend on them was there before the kernel that writes them began: it is worked out while that one still runs.)
+// CTAs behind those of the tokens have columns of dbias.
+struct FinishArgs {
+  const float *plane, *segments;
+  size_t ldd;
+  const uint32_t* count;
+  uint32_t rows;
+  const int32_t* row;
+  uint32_t tile_m, bn, wide;      // wide: columns of a segment
+  uint32_t first, units;
+  const float* scale;
+  uint32_t t, each, d;
+  __nv_bfloat16* dx;
+  size_t lddx;
+  int aligned;
+  uint32_t ctas;
+};
+__global__ void __launch_bounds__(256) dx_finish_kernel(const FinishArgs a, const DbiasArgs db) {
+  if (blockIdx.x >= a.ctas) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    dbias_block(db, blockIdx.x - ctas);
+    dbias_block(db, blockIdx.x - a.ctas);
     return;
   }
-  __shared__ uint8_t shares[2][kMaxTilesN];
+  __shared__ uint16_t start[2][kMaxTilesN];      // of a tile: its first segment,
+  __shared__ uint8_t many[2][kMaxTilesN];        // and how many it has (0: it is whole)
   __shared__ int32_t row[8];
   __shared__ uint32_t lowest;
-  const uint32_t count = count_at ? *count_at : rows, tiles_n = (d + bn - 1) / bn, t0 = blockIdx.x * each;
-  const float scale = *scale_at;
+  const uint32_t count = a.count ? *a.count : a.rows, tiles_n = (a.d + a.bn - 1) / a.bn, t0 = blockIdx.x * a.each;
+  const float scale = *a.scale;
   // (tokens that follow one another have rows in at most two tiles)
   if (threadIdx.x < 32) {
     const uint32_t i = t0 + threadIdx.x;
-    const int32_t r = threadIdx.x >= each || i >= t ? -1 : row_of ? row_of[i] : (int32_t)i;
+    const int32_t r = threadIdx.x >= a.each || i >= a.t ? -1 : a.row ? a.row[i] : (int32_t)i;
     if (threadIdx.x < 8) row[threadIdx.x] = r;
-    const uint32_t lo = __reduce_min_sync(0xffffffffu, r < 0 ? 0xffffffffu : (uint32_t)r / tile_m);
+    const uint32_t lo = __reduce_min_sync(0xffffffffu, r < 0 ? 0xffffffffu : (uint32_t)r / a.tile_m);
     if (threadIdx.x == 0) lowest = lo;
   }
   __syncthreads();
   const uint32_t lo = lowest;
   if (lo != 0xffffffffu) {
-    const Ranges r0(count, tile_m, tiles_n, first, units, plane_rows), r1(count, tile_m, tiles_n, last, units, plane_rows);
+    const Ranges r(count, a.tile_m, tiles_n, a.first, a.units);
     for (uint32_t i = threadIdx.x; i < 2 * tiles_n; i += 256) {
-      const uint32_t m = lo + i / tiles_n, n = i % tiles_n;
-      if (m < r0.tiles_m) shares[i / tiles_n][n] = (uint8_t)max(r0.shares(m * tiles_n + n), r1.shares(m * tiles_n + n));
+      const uint32_t m = i / tiles_n, n = i % tiles_n, q = (lo + m) * tiles_n + n;
+      if (q < r.whole || q >= r.tiles) {
+        many[m][n] = 0;
+      } else {
+        start[m][n] = (uint16_t)(q - r.whole + r.first(q - r.whole));
+        many[m][n] = (uint8_t)(r.last(q - r.whole) - r.first(q - r.whole) + 1);
+      }
     }
   }
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const uint32_t per_row = (d + 3) / 4;
-  const size_t plane = (size_t)((count + tile_m - 1) / tile_m) * tile_m * ldd;
-  for (uint32_t i = threadIdx.x; i < each * per_row; i += 256) {
+  const uint32_t per_row = (a.d + 3) / 4;
+  for (uint32_t i = threadIdx.x; i < a.each * per_row; i += 256) {
     const uint32_t k = i / per_row, tok = t0 + k, c = i % per_row * 4;
-    if (tok >= t) break;
+    if (tok >= a.t) break;
     const int32_t at = row[k];
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (at >= 0) {      // (a tile's columns are a multiple of 16: the four lie in one tile)
-      const uint32_t n = shares[at / tile_m - lo][c / bn];
-      const float* from = planes + (size_t)at * ldd + c;
-      for (uint32_t p = 0; p < n; p += 8, from += 8 * plane) {
-        float4 u[8];
+      const uint32_t m = at / a.tile_m - lo, col = c / a.bn, n = many[m][col];
+      if (n == 0) {
+        const float4 u = __ldcs(reinterpret_cast<const float4*>(a.plane + (size_t)at * a.ldd + c));
+        s[0] = u.x; s[1] = u.y; s[2] = u.z; s[3] = u.w;
+      } else {
+        const size_t next = (size_t)a.tile_m * a.wide;
+        const float* from = a.segments + start[m][col] * next + (size_t)(at % a.tile_m) * a.wide + (c - col * a.bn);
+        for (uint32_t p = 0; p < n; p += 8, from += 8 * next) {
+          float4 u[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (p + j < n) u[j] = __ldcs(reinterpret_cast<const float4*>(from + j * plane));
+          for (int j = 0; j < 8; ++j)
+            if (p + j < n) u[j] = __ldcs(reinterpret_cast<const float4*>(from + j * next));
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (p + j < n) { s[0] += u[j].x; s[1] += u[j].y; s[2] += u[j].z; s[3] += u[j].w; }
+          for (int j = 0; j < 8; ++j)
+            if (p + j < n) { s[0] += u[j].x; s[1] += u[j].y; s[2] += u[j].z; s[3] += u[j].w; }
+        }
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[j] *= scale;
     }
-    __nv_bfloat16* to = dx + (size_t)tok * lddx + c;
-    if (aligned && c + 4 <= d) {
+    __nv_bfloat16* to = a.dx + (size_t)tok * a.lddx + c;
+    if (a.aligned && c + 4 <= a.d) {
       *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3]));
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (c + j < d) to[j] = __float2bfloat16_rn(s[j]);
+        if (c + j < a.d) to[j] = __float2bfloat16_rn(s[j]);
     }
   }
 }
@@ -473,7 +494,7 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
 
 template <int CG, int BN, int PARTS, int MT, bool DW, class O>
 cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const void* b, uint64_t b_rows, uint32_t b_cols, size_t ldb, void* out,
-                   uint64_t out_rows, size_t ldo, uint64_t items, GradArgs g, int device, int sms, int* err, cudaStream_t stream) {
+                   uint64_t out_rows, size_t ldo, void* segments, uint64_t items, GradArgs g, int device, int sms, int* err, cudaStream_t stream) {
   using S = GradShape<CG, BN, PARTS, MT>;
   g.count = r.count;
   g.rows = r.rows;
@@ -483,15 +504,16 @@ cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const voi
   g.err = err;
   const uint64_t most = sms / CG;
   g.units = (uint32_t)(items < most ? items : most);
-  CUtensorMap mp, mb, mo = {};
+  CUtensorMap mp, mb, mo = {}, ms = {};
   cudaError_t e = make_tensor_map(&mp, p, 2, (uint64_t)r.most * panels * PARTS, 64, 64, DW ? 64 : 128, 64, true);
   if (e == cudaSuccess) e = make_tensor_map(&mb, b, 2, b_rows, b_cols, ldb, 64, 64, true);
   if (e == cudaSuccess && (!DW || g.aligned)) e = make_tensor_map(&mo, out, sizeof(O), out_rows, DW ? g.n : ldo, ldo, 32, 128 / sizeof(O), true);
+  if (e == cudaSuccess && !DW) e = make_tensor_map(&ms, segments, 4, (uint64_t)Ranges::segments(sms / CG) * 128 * CG * MT, BN, BN, 32, 32, true);
   auto* kernel = vocab_grad_kernel<CG, BN, PARTS, MT, DW, O>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, device, seen);
   if (e != cudaSuccess) return e;
-  return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, g);
+  return launch_with(kernel, g.units * CG, S::kThreads, S::kSmem, CG, true, stream, mp, mb, mo, ms, g);
 }
 
 DbiasArgs dbias_args(const VocabDbias& a, const VocabRows& r) { return {a.part, a.ldb, r.count, r.rows, r.scale, a.cols, a.out}; }
@@ -500,6 +522,8 @@ DbiasArgs dbias_args(const VocabDbias& a, const VocabRows& r) { return {a.part, 
 struct DxShape {
   int cg, mt;
   uint32_t bn;
+  uint32_t tile_m() const { return 128u * cg * mt; }
+  uint32_t widest() const { return 128u * cg; }
 };
 DxShape dx_shape(uint32_t most, uint32_t d) {
   const int cg = most > 128 ? 2 : 1;
@@ -532,7 +556,7 @@ cudaError_t launch_vocab_dw(const VocabDw& a, float* part, int sms, int* err, cu
   const uint64_t items = p.full + (uint64_t)(p.tiles - p.full) * p.splits;
   cudaError_t rc;
   const auto go = [&](auto launch_fn) {
-    return launch_fn(a.r, a.p, a.panels, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, items, g, a.device, sms, err, stream);
+    return launch_fn(a.r, a.p, a.panels, a.r.x, (uint64_t)a.r.rows, a.d, a.r.ldx, a.dw, (uint64_t)a.cols, a.lddw, nullptr, items, g, a.device, sms, err, stream);
   };
   if (a.f32)
     rc = p.cg == 2 ? go(launch<2, 128, 3, 1, true, float>) : go(launch<1, 64, 3, 1, true, float>);
@@ -550,11 +574,10 @@ cudaError_t launch_vocab_dw_join(const VocabDw& a, const float* part, int sms, c
   return launch_join(part, p.splits, p.cg * p.mt * 128, p.bn, p.full, p.tiles - p.full, p.tiles / p.tiles_m, true, a.cols, a.d, a.dw, a.lddw, a.f32, stream);
 }
 
-size_t vocab_dx_rows(uint32_t most, uint32_t d, size_t ldd) {
-  // two planes, and for few tokens more, as long as they are small
+void vocab_dx_space(uint32_t most, uint32_t d, size_t ldd, int sms, size_t* plane, size_t* segments) {
   const DxShape s = dx_shape(most, d);
-  const size_t fit = (16u << 20) / ldd, two = 2 * (size_t)up(most, 128 * s.cg * s.mt);
-  return two > fit ? two : fit;
+  *plane = (size_t)up(most, s.tile_m()) * ldd;
+  *segments = (size_t)Ranges::segments(sms / s.cg) * s.tile_m() * s.widest();
 }
 
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream) {
@@ -564,26 +587,42 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
   g.bn = s.bn;
   g.ksteps = (a.cols + kDepth - 1) / kDepth;
   g.first = (a.first + kDepth - 1) / kDepth;
-  g.plane_rows = a.plane_rows;
   g.begin = a.begin;
   g.beside = a.beside;
   const auto go = [&](auto launch_fn) {
-    return launch_fn(a.r, a.p, a.panels, a.w, (uint64_t)a.cols, a.d, a.ldw, a.planes, (uint64_t)a.plane_rows, a.ldd, (uint64_t)(sms / s.cg), g, a.device,
-                     sms, err, stream);
+    return launch_fn(a.r, a.p, a.panels, a.w, (uint64_t)a.cols, a.d, a.ldw, a.plane, (uint64_t)up(a.r.most, s.tile_m()), a.ldd, a.segments,
+                     (uint64_t)(sms / s.cg), g, a.device, sms, err, stream);
   };
   return s.mt == 2 ? go(launch<2, 256, 1, 2, false, float>) : s.cg == 2 ? go(launch<2, 256, 1, 1, false, float>) : go(launch<1, 128, 1, 1, false, float>);
 }
 
-cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t last, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream) {
+cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream) {
   const DxShape s = dx_shape(a.r.most, a.d);
   // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
   uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
   if (each > 8) each = 8;
-  const uint32_t ctas = (t + each - 1) / each;
+  FinishArgs f;
+  f.plane = a.plane;
+  f.segments = a.segments;
+  f.ldd = a.ldd;
+  f.count = a.r.count;
+  f.rows = a.r.rows;
+  f.row = a.r.row;
+  f.tile_m = s.tile_m();
+  f.bn = s.bn;
+  f.wide = s.widest();
+  f.first = (a.first + kDepth - 1) / kDepth;
+  f.units = (uint32_t)(sms / s.cg);
+  f.scale = a.r.scale;
+  f.t = t;
+  f.each = each;
+  f.d = a.d;
+  f.dx = static_cast<__nv_bfloat16*>(dx);
+  f.lddx = lddx;
+  f.aligned = rows_aligned(dx, lddx * 2);
+  f.ctas = (t + each - 1) / each;
   const DbiasArgs d = db ? dbias_args(*db, a.r) : DbiasArgs{};
-  return launch_with(dx_finish_kernel, dim3(ctas + (d.cols + 31) / 32), dim3(256), 0, 1, true, stream, (const float*)a.planes, a.ldd, a.plane_rows, a.r.count, a.r.rows,
-                     a.r.row, (uint32_t)(128 * s.cg * s.mt), s.bn, (a.first + kDepth - 1) / kDepth, (last + kDepth - 1) / kDepth, (uint32_t)(sms / s.cg), a.r.scale, t, each, a.d,
-                     static_cast<__nv_bfloat16*>(dx), lddx, rows_aligned(dx, lddx * 2), ctas, d);
+  return launch_with(dx_finish_kernel, dim3(f.ctas + (d.cols + 31) / 32), dim3(256), 0, 1, true, stream, f, d);
 }
 
 cudaError_t launch_vocab_dbias(const VocabDbias& a, const VocabRows& r, cudaStream_t stream) {

@@ -137,13 +137,17 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     } else {
       for (uint32_t q = unit; q < ranges.whole; q += a.units)
         if (!f(Item{q, q / tiles_n * kTileM, q % tiles_n * a.bn, 0, a.ksteps, -1})) return;
-      if (ranges.rest == 0 || unit >= ranges.U) return;
-      const uint32_t u = ranges.unit(unit);
-      for (uint32_t r = ranges.tile_first(u); r <= ranges.tile_last(u); ++r) {
+      auto item = [&](uint32_t r, uint32_t k0, uint32_t k1, uint32_t segment) {
         const uint32_t q = ranges.whole + r;
-        const Item it = {q, q / tiles_n * kTileM, q % tiles_n * a.bn, ranges.begin(r, u, a.ksteps), ranges.begin(r, u + 1, a.ksteps), (int)(r + u)};
-        if (!f(it)) return;
+        return Item{q, q / tiles_n * kTileM, q % tiles_n * a.bn, k0, k1, (int)segment};
+      };
+      if (unit < ranges.cut * ranges.parts) {
+        const uint32_t r = unit % ranges.cut, part = unit / ranges.cut;
+        if (!f(item(r, ranges.begin(part, a.ksteps), ranges.begin(part + 1, a.ksteps), ranges.segment(r) + part))) return;
       }
+      if (ranges.left == 0 || unit >= ranges.U) return;
+      for (uint32_t r = ranges.tile_first(unit); r <= ranges.tile_last(unit); ++r)
+        if (!f(item(ranges.cut + r, ranges.begin(r, unit, a.ksteps), ranges.begin(r, unit + 1, a.ksteps), a.units + r + unit))) return;
     }
   };
 
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(256) dbias_kernel(const DbiasArgs a) {
   dbias_block(a, blockIdx.x);
 }
 
-// dx of up to eight tokens to a CTA, four columns to a thread: what the plane has of a whole tile, or the segments of one, added in order.
+// dx of up to four tokens to a CTA, four columns to a thread: what the plane has of a whole tile, or the segments of one, added in order.
 // (What does not depend on them was there before the kernel that writes them began: it is worked out while that one still runs.)
 // CTAs behind those of the tokens have columns of dbias.
 struct FinishArgs {
@@ -374,15 +378,16 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const FinishArgs a, cons
   }
   __shared__ uint16_t start[2][kMaxTilesN];      // of a tile: its first segment,
   __shared__ uint8_t many[2][kMaxTilesN];        // and how many it has (0: it is whole)
-  __shared__ int32_t row[8];
+  __shared__ int32_t row[4];
   __shared__ uint32_t lowest;
-  const uint32_t count = a.count ? *a.count : a.rows, tiles_n = (a.d + a.bn - 1) / a.bn, t0 = blockIdx.x * a.each;
+  const uint32_t count = a.count ? *a.count : a.rows, tiles_n = (a.d + a.bn - 1) / a.bn;
+  const uint32_t t0 = (a.ctas - 1 - blockIdx.x) * a.each;      // (the last tiles have the most segments: they come first)
   const float scale = *a.scale;
   // (tokens that follow one another have rows in at most two tiles)
   if (threadIdx.x < 32) {
     const uint32_t i = t0 + threadIdx.x;
     const int32_t r = threadIdx.x >= a.each || i >= a.t ? -1 : a.row ? a.row[i] : (int32_t)i;
-    if (threadIdx.x < 8) row[threadIdx.x] = r;
+    if (threadIdx.x < 4) row[threadIdx.x] = r;
     const uint32_t lo = __reduce_min_sync(0xffffffffu, r < 0 ? 0xffffffffu : (uint32_t)r / a.tile_m);
     if (threadIdx.x == 0) lowest = lo;
   }
@@ -395,8 +400,8 @@ __global__ void __launch_bounds__(256) dx_finish_kernel(const FinishArgs a, cons
       if (q < r.whole || q >= r.tiles) {
         many[m][n] = 0;
       } else {
-        start[m][n] = (uint16_t)(q - r.whole + r.first(q - r.whole));
-        many[m][n] = (uint8_t)(r.last(q - r.whole) - r.first(q - r.whole) + 1);
+        start[m][n] = (uint16_t)r.segment(q - r.whole);
+        many[m][n] = (uint8_t)r.count(q - r.whole);
       }
     }
   }
@@ -600,7 +605,7 @@ cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t t, void* dx, size_
   const DxShape s = dx_shape(a.r.most, a.d);
   // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
   uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
-  if (each > 8) each = 8;
+  if (each > 4) each = 4;
   FinishArgs f;
   f.plane = a.plane;
   f.segments = a.segments;

@@ -10,43 +10,60 @@
 
 namespace stq {
 
-// The tiles of dx, row by row, and which of `units` (CTAs or pairs) compute what of them.
+// The tiles of dx, row by row, and which of `units` (CTAs or pairs) compute what of them.  What is computed together should lie together:
+// neighbouring tiles read the same rows of p and the same columns of w, so where the units stand at the same place of their sums, those
+// come from memory once.
 //
-// Whole rounds: unit i has tiles i, i + units, ... as long as there is one for each unit.  All units then stand at the same place of their
-// sums, and what neighbouring tiles read (rows of p, columns of w) comes from memory once.
-// The `rest` tiles that are left are cut into U equal ranges, one behind the other: unit u has [u rest / U, (u + 1) rest / U) of them.
-// What a range has of a tile is a segment; tile r has the segments of units first(r) .. last(r), whatever the length of the sums, so
-// that every piece of the vocabulary adds to the same segments.  Segment (r, u) has number r + u, which no other has.
+// Whole rounds: unit i has tiles i, i + units, ... as long as there is one for each unit.
+// Of the `rest`, as many tiles as there are units for are cut into `parts` equal parts: unit i has part i / cut of tile i % cut.
+// What is left then, or all of the rest where parts would be too short, is cut into U equal ranges, one behind the other: unit u has
+// [u left / U, (u + 1) left / U) of these tiles.
+//
+// A part, and what a range has of a tile, is a segment.  Which segments a tile has does not depend on the length of the sums, so every
+// piece of the vocabulary adds to the same ones.  They are numbered: parts first, then (r, u) is units + r + u, which no other has.
 struct Ranges {
-  uint32_t tiles_m, tiles, whole, rest, U, split;
+  uint32_t units, tiles_m, tiles, whole, cut, parts, left, U;
   // k: stages of the sum (of the first piece)
-  STQ_BOTH Ranges(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t k, uint32_t units) {
+  STQ_BOTH Ranges(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t k, uint32_t units_) {
+    units = units_;
     tiles_m = (rows + tile_m - 1) / tile_m;
     tiles = tiles_m * tiles_n;
     whole = tiles / units * units;
-    rest = tiles - whole;
-    const uint64_t most = (uint64_t)rest * k / 4;      // (four stages to a range at least)
-    U = most < rest ? rest : most < units ? (uint32_t)most : units;
-    // few tiles: every tile in as many ranges, if that leaves no more than a sixteenth of the units without one.  Then those that have
-    // the same share of a row of tiles run side by side, and read whole rows of w together.
-    const uint32_t even = rest && U > rest ? U / rest * rest : 0;
-    split = even && U - even <= U / 16 ? even / rest : 0;
-    if (split) U = even;
+    left = tiles - whole;
+    cut = parts = U = 0;
+    if (left == 0) return;
+    const uint32_t even = units / left;      // parts that leave at most a sixteenth of the units without one, and are not too short
+    if (left * even >= units - units / 16 && k >= 4 * even) {
+      cut = left;
+      parts = even;
+    } else {
+      const uint32_t more = even + 1, fit = units / more;
+      // (four stages to a range at least)
+      if ((uint64_t)(left - fit) * k >= 4 * units && k >= 4 * more) {
+        cut = fit;
+        parts = more;
+      }
+    }
+    left -= cut;
+    const uint64_t most = (uint64_t)left * k / (cut ? 8 : 4);      // (next to parts, ranges are short, and every segment is read again)
+    U = most < left ? left : most < units ? (uint32_t)most : units;
   }
-  // The range that the i-th CTA or pair takes (i < U).
-  STQ_BOTH uint32_t unit(uint32_t i) const { return split ? i % rest * split + i / rest : i; }
-  // The tiles of the rest that range u has something of, and the ranges that tile r is in.
-  STQ_BOTH uint32_t tile_first(uint32_t u) const { return u * rest / U; }
-  STQ_BOTH uint32_t tile_last(uint32_t u) const { return ((u + 1) * rest - 1) / U; }
-  STQ_BOTH uint32_t first(uint32_t r) const { return r * U / rest; }
-  STQ_BOTH uint32_t last(uint32_t r) const { return ((r + 1) * U - 1) / rest; }
-  // Where range u begins in tile r, of k stages; it ends where range u + 1 begins.
+  // Tile `cut + r` of the rest: r below `left`.  The tiles that range u has something of, and the ranges that tile r is in.
+  STQ_BOTH uint32_t tile_first(uint32_t u) const { return u * left / U; }
+  STQ_BOTH uint32_t tile_last(uint32_t u) const { return ((u + 1) * left - 1) / U; }
+  STQ_BOTH uint32_t first(uint32_t r) const { return r * U / left; }
+  STQ_BOTH uint32_t last(uint32_t r) const { return ((r + 1) * U - 1) / left; }
+  // Where range u begins in tile r, of k stages (it ends where range u + 1 begins), and where a part does.
   STQ_BOTH uint32_t begin(uint32_t r, uint32_t u, uint32_t k) const {
-    const uint32_t at = u * rest, from = r * U;
+    const uint32_t at = u * left, from = r * U;
     return at <= from ? 0 : at - from >= U ? k : (uint32_t)((uint64_t)(at - from) * k / U);
   }
-  // Segments have numbers below this.
-  STQ_BOTH static uint32_t segments(uint32_t units) { return 2 * units; }
+  STQ_BOTH uint32_t begin(uint32_t part, uint32_t k) const { return (uint32_t)((uint64_t)part * k / parts); }
+  // The segments of a tile of the rest, which follow one another: the first one's number, and how many (r below cut + left).
+  STQ_BOTH uint32_t segment(uint32_t r) const { return r < cut ? r * parts : units + r - cut + first(r - cut); }
+  STQ_BOTH uint32_t count(uint32_t r) const { return r < cut ? parts : last(r - cut) - first(r - cut) + 1; }
+  // All numbers are below this.
+  STQ_BOTH static uint32_t segments(uint32_t units) { return 3 * units; }
 };
 
 }  // namespace stq

@@ -640,11 +640,11 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most,
 
 cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss, float* lse,
                                 cudaStream_t stream) {
-  // (few tokens: more threads to each)
+  // Few tokens: more threads to each.  (8192 tokens: 32 to a CTA 16 us, 8 to a CTA 22; 4096 of which 614 count: 13 and 7.)
   auto go = [&](auto* kernel, uint32_t r) {
     return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts, loss, lse);
   };
-  return a.t <= 2048 ? go(finish_kernel<4>, 4) : go(finish_kernel<8>, 8);
+  return a.t <= 2048 ? go(finish_kernel<4>, 4) : a.t <= 4096 ? go(finish_kernel<8>, 8) : go(finish_kernel<32>, 32);
 }
 
 cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,

@@ -16,41 +16,49 @@ using stq::Ranges;
 // 0: the ranges are what they have to be; else which rule is broken.  k: stages of the first piece, later: of another one.
 extern "C" int check(uint32_t rows, uint32_t tile_m, uint32_t tiles_n, uint32_t k, uint32_t later, uint32_t units) {
   const Ranges r(rows, tile_m, tiles_n, k, units);
+  const uint32_t rest = r.tiles - r.whole;
   if (r.tiles_m != (rows + tile_m - 1) / tile_m || r.tiles != r.tiles_m * tiles_n) return 1;
-  if (r.whole % units || r.whole + r.rest != r.tiles || r.rest >= units) return 2;
-  if (r.rest == 0) return 0;
-  if (r.U < r.rest || r.U > units || (r.split && r.U != r.split * r.rest)) return 3;
-  std::vector<char> taken(r.U), used(Ranges::segments(units));
-  for (uint32_t i = 0; i < r.U; ++i) {
-    if (r.unit(i) >= r.U || taken[r.unit(i)]++) return 4;                    // some range twice
-  }
-  std::vector<uint64_t> length(r.U);
-  for (uint32_t t = 0; t < r.rest; ++t) {
-    if (r.first(t) > r.last(t) || r.last(t) >= r.U) return 5;
-    for (int pass = 0; pass < 2; ++pass) {
-      const uint32_t kk = pass ? later : k;
+  if (r.whole % units || r.whole > r.tiles || rest >= units || r.cut + r.left != rest) return 2;
+  if (r.cut && (r.parts < 1 || r.cut * r.parts > units || k < 4 * r.parts)) return 3;
+  std::vector<char> used(Ranges::segments(units));
+  std::vector<uint64_t> length(units);
+  for (uint32_t t = 0; t < rest; ++t)
+    for (uint32_t i = 0; i < r.count(t); ++i) {
+      if (r.segment(t) + i >= used.size() || used[r.segment(t) + i]++) return 4;      // a number that two have
+    }
+  for (int pass = 0; pass < 2; ++pass) {
+    const uint32_t kk = pass ? later : k;
+    for (uint32_t t = 0; t < r.cut; ++t) {
+      uint32_t at = 0;
+      for (uint32_t p = 0; p < r.parts; ++p) {
+        if (r.begin(p, kk) != at || r.begin(p + 1, kk) < at) return 5;
+        at = r.begin(p + 1, kk);
+        if (!pass) length[p * r.cut + t] += at - r.begin(p, kk);
+      }
+      if (at != kk) return 6;
+    }
+    if (r.left && (r.U < r.left || r.U > units)) return 7;
+    for (uint32_t t = 0; t < r.left; ++t) {
+      if (r.first(t) > r.last(t) || r.last(t) >= r.U) return 8;
       uint32_t at = 0;
       for (uint32_t u = r.first(t); u <= r.last(t); ++u) {
         const uint32_t b = r.begin(t, u, kk), e = r.begin(t, u + 1, kk);
-        if (b != at || e < b || e > kk) return 6;                            // a gap, or twice
-        if (t < r.tile_first(u) || t > r.tile_last(u)) return 7;
-        if (pass == 0) {
-          length[u] += e - b;
-          if (t + u >= used.size() || used[t + u]++) return 8;               // two segments with one number
-        }
+        if (b != at || e < b || e > kk) return 9;                            // a gap, or twice
+        if (t < r.tile_first(u) || t > r.tile_last(u)) return 10;
+        if (r.segment(r.cut + t) + u - r.first(t) != units + t + u) return 11;
+        if (!pass) length[u] += e - b;
         at = e;
       }
-      if (at != kk) return 9;                                                // not the whole sum
+      if (at != kk) return 12;                                               // not the whole sum
     }
   }
-  uint64_t least = ~0ull, most = 0;
-  for (uint32_t u = 0; u < r.U; ++u) {
+  for (uint32_t u = 0; r.left && u < r.U; ++u)
     for (uint32_t t = r.tile_first(u); t <= r.tile_last(u); ++t)
-      if (u < r.first(t) || u > r.last(t)) return 10;                        // the two views differ
-    least = length[u] < least ? length[u] : least;
-    most = length[u] > most ? length[u] : most;
-  }
-  return most - least > 2 ? 11 : 0;                                          // not balanced
+      if (t >= r.left || u < r.first(t) || u > r.last(t)) return 13;         // the two views differ
+  uint64_t most = 0;
+  for (uint64_t l : length) most = l > most ? l : most;
+  // no unit has much more than its share: an eighth, the roundings, and what comes of ranges of eight stages at least
+  return most > (uint64_t)rest * k / units * 9 / 8 + 12 ? 14 : 0;
 }
 """
 

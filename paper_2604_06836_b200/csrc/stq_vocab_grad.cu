@@ -6,7 +6,7 @@
 // dw: its sum is over the tokens, complete within a piece of the vocabulary.  For a bf16 result p is bf16 too (2^-8 a term,
 // random in sign, as large as the rounding of the result).  For an fp32 result p comes in three bf16 parts that are together
 // exactly the fp32 gradient, and the sum leaves the matrix unit, which cuts its sums off instead of rounding them, every 128
-// terms and is added, rounded, to a running sum in tensor memory.
+// terms and is added, rounded, to a running sum in registers.
 //
 // dx: its sum is over the vocabulary, so every piece adds to it, in fp32 in memory (copies that add: nothing is read back).
 // The tiles are few (8192 x 1600: 224 for 74 pairs of CTAs), so the sums of all tiles, one after the other, are cut into
@@ -58,13 +58,15 @@ struct GradShape {
   static constexpr int kStage = kA * PARTS * MT + kB;
   // A writing warp's blocks on their way out; two where there is room for them beside the stages.  (One ragged block takes 4.5 KB.)
   static constexpr int kPlaces = MT == 1 && PARTS == 1 ? 2 : 1;
-  static constexpr int kOut = kPlaces == 2 ? 8192 : MT == 1 ? kStageBytes : 4096;
+  static constexpr bool kRagged = MT == 1;                        // rows that tensor copies cannot write
+  static constexpr int kOut = kPlaces == 2 ? 8192 : kRagged ? kStageBytes : 4096;
   static constexpr int kFit = (224 * 1024 - kWriters * kOut) / kStage;
   static constexpr int kStages = kFit < 8 ? kFit : 8;
   static constexpr int kChunk = PARTS == 3 ? 2 : 1 << 30;         // stages to one accumulator
-  static constexpr int kCols = (PARTS == 3 ? 4 : 2) * BN;         // two accumulators (and the running sum)
+  static constexpr int kCols = 2 * BN;                            // two accumulators
   static constexpr int kSmem = kStages * kStage + kWriters * kOut + 1024;
-  static_assert(MT == 1 || PARTS == 1, "the running sum takes the place of the second block");
+  static_assert(MT == 1 || PARTS == 1, "a running sum is kept of one block of rows");
+  static_assert(!kRagged || kOut >= 32 * kStageRow, "room for a ragged block");
 };
 
 // One work item: tile (its row and column), stages [k0, k1) of its sum, and where the result goes.
@@ -219,12 +221,11 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
     const int quad = warp & 3, group = (warp - 2) / 4, block = MT == 1 ? 0 : group;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16, stage = outs + (warp - 2) * S::kOut;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
-    static_assert(MT > 1 || S::kOut >= 32 * kStageRow, "room for a ragged block");
     uint32_t n = 0, puts = 0;
     constexpr int kC = 128 / sizeof(O);
     const float scale = DW ? *a.scale : 1.f;
     items([&](const Item& w) {
-      const uint32_t within = block * 128 * CG + 128 * rank + quad * 32, row = w.row + within, running = tmem + lanes + 2 * BN;
+      const uint32_t within = block * 128 * CG + 128 * rank + quad * 32, row = w.row + within;
       const uint32_t end = min(a.bn, a.n - w.col);
       const bool add = !DW && !a.begin;
       // Blocks of kC columns; the last one of a tile begins early where the tile is not a whole number of them (what is
@@ -247,7 +248,7 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
             float* part = a.part + ((size_t)w.share * kTileM + within) * a.bn;
 #pragma unroll
             for (int i = 0; i < kC; i += 32) store_part(part + c + i, a.bn, v + i, lane);
-          } else if (MT == 1 && !a.aligned) {
+          } else if (S::kRagged && !a.aligned) {
             if (col < a.n) store_ragged(out, a.ldo, v, rows, (int)min((uint32_t)kC, a.n - col), lane, raw + (stage - smem_addr(raw)));
           } else if (rows > 0) {
             put_block<O, false, S::kPlaces>(&map_o, (int)col, (int)row, v, lane, stage, puts);
@@ -274,37 +275,42 @@ vocab_grad_kernel(const __grid_constant__ CUtensorMap map_p, const __grid_consta
         });
         return true;
       }
+      float run[PARTS == 3 ? BN / 64 : 1][32];
       for (uint32_t k = w.k0; k < w.k1; k += min((uint32_t)S::kChunk, w.k1 - k), ++n) {
         const uint32_t acc = MT == 1 ? n & 1 : block, from = tmem + lanes + acc * BN;
-        const bool first = k == w.k0, last = w.k1 - k <= (uint32_t)S::kChunk;
+        const bool first = k == w.k0;
         ok = bar_wait(done + 8 * acc, (MT == 1 ? n >> 1 : n) & 1);
         if (!(ok = __all_sync(0xffffffffu, ok))) return false;
         mma_fence_after();
-        blocks([&](uint32_t c, uint32_t over) {
-          float v[kC];
-          load_block(from + c, v);
-          if constexpr (PARTS == 3) {
-            static_assert(PARTS == 1 || kC == 32, "one block of columns to a load");
-            if (!first) {
-              float old[32];
-              load_block(running + c, old);
+        if constexpr (PARTS == 3) {      // to the running sum; the results leave below, while the next item is multiplied
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], old[i]);
-            }
-            if (!last) {
-              uint32_t r[32];
+          for (int b = 0; b < BN / 64; ++b) {
+            const uint32_t c = (2 * b + group) * 32;
+            if (c >= end) break;
+            float v[32];
+            load_block(from + c, v);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
-              tmem_store(running + c, r);
-              return;
-            }
+            for (int i = 0; i < 32; ++i) run[b][i] = first ? v[i] : __fadd_rn(run[b][i], v[i]);
           }
-          emit(c, over, v);
-        });
-        if (PARTS == 3) tmem_store_wait();
+        } else {
+          blocks([&](uint32_t c, uint32_t over) {
+            float v[kC];
+            load_block(from + c, v);
+            emit(c, over, v);
+          });
+        }
         mma_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
+      }
+      if constexpr (PARTS == 3) {
+        static_assert(PARTS == 1 || kC == 32, "a block of columns to each part of the running sum");
+#pragma unroll
+        for (int b = 0; b < BN / 64; ++b) {
+          const uint32_t c = (2 * b + group) * 32;
+          if (c >= end) break;
+          emit(c, 0, run[b]);
+        }
       }
       return true;
     });
@@ -455,7 +461,7 @@ uint32_t tile_columns(uint32_t n, uint32_t widest, uint32_t unit) {
 }
 
 struct DwPlan {
-  int cg, bn_max, mt;
+  int cg, mt;
   uint32_t bn, tiles_m, tiles, full, splits;
   double cost;
 };
@@ -471,9 +477,9 @@ DwPlan dw_plan(const VocabDw& a, int sms) {
   DwPlan best = {};
   double least = 1e300;
   for (const auto& sh : shapes[a.f32]) {
-    if (sh.cg == 0 || (sh.mt > 1 && !copy_fits(a.dw, a.d * e, a.lddw * e))) continue;
+    if (sh.cg == 0 || (sh.mt > 1 && !copy_fits(a.dw, a.d * e, a.lddw * e))) continue;      // (two blocks of rows: no room for ragged ones)
     const uint32_t tile_m = 128 * sh.cg * sh.mt;
-    DwPlan p = {sh.cg, sh.bn, sh.mt, tile_columns(a.d, sh.bn, a.f32 ? 32 : 16), (a.cols + tile_m - 1) / tile_m, 0, 0, 0, 0.0};
+    DwPlan p = {sh.cg, sh.mt, tile_columns(a.d, sh.bn, a.f32 ? 32 : 16), (a.cols + tile_m - 1) / tile_m, 0, 0, 0, 0.0};
     p.tiles = p.tiles_m * ((a.d + p.bn - 1) / p.bn);
     const double products = 2.0 * p.bn * parts * sh.mt, stage = products > sh.copies ? products : sh.copies;
     const uint64_t units = sms / p.cg, rounds = p.tiles / units, full = rounds * units, rest = p.tiles - full;

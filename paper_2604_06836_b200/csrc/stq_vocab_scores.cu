@@ -153,12 +153,13 @@ struct ScoreArgs {
 constexpr int kWriters = 8;            // warps that take results out of tensor memory: two to each quarter of its lanes
 
 // The matrix unit cuts its fp32 sums off instead of rounding them, always towards zero: over a sum of 4096 a logit lost 2e-6 of itself,
-// and the loss 4e-6 where the vocabulary is small.  For the loss, and for gradients in three parts (an fp32 result), the sum
-// therefore leaves the unit every kChunk stages and is added, rounded, in registers.  (The accumulators take turns, so the next part is
-// multiplied meanwhile.)  For gradients in one bf16 number that error is nothing.
-template <int CG, int BN, int PLANES>  // PLANES = 0: the loss
+// and the loss 4e-6 where the vocabulary is small.  For the loss and for what becomes an fp32 result (gradients in three parts, dbias) the
+// sum therefore leaves the unit every kChunk stages and is added, rounded, in registers.  (The accumulators take turns, so the next part
+// is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
+// alone that error is nothing, and they take 1 to 2 % less time without.
+template <int CG, int BN, int PLANES, bool SUMS>  // PLANES = 0: the loss; SUMS: gradients in one number, and dbias
 struct ScoreShape {
-  static constexpr bool kExact = PLANES != 1;
+  static constexpr bool kExact = PLANES != 1 || SUMS;
   static constexpr int kChunk = kExact ? 8 : 1 << 30;
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
@@ -182,11 +183,11 @@ __device__ __forceinline__ float lane_sums(float (&v)[32], int lane) {
   return v[0];
 }
 
-template <int CG, int BN, int PLANES>
-__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES>::kThreads), 1)
+template <int CG, int BN, int PLANES, bool SUMS>
+__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES, SUMS>::kThreads), 1)
 score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_p,
              const ScoreArgs a) {
-  using S = ScoreShape<CG, BN, PLANES>;
+  using S = ScoreShape<CG, BN, PLANES, SUMS>;
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
@@ -419,7 +420,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             for (int i = 0; i < 64; ++i)
               if (col + i >= end) v[i] = 0.f;
           }
-          if (a.dbias) {
+          if ((PLANES == 3 || SUMS) && a.dbias) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               float b[32];
@@ -557,9 +558,9 @@ uint32_t units_of(VocabShape s, uint32_t rows, uint32_t tiles_n, int sms) {
 }
 bool merged(VocabShape s, uint32_t most) { return most <= 128u * s.cg; }
 
-template <int CG, int BN, int PLANES>
+template <int CG, int BN, int PLANES, bool SUMS>
 cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
-  using S = ScoreShape<CG, BN, PLANES>;
+  using S = ScoreShape<CG, BN, PLANES, SUMS>;
   s.count = a.r.count;
   s.rows = a.r.rows;
   s.most = a.r.most;
@@ -576,17 +577,17 @@ cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGr
   cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, rows, kDepth, true);
   if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, s.wide / CG, kDepth, true);
   if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->panels * o->planes, 64, 64, 32, 64, true);
-  auto* kernel = score_kernel<CG, BN, PLANES>;
+  auto* kernel = score_kernel<CG, BN, PLANES, SUMS>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, a.device, seen);
   if (e != cudaSuccess) return e;
   return launch_with(kernel, units_of(sh, a.r.rows, s.tiles_n, sms) * CG, S::kThreads, S::kSmem, CG, true, stream, mx, mw, mp, s);
 }
 
-template <int PLANES>
+template <int PLANES, bool SUMS = false>
 cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
   constexpr int kPair = PLANES == 3 ? 128 : 256;
-  return sh.cg == 2 ? launch<2, kPair, PLANES>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES>(a, sh, s, o, sms, stream);
+  return sh.cg == 2 ? launch<2, kPair, PLANES, SUMS>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES, SUMS>(a, sh, s, o, sms, stream);
 }
 
 }  // namespace
@@ -662,7 +663,9 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0,
   s.ldb = o.ldb;
   s.panels = o.panels;
   s.err = err;
-  return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream) : by_shape<1>(a, sh, s, &o, sms, stream);
+  return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream)
+         : o.dbias     ? by_shape<1, true>(a, sh, s, &o, sms, stream)
+                       : by_shape<1>(a, sh, s, &o, sms, stream);
 }
 
 }  // namespace stq

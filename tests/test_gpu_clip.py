@@ -257,3 +257,29 @@ def test_a_step_with_a_norm_that_is_not_finite_is_left_out():
     assert opt.t == 1 and not torch.equal(ps[0], before[0])
     with pytest.raises(ValueError, match="max_norm"):
         STQAdamW(ps, max_norm=0.0)
+
+
+def test_a_tensor_of_more_than_32_bits_of_elements(handle):
+    n = (1 << 31) + 12345
+    g = torch.zeros(n, device="cuda", dtype=BF)
+    g[-5:] = 3.0
+    g[:4] = 1.0
+    r = clip.grad_norm(handle, [g], max_norm=0.5)
+    near(r.norm, 7.0, NORM)
+    clip.clip_grads(handle, [g], 3.5)      # factor 1 / 2, up to eps
+    assert g[-5:].tolist() == [1.5] * 5 and g[:4].tolist() == [0.5] * 4 and float(g[n // 2].float()) == 0.0
+
+
+def test_two_handles_at_once():
+    a, b = stq.Handle(), stq.Handle()
+    one, two = many([1 << 22, 777], [F32], 1), many([1 << 20] * 300, [BF], 2)
+    want = clip.grad_norm(a, one).norm, clip.grad_norm(b, two).norm
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(10):
+        got.append((0, clip.grad_norm(a, one, stream=s[0]).norm))
+        got.append((1, clip.grad_norm(b, two, stream=s[1]).norm))
+    torch.cuda.synchronize()
+    assert all(torch.equal(n, want[i]) for i, n in got)
+    a.close(), b.close()

@@ -113,7 +113,7 @@ SIZES = [(1, 1, 1), (1, 64, 100), (1, 1600, 1283), (2, 8, 2), (3, 77, 131), (61,
 @pytest.mark.parametrize("d", [1, 7, 8, 33, 250, 1000, 1024, 1032, 1601, 2050, 4096, 5000])
 @pytest.mark.parametrize("t", [1, 3, 8, 9, 16, 17])
 def test_few_tokens(handle, t, d):
-    """Up to 16 tokens (and as many as their shared memory holds) go by the matrix, read in other steps than tiles."""
+    """A tile of which most rows are not there."""
     for v in (1, 15, 16, 17, 250, 9001):
         x, w, target, b, dloss = inputs(t, d, v, t + d + v, v % 2 == 1, 0.2 if t > 2 else 0.0)
         out = vocab.loss(handle, x, w, target, bias=b)
@@ -411,3 +411,64 @@ def test_tokens_that_repeat(handle):
     out, grads = run(handle, x, w, target, b, dloss, F32)
     assert (out.loss == out.loss[0]).all() and (grads.dx == grads.dx[0]).all()
     Definition(x, w, target, b, dloss).check(out, grads, F32, "repeated")
+
+
+@pytest.mark.parametrize("t,d,v", [(3, 65536, 70), (300, 65536, 40), (10, 20001, 300), (262144, 24, 900)])
+def test_the_largest_widths_and_batches(handle, t, d, v):
+    x, w, target, b, dloss = inputs(t, d, v, 1, True, 0.1)
+    out, grads = run(handle, x, w, target, b, dloss, F32)
+    Definition(x, w, target, b, dloss).check(out, grads, F32, f"{t} {d} {v}")
+
+
+def test_more_than_the_largest_is_refused(handle):
+    x, w, target, b, dloss = inputs(3, 8, 5, 1)
+    big = torch.zeros(262145, 8, device="cuda", dtype=BF)
+    with pytest.raises(ValueError, match="262144"):
+        vocab.loss(handle, big, w, torch.zeros(262145, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError, match="65536"):
+        vocab.loss(handle, big.view(-1)[:65537].view(1, -1), torch.zeros(2, 65537, device="cuda", dtype=BF), target[:1])
+
+
+def test_offsets_that_pass_32_bits(handle):
+    """A matrix of 2.2e9 elements: the entries behind the 2^31st are where they belong, in z, in dx and in dw."""
+    v, d, t = 540000, 4096, 6
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.empty(v, d, device="cuda", dtype=BF)
+    for i in range(0, v, 20000):
+        w[i:i + 20000] = torch.randn(min(20000, v - i), d, device="cuda", generator=g) / 64.0
+    x = torch.randn(t, d, device="cuda", generator=g).to(BF)
+    target = torch.tensor([0, v - 1, v - 2, 524288, 524287, 100000], device="cuda")
+    dloss = torch.ones(t, device="cuda") / t
+    out = vocab.loss(handle, x, w, target)
+    grads = vocab.loss_backward(handle, dloss, x, w, target, out.lse)
+    z = torch.cat([x.double() @ w[i:i + 20000].double().T for i in range(0, v, 20000)], dim=1)
+    lse = torch.logsumexp(z, 1)
+    assert float((out.lse.double() - lse).abs().max()) <= 1e-4
+    assert float((out.loss.double() - (lse - z.gather(1, target[:, None])[:, 0])).abs().max()) <= 1e-4
+    p = torch.exp(z - lse[:, None])
+    p.scatter_add_(1, target[:, None], -torch.ones(t, 1, device="cuda", dtype=torch.float64))
+    p /= t
+    dx = sum(p[:, i:i + 20000] @ w[i:i + 20000].double() for i in range(0, v, 20000))
+    assert float((grads.dx.double() - dx).norm() / dx.norm()) <= 3 * UB
+    for rows in (slice(0, 300), slice(524200, 524400), slice(v - 300, v)):
+        want = p[:, rows].T @ x.double()
+        assert float((grads.dw[rows].double() - want).norm() / want.norm()) <= 3 * UB
+
+
+def test_two_handles_at_once():
+    """Calls of two handles on two streams overlap and do not disturb one another."""
+    a, b = stq.Handle(), stq.Handle()
+    one, two = inputs(900, 300, 4000, 1, True, 0.2), inputs(400, 512, 7000, 2, False, 0.0)
+    want = run(a, *one, F32), run(b, *two, BF)
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(8):
+        with torch.cuda.stream(s[0]):
+            got.append((0, run(a, *one, F32)))
+        with torch.cuda.stream(s[1]):
+            got.append((1, run(b, *two, BF)))
+    torch.cuda.synchronize()
+    for i, g in got:
+        assert all(torch.equal(x, y) for p, q in zip(g, want[i]) for x, y in zip(p, q) if x is not None)
+    a.close(), b.close()

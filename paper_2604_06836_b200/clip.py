@@ -4,7 +4,8 @@ Thin binding over ``stq_grad_norm`` and ``stq_grad_clip``, in the manner of ``q8
 the current stream of the handle's device (or on ``stream``).  ``optim.STQAdamW(max_norm=...)`` takes the factor into its step, which
 then clips without writing the gradients; ``clip_grads`` is for every other optimizer.
 
-Gradients are float32, bfloat16 or float16, each its own, in any dense layout (no gaps, no overlap); None is passed over.
+Gradients are float32, bfloat16 or float16, each its own, in any dense layout (no gaps, no overlap); None is passed over.  A
+generator of them will do.
 """
 from __future__ import annotations
 
@@ -48,6 +49,11 @@ def _scalar(name, t, dev):
     return t.data_ptr()
 
 
+def _kept(tensors):
+    """A list of them that can be gone through more than once (a generator cannot)."""
+    return tensors if tensors is None or isinstance(tensors, (list, tuple)) else list(tensors)
+
+
 def _call(clipped: bool, handle, grads, out, max_norm, inv_scale, found_inf, eps) -> Norm:
     L, dev = _fn or _lib(), handle.device
     max_norm = math.inf if max_norm is None else float(max_norm)
@@ -70,6 +76,7 @@ def grad_norm(handle: stq.Handle, grads: Sequence[Optional[torch.Tensor]], *, ma
               inv_scale: torch.Tensor | None = None, found_inf: torch.Tensor | None = None, eps: float = 1e-6, stream=None) -> Norm:
     """norm = inv_scale * 2-norm of all gradients, factor = inv_scale * min(1, max_norm / (norm + eps)).  ``inv_scale``: one float32
     on the device (1 / loss scale); ``found_inf``: one float32 on the device, set to 1 where the norm is not finite."""
+    grads = _kept(grads)
     if stream is not None:
         with _On(stream, (*grads, inv_scale, found_inf)):
             return grad_norm(handle, grads, max_norm=max_norm, inv_scale=inv_scale, found_inf=found_inf, eps=eps)
@@ -81,6 +88,7 @@ def clip_grads(handle: stq.Handle, grads: Sequence[Optional[torch.Tensor]], max_
                out: Sequence[Optional[torch.Tensor]] | None = None, stream=None) -> Norm:
     """``grad_norm``, and the gradients times the factor: in place, or written to ``out`` (a tensor for each gradient, of its type or
     float32; the gradients stay as they are)."""
+    grads, out = _kept(grads), _kept(out)
     if stream is not None:
         with _On(stream, (*grads, *(out or ()), inv_scale, found_inf)):
             return clip_grads(handle, grads, max_norm, inv_scale=inv_scale, found_inf=found_inf, eps=eps, out=out)

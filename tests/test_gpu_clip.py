@@ -200,6 +200,24 @@ def test_on_another_stream(handle):
     near(r.norm, 2.0 * 4096, NORM)
 
 
+def test_generators(handle):
+    """A generator is gone through once, also where its tensors are needed twice (on another stream, counted as changed)."""
+    g = [torch.full((100,), 2.0, device="cuda"), None, torch.full((300,), 2.0, device="cuda")]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for stream in (None, s):
+        near(clip.grad_norm(handle, (t for t in g), stream=stream).norm, 40.0, NORM)
+        out = [None if t is None else torch.empty_like(t) for t in g]
+        before = [(t._version, o._version) for t, o in zip(g, out) if t is not None]
+        clip.clip_grads(handle, iter(g), 20.0, out=iter(out), stream=stream)
+        torch.cuda.current_stream().wait_stream(s)
+        assert [(t._version, o._version) for t, o in zip(g, out) if t is not None] == [(a, b + 1) for a, b in before]
+        assert all(torch.allclose(o, t * 0.5) for t, o in zip(g, out) if t is not None)
+    clip.clip_grads(handle, (t for t in g), 20.0, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.allclose(t, torch.ones_like(t)) for t in g if t is not None)
+
+
 def parameters(seed=0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     return [torch.nn.Parameter(torch.randn(n, device="cuda", generator=g)) for n in (4096, 1000, 13, 70000)]

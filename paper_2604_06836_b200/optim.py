@@ -153,7 +153,7 @@ class STQAdamW(torch.optim.Optimizer):
                 loss = closure()
         scale = self._clip_factor()
         if self.found_inf is not None and float(self.found_inf.item()) != 0.0:
-            self.skipped_steps += 1       # nothing is launched, t does not advance, carried statistics are kept
+            self.skipped_steps += 1       # no step is launched, t does not advance, carried statistics are kept
             return loss
         self.t += 1
         t = self.t

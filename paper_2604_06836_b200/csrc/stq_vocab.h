@@ -63,11 +63,12 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
 
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms);
-// (most: the one that the parts were counted for)
-cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, float2* part, int sms, int* err, cudaStream_t stream);
-// loss and lse of all tokens from the parts.  x and ldx: the tokens' hidden states as they were given.
-cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss,
-                                float* lse, cudaStream_t stream);
+// (most: the one that the parts were counted for.)  chosen[row]: the logit of the row's target, if that is in the vocabulary.
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, float2* part, float* chosen, int sms, int* err,
+                               cudaStream_t stream);
+// loss and lse of all tokens from these.
+cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse,
+                                cudaStream_t stream);
 
 // Gradients of the logits of entries [v0, v1), divided by scale: `planes` bf16 numbers (1 or 3) whose sum they are.  They lie in panels
 // of 64 entries, p[plane][(v - v0) / 64][row][(v - v0) % 64], `panels` to a plane and `most` rows to a panel, so that every box that is

@@ -150,10 +150,12 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   const uint32_t parts = vocab_parts(a, shape, most, h->sm_count);
   Arena m;
   float2* part = nullptr;
+  float* chosen = nullptr;
   for (int pass = 0; pass < 2; ++pass) {
     m.at = 0;
     r.place(m, a, most);
     part = m.take<float2>((size_t)parts * most);
+    chosen = m.take<float>(most);
     if (pass == 0) STQ_TRY(workspace(h, m.at, s, &m.base));
   }
   for (uint64_t t0 = 0; t0 < t; t0 += at_once) {
@@ -163,8 +165,8 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     const uint16_t* xb = static_cast<const uint16_t*>(x) + t0 * ldx;
     int launches = 2;
     STQ_CUDA(h, prepare_rows(b, r, xb, ldx, nullptr, t0 == 0, s, &launches));
-    STQ_CUDA(h, launch_vocab_parts(b, shape, most, part, h->sm_count, h->d_err, s));
-    STQ_CUDA(h, launch_vocab_finish(b, xb, ldx, part, parts, loss + t0, lse + t0, s));
+    STQ_CUDA(h, launch_vocab_parts(b, shape, most, part, chosen, h->sm_count, h->d_err, s));
+    STQ_CUDA(h, launch_vocab_finish(b, part, parts, chosen, loss + t0, lse + t0, s));
     h->launches += launches;
   }
   return STQ_OK;

@@ -135,12 +135,13 @@ struct ScoreArgs {
   int merge;               // the loss of a single tile of rows: a CTA's tiles make one part
   uint32_t stage_bytes;    // that are copied to a stage (of a CTA)
   const float* bias;
-  // loss
-  float2* part;
-  // gradients
   const uint32_t* token;
   const int64_t* target;
   int64_t ignore;
+  // loss
+  float2* part;
+  float* chosen;
+  // gradients
   const float* lse;
   const float* dloss;
   const float* scale;
@@ -156,7 +157,8 @@ constexpr int kWriters = 8;            // warps that take results out of tensor 
 // and the loss 4e-6 where the vocabulary is small.  For the loss and for what becomes an fp32 result (gradients in three parts, dbias) the
 // sum therefore leaves the unit every kChunk stages and is added, rounded, in registers.  (The accumulators take turns, so the next part
 // is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
-// alone that error is nothing, and they take 1 to 2 % less time without.
+// alone p is off by no more than 2e-6 |z|, which matters to no gradient but that of a target with p above 0.99, and they take 1 to 2 %
+// less time without (8192 tokens, 50257 entries, 1600 columns: loss and gradients 4113 instead of 4168 us).
 template <int CG, int BN, int PLANES, bool SUMS>  // PLANES = 0: the loss; SUMS: gradients in one number, and dbias
 struct ScoreShape {
   static constexpr bool kExact = PLANES != 1 || SUMS;
@@ -277,20 +279,20 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
       const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + half * (BN / 2);
       const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
-      // gradients: what this row is multiplied with, its normaliser and its target, if that lies in these columns
+      // this row's target, if it lies in these columns; gradients: what the row is multiplied with, and its normaliser
       float g = 0.f, lse = 0.f;
       int32_t hit = -1;
       bool real = false;
-      if constexpr (PLANES > 0) {
-        if (row < count) {
-          const uint32_t t = a.token ? a.token[row] : row;
-          const int64_t to = a.target[t];
-          real = to != a.ignore;
-          if (real) {
+      if (row < count) {
+        const uint32_t t = a.token ? a.token[row] : row;
+        const int64_t to = a.target[t];
+        real = to != a.ignore;
+        if (real) {
+          if constexpr (PLANES > 0) {
             g = __fdiv_rn(a.dloss[t], scale);
             lse = a.lse[t];
-            if (to >= col0 && to < col0 + BN / 2) hit = (int32_t)(to - col0);
           }
+          if (to >= col0 && to < min(end, col0 + BN / 2)) hit = (int32_t)(to - col0);
         }
       }
       float bias[BN / 64];      // of column 32 i + lane
@@ -355,6 +357,14 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < 32; ++i)
               if (col + i >= end) v[i] = -INFINITY;
+          }
+          const int at = hit - c;      // (few rows have their target in the block)
+          if (__any_sync(0xffffffffu, at >= 0 && at < 32)) {
+            float z = 0.f;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (at == i) z = v[i];
+            if (at >= 0 && at < 32) a.chosen[row] = z;
           }
           float tops[4] = {m, m, m, m};
 #pragma unroll
@@ -470,60 +480,25 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(top, __fadd_rn(__fmul_rn(a.y, ex2((a.x - ref) * kLog2e)), __fmul_rn(b.y, ex2((b.x - ref) * kLog2e))));
 }
 
-// R tokens to a CTA: 256 / R threads share the parts of each.  Before that, while the products may still run, a warp forms the logit
-// of a token's target, in fp32 from the bf16 operands.  (Taken from the tensor memory it would carry the matrix unit's cut-off sums.)
+// R tokens to a CTA: 256 / R threads share the parts of each.  The target's logit is the one that went into the sum: where the target has
+// nearly all of it, lse and logit agree in all but their last bits, and what two products round differently would be the loss.  (929
+// columns, loss 0.09, lse 7.6: off by 4e-6 with the logit formed apart in fp32.)  For the same reason the loss comes from the maximum, not
+// from lse, whose rounding is larger.
 template <int R>
-__global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const uint16_t* x, size_t ldx, const float2* part, uint32_t parts,
-                                                     float* loss, float* lse) {
+__global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const float2* part, uint32_t parts, const float* chosen, float* loss,
+                                                     float* lse) {
   __shared__ float2 sums[8][R];
-  __shared__ float chosen[R];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t t0 = blockIdx.x * R;
-  const uint16_t* w = static_cast<const uint16_t*>(a.w);
-  for (int i = warp; i < R; i += 8) {
-    const uint32_t t = t0 + i;
-    float z = 0.f;
-    const int64_t to = t < a.t ? a.target[t] : a.ignore;
-    if (to != a.ignore) {
-      if (to < 0 || to >= (int64_t)a.v) {
-        z = __int_as_float(0x7fc00000);
-      } else {
-        // (a gathered row is aligned; it was there before the products began)
-        const uint16_t *p = a.r.row ? static_cast<const uint16_t*>(a.r.x) + (size_t)a.r.row[t] * a.r.ldx : x + (size_t)t * ldx;
-        const uint16_t* q = w + (size_t)to * a.ldw;
-        float s[2] = {0.f, 0.f};
-        if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0) {
-          const uint32_t whole = a.d & ~7u;
-#pragma unroll 4
-          for (uint32_t c = 8 * lane; c < whole; c += 256) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(p + c)), y = __ldg(reinterpret_cast<const uint4*>(q + c));
-            const uint32_t us[4] = {u.x, u.y, u.z, u.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              s[0] = __fmaf_rn(__uint_as_float(us[j] << 16), __uint_as_float(ys[j] << 16), s[0]);
-              s[1] = __fmaf_rn(__uint_as_float(us[j] & 0xffff0000u), __uint_as_float(ys[j] & 0xffff0000u), s[1]);
-            }
-          }
-          if (lane < (a.d & 7))
-            s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[whole + lane] << 16), __uint_as_float((uint32_t)q[whole + lane] << 16), s[0]);
-        } else {
-#pragma unroll 8
-          for (uint32_t c = lane; c < a.d; c += 32) s[0] = __fmaf_rn(__uint_as_float((uint32_t)p[c] << 16), __uint_as_float((uint32_t)q[c] << 16), s[0]);
-        }
-        z = s[0] + s[1];
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (a.bias) z += a.bias[to];
-      }
-    }
-    if (lane == 0) chosen[i] = z;
-  }
   constexpr int kGroups = 256 / R;
   const int mine = threadIdx.x % R, group = threadIdx.x / R;
   const uint32_t t = t0 + mine;
+  // (targets and rows were there before the products began)
+  const int64_t to = t < a.t ? a.target[t] : a.ignore;
+  int32_t row = -1;
+  if (to != a.ignore) row = a.r.row ? a.r.row[t] : (int32_t)t;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");
-  int32_t row = -1;
-  if (t < a.t) row = a.r.row ? a.r.row[t] : a.target[t] != a.ignore ? (int32_t)t : -1;
   float2 sum = make_float2(-INFINITY, 0.f);
   if (row >= 0) {
     for (uint32_t i0 = group; i0 < parts; i0 += 8 * kGroups) {
@@ -544,10 +519,16 @@ __global__ void __launch_bounds__(256) finish_kernel(const VocabArgs a, const ui
   __syncthreads();
   if (threadIdx.x >= R || t >= a.t) return;
   for (int i = 1; i < 8; ++i) sum = join(sum, sums[i][mine]);
-  const float total = row < 0 ? 0.f : (sum.x == -INFINITY ? 0.f : sum.x) + logf(sum.y), z = chosen[mine];
-  // (the NaN of a target outside the vocabulary goes into lse as well: all gradients of the token are NaN)
-  lse[t] = z != z && row >= 0 ? z : total;
-  loss[t] = row < 0 ? 0.f : total - z;
+  float z = 0.f, top = 0.f, rest = 0.f;
+  if (row >= 0) {
+    // (the NaN of a target outside the vocabulary goes into lse as well: all gradients of the token are NaN)
+    const bool inside = to >= 0 && to < (int64_t)a.v;
+    z = inside ? __ldcg(chosen + row) : __int_as_float(0x7fc00000);
+    top = !inside ? z : sum.x == -INFINITY ? 0.f : sum.x;
+    rest = logf(sum.y);
+  }
+  lse[t] = top + rest;
+  loss[t] = (top - z) + rest;
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -629,21 +610,26 @@ uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms) {
   return 2 * (merged(s, most) ? units_of(s, most, tiles, sms) : tiles);
 }
 
-cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most, float2* part, int sms, int* err, cudaStream_t stream) {
+cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most, float2* part, float* chosen, int sms, int* err,
+                               cudaStream_t stream) {
   ScoreArgs s = {};
   s.v0 = 0;
   s.v1 = a.v;
+  s.token = a.r.token;
+  s.target = a.target;
+  s.ignore = a.ignore;
   s.part = part;
+  s.chosen = chosen;
   s.merge = merged(sh, most);
   s.err = err;
   return by_shape<0>(a, sh, s, nullptr, sms, stream);
 }
 
-cudaError_t launch_vocab_finish(const VocabArgs& a, const void* x, size_t ldx, const float2* part, uint32_t parts, float* loss, float* lse,
+cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse,
                                 cudaStream_t stream) {
   // Few tokens: more threads to each.  (8192 tokens: 32 to a CTA 16 us, 8 to a CTA 22; 4096 of which 614 count: 13 and 7.)
   auto go = [&](auto* kernel, uint32_t r) {
-    return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, static_cast<const uint16_t*>(x), ldx, part, parts, loss, lse);
+    return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, part, parts, chosen, loss, lse);
   };
   return a.t <= 2048 ? go(finish_kernel<4>, 4) : a.t <= 4096 ? go(finish_kernel<8>, 8) : go(finish_kernel<32>, 32);
 }

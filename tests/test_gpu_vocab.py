@@ -123,6 +123,34 @@ def test_few_tokens(handle, t, d):
         assert torch.equal(out.lse, again.lse)
 
 
+@pytest.mark.parametrize("d", [77, 929, 4096])
+@pytest.mark.parametrize("t", [1, 3, 40, 129, 700])
+def test_loss_of_confident_tokens(handle, t, d):
+    """Where the target has nearly all of the sum, the loss is much smaller than lse and the target's logit, and what these are off by must
+    not show.  loss = log(1 + sum of exp(z_j - z_target) over the others): off by those terms' shares times their errors, by 11 additions
+    to a sum that holds a 1 (32 entries: 8 to each of four sums, these joined, and joined to what there was), and by the roundings of
+    log, of the difference and of the result."""
+    v, g = 32, torch.Generator(device="cuda").manual_seed(t + d)
+    w = (torch.randn(v, d, device="cuda", generator=g) * (2 / d ** 0.5)).to(BF)
+    target = torch.randint(0, v, (t,), device="cuda", generator=g)
+    sure = 1 + 3 * torch.rand(t, 1, device="cuda", generator=g)
+    x = (0.3 * torch.randn(t, d, device="cuda", generator=g) + sure * w[target].float()).to(BF)
+    if t > 3:
+        target[::5] = IGNORE
+    out = vocab.loss(handle, x, w, target)
+    x, w, counts = x.double(), w.double(), target != IGNORE
+    at = torch.where(counts, target, 0)[:, None]
+    z, a = x @ w.T, x.abs() @ w.abs().T
+    dz = 2 * U * (d / 16 + 2) * a + U * z.abs()
+    apart = z - z.gather(1, at)
+    others = torch.softmax(z, 1).scatter(1, at, 0.0)
+    loss = torch.logsumexp(apart, 1)
+    off = (others * (dz + dz.gather(1, at) + 8 * U * (apart.abs() + apart.amax(1, keepdim=True) + 2))).sum(1) + 11 * U + 4 * U * loss
+    assert (out.loss[~counts] == 0).all() and (out.loss >= 0).all()
+    bad = counts & ~((out.loss.double() - loss).abs() <= off)
+    assert not bad.any(), ((out.loss.double() - loss)[bad], loss[bad])
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("t,d,v", SIZES)
 def test_loss_and_gradients(handle, t, d, v, dtype):

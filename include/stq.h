@@ -365,7 +365,8 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
 /* Gradients for dloss[t] (fp32) and lse as stq_vocab_loss wrote it; each of dx (bf16 [t][d]), dw ([v][d], bf16 or
  * fp32) and dbias (fp32[v]) may be NULL.  The gradients of the logits, relative to the largest |dloss| of a token that counts, enter
  * the matrix units as bf16, 2^-8 relative a term (in the 2-norm dx and dw are off by 0.002, against 0.0017 of their own
- * rounding; a sum of 4096 columns in the matrix units takes up to 2e-6 off a logit, which shows in a target's p - 1 where p > 0.99); for an fp32 dw as three bf16 numbers that are together exact, at three times the cost of that product. */
+ * rounding; a sum of 4096 columns in the matrix units takes up to 2e-6 off a logit, which shows in a target's p - 1 where p > 0.99);
+ * for an fp32 dw as three bf16 numbers that are together exact, at three times the cost of that product. */
 int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, uint64_t ldx, const void* w, uint64_t ldw,
                             const float* bias, const int64_t* target, int64_t ignore_index, const float* lse, uint64_t t, uint32_t v,
                             uint32_t d, void* dx, uint64_t lddx, void* dw, uint64_t lddw, int dw_dtype, float* dbias, void* stream);

@@ -131,6 +131,7 @@ struct ScoreArgs {
   const uint32_t* count;
   uint32_t rows, most;
   uint32_t v0, v1, ksteps, tiles_n;
+  uint32_t chunk;          // stages after which sums leave the matrix unit, a power of two
   uint32_t wide;           // entries of the vocabulary to a tile, at most BN
   int merge;               // the loss of a single tile of rows: a CTA's tiles make one part
   uint32_t stage_bytes;    // that are copied to a stage (of a CTA)
@@ -155,14 +156,13 @@ constexpr int kWriters = 8;            // warps that take results out of tensor 
 
 // The matrix unit cuts its fp32 sums off instead of rounding them, always towards zero: over a sum of 4096 a logit lost 2e-6 of itself,
 // and the loss 4e-6 where the vocabulary is small.  For the loss and for what becomes an fp32 result (gradients in three parts, dbias) the
-// sum therefore leaves the unit every kChunk stages and is added, rounded, in registers.  (The accumulators take turns, so the next part
-// is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
+// sum therefore leaves the unit every `chunk` stages (VocabShape) and is added, rounded, in registers.  (The accumulators take turns, so the
+// next part is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
 // alone p is off by no more than 2e-6 |z|, which matters to no gradient but that of a target with p above 0.99, and they take 1 to 2 %
 // less time without (8192 tokens, 50257 entries, 1600 columns: loss and gradients 4113 instead of 4168 us).
 template <int CG, int BN, int PLANES, bool SUMS>  // PLANES = 0: the loss; SUMS: gradients in one number, and dbias
 struct ScoreShape {
   static constexpr bool kExact = PLANES != 1 || SUMS;
-  static constexpr int kChunk = kExact ? 8 : 1 << 30;
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
   static constexpr int kOut = PLANES ? kWriters * 2 * 4096 : 0;
@@ -250,7 +250,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       uint32_t it = 0, n = 0;
       for (uint32_t w = unit; ok && w < tiles; w += units) {
         for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
-          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = k % S::kChunk;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = S::kExact ? k & (a.chunk - 1) : k;
           if (place == 0) {
             if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
             mma_fence_after();
@@ -262,7 +262,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           for (int j = 0; j < kDepth / kStepK; ++j)
             mma<CG, false>(tmem + acc * BN, da + j * ((kStepK * 2) >> 4), db + j * ((kStepK * 2) >> 4), id, place != 0 || j != 0);
           mma_commit<CG>(empty + 8 * s);
-          if (place == S::kChunk - 1 || k + 1 == a.ksteps) {
+          if ((S::kExact && place == a.chunk - 1) || k + 1 == a.ksteps) {
             mma_commit<CG>(done + 8 * acc);
             ++n;
           }
@@ -309,7 +309,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       if constexpr (S::kExact) {
 #pragma unroll
         for (int i = 0; i < BN / 2; ++i) z[i] = 0.f;
-        for (uint32_t k = 0; k < a.ksteps; k += S::kChunk, ++n) {
+        for (uint32_t k = 0; k < a.ksteps; k += a.chunk, ++n) {
           ok = bar_wait(done + 8 * (n & 1), (n >> 1) & 1);
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           mma_fence_after();
@@ -552,6 +552,7 @@ cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGr
   // rows.)
   const uint32_t rows = CG == 1 && a.r.rows < 128 ? a.r.rows : 128;
   s.wide = sh.wide;
+  s.chunk = sh.chunk;
   s.tiles_n = (s.v1 - s.v0 + s.wide - 1) / s.wide;
   s.stage_bytes = (rows + s.wide / CG) * kDepth * 2;
   CUtensorMap mx, mw, mp = {};
@@ -582,7 +583,7 @@ cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream) {
 
 VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sms, double* cost) {
   const uint32_t k = (d + kDepth - 1) / kDepth, step = planes ? 64 : 16;
-  VocabShape best = {1, 128};
+  VocabShape best = {1, 128, 0};
   double least = 1e300;
   // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle, and 400 cycles at least (the
   // ring holds six, and what is in flight must cover the memory's latency: 1 token, 1600 x 50257, 38 us in tiles of 64, 30 in tiles of
@@ -598,9 +599,12 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
       const double c = (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
       if (c < 0.99 * least) {
         least = c;
-        best = {cg, wide};
+        best = {cg, wide, 0};
       }
     }
+  // (up to 128 tokens wait for memory, and have the time to add sums up twice as often: 1 token, 1600 x 50257, 0.1 us; 8192 tokens would
+  // take 10 % longer)
+  best.chunk = rows > 128 ? 8 : 4;
   if (cost) *cost = least;
   return best;
 }

@@ -160,9 +160,9 @@ constexpr int kWriters = 8;            // warps that take results out of tensor 
 // next part is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
 // alone p is off by no more than 2e-6 |z|, which matters to no gradient but that of a target with p above 0.99, and they take 1 to 2 %
 // less time without (8192 tokens, 50257 entries, 1600 columns: loss and gradients 4113 instead of 4168 us).
-template <int CG, int BN, int PLANES, bool SUMS>  // PLANES = 0: the loss; SUMS: gradients in one number, and dbias
+// Sums of one part (512 columns at most) are taken from the unit as they are: the same numbers, without the registers that add parts up.
+template <int CG, int BN, int PLANES>
 struct ScoreShape {
-  static constexpr bool kExact = PLANES != 1 || SUMS;
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
   static constexpr int kOut = PLANES ? kWriters * 2 * 4096 : 0;
@@ -185,11 +185,12 @@ __device__ __forceinline__ float lane_sums(float (&v)[32], int lane) {
   return v[0];
 }
 
-template <int CG, int BN, int PLANES, bool SUMS>
-__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES, SUMS>::kThreads), 1)
+// PLANES = 0: the loss, else gradients; ADD: sums leave the unit in parts; SUMS: dbias, beside gradients in one number
+template <int CG, int BN, int PLANES, bool ADD, bool SUMS>
+__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES>::kThreads), 1)
 score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_p,
              const ScoreArgs a) {
-  using S = ScoreShape<CG, BN, PLANES, SUMS>;
+  using S = ScoreShape<CG, BN, PLANES>;
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
@@ -250,7 +251,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       uint32_t it = 0, n = 0;
       for (uint32_t w = unit; ok && w < tiles; w += units) {
         for (uint32_t k = 0; k < a.ksteps; ++k, ++it) {
-          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = S::kExact ? k & (a.chunk - 1) : k;
+          const uint32_t s = it % kStages, ph = (it / kStages) & 1, acc = n & 1, place = ADD ? k & (a.chunk - 1) : k;
           if (place == 0) {
             if (!(ok = bar_wait<CG == 2>(freed + 8 * acc, ((n >> 1) & 1) ^ 1))) break;
             mma_fence_after();
@@ -262,7 +263,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           for (int j = 0; j < kDepth / kStepK; ++j)
             mma<CG, false>(tmem + acc * BN, da + j * ((kStepK * 2) >> 4), db + j * ((kStepK * 2) >> 4), id, place != 0 || j != 0);
           mma_commit<CG>(empty + 8 * s);
-          if ((S::kExact && place == a.chunk - 1) || k + 1 == a.ksteps) {
+          if ((ADD && place == a.chunk - 1) || k + 1 == a.ksteps) {
             mma_commit<CG>(done + 8 * acc);
             ++n;
           }
@@ -275,38 +276,58 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     uint32_t n = 0, puts = 0;
     float m = -INFINITY, s = 0.f;      // the loss: maximum and sum of exp of this row over a part
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16) + half * (BN / 2);
+    // What a tile's row and columns come with.  With short sums the tiles follow one another so quickly that it would be waited for: it is
+    // loaded a tile ahead, and which token the row is another tile ahead of that.  (8192 tokens, 64 columns, 30000 entries: loss 179 -> 164
+    // us.  Where sums are added up there are no registers for that: 768 columns, 50257 entries, bias, 552 -> 610.)
+    struct Row {
+      int64_t to;
+      float dloss, lse;
+      float bias[BN / 64];      // of column 32 i + lane
+    };
+    constexpr uint32_t kNone = 0xffffffffu;
+    auto token_of = [&](uint32_t w) {
+      if (w >= tiles) return kNone;
+      const uint32_t row = w % tiles_m * 128 * CG + 128 * rank + quad * 32 + lane;
+      return row >= count ? kNone : a.token ? a.token[row] : row;
+    };
+    auto fetch = [&](uint32_t w, uint32_t t) {
+      Row r;
+      r.to = t == kNone ? a.ignore : a.target[t];
+      r.dloss = PLANES == 0 || t == kNone ? 0.f : a.dloss[t];
+      r.lse = PLANES == 0 || t == kNone ? 0.f : a.lse[t];
+      if (a.bias && w < tiles) {
+        const uint32_t tile = w / tiles_m, col = a.v0 + tile * a.wide + half * (BN / 2) + lane, end = min(a.v1, a.v0 + (tile + 1) * a.wide);
+#pragma unroll
+        for (int i = 0; i < BN / 64; ++i) r.bias[i] = col + 32 * i < end ? __ldg(a.bias + col + 32 * i) : 0.f;
+      }
+      return r;
+    };
+    Row next = {};
+    uint32_t token = 0;
+    if constexpr (!ADD) {
+      next = fetch(unit, token_of(unit));
+      token = token_of(unit + units);
+    }
     for (uint32_t w = unit; ok && w < tiles; w += units) {
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
       const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + half * (BN / 2);
       const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
       // this row's target, if it lies in these columns; gradients: what the row is multiplied with, and its normaliser
-      float g = 0.f, lse = 0.f;
-      int32_t hit = -1;
-      bool real = false;
-      if (row < count) {
-        const uint32_t t = a.token ? a.token[row] : row;
-        const int64_t to = a.target[t];
-        real = to != a.ignore;
-        if (real) {
-          if constexpr (PLANES > 0) {
-            g = __fdiv_rn(a.dloss[t], scale);
-            lse = a.lse[t];
-          }
-          if (to >= col0 && to < min(end, col0 + BN / 2)) hit = (int32_t)(to - col0);
-        }
+      const Row now = ADD ? fetch(w, token_of(w)) : next;
+      if constexpr (!ADD) {
+        next = fetch(w + units, token);
+        token = token_of(w + 2 * units);
       }
-      float bias[BN / 64];      // of column 32 i + lane
-      if (a.bias) {
-#pragma unroll
-        for (int i = 0; i < BN / 64; ++i) bias[i] = col0 + 32 * i + lane < end ? __ldg(a.bias + col0 + 32 * i + lane) : 0.f;
-      }
-      float z[S::kExact ? BN / 2 : 32];      // logits: of all columns of the tile, or of a block of them
+      const bool real = now.to != a.ignore;
+      const int32_t hit = real && now.to >= col0 && now.to < min(end, col0 + BN / 2) ? (int32_t)(now.to - col0) : -1;
+      const float g = real ? __fdiv_rn(now.dloss, scale) : 0.f, lse = now.lse;
+      float z[ADD ? BN / 2 : 32];      // logits: of all columns of the tile, or of a block of them
       auto release = [&](uint32_t acc) {
         mma_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive_leader<CG>(freed + 8 * acc, freed0 + 8 * acc, leader);
       };
-      if constexpr (S::kExact) {
+      if constexpr (ADD) {
 #pragma unroll
         for (int i = 0; i < BN / 2; ++i) z[i] = 0.f;
         for (uint32_t k = 0; k < a.ksteps; k += a.chunk, ++n) {
@@ -335,7 +356,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
       // the 32 logits from column c (a constant after unrolling) on, with their bias
       auto logits = [&](int c, float(&v)[32]) {
-        if constexpr (S::kExact) {
+        if constexpr (ADD) {
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = z[c + i];
         } else {
@@ -343,7 +364,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
         if (a.bias) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, bias[c / 32], i));
+          for (int i = 0; i < 32; ++i) v[i] = __fadd_rn(v[i], __shfl_sync(0xffffffffu, now.bias[c / 32], i));
         }
       };
       if constexpr (PLANES == 0) {
@@ -457,7 +478,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
           }
         }
       }
-      if constexpr (!S::kExact) {
+      if constexpr (!ADD) {
         release(n & 1);
         ++n;
       }
@@ -539,9 +560,9 @@ uint32_t units_of(VocabShape s, uint32_t rows, uint32_t tiles_n, int sms) {
 }
 bool merged(VocabShape s, uint32_t most) { return most <= 128u * s.cg; }
 
-template <int CG, int BN, int PLANES, bool SUMS>
+template <int CG, int BN, int PLANES, bool ADD, bool SUMS>
 cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
-  using S = ScoreShape<CG, BN, PLANES, SUMS>;
+  using S = ScoreShape<CG, BN, PLANES>;
   s.count = a.r.count;
   s.rows = a.r.rows;
   s.most = a.r.most;
@@ -559,17 +580,23 @@ cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGr
   cudaError_t e = make_tensor_map(&mx, a.r.x, 2, a.r.rows, a.d, a.r.ldx, rows, kDepth, true);
   if (e == cudaSuccess) e = make_tensor_map(&mw, a.w, 2, a.v, a.d, a.ldw, s.wide / CG, kDepth, true);
   if (e == cudaSuccess && o) e = make_tensor_map(&mp, o->p, 2, (uint64_t)a.r.most * o->panels * o->planes, 64, 64, 32, 64, true);
-  auto* kernel = score_kernel<CG, BN, PLANES, SUMS>;
+  auto* kernel = score_kernel<CG, BN, PLANES, ADD, SUMS>;
   static std::atomic<uint64_t> seen;
   if (e == cudaSuccess) e = allow_smem(kernel, S::kSmem, a.device, seen);
   if (e != cudaSuccess) return e;
   return launch_with(kernel, units_of(sh, a.r.rows, s.tiles_n, sms) * CG, S::kThreads, S::kSmem, CG, true, stream, mx, mw, mp, s);
 }
 
-template <int PLANES, bool SUMS = false>
+template <int PLANES, bool ADD, bool SUMS>
 cudaError_t by_shape(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
   constexpr int kPair = PLANES == 3 ? 128 : 256;
-  return sh.cg == 2 ? launch<2, kPair, PLANES, SUMS>(a, sh, s, o, sms, stream) : launch<1, 128, PLANES, SUMS>(a, sh, s, o, sms, stream);
+  return sh.cg == 2 ? launch<2, kPair, PLANES, ADD, SUMS>(a, sh, s, o, sms, stream)
+                    : launch<1, 128, PLANES, ADD, SUMS>(a, sh, s, o, sms, stream);
+}
+template <int PLANES, bool SUMS = false>
+cudaError_t by_length(const VocabArgs& a, VocabShape sh, const ScoreArgs& s, const VocabGradOut* o, int sms, cudaStream_t stream) {
+  return a.d > sh.chunk * kDepth ? by_shape<PLANES, true, SUMS>(a, sh, s, o, sms, stream)
+                                 : by_shape<PLANES, false, SUMS>(a, sh, s, o, sms, stream);
 }
 
 }  // namespace
@@ -626,7 +653,7 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most,
   s.chosen = chosen;
   s.merge = merged(sh, most);
   s.err = err;
-  return by_shape<0>(a, sh, s, nullptr, sms, stream);
+  return by_length<0>(a, sh, s, nullptr, sms, stream);
 }
 
 cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse,
@@ -653,9 +680,9 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0,
   s.ldb = o.ldb;
   s.panels = o.panels;
   s.err = err;
-  return o.planes == 3 ? by_shape<3>(a, sh, s, &o, sms, stream)
-         : o.dbias     ? by_shape<1, true>(a, sh, s, &o, sms, stream)
-                       : by_shape<1>(a, sh, s, &o, sms, stream);
+  return o.planes == 3 ? by_length<3>(a, sh, s, &o, sms, stream)
+         : o.dbias     ? by_length<1, true>(a, sh, s, &o, sms, stream)
+                       : by_shape<1, false, false>(a, sh, s, &o, sms, stream);
 }
 
 }  // namespace stq

@@ -140,7 +140,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   a.ignore = ignore_index;
   a.device = h->device;
   // (the blocks of tokens share one workspace, laid out for the largest)
-  const size_t fit = kPartBytes / (16 * (up(v, 128) / 128)) / 256 * 256;
+  const size_t fit = kPartBytes / (32 * (up(v, 128) / 128)) / 256 * 256;
   const uint32_t at_once = fit < 256 ? 256 : fit < kTokensAtOnce ? (uint32_t)fit : kTokensAtOnce;
   a.t = (uint32_t)(t < at_once ? t : at_once);
   a.target = target;

@@ -152,7 +152,11 @@ struct ScoreArgs {
   int* err;
 };
 
-constexpr int kWriters = 8;            // warps that take results out of tensor memory: two to each quarter of its lanes
+// Warps that take results out of tensor memory, to each quarter of its lanes: with short sums the loss waits for them (for the latency
+// of a maximum, of exp and of a sum that follow one another), and they need few registers.  (8192 tokens, 30000 entries, 64 and 256
+// columns: 165 -> 143 and 143 -> 122 us; 4384 x 344 x 86592: 257 -> 272, there are twice as many parts to join.)
+constexpr int kShort = 4, kLong = 2;
+constexpr int shares_of(int planes, bool add) { return planes == 0 && !add ? kShort : kLong; }
 
 // The matrix unit cuts its fp32 sums off instead of rounding them, always towards zero: over a sum of 4096 a logit lost 2e-6 of itself,
 // and the loss 4e-6 where the vocabulary is small.  For the loss and for what becomes an fp32 result (gradients in three parts, dbias) the
@@ -161,8 +165,9 @@ constexpr int kWriters = 8;            // warps that take results out of tensor 
 // alone p is off by no more than 2e-6 |z|, which matters to no gradient but that of a target with p above 0.99, and they take 1 to 2 %
 // less time without (8192 tokens, 50257 entries, 1600 columns: loss and gradients 4113 instead of 4168 us).
 // Sums of one part (512 columns at most) are taken from the unit as they are: the same numbers, without the registers that add parts up.
-template <int CG, int BN, int PLANES>
+template <int CG, int BN, int PLANES, bool ADD>
 struct ScoreShape {
+  static constexpr int kShares = shares_of(PLANES, ADD), kWriters = 4 * kShares, kCols = BN / kShares;
   static constexpr int kThreads = 32 * (2 + kWriters);
   static constexpr int kA = 128 * kDepth * 2, kB = BN / CG * kDepth * 2, kStage = kA + kB;
   static constexpr int kOut = PLANES ? kWriters * 2 * 4096 : 0;
@@ -187,10 +192,10 @@ __device__ __forceinline__ float lane_sums(float (&v)[32], int lane) {
 
 // PLANES = 0: the loss, else gradients; ADD: sums leave the unit in parts; SUMS: dbias, beside gradients in one number
 template <int CG, int BN, int PLANES, bool ADD, bool SUMS>
-__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES>::kThreads), 1)
+__global__ void __launch_bounds__((ScoreShape<CG, BN, PLANES, ADD>::kThreads), 1)
 score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_p,
              const ScoreArgs a) {
-  using S = ScoreShape<CG, BN, PLANES>;
+  using S = ScoreShape<CG, BN, PLANES, ADD>;
   constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw[];
   __shared__ uint64_t bars[2 * kStages + 4];
@@ -210,7 +215,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(done + 8 * i, 1);
-      bar_init(freed + 8 * i, kWriters * CG);
+      bar_init(freed + 8 * i, S::kWriters * CG);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -271,18 +276,18 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       }
     }
   } else {
-    const int quad = warp & 3, half = (warp - 2) / 4;
+    const int quad = warp & 3, share = (warp - 2) / 4;
     const uint32_t freed0 = CG == 2 ? peer_addr(freed, 0) : freed;
     uint32_t n = 0, puts = 0;
     float m = -INFINITY, s = 0.f;      // the loss: maximum and sum of exp of this row over a part
-    const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16) + half * (BN / 2);
+    const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16) + share * S::kCols;
     // What a tile's row and columns come with.  With short sums the tiles follow one another so quickly that it would be waited for: it is
     // loaded a tile ahead, and which token the row is another tile ahead of that.  (8192 tokens, 64 columns, 30000 entries: loss 179 -> 164
     // us.  Where sums are added up there are no registers for that: 768 columns, 50257 entries, bias, 552 -> 610.)
     struct Row {
       int64_t to;
       float dloss, lse;
-      float bias[BN / 64];      // of column 32 i + lane
+      float bias[S::kCols / 32];      // of column 32 i + lane
     };
     constexpr uint32_t kNone = 0xffffffffu;
     auto token_of = [&](uint32_t w) {
@@ -296,9 +301,9 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       r.dloss = PLANES == 0 || t == kNone ? 0.f : a.dloss[t];
       r.lse = PLANES == 0 || t == kNone ? 0.f : a.lse[t];
       if (a.bias && w < tiles) {
-        const uint32_t tile = w / tiles_m, col = a.v0 + tile * a.wide + half * (BN / 2) + lane, end = min(a.v1, a.v0 + (tile + 1) * a.wide);
+        const uint32_t tile = w / tiles_m, col = a.v0 + tile * a.wide + share * S::kCols + lane, end = min(a.v1, a.v0 + (tile + 1) * a.wide);
 #pragma unroll
-        for (int i = 0; i < BN / 64; ++i) r.bias[i] = col + 32 * i < end ? __ldg(a.bias + col + 32 * i) : 0.f;
+        for (int i = 0; i < S::kCols / 32; ++i) r.bias[i] = col + 32 * i < end ? __ldg(a.bias + col + 32 * i) : 0.f;
       }
       return r;
     };
@@ -310,7 +315,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     }
     for (uint32_t w = unit; ok && w < tiles; w += units) {
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
-      const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + half * (BN / 2);
+      const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + share * S::kCols;
       const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
       // this row's target, if it lies in these columns; gradients: what the row is multiplied with, and its normaliser
       const Row now = ADD ? fetch(w, token_of(w)) : next;
@@ -319,9 +324,9 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         token = token_of(w + 2 * units);
       }
       const bool real = now.to != a.ignore;
-      const int32_t hit = real && now.to >= col0 && now.to < min(end, col0 + BN / 2) ? (int32_t)(now.to - col0) : -1;
+      const int32_t hit = real && now.to >= col0 && now.to < min(end, col0 + S::kCols) ? (int32_t)(now.to - col0) : -1;
       const float g = real ? __fdiv_rn(now.dloss, scale) : 0.f, lse = now.lse;
-      float z[ADD ? BN / 2 : 32];      // logits: of all columns of the tile, or of a block of them
+      float z[ADD ? S::kCols : 32];      // logits: of all columns of the tile, or of a block of them
       auto release = [&](uint32_t acc) {
         mma_fence_before();
         __syncwarp();
@@ -329,13 +334,13 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       };
       if constexpr (ADD) {
 #pragma unroll
-        for (int i = 0; i < BN / 2; ++i) z[i] = 0.f;
+        for (int i = 0; i < S::kCols; ++i) z[i] = 0.f;
         for (uint32_t k = 0; k < a.ksteps; k += a.chunk, ++n) {
           ok = bar_wait(done + 8 * (n & 1), (n >> 1) & 1);
           if (!(ok = __all_sync(0xffffffffu, ok))) break;
           mma_fence_after();
 #pragma unroll
-          for (int c = 0; c < BN / 2; c += 32) {
+          for (int c = 0; c < S::kCols; c += 32) {
             if (col0 + c >= end) break;
             float v[32];
             load_block(mine + (n & 1) * BN + c, v);
@@ -369,7 +374,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
       };
       if constexpr (PLANES == 0) {
 #pragma unroll
-        for (int c = 0; c < BN / 2; c += 32) {
+        for (int c = 0; c < S::kCols; c += 32) {
           const uint32_t col = col0 + c;
           if (col >= end) break;
           float v[32];
@@ -407,7 +412,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
         const uint32_t part = a.merge ? unit : tile;
         if (!a.merge || w + units >= tiles) {
-          if (row < a.most) a.part[(size_t)(2 * part + half) * a.most + row] = make_float2(m, s);
+          if (row < a.most) a.part[(size_t)(S::kShares * part + share) * a.most + row] = make_float2(m, s);
           m = -INFINITY;
           s = 0.f;
         }
@@ -415,7 +420,7 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         const uint32_t out = outs + (warp - 2) * 2 * 4096;
         const float2 less = make_float2(-lse, -lse), scale2 = make_float2(kLog2e, kLog2e), g2 = make_float2(g, g);
 #pragma unroll
-        for (int c = 0; c < BN / 2; c += 64) {
+        for (int c = 0; c < S::kCols; c += 64) {
           const uint32_t col = col0 + c;
           if (col >= end) break;
           float v[64];
@@ -562,7 +567,7 @@ bool merged(VocabShape s, uint32_t most) { return most <= 128u * s.cg; }
 
 template <int CG, int BN, int PLANES, bool ADD, bool SUMS>
 cudaError_t launch(const VocabArgs& a, VocabShape sh, ScoreArgs s, const VocabGradOut* o, int sms, cudaStream_t stream) {
-  using S = ScoreShape<CG, BN, PLANES>;
+  using S = ScoreShape<CG, BN, PLANES, ADD>;
   s.count = a.r.count;
   s.rows = a.r.rows;
   s.most = a.r.most;
@@ -638,7 +643,7 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
 
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms) {
   const uint32_t tiles = (a.v + s.wide - 1) / s.wide;
-  return 2 * (merged(s, most) ? units_of(s, most, tiles, sms) : tiles);
+  return shares_of(0, a.d > s.chunk * kDepth) * (merged(s, most) ? units_of(s, most, tiles, sms) : tiles);
 }
 
 cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most, float2* part, float* chosen, int sms, int* err,

@@ -318,6 +318,10 @@ int check_list(const stq_grad* g, int n, bool write, bool* in_place) try {
   *in_place = true;
   std::vector<std::pair<uintptr_t, uintptr_t>> written;
   std::vector<std::pair<uintptr_t, uintptr_t>> read;
+  if (write) {
+    written.reserve(n);
+    read.reserve(n);
+  }
   for (int i = 0; i < n; ++i) {
     const int dt = g[i].dtype;
     if (dt != STQ_GRAD_F32 && dt != STQ_GRAD_BF16 && dt != STQ_GRAD_F16) return STQ_E_ARG;
@@ -335,10 +339,11 @@ int check_list(const stq_grad* g, int n, bool write, bool* in_place) try {
     }
   }
   // a result may lie where its own gradient does, and nowhere else that is read or written
-  std::sort(written.begin(), written.end());
+  if (!std::is_sorted(written.begin(), written.end())) std::sort(written.begin(), written.end());
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].first < written[i - 1].second) return STQ_E_ALIAS;
   for (const auto& r : read) {
+    if (r.second <= written.front().first || r.first >= written.back().second) continue;
     const auto w = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, (uintptr_t)0));
     if (w != written.begin() && (w - 1)->second > r.first) return STQ_E_ALIAS;
   }
@@ -392,7 +397,10 @@ size_t sums_of(const stq_grad* g, int n, int sms) {
 template <class F>
 cudaError_t by_length(int n, F&& f) {
   if (n <= 64) return f(std::integral_constant<int, 64>());
+  if (n <= 160) return f(std::integral_constant<int, 160>());
   if (n <= 256) return f(std::integral_constant<int, 256>());
+  if (n <= 384) return f(std::integral_constant<int, 384>());
+  if (n <= 512) return f(std::integral_constant<int, 512>());
   if (n <= 640) return f(std::integral_constant<int, 640>());
   return f(std::integral_constant<int, kMost>());
 }

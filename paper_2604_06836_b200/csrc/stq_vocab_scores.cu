@@ -316,7 +316,8 @@ score_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     for (uint32_t w = unit; ok && w < tiles; w += units) {
       const uint32_t row0 = w % tiles_m * 128 * CG + 128 * rank + quad * 32, row = row0 + lane;
       const uint32_t tile = w / tiles_m, col0 = a.v0 + tile * a.wide + share * S::kCols;
-      const uint32_t end = min(a.v1, a.v0 + (tile + 1) * a.wide);
+      // (nothing is read of rows behind the last one, or behind the stage of dw's sums that has it)
+      const uint32_t end = row0 < (PLANES > 0 ? (count + kDepth - 1) / kDepth * kDepth : count) ? min(a.v1, a.v0 + (tile + 1) * a.wide) : 0;
       // this row's target, if it lies in these columns; gradients: what the row is multiplied with, and its normaliser
       const Row now = ADD ? fetch(w, token_of(w)) : next;
       if constexpr (!ADD) {

@@ -350,7 +350,7 @@ int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, ui
  * The logits z are not kept: they are formed tile by tile, again for the gradients.  Tokens whose target is
  * ignore_index have loss 0, lse 0 and no gradient, and take no part in the products.  Any other target outside
  * 0..v-1 gives loss and lse NaN, and NaN gradients.  A bias of -inf takes an entry out of the vocabulary.
- * All sums are held in fp32 and added in a fixed order; those of the loss and of an fp32 dw leave the matrix units,
+ * All sums are held in fp32 and added in a fixed order; those of the logits and of an fp32 dw leave the matrix units,
  * which cut them off, every 512 (up to 128 tokens: 256) and 128 terms.  Workspace, streams and graphs: as for the 8-bit operators above (for
  * the gradients up to 512 MB of gradients of logits, a copy of x in fp32 and one in bf16, and up to 116 MB of partial
  * results; a copy of w where its rows are not aligned to 16 bytes).  t is at most STQ_VOCAB_MAX_TOKENS, d at most
@@ -365,8 +365,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
 /* Gradients for dloss[t] (fp32) and lse as stq_vocab_loss wrote it; each of dx (bf16 [t][d]), dw ([v][d], bf16 or
  * fp32) and dbias (fp32[v]) may be NULL.  The gradients of the logits, relative to the largest |dloss| of a token that counts, enter
  * the matrix units as bf16, 2^-8 relative a term (in the 2-norm dx and dw are off by 0.002, against 0.0017 of their own
- * rounding; a sum of 4096 columns in the matrix units takes up to 2e-6 off a logit, which shows in a target's p - 1 where p > 0.99);
- * for an fp32 dw as three bf16 numbers that are together exact, at three times the cost of that product. */
+ * rounding); for an fp32 dw as three bf16 numbers that are together exact, at three times the cost of that product. */
 int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, uint64_t ldx, const void* w, uint64_t ldw,
                             const float* bias, const int64_t* target, int64_t ignore_index, const float* lse, uint64_t t, uint32_t v,
                             uint32_t d, void* dx, uint64_t lddx, void* dw, uint64_t lddw, int dw_dtype, float* dbias, void* stream);

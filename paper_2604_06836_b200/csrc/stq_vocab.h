@@ -56,8 +56,7 @@ cudaError_t launch_vocab_gather(const GatherArgs& a, cudaStream_t stream);
 // Tiles of the products: `cg` CTAs share 128 * cg rows and `wide` entries of the vocabulary.  The loss (planes = 0) takes any width that
 // the matrix units do, the gradients whole panels (below), those in three parts narrow ones.  cost, if wanted: the time in clock cycles.
 // chunk: how many stages of 64 columns are added up in the matrix unit.  It goes by the number of tokens alone: loss and gradients then round
-// a logit in the same way, and a target's exp(z - lse) - 1 is as exact as lse (but for gradients in one
-// bf16 number without dbias, which take whole sums from the unit).
+// a logit in the same way, and a target's exp(z - lse) - 1 is as exact as lse.
 struct VocabShape {
   int cg;
   uint32_t wide;

@@ -159,11 +159,12 @@ constexpr int kShort = 4, kLong = 2;
 constexpr int shares_of(int planes, bool add) { return planes == 0 && !add ? kShort : kLong; }
 
 // The matrix unit cuts its fp32 sums off instead of rounding them, always towards zero: over a sum of 4096 a logit lost 2e-6 of itself,
-// and the loss 4e-6 where the vocabulary is small.  For the loss and for what becomes an fp32 result (gradients in three parts, dbias) the
-// sum therefore leaves the unit every `chunk` stages (VocabShape) and is added, rounded, in registers.  (The accumulators take turns, so the
-// next part is multiplied meanwhile; 128 sums a thread leave a few registers short, 92 to 148 bytes spilled.)  For gradients in one bf16 number
-// alone p is off by no more than 2e-6 |z|, which matters to no gradient but that of a target with p above 0.99, and they take 1 to 2 %
-// less time without (8192 tokens, 50257 entries, 1600 columns: loss and gradients 4113 instead of 4168 us).
+// and the loss 4e-6 where the vocabulary is small.  The sum therefore leaves the unit every `chunk` stages (VocabShape) and is added, rounded,
+// in registers.  (The accumulators take turns, so the next part is multiplied meanwhile; 128 sums a thread leave a few registers short: 112
+// bytes spilled in the loss, 152 in the gradients, 168 with dbias.)  So it is in the gradients, in one bf16 number too: what all logits of a
+// row are off by alike is also in lse, and drops out of z - lse only where both passes cut off alike.  (With whole sums dx of tokens with p
+// near 1 was off by 22 times what roundings explain.  They take 1 to 2 % less time: 8192 tokens, 50257 entries, 1600 columns, loss and
+// gradients 4113 instead of 4168 us.)
 // Sums of one part (512 columns at most) are taken from the unit as they are: the same numbers, without the registers that add parts up.
 template <int CG, int BN, int PLANES, bool ADD>
 struct ScoreShape {
@@ -688,7 +689,7 @@ cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0,
   s.err = err;
   return o.planes == 3 ? by_length<3>(a, sh, s, &o, sms, stream)
          : o.dbias     ? by_length<1, true>(a, sh, s, &o, sms, stream)
-                       : by_shape<1, false, false>(a, sh, s, &o, sms, stream);
+                       : by_length<1>(a, sh, s, &o, sms, stream);
 }
 
 }  // namespace stq

@@ -500,3 +500,54 @@ def test_two_handles_at_once():
     for i, g in got:
         assert all(torch.equal(x, y) for p, q in zip(g, want[i]) for x, y in zip(p, q) if x is not None)
     a.close(), b.close()
+
+
+@pytest.mark.parametrize("t,d", [(40, 300), (40, 1025), (300, 1025), (300, 4096)])
+def test_a_gradient_does_not_go_by_which_others_are_asked_for(handle, t, d):
+    """Sums of more than one part too; the vocabulary is one piece."""
+    for dtype in (BF, F32):
+        for bias in (True, False):
+            x, w, target, b, dloss = inputs(t, d, 700, t + d, bias, 0.2)
+            out, want = run(handle, x, w, target, b, dloss, dtype, want_dbias=True)
+            for dx, dw, db in ((1, 1, 0), (1, 0, 1), (1, 0, 0), (0, 1, 0), (0, 0, 1)):
+                g = vocab.loss_backward(handle, dloss, x, w, target, out.lse, bias=b, dtype=dtype, want_dx=bool(dx), want_dw=bool(dw),
+                                        want_dbias=bool(db))
+                for got, full, asked in zip(g, want, (dx, dw, db)):
+                    assert (got is not None) == bool(asked) and (got is None or torch.equal(got, full)), (dtype, bias, dx, dw, db)
+
+
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("d", [929, 4096])
+@pytest.mark.parametrize("t", [3, 40, 700])
+def test_gradients_of_confident_tokens(handle, t, d, bias):
+    """Where the target has nearly all of the sum, p - 1 is much smaller than p, and what a logit is off by must not show in it: the loss
+    and its gradients have to round a logit in the same way.  If they do, p_j is off by p_j times the others' shares times what their logits
+    and its own are off by (what all are off by alike drops out), and by the roundings of lse and of z - lse, of exp and of the sum (24 U
+    for the latter two)."""
+    v, g = 32, torch.Generator(device="cuda").manual_seed(t + d)
+    w = (torch.randn(v, d, device="cuda", generator=g) * (2 / d ** 0.5)).to(BF)
+    target = torch.randint(0, v, (t,), device="cuda", generator=g)
+    sure = 1 + 3 * torch.rand(t, 1, device="cuda", generator=g)
+    x = (0.3 * torch.randn(t, d, device="cuda", generator=g) + sure * w[target].float()).to(BF)
+    b = 0.5 * torch.randn(v, device="cuda", generator=g) if bias else None
+    dloss = torch.full((t,), 1 / t, device="cuda")
+    out = vocab.loss(handle, x, w, target, bias=b)
+    x64, w64, b64 = x.double(), w.double(), 0.0 if b is None else b.double()
+    z, a = x64 @ w64.T + b64, x64.abs() @ w64.abs().T + (0.0 if b is None else b64.abs())
+    dz = 2 * U * (d / 16 + 2) * a + U * z.abs()
+    lse, p = torch.logsumexp(z, 1, keepdim=True), torch.softmax(z, 1)
+    hit = torch.nn.functional.one_hot(target, v).double()
+    others = torch.softmax(z, 1).scatter(1, target[:, None], 0.0)
+    grad = (p * (1 - hit) - hit * others.sum(1, keepdim=True)) / t
+    apart = dz * (1 - p).clamp(min=0) + ((p * dz).sum(1, keepdim=True) - p * dz)
+    sure_one = hit * (others * (dz + (hit * dz).sum(1, keepdim=True))).sum(1, keepdim=True)      # (1 - p without its cancellation)
+    off = p / t * (torch.where(hit > 0, sure_one, apart) + U * (2 * lse.abs() + 4 * (z - lse).abs() + 24))
+    rounded = UB * grad.abs() + off * (1 + UB)
+    for dbias in (True, False):
+        got = vocab.loss_backward(handle, dloss, x, w, target, out.lse, bias=b, want_dbias=dbias)
+        want, tol = grad.T @ x64, rounded.T @ x64.abs() + 2 * U * (t / 16 + 34) * (grad.abs().T @ x64.abs())
+        far = ((got.dw.double() - want).abs() / (tol * (1 + UB) + UB * want.abs() + 1e-44)).max()
+        assert far <= 1, ("dw", dbias, float(far))
+        want, tol = grad @ w64, rounded @ w64.abs() + 2 * U * (v / 16 + 64) * (grad.abs() @ w64.abs())
+        far = ((got.dx.double() - want).abs() / (tol * (1 + UB) + UB * want.abs() + 1e-44)).max()
+        assert far <= 1, ("dx", dbias, float(far))

@@ -16,6 +16,7 @@ gradients.  Every tensor starts at ``init_bits`` (16 in the paper).
 """
 from __future__ import annotations
 
+import math
 from typing import Iterable
 
 import numpy as np
@@ -44,7 +45,8 @@ class STQAdamW(torch.optim.Optimizer):
     max_norm: clips the gradients to this 2-norm over all of them (after unscaling).  One more pass reads the
     gradients; the step applies the factor as it reads them, so they are not written.  Statistics of a decision
     step are those of the clipped gradients, in both orders.  ``self.last_norm`` is the norm before clipping, on
-    the device.  With ``found_inf`` set, a norm that is not finite raises it too, and the step is left out.
+    the device.  With ``found_inf`` set, a step whose norm is not finite is left out too (the flag is the caller's: the
+    optimizer reads it and leaves it as it is).
     """
 
     def __init__(self, params: Iterable, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -139,10 +141,18 @@ class STQAdamW(torch.optim.Optimizer):
                 raise ValueError("every parameter needs a gradient (frozen parameters do not belong here)")
             if not p.grad.is_contiguous():
                 p.grad = p.grad.contiguous()
-        r = clip.grad_norm(self.handle, [p.grad for p in self._params], max_norm=self.max_norm, inv_scale=self.grad_scaler_inv,
-                           found_inf=self.found_inf)
+        r = clip.grad_norm(self.handle, [p.grad for p in self._params], max_norm=self.max_norm, inv_scale=self.grad_scaler_inv)
         self.last_norm = r.norm
         return r.factor
+
+    def _left_out(self) -> bool:
+        """Whether the gradients are not finite, as the caller found or as the norm says (one synchronising copy for both)."""
+        if self.found_inf is None:
+            return False
+        if self.max_norm is None:
+            return float(self.found_inf.item()) != 0.0
+        found, norm = torch.stack((self.found_inf.reshape(()), self.last_norm)).tolist()
+        return found != 0.0 or not math.isfinite(norm)
 
     # ---- the step -----------------------------------------------------------------------------------
     @torch.no_grad()
@@ -152,7 +162,7 @@ class STQAdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         scale = self._clip_factor()
-        if self.found_inf is not None and float(self.found_inf.item()) != 0.0:
+        if self._left_out():
             self.skipped_steps += 1       # no step is launched, t does not advance, carried statistics are kept
             return loss
         self.t += 1

@@ -301,3 +301,26 @@ def test_two_handles_at_once():
     torch.cuda.synchronize()
     assert all(torch.equal(n, want[i]) for i, n in got)
     a.close(), b.close()
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("scaled", [False, True])
+def test_a_step_that_is_left_out_does_not_hold_up_the_next(bad, scaled):
+    """found_inf belongs to the caller: the optimizer reads it and leaves it as it is, also where it is set once for all steps."""
+    ps = parameters()
+    opt = STQAdamW(ps, lr=1e-2, policy="fixed", init_bits=8, max_norm=1.0)
+    opt.found_inf = torch.zeros(1, device="cuda")
+    opt.grad_scaler_inv = torch.full((1,), 1 / 128, device="cuda") if scaled else None
+    taken = 0
+    for t, value in enumerate((1.0, bad, 1.0, 1.0, bad, bad, 1.0)):
+        for p in ps:
+            p.grad = torch.ones_like(p)
+        ps[1].grad[3] = value
+        before = ps[0].detach().clone()
+        opt.step()
+        taken += value == 1.0
+        assert (opt.t, opt.skipped_steps) == (taken, t + 1 - taken)
+        assert torch.equal(ps[0], before) == (value != 1.0) and float(opt.found_inf) == 0.0
+    opt.found_inf.fill_(1.0)      # what the caller found
+    opt.step()
+    assert opt.t == taken and float(opt.found_inf) == 1.0

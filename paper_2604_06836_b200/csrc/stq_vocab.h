@@ -66,6 +66,8 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
 
 // Maxima and sums of exp of each row over parts of the vocabulary: part[i][row] for i < vocab_parts(), pitch `most`.
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms);
+// How many parts a tile makes of each of its rows, where there are more than 128 tokens.
+uint32_t vocab_parts_of_tile(uint32_t d);
 // (most: the one that the parts were counted for.)  chosen[row]: the logit of the row's target, if that is in the vocabulary.
 cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, float2* part, float* chosen, int sms, int* err,
                                cudaStream_t stream);

@@ -139,8 +139,8 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
   a.v = v; a.d = d;
   a.ignore = ignore_index;
   a.device = h->device;
-  // (the blocks of tokens share one workspace, laid out for the largest)
-  const size_t fit = kPartBytes / (32 * (up(v, 128) / 128)) / 256 * 256;
+  // (the blocks of tokens share one workspace, laid out for the largest; tiles of so many entries are 128 wide at least)
+  const size_t fit = kPartBytes / (8 * vocab_parts_of_tile(d) * (up(v, 128) / 128)) / 256 * 256;
   const uint32_t at_once = fit < 256 ? 256 : fit < kTokensAtOnce ? (uint32_t)fit : kTokensAtOnce;
   a.t = (uint32_t)(t < at_once ? t : at_once);
   a.target = target;

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kDepth = 64;             // length of the sum per stage: 128 bytes of bf16
 constexpr int kStepK = 16;             // and per product instruction
+constexpr uint32_t kChunk = 8;         // stages after which a logit's sum leaves the matrix unit, with more than 128 tokens
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -638,10 +639,12 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
     }
   // (up to 128 tokens wait for memory, and have the time to add sums up twice as often: 1 token, 1600 x 50257, 0.1 us; 8192 tokens would
   // take 10 % longer)
-  best.chunk = rows > 128 ? 8 : 4;
+  best.chunk = rows > 128 ? kChunk : kChunk / 2;
   if (cost) *cost = least;
   return best;
 }
+
+uint32_t vocab_parts_of_tile(uint32_t d) { return shares_of(0, d > kChunk * kDepth); }
 
 uint32_t vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, int sms) {
   const uint32_t tiles = (a.v + s.wide - 1) / s.wide;

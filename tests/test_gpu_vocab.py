@@ -551,3 +551,14 @@ def test_gradients_of_confident_tokens(handle, t, d, bias):
         want, tol = grad @ w64, rounded @ w64.abs() + 2 * U * (v / 16 + 64) * (grad.abs() @ w64.abs())
         far = ((got.dx.double() - want).abs() / (tol * (1 + UB) + UB * want.abs() + 1e-44)).max()
         assert far <= 1, ("dx", dbias, float(far))
+
+
+@pytest.mark.parametrize("t,d,cuts", [(7000, 16, (1536, 3072, 4608, 6144)), (5000, 520, (3328, 3072))])
+def test_tokens_beside_the_ends_of_blocks(handle, t, d, cuts):
+    """A loss of 600001 entries takes its tokens in blocks, so that its parts fit 256 MB: four parts of eight bytes to 128 entries up to 512
+    columns, two beyond.  The tokens before and behind where blocks end."""
+    x, w, target, b, dloss = inputs(t, d, 600001, 3, True, 0.3, sharp=1.0)
+    out = vocab.loss(handle, x, w, target, bias=b)
+    for at in cuts:
+        rows = slice(at - 40, at + 40)
+        Definition(x[rows], w, target[rows], b, dloss[rows]).check(vocab.LossOut(out.loss[rows], out.lse[rows]), None, BF, str(at))

@@ -1,8 +1,9 @@
-"""Builds libstq.so (the C-ABI library) in-tree with nvcc for sm_100a, and _lists.so (a Python module over torch's headers)."""
+"""Builds libstq.so (the C-ABI library) in-tree with nvcc for sm_100a, and _lists_torch_* (a Python module over torch's headers, for the torch
+and the Python that are there)."""
 from __future__ import annotations
 
-import importlib.util
 import os
+import re
 import subprocess
 import sys
 import sysconfig
@@ -10,7 +11,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstq.so")
-LISTS, LISTS_SOURCE = os.path.join(HERE, "_lists.so"), os.path.join(CSRC, "stq_lists.cpp")
+LISTS_SOURCE = os.path.join(CSRC, "stq_lists.cpp")
 SOURCES = ["stq_step_fast.cu", "stq_step_variants.cu", "stq_step_split.cu", "stq_kernels.cu", "stq_static_stats.cu",
            "stq_q8_rows.cu", "stq_q8_linear.cu", "stq_q8_grad.cu", "stq_q8_tma.cpp", "stq_q8_api.cu",
            "stq_vocab_scores.cu", "stq_vocab_grad.cu", "stq_vocab_api.cu", "stq_clip.cu",
@@ -47,20 +48,32 @@ def stale() -> bool:
     return older(LIB, [os.path.join(CSRC, s) for s in SOURCES] + HEADERS)
 
 
-def build_lists(force: bool = False) -> str:
-    if not force and not older(LISTS, [LISTS_SOURCE, HEADERS[-1]]):
-        return LISTS
-    torch_dir = os.path.dirname(importlib.util.find_spec("torch").origin)
-    inc, tmp = os.path.join(torch_dir, "include"), LISTS + f".tmp{os.getpid()}"
+def lists_name(torch_version: str) -> str:
+    """The module's name: it reads torch's objects in place, so each version has its own."""
+    return "_lists_torch_" + re.sub(r"\W", "_", torch_version)
+
+
+def build_lists(force: bool = False) -> str | None:
+    try:
+        import torch
+    except ImportError:
+        print("torch is not there: the module for lists of tensors is not built (clip.py needs it, libstq does not)", file=sys.stderr)
+        return None
+    name = lists_name(torch.__version__)
+    target = os.path.join(HERE, name + sysconfig.get_config_var("EXT_SUFFIX"))
+    if not force and not older(target, [LISTS_SOURCE, HEADERS[-1]]):
+        return target
+    torch_dir, tmp = os.path.dirname(torch.__file__), target + f".tmp{os.getpid()}"
+    inc = os.path.join(torch_dir, "include")
     subprocess.check_call([
-        "g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-I{inc}", f"-I{inc}/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
+        "g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-DSTQ_LISTS={name}", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+        f"-I{inc}", f"-I{inc}/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}",
         "-o", tmp, LISTS_SOURCE, f"-L{torch_dir}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
-    os.replace(tmp, LISTS)
-    return LISTS
+    os.replace(tmp, target)
+    return target
 
 
-def build(force: bool = False, verbose: bool = False) -> str:
-    build_lists(force)
+def build_lib(force: bool = False, verbose: bool = False) -> str:
     if not force and not stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"
@@ -69,6 +82,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
     return LIB
+
+
+def build(force: bool = False, verbose: bool = False) -> str:
+    lib = build_lib(force, verbose)
+    build_lists(force)
+    return lib
 
 
 if __name__ == "__main__":

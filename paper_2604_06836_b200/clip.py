@@ -10,13 +10,14 @@ generator of them will do.
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import math
-import os
 from typing import NamedTuple, Optional, Sequence
 
 import torch
 
 from . import stq
+from .build import lists_name
 from .q8 import _F32, _empty, _On, _raw_stream
 
 _fn = _lists = None
@@ -26,9 +27,11 @@ def _lib() -> C.CDLL:
     global _fn, _lists
     if _fn is None:
         L = stq.lib()
-        if not os.path.exists(os.path.join(os.path.dirname(stq.LIB_PATH), "_lists.so")):
-            raise RuntimeError("_lists.so is missing: build it with `python -m paper_2604_06836_b200.build`")
-        from . import _lists
+        name = lists_name(torch.__version__)
+        try:
+            _lists = importlib.import_module("." + name, __package__)
+        except ModuleNotFoundError:
+            raise RuntimeError(f"{name} is missing (built for another torch or Python?): build it with `python -m paper_2604_06836_b200.build`") from None
         vp, i, f = C.c_void_p, C.c_int, C.c_float
         for fn in (L.stq_grad_norm, L.stq_grad_clip):
             fn.argtypes = [vp, C.c_char_p, i, vp, f, f, vp, vp, vp, vp]

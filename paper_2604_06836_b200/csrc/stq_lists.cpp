@@ -1,5 +1,6 @@
 // What a call over a list of tensors has to know of each, gathered in one pass of C++ over the list (through the interpreter every
-// question costs 0.1 us a tensor, and a model has hundreds).  A Python module, _lists; libstq itself does not know torch.
+// question costs 0.1 us a tensor, and a model has hundreds).  A Python module, STQ_LISTS, named after the torch that it was built for;
+// libstq itself does not know torch.
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -110,8 +111,10 @@ PyObject* written(PyObject*, PyObject* list) {
 }
 
 PyMethodDef methods[] = {{"rows", rows, METH_VARARGS, nullptr}, {"written", written, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "lists", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__lists() { return PyModule_Create(&module); }
+#define STQ_INIT_OF(name) PyInit_##name
+#define STQ_INIT(name) STQ_INIT_OF(name)
+PyMODINIT_FUNC STQ_INIT(STQ_LISTS)() { return PyModule_Create(&module); }

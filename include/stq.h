@@ -375,7 +375,7 @@ int stq_vocab_loss_backward(stq_handle* h, const float* dloss, const void* x, ui
  * inv_scale: DEVICE pointer to one float, 1 / loss scale, or NULL (1).  norm and factor: DEVICE pointers to one float each,
  * written on `stream`; the calls do not synchronise.  factor is what stq_hparams.inv_grad_scale takes: the step then applies
  * it, and the gradients are not written.  max_norm > 0; infinity: no clipping, factor = inv.  found_inf (optional, DEVICE):
- * set to 1 if the norm is infinite or NaN, else left as it is.  An infinite norm makes the factor 0, a NaN makes it NaN.
+ * set to 1 if the norm is infinite or NaN, else left as it is; the three lie in places of their own (STQ_E_ALIAS).  An infinite norm makes the factor 0, a NaN makes it NaN.
  * Squares are summed in fp32 over up to 64 numbers and in double beyond, in double throughout where fp32's range does not
  * suffice; always in the same order.  Addresses and lengths travel as launch parameters: the gradients may lie elsewhere in every
  * call, and a captured graph keeps those it was captured with.  Workspace, streams and graphs: as for the 8-bit operators. */

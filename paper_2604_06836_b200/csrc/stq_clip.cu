@@ -312,7 +312,8 @@ List<N, OUT> list_of(const stq_grad* g, int n, int& at, uint32_t pieces) {
   return l;
 }
 
-int check_list(const stq_grad* g, int n, bool write, bool* in_place) try {
+// scalars: what the call writes next to the results, 4 bytes each (or null)
+int check_list(const stq_grad* g, int n, bool write, const float* const (&scalars)[3], bool* in_place) try {
   if (n < 0) return STQ_E_ARG;
   if (n > 0 && !g) return STQ_E_NULL;
   *in_place = true;
@@ -346,6 +347,17 @@ int check_list(const stq_grad* g, int n, bool write, bool* in_place) try {
     if (r.second <= written.front().first || r.first >= written.back().second) continue;
     const auto w = std::lower_bound(written.begin(), written.end(), std::make_pair(r.second, (uintptr_t)0));
     if (w != written.begin() && (w - 1)->second > r.first) return STQ_E_ALIAS;
+  }
+  // nor may a scalar lie where a result or another scalar does, or in a gradient that is read again after it has been written
+  for (int i = 0; i < 3; ++i) {
+    const uintptr_t s = reinterpret_cast<uintptr_t>(scalars[i]);
+    if (!s) continue;
+    for (int j = 0; j < i; ++j)
+      if (scalars[j] == scalars[i]) return STQ_E_ALIAS;
+    const auto w = std::lower_bound(written.begin(), written.end(), std::make_pair(s + 4, (uintptr_t)0));
+    if (w != written.begin() && (w - 1)->second > s) return STQ_E_ALIAS;
+    for (const auto& r : read)
+      if (r.first < s + 4 && s < r.second) return STQ_E_ALIAS;
   }
   return STQ_OK;
 } catch (const std::bad_alloc&) {
@@ -433,7 +445,7 @@ int stq_grad_norm(stq_handle* h, const stq_grad* grads, int n, const float* inv_
                   float* found_inf, void* stream) {
   STQ_TRY(check_handle(h));
   bool in_place;
-  STQ_TRY(check_list(grads, n, false, &in_place));
+  STQ_TRY(check_list(grads, n, false, {norm, factor, found_inf}, &in_place));
   STQ_TRY(check_scalars(inv_scale, max_norm, eps, norm, factor, found_inf));
   STQ_CUDA(h, cudaSetDevice(h->device));
   return norm_of(h, grads, n, inv_scale, max_norm, eps, norm, factor, found_inf, static_cast<cudaStream_t>(stream));
@@ -443,7 +455,7 @@ int stq_grad_clip(stq_handle* h, const stq_grad* grads, int n, const float* inv_
                   float* found_inf, void* stream) {
   STQ_TRY(check_handle(h));
   bool in_place;
-  STQ_TRY(check_list(grads, n, true, &in_place));
+  STQ_TRY(check_list(grads, n, true, {norm, factor, found_inf}, &in_place));
   STQ_TRY(check_scalars(inv_scale, max_norm, eps, norm, factor, found_inf));
   STQ_CUDA(h, cudaSetDevice(h->device));
   cudaStream_t s = static_cast<cudaStream_t>(stream);

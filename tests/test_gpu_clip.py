@@ -324,3 +324,26 @@ def test_a_step_that_is_left_out_does_not_hold_up_the_next(bad, scaled):
     opt.found_inf.fill_(1.0)      # what the caller found
     opt.step()
     assert opt.t == taken and float(opt.found_inf) == 1.0
+
+
+def test_scalars_lie_in_places_of_their_own(handle):
+    """A factor or a flag inside of what is scaled would be written while it is read: refused, and nothing is changed."""
+    g, out = torch.full((64,), 3.0, device="cuda"), torch.zeros(64, device="cuda")
+    one, two = out.new_zeros(1), out.new_zeros(1)
+    L, p = clip._lib(), lambda t: t.data_ptr()      # noqa: E731
+    def call(fn, to, norm, factor, flag):      # noqa: E306
+        rows, n = clip._lists.rows([g], None if to is None else [to], 0)
+        return fn(handle._h, rows, n, None, 1.0, 1e-6, p(norm), p(factor), None if flag is None else p(flag), None)
+    for to in (None, out):      # in place, and elsewhere
+        for inside in [g[5:6], g[63:]] + ([] if to is None else [out[:1], out[63:]]):
+            for scalars in ((inside, one, None), (one, inside, None), (one, two, inside)):
+                assert call(L.stq_grad_clip, to, *scalars) == -5
+    for scalars in ((one, one, None), (one, two, one), (one, two, two)):
+        assert call(L.stq_grad_clip, out, *scalars) == -5 and call(L.stq_grad_norm, None, *scalars) == -5
+    torch.cuda.synchronize()
+    assert (g == 3.0).all() and (out == 0.0).all() and float(one) == float(two) == 0.0
+    assert call(L.stq_grad_clip, out[:64], one, two, None) == 0      # (side by side is fine)
+    assert call(L.stq_grad_norm, None, g[5:6], g[6:7], None) == 0      # (a norm reads its gradients once, before it writes)
+    with pytest.raises(stq.StqError) as e:
+        clip.clip_grads(handle, [g], 1.0, found_inf=g[2:3])
+    assert e.value.code == -5

@@ -529,16 +529,17 @@ cudaError_t launch(const VocabRows& r, const void* p, uint32_t panels, const voi
 
 DbiasArgs dbias_args(const VocabDbias& a, const VocabRows& r) { return {a.part, a.ldb, r.count, r.rows, r.scale, a.cols, a.out}; }
 
-// Tiles of dx: a CTA's for few tokens, and two blocks of rows where there are enough of them for every pair.
+// Tiles of dx: a CTA's for few tokens, a pair's else, with one block of rows or two (dx_blocks).
 struct DxShape {
   int cg, mt;
   uint32_t bn;
   uint32_t tile_m() const { return 128u * cg * mt; }
   uint32_t widest() const { return 128u * cg; }
 };
-DxShape dx_shape(uint32_t most, uint32_t d) {
+DxShape dx_shape(uint32_t most, uint32_t d, int sms) {
   const int cg = most > 128 ? 2 : 1;
-  return {cg, most >= 8192 ? 2 : 1, tile_columns(d, 128 * cg, 16)};
+  const uint32_t bn = tile_columns(d, 128 * cg, 16);
+  return {cg, cg == 2 ? dx_blocks(most, 256, (d + bn - 1) / bn, sms / 2) : 1, bn};
 }
 
 }  // namespace
@@ -586,13 +587,13 @@ cudaError_t launch_vocab_dw_join(const VocabDw& a, const float* part, int sms, c
 }
 
 void vocab_dx_space(uint32_t most, uint32_t d, size_t ldd, int sms, size_t* plane, size_t* segments) {
-  const DxShape s = dx_shape(most, d);
+  const DxShape s = dx_shape(most, d, sms);
   *plane = (size_t)up(most, s.tile_m()) * ldd;
   *segments = (size_t)Ranges::segments(sms / s.cg) * s.tile_m() * s.widest();
 }
 
 cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t stream) {
-  const DxShape s = dx_shape(a.r.most, a.d);
+  const DxShape s = dx_shape(a.r.most, a.d, sms);
   GradArgs g = {};
   g.n = a.d;
   g.bn = s.bn;
@@ -608,7 +609,7 @@ cudaError_t launch_vocab_dx(const VocabDx& a, int sms, int* err, cudaStream_t st
 }
 
 cudaError_t launch_vocab_dx_finish(const VocabDx& a, uint32_t t, void* dx, size_t lddx, const VocabDbias* db, int sms, cudaStream_t stream) {
-  const DxShape s = dx_shape(a.r.most, a.d);
+  const DxShape s = dx_shape(a.r.most, a.d, sms);
   // (few tokens: as many CTAs as there are SMs, to have enough loads on the way)
   uint32_t each = t / (4 * sms) < 1 ? 1 : t / (4 * sms);
   if (each > 4) each = 4;

@@ -66,4 +66,14 @@ struct Ranges {
   STQ_BOTH static uint32_t segments(uint32_t units) { return 3 * units; }
 };
 
+// Blocks of rows to a tile of dx.  Two share each stage of w, three quarters of the bytes of a product, but both accumulators are then one
+// tile's, and its results leave while nothing is multiplied.  Two where there is such a tile for every unit at least; with fewer, more and
+// smaller tiles leave less to be cut.  dz and dx over 50257 entries, two blocks against one: 8192 x 1600 (112 tiles for 74 pairs) 2059 and
+// 2406 us, 4096 x 4096 (128) 2561 and 2543, 6000 x 2560 (120) 2501 and 2436; 8192 x 1024 (64) 1487 and 1437, 4096 x 2048 (64) 1370 and 1367,
+// 8192 x 64 (16) 381 and 389.  (Not all of it goes by that: 4096 x 1600, 56 tiles, 1156 and 1255.)  `rows` are those that may count: how
+// many do is known on the device alone.
+inline int dx_blocks(uint32_t rows, uint32_t block, uint32_t tiles_n, uint32_t units) {
+  return (uint64_t)((rows + 2 * block - 1) / (2 * block)) * tiles_n >= units ? 2 : 1;
+}
+
 }  // namespace stq

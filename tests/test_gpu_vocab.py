@@ -562,3 +562,13 @@ def test_tokens_beside_the_ends_of_blocks(handle, t, d, cuts):
     for at in cuts:
         rows = slice(at - 40, at + 40)
         Definition(x[rows], w, target[rows], b, dloss[rows]).check(vocab.LossOut(out.loss[rows], out.lse[rows]), None, BF, str(at))
+
+
+@pytest.mark.parametrize("t,d,masked", [(200, 19000, 0.0), (1500, 6500, 0.2), (2500, 4000, 0.9)])
+def test_many_columns(handle, t, d, masked):
+    """Tiles of two blocks of rows for few tokens, and fewer rows than the plan counted on."""
+    x, w, target, b, dloss = inputs(t, d, 500, t, True, masked)
+    check = Definition(x, w, target, b, dloss)
+    for dtype in (BF, F32):
+        out, grads = run(handle, x, w, target, b, dloss, dtype)
+        check.check(out, grads, dtype, f"{t} {d} {masked}")

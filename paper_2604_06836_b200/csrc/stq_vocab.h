@@ -72,7 +72,7 @@ uint32_t vocab_parts_of_tile(uint32_t d);
 cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape s, uint32_t most, float2* part, float* chosen, int sms, int* err,
                                cudaStream_t stream);
 // loss and lse of all tokens from these.
-cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse,
+cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse, int sms,
                                 cudaStream_t stream);
 
 // Gradients of the logits of entries [v0, v1), divided by scale: `planes` bf16 numbers (1 or 3) whose sum they are.  They lie in panels

@@ -166,7 +166,7 @@ int stq_vocab_loss(stq_handle* h, const void* x, uint64_t ldx, const void* w, ui
     int launches = 2;
     STQ_CUDA(h, prepare_rows(b, r, xb, ldx, nullptr, t0 == 0, s, &launches));
     STQ_CUDA(h, launch_vocab_parts(b, shape, most, part, chosen, h->sm_count, h->d_err, s));
-    STQ_CUDA(h, launch_vocab_finish(b, part, parts, chosen, loss + t0, lse + t0, s));
+    STQ_CUDA(h, launch_vocab_finish(b, part, parts, chosen, loss + t0, lse + t0, h->sm_count, s));
     h->launches += launches;
   }
   return STQ_OK;

@@ -666,13 +666,17 @@ cudaError_t launch_vocab_parts(const VocabArgs& a, VocabShape sh, uint32_t most,
   return by_length<0>(a, sh, s, nullptr, sms, stream);
 }
 
-cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse,
+cudaError_t launch_vocab_finish(const VocabArgs& a, const float2* part, uint32_t parts, const float* chosen, float* loss, float* lse, int sms,
                                 cudaStream_t stream) {
-  // Few tokens: more threads to each.  (8192 tokens: 32 to a CTA 16 us, 8 to a CTA 22; 4096 of which 614 count: 13 and 7.)
+  // As many threads to a token as leave all CTAs resident at once, five to an SM.  The number of parts hardly matters to that.  (Whole losses
+  // from a graph, 4, 8 and 32 tokens to a CTA: 2048 tokens, 64 columns, 30000 entries (470 parts) 33.0, 33.7 and 41.2 us, 576 columns, 8000
+  // entries (63) 25.5, 25.2 and 25.9; 5000 tokens 74, 69 and 76, and 52.0, 47.4 and 48.0; 8192 tokens 120, 118 and 122, and 78, 74 and 73;
+  // 16384 tokens 227, 222 and 221, and 146, 139 and 134.)
   auto go = [&](auto* kernel, uint32_t r) {
     return launch_with(kernel, dim3((a.t + r - 1) / r), dim3(256), 0, 1, true, stream, a, part, parts, chosen, loss, lse);
   };
-  return a.t <= 2048 ? go(finish_kernel<4>, 4) : a.t <= 4096 ? go(finish_kernel<8>, 8) : go(finish_kernel<32>, 32);
+  const uint32_t resident = 5 * sms;
+  return a.t <= 4 * resident ? go(finish_kernel<4>, 4) : a.t <= 8 * resident ? go(finish_kernel<8>, 8) : go(finish_kernel<32>, 32);
 }
 
 cudaError_t launch_vocab_dlogits(const VocabArgs& a, VocabShape sh, uint32_t v0, uint32_t v1, const VocabGradOut& o, int sms, int* err,

@@ -623,7 +623,8 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
   // A stage is 4096 multiply-adds a cycle and SM or, where that is longer, its copies at 62 bytes a cycle, and 400 cycles at least (the
   // ring holds six, and what is in flight must cover the memory's latency: 1 token, 1600 x 50257, 38 us in tiles of 64, 30 in tiles of
   // 128); a tile takes as long as its stages or, beside the next one's, as its results.  Of the widths, the one whose tiles fill their
-  // last round best.
+  // last round best.  (`rows` are those that may count.  How many do is known on the device alone: a plan for tokens of which few count is
+  // that of all.)
   for (int cg = rows > 128 ? 2 : 1; cg > 0; --cg)
     for (uint32_t wide = planes == 3 ? 128 : 128 * cg; wide >= (planes == 3 ? 128u : 64u * cg); wide -= step) {
       const uint64_t tiles = (uint64_t)((rows + 128 * cg - 1) / (128 * cg)) * ((v + wide - 1) / wide), units = sms / cg;
@@ -631,7 +632,11 @@ VocabShape vocab_shape(uint32_t rows, uint32_t v, uint32_t d, int planes, int sm
       double stage = 2.0 * wide > 400.0 ? 2.0 * wide : 400.0;
       if (copied / 62.0 > stage) stage = copied / 62.0;
       const double results = 500.0 + (cg == 2 ? 14.0 : 16.0) * (planes == 3 ? 2.0 : 1.0) * wide;
-      const double c = (double)((tiles + units - 1) / units) * (k * stage > results ? k * stage : results) + results;
+      // (of gradients in three parts the results take so long that a tile is the sum of both: 1024 and 4096 tokens, 256 to 2560 columns, 490
+      // cycles a stage of a pair and 4000 a tile; 300 tokens, 540 of a CTA and 5000)
+      if (planes == 3 && cg == 2) stage = 490.0;
+      const double tile = planes == 3 ? k * stage + results : k * stage > results ? k * stage : results;
+      const double c = (double)((tiles + units - 1) / units) * tile + results;
       if (c < 0.99 * least) {
         least = c;
         best = {cg, wide, 0};

@@ -572,3 +572,53 @@ def test_many_columns(handle, t, d, masked):
     for dtype in (BF, F32):
         out, grads = run(handle, x, w, target, b, dloss, dtype)
         check.check(out, grads, dtype, f"{t} {d} {masked}")
+
+
+@pytest.mark.parametrize("t", [1, 100, 129, 700])
+def test_sums_leave_the_matrix_unit_in_parts(handle, t):
+    """Sums of positive products, where all that is cut off is cut off to the same side: after each product of 16 terms up to one step, 2 U,
+    of the sum so far, which begins anew after 512 terms (up to 128 tokens: 256), and a rounding for each part that is added.  (Whole
+    sums lose 143 U of a logit: about 1.1 U of the sum so far, 256 times.)"""
+    d, v, part = 4096, 300, 256 if t <= 128 else 512
+    g = torch.Generator(device="cuda").manual_seed(t)
+    x = (0.5 + torch.rand(t, d, device="cuda", generator=g)).to(BF)
+    w = ((0.5 + torch.rand(v, d, device="cuda", generator=g)) * (20 / d)).to(BF)
+    target = torch.randint(0, v, (t,), device="cuda", generator=g)
+    out = vocab.loss(handle, x, w, target)
+    z = x.double() @ w.double().T
+    dz, total = torch.zeros_like(z), torch.zeros_like(z)
+    for k in range(0, d, part):
+        inner = torch.zeros_like(z)
+        for i in range(k, k + part, 16):
+            inner += x[:, i:i + 16].double() @ w[:, i:i + 16].double().T
+            dz += 2 * U * inner
+        total += inner
+        dz += U * total
+    lse = torch.logsumexp(z, 1)
+    apart = (z - lse[:, None]).abs().amax(1)
+    tol = dz.amax(1) + U * (2 * lse + 8 * apart + 2 * v / 128 + 64)
+    far = (out.lse.double() - lse).abs()
+    assert (tol < 45 * U * lse).all() and (far <= tol).all(), (float((far / tol).max()), float((far / U / lse).max()))
+
+
+@pytest.mark.parametrize("t,d,v", [(5, 200, 333), (300, 200, 333), (300, 77, 1000), (700, 1025, 600)])
+@pytest.mark.parametrize("extra,shift", [(8, 0), (0, 8), (3, 0), (1, 1), (0, 1)])
+def test_results_of_any_pitch(handle, t, d, v, extra, shift):
+    """dx and dw to rows with gaps, at any element: what lies between the rows and around them stays as it was."""
+    x, w, target, b, dloss = inputs(t, d, v, 8, True, 0.2)
+    lse = vocab.loss(handle, x, w, target, bias=b).lse
+    for dtype, code in ((BF, stq.GRAD_BF16), (F32, stq.GRAD_F32)):
+        want = vocab.loss_backward(handle, dloss, x, w, target, lse, bias=b, dtype=dtype)
+        bufs = [torch.full((r * (d + extra) + shift + 64,), 7.0, device="cuda", dtype=k) for r, k in ((t, BF), (v, dtype))]
+        dx, dw = (a[shift:shift + r * (d + extra)].view(r, d + extra) for a, r in zip(bufs, (t, v)))
+        db = torch.empty(v, device="cuda")
+        p = lambda t: t.data_ptr()      # noqa: E731
+        rc = vocab._lib().stq_vocab_loss_backward(handle._h, p(dloss), p(x), d, p(w), d, p(b), p(target), IGNORE, p(lse), t, v, d, p(dx), d + extra,
+                                                  p(dw), d + extra, code, p(db), torch.cuda.current_stream().cuda_stream)
+        assert rc == 0 and torch.equal(db, want.dbias)
+        for got, full, buf in ((dx, want.dx, bufs[0]), (dw, want.dw, bufs[1])):
+            if got is dx or dtype == F32:
+                assert torch.equal(got[:, :d], full)
+            else:      # (rows off 16 bytes take tiles of one block, whose sums may be shared in another way: one step of bf16, or of the sum)
+                assert ((got[:, :d].double() - full.double()).abs() <= 2 * UB * full.double().abs() + 2 * U * t * float(dloss.abs().max()) * 8).all()
+            assert (got[:, d:] == 7.0).all() and (buf[:shift] == 7.0).all() and (buf[shift + got.numel():] == 7.0).all()

@@ -351,10 +351,12 @@ int stq_q8_bias_grad(stq_handle* h, const void* dy, uint64_t lddy, int dtype, ui
  * ignore_index have loss 0, lse 0 and no gradient, and take no part in the products.  Any other target outside
  * 0..v-1 gives loss and lse NaN, and NaN gradients.  A bias of -inf takes an entry out of the vocabulary.
  * All sums are held in fp32 and added in a fixed order; those of the logits and of an fp32 dw leave the matrix units,
- * which cut them off, every 512 (up to 128 tokens: 256) and 128 terms.  Workspace, streams and graphs: as for the 8-bit operators above (for
- * the gradients up to 512 MB of gradients of logits, a copy of x in fp32 and one in bf16, and up to 116 MB of partial
- * results; a copy of w where its rows are not aligned to 16 bytes).  t is at most STQ_VOCAB_MAX_TOKENS, d at most
- * STQ_VOCAB_MAX_WIDTH, v at most 2^24 (STQ_E_TOO_LARGE). */
+ * which cut them off, every 512 (up to 128 tokens: 256) and 128 terms.  Workspace, streams and graphs: as for
+ * the 8-bit operators above.  It takes, and a quarter more where it grows: for the loss up to 256 MB of parts (256 tokens at least, 4 MB each
+ * at 2^24 entries) and a bf16 copy of up to 32768 rows of x; for the gradients up to 512 MB of gradients of logits (256 entries at least), 128 MB
+ * of partial results of dw, 116 MB of dx, 64 MB of sums for dbias, and copies of x in fp32 and bf16; for both a copy of w where its rows are
+ * not aligned to 16 bytes.  t is at most STQ_VOCAB_MAX_TOKENS, d at most STQ_VOCAB_MAX_WIDTH, v at most 2^24 (STQ_E_TOO_LARGE).
+ * The time of finding the tokens that count grows with t^2 (2.5 ms at the largest t). */
 #define STQ_VOCAB_MAX_TOKENS 262144
 #define STQ_VOCAB_MAX_WIDTH 65536
 

@@ -6,6 +6,9 @@ then clips without writing the gradients; ``clip_grads`` is for every other opti
 
 Gradients are float32, bfloat16 or float16, each its own, in any dense layout (no gaps, no overlap); None is passed over.  A
 generator of them will do.
+
+Where each rank of a job has a part of the parameters (``multi.partition``), this is the norm of one rank's part: the squares of the norms
+have to be added over the ranks before a factor is taken from them.
 """
 from __future__ import annotations
 

@@ -84,7 +84,7 @@ cudaError_t prepare_rows(VocabArgs& a, Rows& r, const void* x, size_t ldx, const
 
 // Entries of the vocabulary to a piece (the last piece has what is left): as many tiles as fit, or somewhat fewer where the tiles of the
 // products then fill their last round better, by half a percent at least: each piece is another beginning and end of dx too, which the
-// cost leaves out (8192 x 768 x 50257, fp32 dw: five pieces 3072 us, six, that cost 0.2 % less by the sums below, 3136).
+// cost leaves out (8192 x 768 x 50257, fp32 dw: five pieces 3068 us, six, that cost 0.2 % less by the sums below, 3109).
 uint32_t piece_of(const VocabArgs& a, VocabDw g, int planes, bool dw, int sms) {
   const uint32_t tiles = (uint32_t)(up(a.v, 256) / 256);
   const size_t fit = kPieceBytes / ((size_t)g.r.most * 2 * planes) / 256;

@@ -8,9 +8,11 @@
 // exactly the fp32 gradient, and the sum leaves the matrix unit, which cuts its sums off instead of rounding them, every 128
 // terms and is added, rounded, to a running sum in registers.
 //
-// dx: its sum is over the vocabulary, so every piece adds to it, in fp32 in memory (copies that add: nothing is read back).
-// The tiles are few (8192 x 1600: 224 for 74 pairs of CTAs), so the sums of all tiles, one after the other, are cut into
-// equal ranges.  What different pairs have of a tile goes to different planes, which are added in a fixed order at the end.
+// dx: its sum is over the vocabulary, so every piece adds to it, in fp32 in memory (copies that add: nothing is read back).  It is
+// bf16 at the end, so p enters as one bf16 number here, the first part where there are three.  The tiles are few (8192 x 1600:
+// 112 of two blocks of rows for 74 pairs of CTAs): whole rounds of them run in step, the rest is cut into parts that run in step, and what
+// is left then into ranges (stq_vocab_ranges.h).  A whole tile's sum goes to one plane, parts and ranges each to a segment of their own;
+// a tile's segments are added in a fixed order at the end.
 #include <cuda_bf16.h>
 
 #include "../../include/stq.h"
@@ -466,7 +468,8 @@ struct DwPlan {
   double cost;
 };
 // Time of a plan in clock cycles, as for the 8-bit products: a stage is 4096 multiply-adds a cycle and SM, a tile has a beginning
-// and an end, partial results go through memory once more.
+// and an end, partial results go through memory once more.  It goes by the tokens that may count, since how many do is known on the device
+// alone (4096 tokens, 85 % masked: 64 stages in the plan, 10 in the run).
 DwPlan dw_plan(const VocabDw& a, int sms) {
   const uint32_t ksteps = (a.r.most + kDepth - 1) / kDepth;
   // CTAs, widest tile, blocks of rows; time of the copies of a stage

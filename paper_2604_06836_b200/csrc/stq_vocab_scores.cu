@@ -33,7 +33,8 @@ __device__ __forceinline__ float ex2(float x) {
 constexpr int kGatherRows = 16;        // tokens to a CTA
 constexpr int kScan = 8;               // targets that a thread has on the way
 
-// Every CTA counts the targets before its tokens and in all, so that nothing has to be passed between CTAs.
+// Every CTA counts the targets before its tokens and in all, so that nothing has to be passed between CTAs.  That reads t^2 / 2 bytes of
+// targets from the cache: 33 MB for 8192 tokens, but 0.5 GB for 32768 (48 us) and 34 GB for 262144 (2.5 ms).
 __global__ void __launch_bounds__(256) gather_kernel(const GatherArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");

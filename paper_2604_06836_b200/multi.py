@@ -9,6 +9,8 @@ data-path collective either, because quantization blocks are independent: ``part
 parameter list into per-rank element ranges on block boundaries, each rank steps its ranges as rows
 of its own table, and on decision steps the per-layer sums are added over ranks
 (``sync_layer_stats``, Sec. 3.1's distributed engine) so that every rank takes the same decision.
+Clipping to a norm over all parameters needs one more number: the squares of the ranks' norms are added
+(``sum_over_ranks``) before the factor is taken; ``clip`` and ``STQAdamW(max_norm=...)`` know one rank's part.
 """
 from __future__ import annotations
 

@@ -46,7 +46,8 @@ class STQAdamW(torch.optim.Optimizer):
     gradients; the step applies the factor as it reads them, so they are not written.  Statistics of a decision
     step are those of the clipped gradients, in both orders.  ``self.last_norm`` is the norm before clipping, on
     the device.  With ``found_inf`` set, a step whose norm is not finite is left out too (the flag is the caller's: the
-    optimizer reads it and leaves it as it is).
+    optimizer reads it and leaves it as it is).  Where each rank steps its own part of the parameters this clips by the
+    norm of that part: without max_norm, ``grad_scaler_inv`` takes a factor from the norm over all ranks.
     """
 
     def __init__(self, params: Iterable, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,

@@ -553,7 +553,7 @@ def test_gradients_of_confident_tokens(handle, t, d, bias):
         assert far <= 1, ("dx", dbias, float(far))
 
 
-@pytest.mark.parametrize("t,d,cuts", [(7000, 16, (1536, 3072, 4608, 6144)), (5000, 520, (3328, 3072))])
+@pytest.mark.parametrize("t,d,cuts", [(7000, 16, (1536, 4608, 6144)), (5000, 520, (3328,))])
 def test_tokens_beside_the_ends_of_blocks(handle, t, d, cuts):
     """A loss of 600001 entries takes its tokens in blocks, so that its parts fit 256 MB: four parts of eight bytes to 128 entries up to 512
     columns, two beyond.  The tokens before and behind where blocks end."""
